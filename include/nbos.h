@@ -404,6 +404,119 @@ int nbos_cluster_sums(const int32_t *gpus_total, const int32_t *gpus_subscribed,
 int nbos_scale_out_deficit(const int32_t *found, int32_t n_snapshots, int64_t batch_per_snapshot,
                            int64_t *out_deficit, void *cuda_stream);
 
+/*
+ * ---- Learned placement policies ------------------------------------------------------------------------
+ * Section 3.2.1 calls the rule that ranks candidate servers a policy that can be replaced. A policy that is
+ * learned scores every host for every request: a table of logits [rows, n_hosts], -inf where the host cannot
+ * take the request. The entry points below train one on the exact rule's decisions (nbos_policy_distill),
+ * keep it from sending everything to few hosts (nbos_policy_balance) and let it answer (nbos_policy_sample).
+ * Read hosts as vocabulary entries or experts and rows as tokens and they are the same operators of a
+ * language model.
+ *
+ *   data        DEVICE, aligned to its element type. Rows that start on 16-byte boundaries (data and row_stride)
+ *               are moved 16 bytes at a time, others element by element.
+ *   row_stride  elements from one row to the next, >= n_hosts (any value when rows <= 1)
+ * All arithmetic is in 32 bits (sums over columns and groups in 64), with one rounding to the logits' type at
+ * the end. Results do not depend on the launch: no floating-point atomics. Every call is asynchronous on
+ * `cuda_stream`; temporaries come from the library's stream-ordered pool. rows == 0 is a no-op (outputs per group
+ * are still written). Errors of all of them: INVALID_ARG, NO_MEMORY, CUDA, UNSUPPORTED_DEVICE.
+ */
+#define NBOS_F32 0
+#define NBOS_BF16 1
+#define NBOS_F16 2
+#define NBOS_POLICY_MAX_ROWS 2147483647
+#define NBOS_POLICY_MAX_K 256    /* hosts per row of a teacher / of a choice  */
+#define NBOS_POLICY_MAX_DRAWS 8  /* hosts drawn per row by nbos_policy_sample */
+
+typedef struct nbos_logits {
+    const void *data;   /* DEVICE [rows][row_stride]              */
+    int64_t rows;       /* 0 .. NBOS_POLICY_MAX_ROWS              */
+    int64_t row_stride; /* elements                               */
+    int32_t n_hosts;    /* 1 .. NBOS_MAX_HOSTS                    */
+    int32_t dtype;      /* NBOS_F32 | NBOS_BF16 | NBOS_F16        */
+} nbos_logits;
+
+/*
+ * Distillation from a teacher's k best hosts per row, forward and gradient.
+ *   Entry j of row r counts if its host index is in 0..n_hosts-1 (-1 = no entry: what nbos_place_batch writes
+ *   can be passed as it is), the row's logit x of that host is above -inf and its teacher logit t is above -inf.
+ *     q = softmax over the row's counting entries of t / T          p = softmax over all hosts of x / T
+ *     loss = T^2 * sum_j q_j (ln q_j - ln p[host_j])
+ *     grad = T * (p - q scattered to its hosts) * grad_scale * grad_loss[r]
+ *   A host that is listed twice counts with both entries. A row without a counting entry has loss 0 and gradient
+ *   0. A NaN or +inf logit makes its row's loss and gradient NaN; a NaN teacher logit does not count.
+ *   hosts           DEVICE [rows * k] int32
+ *   teacher_logits  DEVICE float, row r at r * teacher_stride (0: the same k for every row); NULL = all equal
+ *   temperature     T, finite and > 0
+ *   grad_loss       DEVICE [rows] float, the gradient that arrives at the loss; NULL = 1
+ *   out_loss        DEVICE [rows] float or NULL
+ *   out_stats       DEVICE [rows * 2] float or NULL: (m, S), the row's largest logit and sum of e^((x - m) / T):
+ *                   what nbos_policy_distill_backward needs. (-inf, 0) for a row of -inf.
+ *   out_grad        DEVICE, the logits' type, rows grad_stride elements apart, or NULL (forward only). May be the
+ *                   logits themselves (same stride); must not overlap them otherwise.
+ * With out_grad the logits are read once for both directions. nbos_policy_distill_backward computes the same
+ * gradient later, from the saved statistics.
+ */
+int nbos_policy_distill(const nbos_logits *logits, const int32_t *hosts, const float *teacher_logits,
+                        int64_t teacher_stride, int32_t k, float temperature, const float *grad_loss,
+                        float grad_scale, float *out_loss, float *out_stats, void *out_grad, int64_t grad_stride,
+                        void *cuda_stream);
+int nbos_policy_distill_backward(const nbos_logits *logits, const int32_t *hosts, const float *teacher_logits,
+                                 int64_t teacher_stride, int32_t k, float temperature, const float *stats,
+                                 const float *grad_loss, float grad_scale, void *out_grad, int64_t grad_stride,
+                                 void *cuda_stream);
+
+/*
+ * Load-balance loss with per-host counts, forward and gradient. The rows are n_groups groups of rows / n_groups
+ * (the snapshots of a what-if sweep, the sequences of a batch); each group has its own loss.
+ *   hosts [rows * k]: the k hosts chosen per row, an index outside 0..n_hosts-1 (-1) = none. A row is live if it
+ *   has at least one.
+ *     count_h = how often host h was chosen in the group     f_h = count_h / sum of counts
+ *     P_h     = mean over the group's live rows of softmax(x)_h
+ *     loss    = n_hosts * sum_h f_h P_h                      (1 when either is uniform)
+ *     grad    = n_hosts / live * p_h (f_h - sum_i f_i p_i) * grad_scale * grad_loss[group]; 0 for other rows
+ *   f is a constant for the gradient (it is a count). A group without a live row has loss, shares and gradient
+ *   0. A live row of -inf adds nothing to P and has gradient 0. NaN and +inf logits make their row's gradient, and
+ *   their group's loss and P, NaN.
+ *   out_loss    DEVICE [n_groups] float
+ *   out_counts  DEVICE [n_groups * n_hosts] int32
+ *   out_shares  DEVICE [n_groups * n_hosts] float (P) or NULL
+ *   out_stats   DEVICE [rows * 2] float or NULL: (m, S) per row as above with T = 1, for the backward call; not
+ *               written for rows that are not live
+ *   out_grad    as above. f depends on the choices alone, so one pass over the logits gives both directions.
+ * rows * k and rows / n_groups * k must fit in 31 bits; rows must be a multiple of n_groups.
+ */
+int nbos_policy_balance(const nbos_logits *logits, int32_t n_groups, const int32_t *hosts, int32_t k,
+                        const float *grad_loss, float grad_scale, float *out_loss, int32_t *out_counts,
+                        float *out_shares, float *out_stats, void *out_grad, int64_t grad_stride,
+                        void *cuda_stream);
+int nbos_policy_balance_backward(const nbos_logits *logits, int32_t n_groups, const int32_t *hosts, int32_t k,
+                                 const float *stats, const float *grad_loss, float grad_scale, void *out_grad,
+                                 int64_t grad_stride, void *cuda_stream);
+
+/*
+ * Sampling distinct hosts from given random numbers. Per row, with m the largest logit:
+ *   weight   w_h = floor(2^31 * 2^((x_h - m) * c)), c = float(log2 e) / T, each step in 32-bit floats, 2^y as
+ *            exp2f. A whole number: sums of weights are exact and do not depend on the order they are taken in.
+ *   filters  in the order (x descending, index ascending) keep a first part of the hosts:
+ *              top-k  the first top_k;  <= 0 = off
+ *              top-p  of those, each host before which less than max(1, floor(A * floor(p * 2^24) / 2^24))
+ *                     of weight stands, A the weight of the top-k hosts;  p >= 1 or NaN = off
+ *              min-p  of those, hosts with w >= floor(min_p * 2^31);  <= 0 or NaN = off
+ *   draw d   t = floor(A' * floor(u_d * 2^24) / 2^24), A' the weight left; the lowest host index at which the running
+ *            sum of weights (in index order) exceeds t; its weight is then taken out. -1 once no weight is left.
+ *   T <= 2^-20 or NaN keeps the best host alone (greedy). A NaN logit counts as -inf, +inf as the largest
+ *   finite float. u is clamped to [0, 1 - 2^-24], NaN counts as 0.
+ *   uniforms     DEVICE [rows * draws] float
+ *   temperature, top_p, min_p  DEVICE [rows] float or NULL (1 / off / off);  top_k  DEVICE [rows] int32 or NULL
+ *   draws        1 .. NBOS_POLICY_MAX_DRAWS (three for the replicas of a kernel, one for a token)
+ *   out_hosts    DEVICE [rows * draws] int32, in the order drawn, -1 padding
+ *   out_found    DEVICE [rows] int32 or NULL: how many were drawn
+ */
+int nbos_policy_sample(const nbos_logits *logits, const float *uniforms, const float *temperature,
+                       const int32_t *top_k, const float *top_p, const float *min_p, int32_t draws,
+                       int32_t *out_hosts, int32_t *out_found, void *cuda_stream);
+
 /* Synchronises `cuda_stream` and returns the sticky device status of this snapshot: NBOS_OK, or
  * NBOS_ERR_DEVICE_TIMEOUT if some kernel gave up on a bounded wait (its outputs are then
  * undefined), NBOS_ERR_RANGE / NBOS_ERR_STALE_LAYOUT after an nbos_snapshot_update whose new state

@@ -35,6 +35,13 @@ NBOS_MAX_HOSTS = 1 << 20
 NBOS_MAX_REPLICAS = 1024
 NBOS_SEQUENTIAL_MAX_HOSTS = 65536
 
+NBOS_F32 = 0
+NBOS_BF16 = 1
+NBOS_F16 = 2
+NBOS_POLICY_MAX_ROWS = 2147483647
+NBOS_POLICY_MAX_K = 256
+NBOS_POLICY_MAX_DRAWS = 8
+
 NBOS_PROBE_MIX_ALU = 0
 NBOS_PROBE_MIX_IMAD = 1
 NBOS_PROBE_MIX_BOTH = 2
@@ -47,6 +54,8 @@ EXPORTED_SYMBOLS = (
     "nbos_place_batch_host", "nbos_place_batch_host_async", "nbos_place_batch_host_wait",
     "nbos_place_batch_noalloc", "nbos_select_executors",
     "nbos_cluster_sums", "nbos_scale_out_deficit", "nbos_place_batch_sequential",
+    "nbos_policy_distill", "nbos_policy_distill_backward", "nbos_policy_balance", "nbos_policy_balance_backward",
+    "nbos_policy_sample",
     "nbos_snapshot_status", "nbos_strerror", "nbos_last_error_detail",
     "nbos_probe_int32_issue", "nbos_probe_wait_timeout", "nbos_probe_wait_timeout_on_snapshot",
 )
@@ -86,6 +95,13 @@ class nbos_cluster_state(ctypes.Structure):
         ("gpus_total", ctypes.c_void_p), ("gpus_subscribed", ctypes.c_void_p),
         ("gpus_committed", ctypes.c_void_p), ("vram_gb", ctypes.c_void_p),
         ("millicpus", ctypes.c_void_p), ("mem_mb", ctypes.c_void_p),
+    ]
+
+
+class nbos_logits(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+        ("n_hosts", ctypes.c_int32), ("dtype", ctypes.c_int32),
     ]
 
 
@@ -136,6 +152,12 @@ def load_library() -> ctypes.CDLL:
     lib.nbos_cluster_sums.argtypes = [vp, vp, vp] + [ctypes.c_int32] * 4 + [vp, vp]
     lib.nbos_scale_out_deficit.argtypes = [vp, ctypes.c_int32, i64, vp, vp]
     lib.nbos_place_batch_sequential.argtypes = [vp, vp, i64, vp, vp, vp, vp]
+    f32, i32 = ctypes.c_float, ctypes.c_int32
+    lib.nbos_policy_distill.argtypes = [P(nbos_logits), vp, vp, i64, i32, f32, vp, f32, vp, vp, vp, i64, vp]
+    lib.nbos_policy_distill_backward.argtypes = [P(nbos_logits), vp, vp, i64, i32, f32, vp, vp, f32, vp, i64, vp]
+    lib.nbos_policy_balance.argtypes = [P(nbos_logits), i32, vp, i32, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    lib.nbos_policy_balance_backward.argtypes = [P(nbos_logits), i32, vp, i32, vp, vp, f32, vp, i64, vp]
+    lib.nbos_policy_sample.argtypes = [P(nbos_logits), vp, vp, vp, vp, vp, i32, vp, vp, vp]
     lib.nbos_snapshot_status.argtypes = [vp, vp]
     lib.nbos_strerror.argtypes = [ctypes.c_int]
     lib.nbos_strerror.restype = ctypes.c_char_p
@@ -456,6 +478,174 @@ def nbos_place_batch_sequential(snap: Snapshot, requests, out_hosts, out_found=N
         raise ValueError("out_subscribed must hold n_snapshots * n_hosts values")
     _check(lib.nbos_place_batch_sequential(snap.handle, _ptr(requests), b, _ptr(out_hosts),
                                            _ptr(out_found), _ptr(out_subscribed), _stream_ptr(stream)))
+
+
+# ---- learned placement policies ------------------------------------------------------------
+_POLICY_DTYPES = {torch.float32: NBOS_F32, torch.bfloat16: NBOS_BF16, torch.float16: NBOS_F16}
+
+
+def _table(t: torch.Tensor, what: str):
+    """(rows, row stride, columns) of a CUDA table [..., n] whose rows lie evenly apart."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _POLICY_DTYPES:
+        raise TypeError(f"{what} must be a float32, bfloat16 or float16 torch tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{what} must live on cuda, not {t.device}")
+    if t.dim() < 2:
+        raise ValueError(f"{what} must have at least two dimensions, [..., n_hosts]")
+    n = t.shape[-1]
+    if n > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what} must be contiguous along its hosts")
+    if 0 in t.shape[:-1]:
+        return 0, n, n
+    rows, stride = 1, n
+    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if rows == 1:
+            stride = step
+        elif step != stride * rows:
+            raise ValueError(f"the rows of {what} must lie evenly apart")
+        rows *= size
+    return rows, stride, n
+
+
+def _logits(t: torch.Tensor, what: str = "logits") -> nbos_logits:
+    rows, stride, n = _table(t, what)
+    return nbos_logits(_ptr(t), rows, stride, n, _POLICY_DTYPES[t.dtype])
+
+
+def _dense(t, what: str, dtype, numel: int, like: torch.Tensor):
+    """A contiguous tensor of `numel` values on the device of `like`, or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise TypeError(f"{what} must be a {str(dtype)[6:]} torch tensor")
+    if t.device != like.device:
+        raise ValueError(f"{what} must live on {like.device}, not {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    if t.numel() != numel:
+        raise ValueError(f"{what} must hold {numel} values, not {t.numel()}")
+    return t
+
+
+def _grad_like(grad, logits):
+    if grad is None:
+        return 0
+    if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device:
+        raise ValueError("out_grad must have the logits' shape, type and device")
+    rows, stride, n = _table(grad, "out_grad")
+    return stride
+
+
+def _choices(hosts, logits, rows: int):
+    """hosts [..., k] int32 beside logits [..., n]; returns k."""
+    if not isinstance(hosts, torch.Tensor) or hosts.dtype != torch.int32:
+        raise TypeError("hosts must be an int32 torch tensor")
+    if hosts.shape[:-1] != logits.shape[:-1]:
+        raise ValueError("hosts [..., k] and logits [..., n_hosts] must agree on their rows")
+    _dense(hosts, "hosts", torch.int32, rows * hosts.shape[-1], logits)
+    return hosts.shape[-1]
+
+
+def _teacher(teacher_logits, hosts, logits, rows: int, k: int):
+    """[..., k] like hosts, [k] for all rows alike, or None; returns the row stride."""
+    if teacher_logits is None:
+        return 0
+    shared = teacher_logits.dim() == 1 and hosts.dim() > 1
+    _dense(teacher_logits, "teacher_logits", torch.float32, k if shared else rows * k, logits)
+    if not shared and teacher_logits.shape != hosts.shape:
+        raise ValueError("teacher_logits must have the shape of hosts, or [k]")
+    return 0 if shared else k
+
+
+def nbos_policy_distill(logits, hosts, teacher_logits, out_loss, out_stats=None, grad_loss=None, grad_scale=1.0,
+                        out_grad=None, temperature=1.0, stream=None) -> None:
+    """Distillation from a teacher's k best hosts per row. Device tensors: logits [..., H] (float32, bfloat16,
+    float16; rows evenly apart), hosts [..., k] int32 (-1 = none), teacher_logits [..., k] or [k] float32 or None,
+    out_loss [...] float32 or None, out_stats [..., 2] float32 or None, grad_loss [...] float32 or None; out_grad
+    like logits (or the logits themselves) or None. Asynchronous on the stream."""
+    desc = _logits(logits)
+    k = _choices(hosts, logits, desc.rows)
+    tstride = _teacher(teacher_logits, hosts, logits, desc.rows, k)
+    _dense(out_loss, "out_loss", torch.float32, desc.rows, logits)
+    _dense(out_stats, "out_stats", torch.float32, 2 * desc.rows, logits)
+    _dense(grad_loss, "grad_loss", torch.float32, desc.rows, logits)
+    gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_distill(ctypes.byref(desc), _ptr(hosts), _ptr(teacher_logits), tstride, k,
+                                              temperature, _ptr(grad_loss), grad_scale, _ptr(out_loss),
+                                              _ptr(out_stats), _ptr(out_grad), gstride, _stream_ptr(stream)))
+
+
+def nbos_policy_distill_backward(logits, hosts, teacher_logits, stats, out_grad, grad_loss=None, grad_scale=1.0,
+                                 temperature=1.0, stream=None) -> None:
+    """The gradient of nbos_policy_distill from the statistics it saved (out_stats)."""
+    desc = _logits(logits)
+    k = _choices(hosts, logits, desc.rows)
+    tstride = _teacher(teacher_logits, hosts, logits, desc.rows, k)
+    _dense(stats, "stats", torch.float32, 2 * desc.rows, logits)
+    _dense(grad_loss, "grad_loss", torch.float32, desc.rows, logits)
+    gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_distill_backward(ctypes.byref(desc), _ptr(hosts), _ptr(teacher_logits), tstride,
+                                                       k, temperature, _ptr(stats), _ptr(grad_loss), grad_scale,
+                                                       _ptr(out_grad), gstride, _stream_ptr(stream)))
+
+
+def _groups(logits) -> int:
+    return logits.shape[0] if logits.dim() > 2 else 1
+
+
+def nbos_policy_balance(logits, hosts, out_loss, out_counts, out_shares=None, out_stats=None, grad_loss=None,
+                        grad_scale=1.0, out_grad=None, stream=None) -> None:
+    """Load-balance loss and per-host counts. Device tensors: logits [N, B, H] (N groups) or [B, H] (one), hosts
+    [N, B, k] int32 (-1 = none), out_loss [N] float32, out_counts [N, H] int32, out_shares [N, H] float32 or None,
+    out_stats [N, B, 2] float32 or None, grad_loss [N] float32 or None; out_grad like logits (or the logits
+    themselves) or None. Asynchronous on the stream."""
+    desc = _logits(logits)
+    n = _groups(logits)
+    k = _choices(hosts, logits, desc.rows)
+    _dense(out_loss, "out_loss", torch.float32, n, logits)
+    _dense(out_counts, "out_counts", torch.int32, n * desc.n_hosts, logits)
+    _dense(out_shares, "out_shares", torch.float32, n * desc.n_hosts, logits)
+    _dense(out_stats, "out_stats", torch.float32, 2 * desc.rows, logits)
+    _dense(grad_loss, "grad_loss", torch.float32, n, logits)
+    gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_balance(ctypes.byref(desc), n, _ptr(hosts), k, _ptr(grad_loss), grad_scale,
+                                              _ptr(out_loss), _ptr(out_counts), _ptr(out_shares), _ptr(out_stats),
+                                              _ptr(out_grad), gstride, _stream_ptr(stream)))
+
+
+def nbos_policy_balance_backward(logits, hosts, stats, out_grad, grad_loss=None, grad_scale=1.0, stream=None) -> None:
+    """The gradient of nbos_policy_balance from the statistics it saved (out_stats)."""
+    desc = _logits(logits)
+    n = _groups(logits)
+    k = _choices(hosts, logits, desc.rows)
+    _dense(stats, "stats", torch.float32, 2 * desc.rows, logits)
+    _dense(grad_loss, "grad_loss", torch.float32, n, logits)
+    gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_balance_backward(ctypes.byref(desc), n, _ptr(hosts), k, _ptr(stats),
+                                                       _ptr(grad_loss), grad_scale, _ptr(out_grad), gstride,
+                                                       _stream_ptr(stream)))
+
+
+def nbos_policy_sample(logits, uniforms, out_hosts, out_found=None, temperature=None, top_k=None, top_p=None,
+                       min_p=None, stream=None) -> None:
+    """Draws distinct hosts. Device tensors: logits [..., H], uniforms [..., draws] float32 in [0, 1), out_hosts
+    [..., draws] int32 (-1 padding), out_found [...] int32 or None; temperature, top_p, min_p [...] float32 and
+    top_k [...] int32, one per row, or None (1 / off). Asynchronous on the stream."""
+    desc = _logits(logits)
+    if not isinstance(uniforms, torch.Tensor) or uniforms.shape[:-1] != logits.shape[:-1]:
+        raise ValueError("uniforms [..., draws] and logits [..., n_hosts] must agree on their rows")
+    draws = uniforms.shape[-1]
+    _dense(uniforms, "uniforms", torch.float32, desc.rows * draws, logits)
+    _dense(out_hosts, "out_hosts", torch.int32, desc.rows * draws, logits)
+    _dense(out_found, "out_found", torch.int32, desc.rows, logits)
+    for what, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        _dense(t, what, dtype, desc.rows, logits)
+    _check(load_library().nbos_policy_sample(ctypes.byref(desc), _ptr(uniforms), _ptr(temperature), _ptr(top_k),
+                                             _ptr(top_p), _ptr(min_p), draws, _ptr(out_hosts), _ptr(out_found),
+                                             _stream_ptr(stream)))
 
 
 def nbos_probe_int32_issue(mix: int, iters: int, blocks: int, threads: int, stream=None):

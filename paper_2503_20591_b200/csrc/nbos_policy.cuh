@@ -1,0 +1,210 @@
+// Shared by the learned-policy kernels (distillation, balance loss, sampling): element types, loads and
+// stores of a row, reductions over the lanes, warps and clustered blocks that share a row, and the argument
+// checks the entry points have in common.
+#ifndef NBOS_POLICY_CUH_
+#define NBOS_POLICY_CUH_
+
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "nbos_internal.h"
+
+namespace nbos {
+namespace policy {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr unsigned int kFull = 0xFFFFFFFFu;
+
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xFF800000); }
+
+// ---- elements: 32-bit arithmetic whatever the type, one rounding (to nearest even) at a store -------------
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+template <typename T> constexpr int kPer16 = 16 / (int)sizeof(T);
+
+__device__ __forceinline__ void unpack16(const uint4 &u, float (&v)[4], float)
+{
+    v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
+}
+__device__ __forceinline__ void unpack16(const uint4 &u, float (&v)[8], __nv_bfloat16)
+{
+    const unsigned int w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+}
+__device__ __forceinline__ void unpack16(const uint4 &u, float (&v)[8], __half)
+{
+    const unsigned int w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ uint4 pack16(const float (&v)[4], float)
+{
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint4 pack16(const float (&v)[8], __nv_bfloat16)
+{
+    unsigned int w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const unsigned int *>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 pack16(const float (&v)[8], __half)
+{
+    unsigned int w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const unsigned int *>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// VEC consecutive elements of a row from column `col`; columns from `end` on read as `fill`. VEC is 16 bytes'
+// worth (the row then starts on a 16-byte boundary and col is a multiple of VEC) or 1 (any alignment).
+// Loads are plain (not through the read-only path): the gradient may be written over the logits.
+template <typename T, int VEC>
+__device__ __forceinline__ void load_cols(const T *row, long long col, long long end, float fill, float (&v)[VEC])
+{
+    if constexpr (VEC == 1) {
+        v[0] = col < end ? to_float(__ldcs(row + col)) : fill;
+    } else {
+        if (col + VEC <= end) {
+            unpack16(__ldcs(reinterpret_cast<const uint4 *>(row + col)), v, T());
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = col + i < end ? to_float(__ldcs(row + col + i)) : fill;
+        }
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_cols(T *row, long long col, long long end, const float (&v)[VEC])
+{
+    if constexpr (VEC == 1) {
+        if (col < end) __stcs(row + col, from_float<T>(v[0]));
+    } else {
+        if (col + VEC <= end) {
+            __stcs(reinterpret_cast<uint4 *>(row + col), pack16(v, T()));
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (col + i < end) __stcs(row + col + i, from_float<T>(v[i]));
+        }
+    }
+}
+
+// ---- reductions over `lanes` neighbouring lanes (a power of two; every lane gets the result) ---------------
+__device__ __forceinline__ float lanes_max(float v, int lanes)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        if (off < lanes) v = fmaxf(v, __shfl_xor_sync(kFull, v, off));
+    return v;
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        if (off < lanes) v += __shfl_xor_sync(kFull, v, off);
+    return v;
+}
+
+// 2^((x - m) c); 0 where x is -inf even if m is -inf (a row without a finite logit). The subtraction comes
+// first: near the row's maximum, where the result matters, it is exact or nearly so.
+__device__ __forceinline__ float exp_from(float x, float m, float c)
+{
+    return exp2f((x - (m == neg_inf() ? 0.0f : m)) * c);
+}
+
+// ---- blocks that share a row: a cluster of `cs` blocks, or one block (cs = 1) ------------------------------
+__device__ __forceinline__ int cluster_rank(int cs)
+{
+    return cs > 1 ? (int)cooperative_groups::this_cluster().block_rank() : 0;
+}
+// arrive + wait: every block of the cluster has started, so its shared memory may be written from outside
+__device__ __forceinline__ void cluster_arrive(int cs)
+{
+    if (cs > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait(int cs)
+{
+    if (cs > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_sync(int cs)
+{
+    if (cs > 1)
+        cooperative_groups::this_cluster().sync();
+    else
+        __syncthreads();
+}
+template <typename V>
+__device__ __forceinline__ V *cluster_peer(V *shared, int rank, int cs)
+{
+    return cs > 1 ? cooperative_groups::this_cluster().map_shared_rank(shared, rank) : shared;
+}
+
+// ---- host side --------------------------------------------------------------------------------------------
+inline size_t dtype_bytes(int dtype) { return dtype == NBOS_F32 ? 4 : 2; }
+inline bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+inline int check_logits(const nbos_logits *l)
+{
+    if (!l) return fail(NBOS_ERR_INVALID_ARG, "logits is NULL");
+    if (l->dtype != NBOS_F32 && l->dtype != NBOS_BF16 && l->dtype != NBOS_F16)
+        return fail(NBOS_ERR_INVALID_ARG, "unknown dtype %d", l->dtype);
+    if (l->n_hosts < 1 || l->n_hosts > NBOS_MAX_HOSTS)
+        return fail(NBOS_ERR_INVALID_ARG, "n_hosts must be in 1..%d (got %d)", NBOS_MAX_HOSTS, l->n_hosts);
+    if (l->rows < 0 || l->rows > NBOS_POLICY_MAX_ROWS)
+        return fail(NBOS_ERR_INVALID_ARG, "rows must be in 0..2^31 - 1 (got %lld)", (long long)l->rows);
+    if (l->rows > 1 && (l->row_stride < l->n_hosts || l->row_stride > ((int64_t)1 << 40)))
+        return fail(NBOS_ERR_INVALID_ARG, "row_stride must be in n_hosts..2^40 (got %lld)", (long long)l->row_stride);
+    if (l->rows > 0 && !l->data) return fail(NBOS_ERR_INVALID_ARG, "logits->data is NULL");
+    if (!aligned_to(l->data, dtype_bytes(l->dtype)))
+        return fail(NBOS_ERR_INVALID_ARG, "logits->data is not aligned to its element type");
+    return NBOS_OK;
+}
+inline int check_grad(const nbos_logits *l, const void *grad, int64_t grad_stride)
+{
+    if (!aligned_to(grad, dtype_bytes(l->dtype)))
+        return fail(NBOS_ERR_INVALID_ARG, "out_grad is not aligned to its element type");
+    if (l->rows > 1 && (grad_stride < l->n_hosts || grad_stride > ((int64_t)1 << 40)))
+        return fail(NBOS_ERR_INVALID_ARG, "grad_stride must be in n_hosts..2^40 (got %lld)", (long long)grad_stride);
+    return NBOS_OK;
+}
+inline int check_k(int32_t k)
+{
+    if (k < 1 || k > NBOS_POLICY_MAX_K) return fail(NBOS_ERR_INVALID_ARG, "k must be in 1..%d (got %d)", NBOS_POLICY_MAX_K, k);
+    return NBOS_OK;
+}
+inline int check_sm100(int *sms, int *device)
+{
+    int major = 0;
+    NBOS_CUDA_TRY(cudaGetDevice(device));
+    NBOS_CUDA_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *device));
+    if (major != 10) return fail(NBOS_ERR_UNSUPPORTED_DEVICE, "device %d has compute capability %d.x", *device, major);
+    NBOS_CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device));
+    return NBOS_OK;
+}
+// every row of `p` starts on a 16-byte boundary
+inline bool rows_aligned16(const void *p, int64_t rows, int64_t stride, size_t elem)
+{
+    return aligned_to(p, 16) && (rows <= 1 || (stride * elem) % 16 == 0);
+}
+
+}  // namespace policy
+}  // namespace nbos
+#endif

@@ -1,0 +1,444 @@
+// Distillation of a placement policy from a teacher's k best hosts per row (nbos_policy_distill).
+//
+// Per row with logits x, m = max x, S = sum_j 2^((x_j - m) c), c = log2(e) / T, p_j = 2^((x_j - m) c) / S and the
+// teacher's q over its counting entries:
+//   loss = T^2 sum_k q_k (ln q_k - ln p_k),  d loss / d x_j = T (p_j - q_j).
+// What bounds it: the logits' bytes, read once, and as many written for the gradient. So a row stays in registers
+// between its reduction and its gradient (32 elements a thread): a power of two of lanes of one warp share a short
+// row (up to 1,024 hosts), a block or a cluster of up to 8 blocks a longer one; only rows of more than 262,144
+// hosts are read twice. Each exponential is computed once; threads keep it relative to their warp's maximum and
+// scale it by 2^((m_warp - m) c) / S when the row's statistics are known.
+#include <math.h>
+
+#include "nbos_policy.cuh"
+
+namespace nbos {
+namespace {
+
+using namespace policy;
+
+constexpr int kElems = 32;             // row elements a thread holds in the block form
+constexpr int kMaxCluster = 8;
+constexpr int kWarpRow = 32 * kElems;  // longest row of the warp form
+
+struct DistillArgs {
+    const void *x;
+    long long rows, stride;
+    int n;
+    const int32_t *hosts;
+    const float *teacher;
+    long long tstride;
+    int k;
+    float T, c, inv_t;
+    const float *grad_loss;
+    float grad_scale;
+    float *loss;
+    float *stats;
+    const float *stats_in;
+    void *grad;
+    long long gstride;
+};
+
+struct Entry {
+    int host;   // -1: does not count
+    float t, x;
+};
+
+template <typename T>
+__device__ __forceinline__ Entry load_entry(const DistillArgs &a, long long row, const T *x, int k)
+{
+    Entry e;
+    e.host = a.hosts[row * a.k + k];
+    e.t = a.teacher ? a.teacher[row * a.tstride + k] : 0.0f;
+    e.x = neg_inf();
+    if (e.host >= 0 && e.host < a.n) e.x = to_float(x[e.host]);
+    // comparisons with NaN are false: a NaN teacher logit does not count; a NaN student logit does (its row is NaN)
+    if (!(e.t > neg_inf()) || e.x == neg_inf()) e.host = -1;
+    return e;
+}
+
+// The teacher's softmax over `lanes` lanes: largest teacher logit of the row (-inf: no entry counts) and the sum.
+template <typename T>
+__device__ __forceinline__ void teacher_stats(const DistillArgs &a, long long row, const T *x, bool active, int sub,
+                                              int lanes, const Entry &first, float &tm, float &z)
+{
+    tm = neg_inf();
+    for (int k = sub; active && k < a.k; k += lanes) {
+        const Entry e = k == sub ? first : load_entry(a, row, x, k);
+        if (e.host >= 0) tm = fmaxf(tm, e.t);
+    }
+    tm = lanes_max(tm, lanes);
+    z = 0.0f;
+    for (int k = sub; active && k < a.k; k += lanes) {
+        const Entry e = k == sub ? first : load_entry(a, row, x, k);
+        if (e.host >= 0) z += exp_from(e.t, tm, a.c);
+    }
+    z = lanes_sum(z, lanes);
+}
+
+template <typename T>
+__device__ __forceinline__ float row_loss(const DistillArgs &a, long long row, const T *x, bool active, int sub, int lanes,
+                                          const Entry &first, float tm, float z, float m, float s)
+{
+    const float shift = logf(s) - logf(z);
+    float l = 0.0f;
+    for (int k = sub; active && k < a.k; k += lanes) {
+        const Entry e = k == sub ? first : load_entry(a, row, x, k);
+        if (e.host < 0) continue;
+        const float q = exp_from(e.t, tm, a.c) / z;
+        // q underflows to 0 before ln q leaves the range of 32 bits; 0 * -inf is kept out
+        const float v = q * (((e.t - tm) - (e.x - m)) * a.inv_t + shift);
+        l += q == 0.0f ? 0.0f : v;
+    }
+    return lanes_sum(l, lanes) * a.T * a.T;
+}
+
+// The gradient at the listed hosts, written over what the row's owner wrote there: p - (all of q that goes there).
+template <typename T>
+__device__ __forceinline__ void fix_entries(const DistillArgs &a, long long row, const T *x, const Entry &e, T *grad,
+                                            float tm, float z, float m, float s, float gmul)
+{
+    float q = 0.0f;
+    for (int k = 0; k < a.k; ++k) {
+        if (a.hosts[row * a.k + k] != e.host) continue;
+        const float t = a.teacher ? a.teacher[row * a.tstride + k] : 0.0f;
+        if (t > neg_inf()) q += exp_from(t, tm, a.c) / z;
+    }
+    grad[e.host] = from_float<T>(gmul * (exp_from(e.x, m, a.c) / s - q));
+}
+
+__device__ __forceinline__ float grad_multiplier(const DistillArgs &a, long long row)
+{
+    return a.T * a.grad_scale * (a.grad_loss ? a.grad_loss[row] : 1.0f);
+}
+
+// ---- warp form: `lanes` lanes per row, CH * VEC elements each ----------------------------------------------
+template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
+__global__ void __launch_bounds__(128) distill_warp_kernel(DistillArgs a, int lanes)
+{
+    const int lane = threadIdx.x & 31, sub = lane & (lanes - 1);
+    const long long warp = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const long long row = warp * (32 / lanes) + lane / lanes;
+    const bool active = row < a.rows;
+    const T *x = static_cast<const T *>(a.x) + (active ? row : 0) * a.stride;
+    Entry first{-1, 0.0f, 0.0f};
+    float v[CH][VEC];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load_cols<T, VEC>(x, (c * lanes + sub) * VEC, active ? a.n : 0, neg_inf(), v[c]);
+    if (active && sub < a.k) first = load_entry(a, row, x, sub);
+    float m, s;
+    if (SAVED) {
+        m = active ? a.stats_in[2 * row] : 0.0f;
+        s = active ? a.stats_in[2 * row + 1] : 1.0f;
+    } else {
+        m = neg_inf();
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
+        m = lanes_max(m, lanes);
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            v[c][i] = exp_from(v[c][i], m, a.c);
+            sum += v[c][i];
+        }
+    if (!SAVED) s = lanes_sum(sum, lanes);
+    float tm, z;
+    teacher_stats(a, row, x, active, sub, lanes, first, tm, z);
+    const bool any = tm > neg_inf();
+    if (!SAVED) {
+        const float l = row_loss(a, row, x, active && any, sub, lanes, first, tm, z, m, s);
+        if (active && sub == 0) {
+            if (a.loss) a.loss[row] = any ? l : 0.0f;
+            if (a.stats) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+        }
+    }
+    if (GRAD) {
+        T *grad = static_cast<T *>(a.grad) + (active ? row : 0) * a.gstride;
+        const float gmul = active ? grad_multiplier(a, row) : 0.0f;
+        const float fac = gmul / s;
+        __syncwarp();   // a gradient written over the logits: the entries' logits have been read
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[c][i] = any ? v[c][i] * fac : 0.0f;
+            store_cols<T, VEC>(grad, (c * lanes + sub) * VEC, active ? a.n : 0, v[c]);
+        }
+        __syncwarp();
+        // entries beyond the lanes re-read their logits, which a gradient written over them has replaced: those
+        // are taken from the statistics' side instead (see the block form, which such k always use)
+        if (active && first.host >= 0) fix_entries(a, row, x, first, grad, tm, z, m, s, gmul);
+    }
+}
+
+// (m, s) with s relative to m, merged with (m2, s2)
+__device__ __forceinline__ void merge_stats(float &m, float &s, float m2, float s2, float c)
+{
+    const float top = fmaxf(m, m2);
+    s = s * exp_from(m, top, c) + s2 * exp_from(m2, top, c);
+    m = top;
+}
+
+// ---- block form: blockDim.x * CS threads per row, CS = cluster size ----------------------------------------
+// KEEP: the row stays in registers; otherwise (rows too long) it is read once more for the gradient.
+template <typename T, int VEC, bool KEEP, bool GRAD, bool SAVED>
+__global__ void __launch_bounds__(1024, 1) distill_block_kernel(DistillArgs a, int cs, int span)
+{
+    constexpr int CH = kElems / VEC;
+    __shared__ float2 s_stats[kMaxCluster * 32];
+    __shared__ float s_teacher[2];
+    __shared__ float s_entry_x[NBOS_POLICY_MAX_K];
+    const int rank = cluster_rank(cs);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const long long row = blockIdx.x / cs;
+    const T *x = static_cast<const T *>(a.x) + row * a.stride;
+    const long long first_col = (long long)rank * span, end_col = min((long long)a.n, first_col + span);
+    const long long chunk = (long long)blockDim.x * VEC;
+
+    cluster_arrive(cs);
+    float v[CH][VEC];
+    float m = neg_inf(), s = 0.0f;
+    if (KEEP) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            load_cols<T, VEC>(x, first_col + c * chunk + threadIdx.x * VEC, end_col, neg_inf(), v[c]);
+    }
+    if (SAVED) {
+        m = a.stats_in[2 * row];
+        s = a.stats_in[2 * row + 1];
+    } else if (KEEP) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
+        m = lanes_max(m, 32);
+    }
+    if (KEEP) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                v[c][i] = exp_from(v[c][i], m, a.c);
+                sum += v[c][i];
+            }
+        if (!SAVED) s = lanes_sum(sum, 32);
+    } else if (!SAVED) {
+        for (long long col = first_col + threadIdx.x * VEC; col < end_col; col += chunk) {
+            float w[VEC];
+            load_cols<T, VEC>(x, col, end_col, neg_inf(), w);
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) top = fmaxf(top, w[i]);
+            s *= exp_from(m, top, a.c);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s += exp_from(w[i], top, a.c);
+            m = top;
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1)
+            merge_stats(m, s, __shfl_xor_sync(kFull, m, off), __shfl_xor_sync(kFull, s, off), a.c);
+    }
+    const float m_warp = m;
+    Entry first{-1, 0.0f, 0.0f};
+    float tm = neg_inf(), z = 0.0f;
+    if (warp == 0) {
+        if (lane < a.k) first = load_entry(a, row, x, lane);
+        teacher_stats(a, row, x, true, lane, 32, first, tm, z);
+        if (lane == 0) s_teacher[0] = tm, s_teacher[1] = z;
+    }
+    // the listed hosts' logits, before a gradient may be written over them
+    for (int k = threadIdx.x; GRAD && k < a.k; k += blockDim.x) s_entry_x[k] = load_entry(a, row, x, k).x;
+    cluster_wait(cs);   // the other blocks run: their shared memory may be written
+    if (!SAVED) {
+        // every warp's (m, s) goes to every block of the cluster; each warp then merges all of them
+        if (lane < cs) {
+            float2 *dst = cluster_peer(s_stats, lane, cs);
+            dst[rank * warps + warp] = make_float2(m, s);
+        }
+    }
+    cluster_sync(cs);   // also: no block writes its gradient before the others have read the entries
+    if (!SAVED) {
+        m = neg_inf(), s = 0.0f;
+        for (int i = lane; i < cs * warps; i += 32) merge_stats(m, s, s_stats[i].x, s_stats[i].y, a.c);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1)
+            merge_stats(m, s, __shfl_xor_sync(kFull, m, off), __shfl_xor_sync(kFull, s, off), a.c);
+    }
+    tm = s_teacher[0], z = s_teacher[1];
+    const bool any = tm > neg_inf();
+    if (!SAVED && warp == 0 && rank == 0) {
+        // listed hosts beyond the first 32 are re-read here: with a gradient the loss is taken before the barrier below
+        const float l = row_loss(a, row, x, any, lane, 32, first, tm, z, m, s);
+        if (lane == 0) {
+            if (a.loss) a.loss[row] = any ? l : 0.0f;
+            if (a.stats) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+        }
+    }
+    if (GRAD) {
+        T *grad = static_cast<T *>(a.grad) + row * a.gstride;
+        const float gmul = grad_multiplier(a, row);
+        const float fac = KEEP ? gmul / s * exp_from(m_warp, m, a.c) : gmul / s;
+        if (a.k > 32) cluster_sync(cs);   // row_loss has re-read logits that the next lines may write over
+        if (KEEP) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[c][i] = any ? v[c][i] * fac : 0.0f;
+                store_cols<T, VEC>(grad, first_col + c * chunk + threadIdx.x * VEC, end_col, v[c]);
+            }
+        } else {
+            for (long long col = first_col + threadIdx.x * VEC; col < end_col; col += chunk) {
+                float w[VEC];
+                load_cols<T, VEC>(x, col, end_col, neg_inf(), w);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) w[i] = any ? exp_from(w[i], m, a.c) * fac : 0.0f;
+                store_cols<T, VEC>(grad, col, end_col, w);
+            }
+        }
+        __syncthreads();
+        for (int k = threadIdx.x; any && k < a.k; k += blockDim.x) {
+            Entry e;
+            e.host = a.hosts[row * a.k + k];
+            e.t = a.teacher ? a.teacher[row * a.tstride + k] : 0.0f;
+            e.x = s_entry_x[k];
+            if (e.host < first_col || e.host >= end_col || !(e.t > neg_inf()) || e.x == neg_inf()) continue;
+            fix_entries(a, row, x, e, grad, tm, z, m, s, gmul);
+        }
+    }
+}
+
+template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
+cudaError_t launch_warp(const DistillArgs &a, int lanes, cudaStream_t stream)
+{
+    const long long rows_per_block = (128 / 32) * (32 / lanes);
+    const long long blocks = (a.rows + rows_per_block - 1) / rows_per_block;
+    distill_warp_kernel<T, VEC, CH, GRAD, SAVED><<<(unsigned int)blocks, 128, 0, stream>>>(a, lanes);
+    return cudaGetLastError();
+}
+
+template <typename T, int VEC, bool GRAD, bool SAVED>
+cudaError_t launch(const DistillArgs &a, int sms, cudaStream_t stream)
+{
+    // The warp form keeps one teacher entry per lane (its logit must outlive an in-place gradient): longer lists
+    // go to the block form.
+    int lanes = 1;
+    while (lanes < 32 && lanes * VEC < a.n) lanes *= 2;
+    while (lanes < 32 && lanes < a.k) lanes *= 2;
+    if (a.n <= kWarpRow && a.k <= 32) {
+        const int need = (a.n + lanes * VEC - 1) / (lanes * VEC);
+        if (need <= 1) return launch_warp<T, VEC, 1, GRAD, SAVED>(a, lanes, stream);
+        if (need <= 2) return launch_warp<T, VEC, 2, GRAD, SAVED>(a, lanes, stream);
+        if (VEC >= 4 || need <= 4) return launch_warp<T, VEC, (VEC == 4 ? 8 : 4), GRAD, SAVED>(a, lanes, stream);
+        if constexpr (VEC == 1) {
+            if (need <= 8) return launch_warp<T, VEC, 8, GRAD, SAVED>(a, lanes, stream);
+            if (need <= 16) return launch_warp<T, VEC, 16, GRAD, SAVED>(a, lanes, stream);
+            return launch_warp<T, VEC, 32, GRAD, SAVED>(a, lanes, stream);
+        }
+    }
+    // One block per row while the rows fill the GPU; more blocks per row when they do not, or when the row needs them
+    const bool keep = a.n <= kMaxCluster * 1024 * kElems;
+    int cs = 1;
+    auto threads_for = [&](int c) { return ((a.n + c * kElems - 1) / (c * kElems) + 31) / 32 * 32; };
+    while (cs < kMaxCluster && (threads_for(cs) > 1024 || (a.rows * cs < 2 * sms && threads_for(cs) > 128))) cs *= 2;
+    const int threads = keep ? threads_for(cs) : 1024;
+    const int span = ((a.n + cs - 1) / cs + VEC - 1) / VEC * VEC;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cs;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    // grid.x holds rows * cs blocks: 2^31 - 1 at most, so very many rows go in several launches
+    const long long rows_per_launch = 2147483647ll / kMaxCluster;
+    for (long long r = 0; r < a.rows; r += rows_per_launch) {
+        DistillArgs b = a;
+        b.rows = a.rows - r < rows_per_launch ? a.rows - r : rows_per_launch;
+        b.x = static_cast<const T *>(a.x) + r * a.stride;
+        b.hosts += r * a.k;
+        if (b.teacher) b.teacher += r * a.tstride;
+        if (b.grad_loss) b.grad_loss += r;
+        if (b.loss) b.loss += r;
+        if (b.stats) b.stats += 2 * r;
+        if (b.stats_in) b.stats_in += 2 * r;
+        if (b.grad) b.grad = static_cast<T *>(a.grad) + r * a.gstride;
+        cfg.gridDim = dim3((unsigned int)(b.rows * cs));
+        cudaError_t e = keep ? cudaLaunchKernelEx(&cfg, distill_block_kernel<T, VEC, true, GRAD, SAVED>, b, cs, span)
+                             : cudaLaunchKernelEx(&cfg, distill_block_kernel<T, VEC, false, GRAD, SAVED>, b, cs, span);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+template <typename T>
+cudaError_t dispatch(const DistillArgs &a, int sms, cudaStream_t stream)
+{
+    const bool vec = rows_aligned16(a.x, a.rows, a.stride, sizeof(T)) &&
+                     (!a.grad || rows_aligned16(a.grad, a.rows, a.gstride, sizeof(T)));
+    constexpr int V = kPer16<T>;
+    if (a.stats_in) return vec ? launch<T, V, true, true>(a, sms, stream) : launch<T, 1, true, true>(a, sms, stream);
+    if (a.grad) return vec ? launch<T, V, true, false>(a, sms, stream) : launch<T, 1, true, false>(a, sms, stream);
+    return vec ? launch<T, V, false, false>(a, sms, stream) : launch<T, 1, false, false>(a, sms, stream);
+}
+
+int distill(const nbos_logits *l, const int32_t *hosts, const float *teacher, int64_t tstride, int32_t k, float T,
+            const float *stats_in, const float *grad_loss, float grad_scale, float *out_loss, float *out_stats,
+            void *out_grad, int64_t gstride, cudaStream_t stream)
+{
+    int rc = check_logits(l);
+    if (rc || (rc = check_k(k))) return rc;
+    if (!(T > 0.0f) || !isfinite(T) || !isfinite(kLog2e / T) || !isfinite(T * T))
+        return fail(NBOS_ERR_INVALID_ARG, "temperature must be finite and > 0 (as must 1 / T and T^2)");
+    if (tstride != 0 && (tstride < k || tstride > ((int64_t)1 << 40)))
+        return fail(NBOS_ERR_INVALID_ARG, "teacher_stride must be 0 or in k..2^40 (got %lld)", (long long)tstride);
+    if (l->rows == 0) return NBOS_OK;
+    if (!out_loss && !out_stats && !out_grad) return fail(NBOS_ERR_INVALID_ARG, "no output asked for");
+    if (!hosts) return fail(NBOS_ERR_INVALID_ARG, "hosts is NULL");
+    if (out_grad && (rc = check_grad(l, out_grad, gstride))) return rc;
+    if (out_grad == l->data && out_grad && l->rows > 1 && gstride != l->row_stride)
+        return fail(NBOS_ERR_INVALID_ARG, "a gradient written over the logits needs their row_stride");
+    if (!aligned_to(hosts, 4) || !aligned_to(teacher, 4) || !aligned_to(grad_loss, 4) || !aligned_to(out_loss, 4) ||
+        !aligned_to(out_stats, 4) || !aligned_to(stats_in, 4))
+        return fail(NBOS_ERR_INVALID_ARG, "an int32 / float array is not 4-byte aligned");
+    int sms = 0, device = 0;
+    if ((rc = check_sm100(&sms, &device))) return rc;
+    DistillArgs a{l->data, l->rows, l->row_stride, l->n_hosts, hosts, teacher, tstride, k, T, kLog2e / T, 1.0f / T,
+                  grad_loss, grad_scale, out_loss, out_stats, stats_in, out_grad, gstride};
+    if (a.rows == 1) a.stride = a.gstride = l->n_hosts;
+    const cudaError_t e = l->dtype == NBOS_F32    ? dispatch<float>(a, sms, stream)
+                          : l->dtype == NBOS_BF16 ? dispatch<__nv_bfloat16>(a, sms, stream)
+                                                  : dispatch<__half>(a, sms, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "distillation launch");
+    return NBOS_OK;
+}
+
+}  // namespace
+}  // namespace nbos
+
+using namespace nbos;
+
+extern "C" int nbos_policy_distill(const nbos_logits *logits, const int32_t *hosts, const float *teacher_logits,
+                                   int64_t teacher_stride, int32_t k, float temperature, const float *grad_loss,
+                                   float grad_scale, float *out_loss, float *out_stats, void *out_grad,
+                                   int64_t grad_stride, void *cuda_stream)
+{
+    return distill(logits, hosts, teacher_logits, teacher_stride, k, temperature, nullptr, grad_loss, grad_scale,
+                   out_loss, out_stats, out_grad, grad_stride, static_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" int nbos_policy_distill_backward(const nbos_logits *logits, const int32_t *hosts,
+                                            const float *teacher_logits, int64_t teacher_stride, int32_t k,
+                                            float temperature, const float *stats, const float *grad_loss,
+                                            float grad_scale, void *out_grad, int64_t grad_stride, void *cuda_stream)
+{
+    if (logits && logits->rows > 0 && (!stats || !out_grad)) return fail(NBOS_ERR_INVALID_ARG, "stats / out_grad is NULL");
+    return distill(logits, hosts, teacher_logits, teacher_stride, k, temperature, stats, grad_loss, grad_scale,
+                   nullptr, nullptr, out_grad, grad_stride, static_cast<cudaStream_t>(cuda_stream));
+}
