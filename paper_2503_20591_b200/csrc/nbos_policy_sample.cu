@@ -41,6 +41,20 @@ __device__ __forceinline__ unsigned int key_of(float x)
     return b ^ ((unsigned int)((int)b >> 31) | 0x80000000u);
 }
 
+// logits, NaN as -inf, +inf as the largest finite float, -0 as 0 (equal logits have equal keys)
+__device__ __forceinline__ float clean(float v) { return fminf(fmaxf(v, neg_inf()), 3.402823466e38f) + 0.0f; }
+
+// floor(2^31 * 2^((x - m) scale)): difference and product are rounded one by one (no contraction). The power is at
+// most 1, so its significand shifted by its exponent is the whole number; below 2^-31 nothing is left.
+__device__ __forceinline__ unsigned int weight_of(float x, float m, float scale)
+{
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__fmul_rn(__fsub_rn(x, m), scale)));
+    const unsigned int b = __float_as_uint(e), shift = 127u - (b >> 23);
+    const unsigned int w = (b << 8) | 0x80000000u;
+    return shift < 32u ? w >> shift : 0u;
+}
+
 // sum over the warp of values below 2^52, by two 26-bit halves
 __device__ __forceinline__ u64 warp_sum(u64 v)
 {
@@ -48,8 +62,17 @@ __device__ __forceinline__ u64 warp_sum(u64 v)
     const unsigned int hi = __reduce_add_sync(kFull, (unsigned int)(v >> 26));
     return ((u64)hi << 26) + lo;
 }
+__device__ __forceinline__ u64 warp_scan(u64 v, int lane)   // inclusive
+{
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const u64 other = __shfl_up_sync(kFull, v, off);
+        if (lane >= off) v += other;
+    }
+    return v;
+}
 
-// floor(total * floor(share * 2^24) / 2^24) for a share in [0, 1]; total below 2^52
+// floor(total * steps / 2^24); total below 2^52, steps at most 2^24
 __device__ __forceinline__ u64 share_of(u64 total, unsigned int steps)
 {
     return (u64)steps * (total >> 24) + (((u64)steps * (total & 0xFFFFFFu)) >> 24);
@@ -61,7 +84,7 @@ struct Team {
     ulonglong2 (*slots)[kMaxCluster * 32];   // two sets, taken in turn
     int warps, cs, me, lane, turn;           // me: this warp's place among all of the row
 
-    // every warp's (a, b), which the lanes of a warp agree on, to every warp; then slots[done]
+    // every warp's (a, b), which the lanes of a warp agree on, to every warp, in slots[result]
     __device__ __forceinline__ int exchange(u64 a, u64 b)
     {
         const int now = turn;
@@ -79,6 +102,29 @@ struct Team {
         for (int i = lane; i < warps; i += 32) a += slots[now][i].x, b += slots[now][i].y;
         a = warp_sum(a), b = warp_sum(b);
     }
+    // a lane's sum of at most 32 weights with their number above bit 44, as one value: mass and number over the row
+    __device__ __forceinline__ void sum_packed(u64 v, u64 &mass, u64 &number)
+    {
+        const unsigned int lo = __reduce_add_sync(kFull, (unsigned int)v & 0x3FFFFFFu);
+        const unsigned int hi = __reduce_add_sync(kFull, (unsigned int)(v >> 26) & 0x3FFFFu);
+        mass = ((u64)hi << 26) + lo;
+        number = __reduce_add_sync(kFull, (unsigned int)(v >> 44));
+        if (!MULTI) return;
+        const int now = exchange(mass, number);
+        u64 a = 0;
+        unsigned int b = 0;
+        for (int i = lane; i < warps; i += 32) a += slots[now][i].x, b += (unsigned int)slots[now][i].y;
+        mass = warp_sum(a), number = __reduce_add_sync(kFull, b);
+    }
+    __device__ __forceinline__ unsigned int count(unsigned int v)
+    {
+        v = __reduce_add_sync(kFull, v);
+        if (!MULTI) return v;
+        const int now = exchange(v, 0);
+        v = 0;
+        for (int i = lane; i < warps; i += 32) v += (unsigned int)slots[now][i].x;
+        return __reduce_add_sync(kFull, v);
+    }
     __device__ __forceinline__ float max(float v)
     {
         v = lanes_max(v, 32);
@@ -88,14 +134,19 @@ struct Team {
         for (int i = lane; i < warps; i += 32) v = fmaxf(v, __uint_as_float((unsigned int)slots[now][i].x));
         return lanes_max(v, 32);
     }
-    // weight in the warps before this one
-    __device__ __forceinline__ u64 before(u64 mine)
+    // sums of `mine`, which the lanes of a warp agree on: over the warps before this one, and over all
+    __device__ __forceinline__ void prefix(u64 mine, u64 &before, u64 &all)
     {
-        if (!MULTI) return 0;
+        before = 0, all = mine;
+        if (!MULTI) return;
         const int now = exchange(mine, 0);
-        u64 sum = 0;
-        for (int i = lane; i < me; i += 32) sum += slots[now][i].x;
-        return warp_sum(sum);
+        u64 b = 0, a = 0;
+        for (int i = lane; i < warps; i += 32) {
+            const u64 v = slots[now][i].x;
+            a += v;
+            if (i < me) b += v;
+        }
+        before = warp_sum(b), all = warp_sum(a);
     }
     // the warp that has something (has: agreed in the warp) tells all
     __device__ __forceinline__ void tell(bool has, u64 &a, u64 &b)
@@ -109,90 +160,90 @@ struct Team {
     }
 };
 
-// A lane's elements: registers (REGS), or the workspace for rows that do not fit. chunk c of the lane covers the
-// columns base + (c * 32 + lane) * VEC ...
-template <int VEC, int CH, bool REGS>
+// A lane's elements: registers (REGS), or the workspace for rows that do not fit. Chunk c of the lane covers the
+// columns base + c * 32 * VEC + 0 .. VEC - 1.
+template <int VEC_, int CH_, bool REGS_>
 struct Elems {
+    static constexpr int VEC = VEC_, CH = CH_;
+    static constexpr bool REGS = REGS_;
     unsigned int r[REGS ? CH * VEC : 1];
     unsigned int *store;
     int chunks;
-    long long base, n;   // first column of the lane's chunk 0; columns of the row
+    int base, n;   // first column of the lane's chunk 0; columns of the row
     template <typename F>
     __device__ __forceinline__ void each(F f)   // f(value &, column)
     {
-        if (REGS) {
+        if constexpr (REGS) {
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) f(r[c * VEC + i], (int)base + c * 32 * VEC + i);
+                for (int i = 0; i < VEC; ++i) f(r[c * VEC + i], base + c * 32 * VEC + i);
         } else {
             for (int c = 0; c < chunks; ++c)
                 for (int i = 0; i < VEC; ++i) {
-                    const long long col = base + (long long)c * 32 * VEC + i;
+                    const int col = base + c * 32 * VEC + i;
                     if (col >= n) return;
                     unsigned int v = store[col];
-                    f(v, (int)col);
+                    f(v, col);
                     store[col] = v;
                 }
         }
     }
-    // the first column, in index order over the warp, at which the running sum of value(element, column) from `from`
-    // exceeds t; the warp must hold it. Returns the column and the value there.
+    // the sum of value(element, column) over the lane's part of chunk c
     template <typename F>
-    __device__ __forceinline__ void find(u64 t, u64 from, int lane, F value, int &col_out, u64 &val_out)
+    __device__ __forceinline__ u64 chunk_sum(int c, F value)
+    {
+        u64 s = 0;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int col = base + c * 32 * VEC + i;
+            if constexpr (REGS)
+                s += value(r[c * VEC + i], col);
+            else
+                s += col < n ? value(store[col], col) : 0;
+        }
+        return s;
+    }
+    // The first column, in index order over the warp, at which the running sum of value(element, column) from `from`
+    // exceeds t, and the value there; the warp must hold it. sum_of(c): the lane's sum over chunk c.
+    template <typename S, typename F>
+    __device__ __forceinline__ void find(u64 t, u64 from, int lane, S sum_of, F value, int &col_out, u64 &val_out)
     {
         u64 run = from, s_found = 0, run_found = 0;
         int c_found = -1;
         auto step = [&](int c) {
             if (c_found >= 0) return;
-            u64 s = 0;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) s += at(c, i, value);
-            const u64 total = warp_sum(s);
+            const u64 s = sum_of(c), total = warp_sum(s);
             if (t < run + total) c_found = c, s_found = s, run_found = run;
             run += total;
         };
-        if (REGS) {
+        if constexpr (REGS) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) step(c);
         } else {
             for (int c = 0; c < chunks; ++c) step(c);
         }
-        u64 upto = s_found;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const u64 other = __shfl_up_sync(kFull, upto, off);
-            if (lane >= off) upto += other;
-        }
-        upto += run_found;
-        const unsigned int over = __ballot_sync(kFull, t < upto);
-        const int owner = __ffs(over) - 1;
+        const u64 upto = run_found + warp_scan(s_found, lane);
+        const int owner = __ffs(__ballot_sync(kFull, t < upto)) - 1;
         u64 acc = upto - s_found, val = 0;
         int col = -1;
-        auto look = [&](int c) {
-            if (c != c_found) return;
+        const int first = base + c_found * 32 * VEC;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const u64 v = at(c, i, value);
-                acc += v;
-                if (col < 0 && t < acc) col = (int)(base + (long long)c * 32 * VEC + i), val = v;
+        for (int i = 0; i < VEC; ++i) {
+            u64 v = 0;
+            if constexpr (REGS) {
+                unsigned int raw = r[i];
+#pragma unroll
+                for (int c = 1; c < CH; ++c) raw = c == c_found ? r[c * VEC + i] : raw;
+                v = value(raw, first + i);
+            } else if (c_found >= 0 && first + i < n) {
+                v = value(store[first + i], first + i);
             }
-        };
-        if (REGS) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c) look(c);
-        } else {
-            if (c_found >= 0) look(c_found);
+            acc += v;
+            if (col < 0 && t < acc) col = first + i, val = v;
         }
         col_out = __shfl_sync(kFull, col, owner);
         val_out = __shfl_sync(kFull, val, owner);
-    }
-    template <typename F>
-    __device__ __forceinline__ u64 at(int c, int i, F value)
-    {
-        const long long col = base + (long long)c * 32 * VEC + i;
-        if (REGS) return value(r[c * VEC + i], (int)col);
-        return col < n ? value(store[col], (int)col) : 0;
     }
 };
 
@@ -201,106 +252,69 @@ template <bool MULTI, typename E, typename F>
 __device__ __forceinline__ int nth_column(Team<MULTI> &team, E &e, u64 m, F pick)
 {
     auto one = [&](unsigned int v, int col) -> u64 { return pick(v, col) ? 1 : 0; };
-    u64 mine = 0;
-    e.each([&](unsigned int &v, int col) { mine += one(v, col); });
-    mine = warp_sum(mine);
-    const u64 before = team.before(mine);
+    unsigned int here = 0;
+    e.each([&](unsigned int &v, int col) { here += pick(v, col) ? 1u : 0u; });
+    const u64 mine = __reduce_add_sync(kFull, here);
+    u64 before, all;
+    team.prefix(mine, before, all);
     int col = -1;
-    u64 val = 0, where = 0;
+    u64 val = 0;
     const bool has = m >= before && m < before + mine;
-    if (has) e.find(m, before, team.lane, one, col, val);
-    where = (u64)(unsigned int)col;
+    if (has) e.find(m, before, team.lane, [&](int c) { return e.chunk_sum(c, one); }, one, col, val);
+    u64 where = (u64)(unsigned int)col;
     team.tell(has, where, val);
     return (int)(unsigned int)where;
 }
 
-template <typename T, int CH, bool MULTI, bool REGS>
-__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team<MULTI> team, unsigned int *store, int chunks)
+struct Row {
+    float m, scale, top_p, min_p;
+    int k;          // 0: off
+    bool greedy, none;
+};
+
+// Filters and draws. e holds logits (as bits); logit(col) reads one again, host(col) names the column's host.
+template <bool MULTI, typename E, typename X, typename H>
+__device__ __forceinline__ void decide(const SampleArgs &a, long long row, const Row &p, Team<MULTI> &team, E &e, X logit, H host)
 {
-    constexpr int VEC = kPer16<T>;
-    const T *x = static_cast<const T *>(a.x) + row * a.stride;
     const int lane = team.lane;
-    Elems<VEC, CH, REGS> e;
-    e.store = store, e.chunks = chunks, e.n = a.n;
-    e.base = (long long)team.me * (REGS ? CH : chunks) * 32 * VEC + lane * VEC;
-
-    // logits, NaN as -inf, +inf as the largest finite float
-    auto clean = [](float v) { return fminf(fmaxf(v, neg_inf()), 3.402823466e38f); };
-    float m = neg_inf();
-    if (REGS) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const long long col = e.base + c * 32 * VEC;
-            float v[VEC];
-            if (a.aligned) {
-                load_cols<T, VEC>(x, col, a.n, neg_inf(), v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[i] = col + i < a.n ? to_float(x[col + i]) : neg_inf();
-            }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float f = clean(v[i]);
-                m = fmaxf(m, f);
-                e.r[c * VEC + i] = __float_as_uint(f);
-            }
-        }
-    } else {
-        e.each([&](unsigned int &v, int col) {
-            const float f = clean(to_float(x[col]));
-            m = fmaxf(m, f);
-            v = __float_as_uint(f);
-        });
-    }
-    m = team.max(m);
-    const float temperature = a.temperature ? a.temperature[row] : 1.0f;
-    const bool greedy = !(temperature > 0x1p-20f);
-    const float scale = __fdiv_rn(kLog2e, greedy ? 1.0f : temperature);
-    // no contraction of the subtraction and the product: each is rounded
-    auto weight = [&](float v) -> unsigned int {
-        return (unsigned int)(exp2f(__fmul_rn(__fsub_rn(v, m), scale)) * 0x1p31f);
-    };
-    int k = greedy ? 1 : (a.top_k ? a.top_k[row] : 0);
-    const bool none = m == neg_inf();
-
-    // top-k: cut_key = the k-th largest key; of its ties the first `ties` in index order stay. Hosts below m - 32 / c
-    // have weight 0: if at most k are above that, top-k changes nothing.
+    // top-k: cut_key = the k-th largest key; of its ties the first in index order stay. Hosts below m - 32 / c have
+    // weight 0: if at most k are above that, top-k changes nothing.
     unsigned int cut_key = 0;   // keys above it stay
     int tie_col = -1;           // and of the keys equal to it the columns up to this one
-    if (!none && k > 0 && k < a.n) {
-        auto above = [&](unsigned int key) -> u64 {
-            u64 c = 0, d = 0;
-            e.each([&](unsigned int &v, int) { c += key_of(__uint_as_float(v)) > key; });
-            team.sum2(c, d);
-            return c;
+    if (!p.none && p.k > 0 && p.k < e.n) {
+        const unsigned int k = (unsigned int)p.k;
+        auto above = [&](float x) -> unsigned int {
+            unsigned int c = 0;
+            e.each([&](unsigned int &v, int) { c += __uint_as_float(v) > x ? 1u : 0u; });
+            return team.count(c);
         };
-        float lo_f = __fsub_rn(m, __fdiv_rn(32.0f, scale)), hi_f = m;
-        unsigned int lo = key_of(lo_f), hi = key_of(m);
-        if (lo >= hi) lo = key_of(neg_inf());   // m so large that the distance vanishes
-        u64 above_lo = above(lo), above_hi = 0;
-        bool exact = above_lo <= (u64)k;
+        float lo_f = __fsub_rn(p.m, __fdiv_rn(32.0f, p.scale)), hi_f = p.m;
+        if (!(lo_f < hi_f)) lo_f = neg_inf();   // m so large that the distance vanishes
+        unsigned int lo = key_of(lo_f), hi = key_of(hi_f);
+        unsigned int above_hi = 0;
+        bool exact = above(lo_f) <= k;
         // invariant: above(hi) < k <= above(lo)
         for (int it = 0; !exact && hi - lo > 1; ++it) {
             unsigned int mid = lo + (hi - lo) / 2;
             if (it < 24) {   // halving the values converges faster than halving the keys at first
-                const float f = 0.5f * lo_f + 0.5f * hi_f;
-                const unsigned int g = key_of(f);
+                const unsigned int g = key_of(0.5f * lo_f + 0.5f * hi_f);
                 if (g > lo && g < hi) mid = g;
             }
-            const unsigned int b = mid & 0x80000000u ? mid ^ 0x80000000u : ~mid;
-            const u64 c = above(mid);
-            if (c >= (u64)k) {
-                lo = mid, lo_f = __uint_as_float(b), above_lo = c;
-                exact = c == (u64)k;
+            // no logit is -0: what lies above its key is what lies above the float before it
+            const float mid_f = __uint_as_float(mid & 0x80000000u ? mid ^ 0x80000000u : mid == 0x7FFFFFFFu ? 0x80000001u : ~mid);
+            const unsigned int c = above(mid_f);
+            if (c >= k) {
+                lo = mid, lo_f = mid_f;
+                exact = c == k;
             } else {
-                hi = mid, hi_f = __uint_as_float(b), above_hi = c;
+                hi = mid, hi_f = mid_f, above_hi = c;
             }
         }
         if (exact) {
             cut_key = lo;
         } else {
             cut_key = hi;
-            tie_col = nth_column(team, e, (u64)k - above_hi - 1, [&](unsigned int v, int) { return key_of(__uint_as_float(v)) == cut_key; });
+            tie_col = nth_column(team, e, k - above_hi - 1, [&](unsigned int v, int) { return key_of(__uint_as_float(v)) == cut_key; });
         }
     }
     // weights from here on
@@ -308,29 +322,39 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
     e.each([&](unsigned int &v, int col) {
         const float f = __uint_as_float(v);
         const unsigned int key = key_of(f);
-        v = !none && (key > cut_key || (key == cut_key && col <= tie_col)) ? weight(f) : 0u;
+        v = !p.none && (key > cut_key || (key == cut_key && col <= tie_col)) ? weight_of(f, p.m, p.scale) : 0u;
         total += v;
         count += v != 0;
     });
     team.sum2(total, count);
 
-    const float p = a.top_p ? a.top_p[row] : 1.0f;
-    if (p < 1.0f && !greedy && total > 0) {
-        const unsigned int steps = (unsigned int)(fmaxf(p, 0.0f) * 0x1p24f);
-        u64 limit = share_of(total, steps);
+    if (p.top_p < 1.0f && !p.greedy && total > 0) {
+        u64 limit = share_of(total, (unsigned int)(fmaxf(p.top_p, 0.0f) * 0x1p24f));
         if (limit == 0) limit = 1;
         // invariant: mass(w > hi) < limit <= mass(w > lo)
         unsigned int lo = 0, hi = 0x80000000u;
         u64 mass_hi = 0, count_hi = 0, count_lo = count;
+        // Weights below (total - limit) / n together hold less than what may be left out: the cut lies above them.
+        const u64 least = (total - limit) / (unsigned int)e.n;
+        bool first = least > 1;
         while (hi - lo > 1 && count_lo - count_hi > 1) {
             // halfway between the logarithms; at the ends of that, halfway between the values
             unsigned int mid = __float2uint_rd(__uint_as_float((__float_as_uint(__uint2float_rn(lo ? lo : 1)) + __float_as_uint(__uint2float_rn(hi))) / 2));
+            if (first) mid = (unsigned int)least - 1, first = false;
             if (mid <= lo || mid >= hi) mid = lo + (hi - lo) / 2;
             u64 mass = 0, c = 0;
-            e.each([&](unsigned int &v, int) {
-                if (v > mid) mass += v, ++c;
-            });
-            team.sum2(mass, c);
+            if constexpr (E::REGS) {
+                u64 both = 0;   // the number of weights above bit 44 rides along in the high word
+                e.each([&](unsigned int &v, int) {
+                    if (v > mid) both += (u64)v + (1ull << 44);
+                });
+                team.sum_packed(both, mass, c);
+            } else {
+                e.each([&](unsigned int &v, int) {
+                    if (v > mid) mass += v, ++c;
+                });
+                team.sum2(mass, c);
+            }
             if (mass < limit)
                 hi = mid, mass_hi = mass, count_hi = c;
             else
@@ -338,22 +362,22 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
         }
         // One host between the bounds: it is the one that reaches the limit, and stays. Else all of them have
         // weight hi and the first ceil((limit - mass_hi) / hi) in (x descending, index ascending) stay.
-        unsigned int cut = lo;   // weights above it stay
+        const unsigned int cut = lo;   // weights above it stay
         const u64 ties = count_lo - count_hi;
         if (ties > 1) {
             const u64 keep = (limit - mass_hi + hi - 1) / hi;
             if (keep < ties) {
                 // the ties' logits may still differ: bisection on their keys
-                auto key_at = [&](int col) { return key_of(clean(to_float(x[col]))); };
+                auto key_at = [&](int col) { return key_of(logit(col)); };
                 unsigned int klo = 0, khi = 0xFFFFFFFFu;   // above(khi) < keep <= above(klo) among the ties
                 u64 above_khi = 0, above_klo = ties;
                 while (khi - klo > 1 && above_klo > keep) {
                     const unsigned int mid = klo + (khi - klo) / 2;
-                    u64 c = 0, d = 0;
+                    unsigned int c = 0;
                     e.each([&](unsigned int &v, int col) {
-                        if (v == hi) c += key_at(col) > mid;
+                        if (v == hi) c += key_at(col) > mid ? 1u : 0u;
                     });
-                    team.sum2(c, d);
+                    c = team.count(c);
                     if (c >= keep)
                         klo = mid, above_klo = c;
                     else
@@ -376,47 +400,55 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
             if (v <= cut) v = 0;
         });
     }
-    const float min_p = a.min_p ? a.min_p[row] : 0.0f;
-    if (min_p > 0.0f) {
-        const unsigned int least = (unsigned int)(fminf(min_p, 1.0f) * 0x1p31f);
+    if (p.min_p > 0.0f) {
+        const unsigned int least = (unsigned int)(fminf(p.min_p, 1.0f) * 0x1p31f);
         e.each([&](unsigned int &v, int) {
             if (v < least) v = 0;
         });
     }
-    u64 mine = 0;
-    e.each([&](unsigned int &v, int) { mine += v; });
+
+    auto as_is = [](unsigned int v, int) -> u64 { return v; };
+    u64 sums[E::REGS ? E::CH : 1], mine = 0;   // the lane's weight in each chunk; the warp's
+    if constexpr (E::REGS) {
+#pragma unroll
+        for (int c = 0; c < E::CH; ++c) sums[c] = e.chunk_sum(c, as_is), mine += sums[c];
+    } else {
+        e.each([&](unsigned int &v, int) { mine += v; });
+    }
     mine = warp_sum(mine);
     int found = 0;
     for (int d = 0; d < a.draws; ++d) {
-        u64 before = 0, left = mine;
-        if (MULTI) {
-            const int now = team.exchange(mine, 0);
-            u64 all = 0;
-            for (int i = lane; i < team.warps; i += 32) {
-                const u64 v = team.slots[now][i].x;
-                all += v;
-                if (i < team.me) before += v;
-            }
-            left = warp_sum(all), before = warp_sum(before);
-        }
+        u64 before, left;
+        team.prefix(mine, before, left);
         int col = -1;
         if (left > 0) {
-            const float u = a.u[row * a.draws + d];
-            unsigned int steps = (unsigned int)(fminf(fmaxf(u, 0.0f), 1.0f) * 0x1p24f);
+            unsigned int steps = (unsigned int)(fminf(fmaxf(a.u[row * a.draws + d], 0.0f), 1.0f) * 0x1p24f);
             if (steps > 0xFFFFFFu) steps = 0xFFFFFFu;
             const u64 t = share_of(left, steps);
             const bool has = t >= before && t < before + mine;
-            u64 val = 0, where = 0;
+            u64 val = 0;
             if (has) {
-                e.find(t, before, lane, [](unsigned int v, int) -> u64 { return v; }, col, val);
+                if constexpr (E::REGS)
+                    e.find(t, before, lane, [&](int c) { return sums[c]; }, as_is, col, val);
+                else
+                    e.find(t, before, lane, [&](int c) { return e.chunk_sum(c, as_is); }, as_is, col, val);
                 mine -= val;
-                e.each([&](unsigned int &v, int at) {
-                    if (at == col) v = 0;
-                });
+                if (d + 1 < a.draws) {   // out of what is left
+                    e.each([&](unsigned int &v, int at) {
+                        if (at == col) v = 0;
+                    });
+                    if constexpr (E::REGS) {
+#pragma unroll
+                        for (int c = 0; c < E::CH; ++c) {
+                            const int off = col - e.base - c * 32 * E::VEC;
+                            if (off >= 0 && off < E::VEC) sums[c] -= val;
+                        }
+                    }
+                }
             }
-            where = (u64)(unsigned int)col;
+            u64 where = (u64)(unsigned int)col;
             team.tell(has, where, val);
-            col = (int)(unsigned int)where;
+            col = host((int)(unsigned int)where);
             ++found;
         }
         if (team.me == 0 && lane == 0) a.hosts[row * a.draws + d] = col;
@@ -424,27 +456,175 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
     if (a.found && team.me == 0 && lane == 0) a.found[row] = found;
 }
 
+constexpr int kList = 256;      // hosts a short list holds: 8 a lane of one warp
+constexpr int kListK = 128;     // largest top-k that tries for one
+struct ShortList {
+    float x[kList];
+    int col[kList];
+};
+
+// top-k of a long row leaves few hosts. A threshold that at least k of the lanes' chunk maxima exceed is exceeded by all
+// of the k best, and by not many others: those go, in index order, to a list that one warp finishes alone. Returns
+// the list's length, or -1 if it would be too long (many equal logits).
+template <bool MULTI, typename E>
+__device__ __forceinline__ int short_list(const Row &p, Team<MULTI> &team, E &e, ShortList *list)
+{
+    constexpr int VEC = E::VEC, CH = E::CH;
+    float top[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        top[c] = neg_inf();
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) top[c] = fmaxf(top[c], __uint_as_float(e.r[c * VEC + i]));
+    }
+    auto above = [&](float x) -> unsigned int {
+        unsigned int n = 0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) n += top[c] > x ? 1u : 0u;
+        return team.count(n);
+    };
+    const unsigned int k = (unsigned int)p.k;
+    float lo = __fsub_rn(p.m, __fdiv_rn(32.0f, p.scale)), hi = p.m;   // weights at and below lo are 0
+    if (!(lo < hi)) lo = neg_inf();
+    unsigned int n = above(lo);
+    for (int it = 0; it < 10 && n > k + k / 4 + 4; ++it) {
+        const float mid = 0.5f * lo + 0.5f * hi;
+        const unsigned int c = above(mid);
+        if (c >= k)
+            lo = mid, n = c;
+        else
+            hi = mid;
+    }
+    // where each chunk's hosts go: a field per chunk, wide enough for a warp's count in it (32 * VEC)
+    constexpr int F = VEC > 4 ? 16 : 8;
+    static_assert(CH * F <= 64, "a field per chunk");
+    u64 mine = 0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        unsigned int here = 0;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) here += __uint_as_float(e.r[c * VEC + i]) > lo ? 1u : 0u;
+        mine += (u64)here << (c * F);
+    }
+    const u64 incl = warp_scan(mine, team.lane), all = __shfl_sync(kFull, incl, 31), excl = incl - mine;
+    unsigned int total = 0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) total += (unsigned int)(all >> (c * F)) & ((1u << F) - 1u);
+    u64 before, length;
+    team.prefix(total, before, length);
+    if (length > kList) return -1;
+    ShortList *to = MULTI ? cluster_peer(list, 0, team.cs) : list;
+    unsigned int base = (unsigned int)before;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        unsigned int at = base + ((unsigned int)(excl >> (c * F)) & ((1u << F) - 1u));
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float x = __uint_as_float(e.r[c * VEC + i]);
+            if (x > lo) {
+                to->x[at] = x;
+                to->col[at] = e.base + c * 32 * VEC + i;
+                ++at;
+            }
+        }
+        base += (unsigned int)(all >> (c * F)) & ((1u << F) - 1u);
+    }
+    return (int)length;
+}
+
+template <typename T, int CH, bool MULTI, bool REGS>
+__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team<MULTI> team, ShortList *list, unsigned int *store, int chunks)
+{
+    constexpr int VEC = kPer16<T>;
+    const T *x = static_cast<const T *>(a.x) + row * a.stride;
+    const int lane = team.lane;
+    Elems<VEC, CH, REGS> e;
+    e.store = store, e.chunks = chunks, e.n = a.n;
+    e.base = team.me * (REGS ? CH : chunks) * 32 * VEC + lane * VEC;
+    Row p;
+    const float temperature = a.temperature ? a.temperature[row] : 1.0f;
+    p.greedy = !(temperature > 0x1p-20f);
+    p.scale = __fdiv_rn(kLog2e, p.greedy ? 1.0f : temperature);
+    p.k = p.greedy ? 1 : (a.top_k ? a.top_k[row] : 0);
+    p.top_p = a.top_p ? a.top_p[row] : 1.0f;
+    p.min_p = a.min_p ? a.min_p[row] : 0.0f;
+
+    float m = neg_inf();
+    if constexpr (REGS) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = e.base + c * 32 * VEC;
+            float v[VEC];
+            if (a.aligned) {
+                load_cols<T, VEC>(x, col, a.n, neg_inf(), v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = col + i < a.n ? to_float(x[col + i]) : neg_inf();
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float f = clean(v[i]);
+                m = fmaxf(m, f);
+                e.r[c * VEC + i] = __float_as_uint(f);
+            }
+        }
+    } else {
+        e.each([&](unsigned int &v, int col) {
+            const float f = clean(to_float(x[col]));
+            m = fmaxf(m, f);
+            v = __float_as_uint(f);
+        });
+    }
+    p.m = team.max(m);
+    p.none = p.m == neg_inf();
+    if constexpr (REGS && CH > 1) {
+        if (!p.none && p.k > 0 && p.k <= kListK && p.k < a.n) {
+            const int length = short_list(p, team, e, list);
+            if (length >= 0) {
+                if (MULTI)
+                    cluster_sync(team.cs);
+                else
+                    __syncwarp();
+                if (team.me != 0) return;
+                Team<false> one{nullptr, 1, 1, 0, lane, 0};
+                Elems<8, kList / 256, true> f;
+                f.store = nullptr, f.chunks = kList / 256, f.n = length, f.base = lane * 8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    f.r[i] = __float_as_uint(lane * 8 + i < length ? list->x[lane * 8 + i] : neg_inf());
+                decide(a, row, p, one, f, [&](int col) { return list->x[col]; }, [&](int col) { return list->col[col]; });
+                return;
+            }
+        }
+    }
+    decide(a, row, p, team, e, [&](int col) { return clean(to_float(x[col])); }, [](int col) { return col; });
+}
+
 template <typename T, int CH>
 __global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a)
 {
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    __shared__ ShortList s_list[CH > 1 ? 4 : 1];
+    const int warp = threadIdx.x >> 5;
+    const long long row = (long long)blockIdx.x * 4 + warp;
     if (row >= a.rows) return;
     Team<false> team{nullptr, 1, 1, 0, (int)(threadIdx.x & 31), 0};
-    sample_row<T, CH, false, true>(a, row, team, nullptr, CH);
+    sample_row<T, CH, false, true>(a, row, team, &s_list[CH > 1 ? warp : 0], nullptr, CH);
 }
 
 // grid: REGS one block / cluster per row; else `clusters` of them take the rows in turn
-template <typename T, bool REGS>
-__global__ void __launch_bounds__(1024, 1) sample_block_kernel(SampleArgs a, int cs, int chunks)
+// THREADS: most threads of a block; blocks of up to 256 get more registers than 1,024 threads leave
+template <typename T, bool REGS, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 3) sample_block_kernel(SampleArgs a, int cs, int chunks)
 {
     __shared__ ulonglong2 s_slots[2][kMaxCluster * 32];
+    __shared__ ShortList s_list;
     const int rank = cluster_rank(cs), warps = blockDim.x >> 5;
     Team<true> team{s_slots, warps * cs, cs, rank * warps + (int)(threadIdx.x >> 5), (int)(threadIdx.x & 31), 0};
     cluster_sync(cs);   // all blocks of the cluster run
     const long long first = blockIdx.x / cs, step = gridDim.x / cs;
     for (long long row = first; row < a.rows; row += step) {
-        sample_row<T, kElems / kPer16<T>, true, REGS>(a, row, team, REGS ? nullptr : a.store + first * a.n, chunks);
-        cluster_sync(cs);   // slots are free again
+        sample_row<T, kElems / kPer16<T>, true, REGS>(a, row, team, &s_list, REGS ? nullptr : a.store + first * a.n, chunks);
+        cluster_sync(cs);   // slots and list are free again
     }
 }
 
@@ -487,8 +667,9 @@ cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = regs ? cudaLaunchKernelEx(&cfg, sample_block_kernel<T, true>, a, cs, chunks)
-                               : cudaLaunchKernelEx(&cfg, sample_block_kernel<T, false>, a, cs, chunks);
+    const cudaError_t e = !regs           ? cudaLaunchKernelEx(&cfg, sample_block_kernel<T, false, 1024>, a, cs, chunks)
+                          : threads > 256 ? cudaLaunchKernelEx(&cfg, sample_block_kernel<T, true, 1024>, a, cs, chunks)
+                                          : cudaLaunchKernelEx(&cfg, sample_block_kernel<T, true, 256>, a, cs, chunks);
     if (store) cudaFreeAsync(store, stream);
     return e;
 }

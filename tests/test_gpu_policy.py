@@ -369,6 +369,7 @@ def test_sample_matches_the_checker_exactly(nb, rows, n, dtype):
         v = -rng.integers(0, depth, size=(rows, n)).astype(np.float64) + rng.integers(-30, 30, size=(rows, 1))
         v[rng.random((rows, n)) < 0.1] = -INF
         v[rng.random((rows, n)) < 0.02] = math.nan
+        v[v == 0] = rng.choice([0.0, -0.0], int((v == 0).sum()))     # equal logits, whatever their sign
         v[0] = -INF
         buf = torch.full((rows * (n + pad) + shift,), 99.0, dtype=getattr(torch, dtype), device="cuda")
         x = buf[shift:].view(rows, n + pad)[:, :n]
