@@ -41,8 +41,13 @@ __device__ __forceinline__ unsigned int key_of(float x)
     return b ^ ((unsigned int)((int)b >> 31) | 0x80000000u);
 }
 
-// logits, NaN as -inf, +inf as the largest finite float, -0 as 0 (equal logits have equal keys)
-__device__ __forceinline__ float clean(float v) { return fminf(fmaxf(v, neg_inf()), 3.402823466e38f) + 0.0f; }
+__device__ __forceinline__ float float_of(unsigned int key)
+{
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+// +inf counts as the largest finite float
+constexpr float kMaxFinite = 3.402823466e38f;
 
 // floor(2^31 * 2^((x - m) scale)): difference and product are rounded one by one (no contraction). The power is at
 // most 1, so its significand shifted by its exponent is the whole number; below 2^-31 nothing is left.
@@ -53,6 +58,17 @@ __device__ __forceinline__ unsigned int weight_of(float x, float m, float scale)
     const unsigned int b = __float_as_uint(e), shift = 127u - (b >> 23);
     const unsigned int w = (b << 8) | 0x80000000u;
     return shift < 32u ? w >> shift : 0u;
+}
+
+// sum += w + 2^44 if w > t: a sum of weights with their number above it, in three instructions
+__device__ __forceinline__ void add_above(unsigned int &lo, unsigned int &hi, unsigned int w, unsigned int t)
+{
+    asm("{\n\t.reg .pred p;\n\t"
+        "setp.gt.u32 p, %2, %3;\n\t"
+        "@p add.cc.u32 %0, %0, %2;\n\t"
+        "@p addc.u32 %1, %1, 4096;\n\t}"
+        : "+r"(lo), "+r"(hi)
+        : "r"(w), "r"(t));
 }
 
 // sum over the warp of values below 2^52, by two 26-bit halves
@@ -67,6 +83,16 @@ __device__ __forceinline__ u64 warp_scan(u64 v, int lane)   // inclusive
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
         const u64 other = __shfl_up_sync(kFull, v, off);
+        if (lane >= off) v += other;
+    }
+    return v;
+}
+
+__device__ __forceinline__ unsigned int warp_scan32(unsigned int v, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const unsigned int other = __shfl_up_sync(kFull, v, off);
         if (lane >= off) v += other;
     }
     return v;
@@ -133,6 +159,15 @@ struct Team {
         v = neg_inf();
         for (int i = lane; i < warps; i += 32) v = fmaxf(v, __uint_as_float((unsigned int)slots[now][i].x));
         return lanes_max(v, 32);
+    }
+    __device__ __forceinline__ unsigned int max_key(unsigned int v)
+    {
+        v = __reduce_max_sync(kFull, v);
+        if (!MULTI) return v;
+        const int now = exchange(v, 0);
+        v = 0;
+        for (int i = lane; i < warps; i += 32) v = ::max(v, (unsigned int)slots[now][i].x);
+        return __reduce_max_sync(kFull, v);
     }
     // sums of `mine`, which the lanes of a warp agree on: over the warps before this one, and over all
     __device__ __forceinline__ void prefix(u64 mine, u64 &before, u64 &all)
@@ -272,15 +307,112 @@ struct Row {
     bool greedy, none;
 };
 
+constexpr int kSort = 64;   // weights that one warp sorts, two a lane
+
+// descending over (a of lane 0 .. 31, b of lane 0 .. 31), a bitonic network
+__device__ __forceinline__ void sort64(unsigned int &a, unsigned int &b, int lane)
+{
+#pragma unroll
+    for (int k = 2; k <= 64; k *= 2)
+#pragma unroll
+        for (int j = k / 2; j > 0; j /= 2) {
+            if (j == 32) {
+                const unsigned int hi = max(a, b), lo = min(a, b);
+                a = hi, b = lo;
+            } else {
+                const unsigned int oa = __shfl_xor_sync(kFull, a, j), ob = __shfl_xor_sync(kFull, b, j);
+                const bool first = (lane & j) == 0;
+                const bool max_a = ((lane & k) == 0) == first;                 // elements lane and lane + 32
+                const bool max_b = (((lane + 32) & k) == 0) == first;
+                a = max_a ? max(a, oa) : min(a, oa);
+                b = max_b ? max(b, ob) : min(b, ob);
+            }
+        }
+}
+
+// The weight at which the running sum of weights, in descending order, reaches `limit`; the sum of those above it and
+// how many have just it. Bisection (on the logarithm at first, with the bounds moved onto weights that
+// occur every few steps) until at most 64 weights are left between the bounds, which one warp then sorts.
+template <bool MULTI, typename E>
+__device__ __forceinline__ void nucleus(Team<MULTI> &team, E &e, u64 limit, u64 total, u64 count, unsigned int *sort_list,
+                                        unsigned int &cut, u64 &mass_above, u64 &ties)
+{
+    // invariant: mass(w > hi) < limit <= mass(w > lo)
+    unsigned int lo = 0, hi = 0x80000000u;
+    u64 mass_hi = 0, count_hi = 0, count_lo = count;
+    // Weights below (total - limit) / n together hold less than what may be left out: the cut lies above them.
+    const u64 least = (total - limit) / (unsigned int)e.n;
+    for (int it = 0; hi - lo > 1 && count_lo - count_hi > kSort; ++it) {
+        if ((it & 3) == 3) {
+            unsigned int most = 0, least_in = 0xFFFFFFFFu;
+            e.each([&](unsigned int &v, int) {
+                if (v <= hi) most = max(most, v);
+                if (v > lo) least_in = min(least_in, v);
+            });
+            hi = team.max_key(most), lo = ~team.max_key(~least_in) - 1;
+            if (hi - lo <= 1) break;
+        }
+        unsigned int mid = __float2uint_rd(__uint_as_float((__float_as_uint(__uint2float_rn(lo ? lo : 1)) + __float_as_uint(__uint2float_rn(hi))) / 2));
+        if (it == 0 && least > 1) mid = (unsigned int)least - 1;
+        if (mid <= lo || mid >= hi) mid = lo + (hi - lo) / 2;
+        u64 mass = 0, c = 0;
+        if constexpr (E::REGS) {
+            unsigned int sum_lo = 0, sum_hi = 0;
+            e.each([&](unsigned int &v, int) { add_above(sum_lo, sum_hi, v, mid); });
+            team.sum_packed(((u64)sum_hi << 32) | sum_lo, mass, c);
+        } else {
+            e.each([&](unsigned int &v, int) {
+                if (v > mid) mass += v, ++c;
+            });
+            team.sum2(mass, c);
+        }
+        if (mass < limit)
+            hi = mid, mass_hi = mass, count_hi = c;
+        else
+            lo = mid, count_lo = c;
+    }
+    cut = hi, mass_above = mass_hi, ties = count_lo - count_hi;
+    if (hi - lo <= 1) return;
+    unsigned int here = 0;
+    e.each([&](unsigned int &v, int) { here += v - lo - 1 < hi - lo ? 1u : 0u; });
+    const unsigned int incl = warp_scan32(here, team.lane);
+    u64 before, all;
+    team.prefix(__shfl_sync(kFull, incl, 31), before, all);
+    unsigned int *to = MULTI ? cluster_peer(sort_list, 0, team.cs) : sort_list;
+    unsigned int at = (unsigned int)before + incl - here;
+    e.each([&](unsigned int &v, int) {
+        if (v - lo - 1 < hi - lo) to[at++] = v;
+    });
+    if (MULTI)
+        cluster_sync(team.cs);
+    else
+        __syncwarp();
+    u64 packed = 0;
+    if (team.me == 0) {
+        unsigned int a = team.lane < (int)all ? sort_list[team.lane] : 0u, b = team.lane + 32 < (int)all ? sort_list[team.lane + 32] : 0u;
+        sort64(a, b, team.lane);
+        const u64 run_a = mass_hi + warp_scan(a, team.lane);
+        const u64 run_b = __shfl_sync(kFull, run_a, 31) + warp_scan(b, team.lane);
+        const unsigned int in_a = __ballot_sync(kFull, run_a >= limit), in_b = __ballot_sync(kFull, run_b >= limit);
+        cut = in_a ? __shfl_sync(kFull, a, __ffs(in_a) - 1) : __shfl_sync(kFull, b, __ffs(in_b) - 1);
+        mass_above = mass_hi + warp_sum((u64)(a > cut ? a : 0u) + (b > cut ? b : 0u));
+        packed = ((u64)__reduce_add_sync(kFull, (a == cut ? 1u : 0u) + (b == cut ? 1u : 0u)) << 32) | cut;
+    }
+    team.tell(team.me == 0, mass_above, packed);
+    cut = (unsigned int)packed, ties = packed >> 32;
+    if (!MULTI) __syncwarp();   // the list may be written again
+}
+
 // Filters and draws. e holds logits (as bits); logit(col) reads one again, host(col) names the column's host.
 template <bool MULTI, typename E, typename X, typename H>
-__device__ __forceinline__ void decide(const SampleArgs &a, long long row, const Row &p, Team<MULTI> &team, E &e, X logit, H host)
+__device__ __forceinline__ void decide(const SampleArgs &a, long long row, const Row &p, Team<MULTI> &team, E &e,
+                                       unsigned int *sort_list, X logit, H host)
 {
     const int lane = team.lane;
-    // top-k: cut_key = the k-th largest key; of its ties the first in index order stay. Hosts below m - 32 / c have
+    // top-k: cut_x = the k-th largest logit; of its ties the first in index order stay. Hosts below m - 32 / c have
     // weight 0: if at most k are above that, top-k changes nothing.
-    unsigned int cut_key = 0;   // keys above it stay
-    int tie_col = -1;           // and of the keys equal to it the columns up to this one
+    float cut_x = neg_inf();    // logits above it stay
+    int tie_col = -1;           // and of those equal to it the columns up to this one
     if (!p.none && p.k > 0 && p.k < e.n) {
         const unsigned int k = (unsigned int)p.k;
         auto above = [&](float x) -> unsigned int {
@@ -294,14 +426,25 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         unsigned int above_hi = 0;
         bool exact = above(lo_f) <= k;
         // invariant: above(hi) < k <= above(lo)
-        for (int it = 0; !exact && hi - lo > 1; ++it) {
+        for (int it = 1; !exact && hi - lo > 1; ++it) {
+            if ((it & 3) == 0) {   // the bounds onto logits that occur
+                float most = neg_inf();
+                unsigned int least = 0xFFFFFFFFu;
+                e.each([&](unsigned int &v, int) {
+                    const float x = __uint_as_float(v);
+                    if (x <= hi_f) most = fmaxf(most, x);
+                    if (x > lo_f) least = min(least, key_of(x + 0.0f));   // + 0: one zero
+                });
+                hi_f = team.max(most), hi = key_of(hi_f + 0.0f);
+                lo = ~team.max_key(~least) - 1, lo_f = float_of(lo);
+                if (hi - lo <= 1) break;
+            }
             unsigned int mid = lo + (hi - lo) / 2;
             if (it < 24) {   // halving the values converges faster than halving the keys at first
                 const unsigned int g = key_of(0.5f * lo_f + 0.5f * hi_f);
                 if (g > lo && g < hi) mid = g;
             }
-            // no logit is -0: what lies above its key is what lies above the float before it
-            const float mid_f = __uint_as_float(mid & 0x80000000u ? mid ^ 0x80000000u : mid == 0x7FFFFFFFu ? 0x80000001u : ~mid);
+            const float mid_f = float_of(mid);
             const unsigned int c = above(mid_f);
             if (c >= k) {
                 lo = mid, lo_f = mid_f;
@@ -311,101 +454,78 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
             }
         }
         if (exact) {
-            cut_key = lo;
+            cut_x = lo_f;
         } else {
-            cut_key = hi;
-            tie_col = nth_column(team, e, k - above_hi - 1, [&](unsigned int v, int) { return key_of(__uint_as_float(v)) == cut_key; });
+            cut_x = hi_f;
+            tie_col = nth_column(team, e, k - above_hi - 1, [&](unsigned int v, int) { return __uint_as_float(v) == cut_x; });
         }
     }
     // weights from here on
     u64 total = 0, count = 0;
-    e.each([&](unsigned int &v, int col) {
-        const float f = __uint_as_float(v);
-        const unsigned int key = key_of(f);
-        v = !p.none && (key > cut_key || (key == cut_key && col <= tie_col)) ? weight_of(f, p.m, p.scale) : 0u;
-        total += v;
-        count += v != 0;
-    });
-    team.sum2(total, count);
+    if constexpr (E::REGS) {
+        unsigned int sum_lo = 0, sum_hi = 0;
+        e.each([&](unsigned int &v, int col) {
+            const float f = __uint_as_float(v);
+            v = f > cut_x || (f == cut_x && col <= tie_col) ? weight_of(f, p.m, p.scale) : 0u;
+            add_above(sum_lo, sum_hi, v, 0u);
+        });
+        total = ((u64)sum_hi << 32) | sum_lo;
+        if (p.top_p < 1.0f) team.sum_packed(total, total, count);
+    } else {
+        e.each([&](unsigned int &v, int col) {
+            const float f = __uint_as_float(v);
+            v = f > cut_x || (f == cut_x && col <= tie_col) ? weight_of(f, p.m, p.scale) : 0u;
+            total += v;
+            count += v != 0;
+        });
+        if (p.top_p < 1.0f) team.sum2(total, count);
+    }
 
+    unsigned int least = 0;   // weights below it go
+    if (p.min_p > 0.0f) least = (unsigned int)(fminf(p.min_p, 1.0f) * 0x1p31f);
     if (p.top_p < 1.0f && !p.greedy && total > 0) {
         u64 limit = share_of(total, (unsigned int)(fmaxf(p.top_p, 0.0f) * 0x1p24f));
         if (limit == 0) limit = 1;
-        // invariant: mass(w > hi) < limit <= mass(w > lo)
-        unsigned int lo = 0, hi = 0x80000000u;
-        u64 mass_hi = 0, count_hi = 0, count_lo = count;
-        // Weights below (total - limit) / n together hold less than what may be left out: the cut lies above them.
-        const u64 least = (total - limit) / (unsigned int)e.n;
-        bool first = least > 1;
-        while (hi - lo > 1 && count_lo - count_hi > 1) {
-            // halfway between the logarithms; at the ends of that, halfway between the values
-            unsigned int mid = __float2uint_rd(__uint_as_float((__float_as_uint(__uint2float_rn(lo ? lo : 1)) + __float_as_uint(__uint2float_rn(hi))) / 2));
-            if (first) mid = (unsigned int)least - 1, first = false;
-            if (mid <= lo || mid >= hi) mid = lo + (hi - lo) / 2;
-            u64 mass = 0, c = 0;
-            if constexpr (E::REGS) {
-                u64 both = 0;   // the number of weights above bit 44 rides along in the high word
-                e.each([&](unsigned int &v, int) {
-                    if (v > mid) both += (u64)v + (1ull << 44);
-                });
-                team.sum_packed(both, mass, c);
-            } else {
-                e.each([&](unsigned int &v, int) {
-                    if (v > mid) mass += v, ++c;
-                });
-                team.sum2(mass, c);
-            }
-            if (mass < limit)
-                hi = mid, mass_hi = mass, count_hi = c;
-            else
-                lo = mid, count_lo = c;
-        }
-        // One host between the bounds: it is the one that reaches the limit, and stays. Else all of them have
-        // weight hi and the first ceil((limit - mass_hi) / hi) in (x descending, index ascending) stay.
-        const unsigned int cut = lo;   // weights above it stay
-        const u64 ties = count_lo - count_hi;
-        if (ties > 1) {
-            const u64 keep = (limit - mass_hi + hi - 1) / hi;
-            if (keep < ties) {
-                // the ties' logits may still differ: bisection on their keys
-                auto key_at = [&](int col) { return key_of(logit(col)); };
-                unsigned int klo = 0, khi = 0xFFFFFFFFu;   // above(khi) < keep <= above(klo) among the ties
-                u64 above_khi = 0, above_klo = ties;
-                while (khi - klo > 1 && above_klo > keep) {
-                    const unsigned int mid = klo + (khi - klo) / 2;
-                    unsigned int c = 0;
-                    e.each([&](unsigned int &v, int col) {
-                        if (v == hi) c += key_at(col) > mid ? 1u : 0u;
-                    });
-                    c = team.count(c);
-                    if (c >= keep)
-                        klo = mid, above_klo = c;
-                    else
-                        khi = mid, above_khi = c;
-                }
-                unsigned int kcut = klo;
-                int kcol = -1;
-                if (above_klo > keep) {
-                    kcut = khi;
-                    kcol = nth_column(team, e, keep - above_khi - 1, [&](unsigned int v, int col) { return v == hi && key_at(col) == kcut; });
-                }
+        unsigned int cut;
+        u64 mass_above, ties;
+        nucleus(team, e, limit, total, count, sort_list, cut, mass_above, ties);
+        least = max(least, cut);
+        // the first ceil((limit - mass_above) / cut) of the ties in (x descending, index ascending) stay
+        const u64 keep = (limit - mass_above + cut - 1) / cut;
+        if (keep < ties && least == cut) {
+            // the ties' logits may still differ: bisection on their keys
+            auto key_at = [&](int col) { return key_of(fminf(logit(col), kMaxFinite) + 0.0f); };
+            unsigned int klo = 0, khi = 0xFFFFFFFFu;   // above(khi) < keep <= above(klo) among the ties
+            u64 above_khi = 0, above_klo = ties;
+            while (khi - klo > 1 && above_klo > keep) {
+                const unsigned int mid = klo + (khi - klo) / 2;
+                unsigned int c = 0;
                 e.each([&](unsigned int &v, int col) {
-                    if (v != hi) return;
-                    const unsigned int key = key_at(col);
-                    if (!(key > kcut || (key == kcut && col <= kcol))) v = 0;
+                    if (v == cut) c += key_at(col) > mid ? 1u : 0u;
                 });
+                c = team.count(c);
+                if (c >= keep)
+                    klo = mid, above_klo = c;
+                else
+                    khi = mid, above_khi = c;
             }
+            unsigned int kcut = klo;
+            int kcol = -1;
+            if (above_klo > keep) {
+                kcut = khi;
+                kcol = nth_column(team, e, keep - above_khi - 1, [&](unsigned int v, int col) { return v == cut && key_at(col) == kcut; });
+            }
+            e.each([&](unsigned int &v, int col) {
+                if (v != cut) return;
+                const unsigned int key = key_at(col);
+                if (!(key > kcut || (key == kcut && col <= kcol))) v = 0;
+            });
         }
-        e.each([&](unsigned int &v, int) {
-            if (v <= cut) v = 0;
-        });
     }
-    if (p.min_p > 0.0f) {
-        const unsigned int least = (unsigned int)(fminf(p.min_p, 1.0f) * 0x1p31f);
+    if (least > 0)
         e.each([&](unsigned int &v, int) {
             if (v < least) v = 0;
         });
-    }
 
     auto as_is = [](unsigned int v, int) -> u64 { return v; };
     u64 sums[E::REGS ? E::CH : 1], mine = 0;   // the lane's weight in each chunk; the warp's
@@ -459,6 +579,7 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
 constexpr int kList = 256;      // hosts a short list holds: 8 a lane of one warp
 constexpr int kListK = 128;     // largest top-k that tries for one
 struct ShortList {
+    unsigned int sort[kSort];
     float x[kList];
     int col[kList];
 };
@@ -563,19 +684,24 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
             }
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float f = clean(v[i]);
-                m = fmaxf(m, f);
-                e.r[c * VEC + i] = __float_as_uint(f);
+                m = fmaxf(m, v[i]);   // a NaN is never the larger, nor above any bound, and has weight 0
+                e.r[c * VEC + i] = __float_as_uint(v[i]);
             }
         }
     } else {
         e.each([&](unsigned int &v, int col) {
-            const float f = clean(to_float(x[col]));
+            const float f = to_float(x[col]);
             m = fmaxf(m, f);
             v = __float_as_uint(f);
         });
     }
     p.m = team.max(m);
+    if (p.m > kMaxFinite) {
+        p.m = kMaxFinite;
+        e.each([&](unsigned int &v, int) {
+            if (v == 0x7F800000u) v = __float_as_uint(kMaxFinite);
+        });
+    }
     p.none = p.m == neg_inf();
     if constexpr (REGS && CH > 1) {
         if (!p.none && p.k > 0 && p.k <= kListK && p.k < a.n) {
@@ -592,23 +718,23 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     f.r[i] = __float_as_uint(lane * 8 + i < length ? list->x[lane * 8 + i] : neg_inf());
-                decide(a, row, p, one, f, [&](int col) { return list->x[col]; }, [&](int col) { return list->col[col]; });
+                decide(a, row, p, one, f, list->sort, [&](int col) { return list->x[col]; }, [&](int col) { return list->col[col]; });
                 return;
             }
         }
     }
-    decide(a, row, p, team, e, [&](int col) { return clean(to_float(x[col])); }, [](int col) { return col; });
+    decide(a, row, p, team, e, list->sort, [&](int col) { return to_float(x[col]); }, [](int col) { return col; });
 }
 
 template <typename T, int CH>
 __global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a)
 {
-    __shared__ ShortList s_list[CH > 1 ? 4 : 1];
+    __shared__ ShortList s_list[4];
     const int warp = threadIdx.x >> 5;
     const long long row = (long long)blockIdx.x * 4 + warp;
     if (row >= a.rows) return;
     Team<false> team{nullptr, 1, 1, 0, (int)(threadIdx.x & 31), 0};
-    sample_row<T, CH, false, true>(a, row, team, &s_list[CH > 1 ? warp : 0], nullptr, CH);
+    sample_row<T, CH, false, true>(a, row, team, &s_list[warp], nullptr, CH);
 }
 
 // grid: REGS one block / cluster per row; else `clusters` of them take the rows in turn
