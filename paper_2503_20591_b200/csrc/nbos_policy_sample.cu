@@ -495,7 +495,15 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         if (keep < ties && least == cut) {
             // the ties' logits may still differ: bisection on their keys
             auto key_at = [&](int col) { return key_of(fminf(logit(col), kMaxFinite) + 0.0f); };
-            unsigned int klo = 0, khi = 0xFFFFFFFFu;   // above(khi) < keep <= above(klo) among the ties
+            unsigned int least_key = 0xFFFFFFFFu, most_key = 0;
+            e.each([&](unsigned int &v, int col) {
+                if (v == cut) {
+                    const unsigned int key = key_at(col);
+                    least_key = min(least_key, key), most_key = max(most_key, key);
+                }
+            });
+            // above(khi) < keep <= above(klo) among the ties
+            unsigned int klo = ~team.max_key(~least_key) - 1, khi = team.max_key(most_key);
             u64 above_khi = 0, above_klo = ties;
             while (khi - klo > 1 && above_klo > keep) {
                 const unsigned int mid = klo + (khi - klo) / 2;
