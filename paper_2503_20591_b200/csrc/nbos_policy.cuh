@@ -74,6 +74,25 @@ __device__ __forceinline__ uint4 pack16(const float (&v)[8], __half)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// four neighbours that start on a boundary of four elements
+__device__ __forceinline__ void load4(const float *p, float (&v)[4])
+{
+    const float4 f = __ldcs(reinterpret_cast<const float4 *>(p));
+    v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&v)[4])
+{
+    const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p));
+    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void load4(const __half *p, float (&v)[4])
+{
+    const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p));
+    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&u.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&u.y));
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+
 // VEC consecutive elements of a row from column `col`; columns from `end` on read as `fill`. VEC is 16 bytes'
 // worth (the row then starts on a 16-byte boundary and col is a multiple of VEC) or 1 (any alignment).
 // Loads are plain (not through the read-only path): the gradient may be written over the logits.

@@ -3,12 +3,16 @@
 // Weights are whole numbers, w = floor(2^31 * 2^((x - m) c)), c = log2(e) / T: every sum of them is exact, so the
 // split of a row over lanes, warps and blocks cannot change which host a random number selects. top-k, top-p and
 // min-p each keep a first part of the order (x descending, index ascending); the draw runs in index order over what
-// is left, so nothing has to be sorted: top-k finds its last value by bisection on counts, top-p on exact sums.
-// A team of warps shares a row: one warp up to 1,024 hosts, a block up to 32,768, a cluster of up to 8 blocks up to
-// 262,144. Each lane holds 32 elements in registers, as logits until the top-k cut is known and as weights from
-// then on, so the logits are read once. Longer rows keep their elements in the workspace instead.
-// A warp's columns are one stretch of the row and a lane's 16 bytes of it are neighbours, so index order is
-// warp, then 16-byte chunk, then lane.
+// is left, so nothing long has to be sorted: cuts are found by bisection on counts (top-k) and exact sums (top-p)
+// until a short list is left that one warp finishes.
+// A team of warps shares a row, 1,024 hosts each: one warp, a block (up to 32,768 hosts), a cluster of up to 8 blocks
+// (262,144). The logits are read once and stay in shared memory, as logits until the top-k cut is known and as
+// weights from then on. The work is some 20 passes of a few integer instructions over them, which is what bounds
+// it; loops over shared memory keep the code short (unrolled over registers it did not fit the instruction
+// cache) and the registers few, so that many rows are in flight. Longer rows keep their elements in the
+// workspace instead.
+// A warp's columns are one stretch of the row, a lane's four of each 128 are neighbours: index order is warp, then
+// chunk of 128, then lane.
 #include <math.h>
 
 #include "nbos_policy.cuh"
@@ -18,9 +22,14 @@ namespace {
 
 using namespace policy;
 
-constexpr int kElems = 32;
+constexpr int kChunk = 128;            // columns a warp takes at once, four a lane
+constexpr int kWarpChunks = 8;         // chunks of a warp, except of rows in the workspace
+constexpr int kWarpRow = kChunk * kWarpChunks;
 constexpr int kMaxCluster = 8;
-constexpr int kBlockRow = 1024 * kElems;
+constexpr int kBlockRow = 32 * kWarpRow;
+constexpr int kSort = 64;              // weights that one warp sorts, two a lane
+constexpr int kList = 256;             // hosts of the list that top-k leaves
+constexpr int kListK = 192;            // largest top-k that tries for one
 typedef unsigned long long u64;
 
 struct SampleArgs {
@@ -31,7 +40,7 @@ struct SampleArgs {
     const int32_t *top_k;
     const float *top_p, *min_p;
     int32_t *hosts, *found;
-    unsigned int *store;   // rows longer than the registers of a cluster: [clusters][n]
+    unsigned int *store;   // rows longer than the shared memory of a cluster: [clusters][n padded]
 };
 
 // floats in the order of unsigned integers
@@ -40,7 +49,6 @@ __device__ __forceinline__ unsigned int key_of(float x)
     const unsigned int b = __float_as_uint(x);
     return b ^ ((unsigned int)((int)b >> 31) | 0x80000000u);
 }
-
 __device__ __forceinline__ float float_of(unsigned int key)
 {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
@@ -50,7 +58,7 @@ __device__ __forceinline__ float float_of(unsigned int key)
 constexpr float kMaxFinite = 3.402823466e38f;
 
 // floor(2^31 * 2^((x - m) scale)): difference and product are rounded one by one (no contraction). The power is at
-// most 1, so its significand shifted by its exponent is the whole number; below 2^-31 nothing is left.
+// most 1, so its significand shifted by its exponent is the whole number; below 2^-31, and for NaN, it is 0.
 __device__ __forceinline__ unsigned int weight_of(float x, float m, float scale)
 {
     float e;
@@ -78,21 +86,12 @@ __device__ __forceinline__ u64 warp_sum(u64 v)
     const unsigned int hi = __reduce_add_sync(kFull, (unsigned int)(v >> 26));
     return ((u64)hi << 26) + lo;
 }
-__device__ __forceinline__ u64 warp_scan(u64 v, int lane)   // inclusive
+template <typename V>
+__device__ __forceinline__ V warp_scan(V v, int lane)   // inclusive
 {
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const u64 other = __shfl_up_sync(kFull, v, off);
-        if (lane >= off) v += other;
-    }
-    return v;
-}
-
-__device__ __forceinline__ unsigned int warp_scan32(unsigned int v, int lane)
-{
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const unsigned int other = __shfl_up_sync(kFull, v, off);
+        const V other = __shfl_up_sync(kFull, v, off);
         if (lane >= off) v += other;
     }
     return v;
@@ -104,12 +103,19 @@ __device__ __forceinline__ u64 share_of(u64 total, unsigned int steps)
     return (u64)steps * (total >> 24) + (((u64)steps * (total & 0xFFFFFFu)) >> 24);
 }
 
-// The warps that share a row. MULTI = false: one warp, no shared memory.
-template <bool MULTI>
+// The warps that share a row (one warp: nothing is exchanged).
 struct Team {
     ulonglong2 (*slots)[kMaxCluster * 32];   // two sets, taken in turn
     int warps, cs, me, lane, turn;           // me: this warp's place among all of the row
 
+    __device__ __forceinline__ bool alone() const { return warps == 1; }
+    __device__ __forceinline__ void sync() const
+    {
+        if (alone())
+            __syncwarp();
+        else
+            cluster_sync(cs);
+    }
     // every warp's (a, b), which the lanes of a warp agree on, to every warp, in slots[result]
     __device__ __forceinline__ int exchange(u64 a, u64 b)
     {
@@ -119,61 +125,53 @@ struct Team {
         turn ^= 1;
         return now;
     }
-    __device__ __forceinline__ void sum2(u64 &a, u64 &b)
+    // mass and number over the row, from a lane's own
+    __device__ __forceinline__ void sum(u64 &mass, unsigned int &number)
     {
-        a = warp_sum(a), b = warp_sum(b);
-        if (!MULTI) return;
-        const int now = exchange(a, b);
-        a = 0, b = 0;
-        for (int i = lane; i < warps; i += 32) a += slots[now][i].x, b += slots[now][i].y;
-        a = warp_sum(a), b = warp_sum(b);
-    }
-    // a lane's sum of at most 32 weights with their number above bit 44, as one value: mass and number over the row
-    __device__ __forceinline__ void sum_packed(u64 v, u64 &mass, u64 &number)
-    {
-        const unsigned int lo = __reduce_add_sync(kFull, (unsigned int)v & 0x3FFFFFFu);
-        const unsigned int hi = __reduce_add_sync(kFull, (unsigned int)(v >> 26) & 0x3FFFFu);
-        mass = ((u64)hi << 26) + lo;
-        number = __reduce_add_sync(kFull, (unsigned int)(v >> 44));
-        if (!MULTI) return;
+        mass = warp_sum(mass), number = __reduce_add_sync(kFull, number);
+        if (alone()) return;
         const int now = exchange(mass, number);
-        u64 a = 0;
-        unsigned int b = 0;
-        for (int i = lane; i < warps; i += 32) a += slots[now][i].x, b += (unsigned int)slots[now][i].y;
-        mass = warp_sum(a), number = __reduce_add_sync(kFull, b);
+        mass = 0, number = 0;
+        for (int i = lane; i < warps; i += 32) mass += slots[now][i].x, number += (unsigned int)slots[now][i].y;
+        mass = warp_sum(mass), number = __reduce_add_sync(kFull, number);
     }
-    __device__ __forceinline__ unsigned int count(unsigned int v)
+    // the row's number and the warp's own
+    __device__ __forceinline__ unsigned int count(unsigned int v, unsigned int &mine)
     {
-        v = __reduce_add_sync(kFull, v);
-        if (!MULTI) return v;
+        mine = v = __reduce_add_sync(kFull, v);
+        if (alone()) return v;
         const int now = exchange(v, 0);
         v = 0;
         for (int i = lane; i < warps; i += 32) v += (unsigned int)slots[now][i].x;
         return __reduce_add_sync(kFull, v);
     }
-    __device__ __forceinline__ float max(float v)
+    __device__ __forceinline__ unsigned int count(unsigned int v)
+    {
+        unsigned int mine;
+        return count(v, mine);
+    }
+    // the largest a and the smallest b of the row
+    __device__ __forceinline__ void bounds(unsigned int &a, unsigned int &b)
+    {
+        a = __reduce_max_sync(kFull, a), b = __reduce_min_sync(kFull, b);
+        if (alone()) return;
+        const int now = exchange(a, b);
+        for (int i = lane; i < warps; i += 32) a = max(a, (unsigned int)slots[now][i].x), b = min(b, (unsigned int)slots[now][i].y);
+        a = __reduce_max_sync(kFull, a), b = __reduce_min_sync(kFull, b);
+    }
+    __device__ __forceinline__ float max_of(float v)
     {
         v = lanes_max(v, 32);
-        if (!MULTI) return v;
+        if (alone()) return v;
         const int now = exchange(__float_as_uint(v), 0);
-        v = neg_inf();
         for (int i = lane; i < warps; i += 32) v = fmaxf(v, __uint_as_float((unsigned int)slots[now][i].x));
         return lanes_max(v, 32);
-    }
-    __device__ __forceinline__ unsigned int max_key(unsigned int v)
-    {
-        v = __reduce_max_sync(kFull, v);
-        if (!MULTI) return v;
-        const int now = exchange(v, 0);
-        v = 0;
-        for (int i = lane; i < warps; i += 32) v = ::max(v, (unsigned int)slots[now][i].x);
-        return __reduce_max_sync(kFull, v);
     }
     // sums of `mine`, which the lanes of a warp agree on: over the warps before this one, and over all
     __device__ __forceinline__ void prefix(u64 mine, u64 &before, u64 &all)
     {
         before = 0, all = mine;
-        if (!MULTI) return;
+        if (alone()) return;
         const int now = exchange(mine, 0);
         u64 b = 0, a = 0;
         for (int i = lane; i < warps; i += 32) {
@@ -186,7 +184,7 @@ struct Team {
     // the warp that has something (has: agreed in the warp) tells all
     __device__ __forceinline__ void tell(bool has, u64 &a, u64 &b)
     {
-        if (!MULTI) return;
+        if (alone()) return;
         const int now = turn;
         if (has && lane < cs) cluster_peer(slots[now], lane, cs)[0] = make_ulonglong2(a, b);
         cluster_sync(cs);
@@ -195,87 +193,61 @@ struct Team {
     }
 };
 
-// A lane's elements: registers (REGS), or the workspace for rows that do not fit. Chunk c of the lane covers the
-// columns base + c * 32 * VEC + 0 .. VEC - 1.
-template <int VEC_, int CH_, bool REGS_>
+// A warp's elements, chunk after chunk: the lane's four of chunk c are at store[c * 128 + lane * 4] and belong to the
+// columns first + c * 128 + lane * 4 ... Beyond the row they are logits of -inf, later weights of 0.
 struct Elems {
-    static constexpr int VEC = VEC_, CH = CH_;
-    static constexpr bool REGS = REGS_;
-    unsigned int r[REGS ? CH * VEC : 1];
     unsigned int *store;
     int chunks;
-    int base, n;   // first column of the lane's chunk 0; columns of the row
+    int first;   // column of store[0]
+    int n;       // columns of the row
+
+    __device__ __forceinline__ uint4 &at(int c, int lane) const { return reinterpret_cast<uint4 *>(store)[c * 32 + lane]; }
     template <typename F>
-    __device__ __forceinline__ void each(F f)   // f(value &, column)
+    __device__ __forceinline__ void each(int lane, F f) const   // f(value, column)
     {
-        if constexpr (REGS) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) f(r[c * VEC + i], base + c * 32 * VEC + i);
-        } else {
-            for (int c = 0; c < chunks; ++c)
-                for (int i = 0; i < VEC; ++i) {
-                    const int col = base + c * 32 * VEC + i;
-                    if (col >= n) return;
-                    unsigned int v = store[col];
-                    f(v, col);
-                    store[col] = v;
-                }
+#pragma unroll 2
+        for (int c = 0; c < chunks; ++c) {
+            const uint4 v = at(c, lane);
+            const int col = first + c * kChunk + lane * 4;
+            f(v.x, col), f(v.y, col + 1), f(v.z, col + 2), f(v.w, col + 3);
         }
     }
-    // the sum of value(element, column) over the lane's part of chunk c
     template <typename F>
-    __device__ __forceinline__ u64 chunk_sum(int c, F value)
+    __device__ __forceinline__ void change(int lane, F f) const   // value = f(value, column)
     {
-        u64 s = 0;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int col = base + c * 32 * VEC + i;
-            if constexpr (REGS)
-                s += value(r[c * VEC + i], col);
-            else
-                s += col < n ? value(store[col], col) : 0;
+        for (int c = 0; c < chunks; ++c) {
+            uint4 v = at(c, lane);
+            const int col = first + c * kChunk + lane * 4;
+            v.x = f(v.x, col), v.y = f(v.y, col + 1), v.z = f(v.z, col + 2), v.w = f(v.w, col + 3);
+            at(c, lane) = v;
         }
-        return s;
     }
-    // The first column, in index order over the warp, at which the running sum of value(element, column) from `from`
-    // exceeds t, and the value there; the warp must hold it. sum_of(c): the lane's sum over chunk c.
-    template <typename S, typename F>
-    __device__ __forceinline__ void find(u64 t, u64 from, int lane, S sum_of, F value, int &col_out, u64 &val_out)
+    // The first column, in index order over the warp, at which the running sum of value(element, column) from `run`
+    // exceeds t, and the value there; the warp must hold it.
+    template <typename F>
+    __device__ __forceinline__ void find(u64 t, u64 run, int lane, F value, int &col_out, u64 &val_out) const
     {
-        u64 run = from, s_found = 0, run_found = 0;
-        int c_found = -1;
-        auto step = [&](int c) {
-            if (c_found >= 0) return;
-            const u64 s = sum_of(c), total = warp_sum(s);
-            if (t < run + total) c_found = c, s_found = s, run_found = run;
+        unsigned int v[4] = {0, 0, 0, 0};
+        u64 mine = 0;
+        int c = 0;
+        for (; c < chunks; ++c) {
+            const uint4 raw = at(c, lane);
+            const int col = first + c * kChunk + lane * 4;
+            v[0] = value(raw.x, col), v[1] = value(raw.y, col + 1), v[2] = value(raw.z, col + 2), v[3] = value(raw.w, col + 3);
+            mine = (u64)v[0] + v[1] + v[2] + v[3];
+            const u64 total = warp_sum(mine);
+            if (t < run + total) break;
             run += total;
-        };
-        if constexpr (REGS) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c) step(c);
-        } else {
-            for (int c = 0; c < chunks; ++c) step(c);
         }
-        const u64 upto = run_found + warp_scan(s_found, lane);
+        const u64 upto = run + warp_scan(mine, lane);
         const int owner = __ffs(__ballot_sync(kFull, t < upto)) - 1;
-        u64 acc = upto - s_found, val = 0;
+        u64 acc = upto - mine;
         int col = -1;
-        const int first = base + c_found * 32 * VEC;
+        unsigned int val = 0;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            u64 v = 0;
-            if constexpr (REGS) {
-                unsigned int raw = r[i];
-#pragma unroll
-                for (int c = 1; c < CH; ++c) raw = c == c_found ? r[c * VEC + i] : raw;
-                v = value(raw, first + i);
-            } else if (c_found >= 0 && first + i < n) {
-                v = value(store[first + i], first + i);
-            }
-            acc += v;
-            if (col < 0 && t < acc) col = first + i, val = v;
+        for (int i = 0; i < 4; ++i) {
+            acc += v[i];
+            if (col < 0 && t < acc) col = first + c * kChunk + lane * 4 + i, val = v[i];
         }
         col_out = __shfl_sync(kFull, col, owner);
         val_out = __shfl_sync(kFull, val, owner);
@@ -283,19 +255,18 @@ struct Elems {
 };
 
 // The column of the m-th (from 0) element, in index order over the row, that `pick` accepts.
-template <bool MULTI, typename E, typename F>
-__device__ __forceinline__ int nth_column(Team<MULTI> &team, E &e, u64 m, F pick)
+template <typename F>
+__device__ __forceinline__ int nth_column(Team &team, const Elems &e, u64 m, F pick)
 {
-    auto one = [&](unsigned int v, int col) -> u64 { return pick(v, col) ? 1 : 0; };
+    auto one = [&](unsigned int v, int col) -> unsigned int { return pick(v, col) ? 1u : 0u; };
     unsigned int here = 0;
-    e.each([&](unsigned int &v, int col) { here += pick(v, col) ? 1u : 0u; });
+    e.each(team.lane, [&](unsigned int v, int col) { here += one(v, col); });
     const u64 mine = __reduce_add_sync(kFull, here);
-    u64 before, all;
+    u64 before, all, val = 0;
     team.prefix(mine, before, all);
     int col = -1;
-    u64 val = 0;
     const bool has = m >= before && m < before + mine;
-    if (has) e.find(m, before, team.lane, [&](int c) { return e.chunk_sum(c, one); }, one, col, val);
+    if (has) e.find(m, before, team.lane, one, col, val);
     u64 where = (u64)(unsigned int)col;
     team.tell(has, where, val);
     return (int)(unsigned int)where;
@@ -304,10 +275,15 @@ __device__ __forceinline__ int nth_column(Team<MULTI> &team, E &e, u64 m, F pick
 struct Row {
     float m, scale, top_p, min_p;
     int k;          // 0: off
-    bool greedy, none;
+    bool greedy;
 };
 
-constexpr int kSort = 64;   // weights that one warp sorts, two a lane
+// weights at and below this logit are 0
+__device__ __forceinline__ float zero_below(const Row &p)
+{
+    const float lo = __fsub_rn(p.m, __fdiv_rn(32.0f, p.scale));
+    return lo < p.m ? lo : neg_inf();   // m so large that the distance vanishes
+}
 
 // descending over (a of lane 0 .. 31, b of lane 0 .. 31), a bitonic network
 __device__ __forceinline__ void sort64(unsigned int &a, unsigned int &b, int lane)
@@ -330,42 +306,47 @@ __device__ __forceinline__ void sort64(unsigned int &a, unsigned int &b, int lan
         }
 }
 
+struct ShortList {
+    unsigned int sort[kSort];
+    unsigned int x[kList];
+    int col[kList];
+};
+
 // The weight at which the running sum of weights, in descending order, reaches `limit`; the sum of those above it and
 // how many have just it. Bisection (on the logarithm at first, with the bounds moved onto weights that
 // occur every few steps) until at most 64 weights are left between the bounds, which one warp then sorts.
-template <bool MULTI, typename E>
-__device__ __forceinline__ void nucleus(Team<MULTI> &team, E &e, u64 limit, u64 total, u64 count, unsigned int *sort_list,
-                                        unsigned int &cut, u64 &mass_above, u64 &ties)
+__device__ __forceinline__ void nucleus(Team &team, const Elems &e, u64 limit, u64 total, unsigned int count,
+                                        unsigned int *sort_list, unsigned int &cut, u64 &mass_above, u64 &ties)
 {
+    const int lane = team.lane;
     // invariant: mass(w > hi) < limit <= mass(w > lo)
-    unsigned int lo = 0, hi = 0x80000000u;
-    u64 mass_hi = 0, count_hi = 0, count_lo = count;
+    unsigned int lo = 0, hi = 0x80000000u, count_hi = 0, count_lo = count;
+    u64 mass_hi = 0;
     // Weights below (total - limit) / n together hold less than what may be left out: the cut lies above them.
     const u64 least = (total - limit) / (unsigned int)e.n;
     for (int it = 0; hi - lo > 1 && count_lo - count_hi > kSort; ++it) {
         if ((it & 3) == 3) {
-            unsigned int most = 0, least_in = 0xFFFFFFFFu;
-            e.each([&](unsigned int &v, int) {
-                if (v <= hi) most = max(most, v);
+            unsigned int most_in = 0, least_in = 0xFFFFFFFFu;
+            e.each(lane, [&](unsigned int v, int) {
+                if (v <= hi) most_in = max(most_in, v);
                 if (v > lo) least_in = min(least_in, v);
             });
-            hi = team.max_key(most), lo = ~team.max_key(~least_in) - 1;
+            team.bounds(most_in, least_in);
+            hi = most_in, lo = least_in - 1;
             if (hi - lo <= 1) break;
         }
         unsigned int mid = __float2uint_rd(__uint_as_float((__float_as_uint(__uint2float_rn(lo ? lo : 1)) + __float_as_uint(__uint2float_rn(hi))) / 2));
         if (it == 0 && least > 1) mid = (unsigned int)least - 1;
         if (mid <= lo || mid >= hi) mid = lo + (hi - lo) / 2;
-        u64 mass = 0, c = 0;
-        if constexpr (E::REGS) {
+        u64 mass = 0;
+        unsigned int c = 0;
+        for (int at = 0; at < e.chunks; at += kWarpChunks) {   // 2^44 above 32 weights: a warp's usual chunks
             unsigned int sum_lo = 0, sum_hi = 0;
-            e.each([&](unsigned int &v, int) { add_above(sum_lo, sum_hi, v, mid); });
-            team.sum_packed(((u64)sum_hi << 32) | sum_lo, mass, c);
-        } else {
-            e.each([&](unsigned int &v, int) {
-                if (v > mid) mass += v, ++c;
-            });
-            team.sum2(mass, c);
+            const Elems part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0};
+            part.each(lane, [&](unsigned int v, int) { add_above(sum_lo, sum_hi, v, mid); });
+            mass += ((u64)(sum_hi & 0xFFFu) << 32) | sum_lo, c += sum_hi >> 12;
         }
+        team.sum(mass, c);
         if (mass < limit)
             hi = mid, mass_hi = mass, count_hi = c;
         else
@@ -374,25 +355,22 @@ __device__ __forceinline__ void nucleus(Team<MULTI> &team, E &e, u64 limit, u64 
     cut = hi, mass_above = mass_hi, ties = count_lo - count_hi;
     if (hi - lo <= 1) return;
     unsigned int here = 0;
-    e.each([&](unsigned int &v, int) { here += v - lo - 1 < hi - lo ? 1u : 0u; });
-    const unsigned int incl = warp_scan32(here, team.lane);
+    e.each(lane, [&](unsigned int v, int) { here += v - lo - 1 < hi - lo ? 1u : 0u; });
+    const unsigned int incl = warp_scan(here, lane);
     u64 before, all;
     team.prefix(__shfl_sync(kFull, incl, 31), before, all);
-    unsigned int *to = MULTI ? cluster_peer(sort_list, 0, team.cs) : sort_list;
-    unsigned int at = (unsigned int)before + incl - here;
-    e.each([&](unsigned int &v, int) {
-        if (v - lo - 1 < hi - lo) to[at++] = v;
+    unsigned int *to = team.alone() ? sort_list : cluster_peer(sort_list, 0, team.cs);
+    unsigned int pos = (unsigned int)before + incl - here;
+    e.each(lane, [&](unsigned int v, int) {
+        if (v - lo - 1 < hi - lo) to[pos++] = v;
     });
-    if (MULTI)
-        cluster_sync(team.cs);
-    else
-        __syncwarp();
+    team.sync();
     u64 packed = 0;
     if (team.me == 0) {
-        unsigned int a = team.lane < (int)all ? sort_list[team.lane] : 0u, b = team.lane + 32 < (int)all ? sort_list[team.lane + 32] : 0u;
-        sort64(a, b, team.lane);
-        const u64 run_a = mass_hi + warp_scan(a, team.lane);
-        const u64 run_b = __shfl_sync(kFull, run_a, 31) + warp_scan(b, team.lane);
+        unsigned int a = lane < (int)all ? sort_list[lane] : 0u, b = lane + 32 < (int)all ? sort_list[lane + 32] : 0u;
+        sort64(a, b, lane);
+        const u64 run_a = mass_hi + warp_scan((u64)a, lane);
+        const u64 run_b = __shfl_sync(kFull, run_a, 31) + warp_scan((u64)b, lane);
         const unsigned int in_a = __ballot_sync(kFull, run_a >= limit), in_b = __ballot_sync(kFull, run_b >= limit);
         cut = in_a ? __shfl_sync(kFull, a, __ffs(in_a) - 1) : __shfl_sync(kFull, b, __ffs(in_b) - 1);
         mass_above = mass_hi + warp_sum((u64)(a > cut ? a : 0u) + (b > cut ? b : 0u));
@@ -400,43 +378,35 @@ __device__ __forceinline__ void nucleus(Team<MULTI> &team, E &e, u64 limit, u64 
     }
     team.tell(team.me == 0, mass_above, packed);
     cut = (unsigned int)packed, ties = packed >> 32;
-    if (!MULTI) __syncwarp();   // the list may be written again
 }
 
-// Filters and draws. e holds logits (as bits); logit(col) reads one again, host(col) names the column's host.
-template <bool MULTI, typename E, typename X, typename H>
-__device__ __forceinline__ void decide(const SampleArgs &a, long long row, const Row &p, Team<MULTI> &team, E &e,
-                                       unsigned int *sort_list, X logit, H host)
+// Filters and draws. e holds logits (as bits); of a short list, hosts[column] names the host (otherwise NULL).
+template <typename T>
+__device__ __forceinline__ void decide(const SampleArgs &a, long long row, const T *x, const Row &p, Team &team,
+                                       const Elems &e, unsigned int *sort_list, const int *hosts)
 {
     const int lane = team.lane;
-    // top-k: cut_x = the k-th largest logit; of its ties the first in index order stay. Hosts below m - 32 / c have
-    // weight 0: if at most k are above that, top-k changes nothing.
+    // top-k: cut_x = the k-th largest logit; of its ties the first in index order stay. If at most k logits have a
+    // weight above 0, top-k changes nothing.
     float cut_x = neg_inf();    // logits above it stay
     int tie_col = -1;           // and of those equal to it the columns up to this one
-    if (!p.none && p.k > 0 && p.k < e.n) {
+    if (p.k > 0 && p.k < e.n) {
         const unsigned int k = (unsigned int)p.k;
-        auto above = [&](float x) -> unsigned int {
-            unsigned int c = 0;
-            e.each([&](unsigned int &v, int) { c += __uint_as_float(v) > x ? 1u : 0u; });
-            return team.count(c);
-        };
-        float lo_f = __fsub_rn(p.m, __fdiv_rn(32.0f, p.scale)), hi_f = p.m;
-        if (!(lo_f < hi_f)) lo_f = neg_inf();   // m so large that the distance vanishes
-        unsigned int lo = key_of(lo_f), hi = key_of(hi_f);
-        unsigned int above_hi = 0;
-        bool exact = above(lo_f) <= k;
-        // invariant: above(hi) < k <= above(lo)
-        for (int it = 1; !exact && hi - lo > 1; ++it) {
-            if ((it & 3) == 0) {   // the bounds onto logits that occur
-                float most = neg_inf();
-                unsigned int least = 0xFFFFFFFFu;
-                e.each([&](unsigned int &v, int) {
-                    const float x = __uint_as_float(v);
-                    if (x <= hi_f) most = fmaxf(most, x);
-                    if (x > lo_f) least = min(least, key_of(x + 0.0f));   // + 0: one zero
+        float lo_f = zero_below(p), hi_f = p.m;
+        unsigned int lo = key_of(lo_f), hi = key_of(hi_f), above_hi = 0;
+        bool exact = false;
+        // invariant: above(hi) < k <= above(lo); the first step looks at lo
+        for (int it = 0; !exact && hi - lo > 1; ++it) {
+            if ((it & 3) == 3) {   // the bounds onto logits that occur
+                unsigned int most_in = 0, least_in = 0xFFFFFFFFu;
+                e.each(lane, [&](unsigned int v, int) {
+                    const float f = __uint_as_float(v);
+                    const unsigned int key = key_of(f + 0.0f);   // + 0: one zero
+                    if (f <= hi_f) most_in = max(most_in, key);
+                    if (f > lo_f) least_in = min(least_in, key);
                 });
-                hi_f = team.max(most), hi = key_of(hi_f + 0.0f);
-                lo = ~team.max_key(~least) - 1, lo_f = float_of(lo);
+                team.bounds(most_in, least_in);
+                hi = most_in, hi_f = float_of(hi), lo = least_in - 1, lo_f = float_of(lo);
                 if (hi - lo <= 1) break;
             }
             unsigned int mid = lo + (hi - lo) / 2;
@@ -444,9 +414,13 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
                 const unsigned int g = key_of(0.5f * lo_f + 0.5f * hi_f);
                 if (g > lo && g < hi) mid = g;
             }
-            const float mid_f = float_of(mid);
-            const unsigned int c = above(mid_f);
-            if (c >= k) {
+            const float mid_f = it == 0 ? lo_f : float_of(mid);
+            unsigned int c = 0;
+            e.each(lane, [&](unsigned int v, int) { c += __uint_as_float(v) > mid_f ? 1u : 0u; });
+            c = team.count(c);
+            if (it == 0) {
+                exact = c <= k;
+            } else if (c >= k) {
                 lo = mid, lo_f = mid_f;
                 exact = c == k;
             } else {
@@ -461,29 +435,21 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         }
     }
     // weights from here on
-    u64 total = 0, count = 0;
-    if constexpr (E::REGS) {
-        unsigned int sum_lo = 0, sum_hi = 0;
-        e.each([&](unsigned int &v, int col) {
-            const float f = __uint_as_float(v);
-            v = f > cut_x || (f == cut_x && col <= tie_col) ? weight_of(f, p.m, p.scale) : 0u;
-            add_above(sum_lo, sum_hi, v, 0u);
-        });
-        total = ((u64)sum_hi << 32) | sum_lo;
-        if (p.top_p < 1.0f) team.sum_packed(total, total, count);
-    } else {
-        e.each([&](unsigned int &v, int col) {
-            const float f = __uint_as_float(v);
-            v = f > cut_x || (f == cut_x && col <= tie_col) ? weight_of(f, p.m, p.scale) : 0u;
-            total += v;
-            count += v != 0;
-        });
-        if (p.top_p < 1.0f) team.sum2(total, count);
-    }
+    u64 total = 0;
+    unsigned int count = 0;
+    e.change(lane, [&](unsigned int v, int col) {
+        const float f = __uint_as_float(v);
+        const unsigned int w = f > cut_x || (f == cut_x && col <= tie_col) ? weight_of(f, p.m, p.scale) : 0u;
+        total += w;
+        count += w != 0;
+        return w;
+    });
 
     unsigned int least = 0;   // weights below it go
     if (p.min_p > 0.0f) least = (unsigned int)(fminf(p.min_p, 1.0f) * 0x1p31f);
-    if (p.top_p < 1.0f && !p.greedy && total > 0) {
+    u64 mine = total;
+    if (p.top_p < 1.0f && !p.greedy) {
+        team.sum(total, count);
         u64 limit = share_of(total, (unsigned int)(fmaxf(p.top_p, 0.0f) * 0x1p24f));
         if (limit == 0) limit = 1;
         unsigned int cut;
@@ -494,21 +460,21 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         const u64 keep = (limit - mass_above + cut - 1) / cut;
         if (keep < ties && least == cut) {
             // the ties' logits may still differ: bisection on their keys
-            auto key_at = [&](int col) { return key_of(fminf(logit(col), kMaxFinite) + 0.0f); };
+            auto key_at = [&](int col) { return key_of(fminf(to_float(x[hosts ? hosts[col] : col]), kMaxFinite) + 0.0f); };
             unsigned int least_key = 0xFFFFFFFFu, most_key = 0;
-            e.each([&](unsigned int &v, int col) {
-                if (v == cut) {
-                    const unsigned int key = key_at(col);
-                    least_key = min(least_key, key), most_key = max(most_key, key);
-                }
+            e.each(lane, [&](unsigned int v, int col) {
+                if (v != cut) return;
+                const unsigned int key = key_at(col);
+                least_key = min(least_key, key), most_key = max(most_key, key);
             });
+            team.bounds(most_key, least_key);
             // above(khi) < keep <= above(klo) among the ties
-            unsigned int klo = ~team.max_key(~least_key) - 1, khi = team.max_key(most_key);
+            unsigned int klo = least_key - 1, khi = most_key;
             u64 above_khi = 0, above_klo = ties;
             while (khi - klo > 1 && above_klo > keep) {
                 const unsigned int mid = klo + (khi - klo) / 2;
                 unsigned int c = 0;
-                e.each([&](unsigned int &v, int col) {
+                e.each(lane, [&](unsigned int v, int col) {
                     if (v == cut) c += key_at(col) > mid ? 1u : 0u;
                 });
                 c = team.count(c);
@@ -523,27 +489,24 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
                 kcut = khi;
                 kcol = nth_column(team, e, keep - above_khi - 1, [&](unsigned int v, int col) { return v == cut && key_at(col) == kcut; });
             }
-            e.each([&](unsigned int &v, int col) {
-                if (v != cut) return;
+            e.change(lane, [&](unsigned int v, int col) {
+                if (v != cut) return v;
                 const unsigned int key = key_at(col);
-                if (!(key > kcut || (key == kcut && col <= kcol))) v = 0;
+                return key > kcut || (key == kcut && col <= kcol) ? v : 0u;
             });
         }
     }
-    if (least > 0)
-        e.each([&](unsigned int &v, int) {
-            if (v < least) v = 0;
+    if (least > 0) {
+        mine = 0;
+        e.change(lane, [&](unsigned int v, int) {
+            const unsigned int w = v < least ? 0u : v;
+            mine += w;
+            return w;
         });
-
-    auto as_is = [](unsigned int v, int) -> u64 { return v; };
-    u64 sums[E::REGS ? E::CH : 1], mine = 0;   // the lane's weight in each chunk; the warp's
-    if constexpr (E::REGS) {
-#pragma unroll
-        for (int c = 0; c < E::CH; ++c) sums[c] = e.chunk_sum(c, as_is), mine += sums[c];
-    } else {
-        e.each([&](unsigned int &v, int) { mine += v; });
     }
     mine = warp_sum(mine);
+
+    auto as_is = [](unsigned int v, int) { return v; };
     int found = 0;
     for (int d = 0; d < a.draws; ++d) {
         u64 before, left;
@@ -556,27 +519,15 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
             const bool has = t >= before && t < before + mine;
             u64 val = 0;
             if (has) {
-                if constexpr (E::REGS)
-                    e.find(t, before, lane, [&](int c) { return sums[c]; }, as_is, col, val);
-                else
-                    e.find(t, before, lane, [&](int c) { return e.chunk_sum(c, as_is); }, as_is, col, val);
+                e.find(t, before, lane, as_is, col, val);
                 mine -= val;
-                if (d + 1 < a.draws) {   // out of what is left
-                    e.each([&](unsigned int &v, int at) {
-                        if (at == col) v = 0;
-                    });
-                    if constexpr (E::REGS) {
-#pragma unroll
-                        for (int c = 0; c < E::CH; ++c) {
-                            const int off = col - e.base - c * 32 * E::VEC;
-                            if (off >= 0 && off < E::VEC) sums[c] -= val;
-                        }
-                    }
-                }
+                if (lane == 0) e.store[col - e.first] = 0;   // out of what is left
+                __syncwarp();
             }
             u64 where = (u64)(unsigned int)col;
             team.tell(has, where, val);
-            col = host((int)(unsigned int)where);
+            col = (int)(unsigned int)where;
+            if (hosts) col = hosts[col];
             ++found;
         }
         if (team.me == 0 && lane == 0) a.hosts[row * a.draws + d] = col;
@@ -584,92 +535,60 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
     if (a.found && team.me == 0 && lane == 0) a.found[row] = found;
 }
 
-constexpr int kList = 256;      // hosts a short list holds: 8 a lane of one warp
-constexpr int kListK = 128;     // largest top-k that tries for one
-struct ShortList {
-    unsigned int sort[kSort];
-    float x[kList];
-    int col[kList];
-};
-
-// top-k of a long row leaves few hosts. A threshold that at least k of the lanes' chunk maxima exceed is exceeded by all
-// of the k best, and by not many others: those go, in index order, to a list that one warp finishes alone. Returns
-// the list's length, or -1 if it would be too long (many equal logits).
-template <bool MULTI, typename E>
-__device__ __forceinline__ int short_list(const Row &p, Team<MULTI> &team, E &e, ShortList *list)
+// top-k of a long row leaves few hosts: those above a threshold that at least k and at most 256 logits exceed go, in
+// index order, to a list that one warp finishes alone. Returns the list's length, or -1 if no threshold was found
+// (many equal logits).
+__device__ __forceinline__ int short_list(const Row &p, Team &team, const Elems &e, ShortList *list)
 {
-    constexpr int VEC = E::VEC, CH = E::CH;
-    float top[CH];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        top[c] = neg_inf();
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) top[c] = fmaxf(top[c], __uint_as_float(e.r[c * VEC + i]));
-    }
-    auto above = [&](float x) -> unsigned int {
-        unsigned int n = 0;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) n += top[c] > x ? 1u : 0u;
-        return team.count(n);
-    };
+    const int lane = team.lane;
     const unsigned int k = (unsigned int)p.k;
-    float lo = __fsub_rn(p.m, __fdiv_rn(32.0f, p.scale)), hi = p.m;   // weights at and below lo are 0
-    if (!(lo < hi)) lo = neg_inf();
-    unsigned int n = above(lo);
-    for (int it = 0; it < 10 && n > k + k / 4 + 4; ++it) {
-        const float mid = 0.5f * lo + 0.5f * hi;
-        const unsigned int c = above(mid);
-        if (c >= k)
-            lo = mid, n = c;
+    float lo = zero_below(p), hi = p.m;
+    unsigned int n = 0, mine = 0;
+    for (int it = 0; it < 12; ++it) {
+        const float mid = it ? 0.5f * lo + 0.5f * hi : lo;
+        unsigned int c = 0, own;
+        e.each(lane, [&](unsigned int v, int) { c += __uint_as_float(v) > mid ? 1u : 0u; });
+        c = team.count(c, own);
+        if (it == 0 || c >= k)
+            lo = mid, n = c, mine = own;
         else
             hi = mid;
+        if (n <= kList) break;
     }
-    // where each chunk's hosts go: a field per chunk, wide enough for a warp's count in it (32 * VEC)
-    constexpr int F = VEC > 4 ? 16 : 8;
-    static_assert(CH * F <= 64, "a field per chunk");
-    u64 mine = 0;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
+    if (n > kList) return -1;
+    u64 before, all;
+    team.prefix(mine, before, all);
+    ShortList *to = team.alone() ? list : cluster_peer(list, 0, team.cs);
+    unsigned int base = (unsigned int)before;
+    for (int c = 0; c < e.chunks; ++c) {
+        const uint4 v = e.at(c, lane);
+        const unsigned int x[4] = {v.x, v.y, v.z, v.w};
         unsigned int here = 0;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) here += __uint_as_float(e.r[c * VEC + i]) > lo ? 1u : 0u;
-        mine += (u64)here << (c * F);
-    }
-    const u64 incl = warp_scan(mine, team.lane), all = __shfl_sync(kFull, incl, 31), excl = incl - mine;
-    unsigned int total = 0;
+        for (int i = 0; i < 4; ++i) here += __uint_as_float(x[i]) > lo ? 1u : 0u;
+        if (!__any_sync(kFull, here)) continue;
+        const unsigned int incl = warp_scan(here, lane);
+        unsigned int pos = base + incl - here;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) total += (unsigned int)(all >> (c * F)) & ((1u << F) - 1u);
-    u64 before, length;
-    team.prefix(total, before, length);
-    if (length > kList) return -1;
-    ShortList *to = MULTI ? cluster_peer(list, 0, team.cs) : list;
-    unsigned int base = (unsigned int)before;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        unsigned int at = base + ((unsigned int)(excl >> (c * F)) & ((1u << F) - 1u));
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float x = __uint_as_float(e.r[c * VEC + i]);
-            if (x > lo) {
-                to->x[at] = x;
-                to->col[at] = e.base + c * 32 * VEC + i;
-                ++at;
+        for (int i = 0; i < 4; ++i)
+            if (__uint_as_float(x[i]) > lo) {
+                to->x[pos] = x[i];
+                to->col[pos] = e.first + c * kChunk + lane * 4 + i;
+                ++pos;
             }
-        }
-        base += (unsigned int)(all >> (c * F)) & ((1u << F) - 1u);
+        base += __shfl_sync(kFull, incl, 31);
     }
-    return (int)length;
+    // up to whole chunks of the list
+    if (team.me == 0)
+        for (unsigned int i = n + lane; i < ((n + kChunk - 1) & ~(kChunk - 1u)); i += 32) list->x[i] = 0xFF800000u;
+    return (int)n;
 }
 
-template <typename T, int CH, bool MULTI, bool REGS>
-__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team<MULTI> team, ShortList *list, unsigned int *store, int chunks)
+template <typename T>
+__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team team, Elems e, ShortList *list)
 {
-    constexpr int VEC = kPer16<T>;
     const T *x = static_cast<const T *>(a.x) + row * a.stride;
     const int lane = team.lane;
-    Elems<VEC, CH, REGS> e;
-    e.store = store, e.chunks = chunks, e.n = a.n;
-    e.base = team.me * (REGS ? CH : chunks) * 32 * VEC + lane * VEC;
     Row p;
     const float temperature = a.temperature ? a.temperature[row] : 1.0f;
     p.greedy = !(temperature > 0x1p-20f);
@@ -678,122 +597,112 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
     p.top_p = a.top_p ? a.top_p[row] : 1.0f;
     p.min_p = a.min_p ? a.min_p[row] : 0.0f;
 
+    // a NaN is never the larger, nor above any bound, and has weight 0
     float m = neg_inf();
-    if constexpr (REGS) {
+#pragma unroll 4
+    for (int c = 0; c < e.chunks; ++c) {
+        const int col = e.first + c * kChunk + lane * 4;
+        float v[4];
+        if (a.aligned && col + 4 <= a.n) {
+            load4(x + col, v);
+        } else {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int col = e.base + c * 32 * VEC;
-            float v[VEC];
-            if (a.aligned) {
-                load_cols<T, VEC>(x, col, a.n, neg_inf(), v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[i] = col + i < a.n ? to_float(x[col + i]) : neg_inf();
-            }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                m = fmaxf(m, v[i]);   // a NaN is never the larger, nor above any bound, and has weight 0
-                e.r[c * VEC + i] = __float_as_uint(v[i]);
-            }
+            for (int i = 0; i < 4; ++i) v[i] = col + i < a.n ? to_float(x[col + i]) : neg_inf();
         }
-    } else {
-        e.each([&](unsigned int &v, int col) {
-            const float f = to_float(x[col]);
-            m = fmaxf(m, f);
-            v = __float_as_uint(f);
-        });
+        m = fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
+        e.at(c, lane) = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
-    p.m = team.max(m);
+    p.m = team.max_of(m);
+    if (p.m == neg_inf()) {
+        if (team.me == 0 && lane == 0) {
+            for (int d = 0; d < a.draws; ++d) a.hosts[row * a.draws + d] = -1;
+            if (a.found) a.found[row] = 0;
+        }
+        return;
+    }
     if (p.m > kMaxFinite) {
         p.m = kMaxFinite;
-        e.each([&](unsigned int &v, int) {
-            if (v == 0x7F800000u) v = __float_as_uint(kMaxFinite);
-        });
+        e.change(lane, [&](unsigned int v, int) { return v == 0x7F800000u ? __float_as_uint(kMaxFinite) : v; });
     }
-    p.none = p.m == neg_inf();
-    if constexpr (REGS && CH > 1) {
-        if (!p.none && p.k > 0 && p.k <= kListK && p.k < a.n) {
-            const int length = short_list(p, team, e, list);
-            if (length >= 0) {
-                if (MULTI)
-                    cluster_sync(team.cs);
-                else
-                    __syncwarp();
-                if (team.me != 0) return;
-                Team<false> one{nullptr, 1, 1, 0, lane, 0};
-                Elems<8, kList / 256, true> f;
-                f.store = nullptr, f.chunks = kList / 256, f.n = length, f.base = lane * 8;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    f.r[i] = __float_as_uint(lane * 8 + i < length ? list->x[lane * 8 + i] : neg_inf());
-                decide(a, row, p, one, f, list->sort, [&](int col) { return list->x[col]; }, [&](int col) { return list->col[col]; });
-                return;
-            }
+    const int *hosts = nullptr;
+    if (p.k > 0 && p.k <= kListK && a.n > kList) {
+        const int length = short_list(p, team, e, list);
+        if (length >= 0) {
+            team.sync();
+            if (team.me != 0) return;
+            team.warps = team.cs = 1;
+            e.store = list->x, e.chunks = (length + kChunk - 1) / kChunk, e.first = 0, e.n = length;
+            hosts = list->col;
         }
     }
-    decide(a, row, p, team, e, list->sort, [&](int col) { return to_float(x[col]); }, [](int col) { return col; });
+    decide(a, row, x, p, team, e, list->sort, hosts);
 }
 
-template <typename T, int CH>
-__global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a)
+// one warp per row; shared memory per warp: the row, the lists
+template <typename T>
+__global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a, int chunks, int warp_bytes)
 {
-    __shared__ ShortList s_list[4];
-    const int warp = threadIdx.x >> 5;
+    extern __shared__ __align__(16) char s_mem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * 4 + warp;
     if (row >= a.rows) return;
-    Team<false> team{nullptr, 1, 1, 0, (int)(threadIdx.x & 31), 0};
-    sample_row<T, CH, false, true>(a, row, team, &s_list[warp], nullptr, CH);
+    ShortList *list = reinterpret_cast<ShortList *>(s_mem + warp * warp_bytes);
+    unsigned int *store = reinterpret_cast<unsigned int *>(s_mem + (warp + 1) * warp_bytes) - chunks * kChunk;
+    sample_row<T>(a, row, Team{nullptr, 1, 1, 0, lane, 0}, Elems{store, chunks, 0, a.n}, list);
 }
 
-// grid: REGS one block / cluster per row; else `clusters` of them take the rows in turn
-// THREADS: most threads of a block; blocks of up to 256 get more registers than 1,024 threads leave
-template <typename T, bool REGS, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : 3) sample_block_kernel(SampleArgs a, int cs, int chunks)
+// grid: SHARED one block / cluster per row; else as many as the workspace has rows take them in turn
+template <typename T, bool SHARED>
+__global__ void __launch_bounds__(1024, 1) sample_block_kernel(SampleArgs a, int cs, int chunks)
 {
+    extern __shared__ __align__(16) char s_mem[];
     __shared__ ulonglong2 s_slots[2][kMaxCluster * 32];
     __shared__ ShortList s_list;
-    const int rank = cluster_rank(cs), warps = blockDim.x >> 5;
-    Team<true> team{s_slots, warps * cs, cs, rank * warps + (int)(threadIdx.x >> 5), (int)(threadIdx.x & 31), 0};
-    cluster_sync(cs);   // all blocks of the cluster run
+    const int rank = cluster_rank(cs), warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
+    const Team team{s_slots, warps * cs, cs, rank * warps + warp, (int)(threadIdx.x & 31), 0};
     const long long first = blockIdx.x / cs, step = gridDim.x / cs;
+    const int span = chunks * kChunk;
+    unsigned int *store = SHARED ? reinterpret_cast<unsigned int *>(s_mem) + warp * span
+                                 : a.store + (size_t)first * span * warps * cs + (size_t)team.me * span;
+    cluster_sync(cs);   // all blocks of the cluster run
     for (long long row = first; row < a.rows; row += step) {
-        sample_row<T, kElems / kPer16<T>, true, REGS>(a, row, team, &s_list, REGS ? nullptr : a.store + first * a.n, chunks);
-        cluster_sync(cs);   // slots and list are free again
+        sample_row<T>(a, row, team, Elems{store, chunks, team.me * span, a.n}, &s_list);
+        cluster_sync(cs);   // slots and lists are free again
     }
 }
 
 template <typename T>
 cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
 {
-    constexpr int VEC = kPer16<T>;
-    if (a.n <= 32 * kElems) {
-        const unsigned int blocks = (unsigned int)((a.rows + 3) / 4);
-        if (a.n <= 32 * VEC)
-            sample_warp_kernel<T, 1><<<blocks, 128, 0, stream>>>(a);
-        else
-            sample_warp_kernel<T, kElems / VEC><<<blocks, 128, 0, stream>>>(a);
+    if (a.n <= kWarpRow) {
+        const int chunks = (a.n + kChunk - 1) / kChunk;
+        // short rows make no list of hosts, only the sorted one
+        const int lists = a.n > kList ? (int)sizeof(ShortList) : kSort * 4;
+        const int warp_bytes = lists + chunks * kChunk * 4;
+        sample_warp_kernel<T><<<(unsigned int)((a.rows + 3) / 4), 128, 4 * warp_bytes, stream>>>(a, chunks, warp_bytes);
         return cudaGetLastError();
     }
-    const bool regs = a.n <= kMaxCluster * kBlockRow;
-    auto threads_for = [&](int c) { return ((a.n + c * kElems - 1) / (c * kElems) + 31) / 32 * 32; };
+    const bool shared = a.n <= kMaxCluster * kBlockRow;
+    auto warps_for = [&](int c) { return (a.n + c * kWarpRow - 1) / (c * kWarpRow); };
     int cs = 1;
-    while (cs < kMaxCluster && (threads_for(cs) > 1024 || (a.rows * cs < sms && threads_for(cs) > 256))) cs *= 2;
-    const int threads = regs ? threads_for(cs) : 1024;
-    const int warps = threads / 32 * cs;
-    const int chunks = regs ? kElems / VEC : (a.n + warps * 32 * VEC - 1) / (warps * 32 * VEC);
+    while (cs < kMaxCluster && (warps_for(cs) > 32 || (a.rows * cs < sms && warps_for(cs) > 8))) cs *= 2;
+    const int warps = shared ? warps_for(cs) : 32;
+    const int chunks = shared ? kWarpChunks : (a.n + warps * cs * kChunk - 1) / (warps * cs * kChunk);
     long long clusters = a.rows < (1ll << 27) ? a.rows : (1ll << 27);
     void *store = nullptr;
-    if (!regs) {
+    if (!shared) {
         if (clusters > sms / cs) clusters = sms / cs;
         cudaMemPool_t pool = nullptr;
         if (library_pool(device, &pool)) return cudaErrorMemoryAllocation;
-        const cudaError_t e = cudaMallocFromPoolAsync(&store, (size_t)clusters * a.n * sizeof(unsigned int), pool, stream);
+        const cudaError_t e = cudaMallocFromPoolAsync(&store, (size_t)clusters * chunks * kChunk * warps * cs * 4, pool, stream);
         if (e != cudaSuccess) return e;
         a.store = static_cast<unsigned int *>(store);
     }
+    auto *kernel = shared ? sample_block_kernel<T, true> : sample_block_kernel<T, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned int)(clusters * cs));
-    cfg.blockDim = dim3(threads);
+    cfg.blockDim = dim3(warps * 32);
+    cfg.dynamicSmemBytes = shared ? (size_t)warps * kWarpRow * 4 : 0;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -801,9 +710,9 @@ cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = !regs           ? cudaLaunchKernelEx(&cfg, sample_block_kernel<T, false, 1024>, a, cs, chunks)
-                          : threads > 256 ? cudaLaunchKernelEx(&cfg, sample_block_kernel<T, true, 1024>, a, cs, chunks)
-                                          : cudaLaunchKernelEx(&cfg, sample_block_kernel<T, true, 256>, a, cs, chunks);
+    cudaError_t e = cudaSuccess;
+    if (cfg.dynamicSmemBytes > 32 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlockRow * 4);
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, a, cs, chunks);
     if (store) cudaFreeAsync(store, stream);
     return e;
 }
@@ -831,7 +740,9 @@ extern "C" int nbos_policy_sample(const nbos_logits *logits, const float *unifor
     SampleArgs a{logits->data, logits->rows, logits->row_stride, logits->n_hosts, draws, 0, uniforms, temperature, top_k,
                  top_p, min_p, out_hosts, out_found, nullptr};
     if (a.rows == 1) a.stride = a.n;
-    a.aligned = rows_aligned16(a.x, a.rows, a.stride, dtype_bytes(logits->dtype));
+    // four elements at a time
+    const size_t four = 4 * dtype_bytes(logits->dtype);
+    a.aligned = aligned_to(a.x, four) && (a.rows == 1 || a.stride % 4 == 0);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const cudaError_t e = logits->dtype == NBOS_F32    ? launch<float>(a, sms, device, stream)
                           : logits->dtype == NBOS_BF16 ? launch<__nv_bfloat16>(a, sms, device, stream)
