@@ -63,9 +63,10 @@ __device__ __forceinline__ unsigned int weight_of(float x, float m, float scale)
 {
     float e;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__fmul_rn(__fsub_rn(x, m), scale)));
-    const unsigned int b = __float_as_uint(e), shift = 127u - (b >> 23);
-    const unsigned int w = (b << 8) | 0x80000000u;
-    return shift < 32u ? w >> shift : 0u;
+    const unsigned int b = __float_as_uint(e);
+    unsigned int w;
+    asm("shr.u32 %0, %1, %2;" : "=r"(w) : "r"((b << 8) | 0x80000000u), "r"(127u - (b >> 23)));   // shifts above 31 give 0
+    return w;
 }
 
 // sum += w + 2^44 if w > t: a sum of weights with their number above it, in three instructions
@@ -200,6 +201,8 @@ struct Elems {
     int chunks;
     int first;   // column of store[0]
     int n;       // columns of the row
+    unsigned int *block_store;   // of the block's first warp
+    int block_columns;           // of all its warps
 
     __device__ __forceinline__ uint4 &at(int c, int lane) const { return reinterpret_cast<uint4 *>(store)[c * 32 + lane]; }
     template <typename F>
@@ -275,7 +278,7 @@ __device__ __forceinline__ int nth_column(Team &team, const Elems &e, u64 m, F p
 struct Row {
     float m, scale, top_p, min_p;
     int k;          // 0: off
-    bool greedy;
+    bool greedy;   // T too small to divide by: the best host
 };
 
 // weights at and below this logit are 0
@@ -306,17 +309,24 @@ __device__ __forceinline__ void sort64(unsigned int &a, unsigned int &b, int lan
         }
 }
 
+struct SortList {
+    unsigned int w[kSort];
+    int col[kSort];
+};
 struct ShortList {
-    unsigned int sort[kSort];
+    SortList sort;
     unsigned int x[kList];
     int col[kList];
 };
 
-// The weight at which the running sum of weights, in descending order, reaches `limit`; the sum of those above it and
-// how many have just it. Bisection (on the logarithm at first, with the bounds moved onto weights that
+// The nucleus: the first weights, in (x descending, index ascending) order, before which less than `limit` stands.
+// Returns the weight of the last of them. Of the `ties` that have just this weight the first `keep` are to stay (0: all that
+// are left in the row: the others have been taken out). Bisection (on the logarithm at first, with the bounds moved onto weights that
 // occur every few steps) until at most 64 weights are left between the bounds, which one warp then sorts.
-__device__ __forceinline__ void nucleus(Team &team, const Elems &e, u64 limit, u64 total, unsigned int count,
-                                        unsigned int *sort_list, unsigned int &cut, u64 &mass_above, u64 &ties)
+// key_at(column): the order of the logit there.
+template <typename K>
+__device__ __forceinline__ unsigned int nucleus(Team &team, const Elems &e, u64 limit, u64 total, unsigned int count,
+                                                SortList *list, u64 &keep, u64 &ties, K key_at)
 {
     const int lane = team.lane;
     // invariant: mass(w > hi) < limit <= mass(w > lo)
@@ -325,7 +335,7 @@ __device__ __forceinline__ void nucleus(Team &team, const Elems &e, u64 limit, u
     // Weights below (total - limit) / n together hold less than what may be left out: the cut lies above them.
     const u64 least = (total - limit) / (unsigned int)e.n;
     for (int it = 0; hi - lo > 1 && count_lo - count_hi > kSort; ++it) {
-        if ((it & 3) == 3) {
+        if ((it & 3) == 2 && it > 4) {
             unsigned int most_in = 0, least_in = 0xFFFFFFFFu;
             e.each(lane, [&](unsigned int v, int) {
                 if (v <= hi) most_in = max(most_in, v);
@@ -342,7 +352,7 @@ __device__ __forceinline__ void nucleus(Team &team, const Elems &e, u64 limit, u
         unsigned int c = 0;
         for (int at = 0; at < e.chunks; at += kWarpChunks) {   // 2^44 above 32 weights: a warp's usual chunks
             unsigned int sum_lo = 0, sum_hi = 0;
-            const Elems part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0};
+            const Elems part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0, nullptr, 0};
             part.each(lane, [&](unsigned int v, int) { add_above(sum_lo, sum_hi, v, mid); });
             mass += ((u64)(sum_hi & 0xFFFu) << 32) | sum_lo, c += sum_hi >> 12;
         }
@@ -352,44 +362,77 @@ __device__ __forceinline__ void nucleus(Team &team, const Elems &e, u64 limit, u
         else
             lo = mid, count_lo = c;
     }
-    cut = hi, mass_above = mass_hi, ties = count_lo - count_hi;
-    if (hi - lo <= 1) return;
+    if (hi - lo <= 1) {
+        ties = count_lo - count_hi;
+        keep = (limit - mass_hi + hi - 1) / hi;
+        if (keep >= ties) keep = 0;
+        return hi;
+    }
     unsigned int here = 0;
     e.each(lane, [&](unsigned int v, int) { here += v - lo - 1 < hi - lo ? 1u : 0u; });
     const unsigned int incl = warp_scan(here, lane);
     u64 before, all;
     team.prefix(__shfl_sync(kFull, incl, 31), before, all);
-    unsigned int *to = team.alone() ? sort_list : cluster_peer(sort_list, 0, team.cs);
+    SortList *to = team.alone() ? list : cluster_peer(list, 0, team.cs);
     unsigned int pos = (unsigned int)before + incl - here;
-    e.each(lane, [&](unsigned int v, int) {
-        if (v - lo - 1 < hi - lo) to[pos++] = v;
+    e.each(lane, [&](unsigned int v, int col) {
+        if (v - lo - 1 < hi - lo) to->w[pos] = v, to->col[pos++] = col;
     });
     team.sync();
-    u64 packed = 0;
+    u64 cut = 0, none = 0;
     if (team.me == 0) {
-        unsigned int a = lane < (int)all ? sort_list[lane] : 0u, b = lane + 32 < (int)all ? sort_list[lane + 32] : 0u;
+        const bool has_a = lane < (int)all, has_b = lane + 32 < (int)all;
+        const unsigned int wa = has_a ? list->w[lane] : 0u, wb = has_b ? list->w[lane + 32] : 0u;
+        unsigned int a = wa, b = wb;
         sort64(a, b, lane);
         const u64 run_a = mass_hi + warp_scan((u64)a, lane);
         const u64 run_b = __shfl_sync(kFull, run_a, 31) + warp_scan((u64)b, lane);
         const unsigned int in_a = __ballot_sync(kFull, run_a >= limit), in_b = __ballot_sync(kFull, run_b >= limit);
         cut = in_a ? __shfl_sync(kFull, a, __ffs(in_a) - 1) : __shfl_sync(kFull, b, __ffs(in_b) - 1);
-        mass_above = mass_hi + warp_sum((u64)(a > cut ? a : 0u) + (b > cut ? b : 0u));
-        packed = ((u64)__reduce_add_sync(kFull, (a == cut ? 1u : 0u) + (b == cut ? 1u : 0u)) << 32) | cut;
+        const u64 above = mass_hi + warp_sum((u64)(a > cut ? a : 0u) + (b > cut ? b : 0u));
+        unsigned int tie_a = __ballot_sync(kFull, wa == cut), tie_b = __ballot_sync(kFull, wb == cut);
+        const unsigned int stay = (unsigned int)min((limit - above + cut - 1) / cut, (u64)kSort);
+        if (stay < (unsigned int)(__popc(tie_a) + __popc(tie_b))) {
+            // each tie's place among them by logit, then index; those from `stay` on go
+            const int col_a = wa == cut ? list->col[lane] : 0, col_b = wb == cut ? list->col[lane + 32] : 0;
+            const unsigned int key_a = wa == cut ? key_at(col_a) : 0u, key_b = wb == cut ? key_at(col_b) : 0u;
+            unsigned int place_a = 0, place_b = 0;
+            while (tie_a | tie_b) {
+                const bool from_a = tie_a != 0;
+                const int src = __ffs(from_a ? tie_a : tie_b) - 1;
+                if (from_a)
+                    tie_a &= tie_a - 1;
+                else
+                    tie_b &= tie_b - 1;
+                const unsigned int key = __shfl_sync(kFull, from_a ? key_a : key_b, src);
+                const int col = __shfl_sync(kFull, from_a ? col_a : col_b, src);
+                place_a += key > key_a || (key == key_a && col < col_a);
+                place_b += key > key_b || (key == key_b && col < col_b);
+            }
+            auto out = [&](int col) {
+                const int rank = team.cs > 1 ? col / e.block_columns : 0;
+                unsigned int *at = team.cs > 1 && e.block_columns < (1 << 30) ? cluster_peer(e.block_store, rank, team.cs) : e.block_store;
+                at[col - rank * e.block_columns] = 0;
+            };
+            if (wa == cut && place_a >= stay) out(col_a);
+            if (wb == cut && place_b >= stay) out(col_b);
+            __syncwarp();
+        }
     }
-    team.tell(team.me == 0, mass_above, packed);
-    cut = (unsigned int)packed, ties = packed >> 32;
+    team.tell(team.me == 0, cut, none);
+    keep = 0;
+    return (unsigned int)cut;
 }
 
 // Filters and draws. e holds logits (as bits); of a short list, hosts[column] names the host (otherwise NULL).
 template <typename T>
 __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const T *x, const Row &p, Team &team,
-                                       const Elems &e, unsigned int *sort_list, const int *hosts)
+                                       const Elems &e, SortList *sort_list, const int *hosts)
 {
     const int lane = team.lane;
     // top-k: cut_x = the k-th largest logit; of its ties the first in index order stay. If at most k logits have a
     // weight above 0, top-k changes nothing.
-    float cut_x = neg_inf();    // logits above it stay
-    int tie_col = -1;           // and of those equal to it the columns up to this one
+    float cut_x = neg_inf();    // logits from it on stay
     if (p.k > 0 && p.k < e.n) {
         const unsigned int k = (unsigned int)p.k;
         float lo_f = zero_below(p), hi_f = p.m;
@@ -428,39 +471,41 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
             }
         }
         if (exact) {
-            cut_x = lo_f;
+            cut_x = float_of(lo + 1);
         } else {
             cut_x = hi_f;
-            tie_col = nth_column(team, e, k - above_hi - 1, [&](unsigned int v, int) { return __uint_as_float(v) == cut_x; });
+            const int tie_col = nth_column(team, e, k - above_hi - 1, [&](unsigned int v, int) { return __uint_as_float(v) == cut_x; });
+            e.change(lane, [&](unsigned int v, int col) { return __uint_as_float(v) == cut_x && col > tie_col ? 0xFF800000u : v; });
         }
     }
     // weights from here on
-    u64 total = 0;
+    u64 mine = 0;
     unsigned int count = 0;
-    e.change(lane, [&](unsigned int v, int col) {
-        const float f = __uint_as_float(v);
-        const unsigned int w = f > cut_x || (f == cut_x && col <= tie_col) ? weight_of(f, p.m, p.scale) : 0u;
-        total += w;
-        count += w != 0;
-        return w;
-    });
+    for (int at = 0; at < e.chunks; at += kWarpChunks) {
+        unsigned int sum_lo = 0, sum_hi = 0;
+        const Elems part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0, nullptr, 0};
+        part.change(lane, [&](unsigned int v, int) {
+            const float f = __uint_as_float(v);
+            const unsigned int w = f >= cut_x ? weight_of(f, p.m, p.scale) : 0u;
+            add_above(sum_lo, sum_hi, w, 0u);
+            return w;
+        });
+        mine += ((u64)(sum_hi & 0xFFFu) << 32) | sum_lo, count += sum_hi >> 12;
+    }
 
     unsigned int least = 0;   // weights below it go
     if (p.min_p > 0.0f) least = (unsigned int)(fminf(p.min_p, 1.0f) * 0x1p31f);
-    u64 mine = total;
-    if (p.top_p < 1.0f && !p.greedy) {
+    if (p.top_p < 1.0f) {
+        u64 total = mine;
         team.sum(total, count);
         u64 limit = share_of(total, (unsigned int)(fmaxf(p.top_p, 0.0f) * 0x1p24f));
         if (limit == 0) limit = 1;
-        unsigned int cut;
-        u64 mass_above, ties;
-        nucleus(team, e, limit, total, count, sort_list, cut, mass_above, ties);
+        auto key_at = [&](int col) { return key_of(fminf(to_float(x[hosts ? hosts[col] : col]), kMaxFinite) + 0.0f); };
+        u64 keep, ties;
+        const unsigned int cut = nucleus(team, e, limit, total, count, sort_list, keep, ties, key_at);
         least = max(least, cut);
-        // the first ceil((limit - mass_above) / cut) of the ties in (x descending, index ascending) stay
-        const u64 keep = (limit - mass_above + cut - 1) / cut;
-        if (keep < ties && least == cut) {
-            // the ties' logits may still differ: bisection on their keys
-            auto key_at = [&](int col) { return key_of(fminf(to_float(x[hosts ? hosts[col] : col]), kMaxFinite) + 0.0f); };
+        if (keep > 0 && least == cut) {
+            // many ties, whose logits may still differ: bisection on their keys
             unsigned int least_key = 0xFFFFFFFFu, most_key = 0;
             e.each(lane, [&](unsigned int v, int col) {
                 if (v != cut) return;
@@ -593,7 +638,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
     const float temperature = a.temperature ? a.temperature[row] : 1.0f;
     p.greedy = !(temperature > 0x1p-20f);
     p.scale = __fdiv_rn(kLog2e, p.greedy ? 1.0f : temperature);
-    p.k = p.greedy ? 1 : (a.top_k ? a.top_k[row] : 0);
+    p.k = a.top_k ? a.top_k[row] : 0;
     p.top_p = a.top_p ? a.top_p[row] : 1.0f;
     p.min_p = a.min_p ? a.min_p[row] : 0.0f;
 
@@ -624,6 +669,18 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
         p.m = kMaxFinite;
         e.change(lane, [&](unsigned int v, int) { return v == 0x7F800000u ? __float_as_uint(kMaxFinite) : v; });
     }
+    if (p.greedy) {   // the first host with the largest logit
+        unsigned int none = 0, col = 0xFFFFFFFFu;
+        e.each(lane, [&](unsigned int v, int at) {
+            if (__uint_as_float(v) == p.m) col = min(col, (unsigned int)at);
+        });
+        team.bounds(none, col);
+        if (team.me == 0 && lane == 0) {
+            for (int d = 0; d < a.draws; ++d) a.hosts[row * a.draws + d] = d ? -1 : (int)col;
+            if (a.found) a.found[row] = 1;
+        }
+        return;
+    }
     const int *hosts = nullptr;
     if (p.k > 0 && p.k <= kListK && a.n > kList) {
         const int length = short_list(p, team, e, list);
@@ -631,11 +688,11 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
             team.sync();
             if (team.me != 0) return;
             team.warps = team.cs = 1;
-            e.store = list->x, e.chunks = (length + kChunk - 1) / kChunk, e.first = 0, e.n = length;
+            e.store = e.block_store = list->x, e.chunks = (length + kChunk - 1) / kChunk, e.first = 0, e.n = length;
             hosts = list->col;
         }
     }
-    decide(a, row, x, p, team, e, list->sort, hosts);
+    decide(a, row, x, p, team, e, &list->sort, hosts);
 }
 
 // one warp per row; shared memory per warp: the row, the lists
@@ -648,7 +705,7 @@ __global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a, int chun
     if (row >= a.rows) return;
     ShortList *list = reinterpret_cast<ShortList *>(s_mem + warp * warp_bytes);
     unsigned int *store = reinterpret_cast<unsigned int *>(s_mem + (warp + 1) * warp_bytes) - chunks * kChunk;
-    sample_row<T>(a, row, Team{nullptr, 1, 1, 0, lane, 0}, Elems{store, chunks, 0, a.n}, list);
+    sample_row<T>(a, row, Team{nullptr, 1, 1, 0, lane, 0}, Elems{store, chunks, 0, a.n, store, 0}, list);
 }
 
 // grid: SHARED one block / cluster per row; else as many as the workspace has rows take them in turn
@@ -662,11 +719,12 @@ __global__ void __launch_bounds__(1024, 1) sample_block_kernel(SampleArgs a, int
     const Team team{s_slots, warps * cs, cs, rank * warps + warp, (int)(threadIdx.x & 31), 0};
     const long long first = blockIdx.x / cs, step = gridDim.x / cs;
     const int span = chunks * kChunk;
-    unsigned int *store = SHARED ? reinterpret_cast<unsigned int *>(s_mem) + warp * span
-                                 : a.store + (size_t)first * span * warps * cs + (size_t)team.me * span;
+    // the cluster's part of the workspace is one stretch: `cluster_peer` is not asked there
+    unsigned int *block_store = SHARED ? reinterpret_cast<unsigned int *>(s_mem) : a.store + ((size_t)first * cs + rank) * span * warps;
+    unsigned int *store = block_store + warp * span;
     cluster_sync(cs);   // all blocks of the cluster run
     for (long long row = first; row < a.rows; row += step) {
-        sample_row<T>(a, row, team, Elems{store, chunks, team.me * span, a.n}, &s_list);
+        sample_row<T>(a, row, team, Elems{store, chunks, team.me * span, a.n, SHARED ? block_store : block_store - (size_t)rank * span * warps, SHARED ? span * warps : 1 << 30}, &s_list);
         cluster_sync(cs);   // slots and lists are free again
     }
 }
@@ -677,7 +735,7 @@ cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
     if (a.n <= kWarpRow) {
         const int chunks = (a.n + kChunk - 1) / kChunk;
         // short rows make no list of hosts, only the sorted one
-        const int lists = a.n > kList ? (int)sizeof(ShortList) : kSort * 4;
+        const int lists = a.n > kList ? (int)sizeof(ShortList) : (int)sizeof(SortList);
         const int warp_bytes = lists + chunks * kChunk * 4;
         sample_warp_kernel<T><<<(unsigned int)((a.rows + 3) / 4), 128, 4 * warp_bytes, stream>>>(a, chunks, warp_bytes);
         return cudaGetLastError();
