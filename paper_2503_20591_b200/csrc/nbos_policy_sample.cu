@@ -28,8 +28,8 @@ constexpr int kWarpRow = kChunk * kWarpChunks;
 constexpr int kMaxCluster = 8;
 constexpr int kBlockRow = 32 * kWarpRow;
 constexpr int kSort = 64;              // weights that one warp sorts, two a lane
-constexpr int kList = 256;             // hosts of the list that top-k leaves
-constexpr int kListK = 192;            // largest top-k that tries for one
+constexpr int kList = 128;             // hosts of a list that one warp holds in registers, four a lane
+constexpr int kListK = 112;            // largest top-k that tries for one
 typedef unsigned long long u64;
 
 struct SampleArgs {
@@ -313,10 +313,13 @@ struct SortList {
     unsigned int w[kSort];
     int col[kSort];
 };
-struct ShortList {
-    SortList sort;
+struct ShortList {   // hosts, in index order
     unsigned int x[kList];
     int col[kList];
+};
+union Lists {        // a row makes one or the other
+    SortList sort;
+    ShortList hosts;
 };
 
 // The nucleus: the first weights, in (x descending, index ascending) order, before which less than `limit` stands.
@@ -424,10 +427,10 @@ __device__ __forceinline__ unsigned int nucleus(Team &team, const Elems &e, u64 
     return (unsigned int)cut;
 }
 
-// Filters and draws. e holds logits (as bits); of a short list, hosts[column] names the host (otherwise NULL).
+// Filters and draws of a row whose logits (as bits) e holds.
 template <typename T>
 __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const T *x, const Row &p, Team &team,
-                                       const Elems &e, SortList *sort_list, const int *hosts)
+                                       const Elems &e, SortList *sort_list)
 {
     const int lane = team.lane;
     // top-k: cut_x = the k-th largest logit; of its ties the first in index order stay. If at most k logits have a
@@ -500,7 +503,7 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         team.sum(total, count);
         u64 limit = share_of(total, (unsigned int)(fmaxf(p.top_p, 0.0f) * 0x1p24f));
         if (limit == 0) limit = 1;
-        auto key_at = [&](int col) { return key_of(fminf(to_float(x[hosts ? hosts[col] : col]), kMaxFinite) + 0.0f); };
+        auto key_at = [&](int col) { return key_of(fminf(to_float(x[col]), kMaxFinite) + 0.0f); };
         u64 keep, ties;
         const unsigned int cut = nucleus(team, e, limit, total, count, sort_list, keep, ties, key_at);
         least = max(least, cut);
@@ -572,7 +575,6 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
             u64 where = (u64)(unsigned int)col;
             team.tell(has, where, val);
             col = (int)(unsigned int)where;
-            if (hosts) col = hosts[col];
             ++found;
         }
         if (team.me == 0 && lane == 0) a.hosts[row * a.draws + d] = col;
@@ -580,21 +582,151 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
     if (a.found && team.me == 0 && lane == 0) a.found[row] = found;
 }
 
-// top-k of a long row leaves few hosts: those above a threshold that at least k and at most 256 logits exceed go, in
+// descending over the positions lane + 32 j, a bitonic network
+__device__ __forceinline__ void sort128(unsigned int (&s)[4], int lane)
+{
+#pragma unroll
+    for (int k = 2; k <= 128; k *= 2)
+#pragma unroll
+        for (int d = k / 2; d > 0; d /= 2) {
+            if (d >= 32) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int o = j ^ (d / 32);
+                    if (o < j) continue;
+                    const unsigned int hi = max(s[j], s[o]), lo = min(s[j], s[o]);
+                    const bool down = ((32 * j) & k) == 0;
+                    s[j] = down ? hi : lo, s[o] = down ? lo : hi;
+                }
+            } else {
+                const bool first = (lane & d) == 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned int other = __shfl_xor_sync(kFull, s[j], d);
+                    s[j] = (((lane + 32 * j) & k) == 0) == first ? max(s[j], other) : min(s[j], other);
+                }
+            }
+        }
+}
+
+// Filters and draws of at most 128 hosts, in index order over the positions lane + 32 j: key[j] orders the logit there,
+// 0 = no host. cols[position] names the host; NULL: the position does.
+__device__ __forceinline__ void finish(const SampleArgs &a, long long row, const Row &p, unsigned int (&key)[4], int lane, const int *cols)
+{
+    const unsigned int below = (1u << lane) - 1;
+    unsigned int s[4], hosts = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        s[j] = key[j];
+        hosts += __popc(__ballot_sync(kFull, key[j] != 0));
+    }
+    const bool cut_k = p.k > 0 && p.k < (int)hosts;
+    if (cut_k || p.top_p < 1.0f) sort128(s, lane);
+    auto at_place = [&](unsigned int i) {
+        const unsigned int v = i < 64 ? (i < 32 ? s[0] : s[1]) : (i < 96 ? s[2] : s[3]);
+        return __shfl_sync(kFull, v, i & 31);
+    };
+    // keep what has a key above v, and the first `stay` of those with v
+    auto keep = [&](unsigned int v, unsigned int stay) {
+        unsigned int before = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const unsigned int ties = __ballot_sync(kFull, key[j] == v);
+            if (key[j] < v || (key[j] == v && before + __popc(ties & below) >= stay)) key[j] = 0;
+            before += __popc(ties);
+        }
+    };
+    if (cut_k) {
+        const unsigned int v = at_place(p.k - 1);
+        unsigned int above = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) above += __popc(__ballot_sync(kFull, key[j] > v));
+        keep(v, (unsigned int)p.k - above);
+        hosts = p.k;
+    }
+    auto weight = [&](unsigned int k) { return k ? weight_of(float_of(k), p.m, p.scale) : 0u; };
+    unsigned int w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = weight(key[j]);
+    if (p.top_p < 1.0f) {
+        u64 limit = share_of(warp_sum((u64)w[0] + w[1] + w[2] + w[3]), (unsigned int)(fmaxf(p.top_p, 0.0f) * 0x1p24f));
+        if (limit == 0) limit = 1;
+        u64 run = 0;
+        unsigned int v = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (v != 0) continue;
+            const u64 upto = run + warp_scan((u64)(lane + 32 * j < (int)hosts ? weight(s[j]) : 0u), lane);
+            const unsigned int in = __ballot_sync(kFull, upto >= limit);
+            if (in) v = __shfl_sync(kFull, s[j], __ffs(in) - 1);
+            run = __shfl_sync(kFull, upto, 31);
+        }
+        u64 above = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) above += key[j] > v ? w[j] : 0u;
+        above = warp_sum(above);
+        const unsigned int cut = weight(v);
+        keep(v, (unsigned int)((limit - above + cut - 1) / cut));
+    }
+    unsigned int least = 0;
+    if (p.min_p > 0.0f) least = (unsigned int)(fminf(p.min_p, 1.0f) * 0x1p31f);
+    u64 upto[4], left = 0;   // running sums of the weights in index order
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (key[j] == 0 || w[j] < least) w[j] = 0;
+        upto[j] = left;
+        if (__any_sync(kFull, w[j])) {
+            upto[j] = left + warp_scan((u64)w[j], lane);
+            left = __shfl_sync(kFull, upto[j], 31);
+        }
+    }
+    int found = 0;
+    for (int d = 0; d < a.draws; ++d) {
+        int host = -1;
+        if (left > 0) {
+            unsigned int steps = (unsigned int)(fminf(fmaxf(a.u[row * a.draws + d], 0.0f), 1.0f) * 0x1p24f);
+            if (steps > 0xFFFFFFu) steps = 0xFFFFFFu;
+            const u64 t = share_of(left, steps);
+            int place = -1;
+            unsigned int val = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned int over = __ballot_sync(kFull, upto[j] > t);
+                if (place < 0 && over) {
+                    place = 32 * j + __ffs(over) - 1;
+                    val = __shfl_sync(kFull, w[j], place & 31);
+                }
+            }
+            // out of what is left: its own running sum falls to the one before it
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (lane + 32 * j >= place) upto[j] -= val;
+            left -= val;
+            host = cols ? cols[place] : place;
+            ++found;
+        }
+        if (lane == 0) a.hosts[row * a.draws + d] = host;
+    }
+    if (a.found && lane == 0) a.found[row] = found;
+}
+
+// top-k of a long row leaves few hosts: those above a threshold that at least k and at most 128 logits exceed go, in
 // index order, to a list that one warp finishes alone. Returns the list's length, or -1 if no threshold was found
 // (many equal logits).
 __device__ __forceinline__ int short_list(const Row &p, Team &team, const Elems &e, ShortList *list)
 {
     const int lane = team.lane;
     const unsigned int k = (unsigned int)p.k;
+    // bisection between the largest logit and where weights end, first at a quarter of the way
     float lo = zero_below(p), hi = p.m;
-    unsigned int n = 0, mine = 0;
-    for (int it = 0; it < 12; ++it) {
-        const float mid = it ? 0.5f * lo + 0.5f * hi : lo;
+    unsigned int n = 0xFFFFFFFFu, mine = 0;
+    for (int it = 0; it < 14; ++it) {
+        float mid = it == 0 ? 0.25f * lo + 0.75f * hi : 0.5f * lo + 0.5f * hi;
+        if (it == 6 && n == 0xFFFFFFFFu) mid = lo;   // perhaps there are no k with a weight
         unsigned int c = 0, own;
         e.each(lane, [&](unsigned int v, int) { c += __uint_as_float(v) > mid ? 1u : 0u; });
         c = team.count(c, own);
-        if (it == 0 || c >= k)
+        if (c >= k || mid == lo)
             lo = mid, n = c, mine = own;
         else
             hi = mid;
@@ -623,24 +755,33 @@ __device__ __forceinline__ int short_list(const Row &p, Team &team, const Elems 
             }
         base += __shfl_sync(kFull, incl, 31);
     }
-    // up to whole chunks of the list
-    if (team.me == 0)
-        for (unsigned int i = n + lane; i < ((n + kChunk - 1) & ~(kChunk - 1u)); i += 32) list->x[i] = 0xFF800000u;
     return (int)n;
 }
 
-template <typename T>
-__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team team, Elems e, ShortList *list)
+__device__ __forceinline__ Row row_settings(const SampleArgs &a, long long row)
 {
-    const T *x = static_cast<const T *>(a.x) + row * a.stride;
-    const int lane = team.lane;
     Row p;
+    p.m = neg_inf();
     const float temperature = a.temperature ? a.temperature[row] : 1.0f;
     p.greedy = !(temperature > 0x1p-20f);
     p.scale = __fdiv_rn(kLog2e, p.greedy ? 1.0f : temperature);
     p.k = a.top_k ? a.top_k[row] : 0;
     p.top_p = a.top_p ? a.top_p[row] : 1.0f;
     p.min_p = a.min_p ? a.min_p[row] : 0.0f;
+    return p;
+}
+__device__ __forceinline__ void write_one(const SampleArgs &a, long long row, int host)   // host or none
+{
+    for (int d = 0; d < a.draws; ++d) a.hosts[row * a.draws + d] = d ? -1 : host;
+    if (a.found) a.found[row] = host >= 0;
+}
+
+template <typename T>
+__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team team, const Elems &e, Lists *lists)
+{
+    const T *x = static_cast<const T *>(a.x) + row * a.stride;
+    const int lane = team.lane;
+    Row p = row_settings(a, row);
 
     // a NaN is never the larger, nor above any bound, and has weight 0
     float m = neg_inf();
@@ -659,10 +800,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
     }
     p.m = team.max_of(m);
     if (p.m == neg_inf()) {
-        if (team.me == 0 && lane == 0) {
-            for (int d = 0; d < a.draws; ++d) a.hosts[row * a.draws + d] = -1;
-            if (a.found) a.found[row] = 0;
-        }
+        if (team.me == 0 && lane == 0) write_one(a, row, -1);
         return;
     }
     if (p.m > kMaxFinite) {
@@ -675,24 +813,56 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
             if (__uint_as_float(v) == p.m) col = min(col, (unsigned int)at);
         });
         team.bounds(none, col);
-        if (team.me == 0 && lane == 0) {
-            for (int d = 0; d < a.draws; ++d) a.hosts[row * a.draws + d] = d ? -1 : (int)col;
-            if (a.found) a.found[row] = 1;
-        }
+        if (team.me == 0 && lane == 0) write_one(a, row, (int)col);
         return;
     }
-    const int *hosts = nullptr;
-    if (p.k > 0 && p.k <= kListK && a.n > kList) {
-        const int length = short_list(p, team, e, list);
+    if (p.k > 0 && p.k <= kListK) {
+        const int length = short_list(p, team, e, &lists->hosts);
         if (length >= 0) {
             team.sync();
             if (team.me != 0) return;
-            team.warps = team.cs = 1;
-            e.store = e.block_store = list->x, e.chunks = (length + kChunk - 1) / kChunk, e.first = 0, e.n = length;
-            hosts = list->col;
+            unsigned int key[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                key[j] = lane + 32 * j < length ? key_of(__uint_as_float(lists->hosts.x[lane + 32 * j]) + 0.0f) : 0u;
+            finish(a, row, p, key, lane, lists->hosts.col);
+            return;
         }
     }
-    decide(a, row, x, p, team, e, &list->sort, hosts);
+    decide(a, row, x, p, team, e, &lists->sort);
+}
+
+// rows of at most 128 hosts: one warp per row, in registers
+template <typename T>
+__global__ void __launch_bounds__(128) sample_short_kernel(SampleArgs a)
+{
+    const int lane = threadIdx.x & 31;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= a.rows) return;
+    const T *x = static_cast<const T *>(a.x) + row * a.stride;
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = lane + 32 * j < a.n ? to_float(x[lane + 32 * j]) : neg_inf();
+    Row p = row_settings(a, row);
+    unsigned int key[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j] = fminf(fmaxf(v[j], neg_inf()), kMaxFinite);   // NaN as -inf
+        p.m = fmaxf(p.m, v[j]);
+        key[j] = v[j] > neg_inf() ? key_of(v[j] + 0.0f) : 0u;
+    }
+    p.m = lanes_max(p.m, 32);
+    if (p.greedy && p.m > neg_inf()) {
+        int col = -1;
+#pragma unroll
+        for (int j = 3; j >= 0; --j) {
+            const unsigned int here = __ballot_sync(kFull, v[j] == p.m);
+            if (here) col = 32 * j + __ffs(here) - 1;
+        }
+        if (lane == 0) write_one(a, row, col);
+        return;
+    }
+    finish(a, row, p, key, lane, nullptr);
 }
 
 // one warp per row; shared memory per warp: the row, the lists
@@ -703,9 +873,9 @@ __global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a, int chun
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * 4 + warp;
     if (row >= a.rows) return;
-    ShortList *list = reinterpret_cast<ShortList *>(s_mem + warp * warp_bytes);
+    Lists *lists = reinterpret_cast<Lists *>(s_mem + warp * warp_bytes);
     unsigned int *store = reinterpret_cast<unsigned int *>(s_mem + (warp + 1) * warp_bytes) - chunks * kChunk;
-    sample_row<T>(a, row, Team{nullptr, 1, 1, 0, lane, 0}, Elems{store, chunks, 0, a.n, store, 0}, list);
+    sample_row<T>(a, row, Team{nullptr, 1, 1, 0, lane, 0}, Elems{store, chunks, 0, a.n, store, 0}, lists);
 }
 
 // grid: SHARED one block / cluster per row; else as many as the workspace has rows take them in turn
@@ -714,7 +884,7 @@ __global__ void __launch_bounds__(1024, 1) sample_block_kernel(SampleArgs a, int
 {
     extern __shared__ __align__(16) char s_mem[];
     __shared__ ulonglong2 s_slots[2][kMaxCluster * 32];
-    __shared__ ShortList s_list;
+    __shared__ Lists s_lists;
     const int rank = cluster_rank(cs), warps = blockDim.x >> 5, warp = threadIdx.x >> 5;
     const Team team{s_slots, warps * cs, cs, rank * warps + warp, (int)(threadIdx.x & 31), 0};
     const long long first = blockIdx.x / cs, step = gridDim.x / cs;
@@ -724,7 +894,7 @@ __global__ void __launch_bounds__(1024, 1) sample_block_kernel(SampleArgs a, int
     unsigned int *store = block_store + warp * span;
     cluster_sync(cs);   // all blocks of the cluster run
     for (long long row = first; row < a.rows; row += step) {
-        sample_row<T>(a, row, team, Elems{store, chunks, team.me * span, a.n, SHARED ? block_store : block_store - (size_t)rank * span * warps, SHARED ? span * warps : 1 << 30}, &s_list);
+        sample_row<T>(a, row, team, Elems{store, chunks, team.me * span, a.n, SHARED ? block_store : block_store - (size_t)rank * span * warps, SHARED ? span * warps : 1 << 30}, &s_lists);
         cluster_sync(cs);   // slots and lists are free again
     }
 }
@@ -732,11 +902,13 @@ __global__ void __launch_bounds__(1024, 1) sample_block_kernel(SampleArgs a, int
 template <typename T>
 cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
 {
+    if (a.n <= kList) {
+        sample_short_kernel<T><<<(unsigned int)((a.rows + 3) / 4), 128, 0, stream>>>(a);
+        return cudaGetLastError();
+    }
     if (a.n <= kWarpRow) {
         const int chunks = (a.n + kChunk - 1) / kChunk;
-        // short rows make no list of hosts, only the sorted one
-        const int lists = a.n > kList ? (int)sizeof(ShortList) : (int)sizeof(SortList);
-        const int warp_bytes = lists + chunks * kChunk * 4;
+        const int warp_bytes = (int)sizeof(Lists) + chunks * kChunk * 4;
         sample_warp_kernel<T><<<(unsigned int)((a.rows + 3) / 4), 128, 4 * warp_bytes, stream>>>(a, chunks, warp_bytes);
         return cudaGetLastError();
     }
