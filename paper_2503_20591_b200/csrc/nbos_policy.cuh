@@ -74,24 +74,38 @@ __device__ __forceinline__ uint4 pack16(const float (&v)[8], __half)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// four neighbours that start on a boundary of four elements
-__device__ __forceinline__ void load4(const float *p, float (&v)[4])
-{
-    const float4 f = __ldcs(reinterpret_cast<const float4 *>(p));
-    v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&v)[4])
-{
-    const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p));
-    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
-    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
-}
-__device__ __forceinline__ void load4(const __half *p, float (&v)[4])
-{
-    const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p));
-    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&u.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&u.y));
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
-}
+// four neighbouring elements as they are in memory, from a boundary of four elements
+template <typename T> struct Raw4;
+template <> struct Raw4<float> {
+    float4 v;
+    __device__ __forceinline__ void load(const float *p) { v = __ldcs(reinterpret_cast<const float4 *>(p)); }
+    __device__ __forceinline__ void set(int i, float x) { (i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w) = x; }
+    __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w; }
+};
+template <typename T> struct Raw4Half {
+    uint2 v;
+    __device__ __forceinline__ void load(const T *p) { v = __ldcs(reinterpret_cast<const uint2 *>(p)); }
+    __device__ __forceinline__ void set(int i, T x)
+    {
+        const unsigned int b = *reinterpret_cast<const unsigned short *>(&x);
+        unsigned int &w = i < 2 ? v.x : v.y;
+        w = i % 2 ? (w & 0xFFFFu) | (b << 16) : (w & 0xFFFF0000u) | b;
+    }
+};
+template <> struct Raw4<__nv_bfloat16> : Raw4Half<__nv_bfloat16> {
+    __device__ __forceinline__ void get(float (&f)[4]) const
+    {
+        f[0] = __uint_as_float(v.x << 16), f[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        f[2] = __uint_as_float(v.y << 16), f[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    }
+};
+template <> struct Raw4<__half> : Raw4Half<__half> {
+    __device__ __forceinline__ void get(float (&f)[4]) const
+    {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&v.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&v.y));
+        f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
+    }
+};
 
 // VEC consecutive elements of a row from column `col`; columns from `end` on read as `fill`. VEC is 16 bytes'
 // worth (the row then starts on a 16-byte boundary and col is a multiple of VEC) or 1 (any alignment).

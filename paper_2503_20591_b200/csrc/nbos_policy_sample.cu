@@ -582,16 +582,17 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
     if (a.found && team.me == 0 && lane == 0) a.found[row] = found;
 }
 
-// descending over the positions lane + 32 j, a bitonic network
-__device__ __forceinline__ void sort128(unsigned int (&s)[4], int lane)
+// descending over the positions lane + 32 j, j < R, a bitonic network
+template <int R>
+__device__ __forceinline__ void sort_places(unsigned int (&s)[4], int lane)
 {
 #pragma unroll
-    for (int k = 2; k <= 128; k *= 2)
+    for (int k = 2; k <= 32 * R; k *= 2)
 #pragma unroll
         for (int d = k / 2; d > 0; d /= 2) {
             if (d >= 32) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < R; ++j) {
                     const int o = j ^ (d / 32);
                     if (o < j) continue;
                     const unsigned int hi = max(s[j], s[o]), lo = min(s[j], s[o]);
@@ -601,7 +602,7 @@ __device__ __forceinline__ void sort128(unsigned int (&s)[4], int lane)
             } else {
                 const bool first = (lane & d) == 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < R; ++j) {
                     const unsigned int other = __shfl_xor_sync(kFull, s[j], d);
                     s[j] = (((lane + 32 * j) & k) == 0) == first ? max(s[j], other) : min(s[j], other);
                 }
@@ -609,9 +610,9 @@ __device__ __forceinline__ void sort128(unsigned int (&s)[4], int lane)
         }
 }
 
-// Filters and draws of at most 128 hosts, in index order over the positions lane + 32 j: key[j] orders the logit there,
+// Filters and draws of `places` (at most 128) hosts, in index order over the positions lane + 32 j: key[j] orders the logit there,
 // 0 = no host. cols[position] names the host; NULL: the position does.
-__device__ __forceinline__ void finish(const SampleArgs &a, long long row, const Row &p, unsigned int (&key)[4], int lane, const int *cols)
+__device__ __forceinline__ void finish(const SampleArgs &a, long long row, const Row &p, unsigned int (&key)[4], int places, int lane, const int *cols)
 {
     const unsigned int below = (1u << lane) - 1;
     unsigned int s[4], hosts = 0;
@@ -621,7 +622,12 @@ __device__ __forceinline__ void finish(const SampleArgs &a, long long row, const
         hosts += __popc(__ballot_sync(kFull, key[j] != 0));
     }
     const bool cut_k = p.k > 0 && p.k < (int)hosts;
-    if (cut_k || p.top_p < 1.0f) sort128(s, lane);
+    if (cut_k || p.top_p < 1.0f) {   // places above the last host hold 0 already
+        if (places <= 32)
+            sort_places<1>(s, lane);
+        else
+            sort_places<4>(s, lane);
+    }
     auto at_place = [&](unsigned int i) {
         const unsigned int v = i < 64 ? (i < 32 ? s[0] : s[1]) : (i < 96 ? s[2] : s[3]);
         return __shfl_sync(kFull, v, i & 31);
@@ -783,20 +789,29 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
     const int lane = team.lane;
     Row p = row_settings(a, row);
 
-    // a NaN is never the larger, nor above any bound, and has weight 0
+    // all of a warp's loads in flight at once; a NaN is never the larger, nor above any bound, and has weight 0
     float m = neg_inf();
-#pragma unroll 4
-    for (int c = 0; c < e.chunks; ++c) {
-        const int col = e.first + c * kChunk + lane * 4;
-        float v[4];
-        if (a.aligned && col + 4 <= a.n) {
-            load4(x + col, v);
-        } else {
+    for (int c0 = 0; c0 < e.chunks; c0 += kWarpChunks) {
+        Raw4<T> raw[kWarpChunks];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = col + i < a.n ? to_float(x[col + i]) : neg_inf();
+        for (int c = 0; c < kWarpChunks; ++c) {
+            const int col = e.first + (c0 + c) * kChunk + lane * 4;
+            if (c0 + c >= e.chunks) break;
+            if (a.aligned && col + 4 <= a.n) {
+                raw[c].load(x + col);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[c].set(i, col + i < a.n ? x[col + i] : from_float<T>(neg_inf()));
+            }
         }
-        m = fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
-        e.at(c, lane) = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+#pragma unroll
+        for (int c = 0; c < kWarpChunks; ++c) {
+            if (c0 + c >= e.chunks) break;
+            float v[4];
+            raw[c].get(v);
+            m = fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
+            e.at(c0 + c, lane) = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        }
     }
     p.m = team.max_of(m);
     if (p.m == neg_inf()) {
@@ -825,7 +840,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 key[j] = lane + 32 * j < length ? key_of(__uint_as_float(lists->hosts.x[lane + 32 * j]) + 0.0f) : 0u;
-            finish(a, row, p, key, lane, lists->hosts.col);
+            finish(a, row, p, key, length, lane, lists->hosts.col);
             return;
         }
     }
@@ -862,7 +877,7 @@ __global__ void __launch_bounds__(128) sample_short_kernel(SampleArgs a)
         if (lane == 0) write_one(a, row, col);
         return;
     }
-    finish(a, row, p, key, lane, nullptr);
+    finish(a, row, p, key, a.n, lane, nullptr);
 }
 
 // one warp per row; shared memory per warp: the row, the lists
