@@ -156,11 +156,73 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes)
     return v;
 }
 
+// 2^y to 2 ulp; results below the smallest normal number are 0
+__device__ __forceinline__ float exp2_fast(float y)
+{
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(y));
+    return e;
+}
 // 2^((x - m) c); 0 where x is -inf even if m is -inf (a row without a finite logit). The subtraction comes
 // first: near the row's maximum, where the result matters, it is exact or nearly so.
 __device__ __forceinline__ float exp_from(float x, float m, float c)
 {
-    return exp2f((x - (m == neg_inf() ? 0.0f : m)) * c);
+    return exp2_fast((x - (m == neg_inf() ? 0.0f : m)) * c);
+}
+__device__ __forceinline__ float reciprocal(float x) { return __fdividef(1.0f, x); }   // 2 ulp
+
+// ---- rows staged in shared memory by asynchronous copies ----------------------------------------------------
+constexpr int kStages = 3;   // rows on their way or in use per team (a warp, or a block)
+
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void *src, int bytes)   // the rest of the 16 becomes 0
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_async4(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
+
+// Bytes between the 16-byte boundary before a row and the row itself; they are staged along.
+template <typename T, int VEC>
+__device__ __forceinline__ int row_shift(const T *row)
+{
+    return VEC == 1 ? (int)(reinterpret_cast<uintptr_t>(row) & 15) : 0;
+}
+// Queues the copies of n elements from `row` to `dst` (16-byte aligned; the row itself lands row_shift bytes further),
+// thread `sub` of `team`. The bytes before an unaligned row belong to the rows before it (or the gaps between them);
+// where the table does not have that many (`offset`: the row's, in bytes), the first, partial 16 bytes go element by
+// element.
+template <typename T, int VEC>
+__device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long long offset, int sub, int team)
+{
+    const int shift = row_shift<T, VEC>(row), total = shift + n * (int)sizeof(T);
+    const char *src = reinterpret_cast<const char *>(row) - shift;
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
+    int g = sub;
+    if (VEC == 1 && offset < shift) {
+        for (int i = sub; i < n && shift + (i + 1) * (int)sizeof(T) <= 16; i += team) reinterpret_cast<T *>(dst + shift)[i] = row[i];
+        g += team;
+        if (sub != 0) g = sub;   // pieces 1, 2, ... of 16 bytes; thread 0 starts at `team`
+    }
+    for (; g * 16 < total; g += team) copy_async16(to + g * 16, src + g * 16, total - g * 16 < 16 ? total - g * 16 : 16);
+}
+// VEC elements of a staged row from column `col`; from n on they read as -inf
+template <typename T, int VEC>
+__device__ __forceinline__ void staged_cols(const T *row, int col, int n, float (&v)[VEC])
+{
+    if constexpr (VEC == 1) {
+        v[0] = col < n ? to_float(row[col]) : neg_inf();
+    } else {
+        if (col + VEC <= n) {
+            unpack16(*reinterpret_cast<const uint4 *>(row + col), v, T());
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = col + i < n ? to_float(row[col + i]) : neg_inf();
+        }
+    }
 }
 
 // ---- blocks that share a row: a cluster of `cs` blocks, or one block (cs = 1) ------------------------------
@@ -231,6 +293,26 @@ inline int check_sm100(int *sms, int *device)
     if (major != 10) return fail(NBOS_ERR_UNSUPPORTED_DEVICE, "device %d has compute capability %d.x", *device, major);
     NBOS_CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device));
     return NBOS_OK;
+}
+// Blocks of a kernel that an SM holds at once: what a persistent grid is sized by. regs: the kernel's registers.
+inline int resident_blocks(int regs, int threads, size_t shared)
+{
+    const int by_regs = 65536 / (((regs + 7) & ~7) * threads);
+    const int by_shared = (int)((228 * 1024) / (shared + 1024));
+    const int by_threads = 2048 / threads;
+    int n = by_regs < by_shared ? by_regs : by_shared;
+    n = n < by_threads ? n : by_threads;
+    return n < 1 ? 1 : n;
+}
+template <typename K>
+inline int kernel_registers(K *kernel)
+{
+    cudaFuncAttributes attr;
+    if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess) {
+        cudaGetLastError();
+        return 128;
+    }
+    return attr.numRegs;
 }
 // every row of `p` starts on a 16-byte boundary
 inline bool rows_aligned16(const void *p, int64_t rows, int64_t stride, size_t elem)

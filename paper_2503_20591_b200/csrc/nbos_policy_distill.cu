@@ -5,8 +5,9 @@
 //   loss = T^2 sum_k q_k (ln q_k - ln p_k),  d loss / d x_j = T (p_j - q_j).
 // What bounds it: the logits' bytes, read once, and as many written for the gradient. So a row stays in registers
 // between its reduction and its gradient (32 elements a thread): a power of two of lanes of one warp share a short
-// row (up to 1,024 hosts), a block or a cluster of up to 8 blocks a longer one; only rows of more than 262,144
-// hosts are read twice. Each exponential is computed once; threads keep it relative to their warp's maximum and
+// row (up to 1,024 hosts), a block a longer one (up to 16,384). Both stay on their SM and walk over the rows, with the
+// next two rows on their way to shared memory by asynchronous copies. Longer rows, or few of them, take a cluster
+// of up to 8 blocks each; only rows of more than 262,144 hosts are read twice. Each exponential is computed once; threads keep it relative to their warp's maximum and
 // scale it by 2^((m_warp - m) c) / S when the row's statistics are known.
 #include <math.h>
 
@@ -85,7 +86,7 @@ __device__ __forceinline__ float row_loss(const DistillArgs &a, long long row, c
     for (int k = sub; active && k < a.k; k += lanes) {
         const Entry e = k == sub ? first : load_entry(a, row, x, k);
         if (e.host < 0) continue;
-        const float q = exp_from(e.t, tm, a.c) / z;
+        const float q = exp_from(e.t, tm, a.c) * reciprocal(z);
         // q underflows to 0 before ln q leaves the range of 32 bits; 0 * -inf is kept out
         const float v = q * (((e.t - tm) - (e.x - m)) * a.inv_t + shift);
         l += q == 0.0f ? 0.0f : v;
@@ -102,9 +103,9 @@ __device__ __forceinline__ void fix_entries(const DistillArgs &a, long long row,
     for (int k = 0; k < a.k; ++k) {
         if (a.hosts[row * a.k + k] != e.host) continue;
         const float t = a.teacher ? a.teacher[row * a.tstride + k] : 0.0f;
-        if (t > neg_inf()) q += exp_from(t, tm, a.c) / z;
+        if (t > neg_inf()) q += exp_from(t, tm, a.c) * reciprocal(z);
     }
-    grad[e.host] = from_float<T>(gmul * (exp_from(e.x, m, a.c) / s - q));
+    grad[e.host] = from_float<T>(gmul * (exp_from(e.x, m, a.c) * reciprocal(s) - q));
 }
 
 __device__ __forceinline__ float grad_multiplier(const DistillArgs &a, long long row)
@@ -112,66 +113,320 @@ __device__ __forceinline__ float grad_multiplier(const DistillArgs &a, long long
     return a.T * a.grad_scale * (a.grad_loss ? a.grad_loss[row] : 1.0f);
 }
 
-// ---- warp form: `lanes` lanes per row, CH * VEC elements each ----------------------------------------------
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
-__global__ void __launch_bounds__(128) distill_warp_kernel(DistillArgs a, int lanes)
+// ---- rows that a warp or a block holds, staged -------------------------------------------------------------
+// What a team needs of one row, in shared memory: the row, its entries, (grad_loss, m, S).
+template <typename T>
+struct Staged {
+    const T *x;
+    const int *hosts;
+    const float *teacher, *given;
+    int n, k;
+    bool has_teacher;
+    __device__ __forceinline__ Entry entry(int i) const
+    {
+        Entry e;
+        e.host = hosts[i];
+        e.t = has_teacher ? teacher[i] : 0.0f;
+        e.x = neg_inf();
+        if (e.host >= 0 && e.host < n) e.x = to_float(x[e.host]);
+        // comparisons with NaN are false: a NaN teacher logit does not count; a NaN student logit does
+        if (!(e.t > neg_inf()) || e.x == neg_inf()) e.host = -1;
+        return e;
+    }
+};
+struct Layout {   // bytes of a stage: rows, then entries, then what is given per row
+    int row_bytes, rows, k;
+    __host__ __device__ int hosts_at() const { return row_bytes * rows; }
+    __host__ __device__ int teacher_at() const { return hosts_at() + rows * k * 4; }
+    __host__ __device__ int given_at() const { return teacher_at() + rows * k * 4; }
+    __host__ __device__ int bytes() const { return (given_at() + rows * 12 + 15) & ~15; }
+};
+
+template <typename T, int VEC, bool GRAD, bool SAVED>
+__device__ __forceinline__ void stage(const DistillArgs &a, const Layout &lay, char *at, int slot, long long row, int sub, int team)
 {
-    const int lane = threadIdx.x & 31, sub = lane & (lanes - 1);
-    const long long warp = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    const long long row = warp * (32 / lanes) + lane / lanes;
-    const bool active = row < a.rows;
-    const T *x = static_cast<const T *>(a.x) + (active ? row : 0) * a.stride;
-    Entry first{-1, 0.0f, 0.0f};
-    float v[CH][VEC];
+    const T *x = static_cast<const T *>(a.x) + row * a.stride;
+    stage_row<T, VEC>(at + slot * lay.row_bytes, x, a.n, row * a.stride * (long long)sizeof(T), sub, team);
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at));
+    for (int i = sub; i < a.k; i += team) {
+        copy_async4(to + lay.hosts_at() + (slot * a.k + i) * 4, a.hosts + row * a.k + i);
+        if (a.teacher) copy_async4(to + lay.teacher_at() + (slot * a.k + i) * 4, a.teacher + row * a.tstride + i);
+    }
+    if (sub == 0) {
+        if (GRAD && a.grad_loss) copy_async4(to + lay.given_at() + slot * 12, a.grad_loss + row);
+        if (SAVED) {
+            copy_async4(to + lay.given_at() + slot * 12 + 4, a.stats_in + 2 * row);
+            copy_async4(to + lay.given_at() + slot * 12 + 8, a.stats_in + 2 * row + 1);
+        }
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Staged<T> staged_row(const DistillArgs &a, const Layout &lay, const char *at, int slot, long long row)
+{
+    Staged<T> s;
+    s.x = reinterpret_cast<const T *>(at + slot * lay.row_bytes + row_shift<T, VEC>(static_cast<const T *>(a.x) + row * a.stride));
+    s.hosts = reinterpret_cast<const int *>(at + lay.hosts_at()) + slot * a.k;
+    s.teacher = reinterpret_cast<const float *>(at + lay.teacher_at()) + slot * a.k;
+    s.given = reinterpret_cast<const float *>(at + lay.given_at()) + slot * 3;
+    s.n = a.n, s.k = a.k, s.has_teacher = a.teacher != nullptr;
+    return s;
+}
+
+// largest teacher logit of the row (-inf: no entry counts) and the sum of its softmax, over `lanes` lanes
+template <typename T>
+__device__ __forceinline__ void teacher_sums(const DistillArgs &a, const Staged<T> &r, bool active, int sub, int lanes, float &tm, float &z)
+{
+    tm = neg_inf();
+    for (int i = sub; active && i < a.k; i += lanes) {
+        const Entry e = r.entry(i);
+        if (e.host >= 0) tm = fmaxf(tm, e.t);
+    }
+    tm = lanes_max(tm, lanes);
+    z = 0.0f;
+    for (int i = sub; active && i < a.k; i += lanes) {
+        const Entry e = r.entry(i);
+        if (e.host >= 0) z += exp_from(e.t, tm, a.c);
+    }
+    z = lanes_sum(z, lanes);
+}
+template <typename T>
+__device__ __forceinline__ float entries_loss(const DistillArgs &a, const Staged<T> &r, bool active, int sub, int lanes, float tm, float z, float m, float s)
+{
+    const float shift = logf(s) - logf(z);
+    float l = 0.0f;
+    for (int i = sub; active && i < a.k; i += lanes) {
+        const Entry e = r.entry(i);
+        if (e.host < 0) continue;
+        const float q = exp_from(e.t, tm, a.c) * reciprocal(z);
+        // q underflows to 0 before ln q leaves the range of 32 bits; 0 * -inf is kept out
+        const float v = q * (((e.t - tm) - (e.x - m)) * a.inv_t + shift);
+        l += q == 0.0f ? 0.0f : v;
+    }
+    return lanes_sum(l, lanes) * a.T * a.T;
+}
+// the gradient at an entry's host: p - (all of q that goes there)
+template <typename T>
+__device__ __forceinline__ float entry_grad(const DistillArgs &a, const Staged<T> &r, const Entry &e, float tm, float z, float m, float s, float gmul)
+{
+    float q = 0.0f;
+    for (int i = 0; i < a.k; ++i) {
+        const float t = r.has_teacher ? r.teacher[i] : 0.0f;
+        if (r.hosts[i] == e.host && t > neg_inf()) q += exp_from(t, tm, a.c) * reciprocal(z);
+    }
+    return gmul * (exp_from(e.x, m, a.c) * reciprocal(s) - q);
+}
+
+// ---- warp form: `lanes` lanes per row, CH * VEC elements each; the grid stays and walks over the rows -------
+constexpr int kWarps = 8;
+
+template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
+__global__ void __launch_bounds__(kWarps * 32, 2) distill_warp_kernel(DistillArgs a, int lanes, int entry_lanes, Layout lay)
+{
+    extern __shared__ __align__(16) char s_mem[];
+    const int lane = threadIdx.x & 31, sub = lane & (lanes - 1), slot = lane / lanes, at_once = 32 / lanes;
+    const int stage_bytes = lay.bytes();
+    char *mine = s_mem + (threadIdx.x >> 5) * kStages * stage_bytes;
+    const long long step = (long long)gridDim.x * kWarps * at_once;
+    const long long row0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * at_once;
+    auto queue = [&](long long base, int st) {
+        if (base + slot < a.rows) stage<T, VEC, GRAD, SAVED>(a, lay, mine + st * stage_bytes, slot, base + slot, sub, lanes);
+        copies_commit();
+    };
 #pragma unroll
-    for (int c = 0; c < CH; ++c) load_cols<T, VEC>(x, (c * lanes + sub) * VEC, active ? a.n : 0, neg_inf(), v[c]);
-    if (active && sub < a.k) first = load_entry(a, row, x, sub);
-    float m, s;
-    if (SAVED) {
-        m = active ? a.stats_in[2 * row] : 0.0f;
-        s = active ? a.stats_in[2 * row + 1] : 1.0f;
-    } else {
-        m = neg_inf();
+    for (int st = 0; st < kStages - 1; ++st) queue(row0 + st * step, st);
+    int st = 0;
+    for (long long base = row0; base < a.rows; base += step) {
+        queue(base + (kStages - 1) * step, st == 0 ? kStages - 1 : st - 1);
+        copies_wait();
+        __syncwarp();
+        const bool active = base + slot < a.rows;
+        const long long row = active ? base + slot : base;
+        const Staged<T> r = staged_row<T, VEC>(a, lay, mine + st * stage_bytes, active ? slot : 0, row);
+        float v[CH][VEC];
+        float m = neg_inf(), s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            staged_cols<T, VEC>(r.x, (c * lanes + sub) * VEC, a.n, v[c]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
+        }
+        m = SAVED ? r.given[1] : lanes_max(m, lanes);
+        const float m0 = m == neg_inf() ? 0.0f : m;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
-        m = lanes_max(m, lanes);
-    }
-    float sum = 0.0f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            v[c][i] = exp_from(v[c][i], m, a.c);
-            sum += v[c][i];
+            for (int i = 0; i < VEC; ++i) {
+                v[c][i] = exp2_fast((v[c][i] - m0) * a.c);
+                s += v[c][i];
+            }
+        s = SAVED ? r.given[2] : lanes_sum(s, lanes);
+        const float inv_s = reciprocal(s);
+        const float gmul = GRAD ? a.T * a.grad_scale * (a.grad_loss ? r.given[0] : 1.0f) : 0.0f;
+        float tm = neg_inf(), z = 0.0f, entry_g = 0.0f, l = 0.0f;
+        Entry e{-1, 0.0f, 0.0f};   // k <= lanes: the lane's entry
+        bool any;
+        if (a.k <= lanes) {
+            if (active && sub < a.k) e = r.entry(sub);
+            const unsigned int group = lanes == 32 ? kFull : ((1u << lanes) - 1) << (slot * lanes);
+            any = (__ballot_sync(kFull, e.host >= 0) & group) != 0;
+            // the entries are in the group's first entry_lanes lanes
+            tm = lanes_max(e.host >= 0 ? e.t : neg_inf(), entry_lanes);
+            float q = e.host >= 0 ? exp2_fast((e.t - tm) * a.c) : 0.0f;
+            z = lanes_sum(q, entry_lanes);
+            q *= reciprocal(z);
+            // q underflows to 0 before ln q leaves the range of 32 bits; 0 * -inf is kept out
+            if (!SAVED) {
+                l = q * (((e.t - tm) - (e.x - m0)) * a.inv_t + logf(s * reciprocal(z)));
+                l = lanes_sum(e.host < 0 || q == 0.0f ? 0.0f : l, entry_lanes) * a.T * a.T;
+            }
+            if (GRAD) {
+                float all = 0.0f;   // a host may be listed more than once
+                for (int i = 0; i < a.k; ++i) {
+                    const float other = __shfl_sync(kFull, q, i, lanes);
+                    if (__shfl_sync(kFull, e.host, i, lanes) == e.host) all += other;
+                }
+                entry_g = gmul * (exp2_fast((e.x - m0) * a.c) * inv_s - all);
+            }
+        } else {
+            teacher_sums(a, r, active, sub, lanes, tm, z);
+            any = tm > neg_inf();
+            if (!SAVED) l = entries_loss(a, r, active && any, sub, lanes, tm, z, m, s);
         }
-    if (!SAVED) s = lanes_sum(sum, lanes);
-    float tm, z;
-    teacher_stats(a, row, x, active, sub, lanes, first, tm, z);
-    const bool any = tm > neg_inf();
-    if (!SAVED) {
-        const float l = row_loss(a, row, x, active && any, sub, lanes, first, tm, z, m, s);
-        if (active && sub == 0) {
+        if (!SAVED && active && sub == 0) {
             if (a.loss) a.loss[row] = any ? l : 0.0f;
             if (a.stats) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
         }
+        if (GRAD) {
+            T *grad = static_cast<T *>(a.grad) + row * a.gstride;
+            const float fac = gmul * inv_s;
+            if (__any_sync(kFull, !any)) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) v[c][i] = any ? v[c][i] : 0.0f;
+            }
+            const float fac0 = any ? fac : 0.0f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[c][i] *= fac0;
+                store_cols<T, VEC>(grad, (c * lanes + sub) * VEC, active ? a.n : 0, v[c]);
+            }
+            __syncwarp();   // the listed hosts' gradients go over what their columns' lanes wrote
+            if (a.k <= lanes) {
+                if (e.host >= 0) grad[e.host] = from_float<T>(entry_g);
+            } else {
+                for (int i = sub; active && i < a.k; i += lanes) {
+                    const Entry o = r.entry(i);
+                    if (o.host >= 0) grad[o.host] = from_float<T>(entry_grad(a, r, o, tm, z, m, s, gmul));
+                }
+            }
+        }
+        __syncwarp();   // the stage may be filled again
+        st = st == kStages - 1 ? 0 : st + 1;
     }
-    if (GRAD) {
-        T *grad = static_cast<T *>(a.grad) + (active ? row : 0) * a.gstride;
-        const float gmul = active ? grad_multiplier(a, row) : 0.0f;
-        const float fac = gmul / s;
-        __syncwarp();   // a gradient written over the logits: the entries' logits have been read
+}
+
+// ---- block form: one row at a time per block, kElems elements a thread -------------------------------------
+__device__ __forceinline__ void merge_stats(float &m, float &s, float m2, float s2, float c);
+
+template <typename T, int VEC, bool GRAD, bool SAVED>
+__global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, Layout lay)
+{
+    constexpr int CH = kElems / VEC;
+    extern __shared__ __align__(16) char s_mem[];
+    __shared__ float2 s_stats[2][16];
+    __shared__ float s_fix[NBOS_POLICY_MAX_K];
+    __shared__ int s_fix_host[NBOS_POLICY_MAX_K];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int chunk = blockDim.x * VEC, stage_bytes = lay.bytes();
+    auto queue = [&](long long row, int st) {
+        if (row < a.rows) stage<T, VEC, GRAD, SAVED>(a, lay, s_mem + st * stage_bytes, 0, row, threadIdx.x, blockDim.x);
+        copies_commit();
+    };
+#pragma unroll
+    for (int st = 0; st < kStages - 1; ++st) queue(blockIdx.x + (long long)st * gridDim.x, st);
+    int st = 0, turn = 0;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        queue(row + (kStages - 1) * (long long)gridDim.x, st == 0 ? kStages - 1 : st - 1);
+        copies_wait();
+        const Staged<T> r = staged_row<T, VEC>(a, lay, s_mem + st * stage_bytes, 0, row);
+        // 16 bytes a thread has copied itself; single elements came through other threads
+        if (VEC == 1 || SAVED) __syncthreads();
+        float v[CH][VEC];
+        float m = neg_inf(), s = 0.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
+            staged_cols<T, VEC>(r.x, c * chunk + threadIdx.x * VEC, a.n, v[c]);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) v[c][i] = any ? v[c][i] * fac : 0.0f;
-            store_cols<T, VEC>(grad, (c * lanes + sub) * VEC, active ? a.n : 0, v[c]);
+            for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
         }
-        __syncwarp();
-        // entries beyond the lanes re-read their logits, which a gradient written over them has replaced: those
-        // are taken from the statistics' side instead (see the block form, which such k always use)
-        if (active && first.host >= 0) fix_entries(a, row, x, first, grad, tm, z, m, s, gmul);
+        m = SAVED ? r.given[1] : lanes_max(m, 32);
+        const float m_warp = m;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                v[c][i] = exp_from(v[c][i], m, a.c);
+                s += v[c][i];
+            }
+        if (SAVED) {
+            s = r.given[2];
+        } else {
+            s = lanes_sum(s, 32);
+            if (lane == 0) s_stats[turn][warp] = make_float2(m, s);
+            __syncthreads();
+            const float2 w = lane < warps ? s_stats[turn][lane] : make_float2(neg_inf(), 0.0f);
+            m = lanes_max(w.x, 16);
+            m = __shfl_sync(kFull, m, 0);
+            s = lanes_sum(w.y * exp_from(w.x, m, a.c), 16);
+            s = __shfl_sync(kFull, s, 0);
+        }
+        // every warp finds out whether an entry counts; the first one does what is to be done with them
+        float tm = neg_inf();
+        for (int i = lane; i < a.k; i += 32) {
+            const Entry e = r.entry(i);
+            if (e.host >= 0) tm = fmaxf(tm, e.t);
+        }
+        tm = lanes_max(tm, 32);
+        const bool any = tm > neg_inf();
+        const float gmul = a.T * a.grad_scale * (GRAD && a.grad_loss ? r.given[0] : 1.0f);
+        if (warp == 0) {
+            float z = 0.0f;
+            for (int i = lane; i < a.k; i += 32) {
+                const Entry e = r.entry(i);
+                if (e.host >= 0) z += exp_from(e.t, tm, a.c);
+            }
+            z = lanes_sum(z, 32);
+            if (!SAVED) {
+                const float l = entries_loss(a, r, any, lane, 32, tm, z, m, s);
+                if (lane == 0) {
+                    if (a.loss) a.loss[row] = any ? l : 0.0f;
+                    if (a.stats) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+                }
+            }
+            for (int i = lane; GRAD && any && i < a.k; i += 32) {
+                const Entry e = r.entry(i);
+                s_fix_host[i] = e.host;
+                if (e.host >= 0) s_fix[i] = entry_grad(a, r, e, tm, z, m, s, gmul);
+            }
+        }
+        if (GRAD) {
+            T *grad = static_cast<T *>(a.grad) + row * a.gstride;
+            const float fac = gmul * reciprocal(s) * (SAVED ? 1.0f : exp_from(m_warp, m, a.c));
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[c][i] = any ? v[c][i] * fac : 0.0f;
+                store_cols<T, VEC>(grad, c * chunk + threadIdx.x * VEC, a.n, v[c]);
+            }
+            __syncthreads();   // the listed hosts' gradients go over what others wrote; the stage may be filled again
+            for (int i = lane; warp == 0 && any && i < a.k; i += 32)
+                if (s_fix_host[i] >= 0) grad[s_fix_host[i]] = from_float<T>(s_fix[i]);
+        } else {
+            __syncthreads();   // the stage may be filled again
+        }
+        st = st == kStages - 1 ? 0 : st + 1;
     }
 }
 
@@ -282,7 +537,7 @@ __global__ void __launch_bounds__(1024, 1) distill_block_kernel(DistillArgs a, i
     if (GRAD) {
         T *grad = static_cast<T *>(a.grad) + row * a.gstride;
         const float gmul = grad_multiplier(a, row);
-        const float fac = KEEP ? gmul / s * exp_from(m_warp, m, a.c) : gmul / s;
+        const float fac = gmul * reciprocal(s) * (KEEP ? exp_from(m_warp, m, a.c) : 1.0f);
         if (a.k > 32) cluster_sync(cs);   // row_loss has re-read logits that the next lines may write over
         if (KEEP) {
 #pragma unroll
@@ -312,33 +567,63 @@ __global__ void __launch_bounds__(1024, 1) distill_block_kernel(DistillArgs a, i
     }
 }
 
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
-cudaError_t launch_warp(const DistillArgs &a, int lanes, cudaStream_t stream)
+template <typename T, int VEC>
+int row_bytes(int n)   // of a staged row, with what precedes an unaligned one
 {
-    const long long rows_per_block = (128 / 32) * (32 / lanes);
-    const long long blocks = (a.rows + rows_per_block - 1) / rows_per_block;
-    distill_warp_kernel<T, VEC, CH, GRAD, SAVED><<<(unsigned int)blocks, 128, 0, stream>>>(a, lanes);
+    return (n * (int)sizeof(T) + (VEC == 1 ? 15 : 0) + 15) & ~15;
+}
+template <typename K>
+cudaError_t allow_shared(K *kernel, int bytes)
+{
+    return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+}
+
+template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
+cudaError_t launch_warp(const DistillArgs &a, int lanes, int sms, cudaStream_t stream)
+{
+    auto *kernel = distill_warp_kernel<T, VEC, CH, GRAD, SAVED>;
+    static const int regs = kernel_registers(kernel);
+    int entry_lanes = 1;
+    while (entry_lanes < a.k && entry_lanes < lanes) entry_lanes *= 2;
+    const Layout lay{row_bytes<T, VEC>(a.n), 32 / lanes, a.k};
+    const int shared = kWarps * kStages * lay.bytes();
+    const cudaError_t e = allow_shared(kernel, shared);
+    if (e != cudaSuccess) return e;
+    const long long per_block = kWarps * (32 / lanes), wanted = (a.rows + per_block - 1) / per_block;
+    const long long fit = (long long)sms * resident_blocks(regs, kWarps * 32, shared);
+    kernel<<<(unsigned int)(wanted < fit ? wanted : fit), kWarps * 32, shared, stream>>>(a, lanes, entry_lanes, lay);
     return cudaGetLastError();
 }
 
 template <typename T, int VEC, bool GRAD, bool SAVED>
 cudaError_t launch(const DistillArgs &a, int sms, cudaStream_t stream)
 {
-    // The warp form keeps one teacher entry per lane (its logit must outlive an in-place gradient): longer lists
-    // go to the block form.
     int lanes = 1;
     while (lanes < 32 && lanes * VEC < a.n) lanes *= 2;
-    while (lanes < 32 && lanes < a.k) lanes *= 2;
-    if (a.n <= kWarpRow && a.k <= 32) {
+    // (long lists of entries would leave room for one block only)
+    const Layout warp_lay{row_bytes<T, VEC>(a.n), 32 / lanes, a.k};
+    if (a.n <= kWarpRow && kWarps * kStages * warp_lay.bytes() <= 112 * 1024) {
         const int need = (a.n + lanes * VEC - 1) / (lanes * VEC);
-        if (need <= 1) return launch_warp<T, VEC, 1, GRAD, SAVED>(a, lanes, stream);
-        if (need <= 2) return launch_warp<T, VEC, 2, GRAD, SAVED>(a, lanes, stream);
-        if (VEC >= 4 || need <= 4) return launch_warp<T, VEC, (VEC == 4 ? 8 : 4), GRAD, SAVED>(a, lanes, stream);
+        if (need <= 1) return launch_warp<T, VEC, 1, GRAD, SAVED>(a, lanes, sms, stream);
+        if (need <= 2) return launch_warp<T, VEC, 2, GRAD, SAVED>(a, lanes, sms, stream);
+        if (VEC >= 4 || need <= 4) return launch_warp<T, VEC, (VEC == 4 ? 8 : 4), GRAD, SAVED>(a, lanes, sms, stream);
         if constexpr (VEC == 1) {
-            if (need <= 8) return launch_warp<T, VEC, 8, GRAD, SAVED>(a, lanes, stream);
-            if (need <= 16) return launch_warp<T, VEC, 16, GRAD, SAVED>(a, lanes, stream);
-            return launch_warp<T, VEC, 32, GRAD, SAVED>(a, lanes, stream);
+            if (need <= 8) return launch_warp<T, VEC, 8, GRAD, SAVED>(a, lanes, sms, stream);
+            if (need <= 16) return launch_warp<T, VEC, 16, GRAD, SAVED>(a, lanes, sms, stream);
+            return launch_warp<T, VEC, 32, GRAD, SAVED>(a, lanes, sms, stream);
         }
+    }
+    const int threads_one = ((a.n + kElems - 1) / kElems + 31) / 32 * 32;
+    if (threads_one <= 512 && a.rows >= 2 * sms) {
+        auto *kernel = distill_staged_kernel<T, VEC, GRAD, SAVED>;
+        static const int regs = kernel_registers(kernel);
+        const Layout lay{row_bytes<T, VEC>(a.n), 1, a.k};
+        const int shared = kStages * lay.bytes();
+        const cudaError_t e = allow_shared(kernel, shared);
+        if (e != cudaSuccess) return e;
+        const long long fit = (long long)sms * resident_blocks(regs, threads_one, shared + 2048);
+        kernel<<<(unsigned int)(a.rows < fit ? a.rows : fit), threads_one, shared, stream>>>(a, lay);
+        return cudaGetLastError();
     }
     // One block per row while the rows fill the GPU; more blocks per row when they do not, or when the row needs them
     const bool keep = a.n <= kMaxCluster * 1024 * kElems;
