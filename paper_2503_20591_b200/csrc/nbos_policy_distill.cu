@@ -219,10 +219,12 @@ __device__ __forceinline__ float entry_grad(const DistillArgs &a, const Staged<T
 // ---- warp form: `lanes` lanes per row, CH * VEC elements each; the grid stays and walks over the rows -------
 constexpr int kWarps = 8;
 
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
-__global__ void __launch_bounds__(kWarps * 32, 2) distill_warp_kernel(DistillArgs a, int lanes, int entry_lanes, Layout lay)
+// FULL: a row takes the whole warp (known when the kernel is compiled)
+template <typename T, int VEC, int CH, bool GRAD, bool SAVED, bool FULL>
+__global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArgs a, int lanes_, int entry_lanes, Layout lay)
 {
     extern __shared__ __align__(16) char s_mem[];
+    const int lanes = FULL ? 32 : lanes_;
     const int lane = threadIdx.x & 31, sub = lane & (lanes - 1), slot = lane / lanes, at_once = 32 / lanes;
     const int stage_bytes = lay.bytes();
     char *mine = s_mem + (threadIdx.x >> 5) * kStages * stage_bytes;
@@ -578,10 +580,10 @@ cudaError_t allow_shared(K *kernel, int bytes)
     return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
 }
 
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
+template <typename T, int VEC, int CH, bool GRAD, bool SAVED, bool FULL>
 cudaError_t launch_warp(const DistillArgs &a, int lanes, int sms, cudaStream_t stream)
 {
-    auto *kernel = distill_warp_kernel<T, VEC, CH, GRAD, SAVED>;
+    auto *kernel = distill_warp_kernel<T, VEC, CH, GRAD, SAVED, FULL>;
     static const int regs = kernel_registers(kernel);
     int entry_lanes = 1;
     while (entry_lanes < a.k && entry_lanes < lanes) entry_lanes *= 2;
@@ -604,13 +606,14 @@ cudaError_t launch(const DistillArgs &a, int sms, cudaStream_t stream)
     const Layout warp_lay{row_bytes<T, VEC>(a.n), 32 / lanes, a.k};
     if (a.n <= kWarpRow && kWarps * kStages * warp_lay.bytes() <= 112 * 1024) {
         const int need = (a.n + lanes * VEC - 1) / (lanes * VEC);
-        if (need <= 1) return launch_warp<T, VEC, 1, GRAD, SAVED>(a, lanes, sms, stream);
-        if (need <= 2) return launch_warp<T, VEC, 2, GRAD, SAVED>(a, lanes, sms, stream);
-        if (VEC >= 4 || need <= 4) return launch_warp<T, VEC, (VEC == 4 ? 8 : 4), GRAD, SAVED>(a, lanes, sms, stream);
+        if (need <= 1 && lanes < 32) return launch_warp<T, VEC, 1, GRAD, SAVED, false>(a, lanes, sms, stream);
+        if (need <= 1) return launch_warp<T, VEC, 1, GRAD, SAVED, true>(a, lanes, sms, stream);
+        if (need <= 2) return launch_warp<T, VEC, 2, GRAD, SAVED, true>(a, lanes, sms, stream);
+        if (VEC >= 4 || need <= 4) return launch_warp<T, VEC, (VEC == 4 ? 8 : 4), GRAD, SAVED, true>(a, lanes, sms, stream);
         if constexpr (VEC == 1) {
-            if (need <= 8) return launch_warp<T, VEC, 8, GRAD, SAVED>(a, lanes, sms, stream);
-            if (need <= 16) return launch_warp<T, VEC, 16, GRAD, SAVED>(a, lanes, sms, stream);
-            return launch_warp<T, VEC, 32, GRAD, SAVED>(a, lanes, sms, stream);
+            if (need <= 8) return launch_warp<T, VEC, 8, GRAD, SAVED, true>(a, lanes, sms, stream);
+            if (need <= 16) return launch_warp<T, VEC, 16, GRAD, SAVED, true>(a, lanes, sms, stream);
+            return launch_warp<T, VEC, 32, GRAD, SAVED, true>(a, lanes, sms, stream);
         }
     }
     const int threads_one = ((a.n + kElems - 1) / kElems + 31) / 32 * 32;
