@@ -169,6 +169,68 @@ __device__ __forceinline__ float exp_from(float x, float m, float c)
 {
     return exp2_fast((x - (m == neg_inf() ? 0.0f : m)) * c);
 }
+// two 32-bit operations in one instruction, each rounded to nearest as the single ones are
+__device__ __forceinline__ void add2(float &a0, float &a1, float b0, float b1)   // a += b
+{
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void mul2(float &a0, float &a1, float b0, float b1)   // a *= b
+{
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1)   // d += a b
+{
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmov.b64 z, {%4, %5};\n\t"
+        "fma.rn.f32x2 x, y, z, x;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
+// v = 2^((v - m0) c) over a lane's elements; returns their sum
+template <int VEC, int CH>
+__device__ __forceinline__ float exp_all(float (&v)[CH][VEC], float m0, float c)
+{
+    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        if constexpr (VEC == 1) {
+            v[k][0] = exp2_fast((v[k][0] - m0) * c);
+            (k % 2 ? s1 : s0) += v[k][0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) {
+                add2(v[k][i], v[k][i + 1], -m0, -m0);
+                mul2(v[k][i], v[k][i + 1], c, c);
+                v[k][i] = exp2_fast(v[k][i]), v[k][i + 1] = exp2_fast(v[k][i + 1]);
+                add2(s0, s1, v[k][i], v[k][i + 1]);
+            }
+        }
+    }
+    return s0 + s1;
+}
+// v *= f
+template <int VEC>
+__device__ __forceinline__ void scale_all(float (&v)[VEC], float f)
+{
+    if constexpr (VEC == 1) {
+        v[0] *= f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) mul2(v[i], v[i + 1], f, f);
+    }
+}
+template <int VEC, int CH>
+__device__ __forceinline__ float max_all(const float (&v)[CH][VEC])
+{
+    float m = v[0][0];
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[k][i]);
+    return m;
+}
+
 __device__ __forceinline__ float reciprocal(float x) { return __fdividef(1.0f, x); }   // 2 ulp
 
 // ---- rows staged in shared memory by asynchronous copies ----------------------------------------------------
@@ -177,6 +239,10 @@ constexpr int kStages = 3;   // rows on their way or in use per team (a warp, or
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void *src, int bytes)   // the rest of the 16 becomes 0
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copy_async4(uint32_t dst, const void *src)
 {
@@ -204,10 +270,12 @@ __device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long l
     int g = sub;
     if (VEC == 1 && offset < shift) {
         for (int i = sub; i < n && shift + (i + 1) * (int)sizeof(T) <= 16; i += team) reinterpret_cast<T *>(dst + shift)[i] = row[i];
-        g += team;
-        if (sub != 0) g = sub;   // pieces 1, 2, ... of 16 bytes; thread 0 starts at `team`
+        if (sub == 0) g = team;   // the pieces of 16 bytes after it
     }
-    for (; g * 16 < total; g += team) copy_async16(to + g * 16, src + g * 16, total - g * 16 < 16 ? total - g * 16 : 16);
+    const int whole = total >> 4;
+#pragma unroll 4
+    for (; g < whole; g += team) copy_async16(to + g * 16, src + g * 16);
+    if (g == whole && (total & 15)) copy_async16(to + g * 16, src + g * 16, total & 15);
 }
 // VEC elements of a staged row from column `col`; from n on they read as -inf
 template <typename T, int VEC>

@@ -245,23 +245,12 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
         const long long row = active ? base + slot : base;
         const Staged<T> r = staged_row<T, VEC>(a, lay, mine + st * stage_bytes, active ? slot : 0, row);
         float v[CH][VEC];
-        float m = neg_inf(), s = 0.0f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            staged_cols<T, VEC>(r.x, (c * lanes + sub) * VEC, a.n, v[c]);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
-        }
-        m = SAVED ? r.given[1] : lanes_max(m, lanes);
+        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, (c * lanes + sub) * VEC, a.n, v[c]);
+        const float m = SAVED ? r.given[1] : lanes_max(max_all<VEC, CH>(v), lanes);
         const float m0 = m == neg_inf() ? 0.0f : m;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                v[c][i] = exp2_fast((v[c][i] - m0) * a.c);
-                s += v[c][i];
-            }
-        s = SAVED ? r.given[2] : lanes_sum(s, lanes);
+        const float mine_sum = exp_all<VEC, CH>(v, m0, a.c);
+        const float s = SAVED ? r.given[2] : lanes_sum(mine_sum, lanes);
         const float inv_s = reciprocal(s);
         const float gmul = GRAD ? a.T * a.grad_scale * (a.grad_loss ? r.given[0] : 1.0f) : 0.0f;
         float tm = neg_inf(), z = 0.0f, entry_g = 0.0f, l = 0.0f;
@@ -310,8 +299,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
             const float fac0 = any ? fac : 0.0f;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[c][i] *= fac0;
+                scale_all<VEC>(v[c], fac0);
                 store_cols<T, VEC>(grad, (c * lanes + sub) * VEC, active ? a.n : 0, v[c]);
             }
             __syncwarp();   // the listed hosts' gradients go over what their columns' lanes wrote
@@ -356,22 +344,11 @@ __global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, L
         // 16 bytes a thread has copied itself; single elements came through other threads
         if (VEC == 1 || SAVED) __syncthreads();
         float v[CH][VEC];
-        float m = neg_inf(), s = 0.0f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            staged_cols<T, VEC>(r.x, c * chunk + threadIdx.x * VEC, a.n, v[c]);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
-        }
-        m = SAVED ? r.given[1] : lanes_max(m, 32);
+        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, c * chunk + threadIdx.x * VEC, a.n, v[c]);
+        float m = SAVED ? r.given[1] : lanes_max(max_all<VEC, CH>(v), 32);
         const float m_warp = m;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                v[c][i] = exp_from(v[c][i], m, a.c);
-                s += v[c][i];
-            }
+        float s = exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, a.c);
         if (SAVED) {
             s = r.given[2];
         } else {
@@ -418,8 +395,12 @@ __global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, L
             const float fac = gmul * reciprocal(s) * (SAVED ? 1.0f : exp_from(m_warp, m, a.c));
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
+                if (any) {
+                    scale_all<VEC>(v[c], fac);
+                } else {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) v[c][i] = any ? v[c][i] * fac : 0.0f;
+                    for (int i = 0; i < VEC; ++i) v[c][i] = 0.0f;
+                }
                 store_cols<T, VEC>(grad, c * chunk + threadIdx.x * VEC, a.n, v[c]);
             }
             __syncthreads();   // the listed hosts' gradients go over what others wrote; the stage may be filled again
