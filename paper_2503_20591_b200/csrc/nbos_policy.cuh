@@ -124,25 +124,33 @@ __device__ __forceinline__ void load_cols(const T *row, long long col, long long
         }
     }
 }
+// `wide`: row + col lies on a 16-byte boundary
 template <typename T, int VEC>
-__device__ __forceinline__ void store_cols(T *row, long long col, long long end, const float (&v)[VEC])
+__device__ __forceinline__ void store_cols(T *row, long long col, long long end, const float (&v)[VEC], bool wide = true)
 {
     if constexpr (VEC == 1) {
         if (col < end) __stcs(row + col, from_float<T>(v[0]));
     } else {
-        if (col + VEC <= end) {
+        if (wide && col >= 0 && col + VEC <= end) {
             __stcs(reinterpret_cast<uint4 *>(row + col), pack16(v, T()));
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
-                if (col + i < end) __stcs(row + col + i, from_float<T>(v[i]));
+                if (col + i >= 0 && col + i < end) __stcs(row + col + i, from_float<T>(v[i]));
         }
     }
 }
 
 // ---- reductions over `lanes` neighbouring lanes (a power of two; every lane gets the result) ---------------
+__device__ __forceinline__ float warp_max(float v)   // NaN is never the larger
+{
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
+}
 __device__ __forceinline__ float lanes_max(float v, int lanes)
 {
+    if (lanes == 32) return warp_max(v);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1)
         if (off < lanes) v = fmaxf(v, __shfl_xor_sync(kFull, v, off));
@@ -234,7 +242,7 @@ __device__ __forceinline__ float max_all(const float (&v)[CH][VEC])
 __device__ __forceinline__ float reciprocal(float x) { return __fdividef(1.0f, x); }   // 2 ulp
 
 // ---- rows staged in shared memory by asynchronous copies ----------------------------------------------------
-constexpr int kStages = 3;   // rows on their way or in use per team (a warp, or a block)
+constexpr int kStages = 2;   // rows on their way or in use per team (a warp, or a block); 3 and 4 measured the same
 
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void *src, int bytes)   // the rest of the 16 becomes 0
 {
@@ -252,23 +260,23 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
 
 // Bytes between the 16-byte boundary before a row and the row itself; they are staged along.
-template <typename T, int VEC>
+template <typename T>
 __device__ __forceinline__ int row_shift(const T *row)
 {
-    return VEC == 1 ? (int)(reinterpret_cast<uintptr_t>(row) & 15) : 0;
+    return (int)(reinterpret_cast<uintptr_t>(row) & 15);
 }
 // Queues the copies of n elements from `row` to `dst` (16-byte aligned; the row itself lands row_shift bytes further),
 // thread `sub` of `team`. The bytes before an unaligned row belong to the rows before it (or the gaps between them);
 // where the table does not have that many (`offset`: the row's, in bytes), the first, partial 16 bytes go element by
 // element.
-template <typename T, int VEC>
+template <typename T>
 __device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long long offset, int sub, int team)
 {
-    const int shift = row_shift<T, VEC>(row), total = shift + n * (int)sizeof(T);
+    const int shift = row_shift(row), total = shift + n * (int)sizeof(T);
     const char *src = reinterpret_cast<const char *>(row) - shift;
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
     int g = sub;
-    if (VEC == 1 && offset < shift) {
+    if (offset < shift) {
         for (int i = sub; i < n && shift + (i + 1) * (int)sizeof(T) <= 16; i += team) reinterpret_cast<T *>(dst + shift)[i] = row[i];
         if (sub == 0) g = team;   // the pieces of 16 bytes after it
     }
@@ -277,19 +285,18 @@ __device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long l
     for (; g < whole; g += team) copy_async16(to + g * 16, src + g * 16);
     if (g == whole && (total & 15)) copy_async16(to + g * 16, src + g * 16, total & 15);
 }
-// VEC elements of a staged row from column `col`; from n on they read as -inf
+// Bytes of a staged row, with what precedes an unaligned one.
+inline int staged_row_bytes(int n, int elem, bool aligned) { return (n * elem + (aligned ? 0 : 15) + 15) & ~15; }
+// VEC elements (16 bytes) of a staged row from column `col`, which lies on a 16-byte boundary and may be below 0: columns
+// outside the row read as -inf
 template <typename T, int VEC>
 __device__ __forceinline__ void staged_cols(const T *row, int col, int n, float (&v)[VEC])
 {
-    if constexpr (VEC == 1) {
-        v[0] = col < n ? to_float(row[col]) : neg_inf();
+    if (col >= 0 && col + VEC <= n) {
+        unpack16(*reinterpret_cast<const uint4 *>(row + col), v, T());
     } else {
-        if (col + VEC <= n) {
-            unpack16(*reinterpret_cast<const uint4 *>(row + col), v, T());
-        } else {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = col + i < n ? to_float(row[col + i]) : neg_inf();
-        }
+        for (int i = 0; i < VEC; ++i) v[i] = col + i >= 0 && col + i < n ? to_float(row[col + i]) : neg_inf();
     }
 }
 

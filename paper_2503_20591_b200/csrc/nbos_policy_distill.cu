@@ -38,6 +38,7 @@ struct DistillArgs {
     const float *stats_in;
     void *grad;
     long long gstride;
+    bool wide;   // the gradient's rows lie on 16-byte boundaries where the logits' do: it is written 16 bytes at a time
 };
 
 struct Entry {
@@ -136,17 +137,18 @@ struct Staged {
 };
 struct Layout {   // bytes of a stage: rows, then entries, then what is given per row
     int row_bytes, rows, k;
+    bool aligned;   // every row starts on a 16-byte boundary
     __host__ __device__ int hosts_at() const { return row_bytes * rows; }
     __host__ __device__ int teacher_at() const { return hosts_at() + rows * k * 4; }
     __host__ __device__ int given_at() const { return teacher_at() + rows * k * 4; }
     __host__ __device__ int bytes() const { return (given_at() + rows * 12 + 15) & ~15; }
 };
 
-template <typename T, int VEC, bool GRAD, bool SAVED>
+template <typename T, bool GRAD, bool SAVED>
 __device__ __forceinline__ void stage(const DistillArgs &a, const Layout &lay, char *at, int slot, long long row, int sub, int team)
 {
     const T *x = static_cast<const T *>(a.x) + row * a.stride;
-    stage_row<T, VEC>(at + slot * lay.row_bytes, x, a.n, row * a.stride * (long long)sizeof(T), sub, team);
+    stage_row(at + slot * lay.row_bytes, x, a.n, row * a.stride * (long long)sizeof(T), sub, team);
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at));
     for (int i = sub; i < a.k; i += team) {
         copy_async4(to + lay.hosts_at() + (slot * a.k + i) * 4, a.hosts + row * a.k + i);
@@ -160,11 +162,11 @@ __device__ __forceinline__ void stage(const DistillArgs &a, const Layout &lay, c
         }
     }
 }
-template <typename T, int VEC>
+template <typename T>
 __device__ __forceinline__ Staged<T> staged_row(const DistillArgs &a, const Layout &lay, const char *at, int slot, long long row)
 {
     Staged<T> s;
-    s.x = reinterpret_cast<const T *>(at + slot * lay.row_bytes + row_shift<T, VEC>(static_cast<const T *>(a.x) + row * a.stride));
+    s.x = reinterpret_cast<const T *>(at + slot * lay.row_bytes + row_shift(static_cast<const T *>(a.x) + row * a.stride));
     s.hosts = reinterpret_cast<const int *>(at + lay.hosts_at()) + slot * a.k;
     s.teacher = reinterpret_cast<const float *>(at + lay.teacher_at()) + slot * a.k;
     s.given = reinterpret_cast<const float *>(at + lay.given_at()) + slot * 3;
@@ -216,13 +218,39 @@ __device__ __forceinline__ float entry_grad(const DistillArgs &a, const Staged<T
     return gmul * (exp_from(e.x, m, a.c) * reciprocal(s) - q);
 }
 
+// At most one entry a lane (e, host -1 where there is none), in the first entry_lanes of `lanes` lanes: the row's loss (if
+// LOSS) and, if GRAD, the gradient at the lane's entry.
+template <bool LOSS, bool GRAD>
+__device__ __forceinline__ void entry_math(const DistillArgs &a, const Entry &e, int lanes, int entry_lanes, float m0, float s, float inv_s,
+                                           float gmul, float &loss, float &grad)
+{
+    const float tm = lanes_max(e.host >= 0 ? e.t : neg_inf(), entry_lanes);
+    float q = e.host >= 0 ? exp2_fast((e.t - tm) * a.c) : 0.0f;
+    const float inv_z = reciprocal(lanes_sum(q, entry_lanes));
+    q *= inv_z;
+    if (LOSS) {
+        // q underflows to 0 before ln q leaves the range of 32 bits; 0 * -inf is kept out
+        const float l = q * (((e.t - tm) - (e.x - m0)) * a.inv_t + logf(s * inv_z));
+        loss = lanes_sum(e.host < 0 || q == 0.0f ? 0.0f : l, entry_lanes) * a.T * a.T;
+    }
+    if (GRAD) {
+        float all = 0.0f;   // a host may be listed more than once
+        for (int i = 0; i < a.k; ++i) {
+            const float other = __shfl_sync(kFull, q, i, lanes);
+            if (__shfl_sync(kFull, e.host, i, lanes) == e.host) all += other;
+        }
+        grad = gmul * (exp2_fast((e.x - m0) * a.c) * inv_s - all);
+    }
+}
+
 // ---- warp form: `lanes` lanes per row, CH * VEC elements each; the grid stays and walks over the rows -------
 constexpr int kWarps = 8;
 
 // FULL: a row takes the whole warp (known when the kernel is compiled)
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED, bool FULL>
+template <typename T, int CH, bool GRAD, bool SAVED, bool FULL>
 __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArgs a, int lanes_, int entry_lanes, Layout lay)
 {
+    constexpr int VEC = kPer16<T>;
     extern __shared__ __align__(16) char s_mem[];
     const int lanes = FULL ? 32 : lanes_;
     const int lane = threadIdx.x & 31, sub = lane & (lanes - 1), slot = lane / lanes, at_once = 32 / lanes;
@@ -231,7 +259,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
     const long long step = (long long)gridDim.x * kWarps * at_once;
     const long long row0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * at_once;
     auto queue = [&](long long base, int st) {
-        if (base + slot < a.rows) stage<T, VEC, GRAD, SAVED>(a, lay, mine + st * stage_bytes, slot, base + slot, sub, lanes);
+        if (base + slot < a.rows) stage<T, GRAD, SAVED>(a, lay, mine + st * stage_bytes, slot, base + slot, sub, lanes);
         copies_commit();
     };
 #pragma unroll
@@ -243,10 +271,11 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
         __syncwarp();
         const bool active = base + slot < a.rows;
         const long long row = active ? base + slot : base;
-        const Staged<T> r = staged_row<T, VEC>(a, lay, mine + st * stage_bytes, active ? slot : 0, row);
+        const Staged<T> r = staged_row<T>(a, lay, mine + st * stage_bytes, active ? slot : 0, row);
+        const int first = sub * VEC - row_shift(r.x) / (int)sizeof(T);
         float v[CH][VEC];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, (c * lanes + sub) * VEC, a.n, v[c]);
+        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, first + c * lanes * VEC, a.n, v[c]);
         const float m = SAVED ? r.given[1] : lanes_max(max_all<VEC, CH>(v), lanes);
         const float m0 = m == neg_inf() ? 0.0f : m;
         const float mine_sum = exp_all<VEC, CH>(v, m0, a.c);
@@ -260,24 +289,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
             if (active && sub < a.k) e = r.entry(sub);
             const unsigned int group = lanes == 32 ? kFull : ((1u << lanes) - 1) << (slot * lanes);
             any = (__ballot_sync(kFull, e.host >= 0) & group) != 0;
-            // the entries are in the group's first entry_lanes lanes
-            tm = lanes_max(e.host >= 0 ? e.t : neg_inf(), entry_lanes);
-            float q = e.host >= 0 ? exp2_fast((e.t - tm) * a.c) : 0.0f;
-            z = lanes_sum(q, entry_lanes);
-            q *= reciprocal(z);
-            // q underflows to 0 before ln q leaves the range of 32 bits; 0 * -inf is kept out
-            if (!SAVED) {
-                l = q * (((e.t - tm) - (e.x - m0)) * a.inv_t + logf(s * reciprocal(z)));
-                l = lanes_sum(e.host < 0 || q == 0.0f ? 0.0f : l, entry_lanes) * a.T * a.T;
-            }
-            if (GRAD) {
-                float all = 0.0f;   // a host may be listed more than once
-                for (int i = 0; i < a.k; ++i) {
-                    const float other = __shfl_sync(kFull, q, i, lanes);
-                    if (__shfl_sync(kFull, e.host, i, lanes) == e.host) all += other;
-                }
-                entry_g = gmul * (exp2_fast((e.x - m0) * a.c) * inv_s - all);
-            }
+            entry_math<!SAVED, GRAD>(a, e, lanes, entry_lanes, m0, s, inv_s, gmul, l, entry_g);
         } else {
             teacher_sums(a, r, active, sub, lanes, tm, z);
             any = tm > neg_inf();
@@ -300,7 +312,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 scale_all<VEC>(v[c], fac0);
-                store_cols<T, VEC>(grad, (c * lanes + sub) * VEC, active ? a.n : 0, v[c]);
+                store_cols<T, VEC>(grad, first + c * lanes * VEC, active ? a.n : 0, v[c], a.wide);
             }
             __syncwarp();   // the listed hosts' gradients go over what their columns' lanes wrote
             if (a.k <= lanes) {
@@ -320,10 +332,10 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
 // ---- block form: one row at a time per block, kElems elements a thread -------------------------------------
 __device__ __forceinline__ void merge_stats(float &m, float &s, float m2, float s2, float c);
 
-template <typename T, int VEC, bool GRAD, bool SAVED>
-__global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, Layout lay)
+template <typename T, bool GRAD, bool SAVED>
+__global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_lanes, Layout lay)
 {
-    constexpr int CH = kElems / VEC;
+    constexpr int VEC = kPer16<T>, CH = kElems / VEC;
     extern __shared__ __align__(16) char s_mem[];
     __shared__ float2 s_stats[2][16];
     __shared__ float s_fix[NBOS_POLICY_MAX_K];
@@ -331,7 +343,7 @@ __global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, L
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int chunk = blockDim.x * VEC, stage_bytes = lay.bytes();
     auto queue = [&](long long row, int st) {
-        if (row < a.rows) stage<T, VEC, GRAD, SAVED>(a, lay, s_mem + st * stage_bytes, 0, row, threadIdx.x, blockDim.x);
+        if (row < a.rows) stage<T, GRAD, SAVED>(a, lay, s_mem + st * stage_bytes, 0, row, threadIdx.x, blockDim.x);
         copies_commit();
     };
 #pragma unroll
@@ -340,12 +352,13 @@ __global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, L
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         queue(row + (kStages - 1) * (long long)gridDim.x, st == 0 ? kStages - 1 : st - 1);
         copies_wait();
-        const Staged<T> r = staged_row<T, VEC>(a, lay, s_mem + st * stage_bytes, 0, row);
-        // 16 bytes a thread has copied itself; single elements came through other threads
-        if (VEC == 1 || SAVED) __syncthreads();
+        const Staged<T> r = staged_row<T>(a, lay, s_mem + st * stage_bytes, 0, row);
+        // its 16 bytes a thread has copied itself; the first elements of an unaligned table came through other threads
+        if (!lay.aligned || SAVED) __syncthreads();
+        const int first = threadIdx.x * VEC - row_shift(r.x) / (int)sizeof(T);
         float v[CH][VEC];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, c * chunk + threadIdx.x * VEC, a.n, v[c]);
+        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, first + c * chunk, a.n, v[c]);
         float m = SAVED ? r.given[1] : lanes_max(max_all<VEC, CH>(v), 32);
         const float m_warp = m;
         float s = exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, a.c);
@@ -361,38 +374,38 @@ __global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, L
             s = lanes_sum(w.y * exp_from(w.x, m, a.c), 16);
             s = __shfl_sync(kFull, s, 0);
         }
+        const float inv_s = reciprocal(s);
+        const float gmul = GRAD ? a.T * a.grad_scale * (a.grad_loss ? r.given[0] : 1.0f) : 0.0f;
         // every warp finds out whether an entry counts; the first one does what is to be done with them
-        float tm = neg_inf();
-        for (int i = lane; i < a.k; i += 32) {
-            const Entry e = r.entry(i);
-            if (e.host >= 0) tm = fmaxf(tm, e.t);
-        }
-        tm = lanes_max(tm, 32);
-        const bool any = tm > neg_inf();
-        const float gmul = a.T * a.grad_scale * (GRAD && a.grad_loss ? r.given[0] : 1.0f);
+        bool any = false;
+        for (int i = lane; i < a.k; i += 32) any = any || r.entry(i).host >= 0;
+        any = __any_sync(kFull, any);
         if (warp == 0) {
-            float z = 0.0f;
-            for (int i = lane; i < a.k; i += 32) {
-                const Entry e = r.entry(i);
-                if (e.host >= 0) z += exp_from(e.t, tm, a.c);
-            }
-            z = lanes_sum(z, 32);
-            if (!SAVED) {
-                const float l = entries_loss(a, r, any, lane, 32, tm, z, m, s);
-                if (lane == 0) {
-                    if (a.loss) a.loss[row] = any ? l : 0.0f;
-                    if (a.stats) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+            float l = 0.0f;
+            if (a.k <= 32) {
+                Entry e{-1, 0.0f, 0.0f};
+                if (lane < a.k) e = r.entry(lane);
+                float g = 0.0f;
+                entry_math<!SAVED, GRAD>(a, e, 32, entry_lanes, m == neg_inf() ? 0.0f : m, s, inv_s, gmul, l, g);
+                if (GRAD && lane < a.k) s_fix_host[lane] = e.host, s_fix[lane] = g;
+            } else {
+                float tm, z;
+                teacher_sums(a, r, true, lane, 32, tm, z);
+                if (!SAVED) l = entries_loss(a, r, any, lane, 32, tm, z, m, s);
+                for (int i = lane; GRAD && i < a.k; i += 32) {
+                    const Entry e = r.entry(i);
+                    s_fix_host[i] = e.host;
+                    if (e.host >= 0) s_fix[i] = entry_grad(a, r, e, tm, z, m, s, gmul);
                 }
             }
-            for (int i = lane; GRAD && any && i < a.k; i += 32) {
-                const Entry e = r.entry(i);
-                s_fix_host[i] = e.host;
-                if (e.host >= 0) s_fix[i] = entry_grad(a, r, e, tm, z, m, s, gmul);
+            if (!SAVED && lane == 0) {
+                if (a.loss) a.loss[row] = any ? l : 0.0f;
+                if (a.stats) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
             }
         }
         if (GRAD) {
             T *grad = static_cast<T *>(a.grad) + row * a.gstride;
-            const float fac = gmul * reciprocal(s) * (SAVED ? 1.0f : exp_from(m_warp, m, a.c));
+            const float fac = gmul * inv_s * (SAVED ? 1.0f : exp_from(m_warp, m, a.c));
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 if (any) {
@@ -401,7 +414,7 @@ __global__ void __launch_bounds__(512, 1) distill_staged_kernel(DistillArgs a, L
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) v[c][i] = 0.0f;
                 }
-                store_cols<T, VEC>(grad, c * chunk + threadIdx.x * VEC, a.n, v[c]);
+                store_cols<T, VEC>(grad, first + c * chunk, a.n, v[c], a.wide);
             }
             __syncthreads();   // the listed hosts' gradients go over what others wrote; the stage may be filled again
             for (int i = lane; warp == 0 && any && i < a.k; i += 32)
@@ -527,7 +540,7 @@ __global__ void __launch_bounds__(1024, 1) distill_block_kernel(DistillArgs a, i
             for (int c = 0; c < CH; ++c) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) v[c][i] = any ? v[c][i] * fac : 0.0f;
-                store_cols<T, VEC>(grad, first_col + c * chunk + threadIdx.x * VEC, end_col, v[c]);
+                store_cols<T, VEC>(grad, first_col + c * chunk + threadIdx.x * VEC, end_col, v[c], a.wide);
             }
         } else {
             for (long long col = first_col + threadIdx.x * VEC; col < end_col; col += chunk) {
@@ -535,7 +548,7 @@ __global__ void __launch_bounds__(1024, 1) distill_block_kernel(DistillArgs a, i
                 load_cols<T, VEC>(x, col, end_col, neg_inf(), w);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) w[i] = any ? exp_from(w[i], m, a.c) * fac : 0.0f;
-                store_cols<T, VEC>(grad, col, end_col, w);
+                store_cols<T, VEC>(grad, col, end_col, w, a.wide);
             }
         }
         __syncthreads();
@@ -550,10 +563,11 @@ __global__ void __launch_bounds__(1024, 1) distill_block_kernel(DistillArgs a, i
     }
 }
 
-template <typename T, int VEC>
-int row_bytes(int n)   // of a staged row, with what precedes an unaligned one
+int power_of_two(int n, int most)   // the first that is not below n
 {
-    return (n * (int)sizeof(T) + (VEC == 1 ? 15 : 0) + 15) & ~15;
+    int p = 1;
+    while (p < n && p < most) p *= 2;
+    return p;
 }
 template <typename K>
 cudaError_t allow_shared(K *kernel, int bytes)
@@ -561,54 +575,65 @@ cudaError_t allow_shared(K *kernel, int bytes)
     return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
 }
 
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED, bool FULL>
-cudaError_t launch_warp(const DistillArgs &a, int lanes, int sms, cudaStream_t stream)
+template <typename T, int CH, bool GRAD, bool SAVED, bool FULL>
+cudaError_t launch_warp(const DistillArgs &a, int lanes, const Layout &lay, int sms, cudaStream_t stream)
 {
-    auto *kernel = distill_warp_kernel<T, VEC, CH, GRAD, SAVED, FULL>;
+    auto *kernel = distill_warp_kernel<T, CH, GRAD, SAVED, FULL>;
     static const int regs = kernel_registers(kernel);
-    int entry_lanes = 1;
-    while (entry_lanes < a.k && entry_lanes < lanes) entry_lanes *= 2;
-    const Layout lay{row_bytes<T, VEC>(a.n), 32 / lanes, a.k};
     const int shared = kWarps * kStages * lay.bytes();
     const cudaError_t e = allow_shared(kernel, shared);
     if (e != cudaSuccess) return e;
     const long long per_block = kWarps * (32 / lanes), wanted = (a.rows + per_block - 1) / per_block;
     const long long fit = (long long)sms * resident_blocks(regs, kWarps * 32, shared);
-    kernel<<<(unsigned int)(wanted < fit ? wanted : fit), kWarps * 32, shared, stream>>>(a, lanes, entry_lanes, lay);
+    kernel<<<(unsigned int)(wanted < fit ? wanted : fit), kWarps * 32, shared, stream>>>(a, lanes, power_of_two(a.k, lanes), lay);
     return cudaGetLastError();
+}
+
+// The staged forms; false: not for these sizes.
+template <typename T, bool GRAD, bool SAVED>
+bool launch_staged(const DistillArgs &a, int sms, cudaStream_t stream, cudaError_t &e)
+{
+    constexpr int VEC = kPer16<T>, MOST = kElems / VEC;
+    const bool aligned = rows_aligned16(a.x, a.rows, a.stride, sizeof(T));
+    const int columns = a.n + (aligned ? 0 : VEC - 1);   // with those before an unaligned row
+    // Lanes per row: 32 elements a lane, so that what a row costs besides its elements is shared by the warp's rows; no
+    // fewer than entries; more while there are too few rows to give every SM eight warps.
+    int lanes = power_of_two((columns + kElems - 1) / kElems, 32);
+    while (lanes < 32 && lanes < a.k) lanes *= 2;
+    while (lanes < 32 && lanes * VEC < columns && a.rows * lanes < 32ll * 8 * sms) lanes *= 2;
+    const Layout warp_lay{staged_row_bytes(a.n, sizeof(T), aligned), 32 / lanes, a.k, aligned};
+    // (long lists of entries would leave room for one block only)
+    if (columns <= kWarpRow && kWarps * kStages * warp_lay.bytes() <= 112 * 1024) {
+        const int need = (columns + lanes * VEC - 1) / (lanes * VEC);
+        if (need <= 1)
+            e = launch_warp<T, 1, GRAD, SAVED, false>(a, lanes, warp_lay, sms, stream);
+        else if (need <= 2)
+            e = launch_warp<T, 2, GRAD, SAVED, false>(a, lanes, warp_lay, sms, stream);
+        else if (lanes < 32)
+            e = launch_warp<T, MOST, GRAD, SAVED, false>(a, lanes, warp_lay, sms, stream);
+        else
+            e = launch_warp<T, MOST, GRAD, SAVED, true>(a, lanes, warp_lay, sms, stream);
+        return true;
+    }
+    const int threads = ((columns + kElems - 1) / kElems + 31) / 32 * 32;
+    if (threads > 512 || a.rows < 2 * sms) return false;
+    auto *kernel = distill_staged_kernel<T, GRAD, SAVED>;
+    static const int regs = kernel_registers(kernel);
+    const Layout lay{staged_row_bytes(a.n, sizeof(T), aligned), 1, a.k, aligned};
+    const int shared = kStages * lay.bytes();
+    e = allow_shared(kernel, shared);
+    if (e != cudaSuccess) return true;
+    const long long fit = (long long)sms * resident_blocks(regs, threads, shared + 2560);
+    kernel<<<(unsigned int)(a.rows < fit ? a.rows : fit), threads, shared, stream>>>(a, power_of_two(a.k, 32), lay);
+    e = cudaGetLastError();
+    return true;
 }
 
 template <typename T, int VEC, bool GRAD, bool SAVED>
 cudaError_t launch(const DistillArgs &a, int sms, cudaStream_t stream)
 {
-    int lanes = 1;
-    while (lanes < 32 && lanes * VEC < a.n) lanes *= 2;
-    // (long lists of entries would leave room for one block only)
-    const Layout warp_lay{row_bytes<T, VEC>(a.n), 32 / lanes, a.k};
-    if (a.n <= kWarpRow && kWarps * kStages * warp_lay.bytes() <= 112 * 1024) {
-        const int need = (a.n + lanes * VEC - 1) / (lanes * VEC);
-        if (need <= 1 && lanes < 32) return launch_warp<T, VEC, 1, GRAD, SAVED, false>(a, lanes, sms, stream);
-        if (need <= 1) return launch_warp<T, VEC, 1, GRAD, SAVED, true>(a, lanes, sms, stream);
-        if (need <= 2) return launch_warp<T, VEC, 2, GRAD, SAVED, true>(a, lanes, sms, stream);
-        if (VEC >= 4 || need <= 4) return launch_warp<T, VEC, (VEC == 4 ? 8 : 4), GRAD, SAVED, true>(a, lanes, sms, stream);
-        if constexpr (VEC == 1) {
-            if (need <= 8) return launch_warp<T, VEC, 8, GRAD, SAVED, true>(a, lanes, sms, stream);
-            if (need <= 16) return launch_warp<T, VEC, 16, GRAD, SAVED, true>(a, lanes, sms, stream);
-            return launch_warp<T, VEC, 32, GRAD, SAVED, true>(a, lanes, sms, stream);
-        }
-    }
-    const int threads_one = ((a.n + kElems - 1) / kElems + 31) / 32 * 32;
-    if (threads_one <= 512 && a.rows >= 2 * sms) {
-        auto *kernel = distill_staged_kernel<T, VEC, GRAD, SAVED>;
-        static const int regs = kernel_registers(kernel);
-        const Layout lay{row_bytes<T, VEC>(a.n), 1, a.k};
-        const int shared = kStages * lay.bytes();
-        const cudaError_t e = allow_shared(kernel, shared);
-        if (e != cudaSuccess) return e;
-        const long long fit = (long long)sms * resident_blocks(regs, threads_one, shared + 2048);
-        kernel<<<(unsigned int)(a.rows < fit ? a.rows : fit), threads_one, shared, stream>>>(a, lay);
-        return cudaGetLastError();
-    }
+    cudaError_t staged = cudaSuccess;
+    if (launch_staged<T, GRAD, SAVED>(a, sms, stream, staged)) return staged;
     // One block per row while the rows fill the GPU; more blocks per row when they do not, or when the row needs them
     const bool keep = a.n <= kMaxCluster * 1024 * kElems;
     int cs = 1;
@@ -649,8 +674,8 @@ cudaError_t launch(const DistillArgs &a, int sms, cudaStream_t stream)
 template <typename T>
 cudaError_t dispatch(const DistillArgs &a, int sms, cudaStream_t stream)
 {
-    const bool vec = rows_aligned16(a.x, a.rows, a.stride, sizeof(T)) &&
-                     (!a.grad || rows_aligned16(a.grad, a.rows, a.gstride, sizeof(T)));
+    // the path, and with it every rounding, goes by the logits alone: the loss is the same with a gradient or without
+    const bool vec = rows_aligned16(a.x, a.rows, a.stride, sizeof(T));
     constexpr int V = kPer16<T>;
     if (a.stats_in) return vec ? launch<T, V, true, true>(a, sms, stream) : launch<T, 1, true, true>(a, sms, stream);
     if (a.grad) return vec ? launch<T, V, true, false>(a, sms, stream) : launch<T, 1, true, false>(a, sms, stream);
@@ -679,8 +704,10 @@ int distill(const nbos_logits *l, const int32_t *hosts, const float *teacher, in
     int sms = 0, device = 0;
     if ((rc = check_sm100(&sms, &device))) return rc;
     DistillArgs a{l->data, l->rows, l->row_stride, l->n_hosts, hosts, teacher, tstride, k, T, kLog2e / T, 1.0f / T,
-                  grad_loss, grad_scale, out_loss, out_stats, stats_in, out_grad, gstride};
+                  grad_loss, grad_scale, out_loss, out_stats, stats_in, out_grad, gstride, false};
     if (a.rows == 1) a.stride = a.gstride = l->n_hosts;
+    const long long apart = static_cast<const char *>(l->data) - static_cast<const char *>(out_grad);
+    a.wide = apart % 16 == 0 && (a.stride - a.gstride) * (long long)dtype_bytes(l->dtype) % 16 == 0;
     const cudaError_t e = l->dtype == NBOS_F32    ? dispatch<float>(a, sms, stream)
                           : l->dtype == NBOS_BF16 ? dispatch<__nv_bfloat16>(a, sms, stream)
                                                   : dispatch<__half>(a, sms, stream);
