@@ -124,15 +124,25 @@ __device__ __forceinline__ void load_cols(const T *row, long long col, long long
         }
     }
 }
+__device__ __forceinline__ void store_pair(unsigned short *at, unsigned int w, bool first, bool second);
 // `wide`: row + col lies on a 16-byte boundary
-template <typename T, int VEC>
-__device__ __forceinline__ void store_cols(T *row, long long col, long long end, const float (&v)[VEC], bool wide = true)
+template <typename T, int VEC, typename I>
+__device__ __forceinline__ void store_cols(T *row, I col, I end, const float (&v)[VEC], bool wide = true)
 {
     if constexpr (VEC == 1) {
         if (col < end) __stcs(row + col, from_float<T>(v[0]));
     } else {
         if (wide && col >= 0 && col + VEC <= end) {
             __stcs(reinterpret_cast<uint4 *>(row + col), pack16(v, T()));
+        } else if (col >= end) {
+        } else if (sizeof(T) == 2 && wide) {
+            const uint4 u = pack16(v, T());
+            const unsigned int w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int i = 0; i < VEC / 2; ++i) {
+                const I c = col + 2 * i;
+                store_pair(reinterpret_cast<unsigned short *>(row + c), w[i % 4], c >= 0 && c < end, c + 1 >= 0 && c + 1 < end);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
@@ -292,12 +302,26 @@ inline int staged_row_bytes(int n, int elem, bool aligned) { return (n * elem + 
 template <typename T, int VEC>
 __device__ __forceinline__ void staged_cols(const T *row, int col, int n, float (&v)[VEC])
 {
-    if (col >= 0 && col + VEC <= n) {
+    if (col < n) {   // the boundary before a row and its last 16 bytes are staged whole
         unpack16(*reinterpret_cast<const uint4 *>(row + col), v, T());
+        if (col < 0 || col + VEC > n) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = (unsigned int)(col + i) < (unsigned int)n ? v[i] : neg_inf();
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = col + i >= 0 && col + i < n ? to_float(row[col + i]) : neg_inf();
+        for (int i = 0; i < VEC; ++i) v[i] = neg_inf();
     }
+}
+// two neighbours on a 4-byte boundary, either of them perhaps outside the row
+__device__ __forceinline__ void store_pair(unsigned short *at, unsigned int w, bool first, bool second)
+{
+    if (first && second)
+        __stcs(reinterpret_cast<unsigned int *>(at), w);
+    else if (first)
+        __stcs(at, (unsigned short)w);
+    else if (second)
+        __stcs(at + 1, (unsigned short)(w >> 16));
 }
 
 // ---- blocks that share a row: a cluster of `cs` blocks, or one block (cs = 1) ------------------------------

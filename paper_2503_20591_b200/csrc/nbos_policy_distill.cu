@@ -138,6 +138,7 @@ struct Staged {
 struct Layout {   // bytes of a stage: rows, then entries, then what is given per row
     int row_bytes, rows, k;
     bool aligned;   // every row starts on a 16-byte boundary
+    int whole;      // n if, besides, the gradient is written 16 bytes at a time: columns below it need no look; else 0
     __host__ __device__ int hosts_at() const { return row_bytes * rows; }
     __host__ __device__ int teacher_at() const { return hosts_at() + rows * k * 4; }
     __host__ __device__ int given_at() const { return teacher_at() + rows * k * 4; }
@@ -243,16 +244,15 @@ __device__ __forceinline__ void entry_math(const DistillArgs &a, const Entry &e,
     }
 }
 
-// ---- warp form: `lanes` lanes per row, CH * VEC elements each; the grid stays and walks over the rows -------
+// ---- warp form: LANES lanes per row, CH * VEC elements each; the grid stays and walks over the rows -------
 constexpr int kWarps = 8;
 
-// FULL: a row takes the whole warp (known when the kernel is compiled)
-template <typename T, int CH, bool GRAD, bool SAVED, bool FULL>
-__global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArgs a, int lanes_, int entry_lanes, Layout lay)
+template <typename T, int LANES, int CH, bool GRAD, bool SAVED>
+__global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArgs a, int entry_lanes, Layout lay)
 {
     constexpr int VEC = kPer16<T>;
     extern __shared__ __align__(16) char s_mem[];
-    const int lanes = FULL ? 32 : lanes_;
+    constexpr int lanes = LANES;
     const int lane = threadIdx.x & 31, sub = lane & (lanes - 1), slot = lane / lanes, at_once = 32 / lanes;
     const int stage_bytes = lay.bytes();
     char *mine = s_mem + (threadIdx.x >> 5) * kStages * stage_bytes;
@@ -275,7 +275,12 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
         const int first = sub * VEC - row_shift(r.x) / (int)sizeof(T);
         float v[CH][VEC];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, first + c * lanes * VEC, a.n, v[c]);
+        for (int c = 0; c < CH; ++c) {
+            if ((c + 1) * lanes * VEC <= lay.whole)
+                unpack16(*reinterpret_cast<const uint4 *>(r.x + first + c * lanes * VEC), v[c], T());
+            else
+                staged_cols<T, VEC>(r.x, first + c * lanes * VEC, a.n, v[c]);
+        }
         const float m = SAVED ? r.given[1] : lanes_max(max_all<VEC, CH>(v), lanes);
         const float m0 = m == neg_inf() ? 0.0f : m;
         const float mine_sum = exp_all<VEC, CH>(v, m0, a.c);
@@ -312,7 +317,11 @@ __global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArg
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 scale_all<VEC>(v[c], fac0);
-                store_cols<T, VEC>(grad, first + c * lanes * VEC, active ? a.n : 0, v[c], a.wide);
+                if ((c + 1) * lanes * VEC <= lay.whole) {
+                    if (active) __stcs(reinterpret_cast<uint4 *>(grad + first + c * lanes * VEC), pack16(v[c], T()));
+                } else {
+                    store_cols<T, VEC>(grad, first + c * lanes * VEC, active ? a.n : 0, v[c], a.wide);
+                }
             }
             __syncwarp();   // the listed hosts' gradients go over what their columns' lanes wrote
             if (a.k <= lanes) {
@@ -358,7 +367,12 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
         const int first = threadIdx.x * VEC - row_shift(r.x) / (int)sizeof(T);
         float v[CH][VEC];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) staged_cols<T, VEC>(r.x, first + c * chunk, a.n, v[c]);
+        for (int c = 0; c < CH; ++c) {
+            if ((c + 1) * chunk <= lay.whole)
+                unpack16(*reinterpret_cast<const uint4 *>(r.x + first + c * chunk), v[c], T());
+            else
+                staged_cols<T, VEC>(r.x, first + c * chunk, a.n, v[c]);
+        }
         float m = SAVED ? r.given[1] : lanes_max(max_all<VEC, CH>(v), 32);
         const float m_warp = m;
         float s = exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, a.c);
@@ -414,7 +428,10 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) v[c][i] = 0.0f;
                 }
-                store_cols<T, VEC>(grad, first + c * chunk, a.n, v[c], a.wide);
+                if ((c + 1) * chunk <= lay.whole)
+                    __stcs(reinterpret_cast<uint4 *>(grad + first + c * chunk), pack16(v[c], T()));
+                else
+                    store_cols<T, VEC>(grad, first + c * chunk, a.n, v[c], a.wide);
             }
             __syncthreads();   // the listed hosts' gradients go over what others wrote; the stage may be filled again
             for (int i = lane; warp == 0 && any && i < a.k; i += 32)
@@ -575,17 +592,17 @@ cudaError_t allow_shared(K *kernel, int bytes)
     return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
 }
 
-template <typename T, int CH, bool GRAD, bool SAVED, bool FULL>
-cudaError_t launch_warp(const DistillArgs &a, int lanes, const Layout &lay, int sms, cudaStream_t stream)
+template <typename T, int LANES, int CH, bool GRAD, bool SAVED>
+cudaError_t launch_warp(const DistillArgs &a, const Layout &lay, int sms, cudaStream_t stream)
 {
-    auto *kernel = distill_warp_kernel<T, CH, GRAD, SAVED, FULL>;
+    auto *kernel = distill_warp_kernel<T, LANES, CH, GRAD, SAVED>;
     static const int regs = kernel_registers(kernel);
     const int shared = kWarps * kStages * lay.bytes();
     const cudaError_t e = allow_shared(kernel, shared);
     if (e != cudaSuccess) return e;
-    const long long per_block = kWarps * (32 / lanes), wanted = (a.rows + per_block - 1) / per_block;
+    const long long per_block = kWarps * (32 / LANES), wanted = (a.rows + per_block - 1) / per_block;
     const long long fit = (long long)sms * resident_blocks(regs, kWarps * 32, shared);
-    kernel<<<(unsigned int)(wanted < fit ? wanted : fit), kWarps * 32, shared, stream>>>(a, lanes, power_of_two(a.k, lanes), lay);
+    kernel<<<(unsigned int)(wanted < fit ? wanted : fit), kWarps * 32, shared, stream>>>(a, power_of_two(a.k, LANES), lay);
     return cudaGetLastError();
 }
 
@@ -596,30 +613,30 @@ bool launch_staged(const DistillArgs &a, int sms, cudaStream_t stream, cudaError
     constexpr int VEC = kPer16<T>, MOST = kElems / VEC;
     const bool aligned = rows_aligned16(a.x, a.rows, a.stride, sizeof(T));
     const int columns = a.n + (aligned ? 0 : VEC - 1);   // with those before an unaligned row
-    // Lanes per row: 32 elements a lane, so that what a row costs besides its elements is shared by the warp's rows; no
-    // fewer than entries; more while there are too few rows to give every SM eight warps.
+    // Lanes per row: 32 elements a lane, so that what a row costs besides its elements is shared by the warp's rows, and
+    // no fewer than entries; 16 bytes a lane where that is all there is, or while there are too few rows to give every
+    // SM eight warps.
     int lanes = power_of_two((columns + kElems - 1) / kElems, 32);
-    while (lanes < 32 && lanes < a.k) lanes *= 2;
-    while (lanes < 32 && lanes * VEC < columns && a.rows * lanes < 32ll * 8 * sms) lanes *= 2;
-    const Layout warp_lay{staged_row_bytes(a.n, sizeof(T), aligned), 32 / lanes, a.k, aligned};
+    while (lanes < 4 || (lanes < 32 && lanes < a.k)) lanes *= 2;
+    const int spread = power_of_two((columns + VEC - 1) / VEC, 64);
+    const bool one = spread <= 32 && (spread <= lanes || a.rows * lanes < 32ll * 8 * sms);
+    if (one && lanes < spread) lanes = spread;
+    const Layout warp_lay{staged_row_bytes(a.n, sizeof(T), aligned), 32 / lanes, a.k, aligned, aligned && a.wide ? a.n : 0};
     // (long lists of entries would leave room for one block only)
     if (columns <= kWarpRow && kWarps * kStages * warp_lay.bytes() <= 112 * 1024) {
-        const int need = (columns + lanes * VEC - 1) / (lanes * VEC);
-        if (need <= 1)
-            e = launch_warp<T, 1, GRAD, SAVED, false>(a, lanes, warp_lay, sms, stream);
-        else if (need <= 2)
-            e = launch_warp<T, 2, GRAD, SAVED, false>(a, lanes, warp_lay, sms, stream);
-        else if (lanes < 32)
-            e = launch_warp<T, MOST, GRAD, SAVED, false>(a, lanes, warp_lay, sms, stream);
-        else
-            e = launch_warp<T, MOST, GRAD, SAVED, true>(a, lanes, warp_lay, sms, stream);
+        switch (lanes) {
+        case 4: e = one ? launch_warp<T, 4, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 4, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
+        case 8: e = one ? launch_warp<T, 8, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 8, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
+        case 16: e = one ? launch_warp<T, 16, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 16, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
+        default: e = one ? launch_warp<T, 32, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 32, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
+        }
         return true;
     }
     const int threads = ((columns + kElems - 1) / kElems + 31) / 32 * 32;
     if (threads > 512 || a.rows < 2 * sms) return false;
     auto *kernel = distill_staged_kernel<T, GRAD, SAVED>;
     static const int regs = kernel_registers(kernel);
-    const Layout lay{staged_row_bytes(a.n, sizeof(T), aligned), 1, a.k, aligned};
+    const Layout lay{staged_row_bytes(a.n, sizeof(T), aligned), 1, a.k, aligned, aligned && a.wide ? a.n : 0};
     const int shared = kStages * lay.bytes();
     e = allow_shared(kernel, shared);
     if (e != cudaSuccess) return true;
@@ -707,7 +724,7 @@ int distill(const nbos_logits *l, const int32_t *hosts, const float *teacher, in
                   grad_loss, grad_scale, out_loss, out_stats, stats_in, out_grad, gstride, false};
     if (a.rows == 1) a.stride = a.gstride = l->n_hosts;
     const long long apart = static_cast<const char *>(l->data) - static_cast<const char *>(out_grad);
-    a.wide = apart % 16 == 0 && (a.stride - a.gstride) * (long long)dtype_bytes(l->dtype) % 16 == 0;
+    a.wide = !out_grad || (apart % 16 == 0 && (a.stride - a.gstride) * (long long)dtype_bytes(l->dtype) % 16 == 0);
     const cudaError_t e = l->dtype == NBOS_F32    ? dispatch<float>(a, sms, stream)
                           : l->dtype == NBOS_BF16 ? dispatch<__nv_bfloat16>(a, sms, stream)
                                                   : dispatch<__half>(a, sms, stream);
