@@ -17,10 +17,11 @@ namespace {
 
 using namespace policy;
 
-constexpr int kWarpRow = 1024;      // longest row of the warp form: 32 elements a lane
-constexpr int kElems = 16;          // row elements a thread holds in the block form (as many column sums beside them)
+constexpr int kWarpRow = 1024;      // longest row of the warp form
+constexpr int kElems = 16;          // row elements a thread holds in the cluster form (as many column sums beside them)
 constexpr int kMaxCluster = 8;
 constexpr int kWarps = 8;           // of a block of the warp form
+constexpr int kHeld = 32;           // row elements a thread holds in the staged forms
 constexpr int kHistHosts = 8192;    // counters kept in shared memory while counting
 
 struct BalanceArgs {
@@ -39,6 +40,7 @@ struct BalanceArgs {
     long long gstride;
     float *partial;          // [groups][parts][n] column sums of p
     int parts;
+    bool wide;               // the gradient is written 16 bytes at a time
 };
 
 // counts[g][h] += ..., totals[g] += (valid ids, rows that have one); grid (blocks, groups)
@@ -90,111 +92,272 @@ __device__ __forceinline__ GroupScale group_scale(const BalanceArgs &a, int grou
     return g;
 }
 
-// does any of the row's ids name a host? over `lanes` lanes
-__device__ __forceinline__ bool row_live(const BalanceArgs &a, long long row, bool active, int sub, int lanes)
+// does any of the k ids name a host? over the lanes of `group`, which start at `sub` = 0
+__device__ __forceinline__ bool any_host(const int *ids, int k, int n, bool active, int sub, int lanes, unsigned int group)
 {
-    float some = 0.0f;
-    for (int j = sub; active && j < a.k; j += lanes) {
-        const int h = a.hosts[row * a.k + j];
-        if (h >= 0 && h < a.n) some = 1.0f;
-    }
-    return lanes_max(some, lanes) > 0.0f;
+    bool some = false;
+    for (int j = sub; active && j < k; j += lanes) some = some || (ids[j] >= 0 && ids[j] < n);
+    return (__ballot_sync(kFull, some) & group) != 0;
 }
 
-// ---- warp form: `lanes` lanes per row; grid (parts, groups) ------------------------------------------------
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
-__global__ void __launch_bounds__(kWarps * 32) balance_warp_kernel(BalanceArgs a, int lanes)
+// ---- rows that a warp or a block holds, staged -------------------------------------------------------------
+struct Layout {   // bytes of a stage: rows, then ids, then statistics
+    int row_bytes, rows, k;
+    int whole;   // n if logits and gradient are handled 16 bytes at a time: columns below it need no look; else 0
+    __host__ __device__ int hosts_at() const { return row_bytes * rows; }
+    __host__ __device__ int stats_at() const { return hosts_at() + rows * k * 4; }
+    __host__ __device__ int bytes() const { return (stats_at() + rows * 8 + 15) & ~15; }
+};
+template <typename T>
+__device__ __forceinline__ void stage(const BalanceArgs &a, const Layout &lay, char *at, int slot, long long row, int sub, int team)
 {
-    extern __shared__ float s_f[];   // f of the group's hosts, padded to lanes * CH * VEC; then the column sums
-    const int lane = threadIdx.x & 31, sub = lane & (lanes - 1), warp = threadIdx.x >> 5;
-    const int group = blockIdx.y, width = lanes * CH * VEC;
+    stage_row(at + slot * lay.row_bytes, static_cast<const T *>(a.x) + row * a.stride, a.n, row * a.stride * (long long)sizeof(T), sub, team);
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at));
+    for (int i = sub; i < a.k; i += team) copy_async4(to + lay.hosts_at() + (slot * a.k + i) * 4, a.hosts + row * a.k + i);
+    if (a.stats_in && sub == 0) {
+        copy_async4(to + lay.stats_at() + slot * 8, a.stats_in + 2 * row);
+        copy_async4(to + lay.stats_at() + slot * 8 + 4, a.stats_in + 2 * row + 1);
+    }
+}
+__device__ __forceinline__ float2 staged_pair(const char *at)   // on a 4-byte boundary
+{
+    const float *f = reinterpret_cast<const float *>(at);
+    return make_float2(f[0], f[1]);
+}
+// A lane's elements of a staged row, chunk after chunk of `width` columns, from column `first`. VEC is 16 bytes' worth,
+// or 1 for rows that start anywhere: the columns of a lane have to be the same in every row.
+template <typename T, int VEC, int CH>
+__device__ __forceinline__ void load_staged(const T *row, int first, int width, int n, int whole, float (&v)[CH][VEC])
+{
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = first + c * width;
+        if constexpr (VEC == 1) {
+            v[c][0] = col < n ? to_float(row[col]) : neg_inf();
+        } else {
+            if ((c + 1) * width <= whole)
+                unpack16(*reinterpret_cast<const uint4 *>(row + col), v[c], T());
+            else
+                staged_cols<T, VEC>(row, col, n, v[c]);
+        }
+    }
+}
+// sum of v f over the lane's elements; f lies in shared memory by column
+template <int VEC, int CH>
+__device__ __forceinline__ float dot_all(const float (&v)[CH][VEC], const float *f, int first, int width)
+{
+    float d0 = 0.0f, d1 = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        if constexpr (VEC == 1) {
+            (c % 2 ? d1 : d0) += v[c][0] * f[first + c * width];
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) {
+                const float4 w = *reinterpret_cast<const float4 *>(f + first + c * width + i);
+                fma2(d0, d1, v[c][i], v[c][i + 1], w.x, w.y);
+                fma2(d0, d1, v[c][i + 2], v[c][i + 3], w.z, w.w);
+            }
+        }
+    }
+    return d0 + d1;
+}
+// acc += v inv, then v := v (f - dot) fac, which is written to the row's gradient if GRAD
+template <typename T, int VEC, int CH, bool GRAD>
+__device__ __forceinline__ void finish_row(float (&v)[CH][VEC], float (&acc)[CH][VEC], float inv, float fac, float dot, const float *f,
+                                           T *grad, int first, int width, int n, int whole, bool wide)
+{
+    const float shift = -fac * dot;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = first + c * width;
+        if constexpr (VEC == 1) {
+            acc[c][0] += v[c][0] * inv;
+            if (GRAD && col < n) __stcs(grad + col, from_float<T>(v[c][0] * (f[col] * fac + shift)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) fma2(acc[c][i], acc[c][i + 1], v[c][i], v[c][i + 1], inv, inv);
+            if (GRAD) {
+#pragma unroll
+                for (int i = 0; i < VEC; i += 4) {
+                    const float4 w = *reinterpret_cast<const float4 *>(f + col + i);
+                    float g[4] = {shift, shift, shift, shift};
+                    fma2(g[0], g[1], w.x, w.y, fac, fac);
+                    fma2(g[2], g[3], w.z, w.w, fac, fac);
+                    mul2(v[c][i], v[c][i + 1], g[0], g[1]);
+                    mul2(v[c][i + 2], v[c][i + 3], g[2], g[3]);
+                }
+                if ((c + 1) * width <= whole)
+                    __stcs(reinterpret_cast<uint4 *>(grad + col), pack16(v[c], T()));
+                else
+                    store_cols<T, VEC>(grad, col, n, v[c], wide);
+            }
+        }
+    }
+}
+
+// ---- warp form: LANES lanes per row, CH * VEC elements each; grid (parts, groups), which stays and walks over the rows
+template <typename T, int VEC, int LANES, int CH, bool GRAD>
+__global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArgs a, Layout lay)
+{
+    extern __shared__ __align__(16) char s_mem[];
+    constexpr int width = LANES * VEC, padded = width * CH, at_once = 32 / LANES;
+    float *s_f = reinterpret_cast<float *>(s_mem);   // f of the group's hosts; then the block's column sums
+    const int lane = threadIdx.x & 31, sub = lane & (LANES - 1), slot = lane / LANES, warp = threadIdx.x >> 5;
+    const unsigned int lanes_of_row = LANES == 32 ? kFull : ((1u << (LANES & 31)) - 1) << (slot * LANES);
+    const int group = blockIdx.y, stage_bytes = lay.bytes(), first = sub * VEC;
+    const bool saved = a.stats_in != nullptr;
+    char *mine = s_mem + padded * 4 + warp * kStages * stage_bytes;
+    const long long row0 = (long long)group * a.group_rows, step = (long long)gridDim.x * kWarps * at_once;
+    const long long base0 = ((long long)blockIdx.x * kWarps + warp) * at_once;
+    auto queue = [&](long long base, int st) {
+        if (base + slot < a.group_rows) stage<T>(a, lay, mine + st * stage_bytes, slot, row0 + base + slot, sub, LANES);
+        copies_commit();
+    };
+#pragma unroll
+    for (int st = 0; st < kStages; ++st) queue(base0 + st * step, st);
     const GroupScale gs = group_scale(a, group);
-    for (int i = threadIdx.x; i < width; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
+    for (int i = threadIdx.x; i < padded; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
     __syncthreads();
     float acc[CH][VEC];
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[c][i] = 0.0f;
-    const int rows_at_once = 32 / lanes;
-    const long long first = (long long)group * a.group_rows;
-    for (long long r0 = ((long long)blockIdx.x * kWarps + warp) * rows_at_once; r0 < a.group_rows;
-         r0 += (long long)gridDim.x * kWarps * rows_at_once) {
-        const bool active = r0 + lane / lanes < a.group_rows;
-        const long long row = first + r0 + (active ? lane / lanes : 0);
+    int st = 0;
+    for (long long base = base0; base < a.group_rows; base += step) {
+        copies_wait();
+        __syncwarp();
+        const bool active = base + slot < a.group_rows;
+        const int here = active ? slot : 0;
+        const long long row = row0 + base + here;
+        const char *at = mine + st * stage_bytes;
         const T *x = static_cast<const T *>(a.x) + row * a.stride;
+        const T *r = reinterpret_cast<const T *>(at + here * lay.row_bytes + (VEC == 1 ? row_shift(x) : 0));
+        const float2 given = saved ? staged_pair(at + lay.stats_at() + here * 8) : make_float2(0.0f, 0.0f);
         float v[CH][VEC];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) load_cols<T, VEC>(x, (c * lanes + sub) * VEC, active ? a.n : 0, neg_inf(), v[c]);
-        const bool live = row_live(a, row, active, sub, lanes);
-        float m = neg_inf(), s = 0.0f, dot = 0.0f;
-        if (SAVED) {
-            m = live ? a.stats_in[2 * row] : 0.0f;
-        } else {
+        load_staged<T, VEC, CH>(r, first, width, a.n, lay.whole, v);
+        const bool live = any_host(reinterpret_cast<const int *>(at + lay.hosts_at()) + here * a.k, a.k, a.n, active, sub, LANES, lanes_of_row);
+        __syncwarp();   // all that the stage holds has been read
+        queue(base + kStages * step, st);
+        // rows that are not live take part as rows of -inf, whatever they hold
+        if (__any_sync(kFull, !live)) {
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[c][i]);
-            m = lanes_max(m, lanes);
+                for (int i = 0; i < VEC; ++i) v[c][i] = live ? v[c][i] : neg_inf();
         }
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                v[c][i] = exp_from(v[c][i], m, kLog2e);
-                s += v[c][i];
-                if (GRAD) dot += v[c][i] * s_f[(c * lanes + sub) * VEC + i];
-            }
-        s = SAVED ? (live ? a.stats_in[2 * row + 1] : 1.0f) : lanes_sum(s, lanes);
-        if (GRAD) dot = lanes_sum(dot, lanes);
+        const float m = saved && live ? given.x : lanes_max(max_all<VEC, CH>(v), LANES);
+        float s = exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, kLog2e), dot = 0.0f;
+        if (GRAD) dot = lanes_sum(dot_all<VEC, CH>(v, s_f, first, width), LANES);
+        s = saved ? (live ? given.y : 0.0f) : lanes_sum(s, LANES);
         // a row of -inf has sum 0 and no probabilities
-        const float inv = live && s != 0.0f ? 1.0f / s : 0.0f;
-        if (!SAVED) {
-            if (live && a.stats && sub == 0) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+        const float inv = s != 0.0f ? reciprocal(s) : 0.0f;
+        if (!saved && live && a.stats && sub == 0) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+        // a lane without a row (the group's last ones) writes nothing
+        finish_row<T, VEC, CH, GRAD>(v, acc, inv, gs.grad * inv, dot * inv, s_f, static_cast<T *>(a.grad) + row * a.gstride, first, width,
+                                     active ? a.n : 0, active ? lay.whole : 0, a.wide);
+        st = st == kStages - 1 ? 0 : st + 1;
+    }
+    if (saved) return;
+    // the block's column sums: rows of one warp, then warp after warp
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+#pragma unroll
+            for (int off = 16; off >= LANES; off >>= 1) acc[c][i] += __shfl_xor_sync(kFull, acc[c][i], off);
+    for (int w = 0; w < kWarps; ++w) {
+        __syncthreads();
+        if (warp == w && lane < LANES) {
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[c][i] += live ? v[c][i] * inv : 0.0f;
-        }
-        if (GRAD) {
-            T *grad = static_cast<T *>(a.grad) + row * a.gstride;
-            dot *= inv;
-            const float fac = gs.grad * inv;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    v[c][i] = live ? v[c][i] * fac * (s_f[(c * lanes + sub) * VEC + i] - dot) : 0.0f;
-                store_cols<T, VEC>(grad, (c * lanes + sub) * VEC, active ? a.n : 0, v[c]);
-            }
+                for (int i = 0; i < VEC; ++i) {
+                    float *to = &s_f[first + c * width + i];
+                    *to = w ? *to + acc[c][i] : acc[c][i];
+                }
         }
     }
-    if constexpr (!SAVED) {
-        // the block's column sums: rows of one warp, then warp after warp
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                for (int off = 16; off >= lanes; off >>= 1) acc[c][i] += __shfl_xor_sync(kFull, acc[c][i], off);
-        for (int w = 0; w < kWarps; ++w) {
-            __syncthreads();
-            if (warp == w && lane < lanes) {
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        float *to = &s_f[(c * lanes + sub) * VEC + i];
-                        *to = w ? *to + acc[c][i] : acc[c][i];
-                    }
-            }
-        }
-        __syncthreads();
-        float *out = a.partial + ((size_t)group * a.parts + blockIdx.x) * a.n;
-        for (int i = threadIdx.x; i < a.n; i += blockDim.x) out[i] = s_f[i];
-    }
+    __syncthreads();
+    float *out = a.partial + ((size_t)group * a.parts + blockIdx.x) * a.n;
+    for (int i = threadIdx.x; i < a.n; i += blockDim.x) out[i] = s_f[i];
 }
 
-// ---- block form: one block or cluster of cs blocks per row at a time; grid (parts * cs, groups) -------------
+// ---- block form: one row at a time per block, kHeld elements a thread; grid (parts, groups) -----------------
+template <typename T, int VEC, bool GRAD>
+__global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, Layout lay)
+{
+    constexpr int CH = kHeld / VEC;
+    extern __shared__ __align__(16) char s_mem[];
+    __shared__ float4 s_stats[2][16];
+    float *s_f = reinterpret_cast<float *>(s_mem);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int group = blockIdx.y, stage_bytes = lay.bytes(), width = blockDim.x * VEC, first = threadIdx.x * VEC;
+    const bool saved = a.stats_in != nullptr;
+    char *stages = s_mem + width * CH * 4;
+    const long long row0 = (long long)group * a.group_rows;
+    auto queue = [&](long long r, int st) {
+        if (r < a.group_rows) stage<T>(a, lay, stages + st * stage_bytes, 0, row0 + r, threadIdx.x, blockDim.x);
+        copies_commit();
+    };
+#pragma unroll
+    for (int st = 0; st < kStages; ++st) queue(blockIdx.x + (long long)st * gridDim.x, st);
+    const GroupScale gs = group_scale(a, group);
+    for (int i = threadIdx.x; i < width * CH; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
+    float acc[CH][VEC];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[c][i] = 0.0f;
+    int st = 0, turn = 0;
+    for (long long r = blockIdx.x; r < a.group_rows; r += gridDim.x, turn ^= 1) {
+        copies_wait();
+        __syncthreads();
+        const long long row = row0 + r;
+        const char *at = stages + st * stage_bytes;
+        const T *x = static_cast<const T *>(a.x) + row * a.stride;
+        const T *staged = reinterpret_cast<const T *>(at + (VEC == 1 ? row_shift(x) : 0));
+        const float2 given = saved ? staged_pair(at + lay.stats_at()) : make_float2(0.0f, 0.0f);
+        float v[CH][VEC];
+        load_staged<T, VEC, CH>(staged, first, width, a.n, lay.whole, v);
+        const bool live = any_host(reinterpret_cast<const int *>(at + lay.hosts_at()), a.k, a.n, true, lane, 32, kFull);
+        if (!live) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[c][i] = neg_inf();
+        }
+        float m = saved && live ? given.x : lanes_max(max_all<VEC, CH>(v), 32);
+        const float m_warp = m;
+        float s = lanes_sum(exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, kLog2e), 32), dot = 0.0f;
+        if (GRAD) dot = lanes_sum(dot_all<VEC, CH>(v, s_f, first, width), 32);
+        // one exchange for all three, each relative to the warp's maximum
+        if (lane == 0) s_stats[turn][warp] = make_float4(m, s, dot, 0.0f);
+        __syncthreads();
+        queue(r + kStages * (long long)gridDim.x, st);   // all that the stage holds has been read
+        const float4 w = lane < warps ? s_stats[turn][lane] : make_float4(neg_inf(), 0.0f, 0.0f, 0.0f);
+        if (!saved) m = lanes_max(w.x, 32);
+        const float scale = saved ? 1.0f : exp_from(w.x, m, kLog2e);
+        s = saved ? (live ? given.y : 0.0f) : lanes_sum(w.y * scale, 32);
+        if (GRAD) dot = lanes_sum(w.z * scale, 32);
+        const float inv = s != 0.0f ? reciprocal(s) : 0.0f;
+        if (!saved && live && a.stats && threadIdx.x == 0) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+        const float own = inv * (saved ? 1.0f : exp_from(m_warp, m, kLog2e));
+        finish_row<T, VEC, CH, GRAD>(v, acc, own, gs.grad * own, dot * inv, s_f, static_cast<T *>(a.grad) + row * a.gstride, first, width, a.n,
+                                     lay.whole, a.wide);
+        st = st == kStages - 1 ? 0 : st + 1;
+    }
+    if (saved) return;
+    float *out = a.partial + ((size_t)group * a.parts + blockIdx.x) * a.n;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (first + c * width + i < a.n) out[first + c * width + i] = acc[c][i];
+}
+
+// ---- cluster form: cs blocks per row at a time; grid (parts * cs, groups) -----------------------------------
 // KEEP: row and column sums stay in registers; otherwise the row is read once more and the sums live in `partial`.
 template <typename T, int VEC, bool KEEP, bool GRAD, bool SAVED>
 __global__ void __launch_bounds__(1024, 1) balance_block_kernel(BalanceArgs a, int cs, int span)
@@ -233,7 +396,7 @@ __global__ void __launch_bounds__(1024, 1) balance_block_kernel(BalanceArgs a, i
             for (int c = 0; c < CH; ++c)
                 load_cols<T, VEC>(x, first_col + c * chunk + threadIdx.x * VEC, end_col, neg_inf(), v[c]);
         }
-        const bool live = row_live(a, row, true, lane, 32);
+        const bool live = any_host(a.hosts + row * a.k, a.k, a.n, true, lane, 32, kFull);
         if (SAVED) m = live ? a.stats_in[2 * row] : 0.0f;
         if (KEEP) {
             if (!SAVED) {
@@ -306,7 +469,7 @@ __global__ void __launch_bounds__(1024, 1) balance_block_kernel(BalanceArgs a, i
                     if (!SAVED) acc[c][i] += p;
                     if (GRAD) v[c][i] = live ? p * gs.grad * (s_f[c * chunk + threadIdx.x * VEC + i] - dot) : 0.0f;
                 }
-                if (GRAD) store_cols<T, VEC>(grad, first_col + c * chunk + threadIdx.x * VEC, end_col, v[c]);
+                if (GRAD) store_cols<T, VEC>(grad, first_col + c * chunk + threadIdx.x * VEC, end_col, v[c], a.wide);
             }
         } else {
             for (long long col = first_col + threadIdx.x * VEC; col < end_col; col += chunk) {
@@ -320,7 +483,7 @@ __global__ void __launch_bounds__(1024, 1) balance_block_kernel(BalanceArgs a, i
                         if (GRAD) w[i] = live ? p * gs.grad * ((float)counts[col + i] * gs.inv_total - dot) : 0.0f;
                     }
                 }
-                if (GRAD) store_cols<T, VEC>(grad, col, end_col, w);
+                if (GRAD) store_cols<T, VEC>(grad, col, end_col, w, a.wide);
             }
         }
     }
@@ -376,49 +539,124 @@ __global__ void __launch_bounds__(1024) finish_kernel(BalanceArgs a, float *shar
     if (threadIdx.x == 0) loss[group] = (float)(total * (double)a.n);
 }
 
+enum Form { WARP, BLOCK, CLUSTER };
 struct Plan {
-    bool warp_form, keep;
-    int lanes, need;        // warp form: lanes per row, chunks per lane
-    int cs, threads, span;  // block form
+    Form form;
+    bool keep, vec;
+    int lanes, chunks;      // warp form: lanes per row, chunks per lane
+    int cs, threads, span;  // cluster form (threads: block form too)
     int parts;
+    Layout lay;
+    int shared;
 };
 
-// VEC elements per load; rows of one group
-Plan make_plan(const BalanceArgs &a, int groups, int vec, int sms)
+// The warp form's shape: as many elements a lane as the row fills well, so that what a row costs besides is shared.
+void warp_shape(int n, int vec, int &lanes, int &chunks)
+{
+    const int most = kHeld / vec;
+    if (vec == 1) {
+        lanes = n <= 32 ? 8 : 32;
+        chunks = n <= 32 ? 4 : n <= 64 ? 2 : n <= 256 ? 8 : n <= 512 ? 16 : 32;
+        return;
+    }
+    for (chunks = most; ; chunks = chunks > 2 ? 2 : 1) {
+        lanes = 4;
+        while (lanes < 32 && lanes * vec * chunks < n) lanes *= 2;
+        if (chunks == 1 || lanes * vec * chunks <= n + n / 2 || lanes * vec * 1 < n) break;
+    }
+    if (lanes * vec * chunks < n) chunks = most, lanes = 32;
+}
+
+Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms)
 {
     Plan p = {};
-    p.warp_form = a.n <= kWarpRow;
-    long long wanted;
-    if (p.warp_form) {
-        p.lanes = 1;
-        while (p.lanes < 32 && p.lanes * vec < a.n) p.lanes *= 2;
-        p.need = (a.n + p.lanes * vec - 1) / (p.lanes * vec);
-        const long long at_once = kWarps * (32 / p.lanes);
-        wanted = (a.group_rows + at_once - 1) / at_once;
-        const long long fill = (3ll * sms + groups - 1) / groups;
-        p.parts = (int)(wanted < fill ? wanted : fill);
-    } else {
-        auto threads_for = [&](int c) { return ((a.n + c * kElems - 1) / (c * kElems) + 31) / 32 * 32; };
-        p.keep = a.n <= kMaxCluster * 1024 * kElems;
-        p.cs = 1;
-        while (p.cs < kMaxCluster && (threads_for(p.cs) > 1024 || (a.group_rows * groups * p.cs < 2 * sms && threads_for(p.cs) > 128)))
-            p.cs *= 2;
-        p.threads = p.keep ? threads_for(p.cs) : 1024;
-        p.span = ((a.n + p.cs - 1) / p.cs + vec - 1) / vec * vec;
-        const int resident = p.threads > 512 ? 1 : (1024 / p.threads);
-        const long long fill = ((long long)sms * resident / p.cs + groups - 1) / groups;
-        p.parts = (int)(a.group_rows < fill ? a.group_rows : (fill > 1 ? fill : 1));
+    p.vec = aligned;
+    const int per = aligned ? 16 / elem : 1;
+    p.lay = Layout{staged_row_bytes(a.n, elem, aligned), 1, a.k, aligned && a.wide ? a.n : 0};
+    // rows to go round: one part takes at least a few, and the parts fill the SMs
+    auto parts_for = [&](long long at_once, int resident) {
+        const long long wanted = (a.group_rows + at_once - 1) / at_once;
+        long long fill = ((long long)sms * resident + groups - 1) / groups;
+        if (fill * groups > (long long)sms * resident && groups < sms * resident) fill = (long long)sms * resident / groups;   // one wave
+        if (fill < 1) fill = 1;
+        return (int)(wanted < fill ? wanted : fill);
+    };
+    if (a.n <= kWarpRow) {
+        p.form = WARP;
+        warp_shape(a.n, per, p.lanes, p.chunks);
+        p.lay.rows = 32 / p.lanes;
+        p.shared = p.lanes * per * p.chunks * 4 + kWarps * kStages * p.lay.bytes();
+        if (p.shared <= 112 * 1024) {
+            p.parts = parts_for((long long)kWarps * p.lay.rows, 2);
+            return p;
+        }
+        p.lay.rows = 1;
     }
-    if (p.parts < 1) p.parts = 1;
+    p.threads = ((a.n + kHeld - 1) / kHeld + 31) / 32 * 32;
+    p.shared = p.threads * kHeld * 4 + kStages * p.lay.bytes();
+    if (p.threads <= 512 && p.shared <= 220 * 1024 && a.group_rows * groups >= 2 * sms) {
+        p.form = BLOCK;
+        p.parts = parts_for(1, resident_blocks(128, p.threads, p.shared + 512));
+        return p;
+    }
+    p.form = CLUSTER;
+    auto threads_for = [&](int c) { return ((a.n + c * kElems - 1) / (c * kElems) + 31) / 32 * 32; };
+    p.keep = a.n <= kMaxCluster * 1024 * kElems;
+    p.cs = 1;
+    while (p.cs < kMaxCluster && (threads_for(p.cs) > 1024 || (a.group_rows * groups * p.cs < 2 * sms && threads_for(p.cs) > 128))) p.cs *= 2;
+    p.threads = p.keep ? threads_for(p.cs) : 1024;
+    p.span = ((a.n + p.cs - 1) / p.cs + per - 1) / per * per;
+    const int resident = p.threads > 512 ? 1 : (1024 / p.threads);
+    const long long fill = ((long long)sms * resident / p.cs + groups - 1) / groups;
+    p.parts = (int)(a.group_rows < fill ? a.group_rows : (fill > 1 ? fill : 1));
     return p;
 }
 
-template <typename T, int VEC, int CH, bool GRAD, bool SAVED>
+template <typename K>
+cudaError_t allow_shared(K *kernel, int bytes)
+{
+    return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+}
+template <typename T, int VEC, int LANES, int CH, bool GRAD>
 cudaError_t launch_warp(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
 {
-    const size_t smem = (size_t)p.lanes * CH * VEC * sizeof(float);
-    balance_warp_kernel<T, VEC, CH, GRAD, SAVED><<<dim3(p.parts, groups), kWarps * 32, smem, stream>>>(a, p.lanes);
+    auto *kernel = balance_warp_kernel<T, VEC, LANES, CH, GRAD>;
+    const cudaError_t e = allow_shared(kernel, p.shared);
+    if (e != cudaSuccess) return e;
+    kernel<<<dim3(p.parts, groups), kWarps * 32, p.shared, stream>>>(a, p.lay);
     return cudaGetLastError();
+}
+template <typename T, int VEC, int CH, bool GRAD>
+cudaError_t launch_lanes(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
+{
+    switch (p.lanes) {
+    case 4: return launch_warp<T, VEC, 4, CH, GRAD>(a, groups, p, stream);
+    case 8: return launch_warp<T, VEC, 8, CH, GRAD>(a, groups, p, stream);
+    case 16: return launch_warp<T, VEC, 16, CH, GRAD>(a, groups, p, stream);
+    default: return launch_warp<T, VEC, 32, CH, GRAD>(a, groups, p, stream);
+    }
+}
+template <typename T, bool GRAD>
+cudaError_t launch_rows(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
+{
+    constexpr int V = kPer16<T>;
+    if (p.form == BLOCK) {
+        auto *kernel = p.vec ? balance_staged_kernel<T, V, GRAD> : balance_staged_kernel<T, 1, GRAD>;
+        const cudaError_t e = allow_shared(kernel, p.shared);
+        if (e != cudaSuccess) return e;
+        kernel<<<dim3(p.parts, groups), p.threads, p.shared, stream>>>(a, p.lay);
+        return cudaGetLastError();
+    }
+    if (p.vec) {
+        if (p.chunks == 1) return launch_lanes<T, V, 1, GRAD>(a, groups, p, stream);
+        if (p.chunks == 2) return launch_lanes<T, V, 2, GRAD>(a, groups, p, stream);
+        return launch_lanes<T, V, kHeld / V, GRAD>(a, groups, p, stream);
+    }
+    if (p.lanes == 8) return launch_warp<T, 1, 8, 4, GRAD>(a, groups, p, stream);
+    if (p.chunks == 2) return launch_warp<T, 1, 32, 2, GRAD>(a, groups, p, stream);
+    if (p.chunks == 8) return launch_warp<T, 1, 32, 8, GRAD>(a, groups, p, stream);
+    if (p.chunks == 16) return launch_warp<T, 1, 32, 16, GRAD>(a, groups, p, stream);
+    return launch_warp<T, 1, 32, 32, GRAD>(a, groups, p, stream);
 }
 
 template <typename T, int VEC, bool KEEP, bool GRAD, bool SAVED>
@@ -445,29 +683,19 @@ cudaError_t launch_block(const BalanceArgs &a, int groups, const Plan &p, cudaSt
 }
 
 template <typename T, int VEC, bool GRAD, bool SAVED>
-cudaError_t launch(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
+cudaError_t launch_cluster(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
 {
-    if (!p.warp_form)
-        return p.keep ? launch_block<T, VEC, true, GRAD, SAVED>(a, groups, p, stream)
-                      : launch_block<T, VEC, false, GRAD, SAVED>(a, groups, p, stream);
-    if (p.need <= 1) return launch_warp<T, VEC, 1, GRAD, SAVED>(a, groups, p, stream);
-    if (p.need <= 2) return launch_warp<T, VEC, 2, GRAD, SAVED>(a, groups, p, stream);
-    if (VEC >= 4 || p.need <= 4) return launch_warp<T, VEC, (VEC == 4 ? 8 : 4), GRAD, SAVED>(a, groups, p, stream);
-    if constexpr (VEC == 1) {
-        if (p.need <= 8) return launch_warp<T, VEC, 8, GRAD, SAVED>(a, groups, p, stream);
-        if (p.need <= 16) return launch_warp<T, VEC, 16, GRAD, SAVED>(a, groups, p, stream);
-        return launch_warp<T, VEC, 32, GRAD, SAVED>(a, groups, p, stream);
-    }
-    return cudaErrorUnknown;   // not reached
+    return p.keep ? launch_block<T, VEC, true, GRAD, SAVED>(a, groups, p, stream) : launch_block<T, VEC, false, GRAD, SAVED>(a, groups, p, stream);
 }
 
 template <typename T>
-cudaError_t dispatch(const BalanceArgs &a, int groups, const Plan &p, bool vec, cudaStream_t stream)
+cudaError_t dispatch(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
 {
     constexpr int V = kPer16<T>;
-    if (a.stats_in) return vec ? launch<T, V, true, true>(a, groups, p, stream) : launch<T, 1, true, true>(a, groups, p, stream);
-    if (a.grad) return vec ? launch<T, V, true, false>(a, groups, p, stream) : launch<T, 1, true, false>(a, groups, p, stream);
-    return vec ? launch<T, V, false, false>(a, groups, p, stream) : launch<T, 1, false, false>(a, groups, p, stream);
+    if (p.form != CLUSTER) return a.grad ? launch_rows<T, true>(a, groups, p, stream) : launch_rows<T, false>(a, groups, p, stream);
+    if (a.stats_in) return p.vec ? launch_cluster<T, V, true, true>(a, groups, p, stream) : launch_cluster<T, 1, true, true>(a, groups, p, stream);
+    if (a.grad) return p.vec ? launch_cluster<T, V, true, false>(a, groups, p, stream) : launch_cluster<T, 1, true, false>(a, groups, p, stream);
+    return p.vec ? launch_cluster<T, V, false, false>(a, groups, p, stream) : launch_cluster<T, 1, false, false>(a, groups, p, stream);
 }
 
 int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t k, const float *stats_in,
@@ -501,8 +729,10 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
     a.grad = out_grad, a.gstride = gstride;
     if (l->rows == 1) a.stride = a.gstride = l->n_hosts;
     const size_t elem = dtype_bytes(l->dtype);
-    const bool vec = rows_aligned16(a.x, l->rows, a.stride, elem) && (!a.grad || rows_aligned16(a.grad, l->rows, a.gstride, elem));
-    const Plan p = make_plan(a, groups, vec ? (int)(16 / elem) : 1, sms);
+    // the path, and with it every rounding, goes by the logits alone: the loss is the same with a gradient or without
+    const bool aligned = rows_aligned16(a.x, l->rows, a.stride, elem);
+    a.wide = !a.grad || rows_aligned16(a.grad, l->rows, a.gstride, elem);
+    const Plan p = make_plan(a, groups, (int)elem, aligned, sms);
     a.parts = p.parts;
 
     // workspace: totals and tickets (cleared), the counts if the caller takes none, the loss and column sums in parts
@@ -539,9 +769,9 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
         e = cudaGetLastError();
     }
     if (e == cudaSuccess)
-        e = l->dtype == NBOS_F32    ? dispatch<float>(a, groups, p, vec, stream)
-            : l->dtype == NBOS_BF16 ? dispatch<__nv_bfloat16>(a, groups, p, vec, stream)
-                                    : dispatch<__half>(a, groups, p, vec, stream);
+        e = l->dtype == NBOS_F32    ? dispatch<float>(a, groups, p, stream)
+            : l->dtype == NBOS_BF16 ? dispatch<__nv_bfloat16>(a, groups, p, stream)
+                                    : dispatch<__half>(a, groups, p, stream);
     if (e == cudaSuccess && forward) {
         int at_once = 1;
         while (at_once < 32 && at_once < p.parts) at_once *= 2;
