@@ -39,7 +39,9 @@ struct BalanceArgs {
     void *grad;
     long long gstride;
     float *partial;          // [groups][parts][n] column sums of p
-    int parts;
+    int parts;               // of a group at most
+    int groups;
+    long long block_rows;    // rows of all groups that a block takes, one stretch after the other (staged forms)
     bool wide;               // the gradient is written 16 bytes at a time
 };
 
@@ -79,6 +81,9 @@ __global__ void __launch_bounds__(256) count_kernel(const int32_t *hosts, long l
     for (int i = threadIdx.x; in_shared && i < n; i += blockDim.x)
         if (s_hist[i]) atomicAdd(&out[i], s_hist[i]);
 }
+
+// The blocks that take rows of a group are first_block, first_block + 1, ...: its parts, in this order.
+__device__ __forceinline__ long long first_block(const BalanceArgs &a, long long group) { return group * a.group_rows / a.block_rows; }
 
 struct GroupScale {
     float inv_total, grad;   // 1 / sum of counts; n / live * grad_scale * grad_loss
@@ -196,7 +201,7 @@ __device__ __forceinline__ void finish_row(float (&v)[CH][VEC], float (&acc)[CH]
     }
 }
 
-// ---- warp form: LANES lanes per row, CH * VEC elements each; grid (parts, groups), which stays and walks over the rows
+// ---- warp form: LANES lanes per row, CH * VEC elements each; a block walks over its rows, group after group --
 template <typename T, int VEC, int LANES, int CH, bool GRAD>
 __global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArgs a, Layout lay)
 {
@@ -205,13 +210,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArg
     float *s_f = reinterpret_cast<float *>(s_mem);   // f of the group's hosts; then the block's column sums
     const int lane = threadIdx.x & 31, sub = lane & (LANES - 1), slot = lane / LANES, warp = threadIdx.x >> 5;
     const unsigned int lanes_of_row = LANES == 32 ? kFull : ((1u << (LANES & 31)) - 1) << (slot * LANES);
-    const int group = blockIdx.y, stage_bytes = lay.bytes(), first = sub * VEC;
+    const int stage_bytes = lay.bytes(), first = sub * VEC;
     const bool saved = a.stats_in != nullptr;
     char *mine = s_mem + padded * 4 + warp * kStages * stage_bytes;
-    const long long row0 = (long long)group * a.group_rows, step = (long long)gridDim.x * kWarps * at_once;
-    const long long base0 = ((long long)blockIdx.x * kWarps + warp) * at_once;
-    auto queue = [&](long long base, int st) {
-        if (base + slot < a.group_rows) stage<T>(a, lay, mine + st * stage_bytes, slot, row0 + base + slot, sub, LANES);
+    const long long begin = blockIdx.x * a.block_rows, all_rows = a.group_rows * a.groups;
+    const long long end = begin + a.block_rows < all_rows ? begin + a.block_rows : all_rows;
+    constexpr int step = kWarps * at_once;
+    for (int group = (int)(begin / a.group_rows); group < a.groups && group * a.group_rows < end; ++group) {
+    // the block's rows of this group
+    const long long row0 = max(begin, group * a.group_rows);
+    const int rows = (int)(min(end, (group + 1) * a.group_rows) - row0);
+    const int base0 = warp * at_once;
+    auto queue = [&](int base, int st) {
+        if (base + slot < rows) stage<T>(a, lay, mine + st * stage_bytes, slot, row0 + base + slot, sub, LANES);
         copies_commit();
     };
 #pragma unroll
@@ -225,10 +236,10 @@ __global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArg
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[c][i] = 0.0f;
     int st = 0;
-    for (long long base = base0; base < a.group_rows; base += step) {
+    for (int base = base0; base < rows; base += step) {
         copies_wait();
         __syncwarp();
-        const bool active = base + slot < a.group_rows;
+        const bool active = base + slot < rows;
         const int here = active ? slot : 0;
         const long long row = row0 + base + here;
         const char *at = mine + st * stage_bytes;
@@ -247,7 +258,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArg
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) v[c][i] = live ? v[c][i] : neg_inf();
         }
-        const float m = saved && live ? given.x : lanes_max(max_all<VEC, CH>(v), LANES);
+        // (not a choice between a lane's own value and the exchange: every lane takes part in that)
+        const float top = saved ? given.x : lanes_max(max_all<VEC, CH>(v), LANES);
+        const float m = live ? top : neg_inf();
         float s = exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, kLog2e), dot = 0.0f;
         if (GRAD) dot = lanes_sum(dot_all<VEC, CH>(v, s_f, first, width), LANES);
         s = saved ? (live ? given.y : 0.0f) : lanes_sum(s, LANES);
@@ -259,32 +272,36 @@ __global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArg
                                      active ? a.n : 0, active ? lay.whole : 0, a.wide);
         st = st == kStages - 1 ? 0 : st + 1;
     }
-    if (saved) return;
-    // the block's column sums: rows of one warp, then warp after warp
+    copies_drain();
+    if (!saved) {
+        // the block's column sums: rows of one warp, then warp after warp
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
+            for (int i = 0; i < VEC; ++i)
 #pragma unroll
-            for (int off = 16; off >= LANES; off >>= 1) acc[c][i] += __shfl_xor_sync(kFull, acc[c][i], off);
-    for (int w = 0; w < kWarps; ++w) {
-        __syncthreads();
-        if (warp == w && lane < LANES) {
+                for (int off = 16; off >= LANES; off >>= 1) acc[c][i] += __shfl_xor_sync(kFull, acc[c][i], off);
+        for (int w = 0; w < kWarps; ++w) {
+            __syncthreads();
+            if (warp == w && lane < LANES) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+                for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    float *to = &s_f[first + c * width + i];
-                    *to = w ? *to + acc[c][i] : acc[c][i];
-                }
+                    for (int i = 0; i < VEC; ++i) {
+                        float *to = &s_f[first + c * width + i];
+                        *to = w ? *to + acc[c][i] : acc[c][i];
+                    }
+            }
         }
+        __syncthreads();
+        float *out = a.partial + ((size_t)group * a.parts + (blockIdx.x - first_block(a, group))) * a.n;
+        for (int i = threadIdx.x; i < a.n; i += blockDim.x) out[i] = s_f[i];
     }
-    __syncthreads();
-    float *out = a.partial + ((size_t)group * a.parts + blockIdx.x) * a.n;
-    for (int i = threadIdx.x; i < a.n; i += blockDim.x) out[i] = s_f[i];
+    __syncthreads();   // f of the next group may be written
+    }
 }
 
-// ---- block form: one row at a time per block, kHeld elements a thread; grid (parts, groups) -----------------
+// ---- block form: one row at a time per block, kHeld elements a thread; a block walks over its rows, group after group
 template <typename T, int VEC, bool GRAD>
 __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, Layout lay)
 {
@@ -293,16 +310,22 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
     __shared__ float4 s_stats[2][16];
     float *s_f = reinterpret_cast<float *>(s_mem);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int group = blockIdx.y, stage_bytes = lay.bytes(), width = blockDim.x * VEC, first = threadIdx.x * VEC;
+    const int stage_bytes = lay.bytes(), width = blockDim.x * VEC, first = threadIdx.x * VEC;
     const bool saved = a.stats_in != nullptr;
     char *stages = s_mem + width * CH * 4;
-    const long long row0 = (long long)group * a.group_rows;
-    auto queue = [&](long long r, int st) {
-        if (r < a.group_rows) stage<T>(a, lay, stages + st * stage_bytes, 0, row0 + r, threadIdx.x, blockDim.x);
+    const long long begin = blockIdx.x * a.block_rows, all_rows = a.group_rows * a.groups;
+    const long long end = begin + a.block_rows < all_rows ? begin + a.block_rows : all_rows;
+    int turn = 0;
+    for (int group = (int)(begin / a.group_rows); group < a.groups && group * a.group_rows < end; ++group) {
+    // the block's rows of this group
+    const long long row0 = max(begin, group * a.group_rows);
+    const int rows = (int)(min(end, (group + 1) * a.group_rows) - row0);
+    auto queue = [&](int r, int st) {
+        if (r < rows) stage<T>(a, lay, stages + st * stage_bytes, 0, row0 + r, threadIdx.x, blockDim.x);
         copies_commit();
     };
 #pragma unroll
-    for (int st = 0; st < kStages; ++st) queue(blockIdx.x + (long long)st * gridDim.x, st);
+    for (int st = 0; st < kStages; ++st) queue(st, st);
     const GroupScale gs = group_scale(a, group);
     for (int i = threadIdx.x; i < width * CH; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
     float acc[CH][VEC];
@@ -310,8 +333,8 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[c][i] = 0.0f;
-    int st = 0, turn = 0;
-    for (long long r = blockIdx.x; r < a.group_rows; r += gridDim.x, turn ^= 1) {
+    int st = 0;
+    for (int r = 0; r < rows; ++r, turn ^= 1) {
         copies_wait();
         __syncthreads();
         const long long row = row0 + r;
@@ -328,14 +351,15 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) v[c][i] = neg_inf();
         }
-        float m = saved && live ? given.x : lanes_max(max_all<VEC, CH>(v), 32);
+        const float top = saved ? given.x : lanes_max(max_all<VEC, CH>(v), 32);
+        float m = live ? top : neg_inf();
         const float m_warp = m;
         float s = lanes_sum(exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, kLog2e), 32), dot = 0.0f;
         if (GRAD) dot = lanes_sum(dot_all<VEC, CH>(v, s_f, first, width), 32);
         // one exchange for all three, each relative to the warp's maximum
         if (lane == 0) s_stats[turn][warp] = make_float4(m, s, dot, 0.0f);
         __syncthreads();
-        queue(r + kStages * (long long)gridDim.x, st);   // all that the stage holds has been read
+        queue(r + kStages, st);   // all that the stage holds has been read
         const float4 w = lane < warps ? s_stats[turn][lane] : make_float4(neg_inf(), 0.0f, 0.0f, 0.0f);
         if (!saved) m = lanes_max(w.x, 32);
         const float scale = saved ? 1.0f : exp_from(w.x, m, kLog2e);
@@ -348,13 +372,15 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
                                      lay.whole, a.wide);
         st = st == kStages - 1 ? 0 : st + 1;
     }
-    if (saved) return;
-    float *out = a.partial + ((size_t)group * a.parts + blockIdx.x) * a.n;
+    copies_drain();
+    float *out = a.partial + ((size_t)group * a.parts + (blockIdx.x - first_block(a, group))) * a.n;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
-            if (first + c * width + i < a.n) out[first + c * width + i] = acc[c][i];
+            if (!saved && first + c * width + i < a.n) out[first + c * width + i] = acc[c][i];
+    __syncthreads();   // f of the next group may be written
+    }
 }
 
 // ---- cluster form: cs blocks per row at a time; grid (parts * cs, groups) -----------------------------------
@@ -508,8 +534,9 @@ __global__ void __launch_bounds__(1024) finish_kernel(BalanceArgs a, float *shar
     __shared__ unsigned int s_last;
     const int group = blockIdx.y, col = blockIdx.x * 32 + threadIdx.x;
     double sum = 0.0;
+    const int parts = a.block_rows ? (int)((((long long)group + 1) * a.group_rows - 1) / a.block_rows - first_block(a, group)) + 1 : a.parts;
     if (col < a.n)
-        for (int p = threadIdx.y; p < a.parts; p += blockDim.y) sum += (double)a.partial[((size_t)group * a.parts + p) * a.n + col];
+        for (int p = threadIdx.y; p < parts; p += blockDim.y) sum += (double)a.partial[((size_t)group * a.parts + p) * a.n + col];
     s_sum[threadIdx.y][threadIdx.x] = sum;
     __syncthreads();
     if (threadIdx.y != 0) return;
@@ -545,7 +572,9 @@ struct Plan {
     bool keep, vec;
     int lanes, chunks;      // warp form: lanes per row, chunks per lane
     int cs, threads, span;  // cluster form (threads: block form too)
-    int parts;
+    int parts;              // of a group at most
+    int blocks;             // staged forms
+    long long block_rows;
     Layout lay;
     int shared;
 };
@@ -573,13 +602,13 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     p.vec = aligned;
     const int per = aligned ? 16 / elem : 1;
     p.lay = Layout{staged_row_bytes(a.n, elem, aligned), 1, a.k, aligned && a.wide ? a.n : 0};
-    // rows to go round: one part takes at least a few, and the parts fill the SMs
-    auto parts_for = [&](long long at_once, int resident) {
-        const long long wanted = (a.group_rows + at_once - 1) / at_once;
-        long long fill = ((long long)sms * resident + groups - 1) / groups;
-        if (fill * groups > (long long)sms * resident && groups < sms * resident) fill = (long long)sms * resident / groups;   // one wave
-        if (fill < 1) fill = 1;
-        return (int)(wanted < fill ? wanted : fill);
+    // the rows of all groups in even stretches, as many as there are blocks at once
+    auto stretches = [&](long long at_once, int resident) {
+        const long long rows = a.group_rows * groups, most = (long long)sms * resident;
+        const long long rounds = (rows + most * at_once - 1) / (most * at_once);
+        p.block_rows = rounds * at_once;
+        p.blocks = (int)((rows + p.block_rows - 1) / p.block_rows);
+        p.parts = (int)((a.group_rows - 1) / p.block_rows) + 2;
     };
     if (a.n <= kWarpRow) {
         p.form = WARP;
@@ -587,7 +616,7 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
         p.lay.rows = 32 / p.lanes;
         p.shared = p.lanes * per * p.chunks * 4 + kWarps * kStages * p.lay.bytes();
         if (p.shared <= 112 * 1024) {
-            p.parts = parts_for((long long)kWarps * p.lay.rows, 2);
+            stretches((long long)kWarps * p.lay.rows, 2);
             return p;
         }
         p.lay.rows = 1;
@@ -596,7 +625,7 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     p.shared = p.threads * kHeld * 4 + kStages * p.lay.bytes();
     if (p.threads <= 512 && p.shared <= 220 * 1024 && a.group_rows * groups >= 2 * sms) {
         p.form = BLOCK;
-        p.parts = parts_for(1, resident_blocks(128, p.threads, p.shared + 512));
+        stretches(1, resident_blocks(128, p.threads, p.shared + 512));
         return p;
     }
     p.form = CLUSTER;
@@ -618,45 +647,45 @@ cudaError_t allow_shared(K *kernel, int bytes)
     return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
 }
 template <typename T, int VEC, int LANES, int CH, bool GRAD>
-cudaError_t launch_warp(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
+cudaError_t launch_warp(const BalanceArgs &a, const Plan &p, cudaStream_t stream)
 {
     auto *kernel = balance_warp_kernel<T, VEC, LANES, CH, GRAD>;
     const cudaError_t e = allow_shared(kernel, p.shared);
     if (e != cudaSuccess) return e;
-    kernel<<<dim3(p.parts, groups), kWarps * 32, p.shared, stream>>>(a, p.lay);
+    kernel<<<p.blocks, kWarps * 32, p.shared, stream>>>(a, p.lay);
     return cudaGetLastError();
 }
 template <typename T, int VEC, int CH, bool GRAD>
-cudaError_t launch_lanes(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
+cudaError_t launch_lanes(const BalanceArgs &a, const Plan &p, cudaStream_t stream)
 {
     switch (p.lanes) {
-    case 4: return launch_warp<T, VEC, 4, CH, GRAD>(a, groups, p, stream);
-    case 8: return launch_warp<T, VEC, 8, CH, GRAD>(a, groups, p, stream);
-    case 16: return launch_warp<T, VEC, 16, CH, GRAD>(a, groups, p, stream);
-    default: return launch_warp<T, VEC, 32, CH, GRAD>(a, groups, p, stream);
+    case 4: return launch_warp<T, VEC, 4, CH, GRAD>(a, p, stream);
+    case 8: return launch_warp<T, VEC, 8, CH, GRAD>(a, p, stream);
+    case 16: return launch_warp<T, VEC, 16, CH, GRAD>(a, p, stream);
+    default: return launch_warp<T, VEC, 32, CH, GRAD>(a, p, stream);
     }
 }
 template <typename T, bool GRAD>
-cudaError_t launch_rows(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
+cudaError_t launch_rows(const BalanceArgs &a, const Plan &p, cudaStream_t stream)
 {
     constexpr int V = kPer16<T>;
     if (p.form == BLOCK) {
         auto *kernel = p.vec ? balance_staged_kernel<T, V, GRAD> : balance_staged_kernel<T, 1, GRAD>;
         const cudaError_t e = allow_shared(kernel, p.shared);
         if (e != cudaSuccess) return e;
-        kernel<<<dim3(p.parts, groups), p.threads, p.shared, stream>>>(a, p.lay);
+        kernel<<<p.blocks, p.threads, p.shared, stream>>>(a, p.lay);
         return cudaGetLastError();
     }
     if (p.vec) {
-        if (p.chunks == 1) return launch_lanes<T, V, 1, GRAD>(a, groups, p, stream);
-        if (p.chunks == 2) return launch_lanes<T, V, 2, GRAD>(a, groups, p, stream);
-        return launch_lanes<T, V, kHeld / V, GRAD>(a, groups, p, stream);
+        if (p.chunks == 1) return launch_lanes<T, V, 1, GRAD>(a, p, stream);
+        if (p.chunks == 2) return launch_lanes<T, V, 2, GRAD>(a, p, stream);
+        return launch_lanes<T, V, kHeld / V, GRAD>(a, p, stream);
     }
-    if (p.lanes == 8) return launch_warp<T, 1, 8, 4, GRAD>(a, groups, p, stream);
-    if (p.chunks == 2) return launch_warp<T, 1, 32, 2, GRAD>(a, groups, p, stream);
-    if (p.chunks == 8) return launch_warp<T, 1, 32, 8, GRAD>(a, groups, p, stream);
-    if (p.chunks == 16) return launch_warp<T, 1, 32, 16, GRAD>(a, groups, p, stream);
-    return launch_warp<T, 1, 32, 32, GRAD>(a, groups, p, stream);
+    if (p.lanes == 8) return launch_warp<T, 1, 8, 4, GRAD>(a, p, stream);
+    if (p.chunks == 2) return launch_warp<T, 1, 32, 2, GRAD>(a, p, stream);
+    if (p.chunks == 8) return launch_warp<T, 1, 32, 8, GRAD>(a, p, stream);
+    if (p.chunks == 16) return launch_warp<T, 1, 32, 16, GRAD>(a, p, stream);
+    return launch_warp<T, 1, 32, 32, GRAD>(a, p, stream);
 }
 
 template <typename T, int VEC, bool KEEP, bool GRAD, bool SAVED>
@@ -692,7 +721,7 @@ template <typename T>
 cudaError_t dispatch(const BalanceArgs &a, int groups, const Plan &p, cudaStream_t stream)
 {
     constexpr int V = kPer16<T>;
-    if (p.form != CLUSTER) return a.grad ? launch_rows<T, true>(a, groups, p, stream) : launch_rows<T, false>(a, groups, p, stream);
+    if (p.form != CLUSTER) return a.grad ? launch_rows<T, true>(a, p, stream) : launch_rows<T, false>(a, p, stream);
     if (a.stats_in) return p.vec ? launch_cluster<T, V, true, true>(a, groups, p, stream) : launch_cluster<T, 1, true, true>(a, groups, p, stream);
     if (a.grad) return p.vec ? launch_cluster<T, V, true, false>(a, groups, p, stream) : launch_cluster<T, 1, true, false>(a, groups, p, stream);
     return p.vec ? launch_cluster<T, V, false, false>(a, groups, p, stream) : launch_cluster<T, 1, false, false>(a, groups, p, stream);
@@ -733,7 +762,7 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
     const bool aligned = rows_aligned16(a.x, l->rows, a.stride, elem);
     a.wide = !a.grad || rows_aligned16(a.grad, l->rows, a.gstride, elem);
     const Plan p = make_plan(a, groups, (int)elem, aligned, sms);
-    a.parts = p.parts;
+    a.parts = p.parts, a.block_rows = p.block_rows, a.groups = groups;
 
     // workspace: totals and tickets (cleared), the counts if the caller takes none, the loss and column sums in parts
     auto round256 = [](size_t b) { return (b + 255) & ~(size_t)255; };
