@@ -481,24 +481,37 @@ def nbos_place_batch_sequential(snap: Snapshot, requests, out_hosts, out_found=N
 
 
 # ---- learned placement policies ------------------------------------------------------------
+# Small batches take a few microseconds on the device, so what is checked here is checked once and in few steps:
+# the usual tensors pass on one line, the others are looked at again to say what is wrong with them.
 _POLICY_DTYPES = {torch.float32: NBOS_F32, torch.bfloat16: NBOS_BF16, torch.float16: NBOS_F16}
+
+
+def _policy_stream(stream, device: torch.device) -> int:
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors live on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return _stream_ptr(stream)
 
 
 def _table(t: torch.Tensor, what: str):
     """(rows, row stride, columns) of a CUDA table [..., n] whose rows lie evenly apart."""
     if not isinstance(t, torch.Tensor) or t.dtype not in _POLICY_DTYPES:
         raise TypeError(f"{what} must be a float32, bfloat16 or float16 torch tensor")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{what} must live on cuda, not {t.device}")
-    if t.dim() < 2:
+    shape = t.shape
+    if len(shape) < 2:
         raise ValueError(f"{what} must have at least two dimensions, [..., n_hosts]")
-    n = t.shape[-1]
+    n = shape[-1]
+    if 0 in shape[:-1]:
+        return 0, n, n
+    if n and t.is_contiguous():
+        return t.numel() // n, n, n
     if n > 1 and t.stride(-1) != 1:
         raise ValueError(f"{what} must be contiguous along its hosts")
-    if 0 in t.shape[:-1]:
-        return 0, n, n
     rows, stride = 1, n
-    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for size, step in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
         if size == 1:
             continue
         if rows == 1:
@@ -511,52 +524,52 @@ def _table(t: torch.Tensor, what: str):
 
 def _logits(t: torch.Tensor, what: str = "logits") -> nbos_logits:
     rows, stride, n = _table(t, what)
-    return nbos_logits(_ptr(t), rows, stride, n, _POLICY_DTYPES[t.dtype])
+    return nbos_logits(t.data_ptr(), rows, stride, n, _POLICY_DTYPES[t.dtype])
 
 
-def _dense(t, what: str, dtype, numel: int, like: torch.Tensor):
-    """A contiguous tensor of `numel` values on the device of `like`, or None."""
+def _dense(t, what: str, dtype, numel: int, device: torch.device) -> int:
+    """Address of a contiguous tensor of `numel` values on `device`; 0 for None."""
     if t is None:
-        return None
+        return 0
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.numel() == numel and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or t.dtype != dtype:
         raise TypeError(f"{what} must be a {str(dtype)[6:]} torch tensor")
-    if t.device != like.device:
-        raise ValueError(f"{what} must live on {like.device}, not {t.device}")
+    if t.device != device:
+        raise ValueError(f"{what} must live on {device}, not {t.device}")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
-    if t.numel() != numel:
-        raise ValueError(f"{what} must hold {numel} values, not {t.numel()}")
-    return t
+    raise ValueError(f"{what} must hold {numel} values, not {t.numel()}")
 
 
 def _grad_like(grad, logits):
+    """(address, row stride) of a gradient like `logits`."""
     if grad is None:
-        return 0
-    if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device:
+        return 0, 0
+    if grad is not logits and (grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device):
         raise ValueError("out_grad must have the logits' shape, type and device")
-    rows, stride, n = _table(grad, "out_grad")
-    return stride
+    return grad.data_ptr(), _table(grad, "out_grad")[1]
 
 
 def _choices(hosts, logits, rows: int):
-    """hosts [..., k] int32 beside logits [..., n]; returns k."""
+    """(address, k) of hosts [..., k] int32 beside logits [..., n]."""
     if not isinstance(hosts, torch.Tensor) or hosts.dtype != torch.int32:
         raise TypeError("hosts must be an int32 torch tensor")
-    if hosts.shape[:-1] != logits.shape[:-1]:
+    shape = hosts.shape
+    if shape[:-1] != logits.shape[:-1]:
         raise ValueError("hosts [..., k] and logits [..., n_hosts] must agree on their rows")
-    _dense(hosts, "hosts", torch.int32, rows * hosts.shape[-1], logits)
-    return hosts.shape[-1]
+    return _dense(hosts, "hosts", torch.int32, rows * shape[-1], logits.device), shape[-1]
 
 
-def _teacher(teacher_logits, hosts, logits, rows: int, k: int):
-    """[..., k] like hosts, [k] for all rows alike, or None; returns the row stride."""
+def _teacher(teacher_logits, hosts, device, rows: int, k: int):
+    """(address, row stride) of teacher logits: [..., k] like hosts, [k] for all rows alike, or None."""
     if teacher_logits is None:
-        return 0
-    shared = teacher_logits.dim() == 1 and hosts.dim() > 1
-    _dense(teacher_logits, "teacher_logits", torch.float32, k if shared else rows * k, logits)
-    if not shared and teacher_logits.shape != hosts.shape:
+        return 0, 0
+    if teacher_logits.dim() == 1 and hosts.dim() > 1:
+        return _dense(teacher_logits, "teacher_logits", torch.float32, k, device), 0
+    if teacher_logits.shape != hosts.shape:
         raise ValueError("teacher_logits must have the shape of hosts, or [k]")
-    return 0 if shared else k
+    return _dense(teacher_logits, "teacher_logits", torch.float32, rows * k, device), k
 
 
 def nbos_policy_distill(logits, hosts, teacher_logits, out_loss, out_stats=None, grad_loss=None, grad_scale=1.0,
@@ -566,29 +579,27 @@ def nbos_policy_distill(logits, hosts, teacher_logits, out_loss, out_stats=None,
     out_loss [...] float32 or None, out_stats [..., 2] float32 or None, grad_loss [...] float32 or None; out_grad
     like logits (or the logits themselves) or None. Asynchronous on the stream."""
     desc = _logits(logits)
-    k = _choices(hosts, logits, desc.rows)
-    tstride = _teacher(teacher_logits, hosts, logits, desc.rows, k)
-    _dense(out_loss, "out_loss", torch.float32, desc.rows, logits)
-    _dense(out_stats, "out_stats", torch.float32, 2 * desc.rows, logits)
-    _dense(grad_loss, "grad_loss", torch.float32, desc.rows, logits)
-    gstride = _grad_like(out_grad, logits)
-    _check(load_library().nbos_policy_distill(ctypes.byref(desc), _ptr(hosts), _ptr(teacher_logits), tstride, k,
-                                              temperature, _ptr(grad_loss), grad_scale, _ptr(out_loss),
-                                              _ptr(out_stats), _ptr(out_grad), gstride, _stream_ptr(stream)))
+    rows, device, f32 = desc.rows, logits.device, torch.float32
+    ids, k = _choices(hosts, logits, rows)
+    teacher, tstride = _teacher(teacher_logits, hosts, device, rows, k)
+    grad, gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_distill(
+        ctypes.byref(desc), ids, teacher, tstride, k, temperature, _dense(grad_loss, "grad_loss", f32, rows, device),
+        grad_scale, _dense(out_loss, "out_loss", f32, rows, device), _dense(out_stats, "out_stats", f32, 2 * rows, device),
+        grad, gstride, _policy_stream(stream, device)))
 
 
 def nbos_policy_distill_backward(logits, hosts, teacher_logits, stats, out_grad, grad_loss=None, grad_scale=1.0,
                                  temperature=1.0, stream=None) -> None:
     """The gradient of nbos_policy_distill from the statistics it saved (out_stats)."""
     desc = _logits(logits)
-    k = _choices(hosts, logits, desc.rows)
-    tstride = _teacher(teacher_logits, hosts, logits, desc.rows, k)
-    _dense(stats, "stats", torch.float32, 2 * desc.rows, logits)
-    _dense(grad_loss, "grad_loss", torch.float32, desc.rows, logits)
-    gstride = _grad_like(out_grad, logits)
-    _check(load_library().nbos_policy_distill_backward(ctypes.byref(desc), _ptr(hosts), _ptr(teacher_logits), tstride,
-                                                       k, temperature, _ptr(stats), _ptr(grad_loss), grad_scale,
-                                                       _ptr(out_grad), gstride, _stream_ptr(stream)))
+    rows, device, f32 = desc.rows, logits.device, torch.float32
+    ids, k = _choices(hosts, logits, rows)
+    teacher, tstride = _teacher(teacher_logits, hosts, device, rows, k)
+    grad, gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_distill_backward(
+        ctypes.byref(desc), ids, teacher, tstride, k, temperature, _dense(stats, "stats", f32, 2 * rows, device),
+        _dense(grad_loss, "grad_loss", f32, rows, device), grad_scale, grad, gstride, _policy_stream(stream, device)))
 
 
 def _groups(logits) -> int:
@@ -602,30 +613,26 @@ def nbos_policy_balance(logits, hosts, out_loss, out_counts, out_shares=None, ou
     out_stats [N, B, 2] float32 or None, grad_loss [N] float32 or None; out_grad like logits (or the logits
     themselves) or None. Asynchronous on the stream."""
     desc = _logits(logits)
-    n = _groups(logits)
-    k = _choices(hosts, logits, desc.rows)
-    _dense(out_loss, "out_loss", torch.float32, n, logits)
-    _dense(out_counts, "out_counts", torch.int32, n * desc.n_hosts, logits)
-    _dense(out_shares, "out_shares", torch.float32, n * desc.n_hosts, logits)
-    _dense(out_stats, "out_stats", torch.float32, 2 * desc.rows, logits)
-    _dense(grad_loss, "grad_loss", torch.float32, n, logits)
-    gstride = _grad_like(out_grad, logits)
-    _check(load_library().nbos_policy_balance(ctypes.byref(desc), n, _ptr(hosts), k, _ptr(grad_loss), grad_scale,
-                                              _ptr(out_loss), _ptr(out_counts), _ptr(out_shares), _ptr(out_stats),
-                                              _ptr(out_grad), gstride, _stream_ptr(stream)))
+    n, rows, device, f32 = _groups(logits), desc.rows, logits.device, torch.float32
+    ids, k = _choices(hosts, logits, rows)
+    cells = n * desc.n_hosts
+    grad, gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_balance(
+        ctypes.byref(desc), n, ids, k, _dense(grad_loss, "grad_loss", f32, n, device), grad_scale,
+        _dense(out_loss, "out_loss", f32, n, device), _dense(out_counts, "out_counts", torch.int32, cells, device),
+        _dense(out_shares, "out_shares", f32, cells, device), _dense(out_stats, "out_stats", f32, 2 * rows, device),
+        grad, gstride, _policy_stream(stream, device)))
 
 
 def nbos_policy_balance_backward(logits, hosts, stats, out_grad, grad_loss=None, grad_scale=1.0, stream=None) -> None:
     """The gradient of nbos_policy_balance from the statistics it saved (out_stats)."""
     desc = _logits(logits)
-    n = _groups(logits)
-    k = _choices(hosts, logits, desc.rows)
-    _dense(stats, "stats", torch.float32, 2 * desc.rows, logits)
-    _dense(grad_loss, "grad_loss", torch.float32, n, logits)
-    gstride = _grad_like(out_grad, logits)
-    _check(load_library().nbos_policy_balance_backward(ctypes.byref(desc), n, _ptr(hosts), k, _ptr(stats),
-                                                       _ptr(grad_loss), grad_scale, _ptr(out_grad), gstride,
-                                                       _stream_ptr(stream)))
+    n, rows, device, f32 = _groups(logits), desc.rows, logits.device, torch.float32
+    ids, k = _choices(hosts, logits, rows)
+    grad, gstride = _grad_like(out_grad, logits)
+    _check(load_library().nbos_policy_balance_backward(
+        ctypes.byref(desc), n, ids, k, _dense(stats, "stats", f32, 2 * rows, device),
+        _dense(grad_loss, "grad_loss", f32, n, device), grad_scale, grad, gstride, _policy_stream(stream, device)))
 
 
 def nbos_policy_sample(logits, uniforms, out_hosts, out_found=None, temperature=None, top_k=None, top_p=None,
@@ -637,15 +644,13 @@ def nbos_policy_sample(logits, uniforms, out_hosts, out_found=None, temperature=
     if not isinstance(uniforms, torch.Tensor) or uniforms.shape[:-1] != logits.shape[:-1]:
         raise ValueError("uniforms [..., draws] and logits [..., n_hosts] must agree on their rows")
     draws = uniforms.shape[-1]
-    _dense(uniforms, "uniforms", torch.float32, desc.rows * draws, logits)
-    _dense(out_hosts, "out_hosts", torch.int32, desc.rows * draws, logits)
-    _dense(out_found, "out_found", torch.int32, desc.rows, logits)
-    for what, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-        _dense(t, what, dtype, desc.rows, logits)
-    _check(load_library().nbos_policy_sample(ctypes.byref(desc), _ptr(uniforms), _ptr(temperature), _ptr(top_k),
-                                             _ptr(top_p), _ptr(min_p), draws, _ptr(out_hosts), _ptr(out_found),
-                                             _stream_ptr(stream)))
+    rows, device, f32, i32 = desc.rows, logits.device, torch.float32, torch.int32
+    _check(load_library().nbos_policy_sample(
+        ctypes.byref(desc), _dense(uniforms, "uniforms", f32, rows * draws, device),
+        _dense(temperature, "temperature", f32, rows, device), _dense(top_k, "top_k", i32, rows, device),
+        _dense(top_p, "top_p", f32, rows, device), _dense(min_p, "min_p", f32, rows, device), draws,
+        _dense(out_hosts, "out_hosts", i32, rows * draws, device), _dense(out_found, "out_found", i32, rows, device),
+        _policy_stream(stream, device)))
 
 
 def nbos_probe_int32_issue(mix: int, iters: int, blocks: int, threads: int, stream=None):
