@@ -525,6 +525,113 @@ __global__ void __launch_bounds__(1024, 1) balance_block_kernel(BalanceArgs a, i
     cluster_sync(cs);   // no block leaves while another may still write to its shared memory
 }
 
+// ---- small groups: one block per group does everything, without a workspace --------------------------------
+constexpr int kSmallHosts = 512, kSmallWarps = 32;
+constexpr long long kSmallElements = 64 * 1024;   // rows of a group * hosts
+
+template <typename T, int LANES, int CH, bool GRAD>
+__global__ void __launch_bounds__(kSmallWarps * 32) balance_small_kernel(BalanceArgs a, int32_t *out_counts, float *shares, float *loss)
+{
+    extern __shared__ __align__(16) char s_mem[];
+    constexpr int at_once = 32 / LANES;
+    int *s_counts = reinterpret_cast<int *>(s_mem);
+    float *s_f = reinterpret_cast<float *>(s_mem) + a.n, *s_parts = s_f + a.n;   // [warps][n] column sums
+    __shared__ int s_tot[2];
+    __shared__ double s_loss[kSmallWarps];
+    const int lane = threadIdx.x & 31, sub = lane & (LANES - 1), slot = lane / LANES, warp = threadIdx.x >> 5;
+    const unsigned int lanes_of_row = LANES == 32 ? kFull : ((1u << (LANES & 31)) - 1) << (slot * LANES);
+    const int group = blockIdx.x, rows = (int)a.group_rows;
+    const long long row0 = (long long)group * rows;
+    const bool saved = a.stats_in != nullptr;
+    if (threadIdx.x < 2) s_tot[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < a.n; i += blockDim.x) s_counts[i] = 0;
+    __syncthreads();
+    int valid = 0, living = 0;
+    for (int r = threadIdx.x; r < rows; r += blockDim.x) {
+        int here = 0;
+        for (int j = 0; j < a.k; ++j) {
+            const int h = a.hosts[(row0 + r) * a.k + j];
+            if (h >= 0 && h < a.n) {
+                ++here;
+                atomicAdd(&s_counts[h], 1);
+            }
+        }
+        valid += here;
+        living += here > 0;
+    }
+    valid = __reduce_add_sync(kFull, valid);
+    living = __reduce_add_sync(kFull, living);
+    if (lane == 0 && living) {
+        atomicAdd(&s_tot[0], valid);
+        atomicAdd(&s_tot[1], living);
+    }
+    __syncthreads();
+    const float inv_total = s_tot[0] > 0 ? 1.0f / (float)s_tot[0] : 0.0f;
+    const float scale = s_tot[1] > 0 ? (float)a.n / (float)s_tot[1] * a.grad_scale * (a.grad_loss ? a.grad_loss[group] : 1.0f) : 0.0f;
+    for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+        s_f[i] = (float)s_counts[i] * inv_total;
+        if (out_counts) out_counts[(size_t)group * a.n + i] = s_counts[i];
+    }
+    __syncthreads();
+    float acc[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) acc[c] = 0.0f;
+    for (int base = warp * at_once; base < rows; base += kSmallWarps * at_once) {
+        const bool active = base + slot < rows;
+        const long long row = row0 + base + (active ? slot : 0);
+        const T *x = static_cast<const T *>(a.x) + row * a.stride;
+        const bool live = any_host(a.hosts + row * a.k, a.k, a.n, active, sub, LANES, lanes_of_row);
+        float v[CH][1];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c][0] = live && c * LANES + sub < a.n ? to_float(x[c * LANES + sub]) : neg_inf();
+        const float top = saved ? a.stats_in[2 * row] : lanes_max(max_all<1, CH>(v), LANES);
+        const float m = live ? top : neg_inf();
+        float s = exp_all<1, CH>(v, m == neg_inf() ? 0.0f : m, kLog2e), dot = 0.0f;
+        if (GRAD) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (c * LANES + sub < a.n) dot += v[c][0] * s_f[c * LANES + sub];
+            dot = lanes_sum(dot, LANES);
+        }
+        s = saved ? (live ? a.stats_in[2 * row + 1] : 0.0f) : lanes_sum(s, LANES);
+        const float inv = s != 0.0f ? reciprocal(s) : 0.0f;
+        if (!saved && live && a.stats && sub == 0) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+        const float fac = scale * inv, shift = -fac * (dot * inv);
+        T *grad = static_cast<T *>(a.grad) + row * a.gstride;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            acc[c] += v[c][0] * inv;
+            const int col = c * LANES + sub;
+            if (GRAD && active && col < a.n) grad[col] = from_float<T>(v[c][0] * (s_f[col] * fac + shift));
+        }
+    }
+    if (saved) return;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int off = 16; off >= LANES; off >>= 1) acc[c] += __shfl_xor_sync(kFull, acc[c], off);
+        if (lane < LANES && c * LANES + sub < a.n) s_parts[warp * a.n + c * LANES + sub] = acc[c];
+    }
+    __syncthreads();
+    double part = 0.0;
+    if (threadIdx.x < a.n) {
+        double sum = 0.0;
+        for (int w = 0; w < kSmallWarps; ++w) sum += (double)s_parts[w * a.n + threadIdx.x];
+        const double share = s_tot[1] > 0 ? sum / (double)s_tot[1] : 0.0;
+        if (shares) shares[(size_t)group * a.n + threadIdx.x] = (float)share;
+        if (s_tot[0] > 0) part = share * ((double)s_counts[threadIdx.x] / (double)s_tot[0]);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) part += __shfl_xor_sync(kFull, part, off);
+    if (lane == 0) s_loss[warp] = part;
+    __syncthreads();
+    if (warp != 0) return;
+    part = s_loss[lane];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) part += __shfl_xor_sync(kFull, part, off);
+    if (lane == 0) loss[group] = (float)(part * (double)a.n);
+}
+
 // shares = column sums over the parts / live; loss = n sum f share. blockDim (32 columns, L parts at a time);
 // grid (column blocks, groups). The group's last block adds the column blocks' shares of the loss, in order.
 __global__ void __launch_bounds__(1024) finish_kernel(BalanceArgs a, float *shares, float *loss, double *loss_parts,
@@ -727,6 +834,25 @@ cudaError_t dispatch(const BalanceArgs &a, int groups, const Plan &p, cudaStream
     return p.vec ? launch_cluster<T, V, false, false>(a, groups, p, stream) : launch_cluster<T, 1, false, false>(a, groups, p, stream);
 }
 
+template <typename T, int LANES, int CH>
+cudaError_t launch_small(const BalanceArgs &a, int groups, int32_t *counts, float *shares, float *loss, cudaStream_t stream)
+{
+    auto *kernel = a.grad ? balance_small_kernel<T, LANES, CH, true> : balance_small_kernel<T, LANES, CH, false>;
+    const int shared = (2 + kSmallWarps) * a.n * 4;
+    const cudaError_t e = allow_shared(kernel, shared);
+    if (e != cudaSuccess) return e;
+    kernel<<<groups, kSmallWarps * 32, shared, stream>>>(a, counts, shares, loss);
+    return cudaGetLastError();
+}
+template <typename T>
+cudaError_t small(const BalanceArgs &a, int groups, int32_t *counts, float *shares, float *loss, cudaStream_t stream)
+{
+    if (a.n <= 32) return launch_small<T, 8, 4>(a, groups, counts, shares, loss, stream);
+    if (a.n <= 64) return launch_small<T, 32, 2>(a, groups, counts, shares, loss, stream);
+    if (a.n <= 256) return launch_small<T, 32, 8>(a, groups, counts, shares, loss, stream);
+    return launch_small<T, 32, 16>(a, groups, counts, shares, loss, stream);
+}
+
 int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t k, const float *stats_in,
             const float *grad_loss, float grad_scale, float *out_loss, int32_t *out_counts, float *out_shares,
             float *out_stats, void *out_grad, int64_t gstride, cudaStream_t stream)
@@ -761,6 +887,15 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
     // the path, and with it every rounding, goes by the logits alone: the loss is the same with a gradient or without
     const bool aligned = rows_aligned16(a.x, l->rows, a.stride, elem);
     a.wide = !a.grad || rows_aligned16(a.grad, l->rows, a.gstride, elem);
+    // One launch instead of a workspace, two clears and three kernels: faster as long as one SM gets through a group in the
+    // time that those take to be queued.
+    if (l->n_hosts <= kSmallHosts && a.group_rows * l->n_hosts <= kSmallElements) {
+        const cudaError_t e = l->dtype == NBOS_F32    ? small<float>(a, groups, out_counts, out_shares, out_loss, stream)
+                              : l->dtype == NBOS_BF16 ? small<__nv_bfloat16>(a, groups, out_counts, out_shares, out_loss, stream)
+                                                      : small<__half>(a, groups, out_counts, out_shares, out_loss, stream);
+        if (e != cudaSuccess) return cuda_fail(e, "balance loss launch");
+        return NBOS_OK;
+    }
     const Plan p = make_plan(a, groups, (int)elem, aligned, sms);
     a.parts = p.parts, a.block_rows = p.block_rows, a.groups = groups;
 
