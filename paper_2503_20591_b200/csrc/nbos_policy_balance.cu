@@ -580,10 +580,12 @@ __global__ void __launch_bounds__(kSmallWarps * 32) balance_small_kernel(Balance
         const bool active = base + slot < rows;
         const long long row = row0 + base + (active ? slot : 0);
         const T *x = static_cast<const T *>(a.x) + row * a.stride;
-        const bool live = any_host(a.hosts + row * a.k, a.k, a.n, active, sub, LANES, lanes_of_row);
         float v[CH][1];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c][0] = live && c * LANES + sub < a.n ? to_float(x[c * LANES + sub]) : neg_inf();
+        for (int c = 0; c < CH; ++c) v[c][0] = c * LANES + sub < a.n ? to_float(x[c * LANES + sub]) : neg_inf();
+        const bool live = any_host(a.hosts + row * a.k, a.k, a.n, active, sub, LANES, lanes_of_row);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c][0] = live ? v[c][0] : neg_inf();
         const float top = saved ? a.stats_in[2 * row] : lanes_max(max_all<1, CH>(v), LANES);
         const float m = live ? top : neg_inf();
         float s = exp_all<1, CH>(v, m == neg_inf() ? 0.0f : m, kLog2e), dot = 0.0f;
