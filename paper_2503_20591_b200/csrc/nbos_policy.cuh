@@ -205,16 +205,21 @@ __device__ __forceinline__ void fma2(float &d0, float &d1, float a0, float a1, f
         : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
-// v = 2^((v - m0) c) over a lane's elements; returns their sum
+// v = 2^((v - m0) c) over a lane's elements; returns their sum (single elements: an even number of chunks, or one)
 template <int VEC, int CH>
 __device__ __forceinline__ float exp_all(float (&v)[CH][VEC], float m0, float c)
 {
     float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-        if constexpr (VEC == 1) {
-            v[k][0] = exp2_fast((v[k][0] - m0) * c);
-            (k % 2 ? s1 : s0) += v[k][0];
+        if constexpr (VEC == 1 && CH == 1) {
+            s0 = v[0][0] = exp2_fast((v[0][0] - m0) * c);
+        } else if constexpr (VEC == 1) {
+            if (k % 2) continue;
+            add2(v[k][0], v[k + 1][0], -m0, -m0);
+            mul2(v[k][0], v[k + 1][0], c, c);
+            v[k][0] = exp2_fast(v[k][0]), v[k + 1][0] = exp2_fast(v[k + 1][0]);
+            add2(s0, s1, v[k][0], v[k + 1][0]);
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; i += 2) {
@@ -268,7 +273,11 @@ __device__ __forceinline__ void copy_async4(uint32_t dst, const void *src)
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copies_drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
+template <int PENDING = kStages - 1>
+__device__ __forceinline__ void copies_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+}
 
 // Bytes between the 16-byte boundary before a row and the row itself; they are staged along.
 template <typename T>

@@ -47,11 +47,10 @@ struct BalanceArgs {
 
 // counts[g][h] += ..., totals[g] += (valid ids, rows that have one); grid (blocks, groups)
 __global__ void __launch_bounds__(256) count_kernel(const int32_t *hosts, long long group_rows, int k, int n,
-                                                    int32_t *counts, int2 *totals)
+                                                    bool in_shared, int32_t *counts, int2 *totals)
 {
     extern __shared__ int s_hist[];
     __shared__ int s_tot[2];
-    const bool in_shared = n <= kHistHosts;
     if (threadIdx.x < 2) s_tot[threadIdx.x] = 0;
     for (int i = threadIdx.x; in_shared && i < n; i += blockDim.x) s_hist[i] = 0;
     __syncthreads();
@@ -155,7 +154,7 @@ __device__ __forceinline__ float dot_all(const float (&v)[CH][VEC], const float 
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         if constexpr (VEC == 1) {
-            (c % 2 ? d1 : d0) += v[c][0] * f[first + c * width];
+            if (c % 2 == 0) fma2(d0, d1, v[c][0], v[c + 1][0], f[first + c * width], f[first + (c + 1) * width]);
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; i += 4) {
@@ -177,8 +176,15 @@ __device__ __forceinline__ void finish_row(float (&v)[CH][VEC], float (&acc)[CH]
     for (int c = 0; c < CH; ++c) {
         const int col = first + c * width;
         if constexpr (VEC == 1) {
-            acc[c][0] += v[c][0] * inv;
-            if (GRAD && col < n) __stcs(grad + col, from_float<T>(v[c][0] * (f[col] * fac + shift)));
+            if (c % 2) continue;
+            fma2(acc[c][0], acc[c + 1][0], v[c][0], v[c + 1][0], inv, inv);
+            if (GRAD) {
+                float g[2] = {shift, shift};
+                fma2(g[0], g[1], f[col], f[col + width], fac, fac);
+                mul2(v[c][0], v[c + 1][0], g[0], g[1]);
+                if (col < n) __stcs(grad + col, from_float<T>(v[c][0]));
+                if (col + width < n) __stcs(grad + col + width, from_float<T>(v[c + 1][0]));
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; i += 2) fma2(acc[c][i], acc[c][i + 1], v[c][i], v[c][i + 1], inv, inv);
@@ -634,45 +640,61 @@ __global__ void __launch_bounds__(kSmallWarps * 32) balance_small_kernel(Balance
     if (lane == 0) loss[group] = (float)(part * (double)a.n);
 }
 
-// shares = column sums over the parts / live; loss = n sum f share. blockDim (32 columns, L parts at a time);
-// grid (column blocks, groups). The group's last block adds the column blocks' shares of the loss, in order.
-__global__ void __launch_bounds__(1024) finish_kernel(BalanceArgs a, float *shares, float *loss, double *loss_parts,
-                                                      unsigned int *tickets)
+// shares = column sums over the parts / live; loss = n sum f share. A block of kFinishThreads takes blockDim.x columns, blockDim.y
+// parts at a time (both powers of two; many parts: few columns); grid (column blocks, groups). The group's last block
+// adds the column blocks' shares of the loss. Every sum is taken in the same order each time.
+constexpr int kFinishThreads = 512;
+
+__global__ void __launch_bounds__(kFinishThreads) finish_kernel(BalanceArgs a, float *shares, float *loss, double *loss_parts,
+                                                                unsigned int *tickets)
 {
-    __shared__ double s_sum[32][33];
-    __shared__ unsigned int s_last;
-    const int group = blockIdx.y, col = blockIdx.x * 32 + threadIdx.x;
-    double sum = 0.0;
+    __shared__ double s_sum[kFinishThreads];
+    __shared__ bool s_last;
+    const int cols = blockDim.x, group = blockIdx.y, tid = threadIdx.y * cols + threadIdx.x, col = blockIdx.x * cols + threadIdx.x;
     const int parts = a.block_rows ? (int)((((long long)group + 1) * a.group_rows - 1) / a.block_rows - first_block(a, group)) + 1 : a.parts;
-    if (col < a.n)
-        for (int p = threadIdx.y; p < parts; p += blockDim.y) sum += (double)a.partial[((size_t)group * a.parts + p) * a.n + col];
-    s_sum[threadIdx.y][threadIdx.x] = sum;
-    __syncthreads();
-    if (threadIdx.y != 0) return;
-    for (int y = 1; y < blockDim.y; ++y) sum += s_sum[y][threadIdx.x];
-    const int2 t = a.totals[group];
-    const double share = t.y > 0 ? sum / (double)t.y : 0.0;
-    double part = 0.0;
+    const float *from = a.partial + (size_t)group * a.parts * a.n + col;
+    double sum = 0.0;
     if (col < a.n) {
+#pragma unroll 8
+        for (int p = threadIdx.y; p < parts; p += blockDim.y) sum += (double)from[(size_t)p * a.n];
+    }
+    // adds up s_sum[0 .. 2 half)
+    auto fold = [&](int half) {
+        for (; half > 0; half >>= 1) {
+            __syncthreads();
+            if (tid < half) s_sum[tid] += s_sum[tid + half];
+        }
+        __syncthreads();
+    };
+    s_sum[tid] = sum;
+    for (int half = kFinishThreads / 2; half >= cols; half >>= 1) {   // over the parts
+        __syncthreads();
+        if (tid < half) s_sum[tid] += s_sum[tid + half];
+    }
+    double part = 0.0;
+    if (threadIdx.y == 0 && col < a.n) {
+        const int2 t = a.totals[group];
+        const double share = t.y > 0 ? s_sum[tid] / (double)t.y : 0.0;
         if (shares) shares[(size_t)group * a.n + col] = (float)share;
         if (t.x > 0) part = share * ((double)a.counts[(size_t)group * a.n + col] / (double)t.x);
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) part += __shfl_xor_sync(kFull, part, off);
+    __syncthreads();
+    if (threadIdx.y == 0) s_sum[tid] = part;
+    fold(cols / 2);
     double *mine = loss_parts + (size_t)group * gridDim.x;
-    if (threadIdx.x == 0) {
-        mine[blockIdx.x] = part;
+    if (tid == 0) {
+        mine[blockIdx.x] = s_sum[0];
         __threadfence();
         s_last = atomicAdd(&tickets[group], 1u) == gridDim.x - 1;
         __threadfence();
     }
-    __syncwarp();
+    __syncthreads();
     if (!s_last) return;
     double total = 0.0;
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += 32) total += __ldcg(&mine[i]);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(kFull, total, off);
-    if (threadIdx.x == 0) loss[group] = (float)(total * (double)a.n);
+    for (int i = tid; i < (int)gridDim.x; i += kFinishThreads) total += __ldcg(&mine[i]);
+    s_sum[tid] = total;
+    fold(kFinishThreads / 2);
+    if (tid == 0) loss[group] = (float)(s_sum[0] * (double)a.n);
 }
 
 enum Form { WARP, BLOCK, CLUSTER };
@@ -694,7 +716,7 @@ void warp_shape(int n, int vec, int &lanes, int &chunks)
     const int most = kHeld / vec;
     if (vec == 1) {
         lanes = n <= 32 ? 8 : 32;
-        chunks = n <= 32 ? 4 : n <= 64 ? 2 : n <= 256 ? 8 : n <= 512 ? 16 : 32;
+        chunks = n <= 32 ? 4 : n <= 64 ? 2 : n <= 128 ? 4 : n <= 256 ? 8 : n <= 320 ? 10 : n <= 384 ? 12 : n <= 512 ? 16 : n <= 768 ? 24 : 32;
         return;
     }
     for (chunks = most; ; chunks = chunks > 2 ? 2 : 1) {
@@ -791,10 +813,16 @@ cudaError_t launch_rows(const BalanceArgs &a, const Plan &p, cudaStream_t stream
         return launch_lanes<T, V, kHeld / V, GRAD>(a, p, stream);
     }
     if (p.lanes == 8) return launch_warp<T, 1, 8, 4, GRAD>(a, p, stream);
-    if (p.chunks == 2) return launch_warp<T, 1, 32, 2, GRAD>(a, p, stream);
-    if (p.chunks == 8) return launch_warp<T, 1, 32, 8, GRAD>(a, p, stream);
-    if (p.chunks == 16) return launch_warp<T, 1, 32, 16, GRAD>(a, p, stream);
-    return launch_warp<T, 1, 32, 32, GRAD>(a, p, stream);
+    switch (p.chunks) {
+    case 2: return launch_warp<T, 1, 32, 2, GRAD>(a, p, stream);
+    case 4: return launch_warp<T, 1, 32, 4, GRAD>(a, p, stream);
+    case 8: return launch_warp<T, 1, 32, 8, GRAD>(a, p, stream);
+    case 10: return launch_warp<T, 1, 32, 10, GRAD>(a, p, stream);
+    case 12: return launch_warp<T, 1, 32, 12, GRAD>(a, p, stream);
+    case 16: return launch_warp<T, 1, 32, 16, GRAD>(a, p, stream);
+    case 24: return launch_warp<T, 1, 32, 24, GRAD>(a, p, stream);
+    default: return launch_warp<T, 1, 32, 32, GRAD>(a, p, stream);
+    }
 }
 
 template <typename T, int VEC, bool KEEP, bool GRAD, bool SAVED>
@@ -903,7 +931,9 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
 
     // workspace: totals and tickets (cleared), the counts if the caller takes none, the loss and column sums in parts
     auto round256 = [](size_t b) { return (b + 255) & ~(size_t)255; };
-    const int col_blocks = (int)((n + 31) / 32);
+    int finish_rows = 1;
+    while (finish_rows < 64 && finish_rows < p.parts) finish_rows *= 2;
+    const int finish_cols = kFinishThreads / finish_rows, col_blocks = (int)((n + finish_cols - 1) / finish_cols);
     const bool forward = stats_in == nullptr;
     const size_t b_clear = round256((size_t)groups * (sizeof(int2) + sizeof(unsigned int)));
     const size_t b_counts = out_counts ? 0 : round256(cells * sizeof(int32_t));
@@ -927,11 +957,16 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
     e = cudaMemsetAsync(ws, 0, b_clear + b_counts, stream);
     if (e == cudaSuccess && out_counts) e = cudaMemsetAsync(out_counts, 0, cells * sizeof(int32_t), stream);
     if (e == cudaSuccess) {
-        long long bx = (a.group_rows + 1023) / 1024;
-        const long long cap = (4ll * sms + groups - 1) / groups;
+        // counters of a block's own keep the hot hosts' additions apart; they pay where a block counts more than it has to clear
+        // and hand on, so large groups get no more blocks than that allows beyond one an SM
+        long long bx = (a.group_rows + 255) / 256;
+        const long long cap = (8ll * sms + groups - 1) / groups, one = (sms + groups - 1) / groups;
+        const long long worth = a.group_rows * k / (4ll * (long long)n) > one ? a.group_rows * k / (4ll * (long long)n) : one;
         if (bx > cap) bx = cap;
-        const size_t hist = n <= kHistHosts ? n * sizeof(int) : 0;
-        count_kernel<<<dim3((unsigned int)bx, groups), 256, hist, stream>>>(hosts, a.group_rows, k, a.n, counts, totals);
+        if (bx > worth) bx = worth;
+        const bool in_shared = n <= kHistHosts && a.group_rows * k / bx >= (long long)n / 4;
+        count_kernel<<<dim3((unsigned int)bx, groups), 256, in_shared ? n * sizeof(int) : 0, stream>>>(hosts, a.group_rows, k, a.n, in_shared,
+                                                                                                       counts, totals);
         e = cudaGetLastError();
     }
     if (e == cudaSuccess)
@@ -939,9 +974,7 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
             : l->dtype == NBOS_BF16 ? dispatch<__nv_bfloat16>(a, groups, p, stream)
                                     : dispatch<__half>(a, groups, p, stream);
     if (e == cudaSuccess && forward) {
-        int at_once = 1;
-        while (at_once < 32 && at_once < p.parts) at_once *= 2;
-        finish_kernel<<<dim3(col_blocks, groups), dim3(32, at_once), 0, stream>>>(a, out_shares, out_loss, loss_parts, tickets);
+        finish_kernel<<<dim3(col_blocks, groups), dim3(finish_cols, finish_rows), 0, stream>>>(a, out_shares, out_loss, loss_parts, tickets);
         e = cudaGetLastError();
     }
     cudaFreeAsync(ws, stream);

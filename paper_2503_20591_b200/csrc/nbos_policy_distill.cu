@@ -19,6 +19,7 @@ namespace {
 using namespace policy;
 
 constexpr int kElems = 32;             // row elements a thread holds in the block form
+constexpr int kBlockStages = 3;        // rows of the block form on their way or in use
 constexpr int kMaxCluster = 8;
 constexpr int kWarpRow = 32 * kElems;  // longest row of the warp form
 
@@ -355,15 +356,30 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
         if (row < a.rows) stage<T, GRAD, SAVED>(a, lay, s_mem + st * stage_bytes, 0, row, threadIdx.x, blockDim.x);
         copies_commit();
     };
+    // The listed hosts' gradients go over what their columns' threads wrote; the first warp writes them once all threads
+    // have come to the next row's barrier. That barrier also frees the stage of the row before: three stages.
+    T *fix_grad = nullptr;
+    auto fix = [&]() {
+        if (GRAD && warp == 0 && fix_grad) {
+            for (int i = lane; i < a.k; i += 32)
+                if (s_fix_host[i] >= 0) fix_grad[s_fix_host[i]] = from_float<T>(s_fix[i]);
+            fix_grad = nullptr;
+        }
+    };
 #pragma unroll
-    for (int st = 0; st < kStages - 1; ++st) queue(blockIdx.x + (long long)st * gridDim.x, st);
+    for (int st = 0; st < kBlockStages - 1; ++st) queue(blockIdx.x + (long long)st * gridDim.x, st);
     int st = 0, turn = 0;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        queue(row + (kStages - 1) * (long long)gridDim.x, st == 0 ? kStages - 1 : st - 1);
-        copies_wait();
+        const long long ahead = row + (kBlockStages - 1) * (long long)gridDim.x;
+        const int ahead_st = st == 0 ? kBlockStages - 1 : st - 1;
+        copies_wait<kBlockStages - 2>();
         const Staged<T> r = staged_row<T>(a, lay, s_mem + st * stage_bytes, 0, row);
         // its 16 bytes a thread has copied itself; the first elements of an unaligned table came through other threads
         if (!lay.aligned || SAVED) __syncthreads();
+        if (SAVED) {
+            fix();
+            queue(ahead, ahead_st);
+        }
         const int first = threadIdx.x * VEC - row_shift(r.x) / (int)sizeof(T);
         float v[CH][VEC];
 #pragma unroll
@@ -382,6 +398,8 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
             s = lanes_sum(s, 32);
             if (lane == 0) s_stats[turn][warp] = make_float2(m, s);
             __syncthreads();
+            fix();
+            queue(ahead, ahead_st);
             const float2 w = lane < warps ? s_stats[turn][lane] : make_float2(neg_inf(), 0.0f);
             m = lanes_max(w.x, 16);
             m = __shfl_sync(kFull, m, 0);
@@ -433,14 +451,12 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
                 else
                     store_cols<T, VEC>(grad, first + c * chunk, a.n, v[c], a.wide);
             }
-            __syncthreads();   // the listed hosts' gradients go over what others wrote; the stage may be filled again
-            for (int i = lane; warp == 0 && any && i < a.k; i += 32)
-                if (s_fix_host[i] >= 0) grad[s_fix_host[i]] = from_float<T>(s_fix[i]);
-        } else {
-            __syncthreads();   // the stage may be filled again
+            if (any) fix_grad = grad;
         }
-        st = st == kStages - 1 ? 0 : st + 1;
+        st = st == kBlockStages - 1 ? 0 : st + 1;
     }
+    __syncthreads();
+    fix();
 }
 
 // (m, s) with s relative to m, merged with (m2, s2)
@@ -633,11 +649,11 @@ bool launch_staged(const DistillArgs &a, int sms, cudaStream_t stream, cudaError
         return true;
     }
     const int threads = ((columns + kElems - 1) / kElems + 31) / 32 * 32;
-    if (threads > 512 || a.rows < 2 * sms) return false;
     auto *kernel = distill_staged_kernel<T, GRAD, SAVED>;
     static const int regs = kernel_registers(kernel);
     const Layout lay{staged_row_bytes(a.n, sizeof(T), aligned), 1, a.k, aligned, aligned && a.wide ? a.n : 0};
-    const int shared = kStages * lay.bytes();
+    const int shared = kBlockStages * lay.bytes();
+    if (threads > 512 || shared > 220 * 1024 || a.rows < 2 * sms) return false;
     e = allow_shared(kernel, shared);
     if (e != cudaSuccess) return true;
     const long long fit = (long long)sms * resident_blocks(regs, threads, shared + 2560);
