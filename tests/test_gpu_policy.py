@@ -603,3 +603,13 @@ def test_offsets_beyond_31_bits(nb):
     even, counts = torch.empty(1, device="cuda"), torch.empty((1, n), dtype=torch.int32, device="cuda")
     nb.nbos_policy_balance(x, hosts, even, counts, out_grad=grad)
     assert int(counts.sum()) == 3 * rows and abs(float(even) - 1.0) < 0.05 and bool(torch.isfinite(grad[-1]).all())
+
+
+def test_a_policy_learns_the_rule(nb):
+    """The operators together: a small policy trained on the exact rule's hosts comes to choose them, and what it samples is
+    feasible and distinct."""
+    from paper_2503_20591_b200 import train_policy
+    result = train_policy.train(hosts=64, snapshots=8, batch=256, steps=120, report=lambda text: None)
+    first, last = result["history"][0], result["history"][-1]
+    assert last[0] < 0.6 * first[0] and last[2] > first[2]
+    assert result["feasible"] and result["distinct"] and 0 < result["found"] <= 3
