@@ -25,6 +25,7 @@ using namespace policy;
 constexpr int kChunk = 128;            // columns a warp takes at once, four a lane
 constexpr int kWarpChunks = 8;         // chunks of a warp, except of rows in the workspace
 constexpr int kWarpRow = kChunk * kWarpChunks;
+constexpr int kLoneRow = 4096;
 constexpr int kMaxCluster = 8;
 constexpr int kBlockRow = 32 * kWarpRow;
 constexpr int kSort = 64;              // weights that one warp sorts, two a lane
@@ -886,7 +887,7 @@ __global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a, int chun
 {
     extern __shared__ __align__(16) char s_mem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 4 + warp;
+    const long long row = (long long)blockIdx.x * (blockDim.x >> 5) + warp;
     if (row >= a.rows) return;
     Lists *lists = reinterpret_cast<Lists *>(s_mem + warp * warp_bytes);
     unsigned int *store = reinterpret_cast<unsigned int *>(s_mem + (warp + 1) * warp_bytes) - chunks * kChunk;
@@ -921,10 +922,12 @@ cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
         sample_short_kernel<T><<<(unsigned int)((a.rows + 3) / 4), 128, 0, stream>>>(a);
         return cudaGetLastError();
     }
-    if (a.n <= kWarpRow) {
-        const int chunks = (a.n + kChunk - 1) / kChunk;
+    // One warp alone exchanges nothing and waits for nobody: it takes rows of up to kLoneRow hosts as long as there are
+    // enough of them to fill the SMs that way.
+    if (a.n <= kWarpRow || (a.n <= kLoneRow && a.rows >= 8 * sms)) {
+        const int chunks = (a.n + kChunk - 1) / kChunk, warps = chunks <= kWarpChunks ? 4 : 2;
         const int warp_bytes = (int)sizeof(Lists) + chunks * kChunk * 4;
-        sample_warp_kernel<T><<<(unsigned int)((a.rows + 3) / 4), 128, 4 * warp_bytes, stream>>>(a, chunks, warp_bytes);
+        sample_warp_kernel<T><<<(unsigned int)((a.rows + warps - 1) / warps), warps * 32, warps * warp_bytes, stream>>>(a, chunks, warp_bytes);
         return cudaGetLastError();
     }
     const bool shared = a.n <= kMaxCluster * kBlockRow;
