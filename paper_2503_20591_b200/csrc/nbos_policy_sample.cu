@@ -197,6 +197,8 @@ struct Team {
 
 // A warp's elements, chunk after chunk: the lane's four of chunk c are at store[c * 128 + lane * 4] and belong to the
 // columns first + c * 128 + lane * 4 ... Beyond the row they are logits of -inf, later weights of 0.
+// U: chunks that a pass has under way at once, many where few warps share an SM.
+template <int U>
 struct Elems {
     unsigned int *store;
     int chunks;
@@ -209,7 +211,7 @@ struct Elems {
     template <typename F>
     __device__ __forceinline__ void each(int lane, F f) const   // f(value, column)
     {
-#pragma unroll 2
+#pragma unroll U
         for (int c = 0; c < chunks; ++c) {
             const uint4 v = at(c, lane);
             const int col = first + c * kChunk + lane * 4;
@@ -219,6 +221,7 @@ struct Elems {
     template <typename F>
     __device__ __forceinline__ void change(int lane, F f) const   // value = f(value, column)
     {
+#pragma unroll(U / 2)
         for (int c = 0; c < chunks; ++c) {
             uint4 v = at(c, lane);
             const int col = first + c * kChunk + lane * 4;
@@ -259,8 +262,8 @@ struct Elems {
 };
 
 // The column of the m-th (from 0) element, in index order over the row, that `pick` accepts.
-template <typename F>
-__device__ __forceinline__ int nth_column(Team &team, const Elems &e, u64 m, F pick)
+template <int U, typename F>
+__device__ __forceinline__ int nth_column(Team &team, const Elems<U> &e, u64 m, F pick)
 {
     auto one = [&](unsigned int v, int col) -> unsigned int { return pick(v, col) ? 1u : 0u; };
     unsigned int here = 0;
@@ -328,8 +331,8 @@ union Lists {        // a row makes one or the other
 // are left in the row: the others have been taken out). Bisection (on the logarithm at first, with the bounds moved onto weights that
 // occur every few steps) until at most 64 weights are left between the bounds, which one warp then sorts.
 // key_at(column): the order of the logit there.
-template <typename K>
-__device__ __forceinline__ unsigned int nucleus(Team &team, const Elems &e, u64 limit, u64 total, unsigned int count,
+template <int U, typename K>
+__device__ __forceinline__ unsigned int nucleus(Team &team, const Elems<U> &e, u64 limit, u64 total, unsigned int count,
                                                 SortList *list, u64 &keep, u64 &ties, K key_at)
 {
     const int lane = team.lane;
@@ -356,7 +359,7 @@ __device__ __forceinline__ unsigned int nucleus(Team &team, const Elems &e, u64 
         unsigned int c = 0;
         for (int at = 0; at < e.chunks; at += kWarpChunks) {   // 2^44 above 32 weights: a warp's usual chunks
             unsigned int sum_lo = 0, sum_hi = 0;
-            const Elems part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0, nullptr, 0};
+            const Elems<U> part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0, nullptr, 0};
             part.each(lane, [&](unsigned int v, int) { add_above(sum_lo, sum_hi, v, mid); });
             mass += ((u64)(sum_hi & 0xFFFu) << 32) | sum_lo, c += sum_hi >> 12;
         }
@@ -429,9 +432,9 @@ __device__ __forceinline__ unsigned int nucleus(Team &team, const Elems &e, u64 
 }
 
 // Filters and draws of a row whose logits (as bits) e holds.
-template <typename T>
+template <typename T, int U>
 __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const T *x, const Row &p, Team &team,
-                                       const Elems &e, SortList *sort_list)
+                                       const Elems<U> &e, SortList *sort_list)
 {
     const int lane = team.lane;
     // top-k: cut_x = the k-th largest logit; of its ties the first in index order stay. If at most k logits have a
@@ -487,7 +490,7 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
     unsigned int count = 0;
     for (int at = 0; at < e.chunks; at += kWarpChunks) {
         unsigned int sum_lo = 0, sum_hi = 0;
-        const Elems part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0, nullptr, 0};
+        const Elems<U> part{e.store + at * kChunk, min(kWarpChunks, e.chunks - at), 0, 0, nullptr, 0};
         part.change(lane, [&](unsigned int v, int) {
             const float f = __uint_as_float(v);
             const unsigned int w = f >= cut_x ? weight_of(f, p.m, p.scale) : 0u;
@@ -720,7 +723,8 @@ __device__ __forceinline__ void finish(const SampleArgs &a, long long row, const
 // top-k of a long row leaves few hosts: those above a threshold that at least k and at most 128 logits exceed go, in
 // index order, to a list that one warp finishes alone. Returns the list's length, or -1 if no threshold was found
 // (many equal logits).
-__device__ __forceinline__ int short_list(const Row &p, Team &team, const Elems &e, ShortList *list)
+template <int U>
+__device__ __forceinline__ int short_list(const Row &p, Team &team, const Elems<U> &e, ShortList *list)
 {
     const int lane = team.lane;
     const unsigned int k = (unsigned int)p.k;
@@ -783,8 +787,8 @@ __device__ __forceinline__ void write_one(const SampleArgs &a, long long row, in
     if (a.found) a.found[row] = host >= 0;
 }
 
-template <typename T>
-__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team team, const Elems &e, Lists *lists)
+template <typename T, int U>
+__device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, Team team, const Elems<U> &e, Lists *lists)
 {
     const T *x = static_cast<const T *>(a.x) + row * a.stride;
     const int lane = team.lane;
@@ -792,10 +796,11 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
 
     // all of a warp's loads in flight at once; a NaN is never the larger, nor above any bound, and has weight 0
     float m = neg_inf();
-    for (int c0 = 0; c0 < e.chunks; c0 += kWarpChunks) {
-        Raw4<T> raw[kWarpChunks];
+    constexpr int kLoads = U > 2 ? 2 * kWarpChunks : kWarpChunks;
+    for (int c0 = 0; c0 < e.chunks; c0 += kLoads) {
+        Raw4<T> raw[kLoads];
 #pragma unroll
-        for (int c = 0; c < kWarpChunks; ++c) {
+        for (int c = 0; c < kLoads; ++c) {
             const int col = e.first + (c0 + c) * kChunk + lane * 4;
             if (c0 + c >= e.chunks) break;
             if (a.aligned && col + 4 <= a.n) {
@@ -806,7 +811,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
             }
         }
 #pragma unroll
-        for (int c = 0; c < kWarpChunks; ++c) {
+        for (int c = 0; c < kLoads; ++c) {
             if (c0 + c >= e.chunks) break;
             float v[4];
             raw[c].get(v);
@@ -882,7 +887,7 @@ __global__ void __launch_bounds__(128) sample_short_kernel(SampleArgs a)
 }
 
 // one warp per row; shared memory per warp: the row, the lists
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a, int chunks, int warp_bytes)
 {
     extern __shared__ __align__(16) char s_mem[];
@@ -891,7 +896,7 @@ __global__ void __launch_bounds__(128) sample_warp_kernel(SampleArgs a, int chun
     if (row >= a.rows) return;
     Lists *lists = reinterpret_cast<Lists *>(s_mem + warp * warp_bytes);
     unsigned int *store = reinterpret_cast<unsigned int *>(s_mem + (warp + 1) * warp_bytes) - chunks * kChunk;
-    sample_row<T>(a, row, Team{nullptr, 1, 1, 0, lane, 0}, Elems{store, chunks, 0, a.n, store, 0}, lists);
+    sample_row<T, U>(a, row, Team{nullptr, 1, 1, 0, lane, 0}, Elems<U>{store, chunks, 0, a.n, store, 0}, lists);
 }
 
 // grid: SHARED one block / cluster per row; else as many as the workspace has rows take them in turn
@@ -910,7 +915,7 @@ __global__ void __launch_bounds__(1024, 1) sample_block_kernel(SampleArgs a, int
     unsigned int *store = block_store + warp * span;
     cluster_sync(cs);   // all blocks of the cluster run
     for (long long row = first; row < a.rows; row += step) {
-        sample_row<T>(a, row, team, Elems{store, chunks, team.me * span, a.n, SHARED ? block_store : block_store - (size_t)rank * span * warps, SHARED ? span * warps : 1 << 30}, &s_lists);
+        sample_row<T, 2>(a, row, team, Elems<2>{store, chunks, team.me * span, a.n, SHARED ? block_store : block_store - (size_t)rank * span * warps, SHARED ? span * warps : 1 << 30}, &s_lists);
         cluster_sync(cs);   // slots and lists are free again
     }
 }
@@ -927,7 +932,8 @@ cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
     if (a.n <= kWarpRow || (a.n <= kLoneRow && a.rows >= 8 * sms)) {
         const int chunks = (a.n + kChunk - 1) / kChunk, warps = chunks <= kWarpChunks ? 4 : 2;
         const int warp_bytes = (int)sizeof(Lists) + chunks * kChunk * 4;
-        sample_warp_kernel<T><<<(unsigned int)((a.rows + warps - 1) / warps), warps * 32, warps * warp_bytes, stream>>>(a, chunks, warp_bytes);
+        auto *kernel = chunks <= 2 * kWarpChunks ? sample_warp_kernel<T, 2> : sample_warp_kernel<T, 8>;
+        kernel<<<(unsigned int)((a.rows + warps - 1) / warps), warps * 32, warps * warp_bytes, stream>>>(a, chunks, warp_bytes);
         return cudaGetLastError();
     }
     const bool shared = a.n <= kMaxCluster * kBlockRow;
