@@ -715,8 +715,9 @@ void warp_shape(int n, int vec, int &lanes, int &chunks)
 {
     const int most = kHeld / vec;
     if (vec == 1) {
-        lanes = n <= 32 ? 8 : 32;
-        chunks = n <= 32 ? 4 : n <= 64 ? 2 : n <= 128 ? 4 : n <= 256 ? 8 : n <= 320 ? 10 : n <= 384 ? 12 : n <= 512 ? 16 : n <= 768 ? 24 : 32;
+        // neighbouring lanes write neighbouring elements: at least 16 of them, a sector's worth, but for the shortest rows
+        lanes = n <= 64 ? 8 : n <= 512 ? 16 : 32;
+        chunks = n <= 32 ? 4 : n <= 128 ? 8 : n <= 256 ? 16 : n <= 320 ? 20 : n <= 384 ? 24 : n <= 512 ? 32 : n <= 768 ? 24 : 32;
         return;
     }
     for (chunks = most; ; chunks = chunks > 2 ? 2 : 1) {
@@ -812,16 +813,14 @@ cudaError_t launch_rows(const BalanceArgs &a, const Plan &p, cudaStream_t stream
         if (p.chunks == 2) return launch_lanes<T, V, 2, GRAD>(a, p, stream);
         return launch_lanes<T, V, kHeld / V, GRAD>(a, p, stream);
     }
-    if (p.lanes == 8) return launch_warp<T, 1, 8, 4, GRAD>(a, p, stream);
+    if (p.lanes == 8) return p.chunks == 4 ? launch_warp<T, 1, 8, 4, GRAD>(a, p, stream) : launch_warp<T, 1, 8, 8, GRAD>(a, p, stream);
+    if (p.lanes == 32) return p.chunks == 24 ? launch_warp<T, 1, 32, 24, GRAD>(a, p, stream) : launch_warp<T, 1, 32, 32, GRAD>(a, p, stream);
     switch (p.chunks) {
-    case 2: return launch_warp<T, 1, 32, 2, GRAD>(a, p, stream);
-    case 4: return launch_warp<T, 1, 32, 4, GRAD>(a, p, stream);
-    case 8: return launch_warp<T, 1, 32, 8, GRAD>(a, p, stream);
-    case 10: return launch_warp<T, 1, 32, 10, GRAD>(a, p, stream);
-    case 12: return launch_warp<T, 1, 32, 12, GRAD>(a, p, stream);
-    case 16: return launch_warp<T, 1, 32, 16, GRAD>(a, p, stream);
-    case 24: return launch_warp<T, 1, 32, 24, GRAD>(a, p, stream);
-    default: return launch_warp<T, 1, 32, 32, GRAD>(a, p, stream);
+    case 8: return launch_warp<T, 1, 16, 8, GRAD>(a, p, stream);
+    case 16: return launch_warp<T, 1, 16, 16, GRAD>(a, p, stream);
+    case 20: return launch_warp<T, 1, 16, 20, GRAD>(a, p, stream);
+    case 24: return launch_warp<T, 1, 16, 24, GRAD>(a, p, stream);
+    default: return launch_warp<T, 1, 16, 32, GRAD>(a, p, stream);
     }
 }
 
@@ -933,6 +932,7 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
     auto round256 = [](size_t b) { return (b + 255) & ~(size_t)255; };
     int finish_rows = 1;
     while (finish_rows < 64 && finish_rows < p.parts) finish_rows *= 2;
+    while (finish_rows > 1 && (long long)n * finish_rows / kFinishThreads > 8ll * sms) finish_rows /= 2;   // no more blocks than that
     const int finish_cols = kFinishThreads / finish_rows, col_blocks = (int)((n + finish_cols - 1) / finish_cols);
     const bool forward = stats_in == nullptr;
     const size_t b_clear = round256((size_t)groups * (sizeof(int2) + sizeof(unsigned int)));

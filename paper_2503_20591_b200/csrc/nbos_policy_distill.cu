@@ -247,9 +247,12 @@ __device__ __forceinline__ void entry_math(const DistillArgs &a, const Entry &e,
 
 // ---- warp form: LANES lanes per row, CH * VEC elements each; the grid stays and walks over the rows -------
 constexpr int kWarps = 8;
+// Elements a lane holds at most. 64 (at two thirds of the warps an SM) is worth it where instructions bound: 262,144 x 1,024 bf16
+// 202 us against 218; not for 32-bit logits, bound by their bytes: 441 us against 380.
+template <typename T> constexpr int kMostElems = sizeof(T) == 2 ? 64 : 40;
 
 template <typename T, int LANES, int CH, bool GRAD, bool SAVED>
-__global__ void __launch_bounds__(kWarps * 32, 3) distill_warp_kernel(DistillArgs a, int entry_lanes, Layout lay)
+__global__ void __launch_bounds__(kWarps * 32, CH * kPer16<T> > 32 ? 2 : 3) distill_warp_kernel(DistillArgs a, int entry_lanes, Layout lay)
 {
     constexpr int VEC = kPer16<T>;
     extern __shared__ __align__(16) char s_mem[];
@@ -622,29 +625,45 @@ cudaError_t launch_warp(const DistillArgs &a, const Layout &lay, int sms, cudaSt
     return cudaGetLastError();
 }
 
+template <typename T, int LANES, bool GRAD, bool SAVED>
+cudaError_t launch_chunks(const DistillArgs &a, int chunks, const Layout &lay, int sms, cudaStream_t stream)
+{
+    constexpr int VEC = kPer16<T>;
+    if (chunks == 1) return launch_warp<T, LANES, 1, GRAD, SAVED>(a, lay, sms, stream);
+    if (chunks == 2) return launch_warp<T, LANES, 2, GRAD, SAVED>(a, lay, sms, stream);
+    if (chunks == 32 / VEC) return launch_warp<T, LANES, 32 / VEC, GRAD, SAVED>(a, lay, sms, stream);
+    if (chunks == 40 / VEC) return launch_warp<T, LANES, 40 / VEC, GRAD, SAVED>(a, lay, sms, stream);
+    return launch_warp<T, LANES, kMostElems<T> / VEC, GRAD, SAVED>(a, lay, sms, stream);
+}
+
 // The staged forms; false: not for these sizes.
 template <typename T, bool GRAD, bool SAVED>
 bool launch_staged(const DistillArgs &a, int sms, cudaStream_t stream, cudaError_t &e)
 {
-    constexpr int VEC = kPer16<T>, MOST = kElems / VEC;
+    constexpr int VEC = kPer16<T>;
     const bool aligned = rows_aligned16(a.x, a.rows, a.stride, sizeof(T));
     const int columns = a.n + (aligned ? 0 : VEC - 1);   // with those before an unaligned row
-    // Lanes per row: 32 elements a lane, so that what a row costs besides its elements is shared by the warp's rows, and
-    // no fewer than entries; 16 bytes a lane where that is all there is, or while there are too few rows to give every
-    // SM eight warps.
-    int lanes = power_of_two((columns + kElems - 1) / kElems, 32);
-    while (lanes < 4 || (lanes < 32 && lanes < a.k)) lanes *= 2;
-    const int spread = power_of_two((columns + VEC - 1) / VEC, 64);
-    const bool one = spread <= 32 && (spread <= lanes || a.rows * lanes < 32ll * 8 * sms);
-    if (one && lanes < spread) lanes = spread;
+    // Lanes per row and 16-byte chunks per lane. What a row costs besides its elements, about as much as 36 elements a lane,
+    // is shared by the warp's rows: as few lanes as that makes cheapest, no fewer than entries; but enough to give every SM
+    // eight warps.
+    constexpr int kChunks[] = {1, 2, 32 / VEC, 40 / VEC, 64 / VEC};
+    int lanes = 32, chunks = kChunks[2];
+    long long best = 1ll << 40;
+    for (int l = 4; l <= 32; l *= 2)
+        for (int c : kChunks) {
+            if (l * c * VEC < columns || (l < 32 && l < a.k) || c * VEC > kMostElems<T>) continue;
+            long long cost = (long long)l * (36 + c * VEC);
+            if (l < 32 && a.rows * l < 32ll * 8 * sms) cost += (1ll << 30) / l;
+            if (cost < best) best = cost, lanes = l, chunks = c;
+        }
     const Layout warp_lay{staged_row_bytes(a.n, sizeof(T), aligned), 32 / lanes, a.k, aligned, aligned && a.wide ? a.n : 0};
     // (long lists of entries would leave room for one block only)
     if (columns <= kWarpRow && kWarps * kStages * warp_lay.bytes() <= 112 * 1024) {
         switch (lanes) {
-        case 4: e = one ? launch_warp<T, 4, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 4, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
-        case 8: e = one ? launch_warp<T, 8, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 8, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
-        case 16: e = one ? launch_warp<T, 16, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 16, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
-        default: e = one ? launch_warp<T, 32, 1, GRAD, SAVED>(a, warp_lay, sms, stream) : launch_warp<T, 32, MOST, GRAD, SAVED>(a, warp_lay, sms, stream); break;
+        case 4: e = launch_chunks<T, 4, GRAD, SAVED>(a, chunks, warp_lay, sms, stream); break;
+        case 8: e = launch_chunks<T, 8, GRAD, SAVED>(a, chunks, warp_lay, sms, stream); break;
+        case 16: e = launch_chunks<T, 16, GRAD, SAVED>(a, chunks, warp_lay, sms, stream); break;
+        default: e = launch_chunks<T, 32, GRAD, SAVED>(a, chunks, warp_lay, sms, stream); break;
         }
         return true;
     }
