@@ -289,21 +289,22 @@ __device__ __forceinline__ int row_shift(const T *row)
 // thread `sub` of `team`. The bytes before an unaligned row belong to the rows before it (or the gaps between them);
 // where the table does not have that many (`offset`: the row's, in bytes), the first, partial 16 bytes go element by
 // element.
+// Only the 16-byte pieces from, ..., until - 1.
 template <typename T>
-__device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long long offset, int sub, int team)
+__device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long long offset, int sub, int team, int from = 0, int until = 1 << 30)
 {
     const int shift = row_shift(row), total = shift + n * (int)sizeof(T);
     const char *src = reinterpret_cast<const char *>(row) - shift;
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
-    int g = sub;
-    if (offset < shift) {
+    int g = from + sub;
+    if (offset < shift && from == 0) {
         for (int i = sub; i < n && shift + (i + 1) * (int)sizeof(T) <= 16; i += team) reinterpret_cast<T *>(dst + shift)[i] = row[i];
         if (sub == 0) g = team;   // the pieces of 16 bytes after it
     }
-    const int whole = total >> 4;
+    const int whole = min(total >> 4, until);
 #pragma unroll 4
     for (; g < whole; g += team) copy_async16(to + g * 16, src + g * 16);
-    if (g == whole && (total & 15)) copy_async16(to + g * 16, src + g * 16, total & 15);
+    if (g == total >> 4 && g < until && (total & 15)) copy_async16(to + g * 16, src + g * 16, total & 15);
 }
 // Bytes of a staged row, with what precedes an unaligned one.
 inline int staged_row_bytes(int n, int elem, bool aligned) { return (n * elem + (aligned ? 0 : 15) + 15) & ~15; }
@@ -406,7 +407,8 @@ inline int check_sm100(int *sms, int *device)
 // Blocks of a kernel that an SM holds at once: what a persistent grid is sized by. regs: the kernel's registers.
 inline int resident_blocks(int regs, int threads, size_t shared)
 {
-    const int by_regs = 65536 / (((regs + 7) & ~7) * threads);
+    // a quarter of the SM has 16,384 registers for whole warps
+    const int by_regs = 4 * (512 / ((regs + 7) & ~7)) / ((threads + 31) / 32);
     const int by_shared = (int)((228 * 1024) / (shared + 1024));
     const int by_threads = 2048 / threads;
     int n = by_regs < by_shared ? by_regs : by_shared;

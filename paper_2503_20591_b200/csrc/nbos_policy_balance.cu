@@ -311,14 +311,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArg
 template <typename T, int VEC, bool GRAD>
 __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, Layout lay)
 {
-    constexpr int CH = kHeld / VEC;
+    constexpr int CH = kHeld / VEC, width = 32 * VEC;   // a warp has one stretch of columns: offsets are known when compiled
     extern __shared__ __align__(16) char s_mem[];
     __shared__ float4 s_stats[2][16];
     float *s_f = reinterpret_cast<float *>(s_mem);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int stage_bytes = lay.bytes(), width = blockDim.x * VEC, first = threadIdx.x * VEC;
+    const int stage_bytes = lay.bytes(), base = warp * 32 * kHeld, first = base + lane * VEC;
     const bool saved = a.stats_in != nullptr;
-    char *stages = s_mem + width * CH * 4;
+    char *stages = s_mem + blockDim.x * kHeld * 4;
     const long long begin = blockIdx.x * a.block_rows, all_rows = a.group_rows * a.groups;
     const long long end = begin + a.block_rows < all_rows ? begin + a.block_rows : all_rows;
     int turn = 0;
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
 #pragma unroll
     for (int st = 0; st < kStages; ++st) queue(st, st);
     const GroupScale gs = group_scale(a, group);
-    for (int i = threadIdx.x; i < width * CH; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
+    for (int i = threadIdx.x; i < (int)blockDim.x * kHeld; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
     float acc[CH][VEC];
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
         const T *staged = reinterpret_cast<const T *>(at + (VEC == 1 ? row_shift(x) : 0));
         const float2 given = saved ? staged_pair(at + lay.stats_at()) : make_float2(0.0f, 0.0f);
         float v[CH][VEC];
-        load_staged<T, VEC, CH>(staged, first, width, a.n, lay.whole, v);
+        load_staged<T, VEC, CH>(staged, first, width, a.n, lay.whole - base, v);
         const bool live = any_host(reinterpret_cast<const int *>(at + lay.hosts_at()), a.k, a.n, true, lane, 32, kFull);
         if (!live) {
 #pragma unroll
@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
         if (!saved && live && a.stats && threadIdx.x == 0) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
         const float own = inv * (saved ? 1.0f : exp_from(m_warp, m, kLog2e));
         finish_row<T, VEC, CH, GRAD>(v, acc, own, gs.grad * own, dot * inv, s_f, static_cast<T *>(a.grad) + row * a.gstride, first, width, a.n,
-                                     lay.whole, a.wide);
+                                     lay.whole - base, a.wide);
         st = st == kStages - 1 ? 0 : st + 1;
     }
     copies_drain();

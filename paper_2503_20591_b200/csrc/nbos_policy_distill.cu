@@ -147,10 +147,8 @@ struct Layout {   // bytes of a stage: rows, then entries, then what is given pe
 };
 
 template <typename T, bool GRAD, bool SAVED>
-__device__ __forceinline__ void stage(const DistillArgs &a, const Layout &lay, char *at, int slot, long long row, int sub, int team)
+__device__ __forceinline__ void stage_rest(const DistillArgs &a, const Layout &lay, char *at, int slot, long long row, int sub, int team)
 {
-    const T *x = static_cast<const T *>(a.x) + row * a.stride;
-    stage_row(at + slot * lay.row_bytes, x, a.n, row * a.stride * (long long)sizeof(T), sub, team);
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at));
     for (int i = sub; i < a.k; i += team) {
         copy_async4(to + lay.hosts_at() + (slot * a.k + i) * 4, a.hosts + row * a.k + i);
@@ -263,7 +261,11 @@ __global__ void __launch_bounds__(kWarps * 32, CH * kPer16<T> > 32 ? 2 : 3) dist
     const long long step = (long long)gridDim.x * kWarps * at_once;
     const long long row0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * at_once;
     auto queue = [&](long long base, int st) {
-        if (base + slot < a.rows) stage<T, GRAD, SAVED>(a, lay, mine + st * stage_bytes, slot, base + slot, sub, lanes);
+        if (base + slot < a.rows) {
+            stage_row(mine + st * stage_bytes + slot * lay.row_bytes, static_cast<const T *>(a.x) + (base + slot) * a.stride, a.n,
+                      (base + slot) * a.stride * (long long)sizeof(T), sub, lanes);
+            stage_rest<T, GRAD, SAVED>(a, lay, mine + st * stage_bytes, slot, base + slot, sub, lanes);
+        }
         copies_commit();
     };
 #pragma unroll
@@ -354,9 +356,15 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
     __shared__ float s_fix[NBOS_POLICY_MAX_K];
     __shared__ int s_fix_host[NBOS_POLICY_MAX_K];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int chunk = blockDim.x * VEC, stage_bytes = lay.bytes();
+    // a warp has one stretch of columns: offsets are known when compiled
+    constexpr int chunk = 32 * VEC;
+    const int pieces = warp * 32 * CH, base = pieces * VEC, stage_bytes = lay.bytes();
     auto queue = [&](long long row, int st) {
-        if (row < a.rows) stage<T, GRAD, SAVED>(a, lay, s_mem + st * stage_bytes, 0, row, threadIdx.x, blockDim.x);
+        if (row < a.rows) {
+            stage_row(s_mem + st * stage_bytes, static_cast<const T *>(a.x) + row * a.stride, a.n, row * a.stride * (long long)sizeof(T), lane, 32,
+                      pieces, pieces + 32 * CH);
+            stage_rest<T, GRAD, SAVED>(a, lay, s_mem + st * stage_bytes, 0, row, threadIdx.x, blockDim.x);
+        }
         copies_commit();
     };
     // The listed hosts' gradients go over what their columns' threads wrote; the first warp writes them once all threads
@@ -383,11 +391,11 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
             fix();
             queue(ahead, ahead_st);
         }
-        const int first = threadIdx.x * VEC - row_shift(r.x) / (int)sizeof(T);
+        const int first = base + lane * VEC - row_shift(r.x) / (int)sizeof(T);
         float v[CH][VEC];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            if ((c + 1) * chunk <= lay.whole)
+            if ((c + 1) * chunk <= lay.whole - base)
                 unpack16(*reinterpret_cast<const uint4 *>(r.x + first + c * chunk), v[c], T());
             else
                 staged_cols<T, VEC>(r.x, first + c * chunk, a.n, v[c]);
@@ -449,7 +457,7 @@ __global__ void __maxnreg__(80) distill_staged_kernel(DistillArgs a, int entry_l
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) v[c][i] = 0.0f;
                 }
-                if ((c + 1) * chunk <= lay.whole)
+                if ((c + 1) * chunk <= lay.whole - base)
                     __stcs(reinterpret_cast<uint4 *>(grad + first + c * chunk), pack16(v[c], T()));
                 else
                     store_cols<T, VEC>(grad, first + c * chunk, a.n, v[c], a.wide);
