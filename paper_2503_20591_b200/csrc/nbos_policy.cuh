@@ -205,32 +205,33 @@ __device__ __forceinline__ void fma2(float &d0, float &d1, float a0, float a1, f
         : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
 }
 
-// v = 2^((v - m0) c) over a lane's elements; returns their sum (single elements: an even number of chunks, or one)
+// v = 2^((v - m0) c) over a lane's elements; returns their sum (single elements: an even number of chunks, or one). Two sums
+// in turn: one would have every addition wait for the one before.
 template <int VEC, int CH>
 __device__ __forceinline__ float exp_all(float (&v)[CH][VEC], float m0, float c)
 {
-    float s0 = 0.0f, s1 = 0.0f;
+    float s[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         if constexpr (VEC == 1 && CH == 1) {
-            s0 = v[0][0] = exp2_fast((v[0][0] - m0) * c);
+            s[0][0] = v[0][0] = exp2_fast((v[0][0] - m0) * c);
         } else if constexpr (VEC == 1) {
             if (k % 2) continue;
             add2(v[k][0], v[k + 1][0], -m0, -m0);
             mul2(v[k][0], v[k + 1][0], c, c);
             v[k][0] = exp2_fast(v[k][0]), v[k + 1][0] = exp2_fast(v[k + 1][0]);
-            add2(s0, s1, v[k][0], v[k + 1][0]);
+            add2(s[k / 2 % 2][0], s[k / 2 % 2][1], v[k][0], v[k + 1][0]);
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; i += 2) {
                 add2(v[k][i], v[k][i + 1], -m0, -m0);
                 mul2(v[k][i], v[k][i + 1], c, c);
                 v[k][i] = exp2_fast(v[k][i]), v[k][i + 1] = exp2_fast(v[k][i + 1]);
-                add2(s0, s1, v[k][i], v[k][i + 1]);
+                add2(s[i / 2 % 2][0], s[i / 2 % 2][1], v[k][i], v[k][i + 1]);
             }
         }
     }
-    return s0 + s1;
+    return (s[0][0] + s[0][1]) + (s[1][0] + s[1][1]);
 }
 // v *= f
 template <int VEC>
@@ -246,12 +247,12 @@ __device__ __forceinline__ void scale_all(float (&v)[VEC], float f)
 template <int VEC, int CH>
 __device__ __forceinline__ float max_all(const float (&v)[CH][VEC])
 {
-    float m = v[0][0];
+    float m[4] = {neg_inf(), neg_inf(), neg_inf(), neg_inf()};
 #pragma unroll
     for (int k = 0; k < CH; ++k)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) m = fmaxf(m, v[k][i]);
-    return m;
+        for (int i = 0; i < VEC; ++i) m[(k * VEC + i) % 4] = fmaxf(m[(k * VEC + i) % 4], v[k][i]);
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
 __device__ __forceinline__ float reciprocal(float x) { return __fdividef(1.0f, x); }   // 2 ulp

@@ -150,21 +150,21 @@ __device__ __forceinline__ void load_staged(const T *row, int first, int width, 
 template <int VEC, int CH>
 __device__ __forceinline__ float dot_all(const float (&v)[CH][VEC], const float *f, int first, int width)
 {
-    float d0 = 0.0f, d1 = 0.0f;
+    float d[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         if constexpr (VEC == 1) {
-            if (c % 2 == 0) fma2(d0, d1, v[c][0], v[c + 1][0], f[first + c * width], f[first + (c + 1) * width]);
+            if (c % 2 == 0) fma2(d[c / 2 % 2][0], d[c / 2 % 2][1], v[c][0], v[c + 1][0], f[first + c * width], f[first + (c + 1) * width]);
         } else {
 #pragma unroll
             for (int i = 0; i < VEC; i += 4) {
                 const float4 w = *reinterpret_cast<const float4 *>(f + first + c * width + i);
-                fma2(d0, d1, v[c][i], v[c][i + 1], w.x, w.y);
-                fma2(d0, d1, v[c][i + 2], v[c][i + 3], w.z, w.w);
+                fma2(d[0][0], d[0][1], v[c][i], v[c][i + 1], w.x, w.y);
+                fma2(d[1][0], d[1][1], v[c][i + 2], v[c][i + 3], w.z, w.w);
             }
         }
     }
-    return d0 + d1;
+    return (d[0][0] + d[0][1]) + (d[1][0] + d[1][1]);
 }
 // acc += v inv, then v := v (f - dot) fac, which is written to the row's gradient if GRAD
 template <typename T, int VEC, int CH, bool GRAD>
