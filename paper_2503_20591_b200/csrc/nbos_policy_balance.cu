@@ -23,6 +23,9 @@ constexpr int kMaxCluster = 8;
 constexpr int kWarps = 8;           // of a block of the warp form
 constexpr int kHeld = 32;           // row elements a thread holds in the staged forms
 constexpr int kHistHosts = 8192;    // counters kept in shared memory while counting
+// Chosen ids of a group that one cluster counts: 8,000 rows of 3 in 257 hosts 25 us a call against 27, 2,000 in 2,048 32 against
+// 36; 16,385 rows 31.0 against 31.4, 30,000 in 128 hosts 30 against 28.
+constexpr long long kClusterIds = 48 * 1024;
 
 struct BalanceArgs {
     const void *x;
@@ -79,6 +82,52 @@ __global__ void __launch_bounds__(256) count_kernel(const int32_t *hosts, long l
     if (threadIdx.x < 2 && s_tot[threadIdx.x]) atomicAdd(&reinterpret_cast<int *>(totals + blockIdx.y)[threadIdx.x], s_tot[threadIdx.x]);
     for (int i = threadIdx.x; in_shared && i < n; i += blockDim.x)
         if (s_hist[i]) atomicAdd(&out[i], s_hist[i]);
+}
+
+// The same for a group with few ids, by one cluster: every block counts its part of the rows, then adds up its part of the hosts
+// over the blocks. It writes every counter, so that nothing has to be cleared before; grid (cluster, groups).
+__global__ void __launch_bounds__(512) count_cluster_kernel(const int32_t *hosts, int rows, int k, int n, int cs, int32_t *counts, int2 *totals,
+                                                            unsigned int *tickets)
+{
+    extern __shared__ int s_hist[];
+    __shared__ int s_tot[2];
+    const int rank = cluster_rank(cs), group = blockIdx.y, threads = blockDim.x * cs;
+    if (threadIdx.x < 2) s_tot[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) s_hist[i] = 0;
+    __syncthreads();
+    int valid = 0, live = 0;
+    for (int r = rank * blockDim.x + threadIdx.x; r < rows; r += threads) {
+        const int32_t *ids = hosts + ((long long)group * rows + r) * k;
+        int here = 0;
+        for (int j = 0; j < k; ++j) {
+            const int h = ids[j];
+            if (h >= 0 && h < n) {
+                ++here;
+                atomicAdd(&s_hist[h], 1);
+            }
+        }
+        valid += here;
+        live += here > 0;
+    }
+    valid = __reduce_add_sync(kFull, valid);
+    live = __reduce_add_sync(kFull, live);
+    if ((threadIdx.x & 31) == 0 && live) {
+        atomicAdd(&s_tot[0], valid);
+        atomicAdd(&s_tot[1], live);
+    }
+    cluster_sync(cs);
+    for (int i = rank * blockDim.x + threadIdx.x; i < n; i += threads) {
+        int sum = 0;
+        for (int p = 0; p < cs; ++p) sum += cluster_peer(s_hist, p, cs)[i];
+        counts[(size_t)group * n + i] = sum;
+    }
+    if (rank == 0 && threadIdx.x < 2) {
+        int sum = 0;
+        for (int p = 0; p < cs; ++p) sum += cluster_peer(s_tot, p, cs)[threadIdx.x];
+        reinterpret_cast<int *>(totals + group)[threadIdx.x] = sum;
+    }
+    if (rank == 0 && threadIdx.x == 2) tickets[group] = 0;
+    cluster_sync(cs);   // no block leaves while another may still read its counters
 }
 
 // The blocks that take rows of a group are first_block, first_block + 1, ...: its parts, in this order.
@@ -735,9 +784,10 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     const int per = aligned ? 16 / elem : 1;
     p.lay = Layout{staged_row_bytes(a.n, elem, aligned), 1, a.k, aligned && a.wide ? a.n : 0};
     // the rows of all groups in even stretches, as many as there are blocks at once
-    auto stretches = [&](long long at_once, int resident) {
+    auto stretches = [&](long long at_once, int resident, long long least) {
         const long long rows = a.group_rows * groups, most = (long long)sms * resident;
-        const long long rounds = (rows + most * at_once - 1) / (most * at_once);
+        long long rounds = (rows + most * at_once - 1) / (most * at_once);
+        if (rounds < least) rounds = least;
         p.block_rows = rounds * at_once;
         p.blocks = (int)((rows + p.block_rows - 1) / p.block_rows);
         p.parts = (int)((a.group_rows - 1) / p.block_rows) + 2;
@@ -748,7 +798,7 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
         p.lay.rows = 32 / p.lanes;
         p.shared = p.lanes * per * p.chunks * 4 + kWarps * kStages * p.lay.bytes();
         if (p.shared <= 112 * 1024) {
-            stretches((long long)kWarps * p.lay.rows, 2);
+            stretches((long long)kWarps * p.lay.rows, 2, 1);
             return p;
         }
         p.lay.rows = 1;
@@ -757,7 +807,8 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     p.shared = p.threads * kHeld * 4 + kStages * p.lay.bytes();
     if (p.threads <= 512 && p.shared <= 220 * 1024 && a.group_rows * groups >= 2 * sms) {
         p.form = BLOCK;
-        stretches(1, resident_blocks(128, p.threads, p.shared + 512));
+        // a block's column sums are written and read once more: that should be little beside its rows
+        stretches(1, resident_blocks(128, p.threads, p.shared + 512), 6);
         return p;
     }
     p.form = CLUSTER;
@@ -954,20 +1005,37 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
     a.partial = reinterpret_cast<float *>(ws + b_clear + b_counts + b_loss);
     a.counts = counts, a.totals = totals;
 
-    e = cudaMemsetAsync(ws, 0, b_clear + b_counts, stream);
-    if (e == cudaSuccess && out_counts) e = cudaMemsetAsync(out_counts, 0, cells * sizeof(int32_t), stream);
-    if (e == cudaSuccess) {
-        // counters of a block's own keep the hot hosts' additions apart; they pay where a block counts more than it has to clear
-        // and hand on, so large groups get no more blocks than that allows beyond one an SM
-        long long bx = (a.group_rows + 255) / 256;
-        const long long cap = (8ll * sms + groups - 1) / groups, one = (sms + groups - 1) / groups;
-        const long long worth = a.group_rows * k / (4ll * (long long)n) > one ? a.group_rows * k / (4ll * (long long)n) : one;
-        if (bx > cap) bx = cap;
-        if (bx > worth) bx = worth;
-        const bool in_shared = n <= kHistHosts && a.group_rows * k / bx >= (long long)n / 4;
-        count_kernel<<<dim3((unsigned int)bx, groups), 256, in_shared ? n * sizeof(int) : 0, stream>>>(hosts, a.group_rows, k, a.n, in_shared,
-                                                                                                       counts, totals);
-        e = cudaGetLastError();
+    if (n <= kHistHosts && a.group_rows * k <= kClusterIds) {
+        int cs = 1;
+        while (cs < kMaxCluster && a.group_rows > 512ll * cs) cs *= 2;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(cs, groups);
+        cfg.blockDim = dim3(512);
+        cfg.dynamicSmemBytes = n * sizeof(int);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = cs;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, count_cluster_kernel, hosts, (int)a.group_rows, (int)k, a.n, cs, counts, totals, tickets);
+    } else {
+        e = cudaMemsetAsync(ws, 0, b_clear + b_counts, stream);
+        if (e == cudaSuccess && out_counts) e = cudaMemsetAsync(out_counts, 0, cells * sizeof(int32_t), stream);
+        if (e == cudaSuccess) {
+            // counters of a block's own keep the hot hosts' additions apart; they pay where a block counts more than it has to clear
+            // and hand on, so large groups get no more blocks than that allows beyond one an SM
+            long long bx = (a.group_rows + 255) / 256;
+            const long long cap = (8ll * sms + groups - 1) / groups, one = (sms + groups - 1) / groups;
+            const long long worth = a.group_rows * k / (4ll * (long long)n) > one ? a.group_rows * k / (4ll * (long long)n) : one;
+            if (bx > cap) bx = cap;
+            if (bx > worth) bx = worth;
+            const bool in_shared = n <= kHistHosts && a.group_rows * k / bx >= (long long)n / 4;
+            count_kernel<<<dim3((unsigned int)bx, groups), 256, in_shared ? n * sizeof(int) : 0, stream>>>(hosts, a.group_rows, k, a.n, in_shared,
+                                                                                                           counts, totals);
+            e = cudaGetLastError();
+        }
     }
     if (e == cudaSuccess)
         e = l->dtype == NBOS_F32    ? dispatch<float>(a, groups, p, stream)
