@@ -290,13 +290,14 @@ __device__ __forceinline__ int row_shift(const T *row)
 // thread `sub` of `team`. The bytes before an unaligned row belong to the rows before it (or the gaps between them);
 // where the table does not have that many (`offset`: the row's, in bytes), the first, partial 16 bytes go element by
 // element.
-// Only the 16-byte pieces from, ..., until - 1.
+// Only the 16-byte pieces from, ..., until - 1; piece `origin` lands at `dst`.
 template <typename T>
-__device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long long offset, int sub, int team, int from = 0, int until = 1 << 30)
+__device__ __forceinline__ void stage_row(char *dst, const T *row, int n, long long offset, int sub, int team, int from = 0, int until = 1 << 30,
+                                          int origin = 0)
 {
     const int shift = row_shift(row), total = shift + n * (int)sizeof(T);
     const char *src = reinterpret_cast<const char *>(row) - shift;
-    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(dst)) - origin * 16;
     int g = from + sub;
     if (offset < shift && from == 0) {
         for (int i = sub; i < n && shift + (i + 1) * (int)sizeof(T) <= 16; i += team) reinterpret_cast<T *>(dst + shift)[i] = row[i];

@@ -20,6 +20,7 @@ using namespace policy;
 constexpr int kWarpRow = 1024;      // longest row of the warp form
 constexpr int kElems = 16;          // row elements a thread holds in the cluster form (as many column sums beside them)
 constexpr int kMaxCluster = 8;
+constexpr int kStagedCluster = 4;   // blocks that share a staged row, 16,384 columns each
 constexpr int kWarps = 8;           // of a block of the warp form
 constexpr int kHeld = 32;           // row elements a thread holds in the staged forms
 constexpr int kHistHosts = 8192;    // counters kept in shared memory while counting
@@ -156,15 +157,20 @@ __device__ __forceinline__ bool any_host(const int *ids, int k, int n, bool acti
 // ---- rows that a warp or a block holds, staged -------------------------------------------------------------
 struct Layout {   // bytes of a stage: rows, then ids, then statistics
     int row_bytes, rows, k;
+    bool aligned;   // every row starts on a 16-byte boundary
     int whole;   // n if logits and gradient are handled 16 bytes at a time: columns below it need no look; else 0
     __host__ __device__ int hosts_at() const { return row_bytes * rows; }
     __host__ __device__ int stats_at() const { return hosts_at() + rows * k * 4; }
     __host__ __device__ int bytes() const { return (stats_at() + rows * 8 + 15) & ~15; }
 };
+// (a row's columns from `first` on, `columns` of them, land at the stage's start; first is a multiple of 16 bytes)
 template <typename T>
-__device__ __forceinline__ void stage(const BalanceArgs &a, const Layout &lay, char *at, int slot, long long row, int sub, int team)
+__device__ __forceinline__ void stage(const BalanceArgs &a, const Layout &lay, char *at, int slot, long long row, int sub, int team, int first = 0,
+                                      int columns = 1 << 21)
 {
-    stage_row(at + slot * lay.row_bytes, static_cast<const T *>(a.x) + row * a.stride, a.n, row * a.stride * (long long)sizeof(T), sub, team);
+    const int from = first * (int)sizeof(T) / 16;
+    stage_row(at + slot * lay.row_bytes, static_cast<const T *>(a.x) + row * a.stride, a.n, row * a.stride * (long long)sizeof(T), sub,
+              team, from, from + columns * (int)sizeof(T) / 16 + (lay.aligned ? 0 : 1), from);
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(at));
     for (int i = sub; i < a.k; i += team) copy_async4(to + lay.hosts_at() + (slot * a.k + i) * 4, a.hosts + row * a.k + i);
     if (a.stats_in && sub == 0) {
@@ -356,33 +362,38 @@ __global__ void __launch_bounds__(kWarps * 32, 2) balance_warp_kernel(BalanceArg
     }
 }
 
-// ---- block form: one row at a time per block, kHeld elements a thread; a block walks over its rows, group after group
-template <typename T, int VEC, bool GRAD>
-__global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, Layout lay)
+// ---- block form: one row at a time per block, or per cluster of cs of them, each with its stretch of the columns; kHeld
+// elements a thread; it walks over its rows, group after group
+template <typename T, int VEC, bool GRAD, bool MULTI>
+__global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, int cs_, Layout lay)
 {
+    const int cs = MULTI ? cs_ : 1;
     constexpr int CH = kHeld / VEC, width = 32 * VEC;   // a warp has one stretch of columns: offsets are known when compiled
     extern __shared__ __align__(16) char s_mem[];
-    __shared__ float4 s_stats[2][16];
-    float *s_f = reinterpret_cast<float *>(s_mem);
+    __shared__ float4 s_stats[2][kStagedCluster * 16];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int stage_bytes = lay.bytes(), base = warp * 32 * kHeld, first = base + lane * VEC;
+    // the block's columns: from block_first on, `columns` of them
+    const int rank = MULTI ? cluster_rank(cs) : 0, columns = blockDim.x * kHeld, block_first = rank * columns;
+    const int stage_bytes = lay.bytes(), base = block_first + warp * 32 * kHeld, first = base + lane * VEC;
+    float *s_f = reinterpret_cast<float *>(s_mem) - block_first;   // by column
     const bool saved = a.stats_in != nullptr;
-    char *stages = s_mem + blockDim.x * kHeld * 4;
-    const long long begin = blockIdx.x * a.block_rows, all_rows = a.group_rows * a.groups;
+    char *stages = s_mem + columns * 4;
+    const long long block = blockIdx.x / cs, begin = block * a.block_rows, all_rows = a.group_rows * a.groups;
     const long long end = begin + a.block_rows < all_rows ? begin + a.block_rows : all_rows;
     int turn = 0;
+    if (MULTI) cluster_sync(cs);   // all blocks of the cluster run: their shared memory may be written
     for (int group = (int)(begin / a.group_rows); group < a.groups && group * a.group_rows < end; ++group) {
     // the block's rows of this group
     const long long row0 = max(begin, group * a.group_rows);
     const int rows = (int)(min(end, (group + 1) * a.group_rows) - row0);
     auto queue = [&](int r, int st) {
-        if (r < rows) stage<T>(a, lay, stages + st * stage_bytes, 0, row0 + r, threadIdx.x, blockDim.x);
+        if (r < rows) stage<T>(a, lay, stages + st * stage_bytes, 0, row0 + r, threadIdx.x, blockDim.x, block_first, columns);
         copies_commit();
     };
 #pragma unroll
     for (int st = 0; st < kStages; ++st) queue(st, st);
     const GroupScale gs = group_scale(a, group);
-    for (int i = threadIdx.x; i < (int)blockDim.x * kHeld; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
+    for (int i = block_first + threadIdx.x; i < block_first + columns; i += blockDim.x) s_f[i] = i < a.n ? (float)a.counts[(size_t)group * a.n + i] * gs.inv_total : 0.0f;
     float acc[CH][VEC];
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -395,7 +406,7 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
         const long long row = row0 + r;
         const char *at = stages + st * stage_bytes;
         const T *x = static_cast<const T *>(a.x) + row * a.stride;
-        const T *staged = reinterpret_cast<const T *>(at + (VEC == 1 ? row_shift(x) : 0));
+        const T *staged = reinterpret_cast<const T *>(at + (VEC == 1 ? row_shift(x) : 0)) - block_first;   // by column
         const float2 given = saved ? staged_pair(at + lay.stats_at()) : make_float2(0.0f, 0.0f);
         float v[CH][VEC];
         load_staged<T, VEC, CH>(staged, first, width, a.n, lay.whole - base, v);
@@ -412,23 +423,25 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
         float s = lanes_sum(exp_all<VEC, CH>(v, m == neg_inf() ? 0.0f : m, kLog2e), 32), dot = 0.0f;
         if (GRAD) dot = lanes_sum(dot_all<VEC, CH>(v, s_f, first, width), 32);
         // one exchange for all three, each relative to the warp's maximum
-        if (lane == 0) s_stats[turn][warp] = make_float4(m, s, dot, 0.0f);
-        __syncthreads();
+        if (lane < cs) cluster_peer(s_stats[turn], lane, cs)[rank * warps + warp] = make_float4(m, s, dot, 0.0f);
+        cluster_sync(cs);
         queue(r + kStages, st);   // all that the stage holds has been read
-        const float4 w = lane < warps ? s_stats[turn][lane] : make_float4(neg_inf(), 0.0f, 0.0f, 0.0f);
-        if (!saved) m = lanes_max(w.x, 32);
-        const float scale = saved ? 1.0f : exp_from(w.x, m, kLog2e);
-        s = saved ? (live ? given.y : 0.0f) : lanes_sum(w.y * scale, 32);
-        if (GRAD) dot = lanes_sum(w.z * scale, 32);
+        const int parts = cs * warps;   // 64 at most
+        const float4 none = make_float4(neg_inf(), 0.0f, 0.0f, 0.0f);
+        const float4 w = lane < parts ? s_stats[turn][lane] : none, w2 = MULTI && lane + 32 < parts ? s_stats[turn][lane + 32] : none;
+        if (!saved) m = lanes_max(MULTI ? fmaxf(w.x, w2.x) : w.x, 32);
+        const float scale = saved ? 1.0f : exp_from(w.x, m, kLog2e), scale2 = saved ? 1.0f : exp_from(w2.x, m, kLog2e);
+        s = saved ? (live ? given.y : 0.0f) : lanes_sum(MULTI ? w.y * scale + w2.y * scale2 : w.y * scale, 32);
+        if (GRAD) dot = lanes_sum(MULTI ? w.z * scale + w2.z * scale2 : w.z * scale, 32);
         const float inv = s != 0.0f ? reciprocal(s) : 0.0f;
-        if (!saved && live && a.stats && threadIdx.x == 0) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
+        if (!saved && live && a.stats && threadIdx.x == 0 && rank == 0) a.stats[2 * row] = m, a.stats[2 * row + 1] = s;
         const float own = inv * (saved ? 1.0f : exp_from(m_warp, m, kLog2e));
         finish_row<T, VEC, CH, GRAD>(v, acc, own, gs.grad * own, dot * inv, s_f, static_cast<T *>(a.grad) + row * a.gstride, first, width, a.n,
                                      lay.whole - base, a.wide);
         st = st == kStages - 1 ? 0 : st + 1;
     }
     copies_drain();
-    float *out = a.partial + ((size_t)group * a.parts + (blockIdx.x - first_block(a, group))) * a.n;
+    float *out = a.partial + ((size_t)group * a.parts + (block - first_block(a, group))) * a.n;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -436,6 +449,7 @@ __global__ void __launch_bounds__(512, 1) balance_staged_kernel(BalanceArgs a, L
             if (!saved && first + c * width + i < a.n) out[first + c * width + i] = acc[c][i];
     __syncthreads();   // f of the next group may be written
     }
+    cluster_sync(cs);   // no block leaves while another may still write to its shared memory
 }
 
 // ---- cluster form: cs blocks per row at a time; grid (parts * cs, groups) -----------------------------------
@@ -782,10 +796,10 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     Plan p = {};
     p.vec = aligned;
     const int per = aligned ? 16 / elem : 1;
-    p.lay = Layout{staged_row_bytes(a.n, elem, aligned), 1, a.k, aligned && a.wide ? a.n : 0};
+    p.lay = Layout{staged_row_bytes(a.n, elem, aligned), 1, a.k, aligned, aligned && a.wide ? a.n : 0};
     // the rows of all groups in even stretches, as many as there are blocks at once
-    auto stretches = [&](long long at_once, int resident, long long least) {
-        const long long rows = a.group_rows * groups, most = (long long)sms * resident;
+    auto stretches = [&](long long at_once, int most, long long least) {
+        const long long rows = a.group_rows * groups;
         long long rounds = (rows + most * at_once - 1) / (most * at_once);
         if (rounds < least) rounds = least;
         p.block_rows = rounds * at_once;
@@ -798,17 +812,21 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
         p.lay.rows = 32 / p.lanes;
         p.shared = p.lanes * per * p.chunks * 4 + kWarps * kStages * p.lay.bytes();
         if (p.shared <= 112 * 1024) {
-            stretches((long long)kWarps * p.lay.rows, 2, 1);
+            stretches((long long)kWarps * p.lay.rows, 2 * sms, 1);
             return p;
         }
         p.lay.rows = 1;
     }
-    p.threads = ((a.n + kHeld - 1) / kHeld + 31) / 32 * 32;
+    p.cs = 1;
+    while (p.cs < kStagedCluster && p.cs * 512 * kHeld < a.n) p.cs *= 2;
+    p.threads = ((a.n + p.cs * kHeld - 1) / (p.cs * kHeld) + 31) / 32 * 32;
+    p.lay.row_bytes = staged_row_bytes(p.cs > 1 ? p.threads * kHeld : a.n, elem, aligned);
     p.shared = p.threads * kHeld * 4 + kStages * p.lay.bytes();
-    if (p.threads <= 512 && p.shared <= 220 * 1024 && a.group_rows * groups >= 2 * sms) {
+    if (p.threads <= 512 && p.shared <= 220 * 1024 && a.group_rows * groups * p.cs >= 2 * sms) {
         p.form = BLOCK;
         // a block's column sums are written and read once more: that should be little beside its rows
-        stretches(1, resident_blocks(128, p.threads, p.shared + 512), 6);
+        const int resident = resident_blocks(128, p.threads, p.shared + 2048);
+        stretches(1, sms * resident / p.cs, 6);
         return p;
     }
     p.form = CLUSTER;
@@ -853,11 +871,22 @@ cudaError_t launch_rows(const BalanceArgs &a, const Plan &p, cudaStream_t stream
 {
     constexpr int V = kPer16<T>;
     if (p.form == BLOCK) {
-        auto *kernel = p.vec ? balance_staged_kernel<T, V, GRAD> : balance_staged_kernel<T, 1, GRAD>;
+        auto *kernel = p.cs > 1 ? (p.vec ? balance_staged_kernel<T, V, GRAD, true> : balance_staged_kernel<T, 1, GRAD, true>)
+                                : (p.vec ? balance_staged_kernel<T, V, GRAD, false> : balance_staged_kernel<T, 1, GRAD, false>);
         const cudaError_t e = allow_shared(kernel, p.shared);
         if (e != cudaSuccess) return e;
-        kernel<<<p.blocks, p.threads, p.shared, stream>>>(a, p.lay);
-        return cudaGetLastError();
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned int)p.blocks * p.cs);
+        cfg.blockDim = dim3(p.threads);
+        cfg.dynamicSmemBytes = p.shared;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = p.cs;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, kernel, a, p.cs, p.lay);
     }
     if (p.vec) {
         if (p.chunks == 1) return launch_lanes<T, V, 1, GRAD>(a, p, stream);

@@ -255,7 +255,7 @@ def check_balance(nb, x, x64, hosts, scale, gl, dtype, **kw):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("groups,rows,n", [(1, 5, 1), (3, 7, 2), (2, 33, 3), (1, 640, 31), (5, 90, 32), (1, 1500, 33), (4, 40, 257),
                                            (2, 11, 1000), (3, 60, 1024), (1, 300, 1025), (2, 40, 4096), (1, 9, 4099),
-                                           (2, 3, 16385), (1, 4, 32771), (1, 3, 131072), (1, 3, 131073), (300, 2, 40)])
+                                           (2, 3, 16385), (1, 4, 32771), (1, 160, 16400), (2, 40, 40001), (1, 3, 131072), (1, 3, 131073), (300, 2, 40)])
 def test_balance_matches_the_checker(nb, groups, rows, n, dtype):
     rng = np.random.default_rng(groups * 7919 + rows * 104729 + n)
     for k, pad, shift in ((3, 0, 0), (1, 3, 1), (40, 8, 0)):
