@@ -31,7 +31,8 @@ DTYPES = ["float32", "bfloat16", "float16"]
 INF = math.inf
 # one host; around a warp's and a block's limits, odd sizes, a cluster's rows, rows read twice
 SIZES = [(5, 1), (7, 2), (33, 3), (64, 31), (9, 32), (100, 33), (40, 257), (11, 1000), (6, 1024), (5, 1025),
-         (4, 4096), (3, 4099), (2, 16385), (2, 32768), (3, 32771), (2, 70001), (1, 262144), (2, 262145)]
+         (4, 4096), (3, 4099), (2, 16385), (2, 32768), (3, 32771), (2, 70001), (1, 262144), (2, 262145),
+         (160, 16400), (80, 40001)]
 
 
 @pytest.fixture(scope="module")
