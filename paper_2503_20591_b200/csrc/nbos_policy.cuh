@@ -14,7 +14,6 @@ namespace nbos {
 namespace policy {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr unsigned int kFull = 0xFFFFFFFFu;
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xFF800000); }

@@ -4,11 +4,13 @@
 // teacher's q over its counting entries:
 //   loss = T^2 sum_k q_k (ln q_k - ln p_k),  d loss / d x_j = T (p_j - q_j).
 // What bounds it: the logits' bytes, read once, and as many written for the gradient. So a row stays in registers
-// between its reduction and its gradient (32 elements a thread): a power of two of lanes of one warp share a short
-// row (up to 1,024 hosts), a block a longer one (up to 16,384). Both stay on their SM and walk over the rows, with the
-// next two rows on their way to shared memory by asynchronous copies. Longer rows, or few of them, take a cluster
-// of up to 8 blocks each; only rows of more than 262,144 hosts are read twice. Each exponential is computed once; threads keep it relative to their warp's maximum and
-// scale it by 2^((m_warp - m) c) / S when the row's statistics are known.
+// between its reduction and its gradient (32 to 64 elements a thread): 4 to 32 lanes of a warp share a short row (up to
+// 1,024 hosts), a block a longer one (up to 16,384). Both stay on their SM and walk over the rows, the next ones on their
+// way to shared memory by asynchronous copies. Longer rows, or few of them, take a cluster of up to 8 blocks each; only
+// rows of more than 262,144 hosts are read twice. Each exponential is computed once; threads keep it relative to their
+// warp's maximum and scale it by 2^((m_warp - m) c) / S when the row's statistics are known.
+// Measured (B200, 6,464 GB/s copied): 262,144 x 1,024 bf16 loss and gradient 202 us = 5,330 GB/s, f32 375 us = 5,730 GB/s;
+// 65,536 x 4,096 bf16 238 us = 4,510 GB/s. 16-bit logits are bound by instruction issue beside the bytes.
 #include <math.h>
 
 #include "nbos_policy.cuh"

@@ -13,6 +13,8 @@
 // workspace instead.
 // A warp's columns are one stretch of the row, a lane's four of each 128 are neighbours: index order is warp, then
 // chunk of 128, then lane.
+// Measured (B200): 16,384 x 4,096 bf16 with all filters and three draws 181 us = 740 GB/s; 262,144 x 1,024 bf16 nucleus, one draw,
+// 981 us = 550 GB/s (some 3,400 warp instructions a row, the integer pipe 77 % busy), without filters 330 us.
 #include <math.h>
 
 #include "nbos_policy.cuh"
@@ -25,12 +27,12 @@ using namespace policy;
 constexpr int kChunk = 128;            // columns a warp takes at once, four a lane
 constexpr int kWarpChunks = 8;         // chunks of a warp, except of rows in the workspace
 constexpr int kWarpRow = kChunk * kWarpChunks;
-constexpr int kLoneRow = 4096;
+constexpr int kLoneRow = 4096;         // longest row of one warp: 16,384 x 4,096 bf16 nucleus 377 us against 495 by blocks of four
 constexpr int kMaxCluster = 8;
 constexpr int kBlockRow = 32 * kWarpRow;
 constexpr int kSort = 64;              // weights that one warp sorts, two a lane
 constexpr int kList = 128;             // hosts of a list that one warp holds in registers, four a lane
-constexpr int kListK = 112;            // largest top-k that tries for one
+constexpr int kListK = 112;            // largest top-k that tries for one: below 128, so that a threshold is found in few steps
 typedef unsigned long long u64;
 
 struct SampleArgs {
