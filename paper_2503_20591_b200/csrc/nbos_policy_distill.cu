@@ -616,10 +616,11 @@ int power_of_two(int n, int most)   // the first that is not below n
     while (p < n && p < most) p *= 2;
     return p;
 }
+// A launch has 48 KB without asking for more, static and dynamic together; the kernels here have less than 8 KB of the former.
 template <typename K>
 cudaError_t allow_shared(K *kernel, int bytes)
 {
-    return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+    return bytes > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
 }
 
 template <typename T, int LANES, int CH, bool GRAD, bool SAVED>
