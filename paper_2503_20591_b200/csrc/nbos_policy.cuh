@@ -405,6 +405,16 @@ inline int check_sm100(int *sms, int *device)
     NBOS_CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *device));
     return NBOS_OK;
 }
+// Dynamic shared memory that a block of any form takes at most; with the kernels' static part, less than 7 KB, what an SM has.
+constexpr int kMostShared = 220 * 1024;
+// Before a launch with `bytes` of it. A launch has 48 KB, static and dynamic together, unless the kernel has been allowed more. What is
+// allowed belongs to the kernel, not to the launch, and another host thread may be about to launch it with another size: so
+// it is the same for every size.
+template <typename K>
+inline cudaError_t allow_shared(K *kernel, int bytes)
+{
+    return bytes > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) : cudaSuccess;
+}
 // Blocks of a kernel that an SM holds at once: what a persistent grid is sized by. regs: the kernel's registers.
 inline int resident_blocks(int regs, int threads, size_t shared)
 {

@@ -828,7 +828,7 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     p.threads = ((a.n + p.cs * kHeld - 1) / (p.cs * kHeld) + 31) / 32 * 32;
     p.lay.row_bytes = staged_row_bytes(p.cs > 1 ? p.threads * kHeld : a.n, elem, aligned);
     p.shared = p.threads * kHeld * 4 + kStages * p.lay.bytes();
-    if (p.threads <= 512 && p.shared <= 220 * 1024 && a.group_rows * groups * p.cs >= 2 * sms) {
+    if (p.threads <= 512 && p.shared <= kMostShared && a.group_rows * groups * p.cs >= 2 * sms) {
         p.form = BLOCK;
         // a block's column sums are written and read once more: that should be little beside its rows
         const int resident = resident_blocks(128, p.threads, p.shared + 2048);
@@ -848,12 +848,6 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     return p;
 }
 
-// A launch has 48 KB without asking for more, static and dynamic together; the kernels here have less than 8 KB of the former.
-template <typename K>
-cudaError_t allow_shared(K *kernel, int bytes)
-{
-    return bytes > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
-}
 template <typename T, int VEC, int LANES, int CH, bool GRAD>
 cudaError_t launch_warp(const BalanceArgs &a, const Plan &p, cudaStream_t stream)
 {

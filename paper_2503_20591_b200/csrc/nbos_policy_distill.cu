@@ -616,12 +616,6 @@ int power_of_two(int n, int most)   // the first that is not below n
     while (p < n && p < most) p *= 2;
     return p;
 }
-// A launch has 48 KB without asking for more, static and dynamic together; the kernels here have less than 8 KB of the former.
-template <typename K>
-cudaError_t allow_shared(K *kernel, int bytes)
-{
-    return bytes > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
-}
 
 template <typename T, int LANES, int CH, bool GRAD, bool SAVED>
 cudaError_t launch_warp(const DistillArgs &a, const Layout &lay, int sms, cudaStream_t stream)
@@ -684,7 +678,7 @@ bool launch_staged(const DistillArgs &a, int sms, cudaStream_t stream, cudaError
     static const int regs = kernel_registers(kernel);
     const Layout lay{staged_row_bytes(a.n, sizeof(T), aligned), 1, a.k, aligned, aligned && a.wide ? a.n : 0};
     const int shared = kBlockStages * lay.bytes();
-    if (threads > 512 || shared > 220 * 1024 || a.rows < 2 * sms) return false;
+    if (threads > 512 || shared > kMostShared || a.rows < 2 * sms) return false;
     e = allow_shared(kernel, shared);
     if (e != cudaSuccess) return true;
     const long long fit = (long long)sms * resident_blocks(regs, threads, shared + 2560);

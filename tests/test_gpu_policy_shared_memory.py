@@ -55,5 +55,38 @@ def test_first_calls_of_a_process_near_the_limit(which):
     assert done.returncode == 0, done.stdout + done.stderr[-2000:]
 
 
+@pytest.mark.gpu
+def test_two_threads_with_different_sizes():
+    """Two host threads in the same kernel, one with 54 KB a block and one with 96 KB: neither may be refused because of the other."""
+    import threading
+
+    import torch
+    from paper_2503_20591_b200 import binding as nb, build as lib_build
+    lib_build.build()
+    nb.load_library()
+    refused, start = [], threading.Barrier(2)
+
+    def work(n):
+        x = torch.zeros((300, n), dtype=torch.bfloat16, device="cuda")
+        hosts = torch.zeros((300, 3), dtype=torch.int32, device="cuda")
+        loss, grad = torch.empty(300, device="cuda"), torch.empty_like(x)
+        even, counts = torch.empty(1, device="cuda"), torch.empty((1, n), dtype=torch.int32, device="cuda")
+        start.wait()
+        for _ in range(1500):
+            try:
+                nb.nbos_policy_distill(x, hosts, None, loss, out_grad=grad)
+                nb.nbos_policy_balance(x, hosts, even, counts, out_grad=grad)
+            except nb.NbosError as e:
+                refused.append((n, str(e)[:100]))
+        torch.cuda.synchronize()
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in (9000, 16000)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not refused, (len(refused), refused[:2])
+
+
 if __name__ == "__main__":
     sys.exit(min(1, calls(sys.argv[1])))
