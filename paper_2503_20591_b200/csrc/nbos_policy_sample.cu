@@ -46,15 +46,15 @@ struct SampleArgs {
     unsigned int *store;   // rows longer than the shared memory of a cluster: [clusters][n padded]
 };
 
-// floats in the order of unsigned integers
+// floats in the order of unsigned integers; both zeros are 0x80000000, so that key - 1 is the next smaller value
 __device__ __forceinline__ unsigned int key_of(float x)
 {
     const unsigned int b = __float_as_uint(x);
-    return b ^ ((unsigned int)((int)b >> 31) | 0x80000000u);
+    return (int)b < 0 ? 0u - b : b + 0x80000000u;
 }
 __device__ __forceinline__ float float_of(unsigned int key)
 {
-    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+    return __uint_as_float(key & 0x80000000u ? key - 0x80000000u : 0u - key);
 }
 
 // +inf counts as the largest finite float
@@ -453,7 +453,7 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
                 unsigned int most_in = 0, least_in = 0xFFFFFFFFu;
                 e.each(lane, [&](unsigned int v, int) {
                     const float f = __uint_as_float(v);
-                    const unsigned int key = key_of(f + 0.0f);   // + 0: one zero
+                    const unsigned int key = key_of(f);
                     if (f <= hi_f) most_in = max(most_in, key);
                     if (f > lo_f) least_in = min(least_in, key);
                 });
@@ -509,7 +509,7 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         team.sum(total, count);
         u64 limit = share_of(total, (unsigned int)(fmaxf(p.top_p, 0.0f) * 0x1p24f));
         if (limit == 0) limit = 1;
-        auto key_at = [&](int col) { return key_of(fminf(to_float(x[col]), kMaxFinite) + 0.0f); };
+        auto key_at = [&](int col) { return key_of(fminf(to_float(x[col]), kMaxFinite)); };
         u64 keep, ties;
         const unsigned int cut = nucleus(team, e, limit, total, count, sort_list, keep, ties, key_at);
         least = max(least, cut);
@@ -847,7 +847,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs &a, long long row, T
             unsigned int key[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                key[j] = lane + 32 * j < length ? key_of(__uint_as_float(lists->hosts.x[lane + 32 * j]) + 0.0f) : 0u;
+                key[j] = lane + 32 * j < length ? key_of(__uint_as_float(lists->hosts.x[lane + 32 * j])) : 0u;
             finish(a, row, p, key, length, lane, lists->hosts.col);
             return;
         }
@@ -872,7 +872,7 @@ __global__ void __launch_bounds__(128) sample_short_kernel(SampleArgs a)
     for (int j = 0; j < 4; ++j) {
         v[j] = fminf(fmaxf(v[j], neg_inf()), kMaxFinite);   // NaN as -inf
         p.m = fmaxf(p.m, v[j]);
-        key[j] = v[j] > neg_inf() ? key_of(v[j] + 0.0f) : 0u;
+        key[j] = v[j] > neg_inf() ? key_of(v[j]) : 0u;
     }
     p.m = lanes_max(p.m, 32);
     if (p.greedy && p.m > neg_inf()) {
