@@ -447,8 +447,8 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         float lo_f = zero_below(p), hi_f = p.m;
         unsigned int lo = key_of(lo_f), hi = key_of(hi_f), above_hi = 0;
         bool exact = false;
-        // invariant: above(hi) < k <= above(lo); the first step looks at lo
-        for (int it = 0; !exact && hi - lo > 1; ++it) {
+        // invariant: above(hi) < k <= above(lo); the first step looks at lo, and is taken even where hi is the next value
+        for (int it = 0; !exact && (it == 0 || hi - lo > 1); ++it) {
             if ((it & 3) == 3) {   // the bounds onto logits that occur
                 unsigned int most_in = 0, least_in = 0xFFFFFFFFu;
                 e.each(lane, [&](unsigned int v, int) {

@@ -58,3 +58,36 @@ def test_whole_scores_of_which_many_are_zero(nb, rows, n):  # noqa: F811
     u = rng.random((rows, 8)).astype(np.float32)
     kw = dict(temperature=np.full(rows, np.float32(1.4426950408889634)), top_k=top_ks(rng, rows, n))
     same(run_sample(nb, table(v, "float32"), u, **kw), P.sample(v, u, **kw))
+
+
+LOG2E = np.float32(1.4426950408889634)
+
+
+def near_the_best(rng, rows, n, best, below):
+    """Rows in which some 40 hosts have `best`, many `below` (its neighbour in 32 bits), others half of it or nothing."""
+    v = np.full((rows, n), best / 2, np.float32)
+    v[rng.random((rows, n)) < 0.6] = below
+    v[rng.random((rows, n)) < 0.1] = -INF
+    v[rng.random((rows, n)) < 40 / n] = best
+    v[:, n // 2] = best
+    return v
+
+
+@pytest.mark.parametrize("rows,n", FORMS[1:])
+@pytest.mark.parametrize("best,c", [(2.0 ** 28, 1.0), (400.0, 2.0 ** 20)])
+def test_top_k_where_the_next_value_has_no_weight(nb, rows, n, best, c):  # noqa: F811
+    """One step of 32 bits below the best logit is 32 powers of two: nothing but the best has a weight."""
+    rng = np.random.default_rng(rows + n)
+    T = np.float32(LOG2E / np.float32(c))
+    assert LOG2E / T == c
+    below = np.nextafter(np.float32(best), np.float32(0))
+    assert (np.float32(best) - below) * c in (16, 32)       # 2^28 is a power of two: half a step below it
+    if (np.float32(best) - below) * c == 16:
+        best, below = best + 32, best
+    v = near_the_best(rng, rows, n, best, below)
+    u = rng.random((rows, 8)).astype(np.float32)
+    for k in (50, 120, n - 1):
+        kw = dict(temperature=np.full(rows, T), top_k=np.full(rows, k, np.int32))
+        got, want = run_sample(nb, table(v, "float32"), u, **kw), torch_sample(table(v, "float32"), u, **kw)
+        same(got, want)
+        assert (got[1] > 0).all()
