@@ -287,12 +287,9 @@ struct Row {
     bool greedy;   // T too small to divide by: the best host
 };
 
-// weights at and below this logit are 0
-__device__ __forceinline__ float zero_below(const Row &p)
-{
-    const float lo = __fsub_rn(p.m, __fdiv_rn(32.0f, p.scale));
-    return lo < p.m ? lo : neg_inf();   // m so large that the distance vanishes
-}
+// Weights at and below this logit are 0. Rounded down: where neighbouring floats are as far apart as 32 powers of two, the nearest
+// one may lie above m - 32 / scale and have a weight.
+__device__ __forceinline__ float zero_below(const Row &p) { return __fsub_rd(p.m, __fdiv_ru(32.0f, p.scale)); }
 
 // descending over (a of lane 0 .. 31, b of lane 0 .. 31), a bitonic network
 __device__ __forceinline__ void sort64(unsigned int &a, unsigned int &b, int lane)

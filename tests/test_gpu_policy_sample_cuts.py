@@ -63,12 +63,12 @@ def test_whole_scores_of_which_many_are_zero(nb, rows, n):  # noqa: F811
 LOG2E = np.float32(1.4426950408889634)
 
 
-def near_the_best(rng, rows, n, best, below):
-    """Rows in which some 40 hosts have `best`, many `below` (its neighbour in 32 bits), others half of it or nothing."""
+def near_the_best(rng, rows, n, best, below, some=40):
+    """Rows in which `some` hosts or so have `best`, many `below` (its neighbour in 32 bits), others half of it or nothing."""
     v = np.full((rows, n), best / 2, np.float32)
     v[rng.random((rows, n)) < 0.6] = below
     v[rng.random((rows, n)) < 0.1] = -INF
-    v[rng.random((rows, n)) < 40 / n] = best
+    v[rng.random((rows, n)) < some / n] = best
     v[:, n // 2] = best
     return v
 
@@ -91,3 +91,21 @@ def test_top_k_where_the_next_value_has_no_weight(nb, rows, n, best, c):  # noqa
         got, want = run_sample(nb, table(v, "float32"), u, **kw), torch_sample(table(v, "float32"), u, **kw)
         same(got, want)
         assert (got[1] > 0).all()
+
+
+@pytest.mark.parametrize("rows,n", FORMS)
+@pytest.mark.parametrize("best,c", [(2.0 ** 27 + 16, 1.5), (400.0, 1.5 * 2.0 ** 19), (200.0, 0.0)])
+def test_top_k_where_the_next_value_has_a_weight(nb, rows, n, best, c):  # noqa: F811
+    """One step of 32 bits below the best logit is 24 powers of two (22 at 200 with T = 1e-6): its hosts come after the best ones."""
+    rng = np.random.default_rng(rows + n)
+    T = np.float32(LOG2E / np.float32(c)) if c else np.float32(1e-6)
+    below = np.nextafter(np.float32(best), np.float32(0))
+    if c:
+        assert LOG2E / T == np.float32(c) and (np.float32(best) - below) * c == 24
+    v = near_the_best(rng, rows, n, best, below, some=3)
+    u = rng.random((rows, 8)).astype(np.float32)
+    for k in (20, 50, 120, n - 1):
+        kw = dict(temperature=np.full(rows, T), top_k=np.full(rows, k, np.int32))
+        got, want = run_sample(nb, table(v, "float32"), u, **kw), torch_sample(table(v, "float32"), u, **kw)
+        same(got, want)
+        assert (got[1] == 8).all()
