@@ -56,7 +56,10 @@ class _BalanceLoss(torch.autograd.Function):
 
 def distill_loss(logits, hosts, teacher_logits=None, temperature: float = 1.0) -> torch.Tensor:
     """Loss per row [...] of logits [..., H] against the teacher's hosts [..., k] (int32, -1 = none; what
-    nbos_place_batch writes can be passed as it is) with logits [..., k], [k] or None (all equal)."""
+    nbos_place_batch writes can be passed as it is) with logits [..., k], [k] or None (all equal). The gradient is that of
+    `logits`; the teacher has none."""
+    if torch.is_grad_enabled() and isinstance(teacher_logits, torch.Tensor) and teacher_logits.requires_grad:
+        raise ValueError("teacher_logits has no gradient here: detach it")
     return _DistillLoss.apply(logits, hosts, teacher_logits, float(temperature))
 
 
