@@ -64,8 +64,9 @@ def distill_loss(logits, hosts, teacher_logits=None, temperature: float = 1.0) -
 
 
 def balance_loss(logits, hosts):
-    """(loss [N], counts [N, H], mean shares [N, H]) of logits [N, B, H] and the hosts chosen [N, B, k]; without
-    the leading N for logits [B, H]. The loss has a gradient, counts and shares have none."""
+    """(loss [N], counts [N, H], mean shares [N, H]) of logits [N, B, H] and the hosts that the policy chose
+    [N, B, k] (sample_hosts, or its best ones: its own load is what the loss evens out); without the leading N for logits
+    [B, H]. The loss has a gradient, counts and shares have none."""
     if logits.dim() > 3:
         raise ValueError("logits must be [N, B, H] or [B, H]")
     return _BalanceLoss.apply(logits, hosts)

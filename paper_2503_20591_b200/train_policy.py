@@ -3,9 +3,9 @@
     python -m paper_2503_20591_b200.train_policy [--hosts 256] [--snapshots 16] [--batch 512] [--steps 150]
 
 One step: a batch of requests is placed by nbos_place_batch on every snapshot (the teacher); the policy scores every
-host for every request; the distillation loss pulls it to the teacher's three hosts, the balance loss keeps its
-probability from gathering on few of them. Afterwards the policy answers by sampling three distinct hosts per
-request, and both ways of placing are compared.
+host for every request and answers by sampling three distinct hosts; the distillation loss pulls it to the teacher's
+three hosts, the balance loss moves probability away from hosts that its own answers load more than others. Afterwards
+both ways of placing are compared.
 """
 from __future__ import annotations
 
@@ -17,6 +17,7 @@ from . import binding, policy, workloads
 
 BALANCE_WEIGHT = 0.01
 TEACHER_LOGITS = (2.0, 1.0, 0.0)   # best, second, third host
+ANSWER = dict(temperature=0.7, top_k=16, top_p=0.95, min_p=0.01)   # how the policy is asked
 
 
 class TwoTowerPolicy(torch.nn.Module):
@@ -87,13 +88,17 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
             there = wanted[..., :1] >= 0
             return float(((best == wanted).any(-1, keepdim=True) & there).sum() / there.sum())
 
+        def answer(logits):
+            """Three distinct hosts a request, drawn from the policy, and how many were there."""
+            return policy.sample_hosts(logits.detach(), torch.rand((snapshots, batch, 3), generator=gen, device="cuda"), **ANSWER)
+
         history = []
         for step in range(steps):
             requests = draw()
             wanted = cluster.teacher(requests)
             logits = net(request_features(requests), cluster.features, cluster.fits(requests))
             distill = policy.distill_loss(logits, wanted, teacher_logits)
-            even, counts, _ = policy.balance_loss(logits, wanted)
+            even, _, _ = policy.balance_loss(logits, answer(logits)[0])   # the load is the policy's own, not the rule's
             loss = distill.mean() + BALANCE_WEIGHT * even.mean()
             optimizer.zero_grad(set_to_none=True)
             loss.backward()
@@ -107,8 +112,7 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
         fits = cluster.fits(requests)
         with torch.no_grad():
             logits = net(request_features(requests), cluster.features, fits)
-        placed, found = policy.sample_hosts(logits, torch.rand((snapshots, batch, 3), generator=gen, device="cuda"),
-                                            temperature=0.7, top_k=16, top_p=0.95, min_p=0.01)
+        placed, found = answer(logits)
         chosen = placed >= 0
         feasible = fits.gather(2, placed.clamp(min=0).long()) | ~chosen
         distinct = all(((placed[..., i] != placed[..., j]) | ~chosen[..., i] | ~chosen[..., j]).all().item()
