@@ -602,7 +602,12 @@ __global__ void __launch_bounds__(1024, 1) balance_block_kernel(BalanceArgs a, i
 
 // ---- small groups: one block per group does everything, without a workspace --------------------------------
 constexpr int kSmallHosts = 512, kSmallWarps = 32;
-constexpr long long kSmallElements = 64 * 1024;   // rows of a group * hosts
+// Rows of a group that one SM gets through in the time that a workspace, two clears and three kernels take to be queued. What counts is
+// how often the block's warps go round, 4 rows each up to 32 hosts, one row otherwise. One group, bf16, us a call here and by those
+// kernels: 1,024 x 32 14.4 / 18.5, 2,048 x 32 24.6 / 18.5; 512 x 64 18.5 / 19.5, 1,024 x 64 33 / 20.5; 256 x 256 17.3 / 20.2,
+// 512 x 128 28.5 / 19.5; 128 x 512 16.4 / 20.0. By rows * hosts alone 16,384 x 4 took 155 / 23, 65,536 x 1 597 / 29 and, with 256 chosen
+// hosts a row, 10,100 / 113.
+inline int small_rows(int n) { return n <= 32 ? 1024 : n <= 64 ? 512 : n <= 256 ? 256 : n <= kSmallHosts ? 128 : 0; }
 
 template <typename T, int LANES, int CH, bool GRAD>
 __global__ void __launch_bounds__(kSmallWarps * 32) balance_small_kernel(BalanceArgs a, int32_t *out_counts, float *shares, float *loss)
@@ -997,9 +1002,7 @@ int balance(const nbos_logits *l, int32_t groups, const int32_t *hosts, int32_t 
     // the path, and with it every rounding, goes by the logits alone: the loss is the same with a gradient or without
     const bool aligned = rows_aligned16(a.x, l->rows, a.stride, elem);
     a.wide = !a.grad || rows_aligned16(a.grad, l->rows, a.gstride, elem);
-    // One launch instead of a workspace, two clears and three kernels: faster as long as one SM gets through a group in the
-    // time that those take to be queued.
-    if (l->n_hosts <= kSmallHosts && a.group_rows * l->n_hosts <= kSmallElements) {
+    if (a.group_rows <= small_rows(l->n_hosts)) {
         const cudaError_t e = l->dtype == NBOS_F32    ? small<float>(a, groups, out_counts, out_shares, out_loss, stream)
                               : l->dtype == NBOS_BF16 ? small<__nv_bfloat16>(a, groups, out_counts, out_shares, out_loss, stream)
                                                       : small<__half>(a, groups, out_counts, out_shares, out_loss, stream);
