@@ -413,11 +413,12 @@ int nbos_scale_out_deficit(const int32_t *found, int32_t n_snapshots, int64_t ba
  * Read hosts as vocabulary entries or experts and rows as tokens and they are the same operators of a
  * language model.
  *
- *   data        DEVICE, aligned to its element type. Rows that start on 16-byte boundaries (data and row_stride)
- *               are moved 16 bytes at a time, others element by element.
+ *   data        DEVICE, aligned to its element type. Rows may start anywhere; those that start on 16-byte boundaries
+ *               (data and row_stride) are the fastest.
  *   row_stride  elements from one row to the next, >= n_hosts (any value when rows <= 1)
- * All arithmetic is in 32 bits (sums over columns and groups in 64), with one rounding to the logits' type at
- * the end. Results do not depend on the launch: no floating-point atomics. Every call is asynchronous on
+ * All arithmetic is in 32 bits, with one rounding to the logits' type at the end: a row's sums over its hosts, and the balance
+ * loss's sums over the rows that one block takes. That loss's sums over blocks and over hosts are in 64 bits; sampling adds
+ * whole numbers. Results do not change from run to run: no floating-point atomics. Every call is asynchronous on
  * `cuda_stream`; temporaries come from the library's stream-ordered pool. rows == 0 is a no-op (outputs per group
  * are still written). Errors of all of them: INVALID_ARG, NO_MEMORY, CUDA, UNSUPPORTED_DEVICE.
  */

@@ -789,7 +789,10 @@ void warp_shape(int n, int vec, int &lanes, int &chunks)
 {
     const int most = kHeld / vec;
     if (vec == 1) {
-        // neighbouring lanes write neighbouring elements: at least 16 of them, a sector's worth, but for the shortest rows
+        // Neighbouring lanes write neighbouring elements: at least 16 of them, a sector's worth, but for the shortest rows. What
+        // a row does not fill costs as much as what it does: 313,479 x 319 f16 with gradient 163 us by 16 lanes of 20 elements, 173 of 24, 201 of
+        // 32; 261,096 x 383 152 by 24, 173 by 32; 130,378 x 767 136 by 32 lanes of 24, 162 of 32; 400,000 x 250 173 by 16 lanes of
+        // 16, 189 of 20; 1,666,666 x 60 250 by 8 lanes of 8, 479 by 16.
         lanes = n <= 64 ? 8 : n <= 512 ? 16 : 32;
         chunks = n <= 32 ? 4 : n <= 128 ? 8 : n <= 256 ? 16 : n <= 320 ? 20 : n <= 384 ? 24 : n <= 512 ? 32 : n <= 768 ? 24 : 32;
         return;
@@ -833,9 +836,12 @@ Plan make_plan(const BalanceArgs &a, int groups, int elem, bool aligned, int sms
     p.threads = ((a.n + p.cs * kHeld - 1) / (p.cs * kHeld) + 31) / 32 * 32;
     p.lay.row_bytes = staged_row_bytes(p.cs > 1 ? p.threads * kHeld : a.n, elem, aligned);
     p.shared = p.threads * kHeld * 4 + kStages * p.lay.bytes();
+    // Fewer rows leave SMs idle here; the cluster form has several blocks to a row. bf16 with gradient, us here / there: 148 x 4,096
+    // 32.3 / 26.3, 296 x 4,096 32.5 / 27.8, 592 x 4,096 34.6 / 34.3; 296 x 16,384 52.5 / 52.4, 592 x 16,384 56.6 / 63.5.
     if (p.threads <= 512 && p.shared <= kMostShared && a.group_rows * groups * p.cs >= 2 * sms) {
         p.form = BLOCK;
-        // a block's column sums are written and read once more: that should be little beside its rows
+        // a block's column sums are written and read once more: that should be little beside its rows (2,000 x 2,048 bf16 32 us
+        // with at least six rows a block, 37 with two)
         const int resident = resident_blocks(128, p.threads, p.shared + 2048);
         stretches(1, sms * resident / p.cs, 6);
         return p;

@@ -27,7 +27,9 @@ using namespace policy;
 constexpr int kChunk = 128;            // columns a warp takes at once, four a lane
 constexpr int kWarpChunks = 8;         // chunks of a warp, except of rows in the workspace
 constexpr int kWarpRow = kChunk * kWarpChunks;
-constexpr int kLoneRow = 4096;         // longest row of one warp: 16,384 x 4,096 bf16 nucleus 377 us against 495 by blocks of four
+// Longest row of one warp. bf16, us by one warp / by a block of a warp for each 1,024 hosts: 24,000 x 1,040 plain 55 / 176, nucleus 124 / 430,
+// all filters 85 / 300; 24,000 x 3,000 142 / 194, 419 / 566, 193 / 314; 24,000 x 4,096 213 / 216, 580 / 662, 265 / 335.
+constexpr int kLoneRow = 4096;
 constexpr int kMaxCluster = 8;
 constexpr int kBlockRow = 32 * kWarpRow;
 constexpr int kSort = 64;              // weights that one warp sorts, two a lane
@@ -927,7 +929,8 @@ cudaError_t launch(SampleArgs a, int sms, int device, cudaStream_t stream)
         return cudaGetLastError();
     }
     // One warp alone exchanges nothing and waits for nobody: it takes rows of up to kLoneRow hosts as long as there are
-    // enough of them to fill the SMs that way.
+    // enough of them to fill the SMs that way. Nucleus, us by one warp / by blocks: 600 x 4,096 34 / 29, 1,000 x 4,096 37 / 39,
+    // 1,200 x 4,096 44 / 45, 2,400 x 4,096 72 / 79.
     if (a.n <= kWarpRow || (a.n <= kLoneRow && a.rows >= 8 * sms)) {
         const int chunks = (a.n + kChunk - 1) / kChunk, warps = chunks <= kWarpChunks ? 4 : 2;
         const int warp_bytes = (int)sizeof(Lists) + chunks * kChunk * 4;
