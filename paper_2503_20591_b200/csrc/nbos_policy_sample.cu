@@ -289,9 +289,9 @@ struct Row {
     bool greedy;   // T too small to divide by: the best host
 };
 
-// Weights at and below this logit are 0. Rounded down: where neighbouring floats are as far apart as 32 powers of two, the nearest
-// one may lie above m - 32 / scale and have a weight.
-__device__ __forceinline__ float zero_below(const Row &p) { return __fsub_rd(p.m, __fdiv_ru(32.0f, p.scale)); }
+// Weights at and below this logit are 0: 32 powers of two below the best one, and one more for the quotient's rounding. Rounded down: where
+// neighbouring floats are as far apart as that, the nearest one may lie above and have a weight.
+__device__ __forceinline__ float zero_below(const Row &p) { return __fsub_rd(p.m, __fdiv_rn(33.0f, p.scale)); }
 
 // descending over (a of lane 0 .. 31, b of lane 0 .. 31), a bitonic network
 __device__ __forceinline__ void sort64(unsigned int &a, unsigned int &b, int lane)
@@ -446,8 +446,10 @@ __device__ __forceinline__ void decide(const SampleArgs &a, long long row, const
         float lo_f = zero_below(p), hi_f = p.m;
         unsigned int lo = key_of(lo_f), hi = key_of(hi_f), above_hi = 0;
         bool exact = false;
-        // invariant: above(hi) < k <= above(lo); the first step looks at lo, and is taken even where hi is the next value
-        for (int it = 0; !exact && (it == 0 || hi - lo > 1); ++it) {
+        // invariant: above(hi) < k <= above(lo); the first step looks at lo_f. Where that is the next value below hi, lo goes one further
+        // down, so that the step is taken all the same.
+        if (hi - lo == 1) --lo;
+        for (int it = 0; !exact && hi - lo > 1; ++it) {
             if ((it & 3) == 3) {   // the bounds onto logits that occur
                 unsigned int most_in = 0, least_in = 0xFFFFFFFFu;
                 e.each(lane, [&](unsigned int v, int) {

@@ -176,3 +176,28 @@ def test_sample_with_many_long_rows(nb, rows, n, dtype):  # noqa: F811
             got, want = run_sample(nb, x, u, **kw), torch_sample(x, u, **kw)
             np.testing.assert_array_equal(got[0], want[0])
             np.testing.assert_array_equal(got[1], want[1])
+
+
+# ---- as many hosts a row as there may be --------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,n", [(5000, 24), (5000, 400), (2000, 1000), (1300, 3000), (20, 20000)])
+def test_256_hosts_a_row(nb, rows, n, dtype):  # noqa: F811
+    """Long lists of entries leave less room for rows: narrow tables take the block form of the balance loss, for instance."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows + n)
+    x, _ = logits_of(gen, rows, n, dtype)
+    hosts = hosts_of(gen, rows, n, 256)
+    teacher = torch.randn((rows, 256), generator=gen, device="cuda") * 2
+    ones, scale = torch.ones(rows, device="cuda"), 512.0 * rows / n
+    loss, grad = torch.full((rows,), -7.0, device="cuda"), torch.full((rows, n), 99.0, dtype=x.dtype, device="cuda")
+    nb.nbos_policy_distill(x, hosts, teacher, loss, None, ones, 64.0, grad)
+    want_l, tol_l, want_g, size = distill64(x, hosts, teacher, 1.0, ones.double() * 64)
+    within(loss, want_l, tol_l)
+    within(grad, want_g, TOL_P * size + want_g.abs() * (HALF_ULP[dtype] * 1.01) + SMALLEST[dtype])
+    even, counts, shares = torch.empty(1, device="cuda"), torch.empty((1, n), dtype=torch.int32, device="cuda"), torch.empty((1, n), device="cuda")
+    nb.nbos_policy_balance(x[None], hosts[None], even, counts, shares, None, None, scale, grad[None])
+    want = balance64(x, hosts, scale)
+    assert torch.equal(counts[0], want[1])
+    within(shares[0], want[2], want[2] * (TOL_P + 64 * E) + E * 2.0 ** -100)
+    within(even[0], want[0], want[0] * (TOL_P + 64 * E))
+    within(grad, want[3], 2 * TOL_P * want[4] + want[3].abs() * (HALF_ULP[dtype] * 1.01) + SMALLEST[dtype])
