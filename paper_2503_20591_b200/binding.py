@@ -617,11 +617,12 @@ def nbos_policy_balance(logits, hosts, out_loss, out_counts, out_shares=None, ou
     ids, k = _choices(hosts, logits, rows)
     cells = n * desc.n_hosts
     grad, gstride = _grad_like(out_grad, logits)
-    _check(load_library().nbos_policy_balance(
-        ctypes.byref(desc), n, ids, k, _dense(grad_loss, "grad_loss", f32, n, device), grad_scale,
-        _dense(out_loss, "out_loss", f32, n, device), _dense(out_counts, "out_counts", torch.int32, cells, device),
-        _dense(out_shares, "out_shares", f32, cells, device), _dense(out_stats, "out_stats", f32, 2 * rows, device),
-        grad, gstride, _policy_stream(stream, device)))
+    args = (ctypes.byref(desc), n, ids, k, _dense(grad_loss, "grad_loss", f32, n, device), grad_scale,
+            _dense(out_loss, "out_loss", f32, n, device), _dense(out_counts, "out_counts", torch.int32, cells, device),
+            _dense(out_shares, "out_shares", f32, cells, device), _dense(out_stats, "out_stats", f32, 2 * rows, device),
+            grad, gstride, _policy_stream(stream, device))
+    if n:   # no groups: no outputs
+        _check(load_library().nbos_policy_balance(*args))
 
 
 def nbos_policy_balance_backward(logits, hosts, stats, out_grad, grad_loss=None, grad_scale=1.0, stream=None) -> None:
@@ -630,9 +631,10 @@ def nbos_policy_balance_backward(logits, hosts, stats, out_grad, grad_loss=None,
     n, rows, device, f32 = _groups(logits), desc.rows, logits.device, torch.float32
     ids, k = _choices(hosts, logits, rows)
     grad, gstride = _grad_like(out_grad, logits)
-    _check(load_library().nbos_policy_balance_backward(
-        ctypes.byref(desc), n, ids, k, _dense(stats, "stats", f32, 2 * rows, device),
-        _dense(grad_loss, "grad_loss", f32, n, device), grad_scale, grad, gstride, _policy_stream(stream, device)))
+    args = (ctypes.byref(desc), n, ids, k, _dense(stats, "stats", f32, 2 * rows, device),
+            _dense(grad_loss, "grad_loss", f32, n, device), grad_scale, grad, gstride, _policy_stream(stream, device))
+    if n:
+        _check(load_library().nbos_policy_balance_backward(*args))
 
 
 def nbos_policy_sample(logits, uniforms, out_hosts, out_found=None, temperature=None, top_k=None, top_p=None,
