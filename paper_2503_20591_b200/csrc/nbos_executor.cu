@@ -199,6 +199,7 @@ __global__ void __launch_bounds__(512, 2) select_executors_kernel(const ExecArgs
 constexpr int kRingThreads = 512;        // consumers; + one copy warp
 constexpr int kRingTile = kRingThreads;  // kernels per stage, one per consumer thread
 constexpr int kRingStages = 4;
+constexpr size_t kRingShared = 110 * 1024;   // dynamic shared memory of a block at most: two blocks an SM
 constexpr uint32_t kRingStageBytes = kRingTile * (16u + 12u);
 
 __global__ void __launch_bounds__(kRingThreads + 32, 2) select_executors_ring_kernel(const ExecArgs a, const int table_bytes)
@@ -387,9 +388,10 @@ extern "C" int nbos_select_executors(const nbos_cluster_state *state, const int3
         // the plain form from 2^20 kernels, 15 - 25 % faster at 2^22 and above)
         const size_t table_bytes = ((size_t)(H + 1) * (sizeof(uint2) + sizeof(unsigned int)) + 127) & ~(size_t)127;
         const size_t ring_smem = table_bytes + (size_t)kRingStages * kRingStageBytes + 2 * kRingStages * 8 + 16;
-        const bool use_ring = ring_smem <= 110 * 1024 && aligned16(replica_hosts) && n_kernels >= (1ll << 19);
+        const bool use_ring = ring_smem <= kRingShared && aligned16(replica_hosts) && n_kernels >= (1ll << 19);
         if (use_ring) {
-            e = cudaFuncSetAttribute(select_executors_ring_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring_smem);
+            // the limit belongs to the kernel, and another host thread may be launching it with more: the same for every size
+            e = cudaFuncSetAttribute(select_executors_ring_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingShared);
             if (e == cudaSuccess)
                 select_executors_ring_kernel<<<sms * 2, kRingThreads + 32, ring_smem, stream>>>(a, (int)table_bytes);
         } else {
