@@ -51,7 +51,7 @@ def test_top_k_cut_at_zero(nb, rows, n, dtype):  # noqa: F811
 
 @pytest.mark.parametrize("rows,n", [(60, 300), (40, 1024), (10, 3000)])
 def test_whole_scores_of_which_many_are_zero(nb, rows, n):  # noqa: F811
-    """The same against the checker: whole logits at c = 1 have exact weights."""
+    """The same against the oracle: whole logits at c = 1 have exact weights."""
     rng = np.random.default_rng(n)
     v = np.maximum(rng.integers(-9, 6, size=(rows, n)), 0).astype(np.float32)
     v[: rows // 2] = np.where(rng.random((rows // 2, n)) < 20 / n, v[: rows // 2], 0)

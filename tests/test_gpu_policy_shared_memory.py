@@ -1,6 +1,6 @@
 """Calls whose blocks take just under 48 KB of dynamic shared memory, the limit that a kernel has unless it asks for more. That limit
 holds for the static part too, and what a kernel has asked for stays with it for the life of the process: so each list of
-calls below runs in a process of its own, one call per instance of a kernel, and their answers are compared with the 64-bit checker
+calls below runs in a process of its own, one call per instance of a kernel, and their answers are compared with the 64-bit oracle
 within the tolerances derived in test_gpu_policy.py."""
 from __future__ import annotations
 
