@@ -518,6 +518,57 @@ int nbos_policy_sample(const nbos_logits *logits, const float *uniforms, const f
                        const int32_t *top_k, const float *top_p, const float *min_p, int32_t draws,
                        int32_t *out_hosts, int32_t *out_found, void *cuda_stream);
 
+/*
+ * Distillation of a two-tower policy without its table of logits. Such a policy scores a host for a request as the
+ * product of two vectors; with many requests and hosts the table [rows, n_hosts] is far larger than the vectors, and is
+ * never stored here: the forward call keeps a row's maximum and sum, the backward call computes the scores once more and holds
+ * pieces of at most 256 MB (or 256 rows / hosts, where that is more) of their gradient.
+ *   x[g, r, h] = sum_i requests[g, r, i] * hosts[g, h, i], -inf unless the request fits the host: asks[g, r, i] <= room[g, h, i] and
+ *   asks[g, r, i] >= 0 for all four i. (With asks = the requests of nbos_place_batch and room[0] = the GPUs that the host's size and
+ *   subscription limit leave, that is the rule's own test.) asks and room NULL: every request fits every host.
+ * Loss and gradient are those of nbos_policy_distill on these logits, row by row and entry by entry; rows that fit nowhere, or
+ * without a counting entry, have loss and gradient 0 (a vector of theirs that is not finite may still make the other tower's
+ * gradient NaN).
+ *     grad_requests = G hosts, grad_hosts = G^T requests, G = T * (p - q) * grad_scale * grad_loss[r]
+ * Products are of 16-bit values with 32-bit sums, statistics are in 32 bits. G is rounded to the vectors' type (relative: a
+ * factor that follows the largest |grad_loss| keeps it within a 16-bit float's range) before it is multiplied, a
+ * gradient once more at the end.
+ *   towers          vectors DEVICE, NBOS_BF16 or NBOS_F16, of any alignment and row stride >= width; rows on 16-byte boundaries (address,
+ *                   strides) are read as they lie, others are copied first. A group stride may be 0 (one table for all groups).
+ *   hosts, teacher_logits, teacher_stride, k, temperature, grad_loss, grad_scale   as for nbos_policy_distill; hosts
+ *                   [n_groups * rows * k]
+ *   out_loss        DEVICE [n_groups * rows] float or NULL
+ *   out_stats       DEVICE [n_groups * rows * (2 + k)] float or NULL: what the backward call needs (a row's m and S, or (0, inf) if it
+ *                   has no counting entry, and its logits at its hosts, -inf where the entry is none or does not fit)
+ *   out_grad_*      DEVICE, the vectors' type, or NULL; groups must not overlap; may not overlap the inputs
+ * The kernels wait on copies and products with a limit; nbos_policy_towers_status synchronises `cuda_stream` and returns
+ * NBOS_ERR_DEVICE_TIMEOUT, once, if a wait on the current device ran out since it was last asked: outputs since then are undefined
+ * (losses are NaN).
+ */
+#define NBOS_POLICY_MAX_WIDTH 65536
+typedef struct nbos_towers {
+    const void *requests;         /* DEVICE [n_groups][rows][request_stride]    */
+    const void *hosts;            /* DEVICE [n_groups][n_hosts][host_stride]    */
+    int64_t rows;                 /* per group; n_groups * rows < 2^31          */
+    int64_t request_stride, request_group_stride, host_stride, host_group_stride; /* elements */
+    int32_t n_groups;             /* 1 .. 65535 (the snapshots of a sweep)      */
+    int32_t n_hosts;              /* 1 .. NBOS_MAX_HOSTS                        */
+    int32_t width;                /* 1 .. NBOS_POLICY_MAX_WIDTH                 */
+    int32_t dtype;                /* NBOS_BF16 | NBOS_F16                       */
+    const int32_t *asks;          /* DEVICE [n_groups * rows * 4] or NULL, 16-byte aligned    */
+    const int32_t *room;          /* DEVICE [n_groups * n_hosts * 4] or NULL, 16-byte aligned */
+} nbos_towers;
+
+int nbos_policy_towers(const nbos_towers *towers, const int32_t *hosts, const float *teacher_logits,
+                       int64_t teacher_stride, int32_t k, float temperature, float *out_loss, float *out_stats,
+                       void *cuda_stream);
+int nbos_policy_towers_backward(const nbos_towers *towers, const int32_t *hosts, const float *teacher_logits,
+                                int64_t teacher_stride, int32_t k, float temperature, const float *stats,
+                                const float *grad_loss, float grad_scale, void *out_grad_requests,
+                                int64_t grad_request_stride, int64_t grad_request_group_stride, void *out_grad_hosts,
+                                int64_t grad_host_stride, int64_t grad_host_group_stride, void *cuda_stream);
+int nbos_policy_towers_status(void *cuda_stream);
+
 /* Synchronises `cuda_stream` and returns the sticky device status of this snapshot: NBOS_OK, or
  * NBOS_ERR_DEVICE_TIMEOUT if some kernel gave up on a bounded wait (its outputs are then
  * undefined), NBOS_ERR_RANGE / NBOS_ERR_STALE_LAYOUT after an nbos_snapshot_update whose new state

@@ -41,6 +41,7 @@ NBOS_F16 = 2
 NBOS_POLICY_MAX_ROWS = 2147483647
 NBOS_POLICY_MAX_K = 256
 NBOS_POLICY_MAX_DRAWS = 8
+NBOS_POLICY_MAX_WIDTH = 65536
 
 NBOS_PROBE_MIX_ALU = 0
 NBOS_PROBE_MIX_IMAD = 1
@@ -55,7 +56,7 @@ EXPORTED_SYMBOLS = (
     "nbos_place_batch_noalloc", "nbos_select_executors",
     "nbos_cluster_sums", "nbos_scale_out_deficit", "nbos_place_batch_sequential",
     "nbos_policy_distill", "nbos_policy_distill_backward", "nbos_policy_balance", "nbos_policy_balance_backward",
-    "nbos_policy_sample",
+    "nbos_policy_sample", "nbos_policy_towers", "nbos_policy_towers_backward", "nbos_policy_towers_status",
     "nbos_snapshot_status", "nbos_strerror", "nbos_last_error_detail",
     "nbos_probe_int32_issue", "nbos_probe_wait_timeout", "nbos_probe_wait_timeout_on_snapshot",
 )
@@ -102,6 +103,16 @@ class nbos_logits(ctypes.Structure):
     _fields_ = [
         ("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("row_stride", ctypes.c_int64),
         ("n_hosts", ctypes.c_int32), ("dtype", ctypes.c_int32),
+    ]
+
+
+class nbos_towers(ctypes.Structure):
+    _fields_ = [
+        ("requests", ctypes.c_void_p), ("hosts", ctypes.c_void_p), ("rows", ctypes.c_int64),
+        ("request_stride", ctypes.c_int64), ("request_group_stride", ctypes.c_int64),
+        ("host_stride", ctypes.c_int64), ("host_group_stride", ctypes.c_int64),
+        ("n_groups", ctypes.c_int32), ("n_hosts", ctypes.c_int32), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("asks", ctypes.c_void_p), ("room", ctypes.c_void_p),
     ]
 
 
@@ -158,6 +169,9 @@ def load_library() -> ctypes.CDLL:
     lib.nbos_policy_balance.argtypes = [P(nbos_logits), i32, vp, i32, vp, f32, vp, vp, vp, vp, vp, i64, vp]
     lib.nbos_policy_balance_backward.argtypes = [P(nbos_logits), i32, vp, i32, vp, vp, f32, vp, i64, vp]
     lib.nbos_policy_sample.argtypes = [P(nbos_logits), vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.nbos_policy_towers.argtypes = [P(nbos_towers), vp, vp, i64, i32, f32, vp, vp, vp]
+    lib.nbos_policy_towers_backward.argtypes = [P(nbos_towers), vp, vp, i64, i32, f32, vp, vp, f32, vp, i64, i64, vp, i64, i64, vp]
+    lib.nbos_policy_towers_status.argtypes = [vp]
     lib.nbos_snapshot_status.argtypes = [vp, vp]
     lib.nbos_strerror.argtypes = [ctypes.c_int]
     lib.nbos_strerror.restype = ctypes.c_char_p
@@ -653,6 +667,89 @@ def nbos_policy_sample(logits, uniforms, out_hosts, out_found=None, temperature=
         _dense(top_p, "top_p", f32, rows, device), _dense(min_p, "min_p", f32, rows, device), draws,
         _dense(out_hosts, "out_hosts", i32, rows * draws, device), _dense(out_found, "out_found", i32, rows, device),
         _policy_stream(stream, device)))
+
+
+# ---- two towers: distillation without the table of logits --------------------------------
+_TOWER_DTYPES = {torch.bfloat16: NBOS_BF16, torch.float16: NBOS_F16}
+
+
+def _vectors(t, what: str):
+    """(groups, rows, width, row stride, group stride) of vectors [N, rows, width] or [rows, width]."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _TOWER_DTYPES:
+        raise TypeError(f"{what} must be a bfloat16 or float16 torch tensor (cast float32 vectors: the products are of 16-bit values)")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must live on cuda, not {t.device}")
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{what} must be [N, rows, width] or [rows, width]")
+    rows, width = t.shape[-2:]
+    if width > 1 and t.stride(-1) != 1 and t.numel():
+        raise ValueError(f"{what} must be contiguous along its width")
+    if t.dim() == 2:
+        return 1, rows, width, t.stride(0), 0
+    return t.shape[0], rows, width, t.stride(1), t.stride(0)
+
+
+def _towers(requests, host_vectors, hosts, asks, room):
+    """(nbos_towers, rows over all groups, address of hosts, k)"""
+    n, rows, width, rstride, rgroup = _vectors(requests, "requests")
+    m, n_hosts, hwidth, hstride, hgroup = _vectors(host_vectors, "host_vectors")
+    if (n, width, requests.dim(), requests.dtype) != (m, hwidth, host_vectors.dim(), host_vectors.dtype):
+        raise ValueError("requests [..., B, D] and host_vectors [..., H, D] must agree on their groups, width and type")
+    device = requests.device
+    if host_vectors.device != device:
+        raise ValueError(f"host_vectors must live on {device}, not {host_vectors.device}")
+    ids, k = _choices(hosts, requests, n * rows)
+    if (asks is None) != (room is None):
+        raise ValueError("asks and room come together")
+    desc = nbos_towers(requests.data_ptr(), host_vectors.data_ptr(), rows, rstride, rgroup, hstride, hgroup, n, n_hosts, width,
+                       _TOWER_DTYPES[requests.dtype], _dense(asks, "asks", torch.int32, 4 * n * rows, device),
+                       _dense(room, "room", torch.int32, 4 * n * n_hosts, device))
+    return desc, n * rows, ids, k
+
+
+def _grad_vectors(grad, vectors, what: str):
+    """(address, row stride, group stride) of a gradient like `vectors`."""
+    if grad is None:
+        return 0, 0, 0
+    if not isinstance(grad, torch.Tensor) or grad.dtype != vectors.dtype or grad.shape != vectors.shape or grad.device != vectors.device:
+        raise ValueError(f"{what} must have its vectors' shape, type and device")
+    _, _, _, stride, group = _vectors(grad, what)
+    return grad.data_ptr(), stride, group
+
+
+def nbos_policy_towers(requests, host_vectors, hosts, teacher_logits, out_loss, out_stats=None, temperature=1.0, asks=None, room=None,
+                       stream=None) -> None:
+    """Distillation of a two-tower policy, logits = requests @ host_vectors^T never stored. Device tensors: requests [N, B, D]
+    and host_vectors [N, H, D] (or without N) bfloat16 or float16, hosts [N, B, k] int32 (-1 = none), teacher_logits [N, B, k] or [k]
+    float32 or None, out_loss [N, B] float32 or None, out_stats [N, B, 2 + k] float32 or None; asks [N, B, 4] and room
+    [N, H, 4] int32 or None: a request fits a host if its four asks are within the host's room. Asynchronous on the stream."""
+    desc, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room)
+    device, f32 = requests.device, torch.float32
+    teacher, tstride = _teacher(teacher_logits, hosts, device, rows, k)
+    args = (ctypes.byref(desc), ids, teacher, tstride, k, temperature, _dense(out_loss, "out_loss", f32, rows, device),
+            _dense(out_stats, "out_stats", f32, (2 + k) * rows, device), _policy_stream(stream, device))
+    if desc.n_groups:
+        _check(load_library().nbos_policy_towers(*args))
+
+
+def nbos_policy_towers_backward(requests, host_vectors, hosts, teacher_logits, stats, out_grad_requests=None, out_grad_hosts=None,
+                                grad_loss=None, grad_scale=1.0, temperature=1.0, asks=None, room=None, stream=None) -> None:
+    """The gradients of nbos_policy_towers from the statistics it saved (out_stats): out_grad_requests like requests,
+    out_grad_hosts like host_vectors, either may be None; grad_loss [N, B] float32 or None."""
+    desc, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room)
+    device, f32 = requests.device, torch.float32
+    teacher, tstride = _teacher(teacher_logits, hosts, device, rows, k)
+    args = (ctypes.byref(desc), ids, teacher, tstride, k, temperature, _dense(stats, "stats", f32, (2 + k) * rows, device),
+            _dense(grad_loss, "grad_loss", f32, rows, device), grad_scale,
+            *_grad_vectors(out_grad_requests, requests, "out_grad_requests"),
+            *_grad_vectors(out_grad_hosts, host_vectors, "out_grad_hosts"), _policy_stream(stream, device))
+    if desc.n_groups:
+        _check(load_library().nbos_policy_towers_backward(*args))
+
+
+def nbos_policy_towers_status(stream=None) -> int:
+    """Synchronises the stream; NBOS_ERR_DEVICE_TIMEOUT, once, if a wait in a two-tower kernel on the current device ran out."""
+    return load_library().nbos_policy_towers_status(_stream_ptr(stream))
 
 
 def nbos_probe_int32_issue(mix: int, iters: int, blocks: int, threads: int, stream=None):

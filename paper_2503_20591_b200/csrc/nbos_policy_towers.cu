@@ -1,0 +1,1230 @@
+// Distillation of a two-tower policy without its table of logits (nbos_policy_towers, nbos_policy_towers_backward).
+//
+// With a the requests' vectors, b the hosts', c = log2(e) / T, and x_rh = a_r . b_h where the request fits the host, else -inf:
+//   forward   m_r = max_h x_rh,  S_r = sum_h 2^((x_rh - m_r) c)      a matrix product whose tiles never leave the chip
+//             y_rj = x at the row's hosts,  loss_r = T^2 sum_j q_j (ln q_j - (y_rj - m_r) / T + ln S_r)
+//   backward  G_rh = g_r T (p_rh - q_rh), p_rh = 2^((x_rh - m_r) c) / S_r    the product once more
+//             da = G b,  db = G^T a                                           two more products
+// G exists in pieces of rows, in 16 bits (the operands' type): at most kPieceBytes of it.
+#include <math.h>
+
+#include "nbos_policy.cuh"
+#include "nbos_tensor.cuh"
+
+namespace nbos {
+namespace {
+
+using namespace policy;
+using namespace tensor;
+
+constexpr int kTileM = 256;           // rows of a pair's tile; each of its two blocks has 128 of them
+constexpr int kTileN = 256;           // columns; narrower tiles of 128 for gradients of at most 128 columns
+constexpr int kBlockK = 64;           // values of the contraction per stage: one 128-byte row
+constexpr int kEpilogue = 256;        // threads that read the products: 8 warps, two a quarter of the tensor memory
+constexpr int kThreads = kEpilogue + 64;   // and a warp that copies, a warp that multiplies
+constexpr int kTmemColumns = 512;     // two tiles of 32-bit products
+constexpr size_t kPieceBytes = 256u << 20;
+
+enum Kind { STATS, GRAD, GRAD_REQUESTS, GRAD_HOSTS };
+
+struct Tiles {                        // what one launch covers
+    int groups, m_tiles, n_tiles, k_blocks;
+    int splits, split_blocks;         // the contraction in parts, whose sums are added up afterwards
+    long long units;                  // groups * m_tiles * n_tiles * splits
+};
+struct TowerArgs {
+    Tiles t;
+    int a_z0, a_z, b_z0, b_z;         // group g is slice z0 + g * z of the operand
+    int a_m0, b_n0, b_k0;             // first row of the operand
+    int group0, row0, rows, hosts, width;   // rows: of a group
+    int col0, col_end;                // scores: the launch's first host, and how many it has
+    const int4 *asks, *room;
+    float c;                          // log2(e) / T
+    float2 *partial;                  // STATS: [groups][rows][slots] (m, S) of parts of a row
+    int slots;
+    const float *stats;               // GRAD: [groups][rows][stats_stride]: m, S, ...
+    int stats_stride;
+    const float *grad_loss, *range;   // range: factor that keeps G within 16 bits, and its inverse (NULL: 1)
+    float grad_scale;
+    void *out;                        // gradients: the result itself (one part), or
+    float *sums;                      // [splits][groups][m_rows][width] of 32-bit sums, added to those there if `add`
+    long long out_stride, out_group_stride;
+    int m_rows, out_row0, add;        // m_rows: rows that the launch writes, per group
+};
+
+__device__ unsigned int tower_status;   // STATUS_WAIT_TIMEOUT once a wait ran out, until nbos_policy_towers_status is asked
+
+// STATS: pair p of `pairs` takes units [first_unit(p), first_unit(p + 1)), hosts innermost: a pair stays with its rows as long
+// as it can, and all pairs have equally much to do.
+__device__ __host__ __forceinline__ long long first_unit(long long units, int pairs, int p)
+{
+    const long long q = units / pairs, r = units % pairs;
+    return p * q + (p < r ? p : r);
+}
+__device__ __host__ __forceinline__ int pair_of(long long units, int pairs, long long unit)
+{
+    const long long q = units / pairs, r = units % pairs;
+    return (int)(unit < r * (q + 1) ? unit / (q + 1) : r + (unit - r * (q + 1)) / q);
+}
+
+struct Unit {
+    int g, m, n, split, k0, k1;       // k0 .. k1: blocks of the contraction
+};
+template <Kind KIND>
+struct Schedule {
+    long long at, end, step;
+    __device__ __forceinline__ Schedule(const Tiles &t, int pair, int pairs)
+    {
+        if (KIND == STATS)
+            at = first_unit(t.units, pairs, pair), end = first_unit(t.units, pairs, pair + 1), step = 1;
+        else
+            at = pair, end = t.units, step = pairs;
+    }
+    __device__ __forceinline__ bool next(const Tiles &t, Unit &u)
+    {
+        if (at >= end) return false;
+        if (KIND == STATS) {
+            u.n = (int)(at % t.n_tiles);
+            const long long rest = at / t.n_tiles;
+            u.m = (int)(rest % t.m_tiles), u.g = (int)(rest / t.m_tiles);
+            u.split = 0;
+        } else {
+            // bands of 8 tiles along M, so that tiles in flight at one time share both operands
+            const long long per_split = (long long)t.m_tiles * t.n_tiles, part = at / per_split;
+            const int in = (int)(at % per_split), band = in / (8 * t.n_tiles), high = min(8, t.m_tiles - 8 * band);
+            const int rest = in - band * 8 * t.n_tiles;
+            u.m = 8 * band + rest % high, u.n = rest / high;
+            u.split = (int)(part % t.splits), u.g = (int)(part / t.splits);
+        }
+        u.k0 = u.split * t.split_blocks;
+        u.k1 = min(t.k_blocks, u.k0 + t.split_blocks);
+        at += step;
+        return true;
+    }
+};
+
+template <Kind KIND, int BN>
+struct Shape {
+    static constexpr bool kAlongKA = KIND != GRAD_HOSTS, kAlongKB = KIND == STATS || KIND == GRAD;
+    static constexpr int kBytesA = 128 * kBlockK * 2, kBytesB = BN / 2 * kBlockK * 2, kStageBytes = kBytesA + kBytesB;
+    static constexpr int kStaging = KIND == GRAD ? 4 * 128 * 128 : 0;    // G on its way out: four boxes of 128 rows x 64 columns
+    static constexpr int kRoom = KIND == STATS || KIND == GRAD ? 2 * kTileN * 16 : 0;
+    static constexpr int kStages = KIND == GRAD ? 4 : 6;
+    static constexpr int kBytes = kStages * kStageBytes + kStaging + kRoom + 256 /* barriers */ + 1024 /* alignment */;
+};
+
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// d = a b + c, two at a time
+__device__ __forceinline__ void fma2_to(float &d0, float &d1, float a0, float a1, float b, float c)
+{
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %4};\n\tmov.b64 z, {%5, %5};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+}
+__device__ __forceinline__ bool fits(const int4 &ask, const int4 &room)
+{
+    return ask.x <= room.x && ask.y <= room.y && ask.z <= room.z && ask.w <= room.w;
+}
+__device__ __forceinline__ bool never_fits(const int4 &ask) { return (ask.x | ask.y | ask.z | ask.w) < 0; }
+
+// v where the request fits, else -inf: four compares that hand on one predicate (&& became branches: forward of 65,536 x 4,096 hosts at width 256 494 us, this 239)
+__device__ __forceinline__ uint32_t if_fits(uint32_t v, const int4 &ask, const int4 &room)
+{
+    uint32_t out;
+    asm("{\n\t.reg .pred p;\n\tsetp.le.s32 p, %1, %5;\n\tsetp.le.and.s32 p, %2, %6, p;\n\tsetp.le.and.s32 p, %3, %7, p;\n\t"
+        "setp.le.and.s32 p, %4, %8, p;\n\tselp.b32 %0, %9, 0xFF800000, p;\n\t}"
+        : "=r"(out)
+        : "r"(ask.x), "r"(ask.y), "r"(ask.z), "r"(ask.w), "r"(room.x), "r"(room.y), "r"(room.z), "r"(room.w), "r"(v));
+    return out;
+}
+
+// 64 products of one row become logits: -inf where the request does not fit and behind the last host
+template <bool MASK>
+__device__ __forceinline__ void mask64(uint32_t (&u)[32], uint32_t (&v)[32], const int4 *room, const int4 &ask, int left)
+{
+    const uint32_t none = 0xFF800000u;
+    if (MASK) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) u[i] = if_fits(u[i], ask, room[i]);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = if_fits(v[i], ask, room[32 + i]);
+    } else if (left < 64) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) u[i] = i < left ? u[i] : none, v[i] = 32 + i < left ? v[i] : none;
+    }
+}
+
+// running (m, s) of a row over 64 more logits
+__device__ __forceinline__ void add64(float &m, float &s, uint32_t (&u)[32], uint32_t (&v)[32], float c)
+{
+    float top[4] = {m, m, m, m};
+#pragma unroll
+    for (int i = 0; i < 32; i += 4)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], fmaxf(__uint_as_float(u[i + j]), __uint_as_float(v[i + j])));
+    const float to = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    const float base = (to == neg_inf() ? 0.0f : to) * -c;
+    s *= exp2_fast(fmaf(m, c, base));
+    m = to;
+    float sum[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        float e0, e1, f0, f1;
+        fma2_to(e0, e1, __uint_as_float(u[i]), __uint_as_float(u[i + 1]), c, base);
+        fma2_to(f0, f1, __uint_as_float(v[i]), __uint_as_float(v[i + 1]), c, base);
+        add2(sum[0][0], sum[0][1], exp2_fast(e0), exp2_fast(e1));
+        add2(sum[1][0], sum[1][1], exp2_fast(f0), exp2_fast(f1));
+    }
+    s += (sum[0][0] + sum[0][1]) + (sum[1][0] + sum[1][1]);
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// One launch covers its units with pairs of blocks, each a persistent pair: one thread a block copies operand tiles
+// into a ring of stages, one thread of the pair multiplies them into one of two accumulators in tensor memory, eight warps a
+// block read the other. No wait is without a limit: when one runs out the block's flag goes up, copies and products stop, the
+// readers go through the rest of their units without waiting (so that their barriers stay matched), and the status
+// word says that the outputs are undefined.
+template <Kind KIND, int BN, bool MASK, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    tower_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                 const __grid_constant__ CUtensorMap map_g, const __grid_constant__ TowerArgs args)
+{
+    using S = Shape<KIND, BN>;
+    extern __shared__ char raw[];
+    const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
+    char *const shared = raw + (base - smem_addr(raw));
+    const uint32_t staging = base + S::kStages * S::kStageBytes;
+    int4 *const room = reinterpret_cast<int4 *>(shared + S::kStages * S::kStageBytes + S::kStaging);
+    char *const tail = shared + S::kStages * S::kStageBytes + S::kStaging + S::kRoom;
+    const uint32_t full = smem_addr(tail), empty = full + 8 * S::kStages, tmem_full = empty + 8 * S::kStages, tmem_empty = tmem_full + 16;
+    volatile unsigned int *const abort_flag = reinterpret_cast<volatile unsigned int *>(tail + 8 * (2 * S::kStages + 4));
+    const uint32_t tmem_word = tmem_empty + 16 + 4;
+    volatile const uint32_t *const tmem_at = reinterpret_cast<volatile const uint32_t *>(tail + 8 * (2 * S::kStages + 4) + 4);
+
+    const Tiles &t = args.t;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = pair_rank();
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
+        for (int b = 0; b < 2; ++b) mbar_init(tmem_full + 8 * b, 1), mbar_init(tmem_empty + 8 * b, 2 * kEpilogue / 32);
+        *abort_flag = 0u;
+        barriers_visible();
+    }
+    if (warp == kEpilogue / 32) {
+        if (lane == 0) prefetch_map(&map_a), prefetch_map(&map_b);
+        __syncwarp();
+        tmem_alloc(tmem_word, kTmemColumns);
+    }
+    fence_before();
+    __syncthreads();
+    cluster_barrier();
+    fence_after();
+    const uint32_t tmem = *tmem_at;
+
+    Unit u;
+    if (warp == kEpilogue / 32) {   // ---- copies
+        if (lane == 0) {
+            Schedule<KIND> todo(t, pair, pairs);
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            long long copied = 0;
+            while (ok && todo.next(t, u)) {
+                const int az = args.a_z0 + u.g * args.a_z, bz = args.b_z0 + u.g * args.b_z;
+                const int m0 = u.m * kTileM + (int)rank * 128, n0 = u.n * BN + (int)rank * (BN / 2);
+                for (int kb = u.k0; kb < u.k1; ++kb) {
+                    ok = wait_cluster(empty + 8 * stage, phase ^ 1, abort_flag);
+                    if (!ok) break;
+                    const uint32_t bar = peer_addr(full + 8 * stage, 0);
+                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * S::kStageBytes);
+                    const uint32_t a = base + stage * S::kStageBytes, b = a + S::kBytesA;
+                    if (S::kAlongKA) {
+                        load_box(a, &map_a, kb * kBlockK, args.a_m0 + m0, az, bar);
+                    } else {
+                        load_box(a, &map_a, m0, kb * kBlockK, az, bar);
+                        load_box(a + 64 * 128, &map_a, m0 + 64, kb * kBlockK, az, bar);
+                    }
+                    if (S::kAlongKB) {
+                        load_box(b, &map_b, kb * kBlockK, args.b_n0 + n0, bz, bar);
+                    } else {
+                        load_box(b, &map_b, n0, args.b_k0 + kb * kBlockK, bz, bar);
+                        if (BN == 256) load_box(b + 64 * 128, &map_b, n0 + 64, args.b_k0 + kb * kBlockK, bz, bar);
+                    }
+                    ++copied;
+                    if (++stage == S::kStages) stage = 0, phase ^= 1;
+                }
+            }
+            // every stage has been read: no arrival is on its way to this block any more
+            for (int s = 0; ok && s < S::kStages && s < copied; ++s) {
+                if (stage == 0) stage = S::kStages, phase ^= 1;
+                --stage;
+                ok = wait_cluster(empty + 8 * stage, phase, abort_flag);
+            }
+        }
+        __syncwarp();
+    } else if (warp == kEpilogue / 32 + 1) {   // ---- products
+        if (lane == 0 && rank == 0) {
+            Schedule<KIND> todo(t, pair, pairs);
+            constexpr uint32_t instr = instruction<T>(kTileM, BN, S::kAlongKA, S::kAlongKB);
+            constexpr int step_a = S::kAlongKA ? 32 : 2048, step_b = S::kAlongKB ? 32 : 2048;
+            const uint64_t base_a = operand_base(S::kAlongKA, 64 * 128), base_b = operand_base(S::kAlongKB, 64 * 128);
+            int stage = 0, buffer = 0;
+            uint32_t phase = 0, buffer_phase = 0;
+            bool ok = true;
+            while (ok && todo.next(t, u)) {
+                ok = wait_cluster(tmem_empty + 8 * buffer, buffer_phase ^ 1, abort_flag);
+                if (!ok) break;
+                fence_after();
+                const uint32_t d = tmem + buffer * kTileN;
+                for (int kb = u.k0; kb < u.k1; ++kb) {
+                    ok = wait_cluster(full + 8 * stage, phase, abort_flag);
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t a = base + stage * S::kStageBytes, b = a + S::kBytesA;
+#pragma unroll
+                    for (int k = 0; k < kBlockK / 16; ++k)
+                        mma(d, operand(base_a, a + k * step_a), operand(base_b, b + k * step_b), instr, kb > u.k0 || k > 0);
+                    commit_pair(empty + 8 * stage);
+                    if (++stage == S::kStages) stage = 0, phase ^= 1;
+                }
+                if (!ok) break;
+                commit_pair(tmem_full + 8 * buffer);
+                buffer ^= 1;
+                if (buffer == 0) buffer_phase ^= 1;
+            }
+        }
+        __syncwarp();
+    } else {   // ---- reading the products: a row a thread, half of the tile's columns a warp
+        Schedule<KIND> todo(t, pair, pairs);
+        const int half = warp / 4, row_in = (warp % 4) * 32 + lane;
+        const uint32_t lane_at = tmem + ((uint32_t)(warp % 4 * 32) << 16) + half * (BN / 2);
+        const uint32_t freed = peer_addr(tmem_empty, 0);
+        int buffer = 0, last_g = -1, last_m = -1, parity = 0;
+        uint32_t buffer_phase = 0;
+        int4 ask = make_int4(0, 0, 0, 0);
+        // STATS: the row's statistics so far; GRAD: -(m c + log2 S) and the factor of p
+        float run_m = neg_inf(), run_s = 0.0f, minus = 0.0f, factor = 0.0f;
+        bool dead = false, some_dead = false;
+        int slot = 0;
+        auto release = [&] {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(freed + 8 * buffer);
+        };
+        auto flush = [&] {
+            const int row = last_m * kTileM + (int)rank * 128 + row_in;
+            if (last_m < 0 || row >= args.rows) return;
+            if (MASK && never_fits(ask)) run_m = neg_inf(), run_s = 0.0f;
+            args.partial[((long long)last_g * args.rows + row) * args.slots + 2 * slot + half] = make_float2(run_m, run_s);
+        };
+        while (todo.next(t, u)) {
+            const int local = u.m * kTileM + (int)rank * 128 + row_in;   // row of the launch
+            if (KIND == STATS || KIND == GRAD) {
+                if (u.g != last_g || u.m != last_m) {
+                    const int row = args.row0 + local;
+                    const bool inside = row < args.rows;
+                    const long long at = (long long)(args.group0 + u.g) * args.rows + row;
+                    if (KIND == STATS) {
+                        flush();
+                        run_m = neg_inf(), run_s = 0.0f;
+                        slot = pair - pair_of(t.units, pairs, ((long long)u.g * t.m_tiles + u.m) * t.n_tiles);
+                    } else if (inside) {
+                        const float m = args.stats[at * args.stats_stride], s = args.stats[at * args.stats_stride + 1];
+                        dead = s == __int_as_float(0x7F800000);
+                        minus = -fmaf(m, args.c, log2f(s));
+                        factor = args.grad_scale * (args.grad_loss ? args.grad_loss[at] : 1.0f) * (args.range ? args.range[0] : 1.0f);
+                    } else {
+                        dead = true;
+                    }
+                    if (KIND == GRAD) some_dead = __any_sync(kFull, dead);
+                    if (MASK) ask = inside ? args.asks[at] : make_int4(0, 0, 0, 0);
+                    last_g = u.g, last_m = u.m;
+                }
+                const int4 *columns = room + parity * kTileN;
+                if (MASK) {
+                    const int n = u.n * BN + (int)threadIdx.x;
+                    room[parity * kTileN + threadIdx.x] =
+                        n < args.col_end ? args.room[(long long)(args.group0 + u.g) * args.hosts + args.col0 + n] : make_int4(-1, -1, -1, -1);
+                    bar_sync(1, kEpilogue);
+                    columns += half * (BN / 2);
+                    parity ^= 1;
+                }
+                wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
+                fence_after();
+#pragma unroll 1
+                for (int sub = 0; sub < 2; ++sub) {
+                    uint32_t v0[32], v1[32];
+                    const uint32_t at = lane_at + buffer * kTileN + 64 * sub;
+                    tmem_load32(v0, at);
+                    tmem_load32(v1, at + 32);
+                    tmem_wait(v0);
+                    tmem_wait(v1);
+                    if (sub == 1) release();
+                    const int n0 = u.n * BN + half * (BN / 2) + 64 * sub;
+                    mask64<MASK>(v0, v1, columns + 64 * sub, ask, args.col_end - n0);
+                    if constexpr (KIND == STATS) {
+                        add64(run_m, run_s, v0, v1, args.c);
+                    } else {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float e0, e1, f0, f1;
+                        fma2_to(e0, e1, __uint_as_float(v0[i]), __uint_as_float(v0[i + 1]), args.c, minus);
+                        fma2_to(f0, f1, __uint_as_float(v1[i]), __uint_as_float(v1[i + 1]), args.c, minus);
+                        e0 = exp2_fast(e0), e1 = exp2_fast(e1), f0 = exp2_fast(f0), f1 = exp2_fast(f1);
+                        mul2(e0, e1, factor, factor);
+                        mul2(f0, f1, factor, factor);
+                        v0[i / 2] = pack2(e0, e1, T()), v1[i / 2] = pack2(f0, f1, T());
+                    }
+                    if (some_dead && dead) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v0[i] = v1[i] = 0u;
+                    }
+                    const uint32_t box = staging + (2 * half + sub) * 128 * 128, line = box + row_in * 128;
+                    if (threadIdx.x % 128 == 0) stores_read_wait<1>();   // the store of two boxes ago has left this one
+                    bar_sync(2 + half, 128);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t(&w)[32] = j < 4 ? v0 : v1;
+                        const int k = 4 * (j % 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((j ^ (row_in & 7)) << 4)), "r"(w[k]),
+                                     "r"(w[k + 1]), "r"(w[k + 2]), "r"(w[k + 3])
+                                     : "memory");
+                    }
+                    async_proxy_fence();
+                    bar_sync(2 + half, 128);
+                    if (threadIdx.x % 128 == 0) {
+                        const int y = u.m * kTileM + (int)rank * 128;
+                        if (n0 < args.col_end && y < args.m_rows) store_box(&map_g, n0, y, u.g, box);
+                        stores_commit();
+                    }
+                    }
+                }
+            } else {
+                wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
+                fence_after();
+                const float undo = args.range ? args.range[1] : 1.0f;
+                const int n_first = u.n * BN + half * (BN / 2);
+#pragma unroll 1
+                for (int sub = 0; sub < BN / 64; ++sub) {
+                    uint32_t v[32];
+                    tmem_load32(v, lane_at + buffer * kTileN + 32 * sub);
+                    tmem_wait(v);
+                    if (sub == BN / 64 - 1) release();
+                    if (u.k0 >= u.k1) {   // a part behind the end of a shorter piece
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0u;
+                    }
+                    const int n0 = n_first + 32 * sub, cols = min(32, args.width - n0);
+                    if (local >= args.m_rows || cols <= 0) continue;
+                    if (args.sums) {
+                        float *to = args.sums + (((long long)u.split * t.groups + u.g) * args.m_rows + local) * args.width + n0;
+                        if (cols == 32 && args.width % 4 == 0) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4) {
+                                float4 w = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]),
+                                                       __uint_as_float(v[i + 3]));
+                                if (args.add) {
+                                    const float4 old = *reinterpret_cast<const float4 *>(to + i);
+                                    w.x += old.x, w.y += old.y, w.z += old.z, w.w += old.w;
+                                }
+                                *reinterpret_cast<float4 *>(to + i) = w;
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i < cols) to[i] = __uint_as_float(v[i]) + (args.add ? to[i] : 0.0f);
+                        }
+                    } else {
+                        T *to = static_cast<T *>(args.out) + (args.group0 + u.g) * args.out_group_stride +
+                                (args.out_row0 + (long long)local) * args.out_stride + n0;
+                        if (cols == 32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8) {
+                                float w[8];
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) w[j] = __uint_as_float(v[i + j]) * undo;
+                                *reinterpret_cast<uint4 *>(to + i) = pack16(w, T());
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i < cols) to[i] = from_float<T>(__uint_as_float(v[i]) * undo);
+                        }
+                    }
+                }
+            }
+            buffer ^= 1;
+            if (buffer == 0) buffer_phase ^= 1;
+        }
+        if (KIND == STATS) flush();
+        if (KIND == GRAD && threadIdx.x % 128 == 0) stores_drain();
+    }
+
+    fence_before();
+    __syncthreads();
+    if (*abort_flag) {   // copies and products in flight end within microseconds where the device works at all
+        if (threadIdx.x == 0) atomicOr(&tower_status, STATUS_WAIT_TIMEOUT);
+        const unsigned long long t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 1000000ull) __nanosleep(1000);
+    }
+    cluster_barrier();
+    fence_after();
+    if (warp == kEpilogue / 32) tmem_free(tmem, kTmemColumns);
+}
+
+// ---- small kernels around the products ----------------------------------------------------------------------
+// Operands that a tensor copy cannot read (rows off 16-byte boundaries) are laid out once a call: rows of `wide` values, a
+// multiple of 8, zeros behind the last.
+template <typename T>
+__global__ void lay_out_kernel(const T *src, long long stride, long long group_stride, int rows, int width, int wide, T *dst)
+{
+    const int chunks = wide / 8;
+    const long long n = (long long)rows * chunks, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    src += blockIdx.y * group_stride;
+    dst += (long long)blockIdx.y * rows * wide;
+    for (long long i = first; i < n; i += (long long)gridDim.x * blockDim.x) {
+        const int row = (int)(i / chunks), col = (int)(i % chunks) * 8;
+        const T *from = src + row * stride + col;
+        unsigned short w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = col + j < width ? reinterpret_cast<const unsigned short *>(from)[j] : (unsigned short)0;
+        *reinterpret_cast<uint4 *>(dst + row * (long long)wide + col) =
+            make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+    }
+}
+
+struct FinishArgs {
+    const void *a, *b;                // vectors, rows on 16-byte boundaries
+    long long a_stride, a_group_stride, b_stride, b_group_stride;
+    int groups, rows, hosts, width, k, slots, pairs, m_tiles, n_tiles;
+    long long units;
+    const int32_t *ids;
+    const float *teacher;
+    long long teacher_stride;
+    const int4 *asks, *room;
+    float T, c;
+    const float2 *partial;
+    float *loss, *stats;
+};
+
+// pair_of, in 32 bits where they do (a 64-bit division costs as much as a row's products)
+__device__ __forceinline__ int pair_at(const FinishArgs &f, long long unit)
+{
+    if (f.units > 0x7FFFFFFF) return pair_of(f.units, f.pairs, unit);
+    const unsigned int n = (unsigned int)f.units, q = n / f.pairs, r = n % f.pairs, u = (unsigned int)unit;
+    return (int)(u < r * (q + 1) ? u / (q + 1) : r + (u - r * (q + 1)) / q);
+}
+
+// <a, b[u]> over this lane's 16-byte pieces, all U at once and several pieces of each, so that their loads are under way together
+template <typename T, int U>
+__device__ __forceinline__ void dots(float (&out)[U], const T *a, const T *const (&b)[U], int width, int sub, int lanes)
+{
+    constexpr int AHEAD = U == 1 ? 4 : 2;
+    float s[U][2] = {};
+    auto add = [&](const uint4 &p, const uint4 (&w)[U]) {
+        float x[8];
+        unpack16(p, x, T());
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float y[8];
+            unpack16(w[u], y, T());
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) fma2(s[u][0], s[u][1], x[j], x[j + 1], y[j], y[j + 1]);
+        }
+    };
+    const int step = lanes * 8;
+    int i = sub * 8;
+    for (; i + (AHEAD - 1) * step + 8 <= width; i += AHEAD * step) {
+        uint4 p[AHEAD], w[AHEAD][U];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+            p[n] = *reinterpret_cast<const uint4 *>(a + i + n * step);
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[n][u] = *reinterpret_cast<const uint4 *>(b[u] + i + n * step);
+        }
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) add(p[n], w[n]);
+    }
+    for (; i + 8 <= width; i += step) {
+        uint4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = *reinterpret_cast<const uint4 *>(b[u] + i);
+        add(*reinterpret_cast<const uint4 *>(a + i), w);
+    }
+    for (int j = i; j < width && j < i + 8; ++j)
+#pragma unroll
+        for (int u = 0; u < U; ++u) s[u][0] = fmaf(to_float(a[j]), to_float(b[u][j]), s[u][0]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) out[u] = lanes_sum(s[u][0] + s[u][1], lanes);
+}
+
+// TEAM lanes a row: its parts' statistics become one, the logits at its hosts are computed, and the loss. `lanes` of the team
+// share a product, each team takes TEAM / lanes * U of them at a time. (One product after the other, a warp a row:
+// 74 us for 65,536 rows of 256 with three hosts each, this 41 to 49.)
+template <typename T, int TEAM, int U>
+__global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ FinishArgs f, int lanes)
+{
+    const int lane = threadIdx.x % TEAM;
+    const long long team = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / TEAM;
+    const bool inside = team < (long long)f.groups * f.rows;
+    const long long at = inside ? team : 0;
+    const int g = (int)(at / f.rows), row = (int)(at % f.rows);
+    auto team_max = [](float v) {
+#pragma unroll
+        for (int off = TEAM / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, off));
+        return v;
+    };
+
+    const int4 ask = f.asks ? f.asks[at] : make_int4(0, 0, 0, 0);
+    const long long first = ((long long)g * f.m_tiles + row / kTileM) * f.n_tiles;
+    const int parts = 2 * (pair_at(f, first + f.n_tiles - 1) - pair_at(f, first) + 1);
+    float m = neg_inf(), s = 0.0f;
+    for (int i = lane; i < parts; i += TEAM) {
+        const float2 p = f.partial[at * f.slots + i];
+        const float to = fmaxf(m, p.x), base = to == neg_inf() ? 0.0f : to;
+        s = s * exp2_fast((m - base) * f.c) + p.y * exp2_fast((p.x - base) * f.c);
+        m = to;
+    }
+    const float top = team_max(m), base = top == neg_inf() ? 0.0f : top;
+    s = lanes_sum(s * exp2_fast((m - base) * f.c), TEAM);
+
+    const int at_once = TEAM / lanes, sub = lane % lanes;
+    const T *a = static_cast<const T *>(f.a) + g * f.a_group_stride + row * f.a_stride;
+    const T *b = static_cast<const T *>(f.b) + g * f.b_group_stride;
+    // over this lane's entries: largest teacher logit, sum of w = 2^((t - tm) c), sum of w ((t - tm) - (x - m))
+    float tm = neg_inf(), ts = 0.0f, tx = 0.0f;
+    for (int j0 = 0; j0 < f.k; j0 += U * at_once) {
+        const T *of[U];
+        float t[U], x[U];
+        bool there[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * at_once + lane / lanes;
+            const int id = j < f.k ? f.ids[at * f.k + j] : -1;
+            t[u] = j < f.k && f.teacher ? f.teacher[at * f.teacher_stride + j] : 0.0f;
+            there[u] = id >= 0 && id < f.hosts;
+            if (there[u] && f.asks) there[u] = !never_fits(ask) && fits(ask, f.room[(long long)g * f.hosts + id]);
+            of[u] = there[u] ? b + id * f.b_stride : b;   // b: a row that is there, for a product that is not used
+        }
+        dots<T, U>(x, a, of, f.width, sub, lanes);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * at_once + lane / lanes;
+            if (sub != 0 || j >= f.k || !inside) continue;
+            x[u] = there[u] ? x[u] : neg_inf();
+            if (f.stats) f.stats[at * (2 + f.k) + 2 + j] = x[u];
+            if (x[u] != neg_inf() && t[u] > neg_inf()) {   // a NaN logit counts, and spoils its row
+                const float to = fmaxf(tm, t[u]), keep = exp2_fast((tm - to) * f.c), w = exp2_fast((t[u] - to) * f.c);
+                tx = ts > 0.0f ? keep * (tx + ts * (tm - to)) : 0.0f;
+                tx += w * ((t[u] - to) - (x[u] - base));
+                ts = ts * keep + w;
+                tm = to;
+            }
+        }
+    }
+    const float teacher_top = team_max(tm), keep = ts > 0.0f ? exp2_fast((tm - teacher_top) * f.c) : 0.0f;
+    tx = lanes_sum(ts > 0.0f ? keep * (tx + ts * (tm - teacher_top)) : 0.0f, TEAM);
+    ts = lanes_sum(keep * ts, TEAM);
+    if (lane != 0 || !inside) return;
+    const bool some = ts != 0.0f;   // or NaN
+    if (f.loss) {
+        float loss = some ? f.T * (tx / ts) + f.T * f.T * (logf(s) - logf(ts)) : 0.0f;
+        if (tower_status) loss = __int_as_float(0x7FC00000);
+        f.loss[at] = loss;
+    }
+    // a row without a counting entry has no gradient: S = inf makes its p 0
+    if (f.stats) f.stats[at * (2 + f.k)] = some ? top : 0.0f, f.stats[at * (2 + f.k) + 1] = some ? s : __int_as_float(0x7F800000);
+}
+
+// G's factor for 16-bit floats: 2^15 over the power of two at or above the largest |g_r T|, so that p and q, at most 1, use
+// the type's whole range (p of 2^-29 is still a normal number). `largest`: bits of the largest |grad_loss|.
+__global__ void largest_kernel(const float *grad_loss, long long n, unsigned int *largest)
+{
+    float m = 0.0f;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x)
+        m = fmaxf(m, fabsf(grad_loss[i]));
+    m = warp_max(m);
+    if (threadIdx.x % 32 == 0) atomicMax(largest, __float_as_uint(m));   // of floats above 0 the order of their bits
+}
+__global__ void range_kernel(const unsigned int *largest, float scale, float *range)
+{
+    const float g = (largest ? __uint_as_float(*largest) : 1.0f) * fabsf(scale);
+    int e = 0;
+    if (g > 0.0f && g < __int_as_float(0x7F800000)) frexpf(g, &e);
+    e = min(max(e, -100), 100);
+    range[0] = ldexpf(1.0f, 15 - e), range[1] = ldexpf(1.0f, e - 15);
+}
+
+struct PatchArgs {
+    int groups, group0, row0, rows_here, rows, host0, hosts_here, hosts, k;
+    const int32_t *ids;
+    const float *teacher;
+    long long teacher_stride;
+    const float *stats, *grad_loss, *range;
+    float grad_scale, c;
+    void *grad;
+    long long grad_stride, grad_group_stride;
+};
+// G at the teacher's hosts, p - q rounded once. `lanes` lanes a row (a power of two); entries that name one host add up.
+template <typename T>
+__global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ PatchArgs p, int lanes)
+{
+    const long long n = (long long)p.groups * p.rows_here, i = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / lanes;
+    const bool inside = i < n;
+    const int sub = threadIdx.x % lanes, g = inside ? (int)(i / p.rows_here) : 0, row = inside ? (int)(i % p.rows_here) : 0;
+    const long long at = (long long)(p.group0 + g) * p.rows + p.row0 + row;
+    const float *stats = p.stats + at * (2 + p.k), *teacher = p.teacher ? p.teacher + at * p.teacher_stride : nullptr;
+    const int32_t *ids = p.ids + at * p.k;
+    float top = neg_inf(), sum = 0.0f;
+    for (int j = sub; inside && j < p.k; j += lanes) {
+        const float t = teacher ? teacher[j] : 0.0f;
+        if (stats[2 + j] != neg_inf() && t > top) top = t;
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        if (off < lanes) top = fmaxf(top, __shfl_xor_sync(kFull, top, off));
+    for (int j = sub; inside && j < p.k; j += lanes) {
+        const float t = teacher ? teacher[j] : 0.0f;
+        if (stats[2 + j] != neg_inf() && t > neg_inf()) sum += exp2_fast((t - top) * p.c);
+    }
+    sum = lanes_sum(sum, lanes);
+    if (!inside || !(sum > 0.0f)) return;
+    const float minus = -fmaf(stats[0], p.c, log2f(stats[1]));
+    const float factor = p.grad_scale * (p.grad_loss ? p.grad_loss[at] : 1.0f) * (p.range ? p.range[0] : 1.0f);
+    for (int j = sub; j < p.k; j += lanes) {
+        const int id = ids[j];
+        if (id < p.host0 || id >= p.host0 + p.hosts_here || stats[2 + j] == neg_inf()) continue;
+        float q = 0.0f;
+        for (int l = 0; l < p.k; ++l) {
+            const float t = teacher ? teacher[l] : 0.0f;
+            if (ids[l] == id && t > neg_inf()) q += exp2_fast((t - top) * p.c);
+        }
+        const float prob = exp2_fast(fmaf(stats[2 + j], p.c, minus));
+        static_cast<T *>(p.grad)[g * p.grad_group_stride + row * p.grad_stride + id - p.host0] = from_float<T>((prob - q / sum) * factor);
+    }
+}
+
+// The parts' sums become the gradient: [splits][groups][rows][width] -> rows out_stride apart.
+template <typename T>
+__global__ void sums_kernel(const float *sums, int splits, int groups, int rows, int width, const float *range, T *out, long long stride,
+                            long long group_stride)
+{
+    const long long n = (long long)groups * rows * width;
+    const float undo = range ? range[1] : 1.0f;
+    if (width % 4 == 0) {
+        for (long long i = ((long long)blockIdx.x * blockDim.x + threadIdx.x) * 4; i < n; i += (long long)gridDim.x * blockDim.x * 4) {
+            float4 s = *reinterpret_cast<const float4 *>(sums + i);
+            for (int k = 1; k < splits; ++k) {
+                const float4 v = *reinterpret_cast<const float4 *>(sums + k * n + i);
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            }
+            const long long row = i / width;
+            T *to = out + row / rows * group_stride + row % rows * stride + i % width;
+            to[0] = from_float<T>(s.x * undo), to[1] = from_float<T>(s.y * undo), to[2] = from_float<T>(s.z * undo), to[3] = from_float<T>(s.w * undo);
+        }
+        return;
+    }
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
+        float s = sums[i];
+        for (int k = 1; k < splits; ++k) s += sums[k * n + i];
+        const long long row = i / width;
+        out[row / rows * group_stride + row % rows * stride + i % width] = from_float<T>(s * undo);
+    }
+}
+
+// rows of zeros (a batch without requests leaves the hosts' gradient at 0)
+template <typename T>
+__global__ void zero_kernel(T *out, int rows, int width, long long stride)
+{
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < (long long)rows * width; i += (long long)gridDim.x * blockDim.x)
+        out[i / width * stride + i % width] = from_float<T>(0.0f);
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled f = [] {
+        void *at = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &at, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            at = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(at);
+    }();
+    return f;
+}
+
+// A table of 16-bit values [groups][rows][width] whose rows lie on 16-byte boundaries
+struct Table {
+    const void *data;
+    long long stride, group_stride;   // elements; group_stride 0: one slice for all groups
+    int groups, rows, width;
+};
+// boxes of 64 columns (128 bytes, swizzled) x box_rows rows
+int make_map(CUtensorMap *map, const Table &t, int box_rows, int dtype)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return fail(NBOS_ERR_CUDA, "cuTensorMapEncodeTiled is not there");
+    const bool shared = t.group_stride == 0;
+    const cuuint64_t dims[3] = {(cuuint64_t)t.width, (cuuint64_t)t.rows, shared ? 1u : (cuuint64_t)t.groups};
+    const cuuint64_t strides[2] = {(cuuint64_t)t.stride * 2, shared ? (cuuint64_t)t.stride * 2 : (cuuint64_t)t.group_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, steps[3] = {1, 1, 1};
+    const CUresult r = encode(map, dtype == NBOS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                              const_cast<void *>(t.data), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(NBOS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+    return NBOS_OK;
+}
+// whether a tensor copy can read the table as it lies
+bool readable(const void *data, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride)
+{
+    return aligned_to(data, 16) && (rows <= 1 || stride % 8 == 0) && (groups <= 1 || group_stride % 8 == 0);
+}
+
+// One temporary allocation of a call, given back in stream order.
+class Workspace {
+public:
+    size_t add(size_t bytes)
+    {
+        const size_t at = size_;
+        size_ += (bytes + 1023) & ~(size_t)1023;
+        return at;
+    }
+    int allocate(int device, cudaStream_t stream)
+    {
+        cudaMemPool_t pool = nullptr;
+        const int rc = library_pool(device, &pool);
+        if (rc) return rc;
+        const cudaError_t e = cudaMallocFromPoolAsync(reinterpret_cast<void **>(&data_), size_ ? size_ : 1, pool, stream);
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            data_ = nullptr;
+            return fail(NBOS_ERR_NO_MEMORY, "device allocation failed: %s", cudaGetErrorString(e));
+        }
+        stream_ = stream;
+        return NBOS_OK;
+    }
+    template <typename V> V *at(size_t offset) const { return reinterpret_cast<V *>(data_ + offset); }
+    ~Workspace()
+    {
+        if (data_) cudaFreeAsync(data_, stream_);
+    }
+
+private:
+    char *data_ = nullptr;
+    size_t size_ = 0;
+    cudaStream_t stream_ = nullptr;
+};
+
+template <Kind KIND, int BN, bool MASK, typename T>
+cudaError_t launch_tower(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &g, const TowerArgs &args, int pairs, cudaStream_t stream)
+{
+    auto *kernel = tower_kernel<KIND, BN, MASK, T>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<KIND, BN>::kBytes);
+    if (e != cudaSuccess) return e;
+    kernel<<<2 * pairs, kThreads, Shape<KIND, BN>::kBytes, stream>>>(a, b, g, args);
+    return cudaGetLastError();
+}
+
+int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// Parts of the contraction: as many as make the pairs finish soonest, in units of one stage's products. A unit costs three
+// stages besides its own; parts cost a launch and the traffic of their sums.
+void plan_splits(Tiles &t, int pairs)
+{
+    const long long tiles = (long long)t.groups * t.m_tiles * t.n_tiles;
+    double best = 1e300;
+    int best_splits = 1;
+    for (int s = 1; s <= t.k_blocks && s <= 64; ++s) {
+        const int blocks = ceil_div(t.k_blocks, s);
+        if (ceil_div(t.k_blocks, blocks) != s) continue;
+        const double cost = (double)ceil_div(tiles * s, pairs) * (blocks + 3) + (s > 1 ? 6.0 + 0.25 * tiles * s / 74 * 4 : 0.0);
+        if (cost < best) best = cost, best_splits = s;
+    }
+    t.split_blocks = ceil_div(t.k_blocks, best_splits);
+    t.splits = best_splits;
+    t.units = tiles * t.splits;
+}
+
+struct Call {
+    const nbos_towers *in;
+    const int32_t *ids;
+    const float *teacher;
+    int64_t teacher_stride;
+    int32_t k;
+    float T;
+    int device, sms;
+    cudaStream_t stream;
+};
+
+int check(const nbos_towers *in, const int32_t *ids, const float *teacher, int64_t tstride, int32_t k, float T)
+{
+    if (!in) return fail(NBOS_ERR_INVALID_ARG, "towers is NULL");
+    if (in->dtype != NBOS_BF16 && in->dtype != NBOS_F16)
+        return fail(NBOS_ERR_INVALID_ARG, "vectors must be NBOS_BF16 or NBOS_F16 (got dtype %d)", in->dtype);
+    if (in->n_hosts < 1 || in->n_hosts > NBOS_MAX_HOSTS)
+        return fail(NBOS_ERR_INVALID_ARG, "n_hosts must be in 1..%d (got %d)", NBOS_MAX_HOSTS, in->n_hosts);
+    if (in->width < 1 || in->width > NBOS_POLICY_MAX_WIDTH)
+        return fail(NBOS_ERR_INVALID_ARG, "width must be in 1..%d (got %d)", NBOS_POLICY_MAX_WIDTH, in->width);
+    if (in->n_groups < 1 || in->n_groups > 65535) return fail(NBOS_ERR_INVALID_ARG, "n_groups must be in 1..65535 (got %d)", in->n_groups);
+    if (in->rows < 0 || in->rows > NBOS_POLICY_MAX_ROWS / in->n_groups)
+        return fail(NBOS_ERR_INVALID_ARG, "rows must be >= 0 and n_groups * rows below 2^31 (got %lld)", (long long)in->rows);
+    const int64_t far = (int64_t)1 << 38;
+    if (in->rows > 1 && (in->request_stride < in->width || in->request_stride > far))
+        return fail(NBOS_ERR_INVALID_ARG, "request_stride must be in width..2^38 (got %lld)", (long long)in->request_stride);
+    if (in->n_hosts > 1 && (in->host_stride < in->width || in->host_stride > far))
+        return fail(NBOS_ERR_INVALID_ARG, "host_stride must be in width..2^38 (got %lld)", (long long)in->host_stride);
+    if (in->n_groups > 1 && (in->request_group_stride < 0 || in->request_group_stride > far || in->host_group_stride < 0 || in->host_group_stride > far))
+        return fail(NBOS_ERR_INVALID_ARG, "group strides must be in 0..2^38");
+    if (in->rows > 0 && (!in->requests || !in->hosts)) return fail(NBOS_ERR_INVALID_ARG, "towers->requests / hosts is NULL");
+    if (!aligned_to(in->requests, 2) || !aligned_to(in->hosts, 2)) return fail(NBOS_ERR_INVALID_ARG, "vectors are not aligned to their element type");
+    if (!in->asks != !in->room) return fail(NBOS_ERR_INVALID_ARG, "asks and room come together");
+    if (!aligned_to(in->asks, 16) || !aligned_to(in->room, 16)) return fail(NBOS_ERR_INVALID_ARG, "asks / room must be 16-byte aligned");
+    const int rc = check_k(k);
+    if (rc) return rc;
+    if (!(T > 0.0f) || !isfinite(T) || !isfinite(kLog2e / T) || !isfinite(T * T))
+        return fail(NBOS_ERR_INVALID_ARG, "temperature must be finite and > 0 (as must 1 / T and T^2)");
+    if (tstride != 0 && (tstride < k || tstride > ((int64_t)1 << 40)))
+        return fail(NBOS_ERR_INVALID_ARG, "teacher_stride must be 0 or in k..2^40 (got %lld)", (long long)tstride);
+    if (in->rows > 0 && !ids) return fail(NBOS_ERR_INVALID_ARG, "hosts is NULL");
+    if (!aligned_to(ids, 4) || !aligned_to(teacher, 4)) return fail(NBOS_ERR_INVALID_ARG, "an int32 / float array is not 4-byte aligned");
+    return NBOS_OK;
+}
+
+// The two operands as the products read them; `offset`: where the workspace holds a copy that was laid out, else -1.
+struct Operand {
+    Table table;
+    const void *src;
+    long long src_stride, src_group_stride;
+    bool copied;
+    size_t offset;
+};
+Operand plan_operand(Workspace &ws, const void *data, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride, int width)
+{
+    Operand o;
+    const int wide = (width + 7) & ~7;
+    if (rows <= 1) stride = wide;
+    if (groups <= 1) group_stride = 0;
+    o.src = data, o.src_stride = stride, o.src_group_stride = group_stride;
+    o.table = Table{data, stride, group_stride, (int)groups, (int)rows, width};
+    o.copied = !readable(data, rows, stride, groups, group_stride);
+    o.offset = 0;
+    if (o.copied) {
+        const int slices = group_stride == 0 ? 1 : (int)groups;
+        o.offset = ws.add((size_t)slices * rows * wide * 2);
+        o.table.stride = wide, o.table.group_stride = group_stride == 0 ? 0 : (long long)rows * wide;
+    }
+    return o;
+}
+template <typename T>
+cudaError_t lay_out(const Workspace &ws, Operand &o, int sms, cudaStream_t stream)
+{
+    if (!o.copied) return cudaSuccess;
+    T *to = ws.at<T>(o.offset);
+    o.table.data = to;
+    const int slices = o.table.group_stride == 0 ? 1 : o.table.groups, wide = (int)o.table.stride;
+    const long long chunks = (long long)o.table.rows * (wide / 8), most = 8ll * sms;
+    const long long blocks = (chunks + 255) / 256 < most ? (chunks + 255) / 256 : most;
+    lay_out_kernel<T><<<dim3((unsigned int)blocks, slices), 256, 0, stream>>>(static_cast<const T *>(o.src), o.src_stride, o.src_group_stride,
+                                                                              o.table.rows, o.table.width, wide, to);
+    return cudaGetLastError();
+}
+
+template <typename T>
+int forward(const Call &c, float *out_loss, float *out_stats)
+{
+    const nbos_towers *in = c.in;
+    Workspace ws;
+    Operand a = plan_operand(ws, in->requests, in->rows, in->request_stride, in->n_groups, in->request_group_stride, in->width);
+    Operand b = plan_operand(ws, in->hosts, in->n_hosts, in->host_stride, in->n_groups, in->host_group_stride, in->width);
+    TowerArgs args = {};
+    args.t.groups = in->n_groups, args.t.m_tiles = ceil_div(in->rows, kTileM), args.t.n_tiles = ceil_div(in->n_hosts, kTileN);
+    args.t.k_blocks = args.t.split_blocks = ceil_div(in->width, kBlockK), args.t.splits = 1;
+    args.t.units = (long long)args.t.groups * args.t.m_tiles * args.t.n_tiles;
+    const int pairs = args.t.units < c.sms / 2 ? (int)args.t.units : c.sms / 2;
+    // a row's tiles lie with at most this many pairs, each of which leaves one part per half tile
+    args.slots = 2 * ((int)((args.t.n_tiles - 1) / (args.t.units / pairs)) + 2);
+    const size_t o_partial = ws.add(sizeof(float2) * args.slots * in->n_groups * in->rows);
+    int rc = ws.allocate(c.device, c.stream);
+    if (rc) return rc;
+    cudaError_t e = lay_out<T>(ws, a, c.sms, c.stream);
+    if (e == cudaSuccess) e = lay_out<T>(ws, b, c.sms, c.stream);
+    if (e != cudaSuccess) return cuda_fail(e, "towers: layout launch");
+    CUtensorMap map_a, map_b;
+    if ((rc = make_map(&map_a, a.table, 128, in->dtype)) || (rc = make_map(&map_b, b.table, 128, in->dtype))) return rc;
+    args.a_z = a.table.group_stride != 0, args.b_z = b.table.group_stride != 0;
+    args.rows = (int)in->rows, args.hosts = in->n_hosts, args.width = in->width, args.col_end = in->n_hosts;
+    args.asks = reinterpret_cast<const int4 *>(in->asks), args.room = reinterpret_cast<const int4 *>(in->room);
+    args.c = kLog2e / c.T;
+    args.partial = ws.at<float2>(o_partial);
+    e = in->asks ? launch_tower<STATS, kTileN, true, T>(map_a, map_b, map_a, args, pairs, c.stream)
+                 : launch_tower<STATS, kTileN, false, T>(map_a, map_b, map_a, args, pairs, c.stream);
+    if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
+    FinishArgs f = {};
+    f.a = a.table.data, f.b = b.table.data, f.a_stride = a.table.stride, f.a_group_stride = a.table.group_stride;
+    f.b_stride = b.table.stride, f.b_group_stride = b.table.group_stride;
+    f.groups = in->n_groups, f.rows = (int)in->rows, f.hosts = in->n_hosts, f.width = in->width, f.k = c.k, f.slots = args.slots, f.pairs = pairs;
+    f.m_tiles = args.t.m_tiles, f.n_tiles = args.t.n_tiles, f.units = args.t.units;
+    f.ids = c.ids, f.teacher = c.teacher, f.teacher_stride = c.teacher_stride, f.asks = args.asks, f.room = args.room;
+    f.T = c.T, f.c = args.c, f.partial = args.partial, f.loss = out_loss, f.stats = out_stats;
+    const long long rows = in->n_groups * in->rows;
+    // eight lanes a row where there is little to do for each; else a warp, its lanes split over the products
+    int lanes = 1;
+    while (lanes < 32 && lanes * 8 < in->width) lanes *= 2;
+    const unsigned int warp_blocks = (unsigned int)((rows + 7) / 8), eighth_blocks = (unsigned int)((rows + 31) / 32);
+    if (c.k > 4) {
+        while (lanes > 8 && 32 / lanes * 4 < c.k) lanes /= 2;
+        finish_kernel<T, 32, 4><<<warp_blocks, 256, 0, c.stream>>>(f, lanes);
+    } else if (in->width > 512) {
+        if (c.k == 1)
+            finish_kernel<T, 32, 1><<<warp_blocks, 256, 0, c.stream>>>(f, lanes);
+        else
+            finish_kernel<T, 32, 4><<<warp_blocks, 256, 0, c.stream>>>(f, lanes);
+    } else {
+        if (lanes > 8) lanes = 8;
+        if (c.k == 1)
+            finish_kernel<T, 8, 1><<<eighth_blocks, 256, 0, c.stream>>>(f, lanes);
+        else
+            finish_kernel<T, 8, 4><<<eighth_blocks, 256, 0, c.stream>>>(f, lanes);
+    }
+    e = cudaGetLastError();
+    return e == cudaSuccess ? NBOS_OK : cuda_fail(e, "towers: loss launch");
+}
+
+template <Kind KIND, typename T>
+cudaError_t launch_gradient(const CUtensorMap &a, const CUtensorMap &b, const TowerArgs &args, bool narrow, int pairs, cudaStream_t stream)
+{
+    const int p = args.t.units < pairs ? (int)args.t.units : pairs;
+    return narrow ? launch_tower<KIND, 128, false, T>(a, b, a, args, p, stream) : launch_tower<KIND, 256, false, T>(a, b, a, args, p, stream);
+}
+
+template <typename T>
+int backward(const Call &c, const float *stats, const float *grad_loss, float grad_scale, T *grad_a, long long a_stride, long long a_group_stride,
+             T *grad_b, long long b_stride, long long b_group_stride)
+{
+    const nbos_towers *in = c.in;
+    const int groups = in->n_groups, rows = (int)in->rows, hosts = in->n_hosts, width = in->width, pairs = c.sms / 2;
+    // Pieces of G: whole groups while they fit; of a group that does not, runs along its longer side, so that the gradient
+    // that has to be added up over the pieces is the smaller one.
+    const size_t group_bytes = (size_t)rows * ((hosts + 63) & ~63) * 2;
+    int piece_groups = 1, piece_rows = rows, piece_hosts = hosts;
+    if (group_bytes <= kPieceBytes) {
+        piece_groups = (int)(kPieceBytes / group_bytes);
+        if (piece_groups > groups) piece_groups = groups;
+    } else if (rows <= hosts) {
+        piece_hosts = (int)(kPieceBytes / 2 / rows) & ~(kTileN - 1);
+        if (piece_hosts < kTileN) piece_hosts = kTileN;
+    } else {
+        piece_rows = (int)(kPieceBytes / 2 / ((hosts + 63) & ~63)) & ~(kTileM - 1);
+        if (piece_rows < kTileM) piece_rows = kTileM;
+    }
+    const bool cut_rows = piece_rows < rows, cut_hosts = piece_hosts < hosts;
+    const int g_stride = (piece_hosts + 63) & ~63;
+    const bool narrow = width <= 128;
+    const int n_tiles = ceil_div(width, narrow ? 128 : 256);
+
+    auto tiles = [&](int gn, int m, int n, int kb) {
+        Tiles t = {gn, ceil_div(m, kTileM), n, kb, 1, kb, 0};
+        t.units = (long long)gn * t.m_tiles * n;
+        return t;
+    };
+    Tiles ta = tiles(piece_groups, piece_rows, n_tiles, ceil_div(piece_hosts, kBlockK));
+    Tiles tb = tiles(piece_groups, piece_hosts, n_tiles, ceil_div(piece_rows, kBlockK));
+    plan_splits(ta, pairs);
+    plan_splits(tb, pairs);
+    const bool sums_a = ta.splits > 1 || cut_hosts, sums_b = tb.splits > 1 || cut_rows;
+
+    Workspace ws;
+    Operand a = plan_operand(ws, in->requests, rows, in->request_stride, groups, in->request_group_stride, width);
+    Operand b = plan_operand(ws, in->hosts, hosts, in->host_stride, groups, in->host_group_stride, width);
+    const size_t o_g = ws.add((size_t)piece_groups * piece_rows * g_stride * 2);
+    const size_t o_a = ws.add(grad_a && sums_a ? sizeof(float) * ta.splits * piece_groups * piece_rows * width : 0);
+    const size_t o_b = ws.add(grad_b && sums_b ? sizeof(float) * tb.splits * piece_groups * piece_hosts * width : 0);
+    const size_t o_range = ws.add(16);
+    int rc = ws.allocate(c.device, c.stream);
+    if (rc) return rc;
+    cudaError_t e = lay_out<T>(ws, a, c.sms, c.stream);
+    if (e == cudaSuccess) e = lay_out<T>(ws, b, c.sms, c.stream);
+    const float scale = grad_scale * c.T;
+    float *range = nullptr;
+    if (in->dtype == NBOS_F16 && e == cudaSuccess) {
+        range = ws.at<float>(o_range);
+        unsigned int *largest = grad_loss ? reinterpret_cast<unsigned int *>(range + 2) : nullptr;
+        if (largest) {
+            e = cudaMemsetAsync(largest, 0, 4, c.stream);
+            const long long n = (long long)groups * rows, blocks = (n + 1023) / 1024;
+            if (e == cudaSuccess) largest_kernel<<<(unsigned int)(blocks < 2 * c.sms ? blocks : 2 * c.sms), 256, 0, c.stream>>>(grad_loss, n, largest);
+        }
+        if (e == cudaSuccess) range_kernel<<<1, 1, 0, c.stream>>>(largest, scale, range);
+        if (e == cudaSuccess) e = cudaGetLastError();
+    }
+    if (e != cudaSuccess) return cuda_fail(e, "towers: layout launch");
+
+    CUtensorMap a_rows, b_rows, a_cols, b_cols;   // boxes along the vectors, and across them
+    if ((rc = make_map(&a_rows, a.table, 128, in->dtype)) || (rc = make_map(&b_rows, b.table, 128, in->dtype)) ||
+        (rc = make_map(&a_cols, a.table, kBlockK, in->dtype)) || (rc = make_map(&b_cols, b.table, kBlockK, in->dtype)))
+        return rc;
+    const int az = a.table.group_stride != 0, bz = b.table.group_stride != 0;
+    T *g = ws.at<T>(o_g);
+
+    for (int g0 = 0; g0 < groups; g0 += piece_groups)
+        for (int r0 = 0; r0 < rows; r0 += piece_rows)
+            for (int h0 = 0; h0 < hosts; h0 += piece_hosts) {
+                const int gn = groups - g0 < piece_groups ? groups - g0 : piece_groups;
+                const int rn = rows - r0 < piece_rows ? rows - r0 : piece_rows, hn = hosts - h0 < piece_hosts ? hosts - h0 : piece_hosts;
+                const Table piece{g, g_stride, (long long)piece_rows * g_stride, gn, rn, hn};
+                CUtensorMap g_rows, g_cols;
+                if ((rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype))) return rc;
+
+                TowerArgs p = {};
+                p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK));
+                p.a_z = az, p.a_z0 = g0 * az, p.b_z = bz, p.b_z0 = g0 * bz, p.a_m0 = r0, p.b_n0 = h0;
+                p.group0 = g0, p.row0 = r0, p.rows = rows, p.hosts = hosts, p.width = width, p.col0 = h0, p.col_end = hn, p.m_rows = rn;
+                p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
+                p.c = kLog2e / c.T, p.stats = stats, p.stats_stride = 2 + c.k, p.grad_loss = grad_loss, p.grad_scale = scale, p.range = range;
+                const int used = p.t.units < pairs ? (int)p.t.units : pairs;
+                e = in->asks ? launch_tower<GRAD, kTileN, true, T>(a_rows, b_rows, g_rows, p, used, c.stream)
+                             : launch_tower<GRAD, kTileN, false, T>(a_rows, b_rows, g_rows, p, used, c.stream);
+                if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
+
+                PatchArgs q = {};
+                q.groups = gn, q.group0 = g0, q.row0 = r0, q.rows_here = rn, q.rows = rows, q.host0 = h0, q.hosts_here = hn, q.hosts = hosts, q.k = c.k;
+                q.ids = c.ids, q.teacher = c.teacher, q.teacher_stride = c.teacher_stride, q.stats = stats, q.grad_loss = grad_loss, q.range = range;
+                q.grad_scale = scale, q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
+                int lanes = 1;
+                while (lanes < 32 && lanes < c.k) lanes *= 2;
+                patch_kernel<T><<<(unsigned int)(((long long)gn * rn * lanes + 255) / 256), 256, 0, c.stream>>>(q, lanes);
+                if ((e = cudaGetLastError()) != cudaSuccess) return cuda_fail(e, "towers: teacher launch");
+
+                if (grad_a) {
+                    TowerArgs d = {};
+                    d.t = ta, d.t.groups = gn, d.t.m_tiles = ceil_div(rn, kTileM), d.t.k_blocks = ceil_div(hn, kBlockK);
+                    d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
+                    d.a_z = 1, d.b_z = bz, d.b_z0 = g0 * bz, d.b_k0 = h0;
+                    d.group0 = g0, d.width = width, d.range = range, d.m_rows = rn, d.out_row0 = r0;
+                    d.out = grad_a, d.out_stride = a_stride, d.out_group_stride = a_group_stride;
+                    d.sums = sums_a ? ws.at<float>(o_a) : nullptr, d.add = h0 > 0;
+                    e = launch_gradient<GRAD_REQUESTS, T>(g_rows, b_cols, d, narrow, pairs, c.stream);
+                    if (e == cudaSuccess && sums_a && h0 + hn == hosts) {
+                        const long long n = (long long)gn * rn * width, blocks = (n + 1023) / 1024;
+                        sums_kernel<T><<<(unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms), 256, 0, c.stream>>>(
+                            d.sums, ta.splits, gn, rn, width, range, grad_a + g0 * a_group_stride + r0 * a_stride, a_stride, a_group_stride);
+                        e = cudaGetLastError();
+                    }
+                    if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
+                }
+                if (grad_b) {
+                    TowerArgs d = {};
+                    d.t = tb, d.t.groups = gn, d.t.m_tiles = ceil_div(hn, kTileM), d.t.k_blocks = ceil_div(rn, kBlockK);
+                    d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
+                    d.a_z = 1, d.b_z = az, d.b_z0 = g0 * az, d.b_k0 = r0;
+                    d.group0 = g0, d.width = width, d.range = range, d.m_rows = hn, d.out_row0 = h0;
+                    d.out = grad_b, d.out_stride = b_stride, d.out_group_stride = b_group_stride;
+                    d.sums = sums_b ? ws.at<float>(o_b) : nullptr, d.add = r0 > 0;
+                    e = launch_gradient<GRAD_HOSTS, T>(g_cols, a_cols, d, narrow, pairs, c.stream);
+                    if (e == cudaSuccess && sums_b && r0 + rn == rows) {
+                        const long long n = (long long)gn * hn * width, blocks = (n + 1023) / 1024;
+                        sums_kernel<T><<<(unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms), 256, 0, c.stream>>>(
+                            d.sums, tb.splits, gn, hn, width, range, grad_b + g0 * b_group_stride + h0 * b_stride, b_stride, b_group_stride);
+                        e = cudaGetLastError();
+                    }
+                    if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
+                }
+            }
+    return NBOS_OK;
+}
+
+int check_gradient(const char *what, const void *data, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride, int width)
+{
+    if (!data) return NBOS_OK;
+    const int64_t far = (int64_t)1 << 38;
+    if (!aligned_to(data, 2)) return fail(NBOS_ERR_INVALID_ARG, "%s is not aligned to its element type", what);
+    if (rows > 1 && (stride < width || stride > far)) return fail(NBOS_ERR_INVALID_ARG, "%s: the row stride must be in width..2^38", what);
+    if (groups > 1 && (group_stride < (rows > 0 ? (rows - 1) * (rows > 1 ? stride : 0) + width : 0) || group_stride > far))
+        return fail(NBOS_ERR_INVALID_ARG, "%s: groups must not overlap", what);
+    return NBOS_OK;
+}
+
+}  // namespace
+}  // namespace nbos
+
+using namespace nbos;
+using namespace nbos::policy;
+
+extern "C" int nbos_policy_towers(const nbos_towers *towers, const int32_t *hosts, const float *teacher_logits, int64_t teacher_stride,
+                                  int32_t k, float temperature, float *out_loss, float *out_stats, void *cuda_stream)
+{
+    int rc = check(towers, hosts, teacher_logits, teacher_stride, k, temperature);
+    if (rc || towers->rows == 0) return rc;
+    if (!out_loss && !out_stats) return fail(NBOS_ERR_INVALID_ARG, "no output asked for");
+    if (!aligned_to(out_loss, 4) || !aligned_to(out_stats, 4)) return fail(NBOS_ERR_INVALID_ARG, "an int32 / float array is not 4-byte aligned");
+    Call c{towers, hosts, teacher_logits, teacher_stride, k, temperature, 0, 0, static_cast<cudaStream_t>(cuda_stream)};
+    if ((rc = check_sm100(&c.sms, &c.device))) return rc;
+    return towers->dtype == NBOS_BF16 ? forward<__nv_bfloat16>(c, out_loss, out_stats) : forward<__half>(c, out_loss, out_stats);
+}
+
+extern "C" int nbos_policy_towers_backward(const nbos_towers *towers, const int32_t *hosts, const float *teacher_logits,
+                                           int64_t teacher_stride, int32_t k, float temperature, const float *stats,
+                                           const float *grad_loss, float grad_scale, void *out_grad_requests,
+                                           int64_t grad_request_stride, int64_t grad_request_group_stride, void *out_grad_hosts,
+                                           int64_t grad_host_stride, int64_t grad_host_group_stride, void *cuda_stream)
+{
+    int rc = check(towers, hosts, teacher_logits, teacher_stride, k, temperature);
+    if (rc) return rc;
+    const int64_t rows = towers->rows, groups = towers->n_groups;
+    if (rows > 0 && !stats) return fail(NBOS_ERR_INVALID_ARG, "stats is NULL");
+    if (!out_grad_requests && !out_grad_hosts) return rows > 0 ? fail(NBOS_ERR_INVALID_ARG, "no output asked for") : NBOS_OK;
+    if (!aligned_to(stats, 4) || !aligned_to(grad_loss, 4)) return fail(NBOS_ERR_INVALID_ARG, "an int32 / float array is not 4-byte aligned");
+    if ((rc = check_gradient("out_grad_requests", out_grad_requests, rows, grad_request_stride, groups, grad_request_group_stride, towers->width)) ||
+        (rc = check_gradient("out_grad_hosts", out_grad_hosts, towers->n_hosts, grad_host_stride, groups, grad_host_group_stride, towers->width)))
+        return rc;
+    Call c{towers, hosts, teacher_logits, teacher_stride, k, temperature, 0, 0, static_cast<cudaStream_t>(cuda_stream)};
+    if ((rc = check_sm100(&c.sms, &c.device))) return rc;
+    if (rows == 0) {   // no request pulls at a host
+        for (int64_t g = 0; out_grad_hosts && g < groups; ++g) {
+            zero_kernel<<<c.sms, 256, 0, c.stream>>>(static_cast<__half *>(out_grad_hosts) + g * grad_host_group_stride, towers->n_hosts,
+                                                     towers->width, towers->n_hosts > 1 ? (long long)grad_host_stride : 0ll);
+            NBOS_CUDA_TRY(cudaGetLastError());
+        }
+        return NBOS_OK;
+    }
+    auto run = [&](auto zero) {
+        using T = decltype(zero);
+        return backward<T>(c, stats, grad_loss, grad_scale, static_cast<T *>(out_grad_requests), grad_request_stride, grad_request_group_stride,
+                           static_cast<T *>(out_grad_hosts), grad_host_stride, grad_host_group_stride);
+    };
+    return towers->dtype == NBOS_BF16 ? run(__nv_bfloat16()) : run(__half());
+}
+
+extern "C" int nbos_policy_towers_status(void *cuda_stream)
+{
+    int sms = 0, device = 0;
+    const int rc = check_sm100(&sms, &device);
+    if (rc) return rc;
+    unsigned int word = 0, zero = 0;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    NBOS_CUDA_TRY(cudaMemcpyFromSymbolAsync(&word, tower_status, sizeof(word), 0, cudaMemcpyDeviceToHost, stream));
+    NBOS_CUDA_TRY(cudaStreamSynchronize(stream));
+    if (!word) return NBOS_OK;
+    NBOS_CUDA_TRY(cudaMemcpyToSymbolAsync(tower_status, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, stream));
+    NBOS_CUDA_TRY(cudaStreamSynchronize(stream));
+    return fail(NBOS_ERR_DEVICE_TIMEOUT, "a two-tower kernel gave up on a bounded wait; its outputs are undefined");
+}

@@ -54,6 +54,28 @@ class _BalanceLoss(torch.autograd.Function):
         return grad, None
 
 
+class _TowerDistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, requests, host_vectors, hosts, teacher_logits, temperature, asks, room):
+        rows = requests.shape[:-1]
+        loss = torch.empty(rows, dtype=torch.float32, device=requests.device)
+        stats = torch.empty((*rows, 2 + hosts.shape[-1]), dtype=torch.float32, device=requests.device)
+        binding.nbos_policy_towers(requests, host_vectors, hosts, teacher_logits, loss, stats, temperature=temperature, asks=asks, room=room)
+        ctx.save_for_backward(requests, host_vectors, hosts, teacher_logits, asks, room, stats)
+        ctx.temperature = temperature
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        requests, host_vectors, hosts, teacher_logits, asks, room, stats = ctx.saved_tensors
+        grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None
+                 for t, need in zip((requests, host_vectors), ctx.needs_input_grad)]
+        binding.nbos_policy_towers_backward(requests, host_vectors, hosts, teacher_logits, stats, *grads,
+                                            grad_loss=grad_loss.float().contiguous(), temperature=ctx.temperature, asks=asks, room=room)
+        return (*grads, None, None, None, None, None)
+
+
 def distill_loss(logits, hosts, teacher_logits=None, temperature: float = 1.0) -> torch.Tensor:
     """Loss per row [...] of logits [..., H] against the teacher's hosts [..., k] (int32, -1 = none; what
     nbos_place_batch writes can be passed as it is) with logits [..., k], [k] or None (all equal). The gradient is that of
@@ -61,6 +83,15 @@ def distill_loss(logits, hosts, teacher_logits=None, temperature: float = 1.0) -
     if torch.is_grad_enabled() and isinstance(teacher_logits, torch.Tensor) and teacher_logits.requires_grad:
         raise ValueError("teacher_logits has no gradient here: detach it")
     return _DistillLoss.apply(logits, hosts, teacher_logits, float(temperature))
+
+
+def tower_distill_loss(requests, host_vectors, hosts, teacher_logits=None, temperature: float = 1.0, asks=None, room=None) -> torch.Tensor:
+    """distill_loss of a two-tower policy's logits, requests [N, B, D] times host_vectors [N, H, D] (or without N; bfloat16 or
+    float16), -inf where the request's asks [N, B, 4] exceed the host's room [N, H, 4] (int32; None: all fit). The table of
+    logits [N, B, H] is never stored, neither for the loss [N, B] nor for the gradients of both vectors."""
+    if torch.is_grad_enabled() and isinstance(teacher_logits, torch.Tensor) and teacher_logits.requires_grad:
+        raise ValueError("teacher_logits has no gradient here: detach it")
+    return _TowerDistillLoss.apply(requests, host_vectors, hosts, teacher_logits, float(temperature), asks, room)
 
 
 def balance_loss(logits, hosts):
