@@ -569,6 +569,27 @@ int nbos_policy_towers_backward(const nbos_towers *towers, const int32_t *hosts,
                                 int64_t grad_host_stride, int64_t grad_host_group_stride, void *cuda_stream);
 int nbos_policy_towers_status(void *cuda_stream);
 
+/*
+ * The global norm over many tensors (the gradients of a policy), and clipping by it:
+ *     norm = (sum over all values of x^2)^(1/2) [NBOS_NORM_2] or max |x| [NBOS_NORM_INF]
+ *     out  = x * min(1, max_norm / (norm + 1e-6)), rounded once to the tensor's type
+ * Squares are summed in 32 bits within 64 values of a thread, where that neither overflows nor loses small values, and in 64 bits
+ * beyond and otherwise; the sums do not change from run to run. (A norm beyond 32 bits is written as infinity, and
+ * clips by its true value.) A NaN makes the norm and every output NaN; an infinity makes
+ * the norm infinite, finite values 0 and itself NaN (as the formula says). No tensors, or none with values: norm 0.
+ *   data, numel, dtype  HOST arrays [n_tensors]: DEVICE address (aligned to its type), number of values (0 .. 2^40, contiguous) and
+ *                       NBOS_* type of each tensor; types may be mixed
+ *   out                 HOST array [n_tensors] of DEVICE addresses, or NULL: the norm alone. An output may be its own input (nothing is
+ *                       written then when there is nothing to clip); it must not overlap any tensor otherwise.
+ *   max_norm            >= 0; infinity clips nothing
+ *   out_norm            DEVICE float or NULL
+ * The host arrays have been read when the call returns. Asynchronous on `cuda_stream`.
+ */
+#define NBOS_NORM_2 0
+#define NBOS_NORM_INF 1
+int nbos_policy_clip(const void *const *data, void *const *out, const int64_t *numel, const int32_t *dtype,
+                     int32_t n_tensors, float max_norm, int32_t norm_kind, float *out_norm, void *cuda_stream);
+
 /* Synchronises `cuda_stream` and returns the sticky device status of this snapshot: NBOS_OK, or
  * NBOS_ERR_DEVICE_TIMEOUT if some kernel gave up on a bounded wait (its outputs are then
  * undefined), NBOS_ERR_RANGE / NBOS_ERR_STALE_LAYOUT after an nbos_snapshot_update whose new state

@@ -119,3 +119,18 @@ def sample_hosts(logits, uniforms, temperature=None, top_k=None, top_p=None, min
                                top_k=per_row(top_k, torch.int32), top_p=per_row(top_p, torch.float32),
                                min_p=per_row(min_p, torch.float32))
     return hosts, found
+
+
+def clip_gradients(parameters, max_norm: float, norm_type: float = 2.0) -> torch.Tensor:
+    """Scales the gradients of `parameters` in place by min(1, max_norm / (norm + 1e-6)), norm their global 2-norm (or, norm_type
+    inf, their largest magnitude), and returns the norm, a scalar on the device. Parameters without a gradient are passed
+    over. Nothing waits for the device."""
+    kinds = {2.0: binding.NBOS_NORM_2, float("inf"): binding.NBOS_NORM_INF}
+    if norm_type not in kinds:
+        raise ValueError("norm_type must be 2 or inf")
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
+    grads = [p.grad for p in parameters if p.grad is not None]
+    device = grads[0].device if grads else parameters[0].device if parameters else "cuda"
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    binding.nbos_policy_clip(grads, max_norm, norm, grads, norm_kind=kinds[norm_type])
+    return norm
