@@ -570,6 +570,45 @@ int nbos_policy_towers_backward(const nbos_towers *towers, const int32_t *hosts,
 int nbos_policy_towers_status(void *cuda_stream);
 
 /*
+ * The norms around a residual block of a policy's tower: after its branch, with a gate, onto the scaled residual, and before the
+ * next block, in one pass. Row by row, with norm(v) = v / sqrt(mean(v^2) + eps):
+ *     r = residual_scale * residual + gate * (norm(branch) * post_weight)        out_residual
+ *     h = norm(r) * pre_weight                                                   out_normed
+ * h is of the unrounded r; everything is in 32 bits (whose squares overflow beyond 1.8e19) and rounded once.
+ *   residual, branch   DEVICE [rows], row_stride >= width apart, aligned to their type; tables whose rows all start on 16-byte
+ *                      boundaries are the fastest
+ *   gate               DEVICE or NULL (1): row r uses gate row r / rows_per_gate: 1 = a gate for each row, rows per group = one for
+ *                      each group, rows = one for all. rows must be a multiple.
+ *   post_weight, pre_weight  DEVICE [width] or NULL (1)
+ *   gate_dtype, weight_dtype  dtype or NBOS_F32 each; gradients have the same
+ *   out_residual, out_normed  DEVICE, dtype, or NULL; may be residual or branch themselves (same stride), must not overlap any input
+ *                      otherwise
+ *   out_stats          DEVICE [rows * 2] float or NULL: 1 / sqrt(mean + eps) of both norms, for the backward call
+ * Backward: grad_residual is what arrives at out_residual, grad_normed at out_normed (either may be NULL: 0). Any of the outputs may
+ * be NULL. out_grad_residual and out_grad_branch may be grad_residual or grad_normed themselves (same stride). Gradients of weights
+ * and of shared gates are sums over rows in 32 bits, in an order that does not change from run to run.
+ */
+#define NBOS_BLOCK_MAX_WIDTH 16384
+typedef struct nbos_block {
+    const void *residual, *branch, *gate, *post_weight, *pre_weight;
+    int64_t residual_stride, branch_stride, gate_stride; /* elements */
+    int64_t rows;          /* 0 .. NBOS_POLICY_MAX_ROWS */
+    int64_t rows_per_gate; /* >= 1 where there is a gate */
+    int32_t width;         /* 1 .. NBOS_BLOCK_MAX_WIDTH */
+    int32_t dtype, gate_dtype, weight_dtype;
+    float residual_scale;  /* finite       */
+    float eps;             /* finite, >= 0 */
+} nbos_block;
+
+int nbos_policy_block_norm(const nbos_block *block, void *out_residual, int64_t out_residual_stride, void *out_normed,
+                           int64_t out_normed_stride, float *out_stats, void *cuda_stream);
+int nbos_policy_block_norm_backward(const nbos_block *block, const float *stats, const void *grad_residual,
+                                    int64_t grad_residual_stride, const void *grad_normed, int64_t grad_normed_stride,
+                                    void *out_grad_residual, int64_t out_grad_residual_stride, void *out_grad_branch,
+                                    int64_t out_grad_branch_stride, void *out_grad_gate, int64_t out_grad_gate_stride,
+                                    void *out_grad_post, void *out_grad_pre, void *cuda_stream);
+
+/*
  * The global norm over many tensors (the gradients of a policy), and clipping by it:
  *     norm = (sum over all values of x^2)^(1/2) [NBOS_NORM_2] or max |x| [NBOS_NORM_INF]
  *     out  = x * min(1, max_norm / (norm + 1e-6)), rounded once to the tensor's type

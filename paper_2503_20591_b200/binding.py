@@ -44,6 +44,7 @@ NBOS_POLICY_MAX_ROWS = 2147483647
 NBOS_POLICY_MAX_K = 256
 NBOS_POLICY_MAX_DRAWS = 8
 NBOS_POLICY_MAX_WIDTH = 65536
+NBOS_BLOCK_MAX_WIDTH = 16384
 NBOS_NORM_2 = 0
 NBOS_NORM_INF = 1
 
@@ -61,7 +62,7 @@ EXPORTED_SYMBOLS = (
     "nbos_cluster_sums", "nbos_scale_out_deficit", "nbos_place_batch_sequential",
     "nbos_policy_distill", "nbos_policy_distill_backward", "nbos_policy_balance", "nbos_policy_balance_backward",
     "nbos_policy_sample", "nbos_policy_towers", "nbos_policy_towers_backward", "nbos_policy_towers_status",
-    "nbos_policy_clip",
+    "nbos_policy_block_norm", "nbos_policy_block_norm_backward", "nbos_policy_clip",
     "nbos_snapshot_status", "nbos_strerror", "nbos_last_error_detail",
     "nbos_probe_int32_issue", "nbos_probe_wait_timeout", "nbos_probe_wait_timeout_on_snapshot",
 )
@@ -121,6 +122,17 @@ class nbos_towers(ctypes.Structure):
     ]
 
 
+class nbos_block(ctypes.Structure):
+    _fields_ = [
+        ("residual", ctypes.c_void_p), ("branch", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+        ("post_weight", ctypes.c_void_p), ("pre_weight", ctypes.c_void_p),
+        ("residual_stride", ctypes.c_int64), ("branch_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64),
+        ("rows", ctypes.c_int64), ("rows_per_gate", ctypes.c_int64),
+        ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("gate_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+        ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float),
+    ]
+
+
 class nbos_launch_config(ctypes.Structure):
     _fields_ = [
         ("lanes_per_request", ctypes.c_int32), ("requests_per_lane", ctypes.c_int32),
@@ -177,6 +189,8 @@ def load_library() -> ctypes.CDLL:
     lib.nbos_policy_towers.argtypes = [P(nbos_towers), vp, vp, i64, i32, f32, vp, vp, vp]
     lib.nbos_policy_towers_backward.argtypes = [P(nbos_towers), vp, vp, i64, i32, f32, vp, vp, f32, vp, i64, i64, vp, i64, i64, vp]
     lib.nbos_policy_towers_status.argtypes = [vp]
+    lib.nbos_policy_block_norm.argtypes = [P(nbos_block), vp, i64, vp, i64, vp, vp]
+    lib.nbos_policy_block_norm_backward.argtypes = [P(nbos_block), vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp]
     lib.nbos_policy_clip.argtypes = [vp, vp, vp, vp, i32, f32, i32, vp, vp]
     lib.nbos_snapshot_status.argtypes = [vp, vp]
     lib.nbos_strerror.argtypes = [ctypes.c_int]
@@ -757,6 +771,104 @@ def nbos_policy_towers_backward(requests, host_vectors, hosts, teacher_logits, s
 def nbos_policy_towers_status(stream=None) -> int:
     """Synchronises the stream; NBOS_ERR_DEVICE_TIMEOUT, once, if a wait in a two-tower kernel on the current device ran out."""
     return load_library().nbos_policy_towers_status(_stream_ptr(stream))
+
+
+# ---- the norms around a residual block -------------------------------------------------
+def _like(t, like, what: str):
+    """(address, row stride) of a table like `like`, or (0, 0)."""
+    if t is None:
+        return 0, 0
+    if t is not like and (not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device):
+        raise ValueError(f"{what} must have the residual's shape, type and device")
+    if t.is_contiguous():
+        return t.data_ptr(), t.shape[-1]
+    return t.data_ptr(), _table(t, what)[1]
+
+
+def _weight(t, what: str, residual):
+    """Address of weights [width] of the residual's type or float32, or 0."""
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor) or (t.dtype is not torch.float32 and t.dtype is not residual.dtype):
+        raise TypeError(f"{what} must have the residual's type or float32")
+    return _dense(t, what, t.dtype, residual.shape[-1], residual.device)
+
+
+def _gate(gate, residual, rows: int, what: str = "gate"):
+    """(address, row stride, rows per gate row) of a gate [..., D] that stands for the residual's rows: its leading sizes are the
+    residual's, then ones ([N, 1, D] with [N, B, D]: a gate for each n), or it is [D]."""
+    if not isinstance(gate, torch.Tensor) or (gate.dtype is not torch.float32 and gate.dtype is not residual.dtype):
+        raise TypeError(f"{what} must have the residual's type or float32")
+    if gate.device != residual.device:
+        raise ValueError(f"{what} must live on {residual.device}, not {gate.device}")
+    lead, own = residual.shape[:-1], gate.shape[:-1]
+    if gate.shape[-1:] != residual.shape[-1:] or (own and len(own) != len(lead)):
+        raise ValueError(f"{what} must be [D], or have the residual's shape with ones for the last of its leading sizes")
+    if not own:
+        if gate.shape[0] > 1 and gate.stride(0) != 1:
+            raise ValueError(f"{what} must be contiguous")
+        return gate.data_ptr(), 0, max(rows, 1)
+    same = 0
+    while same < len(lead) and own[same] == lead[same]:
+        same += 1
+    if any(n != 1 for n in own[same:]):
+        raise ValueError(f"{what} must be [D], or have the residual's shape with ones for the last of its leading sizes")
+    shared = 1
+    for n in lead[same:]:
+        shared *= n
+    return gate.data_ptr(), _table(gate, what)[1], max(shared, 1)
+
+
+def _block(residual, branch, gate, post_weight, pre_weight, residual_scale, eps) -> nbos_block:
+    rows, stride, width = _table(residual, "residual")
+    at, branch_stride = _like(branch, residual, "branch")
+    if branch is None:
+        raise ValueError("branch is None")
+    dtype = _POLICY_DTYPES[residual.dtype]
+    gate_at, gate_stride, per_gate = (0, 0, 1) if gate is None else _gate(gate, residual, rows)
+    post, pre = _weight(post_weight, "post_weight", residual), _weight(pre_weight, "pre_weight", residual)
+    weight = post_weight if pre_weight is None else pre_weight
+    if post_weight is not None and post_weight.dtype is not weight.dtype:
+        raise TypeError("post_weight and pre_weight must have one type")
+    return nbos_block(residual.data_ptr(), at, gate_at, post, pre, stride, branch_stride, gate_stride, rows, per_gate, width, dtype,
+                      dtype if gate is None else _POLICY_DTYPES[gate.dtype], dtype if weight is None else _POLICY_DTYPES[weight.dtype], residual_scale, eps)
+
+
+def nbos_policy_block_norm(residual, branch, gate, post_weight, pre_weight, out_residual, out_normed=None, out_stats=None,
+                           residual_scale=1.0, eps=1e-6, stream=None) -> None:
+    """out_residual = residual_scale * residual + gate * norm(branch) * post_weight, out_normed = norm(out_residual) * pre_weight. Device
+    tensors: residual and branch [..., D] (float32, bfloat16, float16; rows evenly apart), gate like them, [N, 1, D] beside [N, B, D],
+    [D] or None, weights [D] or None (gate and weights of the same type or float32); outputs like residual or None (residual and
+    branch themselves will do), out_stats [..., 2] float32 or None. Asynchronous on the stream."""
+    desc = _block(residual, branch, gate, post_weight, pre_weight, residual_scale, eps)
+    device = residual.device
+    _check(load_library().nbos_policy_block_norm(
+        ctypes.byref(desc), *_like(out_residual, residual, "out_residual"), *_like(out_normed, residual, "out_normed"),
+        _dense(out_stats, "out_stats", torch.float32, 2 * desc.rows, device), _policy_stream(stream, device)))
+
+
+def nbos_policy_block_norm_backward(residual, branch, gate, post_weight, pre_weight, stats, grad_residual, grad_normed,
+                                    out_grad_residual=None, out_grad_branch=None, out_grad_gate=None, out_grad_post=None, out_grad_pre=None,
+                                    residual_scale=1.0, stream=None) -> None:
+    """The gradients of nbos_policy_block_norm from the statistics it saved (out_stats) and what arrives at its two outputs (either may
+    be None); each output like its input, or None."""
+    desc = _block(residual, branch, gate, post_weight, pre_weight, residual_scale, 0.0)
+    device = residual.device
+    gate_at = gate_stride = 0
+    if out_grad_gate is not None:
+        if gate is None or out_grad_gate.shape != gate.shape or out_grad_gate.dtype != gate.dtype:
+            raise ValueError("out_grad_gate must have the gate's shape and type")
+        gate_at, gate_stride, _ = _gate(out_grad_gate, residual, desc.rows, "out_grad_gate")
+        if desc.rows == 0:
+            out_grad_gate.zero_()   # its rows have none to add up; the library does not know how many they are
+    for got, weight, what in ((out_grad_post, post_weight, "out_grad_post"), (out_grad_pre, pre_weight, "out_grad_pre")):
+        if got is not None and (weight is None or got.dtype != weight.dtype):
+            raise ValueError(f"{what} must have its weight's type")
+    _check(load_library().nbos_policy_block_norm_backward(
+        ctypes.byref(desc), _dense(stats, "stats", torch.float32, 2 * desc.rows, device), *_like(grad_residual, residual, "grad_residual"),
+        *_like(grad_normed, residual, "grad_normed"), *_like(out_grad_residual, residual, "out_grad_residual"),
+        *_like(out_grad_branch, residual, "out_grad_branch"), gate_at, gate_stride, _weight(out_grad_post, "out_grad_post", residual),
+        _weight(out_grad_pre, "out_grad_pre", residual), _policy_stream(stream, device)))
 
 
 # ---- clipping by the global norm ------------------------------------------------------------

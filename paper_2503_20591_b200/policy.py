@@ -76,6 +76,29 @@ class _TowerDistillLoss(torch.autograd.Function):
         return (*grads, None, None, None, None, None)
 
 
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, residual, branch, gate, post_weight, pre_weight, residual_scale, eps):
+        ctx.set_materialize_grads(False)
+        out, normed = (torch.empty(residual.shape, dtype=residual.dtype, device=residual.device) for _ in range(2))
+        stats = torch.empty((*residual.shape[:-1], 2), dtype=torch.float32, device=residual.device)
+        binding.nbos_policy_block_norm(residual, branch, gate, post_weight, pre_weight, out, normed, stats, residual_scale, eps)
+        ctx.save_for_backward(residual, branch, gate, post_weight, pre_weight, stats)
+        ctx.residual_scale = residual_scale
+        return out, normed
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out, grad_normed):
+        *inputs, stats = ctx.saved_tensors
+        grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None for t, need in zip(inputs, ctx.needs_input_grad)]
+        if grad_out is None and grad_normed is None:
+            return (*(None if g is None else g.zero_() for g in grads), None, None)
+        rows_alike = [None if g is None else g.contiguous() for g in (grad_out, grad_normed)]
+        binding.nbos_policy_block_norm_backward(*inputs, stats, *rows_alike, *grads, residual_scale=ctx.residual_scale)
+        return (*grads, None, None)
+
+
 def distill_loss(logits, hosts, teacher_logits=None, temperature: float = 1.0) -> torch.Tensor:
     """Loss per row [...] of logits [..., H] against the teacher's hosts [..., k] (int32, -1 = none; what
     nbos_place_batch writes can be passed as it is) with logits [..., k], [k] or None (all equal). The gradient is that of
@@ -119,6 +142,13 @@ def sample_hosts(logits, uniforms, temperature=None, top_k=None, top_p=None, min
                                top_k=per_row(top_k, torch.int32), top_p=per_row(top_p, torch.float32),
                                min_p=per_row(min_p, torch.float32))
     return hosts, found
+
+
+def block_norm(residual, branch, gate=None, post_weight=None, pre_weight=None, residual_scale: float = 1.0, eps: float = 1e-6):
+    """(r, h) with r = residual_scale * residual + gate * norm(branch) * post_weight, the stream behind a residual block, and
+    h = norm(r) * pre_weight, what the next block reads; norm(v) = v / sqrt(mean(v^2) + eps) over the last dimension. residual, branch
+    [..., D]; gate like them, [N, 1, D] beside [N, B, D], or [D]; weights [D]."""
+    return _BlockNorm.apply(residual, branch, gate, post_weight, pre_weight, float(residual_scale), float(eps))
 
 
 def clip_gradients(parameters, max_norm: float, norm_type: float = 2.0) -> torch.Tensor:
