@@ -25,8 +25,7 @@ __global__ void __maxnreg__((kForwardRegs<WIDE>)) forward_kernel(const __grid_co
         if (!Ring::kStaged) return;
         if (first < end) {
             const unsigned int row = (unsigned int)(first + mine < end ? first + mine : first);
-            Ring::copy(staged, 2 * stage, of(a.y, a.y_stride, row), c);
-            Ring::copy(staged, 2 * stage + 1, of(a.x, a.x_stride, row), c);
+            Ring::copy(staged, 2 * stage, of(a.y, a.y_stride, row), of(a.x, a.x_stride, row), c);
         }
         copies_commit();
     };

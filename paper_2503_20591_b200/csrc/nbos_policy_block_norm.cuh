@@ -170,12 +170,12 @@ __device__ __forceinline__ float row_sum(float v, int team, float4 (*warps)[8], 
 
 // Rows to come, copied ahead into shared memory: each thread copies the pieces that it will read itself, so no barrier is needed, and
 // reads them again in each pass over the row rather than keep them. (Loads into registers: 8 x 8,192 x 2,048 bf16 forward
-// 316 us, backward 651; staged, with 8 values a thread, 256 and 511; this FIXME.) Values of 16 bits that do not lie on 4-byte
-// boundaries cannot be copied like that, and rows beyond 8,192 values do not fit: they come from memory and then from the L1 cache.
+// 316 us, backward 651; staged, with 8 values a thread, 256 and 511; with 16 values, 217 and 545, and then as below.) Single values of 16 bits cannot be
+// copied like that: they are loaded and put there. Rows beyond 8,192 values do not fit: they come from memory and then from the L1 cache.
 template <typename T, int VEC, int CH, bool WIDE>
 struct Ahead {
     static constexpr int kPiece = VEC * (int)sizeof(T);
-    static constexpr bool kStaged = kPiece >= 4 && !WIDE;
+    static constexpr bool kStaged = !WIDE;
     static constexpr int kRowBytes = kStaged ? CH * kPiece : 0;   // a thread's, per table
 
     // Two rows where a thread's pieces are 16 bytes and there is room for two blocks, else one: more rows take shared memory from more
@@ -201,14 +201,36 @@ struct Ahead {
                 char *at = shared + (n * (int)blockDim.x + (int)threadIdx.x) * kPiece;
                 if constexpr (kPiece == 16)
                     *reinterpret_cast<uint4 *>(at) = make_uint4(0, 0, 0, 0);
-                else
+                else if constexpr (kPiece == 4)
                     *reinterpret_cast<unsigned int *>(at) = 0u;
+                else
+                    *reinterpret_cast<unsigned short *>(at) = 0;
             }
         }
     }
-    static __device__ __forceinline__ void copy(char *shared, int table, const T *row, const Columns &c)
+    // two tables' rows at a time (either may be NULL)
+    static __device__ __forceinline__ void copy(char *shared, int table, const T *row, const T *row2, const Columns &c)
     {
-        if constexpr (kStaged) {
+        if constexpr (kStaged && kPiece == 2) {   // single values: loaded, all under way together, and put there
+            unsigned short v[2][CH];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const T *from = (n == 0 ? row : row2);
+#pragma unroll
+                for (int k = 0; k < CH; ++k) v[n][k] = from && c.is_whole(k) ? reinterpret_cast<const unsigned short *>(from)[k * c.team + c.t] : (unsigned short)0;
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int k = 0; k < CH; ++k) *reinterpret_cast<unsigned short *>(shared + slot(table + n, k)) = v[n][k];
+        } else {
+            if (row) copy_one(shared, table, row, c);
+            if (row2) copy_one(shared, table + 1, row2, c);
+        }
+    }
+    static __device__ __forceinline__ void copy_one(char *shared, int table, const T *row, const Columns &c)
+    {
+        if constexpr (kStaged && kPiece >= 4) {
             const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(shared + slot(table, 0)));
             const T *from = row + c.t * VEC;
 #pragma unroll
@@ -285,7 +307,7 @@ enum Gate { NO_GATE, SHARED_GATE, ROW_GATE };
 
 // Registers: what leaves room for enough threads to keep the memory busy. Weights are not among them: they lie in shared memory as
 // 32-bit floats, those of the branch's norm multiplied by the gate that the block's rows share. (Taken from the L1 cache row by row:
-// 8 x 8,192 x 2,048 bf16 forward 191 us, backward 414; this FIXME.)
+// 8 x 8,192 x 2,048 bf16 forward 191 us, backward 414; this 188 and 312.)
 template <bool WIDE> constexpr int kForwardRegs = 64;
 template <bool WIDE> constexpr int kBackwardRegs = WIDE ? 64 : 112;
 

@@ -64,10 +64,8 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
         if (!Ring::kStaged) return;
         if (first < end) {
             const unsigned int row = (unsigned int)(first + mine < end ? first + mine : first);
-            Ring::copy(staged, 4 * stage, of(a.y, a.y_stride, row), c);
-            Ring::copy(staged, 4 * stage + 1, of(a.x, a.x_stride, row), c);
-            if (a.dh) Ring::copy(staged, 4 * stage + 2, of(a.dh, a.dh_stride, row), c);
-            if (a.dr) Ring::copy(staged, 4 * stage + 3, of(a.dr, a.dr_stride, row), c);
+            Ring::copy(staged, 4 * stage, of(a.y, a.y_stride, row), of(a.x, a.x_stride, row), c);
+            Ring::copy(staged, 4 * stage + 2, a.dh ? of(a.dh, a.dh_stride, row) : nullptr, a.dr ? of(a.dr, a.dr_stride, row) : nullptr, c);
         }
         copies_commit();
     };
@@ -260,7 +258,7 @@ template <typename T, Gate GATE>
 cudaError_t run_backward(const BlockArgs &args, Shape s, int sms, ColumnArgs &c, cudaMemPool_t pool, cudaStream_t stream)
 {
     // 32-bit rows of nearly 8,192 values with a shared gate: too much for shared memory, so not staged
-    if (s.block && s.vec * (int)sizeof(T) >= 4 && s.team * 16 * (4 * (int)sizeof(T) + 8) + args.width * 4 > kMostShared) s.wide = true;
+    if (s.block && s.team * 16 * (4 * (int)sizeof(T) + 8) + args.width * 4 > kMostShared) s.wide = true;
     return by_shape<T>(s, [&](auto vec, auto chunks, auto block, auto wide) -> cudaError_t {
         auto *kernel = backward_kernel<T, vec(), chunks(), block(), wide(), GATE>;
         static const int regs = kernel_registers(kernel);
