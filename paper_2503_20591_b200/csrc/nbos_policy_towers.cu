@@ -20,7 +20,8 @@ using namespace tensor;
 constexpr int kTileM = 256;           // rows of a pair's tile; each of its two blocks has 128 of them
 constexpr int kTileN = 256;           // columns; narrower tiles of 128 for gradients of at most 128 columns
 constexpr int kBlockK = 64;           // values of the contraction per stage: one 128-byte row
-constexpr int kEpilogue = 256;        // threads that read the products: 8 warps, two a quarter of the tensor memory
+constexpr int kParts = 4;             // a tile's columns are read in this many parts, each by four warps (32 rows a warp)
+constexpr int kEpilogue = 128 * kParts;
 constexpr int kThreads = kEpilogue + 64;   // and a warp that copies, a warp that multiplies
 constexpr int kTmemColumns = 512;     // two tiles of 32-bit products
 constexpr size_t kPieceBytes = 256u << 20;
@@ -70,35 +71,43 @@ __device__ __host__ __forceinline__ int pair_of(long long units, int pairs, long
 struct Unit {
     int g, m, n, split, k0, k1;       // k0 .. k1: blocks of the contraction
 };
+// Every thread that has a part in a unit goes through the same schedule, so its steps are 32-bit ones: STATS counts on from where the
+// pair starts, the others (fewer than 2^31 units) divide.
 template <Kind KIND>
 struct Schedule {
-    long long at, end, step;
+    unsigned int left, at, step;
+    int n, m, g;   // STATS: the next unit's
     __device__ __forceinline__ Schedule(const Tiles &t, int pair, int pairs)
     {
-        if (KIND == STATS)
-            at = first_unit(t.units, pairs, pair), end = first_unit(t.units, pairs, pair + 1), step = 1;
-        else
-            at = pair, end = t.units, step = pairs;
+        if (KIND == STATS) {
+            const long long from = first_unit(t.units, pairs, pair), rest = from / t.n_tiles;
+            left = (unsigned int)(first_unit(t.units, pairs, pair + 1) - from);
+            n = (int)(from % t.n_tiles), m = (int)(rest % t.m_tiles), g = (int)(rest / t.m_tiles);
+        } else {
+            left = (unsigned int)t.units > (unsigned int)pair ? ((unsigned int)t.units - pair + pairs - 1) / pairs : 0;
+            at = pair, step = pairs;
+        }
     }
     __device__ __forceinline__ bool next(const Tiles &t, Unit &u)
     {
-        if (at >= end) return false;
+        if (left == 0) return false;
+        --left;
         if (KIND == STATS) {
-            u.n = (int)(at % t.n_tiles);
-            const long long rest = at / t.n_tiles;
-            u.m = (int)(rest % t.m_tiles), u.g = (int)(rest / t.m_tiles);
-            u.split = 0;
+            u.n = n, u.m = m, u.g = g, u.split = 0;
+            if (++n == t.n_tiles) {
+                n = 0;
+                if (++m == t.m_tiles) m = 0, ++g;
+            }
         } else {
             // bands of 8 tiles along M, so that tiles in flight at one time share both operands
-            const long long per_split = (long long)t.m_tiles * t.n_tiles, part = at / per_split;
-            const int in = (int)(at % per_split), band = in / (8 * t.n_tiles), high = min(8, t.m_tiles - 8 * band);
-            const int rest = in - band * 8 * t.n_tiles;
-            u.m = 8 * band + rest % high, u.n = rest / high;
+            const unsigned int per_split = (unsigned int)t.m_tiles * t.n_tiles, part = at / per_split, in = at % per_split;
+            const unsigned int band = in / (8u * t.n_tiles), high = min(8u, t.m_tiles - 8 * band), rest = in - band * 8 * t.n_tiles;
+            u.m = (int)(8 * band + rest % high), u.n = (int)(rest / high);
             u.split = (int)(part % t.splits), u.g = (int)(part / t.splits);
+            at += step;
         }
         u.k0 = u.split * t.split_blocks;
         u.k1 = min(t.k_blocks, u.k0 + t.split_blocks);
-        at += step;
         return true;
     }
 };
@@ -107,7 +116,7 @@ template <Kind KIND, int BN>
 struct Shape {
     static constexpr bool kAlongKA = KIND != GRAD_HOSTS, kAlongKB = KIND == STATS || KIND == GRAD;
     static constexpr int kBytesA = 128 * kBlockK * 2, kBytesB = BN / 2 * kBlockK * 2, kStageBytes = kBytesA + kBytesB;
-    static constexpr int kStaging = KIND == GRAD ? 4 * 128 * 128 : 0;    // G on its way out: four boxes of 128 rows x 64 columns
+    static constexpr int kStaging = KIND == GRAD ? 4 * 128 * 128 : 0;    // G on its way out: a box of 32 rows x 64 columns a warp
     static constexpr int kRoom = KIND == STATS || KIND == GRAD ? 2 * kTileN * 16 : 0;
     static constexpr int kStages = KIND == GRAD ? 4 : 6;
     static constexpr int kBytes = kStages * kStageBytes + kStaging + kRoom + 256 /* barriers */ + 1024 /* alignment */;
@@ -139,20 +148,46 @@ __device__ __forceinline__ uint32_t if_fits(uint32_t v, const int4 &ask, const i
     return out;
 }
 
-// 64 products of one row become logits: -inf where the request does not fit and behind the last host
-template <bool MASK>
-__device__ __forceinline__ void mask64(uint32_t (&u)[32], uint32_t (&v)[32], const int4 *room, const int4 &ask, int left)
+// 64 products of one row become logits: -inf behind the last host
+__device__ __forceinline__ void cut64(uint32_t (&u)[32], uint32_t (&v)[32], int left)
 {
-    const uint32_t none = 0xFF800000u;
-    if (MASK) {
+    if (left < 64) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) u[i] = if_fits(u[i], ask, room[i]);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = if_fits(v[i], ask, room[32 + i]);
-    } else if (left < 64) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) u[i] = i < left ? u[i] : none, v[i] = 32 + i < left ? v[i] : none;
+        for (int i = 0; i < 32; ++i) u[i] = i < left ? u[i] : 0xFF800000u, v[i] = 32 + i < left ? v[i] : 0xFF800000u;
     }
+}
+// With capacities a thread has 8 of 32 columns of four rows (v[0]: rows t / 4 and t / 4 + 8, v[1]: 16 further) rather than 64 of one row: it
+// reads a host's room once for four requests. `room`: of column 2 (t % 4).
+__device__ __forceinline__ void mask_rows(uint32_t (&v)[2][16], const int4 *room, const int4 (&ask)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int4 has = room[8 * j + e];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r / 2][4 * j + 2 * (r % 2) + e] = if_fits(v[r / 2][4 * j + 2 * (r % 2) + e], ask[r], has);
+        }
+}
+// running (m, s) of row r of the four over 8 more logits
+__device__ __forceinline__ void add8(float &m, float &s, const uint32_t (&v)[2][16], int r, float c)
+{
+    auto at = [&](int j, int e) { return __uint_as_float(v[r / 2][4 * j + 2 * (r % 2) + e]); };
+    float top[2] = {m, m};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top[j % 2] = fmaxf(top[j % 2], fmaxf(at(j, 0), at(j, 1)));
+    const float to = fmaxf(top[0], top[1]);
+    const float base = (to == neg_inf() ? 0.0f : to) * -c;
+    s *= exp2_fast(fmaf(m, c, base));
+    m = to;
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float e0, e1;
+        fma2_to(e0, e1, at(j, 0), at(j, 1), c, base);
+        add2(sum[0], sum[1], exp2_fast(e0), exp2_fast(e1));
+    }
+    s += sum[0] + sum[1];
 }
 
 // running (m, s) of a row over 64 more logits
@@ -191,7 +226,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __half)
 }
 
 // One launch covers its units with pairs of blocks, each a persistent pair: one thread a block copies operand tiles
-// into a ring of stages, one thread of the pair multiplies them into one of two accumulators in tensor memory, eight warps a
+// into a ring of stages, one thread of the pair multiplies them into one of two accumulators in tensor memory, 16 warps a
 // block read the other. No wait is without a limit: when one runs out the block's flag goes up, copies and products stop, the
 // readers go through the rest of their units without waiting (so that their barriers stay matched), and the status
 // word says that the outputs are undefined.
@@ -307,17 +342,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
         }
         __syncwarp();
-    } else {   // ---- reading the products: a row a thread, half of the tile's columns a warp
+    } else {   // ---- reading the products: a quarter of the tile's columns a warp
         Schedule<KIND> todo(t, pair, pairs);
-        const int half = warp / 4, row_in = (warp % 4) * 32 + lane;
-        const uint32_t lane_at = tmem + ((uint32_t)(warp % 4 * 32) << 16) + half * (BN / 2);
+        const int quarter = warp / 4, row_in = (warp % 4) * 32 + lane;
+        const uint32_t lane_at = tmem + ((uint32_t)(warp % 4 * 32) << 16) + quarter * (BN / kParts);
         const uint32_t freed = peer_addr(tmem_empty, 0);
         int buffer = 0, last_g = -1, last_m = -1, parity = 0;
         uint32_t buffer_phase = 0;
-        int4 ask = make_int4(0, 0, 0, 0);
-        // STATS: the row's statistics so far; GRAD: -(m c + log2 S) and the factor of p
-        float run_m = neg_inf(), run_s = 0.0f, minus = 0.0f, factor = 0.0f;
-        bool dead = false, some_dead = false;
+        // a row a thread, or four (see mask_rows); row i of them
+        constexpr int ROWS = MASK ? 4 : 1;
+        auto row_at = [&](int i) { return MASK ? warp % 4 * 32 + lane / 4 + 8 * i : row_in; };
+        int4 ask[ROWS];
+        // STATS: the rows' statistics so far; GRAD: -(m c + log2 S) and the factor of p
+        float run_m[ROWS], run_s[ROWS], minus[ROWS], factor[ROWS];
+        bool dead[ROWS], some_dead = false;
         int slot = 0;
         auto release = [&] {
             fence_before();
@@ -325,104 +363,145 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (lane == 0) arrive_at(freed + 8 * buffer);
         };
         auto flush = [&] {
-            const int row = last_m * kTileM + (int)rank * 128 + row_in;
-            if (last_m < 0 || row >= args.rows) return;
-            if (MASK && never_fits(ask)) run_m = neg_inf(), run_s = 0.0f;
-            args.partial[((long long)last_g * args.rows + row) * args.slots + 2 * slot + half] = make_float2(run_m, run_s);
+            if (last_m < 0) return;
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (MASK) {   // four lanes have a row
+#pragma unroll
+                    for (int off = 1; off < 4; off *= 2) {
+                        const float m = __shfl_xor_sync(kFull, run_m[i], off), s = __shfl_xor_sync(kFull, run_s[i], off);
+                        const float to = fmaxf(run_m[i], m), base = to == neg_inf() ? 0.0f : to;
+                        run_s[i] = run_s[i] * exp2_fast((run_m[i] - base) * args.c) + s * exp2_fast((m - base) * args.c);
+                        run_m[i] = to;
+                    }
+                    if (lane % 4 != i) continue;
+                    if (never_fits(ask[i])) run_m[i] = neg_inf(), run_s[i] = 0.0f;
+                }
+                const int row = last_m * kTileM + (int)rank * 128 + row_at(i);
+                if (row < args.rows)
+                    args.partial[((long long)last_g * args.rows + row) * args.slots + kParts * slot + quarter] = make_float2(run_m[i], run_s[i]);
+            }
         };
         while (todo.next(t, u)) {
             const int local = u.m * kTileM + (int)rank * 128 + row_in;   // row of the launch
             if (KIND == STATS || KIND == GRAD) {
                 if (u.g != last_g || u.m != last_m) {
-                    const int row = args.row0 + local;
-                    const bool inside = row < args.rows;
-                    const long long at = (long long)(args.group0 + u.g) * args.rows + row;
                     if (KIND == STATS) {
                         flush();
-                        run_m = neg_inf(), run_s = 0.0f;
                         slot = pair - pair_of(t.units, pairs, ((long long)u.g * t.m_tiles + u.m) * t.n_tiles);
-                    } else if (inside) {
-                        const float m = args.stats[at * args.stats_stride], s = args.stats[at * args.stats_stride + 1];
-                        dead = s == __int_as_float(0x7F800000);
-                        minus = -fmaf(m, args.c, log2f(s));
-                        factor = args.grad_scale * (args.grad_loss ? args.grad_loss[at] : 1.0f) * (args.range ? args.range[0] : 1.0f);
-                    } else {
-                        dead = true;
                     }
-                    if (KIND == GRAD) some_dead = __any_sync(kFull, dead);
-                    if (MASK) ask = inside ? args.asks[at] : make_int4(0, 0, 0, 0);
+                    some_dead = false;
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i) {
+                        const int row = args.row0 + u.m * kTileM + (int)rank * 128 + row_at(i);
+                        const bool inside = row < args.rows;
+                        const long long at = (long long)(args.group0 + u.g) * args.rows + row;
+                        run_m[i] = neg_inf(), run_s[i] = minus[i] = factor[i] = 0.0f;
+                        dead[i] = true;
+                        if (KIND == GRAD && inside) {
+                            const float m = args.stats[at * args.stats_stride], s = args.stats[at * args.stats_stride + 1];
+                            dead[i] = s == __int_as_float(0x7F800000);
+                            minus[i] = -fmaf(m, args.c, log2f(s));
+                            factor[i] = args.grad_scale * (args.grad_loss ? args.grad_loss[at] : 1.0f) * (args.range ? args.range[0] : 1.0f);
+                        }
+                        ask[i] = MASK && inside ? args.asks[at] : make_int4(0, 0, 0, 0);
+                        some_dead |= dead[i];
+                    }
+                    some_dead = __any_sync(kFull, some_dead);
                     last_g = u.g, last_m = u.m;
                 }
                 const int4 *columns = room + parity * kTileN;
                 if (MASK) {
                     const int n = u.n * BN + (int)threadIdx.x;
-                    room[parity * kTileN + threadIdx.x] =
-                        n < args.col_end ? args.room[(long long)(args.group0 + u.g) * args.hosts + args.col0 + n] : make_int4(-1, -1, -1, -1);
+                    if (threadIdx.x < kTileN)
+                        room[parity * kTileN + threadIdx.x] = n < args.col_end ? args.room[(long long)(args.group0 + u.g) * args.hosts + args.col0 + n] : make_int4(-1, -1, -1, -1);
                     bar_sync(1, kEpilogue);
-                    columns += half * (BN / 2);
+                    columns += quarter * (BN / kParts) + 2 * (lane % 4);
                     parity ^= 1;
                 }
                 wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
                 fence_after();
+                const uint32_t at = lane_at + buffer * kTileN;
+                const int n0 = u.n * BN + quarter * 64;
+                const uint32_t box = staging + warp * 32 * 128;   // the warp's own, 32 rows
+                if (KIND == GRAD) {
+                    if (lane == 0) stores_read_wait<0>();         // the tile before has left it
+                    __syncwarp();
+                }
+                // p f of two columns in one word
+                auto word = [&](uint32_t x0, uint32_t x1, int r) {
+                    float e0, e1;
+                    fma2_to(e0, e1, __uint_as_float(x0), __uint_as_float(x1), args.c, minus[r]);
+                    e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+                    mul2(e0, e1, factor[r], factor[r]);
+                    const uint32_t w = pack2(e0, e1, T());
+                    return some_dead && dead[r] ? 0u : w;
+                };
+                if constexpr (MASK) {
 #pragma unroll 1
-                for (int sub = 0; sub < 2; ++sub) {
-                    uint32_t v0[32], v1[32];
-                    const uint32_t at = lane_at + buffer * kTileN + 64 * sub;
-                    tmem_load32(v0, at);
-                    tmem_load32(v1, at + 32);
-                    tmem_wait(v0);
-                    tmem_wait(v1);
-                    if (sub == 1) release();
-                    const int n0 = u.n * BN + half * (BN / 2) + 64 * sub;
-                    mask64<MASK>(v0, v1, columns + 64 * sub, ask, args.col_end - n0);
+                    for (int sub = 0; sub < 2; ++sub) {
+                        uint32_t v[2][16];
+                        tmem_load16(v[0], at + 32 * sub), tmem_load16(v[1], at + 32 * sub + (16u << 16));
+                        tmem_wait(v[0]);
+                        tmem_wait(v[1]);
+                        if (sub == 1) release();
+                        mask_rows(v, columns + 32 * sub, ask);
+                        if constexpr (KIND == STATS) {
+#pragma unroll
+                            for (int i = 0; i < ROWS; ++i) add8(run_m[i], run_s[i], v, i, args.c);
+                        } else {   // 16-byte piece 4 sub + j of a line, four lanes a word each
+#pragma unroll
+                            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const int line = row_at(i) % 32, x = 4 * j + 2 * (i % 2);
+                                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(box + line * 128 + (((4 * sub + j) ^ (line & 7)) << 4) + lane % 4 * 4),
+                                                 "r"(word(v[i / 2][x], v[i / 2][x + 1], i))
+                                                 : "memory");
+                                }
+                        }
+                    }
+                } else {
+                    uint32_t v[2][32];
+                    tmem_load32(v[0], at), tmem_load32(v[1], at + 32);
+                    tmem_wait(v[0]);
+                    tmem_wait(v[1]);
+                    release();
+                    cut64(v[0], v[1], args.col_end - n0);
                     if constexpr (KIND == STATS) {
-                        add64(run_m, run_s, v0, v1, args.c);
+                        add64(run_m[0], run_s[0], v[0], v[1], args.c);
                     } else {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float e0, e1, f0, f1;
-                        fma2_to(e0, e1, __uint_as_float(v0[i]), __uint_as_float(v0[i + 1]), args.c, minus);
-                        fma2_to(f0, f1, __uint_as_float(v1[i]), __uint_as_float(v1[i + 1]), args.c, minus);
-                        e0 = exp2_fast(e0), e1 = exp2_fast(e1), f0 = exp2_fast(f0), f1 = exp2_fast(f1);
-                        mul2(e0, e1, factor, factor);
-                        mul2(f0, f1, factor, factor);
-                        v0[i / 2] = pack2(e0, e1, T()), v1[i / 2] = pack2(f0, f1, T());
+                        for (int j = 0; j < 8; ++j) {
+                            const uint32_t(&x)[32] = v[j / 4];
+                            const int k = 8 * (j % 4);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)),
+                                         "r"(word(x[k], x[k + 1], 0)), "r"(word(x[k + 2], x[k + 3], 0)), "r"(word(x[k + 4], x[k + 5], 0)),
+                                         "r"(word(x[k + 6], x[k + 7], 0))
+                                         : "memory");
+                        }
                     }
-                    if (some_dead && dead) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v0[i] = v1[i] = 0u;
-                    }
-                    const uint32_t box = staging + (2 * half + sub) * 128 * 128, line = box + row_in * 128;
-                    if (threadIdx.x % 128 == 0) stores_read_wait<1>();   // the store of two boxes ago has left this one
-                    bar_sync(2 + half, 128);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t(&w)[32] = j < 4 ? v0 : v1;
-                        const int k = 4 * (j % 4);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((j ^ (row_in & 7)) << 4)), "r"(w[k]),
-                                     "r"(w[k + 1]), "r"(w[k + 2]), "r"(w[k + 3])
-                                     : "memory");
-                    }
+                }
+                if (KIND == GRAD) {
                     async_proxy_fence();
-                    bar_sync(2 + half, 128);
-                    if (threadIdx.x % 128 == 0) {
-                        const int y = u.m * kTileM + (int)rank * 128;
+                    __syncwarp();
+                    if (lane == 0) {
+                        const int y = u.m * kTileM + (int)rank * 128 + warp % 4 * 32;
                         if (n0 < args.col_end && y < args.m_rows) store_box(&map_g, n0, y, u.g, box);
                         stores_commit();
-                    }
                     }
                 }
             } else {
                 wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
                 fence_after();
                 const float undo = args.range ? args.range[1] : 1.0f;
-                const int n_first = u.n * BN + half * (BN / 2);
+                const int n_first = u.n * BN + quarter * (BN / kParts);
 #pragma unroll 1
-                for (int sub = 0; sub < BN / 64; ++sub) {
+                for (int sub = 0; sub < BN / kParts / 32; ++sub) {
                     uint32_t v[32];
                     tmem_load32(v, lane_at + buffer * kTileN + 32 * sub);
                     tmem_wait(v);
-                    if (sub == BN / 64 - 1) release();
+                    if (sub == BN / kParts / 32 - 1) release();
                     if (u.k0 >= u.k1) {   // a part behind the end of a shorter piece
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = 0u;
@@ -470,7 +549,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (buffer == 0) buffer_phase ^= 1;
         }
         if (KIND == STATS) flush();
-        if (KIND == GRAD && threadIdx.x % 128 == 0) stores_drain();
+        if (KIND == GRAD && lane == 0) stores_drain();
     }
 
     fence_before();
@@ -590,7 +669,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
 
     const int4 ask = f.asks ? f.asks[at] : make_int4(0, 0, 0, 0);
     const long long first = ((long long)g * f.m_tiles + row / kTileM) * f.n_tiles;
-    const int parts = 2 * (pair_at(f, first + f.n_tiles - 1) - pair_at(f, first) + 1);
+    const int parts = kParts * (pair_at(f, first + f.n_tiles - 1) - pair_at(f, first) + 1);
     float m = neg_inf(), s = 0.0f;
     for (int i = lane; i < parts; i += TEAM) {
         const float2 p = f.partial[at * f.slots + i];
@@ -960,8 +1039,8 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     args.t.k_blocks = args.t.split_blocks = ceil_div(in->width, kBlockK), args.t.splits = 1;
     args.t.units = (long long)args.t.groups * args.t.m_tiles * args.t.n_tiles;
     const int pairs = args.t.units < c.sms / 2 ? (int)args.t.units : c.sms / 2;
-    // a row's tiles lie with at most this many pairs, each of which leaves one part per half tile
-    args.slots = 2 * ((int)((args.t.n_tiles - 1) / (args.t.units / pairs)) + 2);
+    // a row's tiles lie with at most this many pairs, each of which leaves kParts parts
+    args.slots = kParts * ((int)((args.t.n_tiles - 1) / (args.t.units / pairs)) + 2);
     const size_t o_partial = ws.add(sizeof(float2) * args.slots * in->n_groups * in->rows);
     int rc = ws.allocate(c.device, c.stream);
     if (rc) return rc;
@@ -1091,8 +1170,9 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 const int gn = groups - g0 < piece_groups ? groups - g0 : piece_groups;
                 const int rn = rows - r0 < piece_rows ? rows - r0 : piece_rows, hn = hosts - h0 < piece_hosts ? hosts - h0 : piece_hosts;
                 const Table piece{g, g_stride, (long long)piece_rows * g_stride, gn, rn, hn};
-                CUtensorMap g_rows, g_cols;
-                if ((rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype))) return rc;
+                CUtensorMap g_out, g_rows, g_cols;   // written, and read along rows and across them
+                if ((rc = make_map(&g_out, piece, 32, in->dtype)) || (rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype)))
+                    return rc;
 
                 TowerArgs p = {};
                 p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK));
@@ -1101,8 +1181,8 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
                 p.c = kLog2e / c.T, p.stats = stats, p.stats_stride = 2 + c.k, p.grad_loss = grad_loss, p.grad_scale = scale, p.range = range;
                 const int used = p.t.units < pairs ? (int)p.t.units : pairs;
-                e = in->asks ? launch_tower<GRAD, kTileN, true, T>(a_rows, b_rows, g_rows, p, used, c.stream)
-                             : launch_tower<GRAD, kTileN, false, T>(a_rows, b_rows, g_rows, p, used, c.stream);
+                e = in->asks ? launch_tower<GRAD, kTileN, true, T>(a_rows, b_rows, g_out, p, used, c.stream)
+                             : launch_tower<GRAD, kTileN, false, T>(a_rows, b_rows, g_out, p, used, c.stream);
                 if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
 
                 PatchArgs q = {};
