@@ -24,7 +24,7 @@ constexpr int kParts = 4;             // a tile's columns are read in this many 
 constexpr int kEpilogue = 128 * kParts;
 constexpr int kThreads = kEpilogue + 64;   // and a warp that copies, a warp that multiplies
 constexpr int kTmemColumns = 512;     // two tiles of 32-bit products
-constexpr size_t kPieceBytes = 256u << 20;
+constexpr size_t kPieceBytes = 512u << 20;   // 65,536 x 4,096 at width 256, gradients: 48 MB 950 us, 128 MB 650, 256 MB 586, 512 MB 567: launches fill the GPU
 
 enum Kind { STATS, GRAD, GRAD_REQUESTS, GRAD_HOSTS };
 
@@ -137,7 +137,8 @@ __device__ __forceinline__ bool fits(const int4 &ask, const int4 &room)
 }
 __device__ __forceinline__ bool never_fits(const int4 &ask) { return (ask.x | ask.y | ask.z | ask.w) < 0; }
 
-// v where the request fits, else -inf: four compares that hand on one predicate (&& became branches: forward of 65,536 x 4,096 hosts at width 256 494 us, this 239)
+// v where the request fits, else -inf: four compares that hand on one predicate (&& became branches: forward of 65,536 x 4,096 hosts at
+// width 256 494 us, this 239 then). The integer compares are what bounds the kernels with capacities now.
 __device__ __forceinline__ uint32_t if_fits(uint32_t v, const int4 &ask, const int4 &room)
 {
     uint32_t out;
@@ -414,7 +415,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 if (MASK) {
                     const int n = u.n * BN + (int)threadIdx.x;
                     if (threadIdx.x < kTileN)
-                        room[parity * kTileN + threadIdx.x] = n < args.col_end ? args.room[(long long)(args.group0 + u.g) * args.hosts + args.col0 + n] : make_int4(-1, -1, -1, -1);
+                        room[parity * kTileN + threadIdx.x] =
+                            n < args.col_end ? args.room[(long long)(args.group0 + u.g) * args.hosts + args.col0 + n] : make_int4(-1, -1, -1, -1);
                     bar_sync(1, kEpilogue);
                     columns += quarter * (BN / kParts) + 2 * (lane % 4);
                     parity ^= 1;
@@ -429,13 +431,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     __syncwarp();
                 }
                 // p f of two columns in one word
-                auto word = [&](uint32_t x0, uint32_t x1, int r) {
+                auto word = [&](uint32_t x0, uint32_t x1, float from, float by, bool none) {
                     float e0, e1;
-                    fma2_to(e0, e1, __uint_as_float(x0), __uint_as_float(x1), args.c, minus[r]);
+                    fma2_to(e0, e1, __uint_as_float(x0), __uint_as_float(x1), args.c, from);
                     e0 = exp2_fast(e0), e1 = exp2_fast(e1);
-                    mul2(e0, e1, factor[r], factor[r]);
+                    mul2(e0, e1, by, by);
                     const uint32_t w = pack2(e0, e1, T());
-                    return some_dead && dead[r] ? 0u : w;
+                    return some_dead && none ? 0u : w;
                 };
                 if constexpr (MASK) {
 #pragma unroll 1
@@ -456,7 +458,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                                 for (int j = 0; j < 4; ++j) {
                                     const int line = row_at(i) % 32, x = 4 * j + 2 * (i % 2);
                                     asm volatile("st.shared.b32 [%0], %1;" ::"r"(box + line * 128 + (((4 * sub + j) ^ (line & 7)) << 4) + lane % 4 * 4),
-                                                 "r"(word(v[i / 2][x], v[i / 2][x + 1], i))
+                                                 "r"(word(v[i / 2][x], v[i / 2][x + 1], minus[i], factor[i], dead[i]))
                                                  : "memory");
                                 }
                         }
@@ -476,8 +478,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             const uint32_t(&x)[32] = v[j / 4];
                             const int k = 8 * (j % 4);
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)),
-                                         "r"(word(x[k], x[k + 1], 0)), "r"(word(x[k + 2], x[k + 3], 0)), "r"(word(x[k + 4], x[k + 5], 0)),
-                                         "r"(word(x[k + 6], x[k + 7], 0))
+                                         "r"(word(x[k], x[k + 1], minus[0], factor[0], dead[0])), "r"(word(x[k + 2], x[k + 3], minus[0], factor[0], dead[0])), "r"(word(x[k + 4], x[k + 5], minus[0], factor[0], dead[0])),
+                                         "r"(word(x[k + 6], x[k + 7], minus[0], factor[0], dead[0]))
                                          : "memory");
                         }
                     }
@@ -925,8 +927,8 @@ cudaError_t launch_tower(const CUtensorMap &a, const CUtensorMap &b, const CUten
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Parts of the contraction: as many as make the pairs finish soonest, in units of one stage's products. A unit costs three
-// stages besides its own; parts cost a launch and the traffic of their sums.
+// Parts of the contraction: as many as make the pairs finish soonest, in units of one stage's products of a pair (0.4 us). A unit
+// costs three stages besides its own; parts cost a launch and their sums, 256 KB a tile written and read.
 void plan_splits(Tiles &t, int pairs)
 {
     const long long tiles = (long long)t.groups * t.m_tiles * t.n_tiles;
@@ -935,7 +937,7 @@ void plan_splits(Tiles &t, int pairs)
     for (int s = 1; s <= t.k_blocks && s <= 64; ++s) {
         const int blocks = ceil_div(t.k_blocks, s);
         if (ceil_div(t.k_blocks, blocks) != s) continue;
-        const double cost = (double)ceil_div(tiles * s, pairs) * (blocks + 3) + (s > 1 ? 6.0 + 0.25 * tiles * s / 74 * 4 : 0.0);
+        const double cost = (double)ceil_div(tiles * s, pairs) * (blocks + 3) + (s > 1 ? 6.0 + 0.2 * tiles * s : 0.0);
         if (cost < best) best = cost, best_splits = s;
     }
     t.split_blocks = ceil_div(t.k_blocks, best_splits);
@@ -1105,15 +1107,17 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
     // that has to be added up over the pieces is the smaller one.
     const size_t group_bytes = (size_t)rows * ((hosts + 63) & ~63) * 2;
     int piece_groups = 1, piece_rows = rows, piece_hosts = hosts;
+    auto even = [&](int n, int tile) {   // whole tiles, pieces of much the same size
+        const int pieces = (int)((group_bytes + kPieceBytes - 1) / kPieceBytes), size = ceil_div(ceil_div(n, pieces), tile) * tile;
+        return size < n ? size : n;
+    };
     if (group_bytes <= kPieceBytes) {
         piece_groups = (int)(kPieceBytes / group_bytes);
         if (piece_groups > groups) piece_groups = groups;
     } else if (rows <= hosts) {
-        piece_hosts = (int)(kPieceBytes / 2 / rows) & ~(kTileN - 1);
-        if (piece_hosts < kTileN) piece_hosts = kTileN;
+        piece_hosts = even(hosts, kTileN);
     } else {
-        piece_rows = (int)(kPieceBytes / 2 / ((hosts + 63) & ~63)) & ~(kTileM - 1);
-        if (piece_rows < kTileM) piece_rows = kTileM;
+        piece_rows = even(rows, kTileM);
     }
     const bool cut_rows = piece_rows < rows, cut_hosts = piece_hosts < hosts;
     const int g_stride = (piece_hosts + 63) & ~63;

@@ -167,10 +167,10 @@ def test_matches_the_formula(nb, groups, rows, hosts, width, mask, dtype):
         check(nb, c, T, 8.0 if dtype == "float16" else 1.0 / rows, gl)
 
 
-@pytest.mark.parametrize("groups,rows,hosts,width,what", [(1, 2051, 70001, 72, "runs of hosts"), (1, 70003, 2051, 72, "runs of rows"),
-                                                           (3, 1500, 40001, 64, "a group at a time, each with the next")])
+@pytest.mark.parametrize("groups,rows,hosts,width,what", [(1, 4099, 70001, 72, "runs of hosts"), (1, 70003, 4099, 72, "runs of rows"),
+                                                           (5, 1500, 40001, 64, "four groups, then one")])
 def test_gradients_in_pieces(nb, groups, rows, hosts, width, what):
-    """Scores beyond 256 MB: their gradient exists in pieces (with a shorter one at the end), whose products add up."""
+    """Scores beyond 512 MB: their gradient exists in pieces (with a shorter one at the end), whose products add up."""
     check(nb, make(groups, rows, hosts, width, 3, "bfloat16", True, 5), 1.0, 1.0)
 
 
