@@ -1,11 +1,16 @@
 """Trains a small placement policy on the exact rule's decisions and lets it place requests.
 
     python -m paper_2503_20591_b200.train_policy [--hosts 256] [--snapshots 16] [--batch 512] [--steps 150]
+                                                 [--blocks 0] [--max-norm X] [--no-table]
 
 One step: a batch of requests is placed by nbos_place_batch on every snapshot (the teacher); the policy scores every
 host for every request and answers by sampling three distinct hosts; the distillation loss pulls it to the teacher's
 three hosts, the balance loss moves probability away from hosts that its own answers load more than others. Afterwards
 both ways of placing are compared.
+
+--blocks gives either tower residual blocks, --max-norm clips the gradients by their global norm, --no-table trains on the
+two towers' vectors (in bfloat16) without the table of scores: for clusters whose table does not fit. There is no balance loss
+then, which needs the table.
 """
 from __future__ import annotations
 
@@ -20,18 +25,43 @@ TEACHER_LOGITS = (2.0, 1.0, 0.0)   # best, second, third host
 ANSWER = dict(temperature=0.7, top_k=16, top_p=0.95, min_p=0.01)   # how the policy is asked
 
 
+class ResidualBlocks(torch.nn.Module):
+    """Blocks x + gate * norm(branch(norm(x))) behind a tower, with the norms around each branch in one kernel."""
+
+    def __init__(self, width: int, blocks: int):
+        super().__init__()
+        self.branches = torch.nn.ModuleList(torch.nn.Sequential(torch.nn.Linear(width, width), torch.nn.ReLU(), torch.nn.Linear(width, width))
+                                            for _ in range(blocks))
+        self.gates = torch.nn.ParameterList(torch.full((width,), 0.1) for _ in range(blocks))
+        self.post = torch.nn.ParameterList(torch.ones(width) for _ in range(blocks))
+        self.pre = torch.nn.ParameterList(torch.ones(width) for _ in range(blocks))
+
+    def forward(self, x):
+        normed = x
+        for branch, gate, post, pre in zip(self.branches, self.gates, self.post, self.pre):
+            x, normed = policy.block_norm(x, branch(normed), gate, post, pre)
+        return normed
+
+
 class TwoTowerPolicy(torch.nn.Module):
     """logits[n, b, h] = request vector . host vector."""
 
-    def __init__(self, request_features: int, host_features: int, width: int = 64):
+    def __init__(self, request_features: int, host_features: int, width: int = 64, blocks: int = 0):
         super().__init__()
         self.request = torch.nn.Sequential(torch.nn.Linear(request_features, width), torch.nn.ReLU(),
                                            torch.nn.Linear(width, width))
         self.host = torch.nn.Sequential(torch.nn.Linear(host_features, width), torch.nn.ReLU(),
                                         torch.nn.Linear(width, width))
+        if blocks:
+            self.request.append(ResidualBlocks(width, blocks))
+            self.host.append(ResidualBlocks(width, blocks))
+
+    def vectors(self, requests, hosts):
+        return self.request(requests), self.host(hosts)
 
     def forward(self, requests, hosts, fits):
-        logits = self.request(requests) @ self.host(hosts).transpose(1, 2)
+        request, host = self.vectors(requests, hosts)
+        logits = request @ host.transpose(1, 2)
         return logits.masked_fill(~fits, float("-inf"))
 
 
@@ -45,6 +75,11 @@ class Cluster:
         s = {k: v.float() for k, v in self.state.items()}
         self.features = torch.stack([(s["gpus_total"] - s["gpus_committed"]) / 8, s["gpus_subscribed"] / 16, s["gpus_total"] / 8,
                                      s["vram_gb"] / 640, s["millicpus"] / 128_000, s["mem_mb"] / 1_048_576], dim=-1)
+        # what a request may ask for at most, [N, H, 4]: GPUs within the host and within its subscription limit, then the capacities
+        total, held = self.state["gpus_total"].long(), self.state["gpus_subscribed"].long()
+        by_limit = torch.div(total * self.limit[0][:, 0], self.limit[1][:, 0], rounding_mode="floor") - held
+        gpus = torch.where(total >= 1, torch.minimum(total, by_limit), -1).clamp(min=-1)
+        self.room = torch.stack([gpus.int(), self.state["vram_gb"], self.state["millicpus"], self.state["mem_mb"]], dim=-1).contiguous()
 
     def teacher(self, requests):
         """requests [N, B, 4] int32: the exact rule's hosts [N, B, 3], -1 where fewer fit."""
@@ -67,11 +102,12 @@ def request_features(requests):
     return requests.float() / torch.tensor([8.0, 128.0, 16_000.0, 65_536.0], device=requests.device)
 
 
-def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 150, seed: int = 0, report=print) -> dict:
+def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 150, seed: int = 0, report=print,
+          blocks: int = 0, max_norm: float | None = None, table: bool = True) -> dict:
     torch.manual_seed(seed)
     cluster = Cluster(workloads.what_if_sweep(snapshots, hosts, batch))
     try:
-        net = TwoTowerPolicy(4, cluster.features.shape[-1]).cuda()
+        net = TwoTowerPolicy(4, cluster.features.shape[-1], blocks=blocks).cuda()
         optimizer = torch.optim.Adam(net.parameters(), lr=3e-3)
         teacher_logits = torch.tensor(TEACHER_LOGITS, device="cuda")
         gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -96,14 +132,26 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
         for step in range(steps):
             requests = draw()
             wanted = cluster.teacher(requests)
-            logits = net(request_features(requests), cluster.features, cluster.fits(requests))
-            distill = policy.distill_loss(logits, wanted, teacher_logits)
-            even, _, _ = policy.balance_loss(logits, answer(logits)[0])   # the load is the policy's own, not the rule's
-            loss = distill.mean() + BALANCE_WEIGHT * even.mean()
+            reported = step % max(1, steps // 5) == 0 or step == steps - 1
+            if table:
+                logits = net(request_features(requests), cluster.features, cluster.fits(requests))
+                distill = policy.distill_loss(logits, wanted, teacher_logits)
+                even, _, _ = policy.balance_loss(logits, answer(logits)[0])   # the load is the policy's own, not the rule's
+                loss = distill.mean() + BALANCE_WEIGHT * even.mean()
+            else:
+                request, host = (v.bfloat16() for v in net.vectors(request_features(requests), cluster.features))
+                distill = policy.tower_distill_loss(request, host, wanted, teacher_logits, asks=requests, room=cluster.room)
+                loss = distill.mean()
+                if reported:
+                    with torch.no_grad():
+                        logits = net(request_features(requests), cluster.features, cluster.fits(requests))
+                        even, _, _ = policy.balance_loss(logits, answer(logits)[0])
             optimizer.zero_grad(set_to_none=True)
             loss.backward()
+            if max_norm is not None:
+                policy.clip_gradients(net.parameters(), max_norm)
             optimizer.step()
-            if step % max(1, steps // 5) == 0 or step == steps - 1:
+            if reported:
                 history.append((distill.mean().item(), even.mean().item(), agreement(logits.detach(), wanted)))
                 report(f"step {step}: distillation {history[-1][0]:.4f}, balance {history[-1][1]:.2f}, "
                        f"best host among the rule's three {history[-1][2]:.3f}")
@@ -132,6 +180,8 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
 
 if __name__ == "__main__":
     parser = argparse.ArgumentParser(description=__doc__.splitlines()[0])
-    for name, value in (("hosts", 256), ("snapshots", 16), ("batch", 512), ("steps", 150), ("seed", 0)):
+    for name, value in (("hosts", 256), ("snapshots", 16), ("batch", 512), ("steps", 150), ("seed", 0), ("blocks", 0)):
         parser.add_argument(f"--{name}", type=int, default=value)
+    parser.add_argument("--max-norm", type=float, default=None)
+    parser.add_argument("--no-table", dest="table", action="store_false")
     train(**vars(parser.parse_args()))
