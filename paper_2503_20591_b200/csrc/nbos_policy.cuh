@@ -8,6 +8,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <utility>
+
 #include "nbos_internal.h"
 
 namespace nbos {
@@ -363,7 +365,28 @@ __device__ __forceinline__ V *cluster_peer(V *shared, int rank, int cs)
     return cs > 1 ? cooperative_groups::this_cluster().map_shared_rank(shared, rank) : shared;
 }
 
+// ---- kernels in a row --------------------------------------------------------------------------------------
+// A kernel launched by launch_next may start while the one before it in the stream still runs: it sets itself up and
+// then waits, before it touches memory, until that one has finished and its results can be seen. Every kernel of such a row waits.
+__device__ __forceinline__ void previous_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---- host side --------------------------------------------------------------------------------------------
+template <typename... P, typename... A>
+inline cudaError_t launch_next(void (*kernel)(P...), dim3 grid, int threads, size_t shared, cudaStream_t stream, A &&...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
 inline size_t dtype_bytes(int dtype) { return dtype == NBOS_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 

@@ -269,6 +269,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     cluster_barrier();
     fence_after();
     const uint32_t tmem = *tmem_at;
+    next_may_start();
+    previous_done();
 
     Unit u;
     if (warp == kEpilogue / 32) {   // ---- copies
@@ -572,6 +574,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 template <typename T>
 __global__ void lay_out_kernel(const T *src, long long stride, long long group_stride, int rows, int width, int wide, T *dst)
 {
+    next_may_start();
+    previous_done();
     const int chunks = wide / 8;
     const long long n = (long long)rows * chunks, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     src += blockIdx.y * group_stride;
@@ -658,6 +662,8 @@ __device__ __forceinline__ void dots(float (&out)[U], const T *a, const T *const
 template <typename T, int TEAM, int U>
 __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ FinishArgs f, int lanes)
 {
+    next_may_start();
+    previous_done();
     const int lane = threadIdx.x % TEAM;
     const long long team = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / TEAM;
     const bool inside = team < (long long)f.groups * f.rows;
@@ -734,6 +740,8 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
 // the type's whole range (p of 2^-29 is still a normal number). `largest`: bits of the largest |grad_loss|.
 __global__ void largest_kernel(const float *grad_loss, long long n, unsigned int *largest)
 {
+    next_may_start();
+    previous_done();
     float m = 0.0f;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x)
         m = fmaxf(m, fabsf(grad_loss[i]));
@@ -742,6 +750,8 @@ __global__ void largest_kernel(const float *grad_loss, long long n, unsigned int
 }
 __global__ void range_kernel(const unsigned int *largest, float scale, float *range)
 {
+    next_may_start();
+    previous_done();
     const float g = (largest ? __uint_as_float(*largest) : 1.0f) * fabsf(scale);
     int e = 0;
     if (g > 0.0f && g < __int_as_float(0x7F800000)) frexpf(g, &e);
@@ -763,6 +773,8 @@ struct PatchArgs {
 template <typename T>
 __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ PatchArgs p, int lanes)
 {
+    next_may_start();
+    previous_done();
     const long long n = (long long)p.groups * p.rows_here, i = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / lanes;
     const bool inside = i < n;
     const int sub = threadIdx.x % lanes, g = inside ? (int)(i / p.rows_here) : 0, row = inside ? (int)(i % p.rows_here) : 0;
@@ -803,6 +815,8 @@ template <typename T>
 __global__ void sums_kernel(const float *sums, int splits, int groups, int rows, int width, const float *range, T *out, long long stride,
                             long long group_stride)
 {
+    next_may_start();
+    previous_done();
     const long long n = (long long)groups * rows * width;
     const float undo = range ? range[1] : 1.0f;
     if (width % 4 == 0) {
@@ -921,8 +935,7 @@ cudaError_t launch_tower(const CUtensorMap &a, const CUtensorMap &b, const CUten
     auto *kernel = tower_kernel<KIND, BN, MASK, T>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<KIND, BN>::kBytes);
     if (e != cudaSuccess) return e;
-    kernel<<<2 * pairs, kThreads, Shape<KIND, BN>::kBytes, stream>>>(a, b, g, args);
-    return cudaGetLastError();
+    return launch_next(kernel, dim3(2 * pairs), kThreads, Shape<KIND, BN>::kBytes, stream, a, b, g, args);
 }
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
@@ -1024,9 +1037,8 @@ cudaError_t lay_out(const Workspace &ws, Operand &o, int sms, cudaStream_t strea
     const int slices = o.table.group_stride == 0 ? 1 : o.table.groups, wide = (int)o.table.stride;
     const long long chunks = (long long)o.table.rows * (wide / 8), most = 8ll * sms;
     const long long blocks = (chunks + 255) / 256 < most ? (chunks + 255) / 256 : most;
-    lay_out_kernel<T><<<dim3((unsigned int)blocks, slices), 256, 0, stream>>>(static_cast<const T *>(o.src), o.src_stride, o.src_group_stride,
-                                                                              o.table.rows, o.table.width, wide, to);
-    return cudaGetLastError();
+    return launch_next(lay_out_kernel<T>, dim3((unsigned int)blocks, slices), 256, 0, stream, static_cast<const T *>(o.src), o.src_stride,
+                       o.src_group_stride, o.table.rows, o.table.width, wide, to);
 }
 
 template <typename T>
@@ -1073,20 +1085,19 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     const unsigned int warp_blocks = (unsigned int)((rows + 7) / 8), eighth_blocks = (unsigned int)((rows + 31) / 32);
     if (c.k > 4) {
         while (lanes > 8 && 32 / lanes * 4 < c.k) lanes /= 2;
-        finish_kernel<T, 32, 4><<<warp_blocks, 256, 0, c.stream>>>(f, lanes);
+        e = launch_next(finish_kernel<T, 32, 4>, dim3(warp_blocks), 256, 0, c.stream, f, lanes);
     } else if (in->width > 512) {
         if (c.k == 1)
-            finish_kernel<T, 32, 1><<<warp_blocks, 256, 0, c.stream>>>(f, lanes);
+            e = launch_next(finish_kernel<T, 32, 1>, dim3(warp_blocks), 256, 0, c.stream, f, lanes);
         else
-            finish_kernel<T, 32, 4><<<warp_blocks, 256, 0, c.stream>>>(f, lanes);
+            e = launch_next(finish_kernel<T, 32, 4>, dim3(warp_blocks), 256, 0, c.stream, f, lanes);
     } else {
         if (lanes > 8) lanes = 8;
         if (c.k == 1)
-            finish_kernel<T, 8, 1><<<eighth_blocks, 256, 0, c.stream>>>(f, lanes);
+            e = launch_next(finish_kernel<T, 8, 1>, dim3(eighth_blocks), 256, 0, c.stream, f, lanes);
         else
-            finish_kernel<T, 8, 4><<<eighth_blocks, 256, 0, c.stream>>>(f, lanes);
+            e = launch_next(finish_kernel<T, 8, 4>, dim3(eighth_blocks), 256, 0, c.stream, f, lanes);
     }
-    e = cudaGetLastError();
     return e == cudaSuccess ? NBOS_OK : cuda_fail(e, "towers: loss launch");
 }
 
@@ -1154,10 +1165,10 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
         if (largest) {
             e = cudaMemsetAsync(largest, 0, 4, c.stream);
             const long long n = (long long)groups * rows, blocks = (n + 1023) / 1024;
-            if (e == cudaSuccess) largest_kernel<<<(unsigned int)(blocks < 2 * c.sms ? blocks : 2 * c.sms), 256, 0, c.stream>>>(grad_loss, n, largest);
+            if (e == cudaSuccess)
+                e = launch_next(largest_kernel, dim3((unsigned int)(blocks < 2 * c.sms ? blocks : 2 * c.sms)), 256, 0, c.stream, grad_loss, n, largest);
         }
-        if (e == cudaSuccess) range_kernel<<<1, 1, 0, c.stream>>>(largest, scale, range);
-        if (e == cudaSuccess) e = cudaGetLastError();
+        if (e == cudaSuccess) e = launch_next(range_kernel, dim3(1), 1, 0, c.stream, largest, scale, range);
     }
     if (e != cudaSuccess) return cuda_fail(e, "towers: layout launch");
 
@@ -1195,8 +1206,8 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 q.grad_scale = scale, q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
                 int lanes = 1;
                 while (lanes < 32 && lanes < c.k) lanes *= 2;
-                patch_kernel<T><<<(unsigned int)(((long long)gn * rn * lanes + 255) / 256), 256, 0, c.stream>>>(q, lanes);
-                if ((e = cudaGetLastError()) != cudaSuccess) return cuda_fail(e, "towers: teacher launch");
+                e = launch_next(patch_kernel<T>, dim3((unsigned int)(((long long)gn * rn * lanes + 255) / 256)), 256, 0, c.stream, q, lanes);
+                if (e != cudaSuccess) return cuda_fail(e, "towers: teacher launch");
 
                 if (grad_a) {
                     TowerArgs d = {};
@@ -1209,9 +1220,8 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                     e = launch_gradient<GRAD_REQUESTS, T>(g_rows, b_cols, d, narrow, pairs, c.stream);
                     if (e == cudaSuccess && sums_a && h0 + hn == hosts) {
                         const long long n = (long long)gn * rn * width, blocks = (n + 1023) / 1024;
-                        sums_kernel<T><<<(unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms), 256, 0, c.stream>>>(
-                            d.sums, ta.splits, gn, rn, width, range, grad_a + g0 * a_group_stride + r0 * a_stride, a_stride, a_group_stride);
-                        e = cudaGetLastError();
+                        e = launch_next(sums_kernel<T>, dim3((unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms)), 256, 0, c.stream,
+                                        d.sums, ta.splits, gn, rn, width, range, grad_a + g0 * a_group_stride + r0 * a_stride, a_stride, a_group_stride);
                     }
                     if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
                 }
@@ -1226,9 +1236,8 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                     e = launch_gradient<GRAD_HOSTS, T>(g_cols, a_cols, d, narrow, pairs, c.stream);
                     if (e == cudaSuccess && sums_b && r0 + rn == rows) {
                         const long long n = (long long)gn * hn * width, blocks = (n + 1023) / 1024;
-                        sums_kernel<T><<<(unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms), 256, 0, c.stream>>>(
-                            d.sums, tb.splits, gn, hn, width, range, grad_b + g0 * b_group_stride + h0 * b_stride, b_stride, b_group_stride);
-                        e = cudaGetLastError();
+                        e = launch_next(sums_kernel<T>, dim3((unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms)), 256, 0, c.stream,
+                                        d.sums, tb.splits, gn, hn, width, range, grad_b + g0 * b_group_stride + h0 * b_stride, b_stride, b_group_stride);
                     }
                     if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
                 }
