@@ -8,6 +8,8 @@
 // G exists in pieces of rows, in 16 bits (the operands' type): at most kPieceBytes of it.
 #include <math.h>
 
+#include <atomic>
+
 #include "nbos_policy.cuh"
 #include "nbos_tensor.cuh"
 
@@ -24,6 +26,8 @@ constexpr int kParts = 4;             // a tile's columns are read in this many 
 constexpr int kEpilogue = 128 * kParts;
 constexpr int kThreads = kEpilogue + 64;   // and a warp that copies, a warp that multiplies
 constexpr int kTmemColumns = 512;     // two tiles of 32-bit products
+constexpr int kBand = 16;             // tiles of hosts that G's rows go through together
+constexpr int kFewEntries = 4;        // a row's entries that are put into G on its way out; more of them by a kernel of their own
 constexpr size_t kPieceBytes = 512u << 20;   // 65,536 x 4,096 at width 256, gradients: 48 MB 950 us, 128 MB 650, 256 MB 586, 512 MB 567: launches fill the GPU
 
 enum Kind { STATS, GRAD, GRAD_REQUESTS, GRAD_HOSTS };
@@ -45,6 +49,10 @@ struct TowerArgs {
     int slots;
     const float *stats;               // GRAD: [groups][rows][stats_stride]: m, S, ...
     int stats_stride;
+    const int32_t *ids;               // GRAD: the rows' entries, k of them (NULL: too many)
+    const float *teacher;
+    long long teacher_stride;
+    int k;
     const float *grad_loss, *range;   // range: factor that keeps G within 16 bits, and its inverse (NULL: 1)
     float grad_scale;
     void *out;                        // gradients: the result itself (one part), or
@@ -55,7 +63,7 @@ struct TowerArgs {
 
 __device__ unsigned int tower_status;   // STATUS_WAIT_TIMEOUT once a wait ran out, until nbos_policy_towers_status is asked
 
-// STATS: pair p of `pairs` takes units [first_unit(p), first_unit(p + 1)), hosts innermost: a pair stays with its rows as long
+// Scores: pair p of `pairs` takes units [first_unit(p), first_unit(p + 1)), hosts innermost: a pair stays with its rows as long
 // as it can, and all pairs have equally much to do.
 __device__ __host__ __forceinline__ long long first_unit(long long units, int pairs, int p)
 {
@@ -71,18 +79,26 @@ __device__ __host__ __forceinline__ int pair_of(long long units, int pairs, long
 struct Unit {
     int g, m, n, split, k0, k1;       // k0 .. k1: blocks of the contraction
 };
-// Every thread that has a part in a unit goes through the same schedule, so its steps are 32-bit ones: STATS counts on from where the
+// Every thread that has a part in a unit goes through the same schedule, so its steps are 32-bit ones: scores count on from where the
 // pair starts, the others (fewer than 2^31 units) divide.
 template <Kind KIND>
 struct Schedule {
     unsigned int left, at, step;
-    int n, m, g;   // STATS: the next unit's
+    int n, m, g, band, band_end;   // scores: the next unit's, and which columns its band has
     __device__ __forceinline__ Schedule(const Tiles &t, int pair, int pairs)
     {
-        if (KIND == STATS) {
-            const long long from = first_unit(t.units, pairs, pair), rest = from / t.n_tiles;
+        if (KIND == STATS || KIND == GRAD) {
+            const long long from = first_unit(t.units, pairs, pair), per_group = (long long)t.m_tiles * t.n_tiles;
             left = (unsigned int)(first_unit(t.units, pairs, pair + 1) - from);
-            n = (int)(from % t.n_tiles), m = (int)(rest % t.m_tiles), g = (int)(rest / t.m_tiles);
+            g = (int)(from / per_group);
+            // GRAD goes through bands of columns, each for all rows: pairs in flight at one time read the same hosts, and still a pair
+            // stays with its rows for a band's width. (STATS would leave a part of each row's statistics for each band.)
+            const long long in = from % per_group;
+            const int wide = KIND == GRAD ? kBand : t.n_tiles;
+            band = (int)(in / ((long long)t.m_tiles * wide)) * wide;
+            band_end = min(band + wide, t.n_tiles);
+            const long long rest = in - (long long)t.m_tiles * band;
+            m = (int)(rest / (band_end - band)), n = band + (int)(rest % (band_end - band));
         } else {
             left = (unsigned int)t.units > (unsigned int)pair ? ((unsigned int)t.units - pair + pairs - 1) / pairs : 0;
             at = pair, step = pairs;
@@ -92,17 +108,22 @@ struct Schedule {
     {
         if (left == 0) return false;
         --left;
-        if (KIND == STATS) {
+        if (KIND == STATS || KIND == GRAD) {
             u.n = n, u.m = m, u.g = g, u.split = 0;
-            if (++n == t.n_tiles) {
-                n = 0;
-                if (++m == t.m_tiles) m = 0, ++g;
+            if (++n == band_end) {
+                n = band;
+                if (++m == t.m_tiles) {
+                    m = 0;
+                    if (band_end == t.n_tiles) ++g, band_end = 0;
+                    n = band = band_end;
+                    band_end = KIND == GRAD ? min(band + kBand, t.n_tiles) : t.n_tiles;
+                }
             }
         } else {
             // bands of 8 tiles along M, so that tiles in flight at one time share both operands
             const unsigned int per_split = (unsigned int)t.m_tiles * t.n_tiles, part = at / per_split, in = at % per_split;
-            const unsigned int band = in / (8u * t.n_tiles), high = min(8u, t.m_tiles - 8 * band), rest = in - band * 8 * t.n_tiles;
-            u.m = (int)(8 * band + rest % high), u.n = (int)(rest / high);
+            const unsigned int across = in / (8u * t.n_tiles), high = min(8u, t.m_tiles - 8 * across), rest = in - across * 8 * t.n_tiles;
+            u.m = (int)(8 * across + rest % high), u.n = (int)(rest / high);
             u.split = (int)(part % t.splits), u.g = (int)(part / t.splits);
             at += step;
         }
@@ -224,6 +245,41 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __half)
 {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// The entries of row `at`: their columns of this launch's hosts (-1: none) and G there. Entries that name one host add up, and
+// each of them holds the sum.
+template <typename T>
+__device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bool inside, int (&column)[kFewEntries], T (&value)[kFewEntries])
+{
+    const float *stats = a.stats + at * a.stats_stride;
+    float t[kFewEntries], x[kFewEntries], top = neg_inf(), sum = 0.0f;
+    int id[kFewEntries];
+#pragma unroll
+    for (int j = 0; j < kFewEntries; ++j) {
+        const bool there = inside && j < a.k;
+        id[j] = there ? a.ids[at * a.k + j] : -1;
+        x[j] = there ? stats[2 + j] : neg_inf();
+        t[j] = there && x[j] != neg_inf() ? (a.teacher ? a.teacher[at * a.teacher_stride + j] : 0.0f) : neg_inf();
+        if (t[j] > top) top = t[j];
+    }
+#pragma unroll
+    for (int j = 0; j < kFewEntries; ++j) {
+        t[j] = t[j] > neg_inf() ? exp2_fast((t[j] - top) * a.c) : 0.0f;
+        sum += t[j];
+    }
+    const bool some = sum != 0.0f;
+    const float minus = some ? -fmaf(stats[0], a.c, log2f(stats[1])) : 0.0f;
+    const float factor = some ? a.grad_scale * (a.grad_loss ? a.grad_loss[at] : 1.0f) * (a.range ? a.range[0] : 1.0f) : 0.0f;
+#pragma unroll
+    for (int j = 0; j < kFewEntries; ++j) {
+        float q = 0.0f;
+#pragma unroll
+        for (int l = 0; l < kFewEntries; ++l) q += id[l] == id[j] ? t[l] : 0.0f;
+        const bool put = some && x[j] != neg_inf() && id[j] >= a.col0 && id[j] < a.col0 + a.col_end;
+        column[j] = put ? id[j] - a.col0 : -1;
+        value[j] = from_float<T>((exp2_fast(fmaf(x[j], a.c, minus)) - q / sum) * factor);
+    }
 }
 
 // One launch covers its units with pairs of blocks, each a persistent pair: one thread a block copies operand tiles
@@ -359,6 +415,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         // STATS: the rows' statistics so far; GRAD: -(m c + log2 S) and the factor of p
         float run_m[ROWS], run_s[ROWS], minus[ROWS], factor[ROWS];
         bool dead[ROWS], some_dead = false;
+        // GRAD: the few entries of the row that this lane puts in: columns, and what stands there, p - q rounded once
+        const int entry_row = MASK ? lane / 4 + 8 * (lane % 4) : lane;
+        int entry_at[kFewEntries];
+        T entry[kFewEntries];
         int slot = 0;
         auto release = [&] {
             fence_before();
@@ -411,6 +471,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         some_dead |= dead[i];
                     }
                     some_dead = __any_sync(kFull, some_dead);
+                    if (KIND == GRAD && args.ids) {
+                        const int row = args.row0 + u.m * kTileM + (int)rank * 128 + warp % 4 * 32 + entry_row;
+                        row_entries(args, (long long)(args.group0 + u.g) * args.rows + row, row < args.rows, entry_at, entry);
+                    }
                     last_g = u.g, last_m = u.m;
                 }
                 const int4 *columns = room + parity * kTileN;
@@ -487,6 +551,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                 }
                 if (KIND == GRAD) {
+                    if (args.ids) {
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < kFewEntries; ++j) {
+                            const int col = entry_at[j] - n0;
+                            if ((unsigned int)col < 64u)
+                                asm volatile("st.shared.b16 [%0], %1;" ::"r"(box + entry_row * 128 + (((col / 8) ^ (entry_row & 7)) << 4) + col % 8 * 2),
+                                             "h"(*reinterpret_cast<const unsigned short *>(&entry[j]))
+                                             : "memory");
+                        }
+                    }
                     async_proxy_fence();
                     __syncwarp();
                     if (lane == 0) {
@@ -660,7 +735,7 @@ __device__ __forceinline__ void dots(float (&out)[U], const T *a, const T *const
 // share a product, each team takes TEAM / lanes * U of them at a time. (One product after the other, a warp a row:
 // 74 us for 65,536 rows of 256 with three hosts each, this 41 to 49.)
 template <typename T, int TEAM, int U>
-__global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ FinishArgs f, int lanes)
+__global__ void __launch_bounds__(256, 4) finish_kernel(const __grid_constant__ FinishArgs f, int lanes)
 {
     next_may_start();
     previous_done();
@@ -703,8 +778,9 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
             const int id = j < f.k ? f.ids[at * f.k + j] : -1;
             t[u] = j < f.k && f.teacher ? f.teacher[at * f.teacher_stride + j] : 0.0f;
             there[u] = id >= 0 && id < f.hosts;
-            if (there[u] && f.asks) there[u] = !never_fits(ask) && fits(ask, f.room[(long long)g * f.hosts + id]);
             of[u] = there[u] ? b + id * f.b_stride : b;   // b: a row that is there, for a product that is not used
+            // (whether the request fits decides over the product, not over its loads)
+            if (there[u] && f.asks) there[u] = !never_fits(ask) && fits(ask, f.room[(long long)g * f.hosts + id]);
         }
         dots<T, U>(x, a, of, f.width, sub, lanes);
 #pragma unroll
@@ -933,8 +1009,17 @@ template <Kind KIND, int BN, bool MASK, typename T>
 cudaError_t launch_tower(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &g, const TowerArgs &args, int pairs, cudaStream_t stream)
 {
     auto *kernel = tower_kernel<KIND, BN, MASK, T>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<KIND, BN>::kBytes);
+    // once a device (a bit each; two threads that meet here set the same value twice)
+    static std::atomic<unsigned long long> allowed{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<KIND, BN>::kBytes);
+        if (e != cudaSuccess) return e;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
     return launch_next(kernel, dim3(2 * pairs), kThreads, Shape<KIND, BN>::kBytes, stream, a, b, g, args);
 }
 
@@ -1195,19 +1280,23 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 p.group0 = g0, p.row0 = r0, p.rows = rows, p.hosts = hosts, p.width = width, p.col0 = h0, p.col_end = hn, p.m_rows = rn;
                 p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
                 p.c = kLog2e / c.T, p.stats = stats, p.stats_stride = 2 + c.k, p.grad_loss = grad_loss, p.grad_scale = scale, p.range = range;
+                const bool few = c.k <= kFewEntries;
+                if (few) p.ids = c.ids, p.teacher = c.teacher, p.teacher_stride = c.teacher_stride, p.k = c.k;
                 const int used = p.t.units < pairs ? (int)p.t.units : pairs;
                 e = in->asks ? launch_tower<GRAD, kTileN, true, T>(a_rows, b_rows, g_out, p, used, c.stream)
                              : launch_tower<GRAD, kTileN, false, T>(a_rows, b_rows, g_out, p, used, c.stream);
                 if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
 
-                PatchArgs q = {};
-                q.groups = gn, q.group0 = g0, q.row0 = r0, q.rows_here = rn, q.rows = rows, q.host0 = h0, q.hosts_here = hn, q.hosts = hosts, q.k = c.k;
-                q.ids = c.ids, q.teacher = c.teacher, q.teacher_stride = c.teacher_stride, q.stats = stats, q.grad_loss = grad_loss, q.range = range;
-                q.grad_scale = scale, q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
-                int lanes = 1;
-                while (lanes < 32 && lanes < c.k) lanes *= 2;
-                e = launch_next(patch_kernel<T>, dim3((unsigned int)(((long long)gn * rn * lanes + 255) / 256)), 256, 0, c.stream, q, lanes);
-                if (e != cudaSuccess) return cuda_fail(e, "towers: teacher launch");
+                if (!few) {
+                    PatchArgs q = {};
+                    q.groups = gn, q.group0 = g0, q.row0 = r0, q.rows_here = rn, q.rows = rows, q.host0 = h0, q.hosts_here = hn, q.hosts = hosts, q.k = c.k;
+                    q.ids = c.ids, q.teacher = c.teacher, q.teacher_stride = c.teacher_stride, q.stats = stats, q.grad_loss = grad_loss, q.range = range;
+                    q.grad_scale = scale, q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
+                    int lanes = 1;
+                    while (lanes < 32 && lanes < c.k) lanes *= 2;
+                    e = launch_next(patch_kernel<T>, dim3((unsigned int)(((long long)gn * rn * lanes + 255) / 256)), 256, 0, c.stream, q, lanes);
+                    if (e != cudaSuccess) return cuda_fail(e, "towers: teacher launch");
+                }
 
                 if (grad_a) {
                     TowerArgs d = {};
