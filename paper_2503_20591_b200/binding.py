@@ -914,6 +914,10 @@ def nbos_policy_clip(tensors, max_norm, out_norm=None, outs=None, norm_kind=NBOS
         to = _addresses(outs, "outs", device.index)
         if list(map(_dtype_of, outs)) != dtypes or list(map(torch.Tensor.numel, outs)) != numels:
             raise ValueError("outs must have the sizes and types of tensors")
+    if to is not None and len(set(to)) < n:   # (empty tensors may share an address)
+        used = [a for a, size in zip(to, numels) if size]
+        if len(set(used)) < len(used):
+            raise ValueError("a tensor is written twice: its values would depend on the order")
     sizes = array("q", numels)
     _check(load_library().nbos_policy_clip(data.buffer_info()[0], None if to is None else to.buffer_info()[0], sizes.buffer_info()[0],
                                            kinds.buffer_info()[0], n, max_norm, norm_kind, norm, queue))

@@ -145,12 +145,19 @@ struct Shape {
 
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// d = a b + c, two at a time
-__device__ __forceinline__ void fma2_to(float &d0, float &d1, float a0, float a1, float b, float c)
+// d = (a - m) b + c, two at a time. The subtraction comes first: near the row's maximum it is exact or nearly so, and nothing
+// overflows at low temperatures.
+__device__ __forceinline__ void apart2(float &d0, float &d1, uint32_t a0, uint32_t a1, float minus_m, float b)
 {
     asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %4};\n\tmov.b64 z, {%5, %5};\n\t"
-        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
-        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+        "add.rn.f32x2 x, x, y;\n\tmul.rn.f32x2 x, x, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d0), "=f"(d1) : "r"(a0), "r"(a1), "f"(minus_m), "f"(b));
+}
+__device__ __forceinline__ void apart2(float &d0, float &d1, uint32_t a0, uint32_t a1, float minus_m, float b, float c)
+{
+    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %4};\n\tmov.b64 z, {%5, %5};\n\tmov.b64 w, {%6, %6};\n\t"
+        "add.rn.f32x2 x, x, y;\n\tfma.rn.f32x2 x, x, z, w;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d0), "=f"(d1) : "r"(a0), "r"(a1), "f"(minus_m), "f"(b), "f"(c));
 }
 __device__ __forceinline__ bool fits(const int4 &ask, const int4 &room)
 {
@@ -199,14 +206,14 @@ __device__ __forceinline__ void add8(float &m, float &s, const uint32_t (&v)[2][
 #pragma unroll
     for (int j = 0; j < 4; ++j) top[j % 2] = fmaxf(top[j % 2], fmaxf(at(j, 0), at(j, 1)));
     const float to = fmaxf(top[0], top[1]);
-    const float base = (to == neg_inf() ? 0.0f : to) * -c;
-    s *= exp2_fast(fmaf(m, c, base));
+    const float base = to == neg_inf() ? 0.0f : to;
+    s *= exp2_fast((m - base) * c);
     m = to;
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float e0, e1;
-        fma2_to(e0, e1, at(j, 0), at(j, 1), c, base);
+        apart2(e0, e1, __float_as_uint(at(j, 0)), __float_as_uint(at(j, 1)), -base, c);
         add2(sum[0], sum[1], exp2_fast(e0), exp2_fast(e1));
     }
     s += sum[0] + sum[1];
@@ -221,15 +228,15 @@ __device__ __forceinline__ void add64(float &m, float &s, uint32_t (&u)[32], uin
 #pragma unroll
         for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], fmaxf(__uint_as_float(u[i + j]), __uint_as_float(v[i + j])));
     const float to = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-    const float base = (to == neg_inf() ? 0.0f : to) * -c;
-    s *= exp2_fast(fmaf(m, c, base));
+    const float base = to == neg_inf() ? 0.0f : to;
+    s *= exp2_fast((m - base) * c);
     m = to;
     float sum[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
         float e0, e1, f0, f1;
-        fma2_to(e0, e1, __uint_as_float(u[i]), __uint_as_float(u[i + 1]), c, base);
-        fma2_to(f0, f1, __uint_as_float(v[i]), __uint_as_float(v[i + 1]), c, base);
+        apart2(e0, e1, u[i], u[i + 1], -base, c);
+        apart2(f0, f1, v[i], v[i + 1], -base, c);
         add2(sum[0][0], sum[0][1], exp2_fast(e0), exp2_fast(e1));
         add2(sum[1][0], sum[1][1], exp2_fast(f0), exp2_fast(f1));
     }
@@ -269,7 +276,7 @@ __device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bo
         sum += t[j];
     }
     const bool some = sum != 0.0f;
-    const float minus = some ? -fmaf(stats[0], a.c, log2f(stats[1])) : 0.0f;
+    const float m = some ? stats[0] : 0.0f, minus = some ? -log2f(stats[1]) : 0.0f;
     const float factor = some ? a.grad_scale * (a.grad_loss ? a.grad_loss[at] : 1.0f) * (a.range ? a.range[0] : 1.0f) : 0.0f;
 #pragma unroll
     for (int j = 0; j < kFewEntries; ++j) {
@@ -278,7 +285,7 @@ __device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bo
         for (int l = 0; l < kFewEntries; ++l) q += id[l] == id[j] ? t[l] : 0.0f;
         const bool put = some && x[j] != neg_inf() && id[j] >= a.col0 && id[j] < a.col0 + a.col_end;
         column[j] = put ? id[j] - a.col0 : -1;
-        value[j] = from_float<T>((exp2_fast(fmaf(x[j], a.c, minus)) - q / sum) * factor);
+        value[j] = from_float<T>((exp2_fast(fmaf(x[j] - m, a.c, minus)) - q / sum) * factor);
     }
 }
 
@@ -412,7 +419,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         constexpr int ROWS = MASK ? 4 : 1;
         auto row_at = [&](int i) { return MASK ? warp % 4 * 32 + lane / 4 + 8 * i : row_in; };
         int4 ask[ROWS];
-        // STATS: the rows' statistics so far; GRAD: -(m c + log2 S) and the factor of p
+        // STATS: the rows' statistics so far; GRAD: -m (in run_m), -log2 S and the factor of p
         float run_m[ROWS], run_s[ROWS], minus[ROWS], factor[ROWS];
         bool dead[ROWS], some_dead = false;
         // GRAD: the few entries of the row that this lane puts in: columns, and what stands there, p - q rounded once
@@ -464,7 +471,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         if (KIND == GRAD && inside) {
                             const float m = args.stats[at * args.stats_stride], s = args.stats[at * args.stats_stride + 1];
                             dead[i] = s == __int_as_float(0x7F800000);
-                            minus[i] = -fmaf(m, args.c, log2f(s));
+                            run_m[i] = -m, minus[i] = -log2f(s);
                             factor[i] = args.grad_scale * (args.grad_loss ? args.grad_loss[at] : 1.0f) * (args.range ? args.range[0] : 1.0f);
                         }
                         ask[i] = MASK && inside ? args.asks[at] : make_int4(0, 0, 0, 0);
@@ -497,9 +504,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     __syncwarp();
                 }
                 // p f of two columns in one word
-                auto word = [&](uint32_t x0, uint32_t x1, float from, float by, bool none) {
+                auto word = [&](uint32_t x0, uint32_t x1, float from, float less, float by, bool none) {
                     float e0, e1;
-                    fma2_to(e0, e1, __uint_as_float(x0), __uint_as_float(x1), args.c, from);
+                    apart2(e0, e1, x0, x1, from, args.c, less);
                     e0 = exp2_fast(e0), e1 = exp2_fast(e1);
                     mul2(e0, e1, by, by);
                     const uint32_t w = pack2(e0, e1, T());
@@ -524,7 +531,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                                 for (int j = 0; j < 4; ++j) {
                                     const int line = row_at(i) % 32, x = 4 * j + 2 * (i % 2);
                                     asm volatile("st.shared.b32 [%0], %1;" ::"r"(box + line * 128 + (((4 * sub + j) ^ (line & 7)) << 4) + lane % 4 * 4),
-                                                 "r"(word(v[i / 2][x], v[i / 2][x + 1], minus[i], factor[i], dead[i]))
+                                                 "r"(word(v[i / 2][x], v[i / 2][x + 1], run_m[i], minus[i], factor[i], dead[i]))
                                                  : "memory");
                                 }
                         }
@@ -544,8 +551,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             const uint32_t(&x)[32] = v[j / 4];
                             const int k = 8 * (j % 4);
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)),
-                                         "r"(word(x[k], x[k + 1], minus[0], factor[0], dead[0])), "r"(word(x[k + 2], x[k + 3], minus[0], factor[0], dead[0])), "r"(word(x[k + 4], x[k + 5], minus[0], factor[0], dead[0])),
-                                         "r"(word(x[k + 6], x[k + 7], minus[0], factor[0], dead[0]))
+                                         "r"(word(x[k], x[k + 1], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 2], x[k + 3], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 4], x[k + 5], run_m[0], minus[0], factor[0], dead[0])),
+                                         "r"(word(x[k + 6], x[k + 7], run_m[0], minus[0], factor[0], dead[0]))
                                          : "memory");
                         }
                     }
@@ -871,7 +878,7 @@ __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ Patc
     }
     sum = lanes_sum(sum, lanes);
     if (!inside || !(sum > 0.0f)) return;
-    const float minus = -fmaf(stats[0], p.c, log2f(stats[1]));
+    const float m = stats[0], minus = -log2f(stats[1]);
     const float factor = p.grad_scale * (p.grad_loss ? p.grad_loss[at] : 1.0f) * (p.range ? p.range[0] : 1.0f);
     for (int j = sub; j < p.k; j += lanes) {
         const int id = ids[j];
@@ -881,7 +888,7 @@ __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ Patc
             const float t = teacher ? teacher[l] : 0.0f;
             if (ids[l] == id && t > neg_inf()) q += exp2_fast((t - top) * p.c);
         }
-        const float prob = exp2_fast(fmaf(stats[2 + j], p.c, minus));
+        const float prob = exp2_fast(fmaf(stats[2 + j] - m, p.c, minus));
         static_cast<T *>(p.grad)[g * p.grad_group_stride + row * p.grad_stride + id - p.host0] = from_float<T>((prob - q / sum) * factor);
     }
 }

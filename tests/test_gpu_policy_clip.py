@@ -220,6 +220,14 @@ def test_clip_gradients(nb):
     for p, b in zip(net.parameters(), before):
         torch.testing.assert_close(p.grad.double(), b.double() * factor, rtol=14 * E, atol=0.0)
     assert float(policy.clip_gradients(unused, 1.0)) == 0.0
+    # a shared parameter counts once; a gradient that is laid out otherwise is clipped as it lies
+    p, q = torch.nn.Parameter(torch.ones(3, 5, device="cuda")), torch.nn.Parameter(torch.ones(4, 6, device="cuda"))
+    p.grad, q.grad = torch.full((3, 5), 2.0, device="cuda"), torch.full((6, 4), 3.0, device="cuda").t()
+    norm = policy.clip_gradients([p, q, p], 1.0)
+    want = math.sqrt(15 * 4.0 + 24 * 9.0)
+    assert abs(float(norm) - want) <= 11 * E * want and not q.grad.is_contiguous()
+    torch.testing.assert_close(p.grad, torch.full_like(p.grad, 2.0 / want), rtol=1e-6, atol=0.0)
+    torch.testing.assert_close(q.grad, torch.full_like(q.grad, 3.0 / want), rtol=1e-6, atol=0.0)
     assert float(policy.clip_gradients(net.parameters(), 1.0, math.inf)) == max(float(p.grad.abs().max()) for p in net.parameters())
 
 
@@ -230,6 +238,15 @@ def test_the_binding_refuses_wrong_tensors(nb):
                              ([x, 3.0], TypeError, "get_device"), ([x.cpu()], ValueError, "cuda")):
         with pytest.raises(error, match=word):
             nb.nbos_policy_clip(bad, 1.0, norm)
+    with pytest.raises(ValueError, match="twice"):
+        nb.nbos_policy_clip([x, x], 1.0, norm, [x, x])
+    two = [x, x]
+    with pytest.raises(ValueError, match="twice"):
+        nb.nbos_policy_clip(two, 1.0, norm, two)
+    nb.nbos_policy_clip(two, 1.0, norm)   # reading it twice is a sum like any other
+    assert abs(float(norm) - math.sqrt(32.0)) <= 11 * E * 6
+    empty = torch.empty(0, device="cuda")
+    nb.nbos_policy_clip([empty, x, empty], 1.0, norm, [empty, x.clone(), empty])
     for outs, word in (([x, x], "each"), ([x[:2]], "sizes"), ([x.half()], "sizes"), ([x.cpu()], "live on")):
         with pytest.raises(ValueError, match=word):
             nb.nbos_policy_clip([x], 1.0, norm, outs)

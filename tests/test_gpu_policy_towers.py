@@ -174,6 +174,43 @@ def test_gradients_in_pieces(nb, groups, rows, hosts, width, what):
     check(nb, make(groups, rows, hosts, width, 3, "bfloat16", True, 5), 1.0, 1.0)
 
 
+@pytest.mark.parametrize("T", [1e-36, 1e-3, 50.0])
+@pytest.mark.parametrize("mask,k", [(False, 3), (True, 3), (False, 9)])
+def test_temperatures(nb, T, mask, k):
+    """Far below 1 all weight is on the best host: p is 0 or 1 wherever two logits differ by more than 200 T. Rows whose two best, or
+    whose entries' best teacher logits, are that close are left out of the comparison (logits are compared exactly there)."""
+    import torch
+    c = make(1, 200, 700, 32, k, "bfloat16", mask, 21)
+    scale = 1.0 / T if T < 1 else 1.0
+    if T > 1e-30:
+        check(nb, c, T, scale)
+        return
+    loss, da, db = run(nb, c, T, scale, None)
+    a, b = c["requests"][0].double(), c["host_vectors"][0].double()
+    x = a @ b.T
+    if mask:
+        x[(c["asks"][0][:, None] > c["room"][0][None]).any(-1) | (c["asks"][0] < 0).any(-1)[:, None]] = -INF
+    ids = c["hosts"][0].long()
+    inside = (ids >= 0) & (ids < 700)
+    at = x.gather(1, ids * inside)
+    t = torch.where(inside & (at > -INF), c["teacher_logits"][0].double(), -INF)
+    some = (t > -INF).any(1)
+    best, teacher_best = x.argmax(1), (ids * inside).gather(1, t.argmax(1, keepdim=True))[:, 0]
+    G = torch.zeros_like(x)
+    rows = torch.arange(200, device="cuda")
+    G[rows, best] += 1.0
+    G[rows, teacher_best] -= 1.0
+    G *= some[:, None]
+    clear = ~some | ((x.topk(2, 1).values.diff(dim=1)[:, 0] < -1e-3) & (t.topk(2, 1).values.diff(dim=1)[:, 0] < -1e-3))
+    assert int(clear.sum()) > 150
+    # q = 1 at one host, ln p = (x there - the largest) / T: T^2 times that is T times the difference. A logit is off by at most
+    # 32 2^-23 sum |a_i b_i| < 3e-4 (the sums stay below 70).
+    want_loss = torch.where(some, x.amax(1) - x[rows, teacher_best], torch.zeros((), dtype=torch.float64, device="cuda"))
+    assert ((loss[0].double() / T - want_loss).abs() <= 6e-4 + 1e-5 * want_loss)[clear].all()
+    want = G @ b
+    assert ((da[0].double() - want).abs() <= 3 * 2.0 ** -8 * (G.abs() @ b.abs()) + 1e-9)[clear].all()
+
+
 def test_long_lists_of_hosts(nb):
     c = make(1, 60, 500, 96, 256, "float16", True, 3)
     c["hosts"][:, 5] = 17                 # one host 256 times
