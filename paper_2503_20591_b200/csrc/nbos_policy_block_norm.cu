@@ -5,101 +5,132 @@ namespace nbos {
 namespace block_norm {
 namespace {
 
-template <typename T, int VEC, int CH, bool BLOCK, bool WIDE, Gate GATE>
+template <typename T, int CH, bool BLOCK, bool WIDE, bool ANY, Gate GATE>
 __global__ void __maxnreg__((kForwardRegs<WIDE>)) forward_kernel(const __grid_constant__ BlockArgs a, int team, int ahead)
 {
+    constexpr int VEC = kPer16<T>, TABLES = ANY && GATE == ROW_GATE ? 3 : 2;   // branch, residual, and a gate that may start anywhere
+    using Ring = Ahead<T, VEC, CH, BLOCK, WIDE, ANY>;
     __shared__ float4 warps[2][8];
     extern __shared__ uint4 staged_words[];
     char *const staged = reinterpret_cast<char *>(staged_words);
-    using Ring = Ahead<T, VEC, CH, WIDE>;
     int half = 0;
     const int teams = BLOCK ? 1 : blockDim.x / team, t = BLOCK ? threadIdx.x : threadIdx.x % team, mine = BLOCK ? 0 : threadIdx.x / team;
-    const Columns c(team, t, a.width, VEC);
-    float *const post = reinterpret_cast<float *>(staged + ahead * 2 * Ring::kRowBytes * (int)blockDim.x), *const pre = post + team * CH * VEC;
+    const Columns c(team, t, a.width, VEC, mine, teams);
+    const int staged_bytes = Ring::bytes(ahead, TABLES, team, teams);
+    float *const post = reinterpret_cast<float *>(staged + staged_bytes), *const pre = post + team * CH * VEC;
     if (BLOCK) {
         if (threadIdx.x < 16) warps[threadIdx.x / 8][threadIdx.x % 8] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         __syncthreads();
     }
+    const bool gate_staged = Ring::kStaged && TABLES == 3 && (sizeof(T) == 4 || !a.gate_f32);
     auto of = [&](const void *table, long long stride, unsigned int row) { return static_cast<const T *>(table) + row * stride; };
     auto fetch = [&](long long first, long long end, int stage) {
         if (!Ring::kStaged) return;
         if (first < end) {
             const unsigned int row = (unsigned int)(first + mine < end ? first + mine : first);
-            Ring::copy(staged, 2 * stage, of(a.y, a.y_stride, row), of(a.x, a.x_stride, row), c);
+            Ring::copy(staged, TABLES * stage, of(a.y, a.y_stride, row), row * a.y_stride, c);
+            Ring::copy(staged, TABLES * stage + 1, of(a.x, a.x_stride, row), row * a.x_stride, c);
+            if (gate_staged) Ring::copy(staged, TABLES * stage + 2, static_cast<const T *>(gate_at<T>(a, row)), row * a.gate_stride, c);
         }
         copies_commit();
     };
-    Ring::clear(staged, ahead * 2);
+    Ring::clear(staged, staged_bytes);
     const Rows rows(a, GATE == SHARED_GATE);
     if (BLOCK || mine == 0) fill_weights<T, VEC, CH>(pre, a.pre, a.weight_f32, nullptr, false, team, t, a.width);
     for (unsigned int gi = rows.gate_from; gi < rows.gate_to; ++gi) {
-    const long long end = (long long)gi * rows.per_gate + rows.part_to;
-    long long first = (long long)gi * rows.per_gate + rows.part_from;
-    for (int i = 0; i < ahead; ++i) fetch(first + i * teams, end, i);
-    if (!BLOCK) __syncthreads();   // the gate before is done with
-    if (BLOCK || mine == 0)
-        fill_weights<T, VEC, CH>(post, a.post, a.weight_f32, GATE == SHARED_GATE ? gate_at<T>(a, gi) : nullptr, a.gate_f32, team, t, a.width);
-    if (!BLOCK) __syncthreads();   // (a block's threads read their own columns)
-    int stage = 0;
-    for (; first < end; first += teams) {
-        const bool inside = first + mine < end;
-        const unsigned int row = (unsigned int)(inside ? first + mine : first);
-        const T *x = of(a.x, a.x_stride, row), *y = of(a.y, a.y_stride, row);
-        float r[CH][VEC], s[2] = {0.0f, 0.0f};
-        Ring::wait(ahead);
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            Ring::read(r[k], staged, 2 * stage, k, y, c);
-            dot_all(s, r[k], r[k]);
-        }
-        const float root_y = rsqrtf(fmaf(row_sum<BLOCK, WIDE>(s[0] + s[1], team, warps, half), a.per_width, a.eps));
-        s[0] = s[1] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            float w[VEC];
-            scale_all(r[k], root_y);
-            weights(w, post, k, team, t);
-            mul_all(r[k], w);
-            if (GATE == ROW_GATE) {
-                get_either<T, VEC>(w, gate_at<T>(a, row), a.gate_f32, k, c);
-                mul_all(r[k], w);
+        const long long end = (long long)gi * rows.per_gate + rows.part_to;
+        long long first = (long long)gi * rows.per_gate + rows.part_from;
+        if (ANY) team_sync<BLOCK>();   // the gate's rows before have left
+        for (int i = 0; i < (ANY ? 1 : ahead); ++i) fetch(first + i * teams, end, i);
+        if (!BLOCK) __syncthreads();   // the gate before is done with
+        if (BLOCK || mine == 0)
+            fill_weights<T, VEC, CH>(post, a.post, a.weight_f32, GATE == SHARED_GATE ? gate_at<T>(a, gi) : nullptr, a.gate_f32, team, t, a.width);
+        if (!BLOCK) __syncthreads();   // (a block's threads read their own columns)
+        int stage = 0;
+        for (; first < end; first += teams) {
+            const bool inside = first + mine < end;
+            const unsigned int row = (unsigned int)(inside ? first + mine : first);
+            const T *x = of(a.x, a.x_stride, row), *y = of(a.y, a.y_stride, row);
+            float r[CH][VEC], s[2] = {0.0f, 0.0f};
+            if (Ring::kStaged && ANY) {
+                copies_wait<0>();
+                team_sync<BLOCK>();    // all of the row is there, and all of the row before has left
+                if (ahead == 2) fetch(first + teams, end, stage ^ 1);
+            } else if (Ring::kStaged) {
+                if (ahead == 2)
+                    copies_wait<1>();
+                else
+                    copies_wait<0>();
             }
-            Ring::read(w, staged, 2 * stage + 1, k, x, c);
-            add_scaled(r[k], w, a.alpha);
-            dot_all(s, r[k], r[k]);
-        }
-        fetch(first + (long long)ahead * teams, end, stage);
-        stage = stage + 1 == ahead ? 0 : stage + 1;
-        const float root_r = rsqrtf(fmaf(row_sum<BLOCK, WIDE>(s[0] + s[1], team, warps, half), a.per_width, a.eps));
-        if (!inside) continue;
-        if (a.stats && t == 0) a.stats[2ll * row] = root_y, a.stats[2ll * row + 1] = root_r;
 #pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            if (a.out) put<T, VEC>(static_cast<T *>(a.out) + row * a.out_stride, r[k], k, c);
-            if (a.normed) {
+            for (int k = 0; k < CH; ++k) {
+                Ring::read(r[k], staged, TABLES * stage, k, y, c);
+                dot_all(s, r[k], r[k]);
+            }
+            const float root_y = rsqrtf(fmaf(row_sum<BLOCK, WIDE>(s[0] + s[1], team, warps, half), a.per_width, a.eps));
+            s[0] = s[1] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
                 float w[VEC];
-                weights(w, pre, k, team, t);
-                scale_all(r[k], root_r);
+                scale_all(r[k], root_y);
+                weights(w, post, k, team, t);
                 mul_all(r[k], w);
-                put<T, VEC>(static_cast<T *>(a.normed) + row * a.normed_stride, r[k], k, c);
+                if (GATE == ROW_GATE) {
+                    if (gate_staged)
+                        Ring::read(w, staged, TABLES * stage + 2, k, static_cast<const T *>(gate_at<T>(a, row)), c);
+                    else
+                        get_either<T, VEC, ANY>(w, gate_at<T>(a, row), a.gate_f32, k, c);
+                    mul_all(r[k], w);
+                }
+                Ring::read(w, staged, TABLES * stage + 1, k, x, c);
+                add_scaled(r[k], w, a.alpha);
+                dot_all(s, r[k], r[k]);
             }
+            if (Ring::kStaged && !ANY) fetch(first + (long long)ahead * teams, end, stage);
+            const float root_r = rsqrtf(fmaf(row_sum<BLOCK, WIDE>(s[0] + s[1], team, warps, half), a.per_width, a.eps));
+            if (Ring::kStaged && ANY) team_sync<BLOCK>();   // results take the place of what has been read
+            T *const out = static_cast<T *>(a.out) + row * a.out_stride, *const normed = static_cast<T *>(a.normed) + row * a.normed_stride;
+            if (inside) {
+                if (a.stats && t == 0) a.stats[2ll * row] = root_y, a.stats[2ll * row + 1] = root_r;
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+                    if (a.out) Ring::write(out, staged, TABLES * stage, r[k], k, c);
+                    if (a.normed) {
+                        float w[VEC];
+                        weights(w, pre, k, team, t);
+                        scale_all(r[k], root_r);
+                        mul_all(r[k], w);
+                        Ring::write(normed, staged, TABLES * stage + 1, r[k], k, c);
+                    }
+                }
+            }
+            if (Ring::kStaged && ANY) {
+                team_sync<BLOCK>();
+                if (inside && a.out) Ring::row_out(out, staged, TABLES * stage, c);
+                if (inside && a.normed) Ring::row_out(normed, staged, TABLES * stage + 1, c);
+                if (ahead == 1) {
+                    team_sync<BLOCK>();
+                    fetch(first + teams, end, 0);
+                }
+            }
+            stage = stage + 1 == ahead ? 0 : stage + 1;
         }
-    }
     }
 }
 
 template <typename T, Gate GATE>
 cudaError_t run_forward(const BlockArgs &args, const Shape &s, int sms, cudaStream_t stream)
 {
-    return by_shape<T>(s, [&](auto vec, auto chunks, auto block, auto wide) -> cudaError_t {
-        auto *kernel = forward_kernel<T, vec(), chunks(), block(), wide(), GATE>;
+    return by_shape<T>(s, [&](auto chunks, auto block, auto wide, auto any) -> cudaError_t {
+        auto *kernel = forward_kernel<T, chunks(), block(), wide(), any(), GATE>;
         static const int regs = kernel_registers(kernel);
-        using Ring = Ahead<T, vec(), chunks(), wide()>;
-        const int ahead = Ring::rows(2, s.threads), shared = ahead * 2 * Ring::kRowBytes * s.threads + 2 * s.team * vec() * chunks() * (int)sizeof(float);
+        using Ring = Ahead<T, kPer16<T>, chunks(), block(), wide(), any()>;
+        const int tables = any() && GATE == ROW_GATE ? 3 : 2, teams = s.threads / s.team, ahead = Ring::rows(tables, s.team, teams);
+        const int shared = Ring::bytes(ahead, tables, s.team, teams) + 2 * s.team * kPer16<T> * chunks() * (int)sizeof(float);
         const cudaError_t e = allow_shared(kernel, shared);
         if (e != cudaSuccess) return e;
         BlockArgs a = args;
-        const Split split = split_rows(a.rows, a.rows_per_gate, GATE == SHARED_GATE, s.threads / s.team, (long long)sms * resident_blocks(regs, s.threads, shared + 512));
+        const Split split = split_rows(a.rows, a.rows_per_gate, GATE == SHARED_GATE, teams, (long long)sms * resident_blocks(regs, s.threads, shared + 512));
         a.blocks_per_gate = split.share;
         kernel<<<(unsigned int)split.blocks, s.threads, shared, stream>>>(a, s.team, ahead);
         return cudaGetLastError();

@@ -53,87 +53,64 @@ __device__ __forceinline__ float one_value(const void *p, long long i, bool f32,
     return f32 ? static_cast<const float *>(p)[i] : to_float(static_cast<const T *>(p)[i]);
 }
 
-// VEC neighbours that lie in memory as 16 bytes, 4 bytes or one value
-template <typename T, int VEC>
-__device__ __forceinline__ void unpack(float (&v)[VEC], const void *at)
-{
-    if constexpr (VEC == kPer16<T>) {
-        unpack16(*static_cast<const uint4 *>(at), v, T());
-    } else if constexpr (VEC == 2 && sizeof(T) == 2) {
-        const unsigned int w = *static_cast<const unsigned int *>(at);
-        const unsigned short lo = (unsigned short)w, hi = (unsigned short)(w >> 16);
-        v[0] = to_float(*reinterpret_cast<const T *>(&lo)), v[1] = to_float(*reinterpret_cast<const T *>(&hi));
-    } else {
-        v[0] = to_float(*static_cast<const T *>(at));
-    }
-}
-// The columns of a thread: pieces of VEC, `team` of them apart. Piece k is whole, or the row's last and cut off, or behind it.
+// The columns of a thread: pieces of 16 bytes' worth of values (VEC), `team` of them apart. Piece k is whole, or the row's last and cut off,
+// or behind it. `mine`: which of the block's teams the thread is in.
 struct Columns {
-    int team, t, width, whole, rest;
-    __device__ __forceinline__ Columns(int team_, int t_, int width_, int vec) : team(team_), t(t_), width(width_), whole(width_ / vec - t_), rest(width_ % vec) {}
+    int team, t, width, whole, rest, mine, teams;
+    __device__ __forceinline__ Columns(int team_, int t_, int width_, int vec, int mine_, int teams_)
+        : team(team_), t(t_), width(width_), whole(width_ / vec - t_), rest(width_ % vec), mine(mine_), teams(teams_)
+    {
+    }
     __device__ __forceinline__ bool is_whole(int k) const { return k * team < whole; }
     __device__ __forceinline__ bool is_cut(int k) const { return rest != 0 && k * team == whole; }
 };
-// piece k of a row, 0 behind its end
-template <typename T, int VEC>
+// Piece k of a row, 0 behind its end. ANY: the row may start anywhere, else on a 16-byte boundary.
+template <typename T, int VEC, bool ANY>
 __device__ __forceinline__ void get(float (&v)[VEC], const T *row, int k, const Columns &c)
 {
     const T *at = row + (k * c.team + c.t) * VEC;
-    if (c.is_whole(k)) {
-        unpack<T, VEC>(v, at);
+    if (!ANY && c.is_whole(k)) {
+        unpack16(*reinterpret_cast<const uint4 *>(at), v, T());
     } else {
+        const int n = c.is_whole(k) ? VEC : c.is_cut(k) ? c.rest : 0;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = 0.0f;
-        if (VEC > 1 && c.is_cut(k)) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (i < c.rest) v[i] = to_float(at[i]);
-        }
+        for (int i = 0; i < VEC; ++i) v[i] = i < n ? to_float(at[i]) : 0.0f;
     }
 }
-template <typename T, int VEC>
+template <typename T, int VEC, bool ANY>
 __device__ __forceinline__ void get_either(float (&v)[VEC], const void *row, bool f32, int k, const Columns &c)
 {
     if (sizeof(T) == 2 && f32) {
         const float *p = static_cast<const float *>(row) + (k * c.team + c.t) * VEC;
-        if (VEC % 4 == 0 && c.is_whole(k)) {
-            if constexpr (VEC % 4 == 0) {
+        if (!ANY && c.is_whole(k)) {
 #pragma unroll
-                for (int i = 0; i < VEC; i += 4) {
-                    const float4 w = *reinterpret_cast<const float4 *>(p + i);
-                    v[i] = w.x, v[i + 1] = w.y, v[i + 2] = w.z, v[i + 3] = w.w;
-                }
+            for (int i = 0; i < VEC; i += 4) {
+                const float4 w = *reinterpret_cast<const float4 *>(p + i);
+                v[i] = w.x, v[i + 1] = w.y, v[i + 2] = w.z, v[i + 3] = w.w;
             }
-            return;
-        }
-        const int n = c.is_whole(k) ? VEC : c.is_cut(k) ? c.rest : 0;
+        } else {
+            const int n = c.is_whole(k) ? VEC : c.is_cut(k) ? c.rest : 0;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = i < n ? p[i] : 0.0f;
+            for (int i = 0; i < VEC; ++i) v[i] = i < n ? p[i] : 0.0f;
+        }
     } else {
-        get<T, VEC>(v, static_cast<const T *>(row), k, c);
+        get<T, VEC, ANY>(v, static_cast<const T *>(row), k, c);
     }
 }
-template <typename T, int VEC>
+template <typename T, int VEC, bool ANY>
 __device__ __forceinline__ void put(T *row, const float (&v)[VEC], int k, const Columns &c)
 {
     T *at = row + (k * c.team + c.t) * VEC;
-    if (c.is_whole(k)) {
-        if constexpr (VEC == kPer16<T>) {
-            *reinterpret_cast<uint4 *>(at) = pack16(v, T());
-        } else if constexpr (VEC == 2 && sizeof(T) == 2) {
-            const T lo = from_float<T>(v[0]), hi = from_float<T>(v[1]);
-            *reinterpret_cast<unsigned int *>(at) =
-                *reinterpret_cast<const unsigned short *>(&lo) | (unsigned int)*reinterpret_cast<const unsigned short *>(&hi) << 16;
-        } else {
-            at[0] = from_float<T>(v[0]);
-        }
-    } else if (VEC > 1 && c.is_cut(k)) {
+    if (!ANY && c.is_whole(k)) {
+        *reinterpret_cast<uint4 *>(at) = pack16(v, T());
+    } else {
+        const int n = c.is_whole(k) ? VEC : c.is_cut(k) ? c.rest : 0;
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
-            if (i < c.rest) at[i] = from_float<T>(v[i]);
+            if (i < n) at[i] = from_float<T>(v[i]);
     }
 }
-template <typename T, int VEC>
+template <typename T, int VEC, bool ANY>
 __device__ __forceinline__ void put_either(void *row, bool f32, const float (&v)[VEC], int k, const Columns &c)
 {
     if (sizeof(T) == 2 && f32) {
@@ -143,7 +120,7 @@ __device__ __forceinline__ void put_either(void *row, bool f32, const float (&v)
         for (int i = 0; i < VEC; ++i)
             if (i < n) at[i] = v[i];
     } else {
-        put<T, VEC>(static_cast<T *>(row), v, k, c);
+        put<T, VEC, ANY>(static_cast<T *>(row), v, k, c);
     }
 }
 
@@ -168,95 +145,126 @@ __device__ __forceinline__ float row_sum(float v, int team, float4 (*warps)[8], 
     return v;
 }
 
-// Rows to come, copied ahead into shared memory: each thread copies the pieces that it will read itself, so no barrier is needed, and
-// reads them again in each pass over the row rather than keep them. (Loads into registers: 8 x 8,192 x 2,048 bf16 forward
-// 316 us, backward 651; staged, with 8 values a thread, 256 and 511; with 16 values, 217 and 545, and then as below.) Single values of 16 bits cannot be
-// copied like that: they are loaded and put there. Rows beyond 8,192 values do not fit: they come from memory and then from the L1 cache.
-template <typename T, int VEC, int CH, bool WIDE>
-struct Ahead {
-    static constexpr int kPiece = VEC * (int)sizeof(T);
-    static constexpr bool kStaged = !WIDE;
-    static constexpr int kRowBytes = kStaged ? CH * kPiece : 0;   // a thread's, per table
-
-    // Two rows where a thread's pieces are 16 bytes and there is room for two blocks, else one: more rows take shared memory from more
-    // blocks (8 x 8,192 x 2,048 bf16 backward one row ahead 321 us, two 312, three 339; 4,099 x 2,050 f16 112, 116, 147).
-    static int rows(int tables, int threads) { return kPiece == 16 && 2 * tables * kRowBytes * threads <= 100 * 1024 ? 2 : 1; }
-    static __device__ __forceinline__ void wait(int rows)
-    {
-        if (!kStaged) return;
-        if (rows == 2)
-            copies_wait<1>();
-        else
-            copies_wait<0>();
+// 16 of the 32 bytes lo, hi, from byte `from` on
+__device__ __forceinline__ uint4 window16(const uint4 &lo, const uint4 &hi, int from)
+{
+    unsigned int w[7] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z};
+    if (from & 8) w[0] = w[2], w[1] = w[3], w[2] = w[4], w[3] = w[5], w[4] = w[6], w[5] = hi.w;
+    if (from & 4) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = w[4], w[4] = w[5];
+    if (from & 3) {
+        const int bits = (from & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
     }
-    static __device__ __forceinline__ int slot(int table, int k)   // table: of all rows' tables
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <bool BLOCK>
+__device__ __forceinline__ void team_sync()
+{
+    if (BLOCK)
+        __syncthreads();
+    else
+        __syncwarp();
+}
+
+// Rows to come, copied ahead into shared memory and read there again in each pass rather than kept. (Loads into registers, 8 x
+// 8,192 x 2,048 bf16: forward 316 us, backward 651; staged, with 8 values a thread, 256 and 511; with 16 values, 217 and 545, and then as
+// below.) Rows on 16-byte boundaries: each thread copies the pieces that it reads itself, so no barrier is needed. ANY, rows that start
+// anywhere: a team copies the row with the bytes from the boundary before it, a thread puts its pieces together from two neighbours of 16 bytes,
+// and results go the same way back (in pieces of 4 bytes or single values, without: 4,099 x 2,050 f16, forward 45 us, backward 103; this
+// FIXME). Rows that do not fit (beyond 8,192 values, or nearly that many of 32 bits) come from memory and then from the L1 cache.
+template <typename T, int VEC, int CH, bool BLOCK, bool WIDE, bool ANY>
+struct Ahead {
+    static constexpr bool kStaged = !WIDE;
+
+    static __host__ __device__ __forceinline__ int region(int team) { return (CH * team + (ANY ? 2 : 0)) * 16; }   // bytes of a row
+    static __host__ __device__ __forceinline__ int bytes(int rows, int tables, int team, int teams)
     {
-        return ((table * CH + k) * (int)blockDim.x + (int)threadIdx.x) * kPiece;
+        return kStaged ? rows * tables * teams * region(team) : 0;
+    }
+    // Two rows where there is room for two blocks, else one: more rows take shared memory from more blocks (8 x 8,192 x 2,048 bf16
+    // backward one row ahead 321 us, two 312, three 339).
+    static int rows(int tables, int team, int teams) { return bytes(2, tables, team, teams) <= 100 * 1024 ? 2 : 1; }
+
+    static __device__ __forceinline__ char *row_at(char *shared, int table, const Columns &c)   // table: of all rows' tables
+    {
+        return shared + (table * c.teams + c.mine) * region(c.team);
     }
     // what lies behind a row's end stays 0 in all of them
-    static __device__ __forceinline__ void clear(char *shared, int tables)
+    static __device__ __forceinline__ void clear(char *shared, int bytes)
     {
         if constexpr (kStaged) {
-            for (int n = 0; n < tables * CH; ++n) {
-                char *at = shared + (n * (int)blockDim.x + (int)threadIdx.x) * kPiece;
-                if constexpr (kPiece == 16)
-                    *reinterpret_cast<uint4 *>(at) = make_uint4(0, 0, 0, 0);
-                else if constexpr (kPiece == 4)
-                    *reinterpret_cast<unsigned int *>(at) = 0u;
-                else
-                    *reinterpret_cast<unsigned short *>(at) = 0;
-            }
+            for (int i = threadIdx.x; i < bytes / 16; i += blockDim.x) reinterpret_cast<uint4 *>(shared)[i] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
         }
     }
-    // two tables' rows at a time (either may be NULL)
-    static __device__ __forceinline__ void copy(char *shared, int table, const T *row, const T *row2, const Columns &c)
+    // offset: of the row in its table
+    static __device__ __forceinline__ void copy(char *shared, int table, const T *row, long long offset, const Columns &c)
     {
-        if constexpr (kStaged && kPiece == 2) {   // single values: loaded, all under way together, and put there
-            unsigned short v[2][CH];
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const T *from = (n == 0 ? row : row2);
-#pragma unroll
-                for (int k = 0; k < CH; ++k) v[n][k] = from && c.is_whole(k) ? reinterpret_cast<const unsigned short *>(from)[k * c.team + c.t] : (unsigned short)0;
-            }
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int k = 0; k < CH; ++k) *reinterpret_cast<unsigned short *>(shared + slot(table + n, k)) = v[n][k];
-        } else {
-            if (row) copy_one(shared, table, row, c);
-            if (row2) copy_one(shared, table + 1, row2, c);
-        }
-    }
-    static __device__ __forceinline__ void copy_one(char *shared, int table, const T *row, const Columns &c)
-    {
-        if constexpr (kStaged && kPiece >= 4) {
-            const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(shared + slot(table, 0)));
+        if constexpr (kStaged && ANY) {
+            stage_row(row_at(shared, table, c), row, c.width, offset * (long long)sizeof(T), c.t, c.team);
+        } else if constexpr (kStaged) {
+            const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(row_at(shared, table, c))) + c.t * 16;
             const T *from = row + c.t * VEC;
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
-                const uint32_t at = to + k * (int)blockDim.x * kPiece;
-                if (c.is_whole(k)) {
-                    if constexpr (kPiece == 16)
-                        copy_async16(at, from + k * c.team * VEC);
-                    else
-                        copy_async4(at, from + k * c.team * VEC);
-                } else if (VEC > 1 && c.is_cut(k)) {
-                    const int bytes = c.rest * (int)sizeof(T);
-                    if constexpr (kPiece == 16)
-                        copy_async16(at, from + k * c.team * VEC, bytes);
-                    else
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at), "l"(from + k * c.team * VEC), "r"(bytes) : "memory");
+                if (c.is_whole(k))
+                    copy_async16(to + k * c.team * 16, from + k * c.team * VEC);
+                else if (c.is_cut(k))
+                    copy_async16(to + k * c.team * 16, from + k * c.team * VEC, c.rest * (int)sizeof(T));
+            }
+        }
+    }
+    static __device__ __forceinline__ void read(float (&v)[VEC], char *shared, int table, int k, const T *row, const Columns &c)
+    {
+        if constexpr (!kStaged) {
+            get<T, VEC, ANY>(v, row, k, c);
+        } else {
+            const uint4 *at = reinterpret_cast<const uint4 *>(row_at(shared, table, c)) + k * c.team + c.t;
+            if constexpr (!ANY) {
+                unpack16(*at, v, T());
+            } else {
+                if (c.is_whole(k) || c.is_cut(k)) {
+                    const int shift = row_shift(row);
+                    uint4 piece = *at;
+                    if (shift) piece = window16(piece, at[1], shift);
+                    unpack16(piece, v, T());
+                }
+                if (!c.is_whole(k)) {
+                    const int n = c.is_cut(k) ? c.rest : 0;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) v[i] = i < n ? v[i] : 0.0f;
                 }
             }
         }
     }
-    static __device__ __forceinline__ void read(float (&v)[VEC], const char *shared, int table, int k, const T *row, const Columns &c)
+    // A result's piece: to memory at once, or (ANY) to shared memory, in place of a table that has been read, and from there by row_out.
+    static __device__ __forceinline__ void write(T *row, char *shared, int table, const float (&v)[VEC], int k, const Columns &c)
     {
-        if constexpr (kStaged)
-            unpack<T, VEC>(v, shared + slot(table, k));
-        else
-            get<T, VEC>(v, row, k, c);
+        if constexpr (kStaged && ANY) {
+            if (c.is_whole(k) || c.is_cut(k)) reinterpret_cast<uint4 *>(row_at(shared, table, c))[k * c.team + c.t] = pack16(v, T());
+        } else {
+            put<T, VEC, ANY>(row, v, k, c);
+        }
+    }
+    static __device__ __forceinline__ void row_out(T *row, char *shared, int table, const Columns &c)
+    {
+        if constexpr (kStaged && ANY) {
+            const char *from = row_at(shared, table, c);
+            const int shift = row_shift(row), total = shift + c.width * (int)sizeof(T);
+            char *to = reinterpret_cast<char *>(row) - shift;
+            for (int g = c.t; g * 16 < total; g += c.team) {
+                if (g * 16 >= shift && g * 16 + 16 <= total) {
+                    const uint4 *at = reinterpret_cast<const uint4 *>(from) + g;
+                    uint4 piece = *at;
+                    if (shift) piece = window16(at[-1], piece, 16 - shift);
+                    *reinterpret_cast<uint4 *>(to + g * 16) = piece;
+                } else {
+                    for (int i = g * 16; i < g * 16 + 16; i += (int)sizeof(T))
+                        if (i >= shift && i < total) *reinterpret_cast<T *>(to + i) = *reinterpret_cast<const T *>(from + i - shift);
+                }
+            }
+        }
     }
 };
 
@@ -264,42 +272,26 @@ struct Ahead {
 template <int VEC>
 __device__ __forceinline__ void mul_all(float (&v)[VEC], const float (&w)[VEC])
 {
-    if constexpr (VEC == 1) {
-        v[0] *= w[0];
-    } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 2) mul2(v[i], v[i + 1], w[i], w[i + 1]);
-    }
+    for (int i = 0; i < VEC; i += 2) mul2(v[i], v[i + 1], w[i], w[i + 1]);
 }
 template <int VEC>
 __device__ __forceinline__ void dot_all(float (&s)[2], const float (&a)[VEC], const float (&b)[VEC])
 {
-    if constexpr (VEC == 1) {
-        s[0] = fmaf(a[0], b[0], s[0]);
-    } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 2) fma2(s[0], s[1], a[i], a[i + 1], b[i], b[i + 1]);
-    }
+    for (int i = 0; i < VEC; i += 2) fma2(s[0], s[1], a[i], a[i + 1], b[i], b[i + 1]);
 }
 template <int VEC>
 __device__ __forceinline__ void add_product(float (&s)[VEC], const float (&a)[VEC], const float (&b)[VEC])   // s += a b
 {
-    if constexpr (VEC == 1) {
-        s[0] = fmaf(a[0], b[0], s[0]);
-    } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 2) fma2(s[i], s[i + 1], a[i], a[i + 1], b[i], b[i + 1]);
-    }
+    for (int i = 0; i < VEC; i += 2) fma2(s[i], s[i + 1], a[i], a[i + 1], b[i], b[i + 1]);
 }
 template <int VEC>
 __device__ __forceinline__ void add_scaled(float (&s)[VEC], const float (&a)[VEC], float f)   // s += a f
 {
-    if constexpr (VEC == 1) {
-        s[0] = fmaf(a[0], f, s[0]);
-    } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 2) fma2(s[i], s[i + 1], a[i], a[i + 1], f, f);
-    }
+    for (int i = 0; i < VEC; i += 2) fma2(s[i], s[i + 1], a[i], a[i + 1], f, f);
 }
 
 
@@ -349,12 +341,11 @@ __device__ __forceinline__ const void *gate_at(const BlockArgs &a, long long at)
 {
     return static_cast<const char *>(a.gate) + at * a.gate_stride * (a.gate_f32 ? 4 : (int)sizeof(T));
 }
-// Weights as the thread that reads them finds them without bank conflicts: its pieces of four (or fewer) lie `team` pieces apart.
+// Weights as the thread that reads them finds them without bank conflicts: its pieces of four lie `team` pieces apart.
 template <int VEC>
 __device__ __forceinline__ int weight_slot(int k, int i, int team, int t)
 {
-    constexpr int P = VEC < 4 ? VEC : 4;
-    return ((k * (VEC / P) + i / P) * team + t) * P + i % P;
+    return ((k * (VEC / 4) + i / 4) * team + t) * 4 + i % 4;
 }
 // weight * gate (1 where there is none) of the thread's columns
 template <typename T, int VEC, int CH>
@@ -373,34 +364,27 @@ __device__ __forceinline__ void fill_weights(float *to, const void *weight, bool
 template <int VEC>
 __device__ __forceinline__ void weights(float (&v)[VEC], const float *from, int k, int team, int t)
 {
-    if constexpr (VEC % 4 == 0) {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 4) {
-            const float4 w = *reinterpret_cast<const float4 *>(from + weight_slot<VEC>(k, i, team, t));
-            v[i] = w.x, v[i + 1] = w.y, v[i + 2] = w.z, v[i + 3] = w.w;
-        }
-    } else if constexpr (VEC == 2) {
-        const float2 w = *reinterpret_cast<const float2 *>(from + weight_slot<VEC>(k, 0, team, t));
-        v[0] = w.x, v[1] = w.y;
-    } else {
-        v[0] = from[weight_slot<VEC>(k, 0, team, t)];
+    for (int i = 0; i < VEC; i += 4) {
+        const float4 w = *reinterpret_cast<const float4 *>(from + weight_slot<VEC>(k, i, team, t));
+        v[i] = w.x, v[i + 1] = w.y, v[i + 2] = w.z, v[i + 3] = w.w;
     }
 }
 
-// How a row is spread: VEC neighbours at a time as the alignment of all tables allows; 8 values a thread up to 256 (32 lanes), 16 beyond
-// (what a thread does besides its values weighs half as much); up to 512 values a warp's lanes, or fewer, have a row. Beyond
-// 8,192 values that means 1,024 threads, whose 64 registers each do not hold all that a row needs.
+// How a row is spread: pieces of 16 bytes; 8 values a thread up to 256 (32 lanes), 16 beyond (what a thread does besides its values weighs
+// half as much); up to 512 values a warp's lanes, or fewer, have a row. Beyond 8,192 values that means 1,024 threads, whose 64
+// registers each do not hold all that a row needs.
 struct Shape {
-    int vec, chunks, team;
-    bool block, wide;
+    int chunks, team;
+    bool block, wide, any;   // any: some table's rows do not start on 16-byte boundaries
     int threads;
 };
 inline Shape plan(int width, int elem, int align)
 {
     Shape s;
-    s.vec = align >= 16 ? 16 / elem : align >= 4 && elem == 2 ? 2 : 1;
+    s.any = align < 16;
     const int values = width > 256 ? 16 : 8;
-    s.chunks = values / s.vec;
+    s.chunks = values * elem / 16;
     const int need = (width + values - 1) / values;
     s.block = need > 32, s.wide = need > 512;
     s.team = 1;
@@ -422,14 +406,14 @@ template <typename T, typename F>
 cudaError_t by_shape(const Shape &s, F launch)
 {
     constexpr int V = kPer16<T>;
-#define NBOS_SHAPE(VEC, CH, BLOCK, WIDE) \
-    if (s.vec == VEC && s.chunks == CH && s.block == BLOCK && s.wide == WIDE) \
-        return launch(std::integral_constant<int, VEC>(), std::integral_constant<int, CH>(), std::integral_constant<bool, BLOCK>(), std::integral_constant<bool, WIDE>());
-#define NBOS_SHAPES(VEC) NBOS_SHAPE(VEC, 8 / VEC, false, false) NBOS_SHAPE(VEC, 16 / VEC, false, false) \
-    NBOS_SHAPE(VEC, 16 / VEC, true, false) NBOS_SHAPE(VEC, 16 / VEC, true, true)
-    NBOS_SHAPES(V)
-    NBOS_SHAPES(1)
-    if constexpr (sizeof(T) == 2) { NBOS_SHAPES(2) }
+#define NBOS_SHAPE(CH, BLOCK, WIDE, ANY)                                                                                            \
+    if (s.chunks == CH && s.block == BLOCK && s.wide == WIDE && s.any == ANY)                                                       \
+        return launch(std::integral_constant<int, CH>(), std::integral_constant<bool, BLOCK>(), std::integral_constant<bool, WIDE>(), \
+                      std::integral_constant<bool, ANY>());
+#define NBOS_SHAPES(ANY) \
+    NBOS_SHAPE(8 / V, false, false, ANY) NBOS_SHAPE(16 / V, false, false, ANY) NBOS_SHAPE(16 / V, true, false, ANY) NBOS_SHAPE(16 / V, true, true, ANY)
+    NBOS_SHAPES(false)
+    NBOS_SHAPES(true)
 #undef NBOS_SHAPES
 #undef NBOS_SHAPE
     return cudaErrorInvalidConfiguration;

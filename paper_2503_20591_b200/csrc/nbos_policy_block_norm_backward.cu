@@ -5,20 +5,22 @@ namespace nbos {
 namespace block_norm {
 namespace {
 
-template <typename T, int VEC, int CH, bool BLOCK, bool WIDE, Gate GATE>
+template <typename T, int CH, bool BLOCK, bool WIDE, bool ANY, Gate GATE>
 __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_constant__ BlockArgs a, int team, int ahead)
 {
+    constexpr int VEC = kPer16<T>, TABLES = ANY && GATE == ROW_GATE ? 5 : 4;   // branch, residual, dh, dr, and a gate that may start anywhere
+    using Ring = Ahead<T, VEC, CH, BLOCK, WIDE, ANY>;
     __shared__ float4 warps[2][8];
     // the rows to come; the weights; teams of a warp or less: [teams][width] of one sum after the other; shared gates: [width], gate S of the
     // gates behind the block
     extern __shared__ uint4 staged_words[];
     char *const staged = reinterpret_cast<char *>(staged_words);
-    using Ring = Ahead<T, VEC, CH, WIDE>;
-    float *const post = reinterpret_cast<float *>(staged + ahead * 4 * Ring::kRowBytes * (int)blockDim.x), *const pre = post + team * CH * VEC;
-    float *const columns = pre + team * CH * VEC;
     int half = 0;
     const int teams = BLOCK ? 1 : blockDim.x / team, t = BLOCK ? threadIdx.x : threadIdx.x % team, mine = BLOCK ? 0 : threadIdx.x / team;
-    const Columns c(team, t, a.width, VEC);
+    const Columns c(team, t, a.width, VEC, mine, teams);
+    const int staged_bytes = Ring::bytes(ahead, TABLES, team, teams);
+    float *const post = reinterpret_cast<float *>(staged + staged_bytes), *const pre = post + team * CH * VEC;
+    float *const columns = pre + team * CH * VEC;
     float *const sum_q = columns + (BLOCK ? 0 : teams * a.width);
     float sum_s[CH][VEC], sum_p[CH][VEC];
 #pragma unroll
@@ -57,15 +59,19 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
             }
     };
 
-    Ring::clear(staged, ahead * 4);
+    Ring::clear(staged, staged_bytes);
     const Rows rows(a, GATE == SHARED_GATE);
     auto of = [&](const void *table, long long stride, unsigned int row) { return static_cast<const T *>(table) + row * stride; };
+    const bool gate_staged = Ring::kStaged && TABLES == 5 && (sizeof(T) == 4 || !a.gate_f32);
     auto fetch = [&](long long first, long long end, int stage) {
         if (!Ring::kStaged) return;
         if (first < end) {
             const unsigned int row = (unsigned int)(first + mine < end ? first + mine : first);
-            Ring::copy(staged, 4 * stage, of(a.y, a.y_stride, row), of(a.x, a.x_stride, row), c);
-            Ring::copy(staged, 4 * stage + 2, a.dh ? of(a.dh, a.dh_stride, row) : nullptr, a.dr ? of(a.dr, a.dr_stride, row) : nullptr, c);
+            Ring::copy(staged, TABLES * stage, of(a.y, a.y_stride, row), row * a.y_stride, c);
+            Ring::copy(staged, TABLES * stage + 1, of(a.x, a.x_stride, row), row * a.x_stride, c);
+            if (a.dh) Ring::copy(staged, TABLES * stage + 2, of(a.dh, a.dh_stride, row), row * a.dh_stride, c);
+            if (a.dr) Ring::copy(staged, TABLES * stage + 3, of(a.dr, a.dr_stride, row), row * a.dr_stride, c);
+            if (gate_staged) Ring::copy(staged, TABLES * stage + 4, static_cast<const T *>(gate_at<T>(a, row)), row * a.gate_stride, c);
         }
         copies_commit();
     };
@@ -74,7 +80,8 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
         const void *const gate = GATE == SHARED_GATE ? gate_at<T>(a, gi) : nullptr;
         const long long end = (long long)gi * rows.per_gate + rows.part_to;
         int stage = 0;
-        for (int i = 0; i < ahead; ++i) fetch((long long)gi * rows.per_gate + rows.part_from + i * teams, end, i);
+        if (ANY) team_sync<BLOCK>();   // the gate's rows before have left
+        for (int i = 0; i < (ANY ? 1 : ahead); ++i) fetch((long long)gi * rows.per_gate + rows.part_from + i * teams, end, i);
         if (!BLOCK) __syncthreads();   // the gate before is done with
         if (BLOCK || mine == 0) fill_weights<T, VEC, CH>(post, a.post, a.weight_f32, gate, a.gate_f32, team, t, a.width);
         if (!BLOCK) __syncthreads();   // (a block's threads read their own columns)
@@ -85,23 +92,35 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
             const float root_y = a.saved[2ll * row], root_r = a.saved[2ll * row + 1];
             float r[CH][VEC], d[CH][VEC];   // r^, then f;  e, then d
             float s[2] = {0.0f, 0.0f}, mean_r = 0.0f;
-            Ring::wait(ahead);
+            if (Ring::kStaged && ANY) {
+                copies_wait<0>();
+                team_sync<BLOCK>();    // all of the row is there, and all of the row before has left
+                if (ahead == 2) fetch(first + teams, end, stage ^ 1);
+            } else if (Ring::kStaged) {
+                if (ahead == 2)
+                    copies_wait<1>();
+                else
+                    copies_wait<0>();
+            }
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 float w[VEC];
-                Ring::read(r[k], staged, 4 * stage, k, y, c);
+                Ring::read(r[k], staged, TABLES * stage, k, y, c);
                 scale_all(r[k], root_y);
                 weights(w, post, k, team, t);
                 mul_all(r[k], w);
                 if (GATE == ROW_GATE) {
-                    get_either<T, VEC>(w, gate_at<T>(a, row), a.gate_f32, k, c);
+                    if (gate_staged)
+                        Ring::read(w, staged, TABLES * stage + 4, k, static_cast<const T *>(gate_at<T>(a, row)), c);
+                    else
+                        get_either<T, VEC, ANY>(w, gate_at<T>(a, row), a.gate_f32, k, c);
                     mul_all(r[k], w);
                 }
-                Ring::read(w, staged, 4 * stage + 1, k, x, c);
+                Ring::read(w, staged, TABLES * stage + 1, k, x, c);
                 add_scaled(r[k], w, a.alpha);
                 scale_all(r[k], root_r);
                 if (a.dh) {
-                    Ring::read(d[k], staged, 4 * stage + 2, k, of(a.dh, a.dh_stride, row), c);
+                    Ring::read(d[k], staged, TABLES * stage + 2, k, of(a.dh, a.dh_stride, row), c);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) w[i] = inside ? d[k][i] : 0.0f;
                     add_product(sum_p[k], w, r[k]);
@@ -123,15 +142,18 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
                     for (int i = 0; i < VEC; ++i) d[k][i] = 0.0f;
                 }
                 if (a.dr) {
-                    Ring::read(w, staged, 4 * stage + 3, k, of(a.dr, a.dr_stride, row), c);
+                    Ring::read(w, staged, TABLES * stage + 3, k, of(a.dr, a.dr_stride, row), c);
                     add_scaled(d[k], w, 1.0f);
                 }
-                Ring::read(y_hat, staged, 4 * stage, k, y, c);
+                Ring::read(y_hat, staged, TABLES * stage, k, y, c);
                 scale_all(y_hat, root_y);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) r[k][i] = d[k][i];
                 if (GATE == ROW_GATE) {
-                    get_either<T, VEC>(w, gate_at<T>(a, row), a.gate_f32, k, c);
+                    if (gate_staged)
+                        Ring::read(w, staged, TABLES * stage + 4, k, static_cast<const T *>(gate_at<T>(a, row)), c);
+                    else
+                        get_either<T, VEC, ANY>(w, gate_at<T>(a, row), a.gate_f32, k, c);
                     mul_all(r[k], w);
                 }
 #pragma unroll
@@ -142,17 +164,23 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
                 dot_all(s, r[k], y_hat);
             }
             const float mean_y = a.dy ? row_sum<BLOCK, WIDE>(s[0] + s[1], team, warps, half) * a.per_width : 0.0f;
+            if (Ring::kStaged && ANY) team_sync<BLOCK>();   // results take the place of what has been read
+            T *const dx = static_cast<T *>(a.dx) + row * a.dx_stride, *const dy = static_cast<T *>(a.dy) + row * a.dy_stride;
+            char *const dgate = static_cast<char *>(a.dgate) + row * a.dgate_stride * (a.gate_f32 ? 4 : (int)sizeof(T));
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 if (!inside) continue;
                 float v[VEC], y_hat[VEC];
-                Ring::read(y_hat, staged, 4 * stage, k, y, c);
+                Ring::read(y_hat, staged, TABLES * stage, k, y, c);
                 scale_all(y_hat, root_y);
                 if (GATE == ROW_GATE && a.dgate) {
                     weights(v, post, k, team, t);
                     mul_all(v, d[k]);
                     mul_all(v, y_hat);
-                    put_either<T, VEC>(static_cast<char *>(a.dgate) + row * a.dgate_stride * (a.gate_f32 ? 4 : (int)sizeof(T)), a.gate_f32, v, k, c);
+                    if (gate_staged)
+                        Ring::write(reinterpret_cast<T *>(dgate), staged, TABLES * stage + 1, v, k, c);
+                    else
+                        put_either<T, VEC, ANY>(dgate, a.gate_f32, v, k, c);
                 }
                 if (a.dy) {
                     add_scaled(r[k], y_hat, -mean_y);
@@ -160,11 +188,22 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
                 }
                 if (a.dx) {
                     scale_all(d[k], a.alpha);
-                    put<T, VEC>(static_cast<T *>(a.dx) + row * a.dx_stride, d[k], k, c);
+                    Ring::write(dx, staged, TABLES * stage + 3, d[k], k, c);
                 }
-                if (a.dy) put<T, VEC>(static_cast<T *>(a.dy) + row * a.dy_stride, r[k], k, c);
+                if (a.dy) Ring::write(dy, staged, TABLES * stage + 2, r[k], k, c);
             }
-            fetch(first + (long long)ahead * teams, end, stage);
+            if (Ring::kStaged && ANY) {
+                team_sync<BLOCK>();
+                if (inside && a.dx) Ring::row_out(dx, staged, TABLES * stage + 3, c);
+                if (inside && a.dy) Ring::row_out(dy, staged, TABLES * stage + 2, c);
+                if (inside && GATE == ROW_GATE && a.dgate && gate_staged) Ring::row_out(reinterpret_cast<T *>(dgate), staged, TABLES * stage + 1, c);
+                if (ahead == 1) {
+                    team_sync<BLOCK>();
+                    fetch(first + teams, end, 0);
+                }
+            } else if (Ring::kStaged) {
+                fetch(first + (long long)ahead * teams, end, stage);
+            }
             stage = stage + 1 == ahead ? 0 : stage + 1;
         }
         if (GATE == SHARED_GATE && a.blocks_per_gate == 1) {   // all of the gate's rows are this block's
@@ -174,7 +213,7 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
                 const int col = (k * team + t) * VEC;
                 if (mine == 0 && col < a.width) {
                     float g[VEC], v[VEC];
-                    get_either<T, VEC>(g, gate, a.gate_f32, k, c);
+                    get_either<T, VEC, ANY>(g, gate, a.gate_f32, k, c);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) v[i] = a.post && col + i < a.width ? one_value(a.post, col + i, a.weight_f32, T()) : 1.0f;
 #pragma unroll
@@ -183,7 +222,7 @@ __global__ void __maxnreg__((kBackwardRegs<WIDE>)) backward_kernel(const __grid_
                         v[i] *= sum_s[k][i];
                     }
                     if (a.dgate)
-                        put_either<T, VEC>(static_cast<char *>(a.dgate) + gi * a.dgate_stride * (a.gate_f32 ? 4 : (int)sizeof(T)), a.gate_f32, v, k, c);
+                        put_either<T, VEC, ANY>(static_cast<char *>(a.dgate) + gi * a.dgate_stride * (a.gate_f32 ? 4 : (int)sizeof(T)), a.gate_f32, v, k, c);
                 }
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) sum_s[k][i] = 0.0f;
@@ -257,16 +296,17 @@ __global__ void __launch_bounds__(32 * kColumnWarps) columns_kernel(const __grid
 template <typename T, Gate GATE>
 cudaError_t run_backward(const BlockArgs &args, Shape s, int sms, ColumnArgs &c, cudaMemPool_t pool, cudaStream_t stream)
 {
-    // 32-bit rows of nearly 8,192 values with a shared gate: too much for shared memory, so not staged
-    if (s.block && s.team * 16 * (4 * (int)sizeof(T) + 8) + args.width * 4 > kMostShared) s.wide = true;
-    return by_shape<T>(s, [&](auto vec, auto chunks, auto block, auto wide) -> cudaError_t {
-        auto *kernel = backward_kernel<T, vec(), chunks(), block(), wide(), GATE>;
+    const int tables = s.any && GATE == ROW_GATE ? 5 : 4;
+    // 32-bit rows of nearly 8,192 values: staged rows, weights and a shared gate's sums are too much for shared memory, so they are not staged
+    if (s.block && tables * (s.chunks * s.team + 2) * 16 + 2 * s.team * 16 * 4 + args.width * 4 > kMostShared) s.wide = true;
+    return by_shape<T>(s, [&](auto chunks, auto block, auto wide, auto any) -> cudaError_t {
+        auto *kernel = backward_kernel<T, chunks(), block(), wide(), any(), GATE>;
         static const int regs = kernel_registers(kernel);
         BlockArgs a = args;
         const int teams = s.threads / s.team;
-        using Ring = Ahead<T, vec(), chunks(), wide()>;
-        const int ahead = Ring::rows(4, s.threads);
-        const int shared = ahead * 4 * Ring::kRowBytes * s.threads + (2 * s.team * vec() * chunks() + (s.block ? 0 : teams * a.width) +
+        using Ring = Ahead<T, kPer16<T>, chunks(), block(), wide(), any()>;
+        const int ahead = Ring::rows(tables, s.team, teams);
+        const int shared = Ring::bytes(ahead, tables, s.team, teams) + (2 * s.team * kPer16<T> * chunks() + (s.block ? 0 : teams * a.width) +
                            (GATE == SHARED_GATE ? a.width : 0)) * (int)sizeof(float);
         cudaError_t e = allow_shared(kernel, shared);
         if (e != cudaSuccess) return e;
