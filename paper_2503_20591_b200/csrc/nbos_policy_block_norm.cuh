@@ -171,8 +171,9 @@ __device__ __forceinline__ void team_sync()
 // 8,192 x 2,048 bf16: forward 316 us, backward 651; staged, with 8 values a thread, 256 and 511; with 16 values, 217 and 545, and then as
 // below.) Rows on 16-byte boundaries: each thread copies the pieces that it reads itself, so no barrier is needed. ANY, rows that start
 // anywhere: a team copies the row with the bytes from the boundary before it, a thread puts its pieces together from two neighbours of 16 bytes,
-// and results go the same way back (in pieces of 4 bytes or single values, without: 4,099 x 2,050 f16, forward 45 us, backward 103; this
-// FIXME). Rows that do not fit (beyond 8,192 values, or nearly that many of 32 bits) come from memory and then from the L1 cache.
+// and results go the same way back (single values from and to memory instead: 32,768 x 2,051 f16 without a gate, forward 373 us, backward
+// 1,018; this 202 and 550). Rows that do not fit (beyond 8,192 values, or nearly that many of 32 bits) come from memory and then from the L1
+// cache.
 template <typename T, int VEC, int CH, bool BLOCK, bool WIDE, bool ANY>
 struct Ahead {
     static constexpr bool kStaged = !WIDE;
@@ -297,7 +298,7 @@ __device__ __forceinline__ void add_scaled(float (&s)[VEC], const float (&a)[VEC
 
 enum Gate { NO_GATE, SHARED_GATE, ROW_GATE };
 
-// Registers: what leaves room for enough threads to keep the memory busy. Weights are not among them: they lie in shared memory as
+// Registers: what leaves room for enough threads to keep the memory busy (backward with 96: 280 -> 320 us for 32,768 x 2,048 f16). Weights are not among them: they lie in shared memory as
 // 32-bit floats, those of the branch's norm multiplied by the gate that the block's rows share. (Taken from the L1 cache row by row:
 // 8 x 8,192 x 2,048 bf16 forward 191 us, backward 414; this 188 and 312.)
 template <bool WIDE> constexpr int kForwardRegs = 64;
