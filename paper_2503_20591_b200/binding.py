@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from array import array
 from dataclasses import dataclass
 from operator import attrgetter
@@ -186,11 +187,11 @@ def load_library() -> ctypes.CDLL:
     lib.nbos_policy_balance.argtypes = [P(nbos_logits), i32, vp, i32, vp, f32, vp, vp, vp, vp, vp, i64, vp]
     lib.nbos_policy_balance_backward.argtypes = [P(nbos_logits), i32, vp, i32, vp, vp, f32, vp, i64, vp]
     lib.nbos_policy_sample.argtypes = [P(nbos_logits), vp, vp, vp, vp, vp, i32, vp, vp, vp]
-    lib.nbos_policy_towers.argtypes = [P(nbos_towers), vp, vp, i64, i32, f32, vp, vp, vp]
-    lib.nbos_policy_towers_backward.argtypes = [P(nbos_towers), vp, vp, i64, i32, f32, vp, vp, f32, vp, i64, i64, vp, i64, i64, vp]
+    lib.nbos_policy_towers.argtypes = [vp, vp, vp, i64, i32, f32, vp, vp, vp]
+    lib.nbos_policy_towers_backward.argtypes = [vp, vp, vp, i64, i32, f32, vp, vp, f32, vp, i64, i64, vp, i64, i64, vp]
     lib.nbos_policy_towers_status.argtypes = [vp]
-    lib.nbos_policy_block_norm.argtypes = [P(nbos_block), vp, i64, vp, i64, vp, vp]
-    lib.nbos_policy_block_norm_backward.argtypes = [P(nbos_block), vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp]
+    lib.nbos_policy_block_norm.argtypes = [vp, vp, i64, vp, i64, vp, vp]
+    lib.nbos_policy_block_norm_backward.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp]
     lib.nbos_policy_clip.argtypes = [vp, vp, vp, vp, i32, f32, i32, vp, vp]
     lib.nbos_snapshot_status.argtypes = [vp, vp]
     lib.nbos_strerror.argtypes = [ctypes.c_int]
@@ -690,6 +691,7 @@ def nbos_policy_sample(logits, uniforms, out_hosts, out_found=None, temperature=
 
 
 # ---- two towers: distillation without the table of logits --------------------------------
+_TOWERS, _BLOCK = struct.Struct("=2Q5q4i2Q"), struct.Struct("=5Q5q4i2f")   # nbos_towers, nbos_block: packed in a third of the time
 _dtype_of = attrgetter("dtype")
 _TOWER_DTYPES = {torch.bfloat16: NBOS_BF16, torch.float16: NBOS_F16}
 
@@ -711,21 +713,21 @@ def _vectors(t, what: str):
 
 
 def _towers(requests, host_vectors, hosts, asks, room):
-    """(nbos_towers, rows over all groups, address of hosts, k)"""
+    """(nbos_towers as bytes, groups, rows over all of them, address of hosts, k)"""
     n, rows, width, rstride, rgroup = _vectors(requests, "requests")
     m, n_hosts, hwidth, hstride, hgroup = _vectors(host_vectors, "host_vectors")
-    if (n, width, requests.dim(), requests.dtype) != (m, hwidth, host_vectors.dim(), host_vectors.dtype):
+    if n != m or width != hwidth or requests.dim() != host_vectors.dim() or requests.dtype is not host_vectors.dtype:
         raise ValueError("requests [..., B, D] and host_vectors [..., H, D] must agree on their groups, width and type")
     device = requests.device
-    if host_vectors.device != device:
+    if host_vectors.get_device() != device.index:
         raise ValueError(f"host_vectors must live on {device}, not {host_vectors.device}")
     ids, k = _choices(hosts, requests, n * rows)
     if (asks is None) != (room is None):
         raise ValueError("asks and room come together")
-    desc = nbos_towers(requests.data_ptr(), host_vectors.data_ptr(), rows, rstride, rgroup, hstride, hgroup, n, n_hosts, width,
-                       _TOWER_DTYPES[requests.dtype], _dense(asks, "asks", torch.int32, 4 * n * rows, device),
-                       _dense(room, "room", torch.int32, 4 * n * n_hosts, device))
-    return desc, n * rows, ids, k
+    desc = _TOWERS.pack(requests.data_ptr(), host_vectors.data_ptr(), rows, rstride, rgroup, hstride, hgroup, n, n_hosts, width,
+                        _TOWER_DTYPES[requests.dtype], _dense(asks, "asks", torch.int32, 4 * n * rows, device),
+                        _dense(room, "room", torch.int32, 4 * n * n_hosts, device))
+    return desc, n, n * rows, ids, k
 
 
 def _grad_vectors(grad, vectors, what: str):
@@ -744,12 +746,12 @@ def nbos_policy_towers(requests, host_vectors, hosts, teacher_logits, out_loss, 
     and host_vectors [N, H, D] (or without N) bfloat16 or float16, hosts [N, B, k] int32 (-1 = none), teacher_logits [N, B, k] or [k]
     float32 or None, out_loss [N, B] float32 or None, out_stats [N, B, 2 + k] float32 or None; asks [N, B, 4] and room
     [N, H, 4] int32 or None: a request fits a host if its four asks are within the host's room. Asynchronous on the stream."""
-    desc, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room)
+    desc, groups, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room)
     device, f32 = requests.device, torch.float32
     teacher, tstride = _teacher(teacher_logits, hosts, device, rows, k)
-    args = (ctypes.byref(desc), ids, teacher, tstride, k, temperature, _dense(out_loss, "out_loss", f32, rows, device),
+    args = (desc, ids, teacher, tstride, k, temperature, _dense(out_loss, "out_loss", f32, rows, device),
             _dense(out_stats, "out_stats", f32, (2 + k) * rows, device), _policy_stream(stream, device))
-    if desc.n_groups:
+    if groups:
         _check(load_library().nbos_policy_towers(*args))
 
 
@@ -757,14 +759,14 @@ def nbos_policy_towers_backward(requests, host_vectors, hosts, teacher_logits, s
                                 grad_loss=None, grad_scale=1.0, temperature=1.0, asks=None, room=None, stream=None) -> None:
     """The gradients of nbos_policy_towers from the statistics it saved (out_stats): out_grad_requests like requests,
     out_grad_hosts like host_vectors, either may be None; grad_loss [N, B] float32 or None."""
-    desc, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room)
+    desc, groups, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room)
     device, f32 = requests.device, torch.float32
     teacher, tstride = _teacher(teacher_logits, hosts, device, rows, k)
-    args = (ctypes.byref(desc), ids, teacher, tstride, k, temperature, _dense(stats, "stats", f32, (2 + k) * rows, device),
+    args = (desc, ids, teacher, tstride, k, temperature, _dense(stats, "stats", f32, (2 + k) * rows, device),
             _dense(grad_loss, "grad_loss", f32, rows, device), grad_scale,
             *_grad_vectors(out_grad_requests, requests, "out_grad_requests"),
             *_grad_vectors(out_grad_hosts, host_vectors, "out_grad_hosts"), _policy_stream(stream, device))
-    if desc.n_groups:
+    if groups:
         _check(load_library().nbos_policy_towers_backward(*args))
 
 
@@ -774,24 +776,24 @@ def nbos_policy_towers_status(stream=None) -> int:
 
 
 # ---- the norms around a residual block -------------------------------------------------
-def _like(t, like, what: str):
-    """(address, row stride) of a table like `like`, or (0, 0)."""
+def _like(t, like, shape, what: str):
+    """(address, row stride) of a table like `like`, whose shape is `shape`, or (0, 0)."""
     if t is None:
         return 0, 0
-    if t is not like and (not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device):
+    if t is not like and (not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.shape != shape or t.get_device() != like.get_device()):
         raise ValueError(f"{what} must have the residual's shape, type and device")
-    if t.is_contiguous():
-        return t.data_ptr(), t.shape[-1]
-    return t.data_ptr(), _table(t, what)[1]
+    return t.data_ptr(), shape[-1] if t.is_contiguous() else _table(t, what)[1]
 
 
-def _weight(t, what: str, residual):
+def _weight(t, what: str, residual, width: int):
     """Address of weights [width] of the residual's type or float32, or 0."""
     if t is None:
         return 0
     if not isinstance(t, torch.Tensor) or (t.dtype is not torch.float32 and t.dtype is not residual.dtype):
         raise TypeError(f"{what} must have the residual's type or float32")
-    return _dense(t, what, t.dtype, residual.shape[-1], residual.device)
+    if t.numel() == width and t.get_device() == residual.get_device() and t.is_contiguous():
+        return t.data_ptr()
+    return _dense(t, what, t.dtype, width, residual.device)
 
 
 def _gate(gate, residual, rows: int, what: str = "gate"):
@@ -799,15 +801,16 @@ def _gate(gate, residual, rows: int, what: str = "gate"):
     residual's, then ones ([N, 1, D] with [N, B, D]: a gate for each n), or it is [D]."""
     if not isinstance(gate, torch.Tensor) or (gate.dtype is not torch.float32 and gate.dtype is not residual.dtype):
         raise TypeError(f"{what} must have the residual's type or float32")
-    if gate.device != residual.device:
+    if gate.get_device() != residual.get_device():
         raise ValueError(f"{what} must live on {residual.device}, not {gate.device}")
-    lead, own = residual.shape[:-1], gate.shape[:-1]
-    if gate.shape[-1:] != residual.shape[-1:] or (own and len(own) != len(lead)):
+    shape, size = residual.shape, gate.shape
+    if size[-1:] != shape[-1:] or (len(size) > 1 and len(size) != len(shape)):
         raise ValueError(f"{what} must be [D], or have the residual's shape with ones for the last of its leading sizes")
-    if not own:
-        if gate.shape[0] > 1 and gate.stride(0) != 1:
+    if len(size) == 1:
+        if not gate.is_contiguous():
             raise ValueError(f"{what} must be contiguous")
         return gate.data_ptr(), 0, max(rows, 1)
+    lead, own = shape[:-1], size[:-1]
     same = 0
     while same < len(lead) and own[same] == lead[same]:
         same += 1
@@ -819,19 +822,22 @@ def _gate(gate, residual, rows: int, what: str = "gate"):
     return gate.data_ptr(), _table(gate, what)[1], max(shared, 1)
 
 
-def _block(residual, branch, gate, post_weight, pre_weight, residual_scale, eps) -> nbos_block:
+def _block(residual, branch, gate, post_weight, pre_weight, residual_scale, eps):
+    """(nbos_block as bytes, rows, the residual's shape)"""
     rows, stride, width = _table(residual, "residual")
-    at, branch_stride = _like(branch, residual, "branch")
+    shape = residual.shape
+    at, branch_stride = _like(branch, residual, shape, "branch")
     if branch is None:
         raise ValueError("branch is None")
     dtype = _POLICY_DTYPES[residual.dtype]
     gate_at, gate_stride, per_gate = (0, 0, 1) if gate is None else _gate(gate, residual, rows)
-    post, pre = _weight(post_weight, "post_weight", residual), _weight(pre_weight, "pre_weight", residual)
+    post, pre = _weight(post_weight, "post_weight", residual, width), _weight(pre_weight, "pre_weight", residual, width)
     weight = post_weight if pre_weight is None else pre_weight
     if post_weight is not None and post_weight.dtype is not weight.dtype:
         raise TypeError("post_weight and pre_weight must have one type")
-    return nbos_block(residual.data_ptr(), at, gate_at, post, pre, stride, branch_stride, gate_stride, rows, per_gate, width, dtype,
-                      dtype if gate is None else _POLICY_DTYPES[gate.dtype], dtype if weight is None else _POLICY_DTYPES[weight.dtype], residual_scale, eps)
+    desc = _BLOCK.pack(residual.data_ptr(), at, gate_at, post, pre, stride, branch_stride, gate_stride, rows, per_gate, width, dtype,
+                       dtype if gate is None else _POLICY_DTYPES[gate.dtype], dtype if weight is None else _POLICY_DTYPES[weight.dtype], residual_scale, eps)
+    return desc, rows, shape
 
 
 def nbos_policy_block_norm(residual, branch, gate, post_weight, pre_weight, out_residual, out_normed=None, out_stats=None,
@@ -840,11 +846,11 @@ def nbos_policy_block_norm(residual, branch, gate, post_weight, pre_weight, out_
     tensors: residual and branch [..., D] (float32, bfloat16, float16; rows evenly apart), gate like them, [N, 1, D] beside [N, B, D],
     [D] or None, weights [D] or None (gate and weights of the same type or float32); outputs like residual or None (residual and
     branch themselves will do), out_stats [..., 2] float32 or None. Asynchronous on the stream."""
-    desc = _block(residual, branch, gate, post_weight, pre_weight, residual_scale, eps)
+    desc, rows, shape = _block(residual, branch, gate, post_weight, pre_weight, residual_scale, eps)
     device = residual.device
     _check(load_library().nbos_policy_block_norm(
-        ctypes.byref(desc), *_like(out_residual, residual, "out_residual"), *_like(out_normed, residual, "out_normed"),
-        _dense(out_stats, "out_stats", torch.float32, 2 * desc.rows, device), _policy_stream(stream, device)))
+        desc, *_like(out_residual, residual, shape, "out_residual"), *_like(out_normed, residual, shape, "out_normed"),
+        _dense(out_stats, "out_stats", torch.float32, 2 * rows, device), _policy_stream(stream, device)))
 
 
 def nbos_policy_block_norm_backward(residual, branch, gate, post_weight, pre_weight, stats, grad_residual, grad_normed,
@@ -852,23 +858,24 @@ def nbos_policy_block_norm_backward(residual, branch, gate, post_weight, pre_wei
                                     residual_scale=1.0, stream=None) -> None:
     """The gradients of nbos_policy_block_norm from the statistics it saved (out_stats) and what arrives at its two outputs (either may
     be None); each output like its input, or None."""
-    desc = _block(residual, branch, gate, post_weight, pre_weight, residual_scale, 0.0)
+    desc, rows, shape = _block(residual, branch, gate, post_weight, pre_weight, residual_scale, 0.0)
     device = residual.device
     gate_at = gate_stride = 0
     if out_grad_gate is not None:
         if gate is None or out_grad_gate.shape != gate.shape or out_grad_gate.dtype != gate.dtype:
             raise ValueError("out_grad_gate must have the gate's shape and type")
-        gate_at, gate_stride, _ = _gate(out_grad_gate, residual, desc.rows, "out_grad_gate")
-        if desc.rows == 0:
+        gate_at, gate_stride, _ = _gate(out_grad_gate, residual, rows, "out_grad_gate")
+        if rows == 0:
             out_grad_gate.zero_()   # its rows have none to add up; the library does not know how many they are
     for got, weight, what in ((out_grad_post, post_weight, "out_grad_post"), (out_grad_pre, pre_weight, "out_grad_pre")):
         if got is not None and (weight is None or got.dtype != weight.dtype):
             raise ValueError(f"{what} must have its weight's type")
+    width = shape[-1]
     _check(load_library().nbos_policy_block_norm_backward(
-        ctypes.byref(desc), _dense(stats, "stats", torch.float32, 2 * desc.rows, device), *_like(grad_residual, residual, "grad_residual"),
-        *_like(grad_normed, residual, "grad_normed"), *_like(out_grad_residual, residual, "out_grad_residual"),
-        *_like(out_grad_branch, residual, "out_grad_branch"), gate_at, gate_stride, _weight(out_grad_post, "out_grad_post", residual),
-        _weight(out_grad_pre, "out_grad_pre", residual), _policy_stream(stream, device)))
+        desc, _dense(stats, "stats", torch.float32, 2 * rows, device), *_like(grad_residual, residual, shape, "grad_residual"),
+        *_like(grad_normed, residual, shape, "grad_normed"), *_like(out_grad_residual, residual, shape, "out_grad_residual"),
+        *_like(out_grad_branch, residual, shape, "out_grad_branch"), gate_at, gate_stride, _weight(out_grad_post, "out_grad_post", residual, width),
+        _weight(out_grad_pre, "out_grad_pre", residual, width), _policy_stream(stream, device)))
 
 
 # ---- clipping by the global norm ------------------------------------------------------------

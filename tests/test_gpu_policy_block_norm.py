@@ -186,7 +186,7 @@ def test_what_may_be_left_out(nb, dtype):
 
 def test_written_over_the_inputs(nb):
     import torch
-    for shape in ((2, 30, 200), (3, 2048), (5, 9000)):
+    for shape in ((2, 30, 200), (3, 2048), (5, 9000), (700, 333), (900, 1001), (5, 9001)):
         c, dr, dh = make(shape, "bfloat16", "row", 4)
         want = run(nb, c, 0.5, 1e-6, dr, dh)
         stats = torch.empty(*shape[:-1], 2, device="cuda")
@@ -196,6 +196,34 @@ def test_written_over_the_inputs(nb):
         assert torch.equal(a, want["residual"]) and torch.equal(b, want["branch"])
         nb.nbos_policy_block_norm(*(c[n] for n in NAMES), c["residual"], c["branch"], None, 0.5, 1e-6)
         assert torch.equal(c["residual"], want["out"]) and torch.equal(c["branch"], want["normed"])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("gate", ["none", "group", "row"])
+@pytest.mark.parametrize("width", [24, 200, 333, 1000, 5001])
+def test_rows_that_start_anywhere_give_the_same_bits(nb, width, gate, dtype):
+    """The same values in tables on 16-byte boundaries and off them, many rows a block: a row's arithmetic is the same. (Sums over rows go
+    by how many blocks there are room for, which differs: they are compared with the formula.)"""
+    import torch
+    shape = (6, 2500 if width < 1000 else 300, width)
+    c, dr, dh = make(shape, dtype, gate, width)
+    off, dr2, dh2 = make(shape, dtype, gate, width, pad=3, shift=1)
+
+    def aligned(t):
+        per16 = 16 // t.element_size()
+        room = torch.zeros((*t.shape[:-1], (width + per16 - 1) // per16 * per16), dtype=t.dtype, device="cuda")
+        room[..., :width] = t
+        return room[..., :width]
+
+    want = run(nb, {n: aligned(t) if t is not None and t.dim() == 3 and t.shape == shape else t for n, t in c.items()}, 0.7, 1e-6, aligned(dr), aligned(dh),
+               (-width) % (16 // dr.element_size()))
+    got = run(nb, off, 0.7, 1e-6, dr2, dh2, 5)
+    rows = [n for n in want if n in ("out", "normed", "residual", "branch") or (n == "gate" and gate == "row")]
+    assert [n for n in rows if not torch.equal(got[n], want[n])] == []
+    ref = reference(off, 0.7, 1e-6, dr2, dh2)
+    for n in set(want) - set(rows):
+        close(n, got[n], ref[n])
+        close(n, want[n], ref[n])
 
 
 def test_rows_of_zeros_nan_and_infinity_stay_alone(nb):
