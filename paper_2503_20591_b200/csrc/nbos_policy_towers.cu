@@ -37,6 +37,19 @@ struct Tiles {                        // what one launch covers
     int splits, split_blocks;         // the contraction in parts, whose sums are added up afterwards
     long long units;                  // groups * m_tiles * n_tiles * splits
 };
+// G is held in 16 bits, so all of it is multiplied by one factor, and what comes of it divided by it again: the largest |g_r T| becomes
+// `top`, the value of both types just below a power of two. A row's largest entries, p - q near -1, then lose least (values just above
+// a power of two lose twice the share), those of a p near 0 nothing; and 16-bit floats use their whole range: p of 2^-29 is still a
+// normal number.
+struct Range {
+    const unsigned int *largest;      // bits of the largest |grad_loss|; NULL: 1
+    float scale, top;                 // grad_scale T; 1 - 2^-8, in 16-bit floats times 2^15
+    __device__ __forceinline__ float factor() const
+    {
+        const float g = (largest ? __uint_as_float(*largest) : 1.0f) * fabsf(scale);
+        return g > 0.0f && g < __int_as_float(0x7F800000) ? fminf(top / g, 0x1p100f) : 1.0f;
+    }
+};
 struct TowerArgs {
     Tiles t;
     int a_z0, a_z, b_z0, b_z;         // group g is slice z0 + g * z of the operand
@@ -53,8 +66,8 @@ struct TowerArgs {
     const float *teacher;
     long long teacher_stride;
     int k;
-    const float *grad_loss, *range;   // range: factor that keeps G within 16 bits, and its inverse (NULL: 1)
-    float grad_scale;
+    const float *grad_loss;
+    Range range;
     void *out;                        // gradients: the result itself (one part), or
     float *sums;                      // [splits][groups][m_rows][width] of 32-bit sums, added to those there if `add`
     long long out_stride, out_group_stride;
@@ -277,7 +290,7 @@ __device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bo
     }
     const bool some = sum != 0.0f;
     const float m = some ? stats[0] : 0.0f, minus = some ? -log2f(stats[1]) : 0.0f;
-    const float factor = some ? a.grad_scale * (a.grad_loss ? a.grad_loss[at] : 1.0f) * (a.range ? a.range[0] : 1.0f) : 0.0f;
+    const float factor = some ? a.range.scale * (a.grad_loss ? a.grad_loss[at] : 1.0f) * a.range.factor() : 0.0f;
 #pragma unroll
     for (int j = 0; j < kFewEntries; ++j) {
         float q = 0.0f;
@@ -452,6 +465,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     args.partial[((long long)last_g * args.rows + row) * args.slots + kParts * slot + quarter] = make_float2(run_m[i], run_s[i]);
             }
         };
+        const float undo = KIND == GRAD_REQUESTS || KIND == GRAD_HOSTS ? 1.0f / args.range.factor() : 1.0f;
         while (todo.next(t, u)) {
             const int local = u.m * kTileM + (int)rank * 128 + row_in;   // row of the launch
             if (KIND == STATS || KIND == GRAD) {
@@ -472,7 +486,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             const float m = args.stats[at * args.stats_stride], s = args.stats[at * args.stats_stride + 1];
                             dead[i] = s == __int_as_float(0x7F800000);
                             run_m[i] = -m, minus[i] = -log2f(s);
-                            factor[i] = args.grad_scale * (args.grad_loss ? args.grad_loss[at] : 1.0f) * (args.range ? args.range[0] : 1.0f);
+                            factor[i] = args.range.scale * (args.grad_loss ? args.grad_loss[at] : 1.0f) * args.range.factor();
                         }
                         ask[i] = MASK && inside ? args.asks[at] : make_int4(0, 0, 0, 0);
                         some_dead |= dead[i];
@@ -580,7 +594,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             } else {
                 wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
                 fence_after();
-                const float undo = args.range ? args.range[1] : 1.0f;
                 const int n_first = u.n * BN + quarter * (BN / kParts);
 #pragma unroll 1
                 for (int sub = 0; sub < BN / kParts / 32; ++sub) {
@@ -819,8 +832,6 @@ __global__ void __launch_bounds__(256, 4) finish_kernel(const __grid_constant__ 
     if (f.stats) f.stats[at * (2 + f.k)] = some ? top : 0.0f, f.stats[at * (2 + f.k) + 1] = some ? s : __int_as_float(0x7F800000);
 }
 
-// G's factor for 16-bit floats: 2^15 over the power of two at or above the largest |g_r T|, so that p and q, at most 1, use
-// the type's whole range (p of 2^-29 is still a normal number). `largest`: bits of the largest |grad_loss|.
 __global__ void largest_kernel(const float *grad_loss, long long n, unsigned int *largest)
 {
     next_may_start();
@@ -831,24 +842,14 @@ __global__ void largest_kernel(const float *grad_loss, long long n, unsigned int
     m = warp_max(m);
     if (threadIdx.x % 32 == 0) atomicMax(largest, __float_as_uint(m));   // of floats above 0 the order of their bits
 }
-__global__ void range_kernel(const unsigned int *largest, float scale, float *range)
-{
-    next_may_start();
-    previous_done();
-    const float g = (largest ? __uint_as_float(*largest) : 1.0f) * fabsf(scale);
-    int e = 0;
-    if (g > 0.0f && g < __int_as_float(0x7F800000)) frexpf(g, &e);
-    e = min(max(e, -100), 100);
-    range[0] = ldexpf(1.0f, 15 - e), range[1] = ldexpf(1.0f, e - 15);
-}
-
 struct PatchArgs {
     int groups, group0, row0, rows_here, rows, host0, hosts_here, hosts, k;
     const int32_t *ids;
     const float *teacher;
     long long teacher_stride;
-    const float *stats, *grad_loss, *range;
-    float grad_scale, c;
+    const float *stats, *grad_loss;
+    Range range;
+    float c;
     void *grad;
     long long grad_stride, grad_group_stride;
 };
@@ -879,7 +880,7 @@ __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ Patc
     sum = lanes_sum(sum, lanes);
     if (!inside || !(sum > 0.0f)) return;
     const float m = stats[0], minus = -log2f(stats[1]);
-    const float factor = p.grad_scale * (p.grad_loss ? p.grad_loss[at] : 1.0f) * (p.range ? p.range[0] : 1.0f);
+    const float factor = p.range.scale * (p.grad_loss ? p.grad_loss[at] : 1.0f) * p.range.factor();
     for (int j = sub; j < p.k; j += lanes) {
         const int id = ids[j];
         if (id < p.host0 || id >= p.host0 + p.hosts_here || stats[2 + j] == neg_inf()) continue;
@@ -895,13 +896,13 @@ __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ Patc
 
 // The parts' sums become the gradient: [splits][groups][rows][width] -> rows out_stride apart.
 template <typename T>
-__global__ void sums_kernel(const float *sums, int splits, int groups, int rows, int width, const float *range, T *out, long long stride,
+__global__ void sums_kernel(const float *sums, int splits, int groups, int rows, int width, Range range, T *out, long long stride,
                             long long group_stride)
 {
     next_may_start();
     previous_done();
     const long long n = (long long)groups * rows * width;
-    const float undo = range ? range[1] : 1.0f;
+    const float undo = 1.0f / range.factor();
     if (width % 4 == 0) {
         for (long long i = ((long long)blockIdx.x * blockDim.x + threadIdx.x) * 4; i < n; i += (long long)gridDim.x * blockDim.x * 4) {
             float4 s = *reinterpret_cast<const float4 *>(sums + i);
@@ -1244,23 +1245,20 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
     const size_t o_g = ws.add((size_t)piece_groups * piece_rows * g_stride * 2);
     const size_t o_a = ws.add(grad_a && sums_a ? sizeof(float) * ta.splits * piece_groups * piece_rows * width : 0);
     const size_t o_b = ws.add(grad_b && sums_b ? sizeof(float) * tb.splits * piece_groups * piece_hosts * width : 0);
-    const size_t o_range = ws.add(16);
+    const size_t o_largest = ws.add(16);
     int rc = ws.allocate(c.device, c.stream);
     if (rc) return rc;
     cudaError_t e = lay_out<T>(ws, a, c.sms, c.stream);
     if (e == cudaSuccess) e = lay_out<T>(ws, b, c.sms, c.stream);
     const float scale = grad_scale * c.T;
-    float *range = nullptr;
-    if (in->dtype == NBOS_F16 && e == cudaSuccess) {
-        range = ws.at<float>(o_range);
-        unsigned int *largest = grad_loss ? reinterpret_cast<unsigned int *>(range + 2) : nullptr;
-        if (largest) {
-            e = cudaMemsetAsync(largest, 0, 4, c.stream);
-            const long long n = (long long)groups * rows, blocks = (n + 1023) / 1024;
-            if (e == cudaSuccess)
-                e = launch_next(largest_kernel, dim3((unsigned int)(blocks < 2 * c.sms ? blocks : 2 * c.sms)), 256, 0, c.stream, grad_loss, n, largest);
-        }
-        if (e == cudaSuccess) e = launch_next(range_kernel, dim3(1), 1, 0, c.stream, largest, scale, range);
+    Range range = {nullptr, scale, (1.0f - 0x1p-8f) * (in->dtype == NBOS_F16 ? 0x1p15f : 1.0f)};
+    if (grad_loss && e == cudaSuccess) {
+        unsigned int *largest = ws.at<unsigned int>(o_largest);
+        range.largest = largest;
+        e = cudaMemsetAsync(largest, 0, 4, c.stream);
+        const long long n = (long long)groups * rows, blocks = (n + 1023) / 1024;
+        if (e == cudaSuccess)
+            e = launch_next(largest_kernel, dim3((unsigned int)(blocks < 2 * c.sms ? blocks : 2 * c.sms)), 256, 0, c.stream, grad_loss, n, largest);
     }
     if (e != cudaSuccess) return cuda_fail(e, "towers: layout launch");
 
@@ -1286,7 +1284,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 p.a_z = az, p.a_z0 = g0 * az, p.b_z = bz, p.b_z0 = g0 * bz, p.a_m0 = r0, p.b_n0 = h0;
                 p.group0 = g0, p.row0 = r0, p.rows = rows, p.hosts = hosts, p.width = width, p.col0 = h0, p.col_end = hn, p.m_rows = rn;
                 p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
-                p.c = kLog2e / c.T, p.stats = stats, p.stats_stride = 2 + c.k, p.grad_loss = grad_loss, p.grad_scale = scale, p.range = range;
+                p.c = kLog2e / c.T, p.stats = stats, p.stats_stride = 2 + c.k, p.grad_loss = grad_loss, p.range = range;
                 const bool few = c.k <= kFewEntries;
                 if (few) p.ids = c.ids, p.teacher = c.teacher, p.teacher_stride = c.teacher_stride, p.k = c.k;
                 const int used = p.t.units < pairs ? (int)p.t.units : pairs;
@@ -1298,7 +1296,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                     PatchArgs q = {};
                     q.groups = gn, q.group0 = g0, q.row0 = r0, q.rows_here = rn, q.rows = rows, q.host0 = h0, q.hosts_here = hn, q.hosts = hosts, q.k = c.k;
                     q.ids = c.ids, q.teacher = c.teacher, q.teacher_stride = c.teacher_stride, q.stats = stats, q.grad_loss = grad_loss, q.range = range;
-                    q.grad_scale = scale, q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
+                    q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
                     int lanes = 1;
                     while (lanes < 32 && lanes < c.k) lanes *= 2;
                     e = launch_next(patch_kernel<T>, dim3((unsigned int)(((long long)gn * rn * lanes + 255) / 256)), 256, 0, c.stream, q, lanes);
