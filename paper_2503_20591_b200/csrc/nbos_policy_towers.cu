@@ -26,6 +26,7 @@ constexpr int kParts = 4;             // a tile's columns are read in this many 
 constexpr int kEpilogue = 128 * kParts;
 constexpr int kThreads = kEpilogue + 64;   // and a warp that copies, a warp that multiplies
 constexpr int kTmemColumns = 512;     // two tiles of 32-bit products
+constexpr int kFewRows = 64;          // up to as many rows a group, G is held as two 16-bit values, one after the other (see backward)
 constexpr int kBand = 16;             // tiles of hosts that G's rows go through together
 constexpr int kFewEntries = 4;        // a row's entries that are put into G on its way out; more of them by a kernel of their own
 constexpr size_t kPieceBytes = 512u << 20;   // 65,536 x 4,096 at width 256, gradients: 48 MB 950 us, 128 MB 650, 256 MB 586, 512 MB 567: launches fill the GPU
@@ -54,6 +55,7 @@ struct TowerArgs {
     Tiles t;
     int a_z0, a_z, b_z0, b_z;         // group g is slice z0 + g * z of the operand
     int a_m0, b_n0, b_k0;             // first row of the operand
+    int k_plane, plane_z;             // gradients: blocks of the contraction in a plane of G, and slices from one plane to the next
     int group0, row0, rows, hosts, width;   // rows: of a group
     int col0, col_end;                // scores: the launch's first host, and how many it has
     const int4 *asks, *room;
@@ -267,10 +269,13 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __half)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+
 // The entries of row `at`: their columns of this launch's hosts (-1: none) and G there. Entries that name one host add up, and
 // each of them holds the sum.
-template <typename T>
-__device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bool inside, int (&column)[kFewEntries], T (&value)[kFewEntries])
+template <int PLANES, typename T>
+__device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bool inside, int (&column)[kFewEntries], T (&value)[PLANES][kFewEntries])
 {
     const float *stats = a.stats + at * a.stats_stride;
     float t[kFewEntries], x[kFewEntries], top = neg_inf(), sum = 0.0f;
@@ -298,7 +303,9 @@ __device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bo
         for (int l = 0; l < kFewEntries; ++l) q += id[l] == id[j] ? t[l] : 0.0f;
         const bool put = some && x[j] != neg_inf() && id[j] >= a.col0 && id[j] < a.col0 + a.col_end;
         column[j] = put ? id[j] - a.col0 : -1;
-        value[j] = from_float<T>((exp2_fast(fmaf(x[j] - m, a.c, minus)) - q / sum) * factor);
+        const float g = (exp2_fast(fmaf(x[j] - m, a.c, minus)) - q / sum) * factor;
+        value[0][j] = from_float<T>(g);
+        if (PLANES == 2) value[PLANES - 1][j] = from_float<T>(g - to_float(value[0][j]));
     }
 }
 
@@ -307,7 +314,7 @@ __device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bo
 // block read the other. No wait is without a limit: when one runs out the block's flag goes up, copies and products stop, the
 // readers go through the rest of their units without waiting (so that their barriers stay matched), and the status
 // word says that the outputs are undefined.
-template <Kind KIND, int BN, bool MASK, typename T>
+template <Kind KIND, int BN, bool MASK, int PLANES, typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tower_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                  const __grid_constant__ CUtensorMap map_g, const __grid_constant__ TowerArgs args)
@@ -365,17 +372,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     const uint32_t bar = peer_addr(full + 8 * stage, 0);
                     if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * S::kStageBytes);
                     const uint32_t a = base + stage * S::kStageBytes, b = a + S::kBytesA;
+                    const int plane = kb >= args.k_plane, k = (kb - plane * args.k_plane) * kBlockK, z = az + plane * args.plane_z;
                     if (S::kAlongKA) {
-                        load_box(a, &map_a, kb * kBlockK, args.a_m0 + m0, az, bar);
+                        load_box(a, &map_a, k, args.a_m0 + m0, z, bar);
                     } else {
-                        load_box(a, &map_a, m0, kb * kBlockK, az, bar);
-                        load_box(a + 64 * 128, &map_a, m0 + 64, kb * kBlockK, az, bar);
+                        load_box(a, &map_a, m0, k, z, bar);
+                        load_box(a + 64 * 128, &map_a, m0 + 64, k, z, bar);
                     }
                     if (S::kAlongKB) {
-                        load_box(b, &map_b, kb * kBlockK, args.b_n0 + n0, bz, bar);
+                        load_box(b, &map_b, k, args.b_n0 + n0, bz, bar);
                     } else {
-                        load_box(b, &map_b, n0, args.b_k0 + kb * kBlockK, bz, bar);
-                        if (BN == 256) load_box(b + 64 * 128, &map_b, n0 + 64, args.b_k0 + kb * kBlockK, bz, bar);
+                        load_box(b, &map_b, n0, args.b_k0 + k, bz, bar);
+                        if (BN == 256) load_box(b + 64 * 128, &map_b, n0 + 64, args.b_k0 + k, bz, bar);
                     }
                     ++copied;
                     if (++stage == S::kStages) stage = 0, phase ^= 1;
@@ -438,7 +446,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         // GRAD: the few entries of the row that this lane puts in: columns, and what stands there, p - q rounded once
         const int entry_row = MASK ? lane / 4 + 8 * (lane % 4) : lane;
         int entry_at[kFewEntries];
-        T entry[kFewEntries];
+        T entry[PLANES][kFewEntries];
         int slot = 0;
         auto release = [&] {
             fence_before();
@@ -513,82 +521,89 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 const uint32_t at = lane_at + buffer * kTileN;
                 const int n0 = u.n * BN + quarter * 64;
                 const uint32_t box = staging + warp * 32 * 128;   // the warp's own, 32 rows
-                if (KIND == GRAD) {
-                    if (lane == 0) stores_read_wait<0>();         // the tile before has left it
-                    __syncwarp();
-                }
-                // p f of two columns in one word
-                auto word = [&](uint32_t x0, uint32_t x1, float from, float less, float by, bool none) {
-                    float e0, e1;
-                    apart2(e0, e1, x0, x1, from, args.c, less);
-                    e0 = exp2_fast(e0), e1 = exp2_fast(e1);
-                    mul2(e0, e1, by, by);
-                    const uint32_t w = pack2(e0, e1, T());
-                    return some_dead && none ? 0u : w;
-                };
-                if constexpr (MASK) {
 #pragma unroll 1
-                    for (int sub = 0; sub < 2; ++sub) {
-                        uint32_t v[2][16];
-                        tmem_load16(v[0], at + 32 * sub), tmem_load16(v[1], at + 32 * sub + (16u << 16));
+                for (int plane = 0; plane < PLANES; ++plane) {   // GRAD: what is rounded off goes to the second
+                    if (KIND == GRAD) {
+                        if (lane == 0) stores_read_wait<0>();         // what was in it before has left
+                        __syncwarp();
+                    }
+                    // p f of two columns in one word
+                    auto word = [&](uint32_t x0, uint32_t x1, float from, float less, float by, bool none) {
+                        float e0, e1;
+                        apart2(e0, e1, x0, x1, from, args.c, less);
+                        e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+                        mul2(e0, e1, by, by);
+                        uint32_t w = pack2(e0, e1, T());
+                        if (PLANES == 2 && plane == 1) {
+                            const float2 first = unpack2(w, T());
+                            w = pack2(e0 - first.x, e1 - first.y, T());
+                        }
+                        return some_dead && none ? 0u : w;
+                    };
+                    if constexpr (MASK) {
+#pragma unroll 1
+                        for (int sub = 0; sub < 2; ++sub) {
+                            uint32_t v[2][16];
+                            tmem_load16(v[0], at + 32 * sub), tmem_load16(v[1], at + 32 * sub + (16u << 16));
+                            tmem_wait(v[0]);
+                            tmem_wait(v[1]);
+                            if (sub == 1 && plane == PLANES - 1) release();
+                            mask_rows(v, columns + 32 * sub, ask);
+                            if constexpr (KIND == STATS) {
+#pragma unroll
+                                for (int i = 0; i < ROWS; ++i) add8(run_m[i], run_s[i], v, i, args.c);
+                            } else {   // 16-byte piece 4 sub + j of a line, four lanes a word each
+#pragma unroll
+                                for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) {
+                                        const int line = row_at(i) % 32, x = 4 * j + 2 * (i % 2);
+                                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(box + line * 128 + (((4 * sub + j) ^ (line & 7)) << 4) + lane % 4 * 4),
+                                                     "r"(word(v[i / 2][x], v[i / 2][x + 1], run_m[i], minus[i], factor[i], dead[i]))
+                                                     : "memory");
+                                    }
+                            }
+                        }
+                    } else {
+                        uint32_t v[2][32];
+                        tmem_load32(v[0], at), tmem_load32(v[1], at + 32);
                         tmem_wait(v[0]);
                         tmem_wait(v[1]);
-                        if (sub == 1) release();
-                        mask_rows(v, columns + 32 * sub, ask);
+                        if (plane == PLANES - 1) release();
+                        cut64(v[0], v[1], args.col_end - n0);
                         if constexpr (KIND == STATS) {
+                            add64(run_m[0], run_s[0], v[0], v[1], args.c);
+                        } else {
 #pragma unroll
-                            for (int i = 0; i < ROWS; ++i) add8(run_m[i], run_s[i], v, i, args.c);
-                        } else {   // 16-byte piece 4 sub + j of a line, four lanes a word each
-#pragma unroll
-                            for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    const int line = row_at(i) % 32, x = 4 * j + 2 * (i % 2);
-                                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(box + line * 128 + (((4 * sub + j) ^ (line & 7)) << 4) + lane % 4 * 4),
-                                                 "r"(word(v[i / 2][x], v[i / 2][x + 1], run_m[i], minus[i], factor[i], dead[i]))
-                                                 : "memory");
-                                }
-                        }
-                    }
-                } else {
-                    uint32_t v[2][32];
-                    tmem_load32(v[0], at), tmem_load32(v[1], at + 32);
-                    tmem_wait(v[0]);
-                    tmem_wait(v[1]);
-                    release();
-                    cut64(v[0], v[1], args.col_end - n0);
-                    if constexpr (KIND == STATS) {
-                        add64(run_m[0], run_s[0], v[0], v[1], args.c);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const uint32_t(&x)[32] = v[j / 4];
-                            const int k = 8 * (j % 4);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)),
-                                         "r"(word(x[k], x[k + 1], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 2], x[k + 3], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 4], x[k + 5], run_m[0], minus[0], factor[0], dead[0])),
-                                         "r"(word(x[k + 6], x[k + 7], run_m[0], minus[0], factor[0], dead[0]))
-                                         : "memory");
-                        }
-                    }
-                }
-                if (KIND == GRAD) {
-                    if (args.ids) {
-                        __syncwarp();
-#pragma unroll
-                        for (int j = 0; j < kFewEntries; ++j) {
-                            const int col = entry_at[j] - n0;
-                            if ((unsigned int)col < 64u)
-                                asm volatile("st.shared.b16 [%0], %1;" ::"r"(box + entry_row * 128 + (((col / 8) ^ (entry_row & 7)) << 4) + col % 8 * 2),
-                                             "h"(*reinterpret_cast<const unsigned short *>(&entry[j]))
+                            for (int j = 0; j < 8; ++j) {
+                                const uint32_t(&x)[32] = v[j / 4];
+                                const int k = 8 * (j % 4);
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)),
+                                             "r"(word(x[k], x[k + 1], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 2], x[k + 3], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 4], x[k + 5], run_m[0], minus[0], factor[0], dead[0])),
+                                             "r"(word(x[k + 6], x[k + 7], run_m[0], minus[0], factor[0], dead[0]))
                                              : "memory");
+                            }
                         }
                     }
-                    async_proxy_fence();
-                    __syncwarp();
-                    if (lane == 0) {
-                        const int y = u.m * kTileM + (int)rank * 128 + warp % 4 * 32;
-                        if (n0 < args.col_end && y < args.m_rows) store_box(&map_g, n0, y, u.g, box);
-                        stores_commit();
+                    if (KIND == GRAD) {
+                        if (args.ids) {
+                            __syncwarp();
+#pragma unroll
+                            for (int j = 0; j < kFewEntries; ++j) {
+                                const int col = entry_at[j] - n0;
+                                if ((unsigned int)col < 64u)
+                                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(box + entry_row * 128 + (((col / 8) ^ (entry_row & 7)) << 4) + col % 8 * 2),
+                                                 "h"(*reinterpret_cast<const unsigned short *>(&entry[PLANES == 2 ? plane : 0][j]))
+                                                 : "memory");
+                            }
+                        }
+                        async_proxy_fence();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const int y = u.m * kTileM + (int)rank * 128 + warp % 4 * 32;
+                            if (n0 < args.col_end && y < args.m_rows) store_box(&map_g, n0, y, u.g + plane * t.groups, box);
+                            stores_commit();
+                        }
                     }
                 }
             } else {
@@ -851,7 +866,7 @@ struct PatchArgs {
     Range range;
     float c;
     void *grad;
-    long long grad_stride, grad_group_stride;
+    long long grad_stride, grad_group_stride, plane_stride;   // plane_stride 0: one plane
 };
 // G at the teacher's hosts, p - q rounded once. `lanes` lanes a row (a power of two); entries that name one host add up.
 template <typename T>
@@ -890,7 +905,10 @@ __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ Patc
             if (ids[l] == id && t > neg_inf()) q += exp2_fast((t - top) * p.c);
         }
         const float prob = exp2_fast(fmaf(stats[2 + j] - m, p.c, minus));
-        static_cast<T *>(p.grad)[g * p.grad_group_stride + row * p.grad_stride + id - p.host0] = from_float<T>((prob - q / sum) * factor);
+        const float value = (prob - q / sum) * factor;
+        T *const to = static_cast<T *>(p.grad) + g * p.grad_group_stride + row * p.grad_stride + id - p.host0;
+        *to = from_float<T>(value);
+        if (p.plane_stride) to[p.plane_stride] = from_float<T>(value - to_float(from_float<T>(value)));
     }
 }
 
@@ -1013,10 +1031,10 @@ private:
     cudaStream_t stream_ = nullptr;
 };
 
-template <Kind KIND, int BN, bool MASK, typename T>
+template <Kind KIND, int BN, bool MASK, int PLANES, typename T>
 cudaError_t launch_tower(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &g, const TowerArgs &args, int pairs, cudaStream_t stream)
 {
-    auto *kernel = tower_kernel<KIND, BN, MASK, T>;
+    auto *kernel = tower_kernel<KIND, BN, MASK, PLANES, T>;
     // once a device (a bit each; two threads that meet here set the same value twice)
     static std::atomic<unsigned long long> allowed{0};
     int device = 0;
@@ -1143,7 +1161,7 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     Operand b = plan_operand(ws, in->hosts, in->n_hosts, in->host_stride, in->n_groups, in->host_group_stride, in->width);
     TowerArgs args = {};
     args.t.groups = in->n_groups, args.t.m_tiles = ceil_div(in->rows, kTileM), args.t.n_tiles = ceil_div(in->n_hosts, kTileN);
-    args.t.k_blocks = args.t.split_blocks = ceil_div(in->width, kBlockK), args.t.splits = 1;
+    args.t.k_blocks = args.t.split_blocks = args.k_plane = ceil_div(in->width, kBlockK), args.t.splits = 1;
     args.t.units = (long long)args.t.groups * args.t.m_tiles * args.t.n_tiles;
     const int pairs = args.t.units < c.sms / 2 ? (int)args.t.units : c.sms / 2;
     // a row's tiles lie with at most this many pairs, each of which leaves kParts parts
@@ -1161,8 +1179,8 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     args.asks = reinterpret_cast<const int4 *>(in->asks), args.room = reinterpret_cast<const int4 *>(in->room);
     args.c = kLog2e / c.T;
     args.partial = ws.at<float2>(o_partial);
-    e = in->asks ? launch_tower<STATS, kTileN, true, T>(map_a, map_b, map_a, args, pairs, c.stream)
-                 : launch_tower<STATS, kTileN, false, T>(map_a, map_b, map_a, args, pairs, c.stream);
+    e = in->asks ? launch_tower<STATS, kTileN, true, 1, T>(map_a, map_b, map_a, args, pairs, c.stream)
+                 : launch_tower<STATS, kTileN, false, 1, T>(map_a, map_b, map_a, args, pairs, c.stream);
     if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
     FinishArgs f = {};
     f.a = a.table.data, f.b = b.table.data, f.a_stride = a.table.stride, f.a_group_stride = a.table.group_stride;
@@ -1198,7 +1216,7 @@ template <Kind KIND, typename T>
 cudaError_t launch_gradient(const CUtensorMap &a, const CUtensorMap &b, const TowerArgs &args, bool narrow, int pairs, cudaStream_t stream)
 {
     const int p = args.t.units < pairs ? (int)args.t.units : pairs;
-    return narrow ? launch_tower<KIND, 128, false, T>(a, b, a, args, p, stream) : launch_tower<KIND, 256, false, T>(a, b, a, args, p, stream);
+    return narrow ? launch_tower<KIND, 128, false, 1, T>(a, b, a, args, p, stream) : launch_tower<KIND, 256, false, 1, T>(a, b, a, args, p, stream);
 }
 
 template <typename T>
@@ -1209,7 +1227,11 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
     const int groups = in->n_groups, rows = (int)in->rows, hosts = in->n_hosts, width = in->width, pairs = c.sms / 2;
     // Pieces of G: whole groups while they fit; of a group that does not, runs along its longer side, so that the gradient
     // that has to be added up over the pieces is the smaller one.
-    const size_t group_bytes = (size_t)rows * ((hosts + 63) & ~63) * 2;
+    // A gradient of few rows is a sum of few large terms, whose roundings do not average out: there G is held as two 16-bit values,
+    // the second what rounding took off the first, and the contractions go over both. (Errors against 64 bits, relative to the
+    // plain form's: one value 2.5 at one row, 1.5 to 1.6 at two and three, at most 1.45 from 64 on; two values 1.0 throughout.)
+    const int planes = rows <= kFewRows ? 2 : 1;
+    const size_t group_bytes = (size_t)rows * ((hosts + 63) & ~63) * 2 * planes;
     int piece_groups = 1, piece_rows = rows, piece_hosts = hosts;
     auto even = [&](int n, int tile) {   // whole tiles, pieces of much the same size
         const int pieces = (int)((group_bytes + kPieceBytes - 1) / kPieceBytes), size = ceil_div(ceil_div(n, pieces), tile) * tile;
@@ -1233,8 +1255,8 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
         t.units = (long long)gn * t.m_tiles * n;
         return t;
     };
-    Tiles ta = tiles(piece_groups, piece_rows, n_tiles, ceil_div(piece_hosts, kBlockK));
-    Tiles tb = tiles(piece_groups, piece_hosts, n_tiles, ceil_div(piece_rows, kBlockK));
+    Tiles ta = tiles(piece_groups, piece_rows, n_tiles, planes * ceil_div(piece_hosts, kBlockK));
+    Tiles tb = tiles(piece_groups, piece_hosts, n_tiles, planes * ceil_div(piece_rows, kBlockK));
     plan_splits(ta, pairs);
     plan_splits(tb, pairs);
     const bool sums_a = ta.splits > 1 || cut_hosts, sums_b = tb.splits > 1 || cut_rows;
@@ -1242,7 +1264,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
     Workspace ws;
     Operand a = plan_operand(ws, in->requests, rows, in->request_stride, groups, in->request_group_stride, width);
     Operand b = plan_operand(ws, in->hosts, hosts, in->host_stride, groups, in->host_group_stride, width);
-    const size_t o_g = ws.add((size_t)piece_groups * piece_rows * g_stride * 2);
+    const size_t o_g = ws.add((size_t)planes * piece_groups * piece_rows * g_stride * 2);
     const size_t o_a = ws.add(grad_a && sums_a ? sizeof(float) * ta.splits * piece_groups * piece_rows * width : 0);
     const size_t o_b = ws.add(grad_b && sums_b ? sizeof(float) * tb.splits * piece_groups * piece_hosts * width : 0);
     const size_t o_largest = ws.add(16);
@@ -1274,13 +1296,13 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
             for (int h0 = 0; h0 < hosts; h0 += piece_hosts) {
                 const int gn = groups - g0 < piece_groups ? groups - g0 : piece_groups;
                 const int rn = rows - r0 < piece_rows ? rows - r0 : piece_rows, hn = hosts - h0 < piece_hosts ? hosts - h0 : piece_hosts;
-                const Table piece{g, g_stride, (long long)piece_rows * g_stride, gn, rn, hn};
+                const Table piece{g, g_stride, (long long)piece_rows * g_stride, planes * gn, rn, hn};
                 CUtensorMap g_out, g_rows, g_cols;   // written, and read along rows and across them
                 if ((rc = make_map(&g_out, piece, 32, in->dtype)) || (rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype)))
                     return rc;
 
                 TowerArgs p = {};
-                p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK));
+                p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK)), p.k_plane = p.t.k_blocks;
                 p.a_z = az, p.a_z0 = g0 * az, p.b_z = bz, p.b_z0 = g0 * bz, p.a_m0 = r0, p.b_n0 = h0;
                 p.group0 = g0, p.row0 = r0, p.rows = rows, p.hosts = hosts, p.width = width, p.col0 = h0, p.col_end = hn, p.m_rows = rn;
                 p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
@@ -1288,8 +1310,12 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 const bool few = c.k <= kFewEntries;
                 if (few) p.ids = c.ids, p.teacher = c.teacher, p.teacher_stride = c.teacher_stride, p.k = c.k;
                 const int used = p.t.units < pairs ? (int)p.t.units : pairs;
-                e = in->asks ? launch_tower<GRAD, kTileN, true, T>(a_rows, b_rows, g_out, p, used, c.stream)
-                             : launch_tower<GRAD, kTileN, false, T>(a_rows, b_rows, g_out, p, used, c.stream);
+                if (planes == 2)
+                    e = in->asks ? launch_tower<GRAD, kTileN, true, 2, T>(a_rows, b_rows, g_out, p, used, c.stream)
+                                 : launch_tower<GRAD, kTileN, false, 2, T>(a_rows, b_rows, g_out, p, used, c.stream);
+                else
+                    e = in->asks ? launch_tower<GRAD, kTileN, true, 1, T>(a_rows, b_rows, g_out, p, used, c.stream)
+                                 : launch_tower<GRAD, kTileN, false, 1, T>(a_rows, b_rows, g_out, p, used, c.stream);
                 if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
 
                 if (!few) {
@@ -1297,6 +1323,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                     q.groups = gn, q.group0 = g0, q.row0 = r0, q.rows_here = rn, q.rows = rows, q.host0 = h0, q.hosts_here = hn, q.hosts = hosts, q.k = c.k;
                     q.ids = c.ids, q.teacher = c.teacher, q.teacher_stride = c.teacher_stride, q.stats = stats, q.grad_loss = grad_loss, q.range = range;
                     q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
+                    q.plane_stride = planes == 2 ? gn * piece.group_stride : 0;
                     int lanes = 1;
                     while (lanes < 32 && lanes < c.k) lanes *= 2;
                     e = launch_next(patch_kernel<T>, dim3((unsigned int)(((long long)gn * rn * lanes + 255) / 256)), 256, 0, c.stream, q, lanes);
@@ -1305,7 +1332,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
 
                 if (grad_a) {
                     TowerArgs d = {};
-                    d.t = ta, d.t.groups = gn, d.t.m_tiles = ceil_div(rn, kTileM), d.t.k_blocks = ceil_div(hn, kBlockK);
+                    d.t = ta, d.t.groups = gn, d.t.m_tiles = ceil_div(rn, kTileM), d.k_plane = ceil_div(hn, kBlockK), d.plane_z = gn, d.t.k_blocks = planes * d.k_plane;
                     d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
                     d.a_z = 1, d.b_z = bz, d.b_z0 = g0 * bz, d.b_k0 = h0;
                     d.group0 = g0, d.width = width, d.range = range, d.m_rows = rn, d.out_row0 = r0;
@@ -1321,7 +1348,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 }
                 if (grad_b) {
                     TowerArgs d = {};
-                    d.t = tb, d.t.groups = gn, d.t.m_tiles = ceil_div(hn, kTileM), d.t.k_blocks = ceil_div(rn, kBlockK);
+                    d.t = tb, d.t.groups = gn, d.t.m_tiles = ceil_div(hn, kTileM), d.k_plane = ceil_div(rn, kBlockK), d.plane_z = gn, d.t.k_blocks = planes * d.k_plane;
                     d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
                     d.a_z = 1, d.b_z = az, d.b_z0 = g0 * az, d.b_k0 = r0;
                     d.group0 = g0, d.width = width, d.range = range, d.m_rows = hn, d.out_row0 = h0;

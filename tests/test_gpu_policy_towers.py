@@ -9,6 +9,7 @@ Tolerances, derived once. Vectors are 16-bit values, so products of two are exac
   loss: T^2 times the error of ln p and ln q, and of sums of terms of size L: T^2 (2 rho + 64 2^-24 (1 + L)).
   G = f (p - q), f = T scale grad_loss: |dG| <= f (p + q) rho + half a step of the type (2^-8 |G| in bf16, 2^-11 |G| in f16; below
   f16's normal numbers half of its smallest step, 2^-25, over the factor that G carries, at least 2^14 / max f).
+  Up to 64 rows a group G is held as two values, the second what the first's rounding took: half a step of half a step.
   da = G b: |dG| |b| + (H + 64) 2^-23 |G| |b| (sums in 32 bits) + half a step of the result. db alike.
 """
 from __future__ import annotations
@@ -66,8 +67,9 @@ def make(groups, rows, hosts, width, k, dtype, mask, seed, pad=0, shift=0):
     return c
 
 
-def reference(c, T, f):
-    """loss, G's two products, and their tolerances, in 64 bits, one group at a time (f: factor of each row's gradient)."""
+def reference(c, T, f, values=1):
+    """loss, G's two products, and their tolerances, in 64 bits, one group at a time (f: factor of each row's gradient; G is held as
+    so many `values`)."""
     import torch
     out = []
     half = HALF[str(c["requests"].dtype)[6:]]
@@ -105,7 +107,7 @@ def reference(c, T, f):
         G.scatter_add_(1, ids, -q)
         Q = torch.zeros_like(G).scatter_add_(1, ids, q)
         G *= f[g][:, None]
-        dG = f[g].abs()[:, None] * (p + Q) * rho + half * G.abs()
+        dG = f[g].abs()[:, None] * (p + Q) * rho + half ** values * G.abs()
         if small:
             dG += 2.0 ** -25 * 2.0 ** -14 * f.abs().max()
         last = 2.0 ** -25 if small else 2.0 ** -133
@@ -136,14 +138,14 @@ def run(nb, c, T, scale, grad_loss, want=("a", "b")):
     return loss, da, db
 
 
-def check(nb, c, T=1.0, scale=1.0, grad_loss=None):
+def check(nb, c, T=1.0, scale=1.0, grad_loss=None, values=1):
     import torch
     shape = c["hosts"].shape[:-1]
     f = torch.full(shape, T * scale, dtype=torch.float64, device="cuda")
     if grad_loss is not None:
         f = f * grad_loss.double()
     loss, da, db = run(nb, c, T, scale, grad_loss)
-    want = reference(c, T, f)
+    want = reference(c, T, f, values)
     close(loss, *want[:2])
     close(da, *want[2:4])
     close(db, *want[4:])
@@ -165,6 +167,15 @@ def test_matches_the_formula(nb, groups, rows, hosts, width, mask, dtype):
         c = make(groups, rows, hosts, width, k, dtype, mask, 100 * i + rows + width, pad, shift)
         gl = torch.rand((groups, rows), device="cuda") + 0.5 if i != 1 else None
         check(nb, c, T, 8.0 if dtype == "float16" else 1.0 / rows, gl)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("mask,k", [(False, 1), (True, 4), (False, 9)])
+@pytest.mark.parametrize("groups,rows,hosts,width", [(1, 1, 300, 16), (1, 3, 5000, 24), (3, 2, 64, 8), (7, 33, 700, 65), (2, 64, 257, 16), (1, 64, 40000, 32)])
+def test_gradients_of_few_rows(nb, groups, rows, hosts, width, mask, k, dtype):
+    """What the first rounding of G takes off is not lost, the entries' included."""
+    c = make(groups, rows, hosts, width, k, dtype, mask, rows + width)
+    check(nb, c, 1.0, 8.0 if dtype == "float16" else 1.0, None, values=2)
 
 
 @pytest.mark.parametrize("groups,rows,hosts,width,what", [(1, 4099, 70001, 72, "runs of hosts"), (1, 70003, 4099, 72, "runs of rows"),
