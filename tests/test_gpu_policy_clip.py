@@ -252,3 +252,14 @@ def test_the_binding_refuses_wrong_tensors(nb):
             nb.nbos_policy_clip([x], 1.0, norm, outs)
     with pytest.raises(nb.NbosError, match="max_norm"):
         nb.nbos_policy_clip([x], -1.0, norm)
+
+
+def test_outputs_that_are_other_inputs(nb):
+    import torch
+    x, y, z = (torch.ones(32, device="cuda") for _ in range(3))
+    norm = torch.empty((), device="cuda")
+    for tensors, outs in (([x, y], [y, x]), ([x, y], [z, x]), ([x, x], [x, z])):
+        with pytest.raises(ValueError, match="another of the tensors"):
+            nb.nbos_policy_clip(tensors, 1.0, norm, outs)
+    nb.nbos_policy_clip([x, y], 1.0, norm, [x, z])   # one in place, one not
+    assert torch.equal(x, z) and float(x[0]) < 1 and (y == 1).all()
