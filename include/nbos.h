@@ -527,8 +527,8 @@ int nbos_policy_sample(const nbos_logits *logits, const float *uniforms, const f
  *   asks[g, r, i] >= 0 for all four i. (With asks = the requests of nbos_place_batch and room[0] = the GPUs that the host's size and
  *   subscription limit leave, that is the rule's own test.) asks and room NULL: every request fits every host.
  * Loss and gradient are those of nbos_policy_distill on these logits, row by row and entry by entry; rows that fit nowhere, or
- * without a counting entry, have loss and gradient 0 (a vector of theirs that is not finite may still make the other tower's
- * gradient NaN).
+ * without a counting entry, have loss and gradient 0. (A vector that is not finite may make the other tower's gradient NaN,
+ * also where none of its scores counts: 0 times it is not 0.)
  *     grad_requests = G hosts, grad_hosts = G^T requests, G = T * (p - q) * grad_scale * grad_loss[r]
  * Products are of 16-bit values with 32-bit sums, statistics are in 32 bits. G is rounded to the vectors' type (after a
  * factor that brings the largest |grad_loss| to just below a power of two, 2^15 in 16-bit floats) before it is multiplied - up to 64 rows

@@ -893,7 +893,7 @@ __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ Patc
         if (stats[2 + j] != neg_inf() && t > neg_inf()) sum += exp2_fast((t - top) * p.c);
     }
     sum = lanes_sum(sum, lanes);
-    if (!inside || !(sum > 0.0f)) return;
+    if (!inside || sum == 0.0f) return;   // (a sum that is not a number spoils the row)
     const float m = stats[0], minus = -log2f(stats[1]);
     const float factor = p.range.scale * (p.grad_loss ? p.grad_loss[at] : 1.0f) * p.range.factor();
     for (int j = sub; j < p.k; j += lanes) {

@@ -323,6 +323,20 @@ def test_a_row_that_is_not_finite_spoils_itself(nb):
     assert torch.equal(loss[0, rest], before[0][0, rest]) and torch.equal(da[0, rest], before[1][0, rest])
 
 
+@pytest.mark.parametrize("k", [3, 9])
+def test_a_teacher_logit_that_is_infinite_spoils_its_row(nb, k):
+    """Its weight is inf / inf, whichever kernel puts the row's entries in."""
+    import torch
+    c = make(1, 30, 300, 32, k, "float16", False, 22)
+    c["hosts"][...] = torch.arange(k, device="cuda", dtype=torch.int32)
+    before = run(nb, c, 1.0, 1.0, None, "a")
+    c["teacher_logits"][0, 11, 0] = INF
+    loss, da, _ = run(nb, c, 1.0, 1.0, None, "a")
+    rest = torch.arange(30, device="cuda") != 11
+    assert loss[0, 11].isnan() and da[0, 11].isnan().all()
+    assert torch.equal(loss[0, rest], before[0][0, rest]) and torch.equal(da[0, rest], before[1][0, rest])
+
+
 def test_one_table_of_hosts_for_all_groups(nb):
     """A group stride of 0 is read as it is; autograd adds the groups' gradients up."""
     import torch
@@ -432,3 +446,26 @@ def test_streams_and_graphs(nb):
     for _, *got in graphs:
         assert all(torch.equal(x, y) for x, y in zip(got, want[1]))
     del alive
+
+
+@pytest.mark.parametrize("rows,k", [(30, 3), (300, 9)])
+def test_captured_with_a_gradient_for_each_row(nb, rows, k):
+    """Forward and backward in one graph, whose factor follows the grad_loss of each replay."""
+    import torch
+    c = make(2, rows, 400, 44, k, "float16", True, 23)
+    gl = torch.rand(2, rows, device="cuda") + 0.5
+    stats, loss = torch.empty(2, rows, 2 + k, device="cuda"), torch.empty(2, rows, device="cuda")
+    grads = [torch.empty_like(c[n], memory_format=torch.contiguous_format) for n in ("requests", "host_vectors")]
+    args, fit = (c["requests"], c["host_vectors"], c["hosts"], c["teacher_logits"]), dict(asks=c["asks"], room=c["room"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nb.nbos_policy_towers(*args, loss, stats, **fit)
+        nb.nbos_policy_towers_backward(*args, stats, *grads, gl, **fit)
+    for factor in (1.0, 1000.0, 2.0 ** -9):
+        gl *= factor
+        want = run(nb, c, 1.0, 1.0, gl)
+        for t in (loss, *grads):
+            t.fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((loss, *grads), want))
