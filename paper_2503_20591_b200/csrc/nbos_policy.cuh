@@ -365,6 +365,20 @@ __device__ __forceinline__ V *cluster_peer(V *shared, int rank, int cs)
     return cs > 1 ? cooperative_groups::this_cluster().map_shared_rank(shared, rank) : shared;
 }
 
+// 16 of the 32 bytes lo, hi, from byte `from` on
+__device__ __forceinline__ uint4 window16(const uint4 &lo, const uint4 &hi, int from)
+{
+    unsigned int w[7] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z};
+    if (from & 8) w[0] = w[2], w[1] = w[3], w[2] = w[4], w[3] = w[5], w[4] = w[6], w[5] = hi.w;
+    if (from & 4) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = w[4], w[4] = w[5];
+    if (from & 3) {
+        const int bits = (from & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // ---- kernels in a row --------------------------------------------------------------------------------------
 // A kernel launched by launch_next may start while the one before it in the stream still runs: it sets itself up and
 // then waits, before it touches memory, until that one has finished and its results can be seen. Every kernel of such a row waits.

@@ -145,19 +145,6 @@ __device__ __forceinline__ float row_sum(float v, int team, float4 (*warps)[8], 
     return v;
 }
 
-// 16 of the 32 bytes lo, hi, from byte `from` on
-__device__ __forceinline__ uint4 window16(const uint4 &lo, const uint4 &hi, int from)
-{
-    unsigned int w[7] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z};
-    if (from & 8) w[0] = w[2], w[1] = w[3], w[2] = w[4], w[3] = w[5], w[4] = w[6], w[5] = hi.w;
-    if (from & 4) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = w[4], w[4] = w[5];
-    if (from & 3) {
-        const int bits = (from & 3) * 8;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 template <bool BLOCK>
 __device__ __forceinline__ void team_sync()
 {

@@ -55,7 +55,8 @@ struct TowerArgs {
     Tiles t;
     int a_z0, a_z, b_z0, b_z;         // group g is slice z0 + g * z of the operand
     int a_m0, b_n0, b_k0;             // first row of the operand
-    int k_plane, plane_z;             // gradients: blocks of the contraction in a plane of G, and slices from one plane to the next
+    int k_shift, plane_z;             // gradients: 1 if G has two planes, which take turns in the contraction (what both are multiplied with
+                                      // is then read from memory once), and the slices from one to the next
     int group0, row0, rows, hosts, width;   // rows: of a group
     int col0, col_end;                // scores: the launch's first host, and how many it has
     const int4 *asks, *room;
@@ -71,8 +72,9 @@ struct TowerArgs {
     const float *grad_loss;
     Range range;
     void *out;                        // gradients: the result itself (one part), or
-    float *sums;                      // [splits][groups][m_rows][width] of 32-bit sums, added to those there if `add`
+    float *sums;                      // [splits][groups][m_rows][width to a multiple of 4] of 32-bit sums, added to those there if `add`
     long long out_stride, out_group_stride;
+    bool out_wide;                    // rows of the result lie on 16-byte boundaries
     int m_rows, out_row0, add;        // m_rows: rows that the launch writes, per group
 };
 
@@ -152,7 +154,8 @@ template <Kind KIND, int BN>
 struct Shape {
     static constexpr bool kAlongKA = KIND != GRAD_HOSTS, kAlongKB = KIND == STATS || KIND == GRAD;
     static constexpr int kBytesA = 128 * kBlockK * 2, kBytesB = BN / 2 * kBlockK * 2, kStageBytes = kBytesA + kBytesB;
-    static constexpr int kStaging = KIND == GRAD ? 4 * 128 * 128 : 0;    // G on its way out: a box of 32 rows x 64 columns a warp
+    // what is on its way out, a box a warp: G, 32 rows x 64 columns; a gradient, 32 x 32
+    static constexpr int kStaging = KIND == GRAD ? 4 * 128 * 128 : KIND == STATS ? 0 : 4 * 128 * 64;
     static constexpr int kRoom = KIND == STATS || KIND == GRAD ? 2 * kTileN * 16 : 0;
     static constexpr int kStages = KIND == GRAD ? 4 : 6;
     static constexpr int kBytes = kStages * kStageBytes + kStaging + kRoom + 256 /* barriers */ + 1024 /* alignment */;
@@ -372,7 +375,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     const uint32_t bar = peer_addr(full + 8 * stage, 0);
                     if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * S::kStageBytes);
                     const uint32_t a = base + stage * S::kStageBytes, b = a + S::kBytesA;
-                    const int plane = kb >= args.k_plane, k = (kb - plane * args.k_plane) * kBlockK, z = az + plane * args.plane_z;
+                    const int k = (kb >> args.k_shift) * kBlockK, z = az + (kb & args.k_shift) * args.plane_z;
                     if (S::kAlongKA) {
                         load_box(a, &map_a, k, args.a_m0 + m0, z, bar);
                     } else {
@@ -613,6 +616,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                 for (int sub = 0; sub < BN / kParts / 32; ++sub) {
                     uint32_t v[32];
+                    __syncwarp();   // lanes without a row went past the stores
                     tmem_load32(v, lane_at + buffer * kTileN + 32 * sub);
                     tmem_wait(v);
                     if (sub == BN / kParts / 32 - 1) release();
@@ -620,41 +624,54 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = 0u;
                     }
-                    const int n0 = n_first + 32 * sub, cols = min(32, args.width - n0);
-                    if (local >= args.m_rows || cols <= 0) continue;
+                    const int n0 = n_first + 32 * sub, first = u.m * kTileM + (int)rank * 128 + warp % 4 * 32, rows_here = min(32, args.m_rows - first);
+                    if (rows_here <= 0 || n0 >= args.width) continue;
                     if (args.sums) {
-                        float *to = args.sums + (((long long)u.split * t.groups + u.g) * args.m_rows + local) * args.width + n0;
-                        if (cols == 32 && args.width % 4 == 0) {
+                        const int wide = (args.width + 3) & ~3;
+                        float *to = args.sums + (((long long)u.split * t.groups + u.g) * args.m_rows + local) * wide + n0;
 #pragma unroll
-                            for (int i = 0; i < 32; i += 4) {
-                                float4 w = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]),
-                                                       __uint_as_float(v[i + 3]));
-                                if (args.add) {
-                                    const float4 old = *reinterpret_cast<const float4 *>(to + i);
-                                    w.x += old.x, w.y += old.y, w.z += old.z, w.w += old.w;
-                                }
-                                *reinterpret_cast<float4 *>(to + i) = w;
+                        for (int i = 0; i < 32; i += 4) {
+                            if (lane >= rows_here || n0 + i >= wide) break;
+                            float4 w = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+                            if (args.add) {
+                                const float4 old = *reinterpret_cast<const float4 *>(to + i);
+                                w.x += old.x, w.y += old.y, w.z += old.z, w.w += old.w;
                             }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (i < cols) to[i] = __uint_as_float(v[i]) + (args.add ? to[i] : 0.0f);
+                            *reinterpret_cast<float4 *>(to + i) = w;
                         }
+                        continue;
+                    }
+                    T *const out = static_cast<T *>(args.out) + (args.group0 + u.g) * args.out_group_stride + (args.out_row0 + (long long)first) * args.out_stride + n0;
+                    uint4 w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[8 * i + j]) * undo;
+                        w[i] = pack16(x, T());
+                    }
+                    if (args.out_wide && n0 + 32 <= args.width) {
+                        uint4 *const to = reinterpret_cast<uint4 *>(out + lane * args.out_stride);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (lane < rows_here) to[i] = w[i];
                     } else {
-                        T *to = static_cast<T *>(args.out) + (args.group0 + u.g) * args.out_group_stride +
-                                (args.out_row0 + (long long)local) * args.out_stride + n0;
-                        if (cols == 32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+                        // Rows that start anywhere, and their ends: a row at a time, a column a lane, through shared memory. (A row a lane, value by
+                        // value: 6 x 31,616 hosts at width 475, 790 us, this FIXME.)
+                        const uint32_t box = staging + warp * 32 * 64;
+                        __syncwarp();
 #pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                float w[8];
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) w[j] = __uint_as_float(v[i + j]) * undo;
-                                *reinterpret_cast<uint4 *>(to + i) = pack16(w, T());
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (i < cols) to[i] = from_float<T>(__uint_as_float(v[i]) * undo);
+                        for (int i = 0; i < 4; ++i)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 64 + ((i ^ (lane / 2 & 3)) << 4)), "r"(w[i].x), "r"(w[i].y),
+                                         "r"(w[i].z), "r"(w[i].w)
+                                         : "memory");
+                        __syncwarp();
+                        const bool mine = n0 + lane < args.width;
+#pragma unroll 8
+                        for (int r = 0; r < rows_here; ++r) {
+                            unsigned short x;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(box + r * 64 + ((lane / 8 ^ (r / 2 & 3)) << 4) + lane % 8 * 2) : "memory");
+                            if (mine) reinterpret_cast<unsigned short *>(out)[r * args.out_stride + lane] = x;
                         }
                     }
                 }
@@ -686,18 +703,28 @@ __global__ void lay_out_kernel(const T *src, long long stride, long long group_s
 {
     next_may_start();
     previous_done();
-    const int chunks = wide / 8;
+    const unsigned int chunks = wide / 8;
     const long long n = (long long)rows * chunks, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     src += blockIdx.y * group_stride;
     dst += (long long)blockIdx.y * rows * wide;
+    // Eight values from the 16-byte pieces that hold them (of which each holds one at least): 6 x 31,616 rows of 475, value by value 214 us,
+    // this 66.
+#pragma unroll 4
     for (long long i = first; i < n; i += (long long)gridDim.x * blockDim.x) {
-        const int row = (int)(i / chunks), col = (int)(i % chunks) * 8;
-        const T *from = src + row * stride + col;
-        unsigned short w[8];
+        const long long row = n <= 0xFFFFFFFFll ? (unsigned int)i / chunks : i / chunks;
+        const int col = (int)(i - row * chunks) * 8, left = min(8, width - col);
+        const uintptr_t from = reinterpret_cast<uintptr_t>(src + row * stride + col);
+        const int shift = (int)(from & 15);
+        const uint4 *const at = reinterpret_cast<const uint4 *>(from - shift);
+        uint4 w = at[0];
+        if (shift) w = window16(w, shift + 2 * left > 16 ? at[1] : make_uint4(0, 0, 0, 0), shift);
+        if (left < 8) {
+            unsigned int x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = col + j < width ? reinterpret_cast<const unsigned short *>(from)[j] : (unsigned short)0;
-        *reinterpret_cast<uint4 *>(dst + row * (long long)wide + col) =
-            make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16, w[6] | (uint32_t)w[7] << 16);
+            for (int j = 0; j < 4; ++j) x[j] = 2 * j + 1 < left ? x[j] : 2 * j < left ? x[j] & 0xFFFFu : 0u;
+            w = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        *reinterpret_cast<uint4 *>(dst + i * 8) = w;
     }
 }
 
@@ -912,33 +939,31 @@ __global__ void __launch_bounds__(256) patch_kernel(const __grid_constant__ Patc
     }
 }
 
-// The parts' sums become the gradient: [splits][groups][rows][width] -> rows out_stride apart.
+// The parts' sums become the gradient: [splits][groups][rows][width to a multiple of 4] -> rows `stride` apart.
 template <typename T>
 __global__ void sums_kernel(const float *sums, int splits, int groups, int rows, int width, Range range, T *out, long long stride,
                             long long group_stride)
 {
     next_may_start();
     previous_done();
-    const long long n = (long long)groups * rows * width;
+    const unsigned int quads = (width + 3) / 4;
+    const long long n = (long long)groups * rows * quads;
     const float undo = 1.0f / range.factor();
-    if (width % 4 == 0) {
-        for (long long i = ((long long)blockIdx.x * blockDim.x + threadIdx.x) * 4; i < n; i += (long long)gridDim.x * blockDim.x * 4) {
-            float4 s = *reinterpret_cast<const float4 *>(sums + i);
-            for (int k = 1; k < splits; ++k) {
-                const float4 v = *reinterpret_cast<const float4 *>(sums + k * n + i);
-                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-            }
-            const long long row = i / width;
-            T *to = out + row / rows * group_stride + row % rows * stride + i % width;
-            to[0] = from_float<T>(s.x * undo), to[1] = from_float<T>(s.y * undo), to[2] = from_float<T>(s.z * undo), to[3] = from_float<T>(s.w * undo);
-        }
-        return;
-    }
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
-        float s = sums[i];
-        for (int k = 1; k < splits; ++k) s += sums[k * n + i];
-        const long long row = i / width;
-        out[row / rows * group_stride + row % rows * stride + i % width] = from_float<T>(s * undo);
+        const float4 *const from = reinterpret_cast<const float4 *>(sums) + i;
+        float4 s = from[0];
+#pragma unroll 8
+        for (int k = 1; k < splits; ++k) {
+            const float4 v = from[k * n];
+            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+        }
+        const long long row = n <= 0xFFFFFFFFll ? (unsigned int)i / quads : i / quads;
+        const int col = (int)(i - row * quads) * 4;
+        T *const to = out + row / rows * group_stride + row % rows * stride + col;
+        const float x[4] = {s.x * undo, s.y * undo, s.z * undo, s.w * undo};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (col + j < width) to[j] = from_float<T>(x[j]);
     }
 }
 
@@ -1161,7 +1186,7 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     Operand b = plan_operand(ws, in->hosts, in->n_hosts, in->host_stride, in->n_groups, in->host_group_stride, in->width);
     TowerArgs args = {};
     args.t.groups = in->n_groups, args.t.m_tiles = ceil_div(in->rows, kTileM), args.t.n_tiles = ceil_div(in->n_hosts, kTileN);
-    args.t.k_blocks = args.t.split_blocks = args.k_plane = ceil_div(in->width, kBlockK), args.t.splits = 1;
+    args.t.k_blocks = args.t.split_blocks = ceil_div(in->width, kBlockK), args.t.splits = 1;
     args.t.units = (long long)args.t.groups * args.t.m_tiles * args.t.n_tiles;
     const int pairs = args.t.units < c.sms / 2 ? (int)args.t.units : c.sms / 2;
     // a row's tiles lie with at most this many pairs, each of which leaves kParts parts
@@ -1265,8 +1290,8 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
     Operand a = plan_operand(ws, in->requests, rows, in->request_stride, groups, in->request_group_stride, width);
     Operand b = plan_operand(ws, in->hosts, hosts, in->host_stride, groups, in->host_group_stride, width);
     const size_t o_g = ws.add((size_t)planes * piece_groups * piece_rows * g_stride * 2);
-    const size_t o_a = ws.add(grad_a && sums_a ? sizeof(float) * ta.splits * piece_groups * piece_rows * width : 0);
-    const size_t o_b = ws.add(grad_b && sums_b ? sizeof(float) * tb.splits * piece_groups * piece_hosts * width : 0);
+    const size_t o_a = ws.add(grad_a && sums_a ? sizeof(float) * ta.splits * piece_groups * piece_rows * ((width + 3) & ~3) : 0);
+    const size_t o_b = ws.add(grad_b && sums_b ? sizeof(float) * tb.splits * piece_groups * piece_hosts * ((width + 3) & ~3) : 0);
     const size_t o_largest = ws.add(16);
     int rc = ws.allocate(c.device, c.stream);
     if (rc) return rc;
@@ -1302,7 +1327,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                     return rc;
 
                 TowerArgs p = {};
-                p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK)), p.k_plane = p.t.k_blocks;
+                p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK));
                 p.a_z = az, p.a_z0 = g0 * az, p.b_z = bz, p.b_z0 = g0 * bz, p.a_m0 = r0, p.b_n0 = h0;
                 p.group0 = g0, p.row0 = r0, p.rows = rows, p.hosts = hosts, p.width = width, p.col0 = h0, p.col_end = hn, p.m_rows = rn;
                 p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
@@ -1332,11 +1357,11 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
 
                 if (grad_a) {
                     TowerArgs d = {};
-                    d.t = ta, d.t.groups = gn, d.t.m_tiles = ceil_div(rn, kTileM), d.k_plane = ceil_div(hn, kBlockK), d.plane_z = gn, d.t.k_blocks = planes * d.k_plane;
+                    d.t = ta, d.t.groups = gn, d.t.m_tiles = ceil_div(rn, kTileM), d.k_shift = planes - 1, d.plane_z = gn, d.t.k_blocks = planes * ceil_div(hn, kBlockK);
                     d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
                     d.a_z = 1, d.b_z = bz, d.b_z0 = g0 * bz, d.b_k0 = h0;
                     d.group0 = g0, d.width = width, d.range = range, d.m_rows = rn, d.out_row0 = r0;
-                    d.out = grad_a, d.out_stride = a_stride, d.out_group_stride = a_group_stride;
+                    d.out = grad_a, d.out_stride = a_stride, d.out_group_stride = a_group_stride, d.out_wide = readable(grad_a, rows, a_stride, groups, a_group_stride);
                     d.sums = sums_a ? ws.at<float>(o_a) : nullptr, d.add = h0 > 0;
                     e = launch_gradient<GRAD_REQUESTS, T>(g_rows, b_cols, d, narrow, pairs, c.stream);
                     if (e == cudaSuccess && sums_a && h0 + hn == hosts) {
@@ -1348,11 +1373,11 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 }
                 if (grad_b) {
                     TowerArgs d = {};
-                    d.t = tb, d.t.groups = gn, d.t.m_tiles = ceil_div(hn, kTileM), d.k_plane = ceil_div(rn, kBlockK), d.plane_z = gn, d.t.k_blocks = planes * d.k_plane;
+                    d.t = tb, d.t.groups = gn, d.t.m_tiles = ceil_div(hn, kTileM), d.k_shift = planes - 1, d.plane_z = gn, d.t.k_blocks = planes * ceil_div(rn, kBlockK);
                     d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
                     d.a_z = 1, d.b_z = az, d.b_z0 = g0 * az, d.b_k0 = r0;
                     d.group0 = g0, d.width = width, d.range = range, d.m_rows = hn, d.out_row0 = h0;
-                    d.out = grad_b, d.out_stride = b_stride, d.out_group_stride = b_group_stride;
+                    d.out = grad_b, d.out_stride = b_stride, d.out_group_stride = b_group_stride, d.out_wide = readable(grad_b, hosts, b_stride, groups, b_group_stride);
                     d.sums = sums_b ? ws.at<float>(o_b) : nullptr, d.add = r0 > 0;
                     e = launch_gradient<GRAD_HOSTS, T>(g_cols, a_cols, d, narrow, pairs, c.stream);
                     if (e == cudaSuccess && sums_b && r0 + rn == rows) {
