@@ -657,7 +657,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             if (lane < rows_here) to[i] = w[i];
                     } else {
                         // Rows that start anywhere, and their ends: a row at a time, a column a lane, through shared memory. (A row a lane, value by
-                        // value: 6 x 31,616 hosts at width 475, 790 us, this FIXME.)
+                        // value: 6 x 31,616 hosts at width 475, 790 us, this 105.)
                         const uint32_t box = staging + warp * 32 * 64;
                         __syncwarp();
 #pragma unroll
