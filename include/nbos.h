@@ -531,7 +531,7 @@ int nbos_policy_sample(const nbos_logits *logits, const float *uniforms, const f
  * also where none of its scores counts: 0 times it is not 0.)
  *     grad_requests = G hosts, grad_hosts = G^T requests, G = T * (p - q) * grad_scale * grad_loss[r]
  * Products are of 16-bit values with 32-bit sums, statistics are in 32 bits. G is rounded to the vectors' type (after a
- * factor that brings the largest |grad_loss| to just below a power of two, 2^15 in 16-bit floats) before it is multiplied - up to 64 rows
+ * factor that brings the largest finite |grad_loss| of a row that counts to just below a power of two, 2^15 in 16-bit floats) before it is multiplied - up to 64 rows
  * a group as two values, the second what the first's rounding took off -, a gradient once more at the end.
  *   towers          vectors DEVICE, NBOS_BF16 or NBOS_F16, of any alignment and row stride >= width; rows on 16-byte boundaries (address,
  *                   strides) are read as they lie, others are copied first. A group stride may be 0 (one table for all groups).

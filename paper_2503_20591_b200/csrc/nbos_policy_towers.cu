@@ -43,7 +43,7 @@ struct Tiles {                        // what one launch covers
 // a power of two lose twice the share), those of a p near 0 nothing; and 16-bit floats use their whole range: p of 2^-29 is still a
 // normal number.
 struct Range {
-    const unsigned int *largest;      // bits of the largest |grad_loss|; NULL: 1
+    const unsigned int *largest;      // bits of the largest finite |grad_loss| of a row that counts; NULL: 1
     float scale, top;                 // grad_scale T; 1 - 2^-8, in 16-bit floats times 2^15
     __device__ __forceinline__ float factor() const
     {
@@ -874,13 +874,17 @@ __global__ void __launch_bounds__(256, 4) finish_kernel(const __grid_constant__ 
     if (f.stats) f.stats[at * (2 + f.k)] = some ? top : 0.0f, f.stats[at * (2 + f.k) + 1] = some ? s : __int_as_float(0x7F800000);
 }
 
-__global__ void largest_kernel(const float *grad_loss, long long n, unsigned int *largest)
+// Rows without a counting entry (S is inf) have gradient 0 whatever arrives, and what is not finite spoils its row at any range: the
+// range follows neither.
+__global__ void largest_kernel(const float *grad_loss, const float *stats, int stats_stride, long long n, unsigned int *largest)
 {
     next_may_start();
     previous_done();
     float m = 0.0f;
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x)
-        m = fmaxf(m, fabsf(grad_loss[i]));
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
+        const float g = fabsf(grad_loss[i]);
+        if (g < __int_as_float(0x7F800000) && stats[i * stats_stride + 1] != __int_as_float(0x7F800000)) m = fmaxf(m, g);
+    }
     m = warp_max(m);
     if (threadIdx.x % 32 == 0) atomicMax(largest, __float_as_uint(m));   // of floats above 0 the order of their bits
 }
@@ -1305,7 +1309,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
         e = cudaMemsetAsync(largest, 0, 4, c.stream);
         const long long n = (long long)groups * rows, blocks = (n + 1023) / 1024;
         if (e == cudaSuccess)
-            e = launch_next(largest_kernel, dim3((unsigned int)(blocks < 2 * c.sms ? blocks : 2 * c.sms)), 256, 0, c.stream, grad_loss, n, largest);
+            e = launch_next(largest_kernel, dim3((unsigned int)(blocks < 2 * c.sms ? blocks : 2 * c.sms)), 256, 0, c.stream, grad_loss, stats, 2 + c.k, n, largest);
     }
     if (e != cudaSuccess) return cuda_fail(e, "towers: layout launch");
 
