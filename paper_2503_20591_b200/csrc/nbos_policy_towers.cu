@@ -2,7 +2,7 @@
 //
 // With a the requests' vectors, b the hosts', c = log2(e) / T, and x_rh = a_r . b_h where the request fits the host, else -inf:
 //   forward   m_r = max_h x_rh,  S_r = sum_h 2^((x_rh - m_r) c)      a matrix product whose tiles never leave the chip
-//             y_rj = x at the row's hosts,  loss_r = T^2 sum_j q_j (ln q_j - (y_rj - m_r) / T + ln S_r)
+//             y_rj = x at the row's hosts, taken from the same tiles,  loss_r = T^2 sum_j q_j (ln q_j - (y_rj - m_r) / T + ln S_r)
 //   backward  G_rh = g_r T (p_rh - q_rh), p_rh = 2^((x_rh - m_r) c) / S_r    the product once more
 //             da = G b,  db = G^T a                                           two more products
 // G exists in pieces of rows, in 16 bits (the operands' type): at most kPieceBytes of it.
@@ -63,9 +63,13 @@ struct TowerArgs {
     float c;                          // log2(e) / T
     float2 *partial;                  // STATS: [groups][rows][slots] (m, S) of parts of a row
     int slots;
+    const unsigned int *keys;         // STATS: [groups][rows][k], each 32 rows' entries in the order of their tiles (NULL: at most kFewEntries a row)
+    const int *key_starts;            // of each 32 rows' list, five
+    float *entries;                   // STATS: x at a row's entries, rows entry_stride apart
+    int entry_stride;
     const float *stats;               // GRAD: [groups][rows][stats_stride]: m, S, ...
     int stats_stride;
-    const int32_t *ids;               // GRAD: the rows' entries, k of them (NULL: too many)
+    const int32_t *ids;               // the rows' entries, k of them (GRAD: NULL: too many)
     const float *teacher;
     long long teacher_stride;
     int k;
@@ -312,6 +316,99 @@ __device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bo
     }
 }
 
+// STATS: a row's entries are picked from the tiles as these pass, so that their x are the very values that m and S are made of. (Products of
+// their own, summed in another order, are off by some 1e-5: below T of that size p was 0 or infinite at a row's best host.) A warp sees
+// 32 rows, and one of a tile's four quarters, in ascending tiles.
+constexpr unsigned int kNoEntry = 0xFFFFFFFFu;
+// Up to kFewEntries a row: a lane has its row's own, in order, as host << 8 | place in the row's list; at[0] is the next one.
+struct RowEntries {
+    unsigned int at[kFewEntries];
+    float *x;
+    __device__ __forceinline__ void start(const TowerArgs &a, long long row, bool inside, int quarter, int tile)
+    {
+        x = a.entries + row * a.entry_stride;
+#pragma unroll
+        for (int j = 0; j < kFewEntries; ++j) {
+            const int id = inside && j < a.k ? a.ids[row * a.k + j] : -1;
+            at[j] = id >= tile * kTileN && id < a.hosts && id / 64 % 4 == quarter ? (unsigned int)id << 8 | (unsigned int)j : kNoEntry;
+        }
+        auto order = [&](int i, int j) {
+            const unsigned int low = min(at[i], at[j]), high = max(at[i], at[j]);
+            at[i] = low, at[j] = high;
+        };
+        order(0, 1), order(2, 3), order(0, 2), order(1, 3), order(1, 2);
+    }
+    // those in the 64 columns from n0 on, whose products lie at `from` in tensor memory: one load a column, whichever rows have an entry there
+    __device__ __forceinline__ void pick(int n0, uint32_t from)
+    {
+        const unsigned int first = (unsigned int)n0 << 8;
+        for (;;) {
+            const unsigned int column = __reduce_min_sync(kFull, at[0] - first) >> 8;
+            if (column >= 64u) break;
+            uint32_t v;
+            tmem_load1(v, from + column);
+            tmem_wait(v);
+            while ((at[0] - first) >> 8 == column) {   // (a host may be listed twice)
+                x[at[0] & 255u] = __uint_as_float(v);
+#pragma unroll
+                for (int j = 0; j + 1 < kFewEntries; ++j) at[j] = at[j + 1];
+                at[kFewEntries - 1] = kNoEntry;
+            }
+            __syncwarp();
+        }
+    }
+};
+// More of them: the 32 rows' entries come sorted by quarter and tile (sort_entries_kernel); a lane has one of the next 32.
+struct SortedEntries {
+    const unsigned int *list;
+    float *x;
+    int at, end, stride;
+    unsigned int key;                 // tile << 19 | column of the quarter << 13 | row << 8 | place in the row's list
+    __device__ __forceinline__ void fetch() { key = at + (int)(threadIdx.x % 32) < end ? list[at + threadIdx.x % 32] : kNoEntry; }
+    __device__ __forceinline__ void start(const TowerArgs &a, int group, int row, int quarter, int tile)
+    {
+        at = end = 0;
+        if (row < a.rows) {
+            const int *const starts = a.key_starts + 5 * ((long long)group * ((a.rows + 31) / 32) + row / 32);
+            list = a.keys + ((long long)group * a.rows + row) * a.k;
+            x = a.entries + ((long long)group * a.rows + row) * a.entry_stride;
+            stride = a.entry_stride;
+            at = starts[quarter], end = starts[quarter + 1];
+            for (int to = end; tile > 0 && at < to;) {   // a pair that starts inside a row
+                const int mid = (at + to) / 2;
+                if (list[mid] >> 19 < (unsigned int)tile)
+                    at = mid + 1;
+                else
+                    to = mid;
+            }
+        }
+        fetch();
+    }
+    __device__ __forceinline__ void pick(int tile, uint32_t from)
+    {
+        for (;;) {
+            const bool mine = key >> 19 == (unsigned int)tile;
+            const unsigned int all = __ballot_sync(kFull, mine);
+            if (all == 0u) break;
+            unsigned int column = mine ? key >> 13 & 63u : 64u;
+            uint32_t got = 0u;
+            for (;;) {
+                const unsigned int least = __reduce_min_sync(kFull, column);
+                if (least == 64u) break;
+                uint32_t v;
+                tmem_load1(v, from + least);
+                tmem_wait(v);
+                const uint32_t there = __shfl_sync(kFull, v, key >> 8 & 31u);
+                if (column == least) got = there, column = 64u;
+            }
+            if (mine) x[(long long)(key >> 8 & 31u) * stride + (key & 255u)] = __uint_as_float(got);
+            at += __popc(all);
+            fetch();
+            if (all != kFull) break;
+        }
+    }
+};
+
 // One launch covers its units with pairs of blocks, each a persistent pair: one thread a block copies operand tiles
 // into a ring of stages, one thread of the pair multiplies them into one of two accumulators in tensor memory, 16 warps a
 // block read the other. No wait is without a limit: when one runs out the block's flag goes up, copies and products stop, the
@@ -451,6 +548,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         int entry_at[kFewEntries];
         T entry[PLANES][kFewEntries];
         int slot = 0;
+        RowEntries own_entries;
+        SortedEntries sorted_entries;
         auto release = [&] {
             fence_before();
             __syncwarp();
@@ -484,6 +583,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (KIND == STATS) {
                         flush();
                         slot = pair - pair_of(t.units, pairs, ((long long)u.g * t.m_tiles + u.m) * t.n_tiles);
+                        if (args.keys)
+                            sorted_entries.start(args, u.g, local - lane, quarter, u.n);
+                        else
+                            own_entries.start(args, (long long)u.g * args.rows + local, local < args.rows, quarter, u.n);
+                        __syncwarp();
                     }
                     some_dead = false;
 #pragma unroll
@@ -523,6 +627,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 fence_after();
                 const uint32_t at = lane_at + buffer * kTileN;
                 const int n0 = u.n * BN + quarter * 64;
+                if constexpr (KIND == STATS) {
+                    if (args.keys)
+                        sorted_entries.pick(u.n, at);
+                    else
+                        own_entries.pick(n0, at);
+                }
                 const uint32_t box = staging + warp * 32 * 128;   // the warp's own, 32 rows
 #pragma unroll 1
                 for (int plane = 0; plane < PLANES; ++plane) {   // GRAD: what is rounded off goes to the second
@@ -728,10 +838,57 @@ __global__ void lay_out_kernel(const T *src, long long stride, long long group_s
     }
 }
 
+// The entries of 32 rows (of one group) in the order of their quarters and tiles: counted, placed. What comes first within a tile differs from
+// run to run; what is done with it does not. Dynamic shared memory: a counter a quarter of a tile.
+__global__ void __launch_bounds__(256) sort_entries_kernel(const int32_t *ids, int rows, int k, int hosts, int tiles, unsigned int *keys, int *starts)
+{
+    extern __shared__ unsigned int counters[];   // [4][tiles]
+    __shared__ unsigned int warps[8];
+    next_may_start();
+    previous_done();
+    const int lists = (rows + 31) / 32, g = (int)(blockIdx.x / lists), row0 = (int)(blockIdx.x % lists) * 32, n = 4 * tiles;
+    const int count = min(32, rows - row0) * k;
+    ids += ((long long)g * rows + row0) * k, keys += ((long long)g * rows + row0) * k, starts += 5ll * blockIdx.x;
+    auto counter = [&](int id) { return counters + id / 64 % 4 * tiles + id / 256; };
+    for (int i = threadIdx.x; i < n; i += 256) counters[i] = 0u;
+    __syncthreads();
+    for (int e = threadIdx.x; e < count; e += 256) {
+        const int id = ids[e];
+        if (id >= 0 && id < hosts) atomicAdd(counter(id), 1u);
+    }
+    __syncthreads();
+    // how many come before each: a stretch of counters a thread
+    const int stretch = (n + 255) / 256, from = min(n, (int)threadIdx.x * stretch), to = min(n, from + stretch);
+    unsigned int own = 0u;
+    for (int i = from; i < to; ++i) own += counters[i];
+    unsigned int before = own;
+#pragma unroll
+    for (int off = 1; off < 32; off *= 2) {
+        const unsigned int v = __shfl_up_sync(kFull, before, off);
+        if (threadIdx.x % 32 >= off) before += v;
+    }
+    if (threadIdx.x % 32 == 31) warps[threadIdx.x / 32] = before;
+    __syncthreads();
+    before -= own;
+    for (int w = 0; w < (int)threadIdx.x / 32; ++w) before += warps[w];
+    if (threadIdx.x == 255) starts[4] = (int)(before + own);
+    for (int i = from; i < to; ++i) {
+        const unsigned int here = counters[i];
+        counters[i] = before;
+        before += here;
+    }
+    __syncthreads();
+    if (threadIdx.x < 4) starts[threadIdx.x] = (int)counters[threadIdx.x * tiles];
+    __syncthreads();
+    for (int e = threadIdx.x; e < count; e += 256) {
+        const int id = ids[e], row = e / k;
+        if (id >= 0 && id < hosts)
+            keys[atomicAdd(counter(id), 1u)] = (unsigned int)(id / 256) << 19 | (unsigned int)(id % 64) << 13 | (unsigned int)row << 8 | (unsigned int)(e - row * k);
+    }
+}
+
 struct FinishArgs {
-    const void *a, *b;                // vectors, rows on 16-byte boundaries
-    long long a_stride, a_group_stride, b_stride, b_group_stride;
-    int groups, rows, hosts, width, k, slots, pairs, m_tiles, n_tiles;
+    int groups, rows, hosts, k, slots, pairs, m_tiles, n_tiles;
     long long units;
     const int32_t *ids;
     const float *teacher;
@@ -739,6 +896,8 @@ struct FinishArgs {
     const int4 *asks, *room;
     float T, c;
     const float2 *partial;
+    float *entries;                   // x at the entries, rows entry_stride apart
+    int entry_stride;
     float *loss, *stats;
 };
 
@@ -750,54 +909,9 @@ __device__ __forceinline__ int pair_at(const FinishArgs &f, long long unit)
     return (int)(u < r * (q + 1) ? u / (q + 1) : r + (u - r * (q + 1)) / q);
 }
 
-// <a, b[u]> over this lane's 16-byte pieces, all U at once and several pieces of each, so that their loads are under way together
-template <typename T, int U>
-__device__ __forceinline__ void dots(float (&out)[U], const T *a, const T *const (&b)[U], int width, int sub, int lanes)
-{
-    constexpr int AHEAD = U == 1 ? 4 : 2;
-    float s[U][2] = {};
-    auto add = [&](const uint4 &p, const uint4 (&w)[U]) {
-        float x[8];
-        unpack16(p, x, T());
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float y[8];
-            unpack16(w[u], y, T());
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) fma2(s[u][0], s[u][1], x[j], x[j + 1], y[j], y[j + 1]);
-        }
-    };
-    const int step = lanes * 8;
-    int i = sub * 8;
-    for (; i + (AHEAD - 1) * step + 8 <= width; i += AHEAD * step) {
-        uint4 p[AHEAD], w[AHEAD][U];
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n) {
-            p[n] = *reinterpret_cast<const uint4 *>(a + i + n * step);
-#pragma unroll
-            for (int u = 0; u < U; ++u) w[n][u] = *reinterpret_cast<const uint4 *>(b[u] + i + n * step);
-        }
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n) add(p[n], w[n]);
-    }
-    for (; i + 8 <= width; i += step) {
-        uint4 w[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = *reinterpret_cast<const uint4 *>(b[u] + i);
-        add(*reinterpret_cast<const uint4 *>(a + i), w);
-    }
-    for (int j = i; j < width && j < i + 8; ++j)
-#pragma unroll
-        for (int u = 0; u < U; ++u) s[u][0] = fmaf(to_float(a[j]), to_float(b[u][j]), s[u][0]);
-#pragma unroll
-    for (int u = 0; u < U; ++u) out[u] = lanes_sum(s[u][0] + s[u][1], lanes);
-}
-
-// TEAM lanes a row: its parts' statistics become one, the logits at its hosts are computed, and the loss. `lanes` of the team
-// share a product, each team takes TEAM / lanes * U of them at a time. (One product after the other, a warp a row:
-// 74 us for 65,536 rows of 256 with three hosts each, this 41 to 49.)
-template <typename T, int TEAM, int U>
-__global__ void __launch_bounds__(256, 4) finish_kernel(const __grid_constant__ FinishArgs f, int lanes)
+// TEAM lanes a row: its parts' statistics become one, and the logits at its hosts the loss.
+template <int TEAM>
+__global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ FinishArgs f)
 {
     next_may_start();
     previous_done();
@@ -825,39 +939,22 @@ __global__ void __launch_bounds__(256, 4) finish_kernel(const __grid_constant__ 
     const float top = team_max(m), base = top == neg_inf() ? 0.0f : top;
     s = lanes_sum(s * exp2_fast((m - base) * f.c), TEAM);
 
-    const int at_once = TEAM / lanes, sub = lane % lanes;
-    const T *a = static_cast<const T *>(f.a) + g * f.a_group_stride + row * f.a_stride;
-    const T *b = static_cast<const T *>(f.b) + g * f.b_group_stride;
     // over this lane's entries: largest teacher logit, sum of w = 2^((t - tm) c), sum of w ((t - tm) - (x - m))
     float tm = neg_inf(), ts = 0.0f, tx = 0.0f;
-    for (int j0 = 0; j0 < f.k; j0 += U * at_once) {
-        const T *of[U];
-        float t[U], x[U];
-        bool there[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * at_once + lane / lanes;
-            const int id = j < f.k ? f.ids[at * f.k + j] : -1;
-            t[u] = j < f.k && f.teacher ? f.teacher[at * f.teacher_stride + j] : 0.0f;
-            there[u] = id >= 0 && id < f.hosts;
-            of[u] = there[u] ? b + id * f.b_stride : b;   // b: a row that is there, for a product that is not used
-            // (whether the request fits decides over the product, not over its loads)
-            if (there[u] && f.asks) there[u] = !never_fits(ask) && fits(ask, f.room[(long long)g * f.hosts + id]);
-        }
-        dots<T, U>(x, a, of, f.width, sub, lanes);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * at_once + lane / lanes;
-            if (sub != 0 || j >= f.k || !inside) continue;
-            x[u] = there[u] ? x[u] : neg_inf();
-            if (f.stats) f.stats[at * (2 + f.k) + 2 + j] = x[u];
-            if (x[u] != neg_inf() && t[u] > neg_inf()) {   // a NaN logit counts, and spoils its row
-                const float to = fmaxf(tm, t[u]), keep = exp2_fast((tm - to) * f.c), w = exp2_fast((t[u] - to) * f.c);
-                tx = ts > 0.0f ? keep * (tx + ts * (tm - to)) : 0.0f;
-                tx += w * ((t[u] - to) - (x[u] - base));
-                ts = ts * keep + w;
-                tm = to;
-            }
+    for (int j = lane; j < f.k && inside; j += TEAM) {
+        const int id = f.ids[at * f.k + j];
+        const float t = f.teacher ? f.teacher[at * f.teacher_stride + j] : 0.0f;
+        float *const to = f.entries + at * f.entry_stride + j;
+        bool there = id >= 0 && id < f.hosts;
+        if (there && f.asks) there = !never_fits(ask) && fits(ask, f.room[(long long)g * f.hosts + id]);
+        const float x = there ? *to : neg_inf();
+        if (f.stats && !there) *to = x;
+        if (x != neg_inf() && t > neg_inf()) {   // a NaN logit counts, and spoils its row
+            const float top_now = fmaxf(tm, t), keep = exp2_fast((tm - top_now) * f.c), w = exp2_fast((t - top_now) * f.c);
+            tx = ts > 0.0f ? keep * (tx + ts * (tm - top_now)) : 0.0f;
+            tx += w * ((t - top_now) - (x - base));
+            ts = ts * keep + w;
+            tm = top_now;
         }
     }
     const float teacher_top = team_max(tm), keep = ts > 0.0f ? exp2_fast((tm - teacher_top) * f.c) : 0.0f;
@@ -1195,7 +1292,12 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     const int pairs = args.t.units < c.sms / 2 ? (int)args.t.units : c.sms / 2;
     // a row's tiles lie with at most this many pairs, each of which leaves kParts parts
     args.slots = kParts * ((int)((args.t.n_tiles - 1) / (args.t.units / pairs)) + 2);
-    const size_t o_partial = ws.add(sizeof(float2) * args.slots * in->n_groups * in->rows);
+    const long long rows = in->n_groups * in->rows;
+    const size_t o_partial = ws.add(sizeof(float2) * args.slots * rows);
+    const bool few = c.k <= kFewEntries;
+    const long long lists = (long long)in->n_groups * ((in->rows + 31) / 32);
+    const size_t o_keys = ws.add(few ? 0 : sizeof(unsigned int) * c.k * rows), o_starts = ws.add(few ? 0 : sizeof(int) * 5 * lists);
+    const size_t o_entries = ws.add(out_stats ? 0 : sizeof(float) * c.k * rows);
     int rc = ws.allocate(c.device, c.stream);
     if (rc) return rc;
     cudaError_t e = lay_out<T>(ws, a, c.sms, c.stream);
@@ -1208,36 +1310,29 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     args.asks = reinterpret_cast<const int4 *>(in->asks), args.room = reinterpret_cast<const int4 *>(in->room);
     args.c = kLog2e / c.T;
     args.partial = ws.at<float2>(o_partial);
+    args.ids = c.ids, args.k = c.k;
+    args.entries = out_stats ? out_stats + 2 : ws.at<float>(o_entries), args.entry_stride = out_stats ? 2 + c.k : c.k;
+    if (!few) {
+        args.keys = ws.at<unsigned int>(o_keys), args.key_starts = ws.at<int>(o_starts);
+        const int shared = 4 * args.t.n_tiles * (int)sizeof(unsigned int);
+        e = allow_shared(sort_entries_kernel, shared);
+        if (e == cudaSuccess)
+            e = launch_next(sort_entries_kernel, dim3((unsigned int)lists), 256, shared, c.stream, c.ids, (int)in->rows, (int)c.k, (int)in->n_hosts,
+                            args.t.n_tiles, ws.at<unsigned int>(o_keys), ws.at<int>(o_starts));
+        if (e != cudaSuccess) return cuda_fail(e, "towers: entries launch");
+    }
     e = in->asks ? launch_tower<STATS, kTileN, true, 1, T>(map_a, map_b, map_a, args, pairs, c.stream)
                  : launch_tower<STATS, kTileN, false, 1, T>(map_a, map_b, map_a, args, pairs, c.stream);
     if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
     FinishArgs f = {};
-    f.a = a.table.data, f.b = b.table.data, f.a_stride = a.table.stride, f.a_group_stride = a.table.group_stride;
-    f.b_stride = b.table.stride, f.b_group_stride = b.table.group_stride;
-    f.groups = in->n_groups, f.rows = (int)in->rows, f.hosts = in->n_hosts, f.width = in->width, f.k = c.k, f.slots = args.slots, f.pairs = pairs;
+    f.groups = in->n_groups, f.rows = (int)in->rows, f.hosts = in->n_hosts, f.k = c.k, f.slots = args.slots, f.pairs = pairs;
     f.m_tiles = args.t.m_tiles, f.n_tiles = args.t.n_tiles, f.units = args.t.units;
     f.ids = c.ids, f.teacher = c.teacher, f.teacher_stride = c.teacher_stride, f.asks = args.asks, f.room = args.room;
     f.T = c.T, f.c = args.c, f.partial = args.partial, f.loss = out_loss, f.stats = out_stats;
-    const long long rows = in->n_groups * in->rows;
-    // eight lanes a row where there is little to do for each; else a warp, its lanes split over the products
-    int lanes = 1;
-    while (lanes < 32 && lanes * 8 < in->width) lanes *= 2;
-    const unsigned int warp_blocks = (unsigned int)((rows + 7) / 8), eighth_blocks = (unsigned int)((rows + 31) / 32);
-    if (c.k > 4) {
-        while (lanes > 8 && 32 / lanes * 4 < c.k) lanes /= 2;
-        e = launch_next(finish_kernel<T, 32, 4>, dim3(warp_blocks), 256, 0, c.stream, f, lanes);
-    } else if (in->width > 512) {
-        if (c.k == 1)
-            e = launch_next(finish_kernel<T, 32, 1>, dim3(warp_blocks), 256, 0, c.stream, f, lanes);
-        else
-            e = launch_next(finish_kernel<T, 32, 4>, dim3(warp_blocks), 256, 0, c.stream, f, lanes);
-    } else {
-        if (lanes > 8) lanes = 8;
-        if (c.k == 1)
-            e = launch_next(finish_kernel<T, 8, 1>, dim3(eighth_blocks), 256, 0, c.stream, f, lanes);
-        else
-            e = launch_next(finish_kernel<T, 8, 4>, dim3(eighth_blocks), 256, 0, c.stream, f, lanes);
-    }
+    f.entries = args.entries, f.entry_stride = args.entry_stride;
+    // eight lanes a row where there is little to do for each; else a warp
+    e = c.k > 8 || args.slots > 32 ? launch_next(finish_kernel<32>, dim3((unsigned int)((rows + 7) / 8)), 256, 0, c.stream, f)
+                                   : launch_next(finish_kernel<8>, dim3((unsigned int)((rows + 31) / 32)), 256, 0, c.stream, f);
     return e == cudaSuccess ? NBOS_OK : cuda_fail(e, "towers: loss launch");
 }
 

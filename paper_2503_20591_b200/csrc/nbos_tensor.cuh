@@ -136,6 +136,13 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&v)[32])
                  : "memory");
 }
 
+// one column of this warp's 32 lanes
+__device__ __forceinline__ void tmem_load1(uint32_t &v, uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_wait(uint32_t &v) { asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v) : : "memory"); }
+
 // 32 neighbouring columns of 16 lanes: thread t has v[4 j + 2 r + e] = lane t / 4 + 8 r, column 8 j + 2 (t % 4) + e
 __device__ __forceinline__ void tmem_load16(uint32_t (&v)[16], uint32_t at)
 {
