@@ -530,9 +530,12 @@ int nbos_policy_sample(const nbos_logits *logits, const float *uniforms, const f
  * without a counting entry, have loss and gradient 0. (A vector that is not finite may make the other tower's gradient NaN,
  * also where none of its scores counts: 0 times it is not 0.)
  *     grad_requests = G hosts, grad_hosts = G^T requests, G = T * (p - q) * grad_scale * grad_loss[r]
- * Products are of 16-bit values with 32-bit sums, statistics are in 32 bits. G is rounded to the vectors' type (after a
- * factor that brings the largest finite |grad_loss| of a row that counts to just below a power of two, 2^15 in 16-bit floats) before it is multiplied - up to 64 rows
- * a group as two values, the second what the first's rounding took off -, a gradient once more at the end.
+ * Products are of 16-bit values with 32-bit sums, statistics are in 32 bits. Before it is multiplied, G gets a factor that brings the
+ * largest finite |grad_loss| of a row that counts to just below a power of two (2^15 in 16-bit floats), and each entry is held as two
+ * values of the vectors' type, the second what the first's rounding took off; a gradient is rounded once at the end. In 16-bit floats
+ * a row whose grad_loss is 2^-n of the largest keeps its p down to 2^(n - 29) in full and to 2^(n - 39) in part. With gradient_values = 1 an
+ * entry is one value: the backward call is 1.8 times as fast where products bound it, and its gradients are off as G's rounding makes
+ * them, by up to 2^-8 (bf16) or 2^-11 (f16) of each term's size, which is much where a row's terms cancel (vectors with a large part in common).
  *   towers          vectors DEVICE, NBOS_BF16 or NBOS_F16, of any alignment and row stride >= width; rows on 16-byte boundaries (address,
  *                   strides) are read as they lie, others are copied first. A group stride may be 0 (one table for all groups).
  *   hosts, teacher_logits, teacher_stride, k, temperature, grad_loss, grad_scale   as for nbos_policy_distill; hosts
@@ -557,6 +560,7 @@ typedef struct nbos_towers {
     int32_t dtype;                /* NBOS_BF16 | NBOS_F16                       */
     const int32_t *asks;          /* DEVICE [n_groups * rows * 4] or NULL, 16-byte aligned    */
     const int32_t *room;          /* DEVICE [n_groups * n_hosts * 4] or NULL, 16-byte aligned */
+    int32_t gradient_values;      /* backward: 16-bit values that hold an entry of G: 2, or 1; 0: 2 */
 } nbos_towers;
 
 int nbos_policy_towers(const nbos_towers *towers, const int32_t *hosts, const float *teacher_logits,

@@ -119,7 +119,7 @@ class nbos_towers(ctypes.Structure):
         ("request_stride", ctypes.c_int64), ("request_group_stride", ctypes.c_int64),
         ("host_stride", ctypes.c_int64), ("host_group_stride", ctypes.c_int64),
         ("n_groups", ctypes.c_int32), ("n_hosts", ctypes.c_int32), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32),
-        ("asks", ctypes.c_void_p), ("room", ctypes.c_void_p),
+        ("asks", ctypes.c_void_p), ("room", ctypes.c_void_p), ("gradient_values", ctypes.c_int32),
     ]
 
 
@@ -691,7 +691,7 @@ def nbos_policy_sample(logits, uniforms, out_hosts, out_found=None, temperature=
 
 
 # ---- two towers: distillation without the table of logits --------------------------------
-_TOWERS, _BLOCK = struct.Struct("=2Q5q4i2Q"), struct.Struct("=5Q5q4i2f")   # nbos_towers, nbos_block: packed in a third of the time
+_TOWERS, _BLOCK = struct.Struct("=2Q5q4i2Qi4x"), struct.Struct("=5Q5q4i2f")   # nbos_towers, nbos_block: packed in a third of the time
 _dtype_of = attrgetter("dtype")
 _TOWER_DTYPES = {torch.bfloat16: NBOS_BF16, torch.float16: NBOS_F16}
 
@@ -712,7 +712,7 @@ def _vectors(t, what: str):
     return t.shape[0], rows, width, t.stride(1), t.stride(0)
 
 
-def _towers(requests, host_vectors, hosts, asks, room):
+def _towers(requests, host_vectors, hosts, asks, room, gradient_values=2):
     """(nbos_towers as bytes, groups, rows over all of them, address of hosts, k)"""
     n, rows, width, rstride, rgroup = _vectors(requests, "requests")
     m, n_hosts, hwidth, hstride, hgroup = _vectors(host_vectors, "host_vectors")
@@ -726,7 +726,7 @@ def _towers(requests, host_vectors, hosts, asks, room):
         raise ValueError("asks and room come together")
     desc = _TOWERS.pack(requests.data_ptr(), host_vectors.data_ptr(), rows, rstride, rgroup, hstride, hgroup, n, n_hosts, width,
                         _TOWER_DTYPES[requests.dtype], _dense(asks, "asks", torch.int32, 4 * n * rows, device),
-                        _dense(room, "room", torch.int32, 4 * n * n_hosts, device))
+                        _dense(room, "room", torch.int32, 4 * n * n_hosts, device), gradient_values)
     return desc, n, n * rows, ids, k
 
 
@@ -756,10 +756,12 @@ def nbos_policy_towers(requests, host_vectors, hosts, teacher_logits, out_loss, 
 
 
 def nbos_policy_towers_backward(requests, host_vectors, hosts, teacher_logits, stats, out_grad_requests=None, out_grad_hosts=None,
-                                grad_loss=None, grad_scale=1.0, temperature=1.0, asks=None, room=None, stream=None) -> None:
+                                grad_loss=None, grad_scale=1.0, temperature=1.0, asks=None, room=None, stream=None,
+                                gradient_values=2) -> None:
     """The gradients of nbos_policy_towers from the statistics it saved (out_stats): out_grad_requests like requests,
-    out_grad_hosts like host_vectors, either may be None; grad_loss [N, B] float32 or None."""
-    desc, groups, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room)
+    out_grad_hosts like host_vectors, either may be None; grad_loss [N, B] float32 or None. gradient_values = 1: the gradient of the scores
+    is rounded to 16 bits on the way, for up to 1.8 times the speed."""
+    desc, groups, rows, ids, k = _towers(requests, host_vectors, hosts, asks, room, gradient_values)
     device, f32 = requests.device, torch.float32
     teacher, tstride = _teacher(teacher_logits, hosts, device, rows, k)
     args = (desc, ids, teacher, tstride, k, temperature, _dense(stats, "stats", f32, (2 + k) * rows, device),

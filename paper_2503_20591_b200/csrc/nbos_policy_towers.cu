@@ -5,7 +5,7 @@
 //             y_rj = x at the row's hosts, taken from the same tiles,  loss_r = T^2 sum_j q_j (ln q_j - (y_rj - m_r) / T + ln S_r)
 //   backward  G_rh = g_r T (p_rh - q_rh), p_rh = 2^((x_rh - m_r) c) / S_r    the product once more
 //             da = G b,  db = G^T a                                           two more products
-// G exists in pieces of rows, in 16 bits (the operands' type): at most kPieceBytes of it.
+// G exists in pieces (groups, or runs of a group's longer side), its entries as two values of the operands' type: about kPieceBytes of it.
 #include <math.h>
 
 #include <atomic>
@@ -26,10 +26,9 @@ constexpr int kParts = 4;             // a tile's columns are read in this many 
 constexpr int kEpilogue = 128 * kParts;
 constexpr int kThreads = kEpilogue + 64;   // and a warp that copies, a warp that multiplies
 constexpr int kTmemColumns = 512;     // two tiles of 32-bit products
-constexpr int kFewRows = 64;          // up to as many rows a group, G is held as two 16-bit values, one after the other (see backward)
 constexpr int kBand = 16;             // tiles of hosts that G's rows go through together
 constexpr int kFewEntries = 4;        // a row's entries that are put into G on its way out; more of them by a kernel of their own
-constexpr size_t kPieceBytes = 512u << 20;   // 65,536 x 4,096 at width 256, gradients: 48 MB 950 us, 128 MB 650, 256 MB 586, 512 MB 567: launches fill the GPU
+constexpr size_t kPieceBytes = 512u << 20;   // 65,536 x 4,096 at width 256, gradients: 48 MB 950 us, 128 MB 650, 256 MB 586, 512 MB 567 (one value an entry): launches fill the GPU
 
 enum Kind { STATS, GRAD, GRAD_REQUESTS, GRAD_HOSTS };
 
@@ -633,89 +632,113 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     else
                         own_entries.pick(n0, at);
                 }
-                const uint32_t box = staging + warp * 32 * 128;   // the warp's own, 32 rows
+                if constexpr (KIND == STATS && !MASK) {
+                    uint32_t v[2][32];
+                    tmem_load32(v[0], at), tmem_load32(v[1], at + 32);
+                    tmem_wait(v[0]);
+                    tmem_wait(v[1]);
+                    release();
+                    cut64(v[0], v[1], args.col_end - n0);
+                    add64(run_m[0], run_s[0], v[0], v[1], args.c);
+                } else {
+                    // 32 columns at a time. G: with two values, a box of each, of 32 rows x 32 columns; with one, a box of 64 columns
+                    const uint32_t box = staging + warp * 32 * 128;   // the warp's own
+                    constexpr int kLine = PLANES == 2 ? 64 : 128;
+                    // where 16-byte piece j of a line lies: as the tensor copies swizzle lines of that length
+                    auto piece_at = [&](int line, int j) { return box + line * kLine + ((PLANES == 2 ? j ^ (line / 2 & 3) : j ^ (line & 7)) << 4); };
 #pragma unroll 1
-                for (int plane = 0; plane < PLANES; ++plane) {   // GRAD: what is rounded off goes to the second
-                    if (KIND == GRAD) {
-                        if (lane == 0) stores_read_wait<0>();         // what was in it before has left
-                        __syncwarp();
-                    }
-                    // p f of two columns in one word
-                    auto word = [&](uint32_t x0, uint32_t x1, float from, float less, float by, bool none) {
-                        float e0, e1;
-                        apart2(e0, e1, x0, x1, from, args.c, less);
-                        e0 = exp2_fast(e0), e1 = exp2_fast(e1);
-                        mul2(e0, e1, by, by);
-                        uint32_t w = pack2(e0, e1, T());
-                        if (PLANES == 2 && plane == 1) {
-                            const float2 first = unpack2(w, T());
-                            w = pack2(e0 - first.x, e1 - first.y, T());
+                    for (int sub = 0; sub < 2; ++sub) {
+                        const bool first = PLANES == 2 || sub == 0, last = PLANES == 2 || sub == 1;   // of a box
+                        if (KIND == GRAD && first) {
+                            if (lane == 0) stores_read_wait<0>();         // what was in it before has left
+                            __syncwarp();
                         }
-                        return some_dead && none ? 0u : w;
-                    };
-                    if constexpr (MASK) {
-#pragma unroll 1
-                        for (int sub = 0; sub < 2; ++sub) {
+                        // p f of two columns in one word, and (PLANES == 2) what was rounded off in another
+                        auto words = [&](uint32_t (&w)[PLANES], uint32_t x0, uint32_t x1, float from, float less, float by, bool none) {
+                            float e0, e1;
+                            apart2(e0, e1, x0, x1, from, args.c, less);
+                            e0 = exp2_fast(e0), e1 = exp2_fast(e1);
+                            mul2(e0, e1, by, by);
+                            w[0] = pack2(e0, e1, T());
+                            if (PLANES == 2) {
+                                const float2 rounded = unpack2(w[0], T());
+                                w[PLANES - 1] = pack2(e0 - rounded.x, e1 - rounded.y, T());
+                            }
+                            if (some_dead && none) {
+#pragma unroll
+                                for (int i = 0; i < PLANES; ++i) w[i] = 0u;
+                            }
+                        };
+                        if constexpr (MASK) {
                             uint32_t v[2][16];
                             tmem_load16(v[0], at + 32 * sub), tmem_load16(v[1], at + 32 * sub + (16u << 16));
                             tmem_wait(v[0]);
                             tmem_wait(v[1]);
-                            if (sub == 1 && plane == PLANES - 1) release();
+                            if (sub == 1) release();
                             mask_rows(v, columns + 32 * sub, ask);
                             if constexpr (KIND == STATS) {
 #pragma unroll
                                 for (int i = 0; i < ROWS; ++i) add8(run_m[i], run_s[i], v, i, args.c);
-                            } else {   // 16-byte piece 4 sub + j of a line, four lanes a word each
+                            } else {   // four lanes a word of a piece each
 #pragma unroll
                                 for (int i = 0; i < ROWS; ++i)
 #pragma unroll
                                     for (int j = 0; j < 4; ++j) {
-                                        const int line = row_at(i) % 32, x = 4 * j + 2 * (i % 2);
-                                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(box + line * 128 + (((4 * sub + j) ^ (line & 7)) << 4) + lane % 4 * 4),
-                                                     "r"(word(v[i / 2][x], v[i / 2][x + 1], run_m[i], minus[i], factor[i], dead[i]))
-                                                     : "memory");
+                                        const int x = 4 * j + 2 * (i % 2);
+                                        uint32_t w[PLANES];
+                                        words(w, v[i / 2][x], v[i / 2][x + 1], run_m[i], minus[i], factor[i], dead[i]);
+                                        const uint32_t to = piece_at(row_at(i) % 32, PLANES == 2 ? j : 4 * sub + j) + lane % 4 * 4;
+#pragma unroll
+                                        for (int q = 0; q < PLANES; ++q) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + q * 2048), "r"(w[q]) : "memory");
                                     }
                             }
-                        }
-                    } else {
-                        uint32_t v[2][32];
-                        tmem_load32(v[0], at), tmem_load32(v[1], at + 32);
-                        tmem_wait(v[0]);
-                        tmem_wait(v[1]);
-                        if (plane == PLANES - 1) release();
-                        cut64(v[0], v[1], args.col_end - n0);
-                        if constexpr (KIND == STATS) {
-                            add64(run_m[0], run_s[0], v[0], v[1], args.c);
-                        } else {
+                        } else if constexpr (KIND == GRAD) {
+                            uint32_t v[32];
+                            tmem_load32(v, at + 32 * sub);
+                            tmem_wait(v);
+                            if (sub == 1) release();
+                            const int left = args.col_end - n0 - 32 * sub;
+                            if (left < 32) {
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const uint32_t(&x)[32] = v[j / 4];
-                                const int k = 8 * (j % 4);
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((j ^ (lane & 7)) << 4)),
-                                             "r"(word(x[k], x[k + 1], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 2], x[k + 3], run_m[0], minus[0], factor[0], dead[0])), "r"(word(x[k + 4], x[k + 5], run_m[0], minus[0], factor[0], dead[0])),
-                                             "r"(word(x[k + 6], x[k + 7], run_m[0], minus[0], factor[0], dead[0]))
-                                             : "memory");
+                                for (int i = 0; i < 32; ++i) v[i] = i < left ? v[i] : 0xFF800000u;
                             }
-                        }
-                    }
-                    if (KIND == GRAD) {
-                        if (args.ids) {
-                            __syncwarp();
 #pragma unroll
-                            for (int j = 0; j < kFewEntries; ++j) {
-                                const int col = entry_at[j] - n0;
-                                if ((unsigned int)col < 64u)
-                                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(box + entry_row * 128 + (((col / 8) ^ (entry_row & 7)) << 4) + col % 8 * 2),
-                                                 "h"(*reinterpret_cast<const unsigned short *>(&entry[PLANES == 2 ? plane : 0][j]))
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t w[4][PLANES];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) words(w[i], v[8 * j + 2 * i], v[8 * j + 2 * i + 1], run_m[0], minus[0], factor[0], dead[0]);
+                                const uint32_t to = piece_at(lane, PLANES == 2 ? j : 4 * sub + j);
+#pragma unroll
+                                for (int q = 0; q < PLANES; ++q)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + q * 2048), "r"(w[0][q]), "r"(w[1][q]), "r"(w[2][q]), "r"(w[3][q])
                                                  : "memory");
                             }
                         }
-                        async_proxy_fence();
-                        __syncwarp();
-                        if (lane == 0) {
-                            const int y = u.m * kTileM + (int)rank * 128 + warp % 4 * 32;
-                            if (n0 < args.col_end && y < args.m_rows) store_box(&map_g, n0, y, u.g + plane * t.groups, box);
-                            stores_commit();
+                        if (KIND == GRAD && last) {
+                            const int x0 = n0 + (PLANES == 2 ? 32 * sub : 0);
+                            if (args.ids) {
+                                __syncwarp();
+#pragma unroll
+                                for (int j = 0; j < kFewEntries; ++j) {
+                                    const int col = entry_at[j] - x0;
+                                    if ((unsigned int)col < kLine / 2u) {
+                                        const uint32_t to = piece_at(entry_row, col / 8) + col % 8 * 2;
+#pragma unroll
+                                        for (int q = 0; q < PLANES; ++q)
+                                            asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + q * 2048), "h"(*reinterpret_cast<const unsigned short *>(&entry[q][j])) : "memory");
+                                    }
+                                }
+                            }
+                            async_proxy_fence();
+                            __syncwarp();
+                            if (lane == 0) {
+                                const int y = u.m * kTileM + (int)rank * 128 + warp % 4 * 32;
+                                if (x0 < args.col_end && y < args.m_rows) {
+#pragma unroll
+                                    for (int q = 0; q < PLANES; ++q) store_box(&map_g, x0, y, u.g + q * t.groups, box + q * 2048);
+                                }
+                                stores_commit();
+                            }
                         }
                     }
                 }
@@ -1101,18 +1124,18 @@ struct Table {
     long long stride, group_stride;   // elements; group_stride 0: one slice for all groups
     int groups, rows, width;
 };
-// boxes of 64 columns (128 bytes, swizzled) x box_rows rows
-int make_map(CUtensorMap *map, const Table &t, int box_rows, int dtype)
+// boxes of 64 columns (128 bytes), or 32, swizzled, x box_rows rows
+int make_map(CUtensorMap *map, const Table &t, int box_rows, int dtype, int box_columns = 64)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return fail(NBOS_ERR_CUDA, "cuTensorMapEncodeTiled is not there");
     const bool shared = t.group_stride == 0;
     const cuuint64_t dims[3] = {(cuuint64_t)t.width, (cuuint64_t)t.rows, shared ? 1u : (cuuint64_t)t.groups};
     const cuuint64_t strides[2] = {(cuuint64_t)t.stride * 2, shared ? (cuuint64_t)t.stride * 2 : (cuuint64_t)t.group_stride * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, steps[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)box_columns, (cuuint32_t)box_rows, 1}, steps[3] = {1, 1, 1};
     const CUresult r = encode(map, dtype == NBOS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
                               const_cast<void *>(t.data), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                              box_columns == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(NBOS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
     return NBOS_OK;
 }
@@ -1227,6 +1250,7 @@ int check(const nbos_towers *in, const int32_t *ids, const float *teacher, int64
         return fail(NBOS_ERR_INVALID_ARG, "group strides must be in 0..2^38");
     if (in->rows > 0 && (!in->requests || !in->hosts)) return fail(NBOS_ERR_INVALID_ARG, "towers->requests / hosts is NULL");
     if (!aligned_to(in->requests, 2) || !aligned_to(in->hosts, 2)) return fail(NBOS_ERR_INVALID_ARG, "vectors are not aligned to their element type");
+    if (in->gradient_values < 0 || in->gradient_values > 2) return fail(NBOS_ERR_INVALID_ARG, "gradient_values must be 1 or 2, or 0 for 2 (got %d)", in->gradient_values);
     if (!in->asks != !in->room) return fail(NBOS_ERR_INVALID_ARG, "asks and room come together");
     if (!aligned_to(in->asks, 16) || !aligned_to(in->room, 16)) return fail(NBOS_ERR_INVALID_ARG, "asks / room must be 16-byte aligned");
     const int rc = check_k(k);
@@ -1351,10 +1375,12 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
     const int groups = in->n_groups, rows = (int)in->rows, hosts = in->n_hosts, width = in->width, pairs = c.sms / 2;
     // Pieces of G: whole groups while they fit; of a group that does not, runs along its longer side, so that the gradient
     // that has to be added up over the pieces is the smaller one.
-    // A gradient of few rows is a sum of few large terms, whose roundings do not average out: there G is held as two 16-bit values,
-    // the second what rounding took off the first, and the contractions go over both. (Errors against 64 bits, relative to the
-    // plain form's: one value 2.5 at one row, 1.5 to 1.6 at two and three, at most 1.45 from 64 on; two values 1.0 throughout.)
-    const int planes = rows <= kFewRows ? 2 : 1;
+    // An entry of G is held as two 16-bit values, the second what rounding took off the first, and the contractions go over both. With one,
+    // gradients are a sum of rounded terms: their errors against 64 bits are 1.4 times the plain form's, 2.5 where a group has one row, and far
+    // more where the terms cancel. A row's p - q add up to 0, so what all hosts' vectors have in common does: where that is as large as what
+    // tells them apart the error is 1.7 times the plain form's, at ten times as large 9.4 (2,048 x 4,096 of width 128; two values: 1.0 in
+    // all of these). The second value doubles two of four products: 65,536 x 4,096 of width 256, both calls 528 us with one, 881 with two.
+    const int planes = in->gradient_values == 1 ? 1 : 2;
     const size_t group_bytes = (size_t)rows * ((hosts + 63) & ~63) * 2 * planes;
     int piece_groups = 1, piece_rows = rows, piece_hosts = hosts;
     auto even = [&](int n, int tile) {   // whole tiles, pieces of much the same size
@@ -1422,7 +1448,7 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
                 const int rn = rows - r0 < piece_rows ? rows - r0 : piece_rows, hn = hosts - h0 < piece_hosts ? hosts - h0 : piece_hosts;
                 const Table piece{g, g_stride, (long long)piece_rows * g_stride, planes * gn, rn, hn};
                 CUtensorMap g_out, g_rows, g_cols;   // written, and read along rows and across them
-                if ((rc = make_map(&g_out, piece, 32, in->dtype)) || (rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype)))
+                if ((rc = make_map(&g_out, piece, 32, in->dtype, planes == 2 ? 32 : 64)) || (rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype)))
                     return rc;
 
                 TowerArgs p = {};
