@@ -164,7 +164,11 @@ struct Shape {
     static constexpr int kBytes = kStages * kStageBytes + kStaging + kRoom + 256 /* barriers */ + 1024 /* alignment */;
 };
 
-__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_sync(int id, int threads)
+{
+    __syncwarp();   // the barrier counts whole warps
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 
 // d = (a - m) b + c, two at a time. The subtraction comes first: near the row's maximum it is exact or nearly so, and nothing
 // overflows at low temperatures.
@@ -363,7 +367,11 @@ struct SortedEntries {
     float *x;
     int at, end, stride;
     unsigned int key;                 // tile << 19 | column of the quarter << 13 | row << 8 | place in the row's list
-    __device__ __forceinline__ void fetch() { key = at + (int)(threadIdx.x % 32) < end ? list[at + threadIdx.x % 32] : kNoEntry; }
+    __device__ __forceinline__ void fetch()
+    {
+        key = at + (int)(threadIdx.x % 32) < end ? list[at + threadIdx.x % 32] : kNoEntry;
+        __syncwarp();   // what follows reads tensor memory, which the warp does as one
+    }
     __device__ __forceinline__ void start(const TowerArgs &a, int group, int row, int quarter, int tile)
     {
         at = end = 0;
@@ -623,6 +631,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     parity ^= 1;
                 }
                 wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
+                __syncwarp();   // (the loads are the whole warp's)
                 fence_after();
                 const uint32_t at = lane_at + buffer * kTileN;
                 const int n0 = u.n * BN + quarter * 64;
@@ -744,6 +753,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 }
             } else {
                 wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
+                __syncwarp();
                 fence_after();
                 const int n_first = u.n * BN + quarter * (BN / kParts);
 #pragma unroll 1
