@@ -545,8 +545,8 @@ int nbos_policy_sample(const nbos_logits *logits, const float *uniforms, const f
  *                   has no counting entry, and its logits at its hosts, -inf where the entry is none or does not fit)
  *   out_grad_*      DEVICE, the vectors' type, or NULL; groups must not overlap; may not overlap the inputs
  * The kernels wait on copies and products with a limit; nbos_policy_towers_status synchronises `cuda_stream` and returns
- * NBOS_ERR_DEVICE_TIMEOUT, once, if a wait on the current device ran out since it was last asked: outputs since then are undefined
- * (losses are NaN).
+ * NBOS_ERR_DEVICE_TIMEOUT, once, if a wait on the current device ran out since it was last asked. Until it is asked, losses and
+ * gradients are NaN (those of the call whose wait ran out at least where they are missing), statistics undefined.
  */
 #define NBOS_POLICY_MAX_WIDTH 65536
 typedef struct nbos_towers {

@@ -49,6 +49,14 @@ struct nbos_snapshot;
 int nbos_probe_wait_timeout_on_snapshot(struct nbos_snapshot *snap, uint64_t limit_ns, void *cuda_stream,
                                         float *out_ms);
 
+/*
+ * Self-test of the two-tower kernels' bounded waits: the calling thread's next launch of one of them copies nothing, so that its
+ * waits run out, after `limit_ns` (clamped to 1 ms .. 5 s), and its blocks leave by the way that they would leave by if a copy never
+ * came. What the call then gives is what nbos_policy_towers_status tells of. kernel: 0 = the forward call's scores, 1 = the
+ * backward call's, 2 = the requests' gradient, 3 = the hosts'; -1 takes it back.
+ */
+int nbos_probe_towers_stall(int kernel, uint64_t limit_ns);
+
 #ifdef __cplusplus
 }
 #endif

@@ -66,6 +66,7 @@ EXPORTED_SYMBOLS = (
     "nbos_policy_block_norm", "nbos_policy_block_norm_backward", "nbos_policy_clip",
     "nbos_snapshot_status", "nbos_strerror", "nbos_last_error_detail",
     "nbos_probe_int32_issue", "nbos_probe_wait_timeout", "nbos_probe_wait_timeout_on_snapshot",
+    "nbos_probe_towers_stall",
 )
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
@@ -203,6 +204,7 @@ def load_library() -> ctypes.CDLL:
     lib.nbos_probe_wait_timeout.argtypes = [ctypes.c_uint64, vp, P(ctypes.c_int),
                                             P(ctypes.c_float)]
     lib.nbos_probe_wait_timeout_on_snapshot.argtypes = [vp, ctypes.c_uint64, vp, P(ctypes.c_float)]
+    lib.nbos_probe_towers_stall.argtypes = [ctypes.c_int, ctypes.c_uint64]
     for name in EXPORTED_SYMBOLS:
         fn = getattr(lib, name)
         if name not in ("nbos_strerror", "nbos_last_error_detail"):
@@ -957,6 +959,12 @@ def nbos_probe_wait_timeout_on_snapshot(snap: Snapshot, limit_ns: int, stream=No
     _check(load_library().nbos_probe_wait_timeout_on_snapshot(snap.handle, limit_ns, _stream_ptr(stream),
                                                               ctypes.byref(ms)))
     return float(ms.value)
+
+
+def nbos_probe_towers_stall(kernel: int, limit_ns: int) -> None:
+    """Self-test: this thread's next launch of a two-tower kernel (0 forward scores, 1 backward scores, 2 requests' gradient, 3 hosts'
+    gradient; -1 takes it back) copies nothing, so that its waits run out after limit_ns."""
+    _check(load_library().nbos_probe_towers_stall(kernel, limit_ns))
 
 
 def launch_config(lanes_per_request=0, requests_per_lane=0, host_split=0, tile_hosts=0,

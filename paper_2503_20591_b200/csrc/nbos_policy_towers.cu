@@ -11,6 +11,7 @@
 #include <atomic>
 
 #include "nbos_policy.cuh"
+#include "nbos_probe.h"
 #include "nbos_tensor.cuh"
 
 namespace nbos {
@@ -79,6 +80,8 @@ struct TowerArgs {
     long long out_stride, out_group_stride;
     bool out_wide;                    // rows of the result lie on 16-byte boundaries
     int m_rows, out_row0, add;        // m_rows: rows that the launch writes, per group
+    unsigned long long limit_ns;      // of a wait
+    bool stall;                       // self-test: nothing is copied, so that the waits run out
 };
 
 __device__ unsigned int tower_status;   // STATUS_WAIT_TIMEOUT once a wait ran out, until nbos_policy_towers_status is asked
@@ -468,13 +471,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             Schedule<KIND> todo(t, pair, pairs);
             int stage = 0;
             uint32_t phase = 0;
-            bool ok = true;
+            bool ok = !args.stall;
             long long copied = 0;
             while (ok && todo.next(t, u)) {
                 const int az = args.a_z0 + u.g * args.a_z, bz = args.b_z0 + u.g * args.b_z;
                 const int m0 = u.m * kTileM + (int)rank * 128, n0 = u.n * BN + (int)rank * (BN / 2);
                 for (int kb = u.k0; kb < u.k1; ++kb) {
-                    ok = wait_cluster(empty + 8 * stage, phase ^ 1, abort_flag);
+                    ok = wait_cluster(empty + 8 * stage, phase ^ 1, abort_flag, args.limit_ns);
                     if (!ok) break;
                     const uint32_t bar = peer_addr(full + 8 * stage, 0);
                     if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * S::kStageBytes);
@@ -500,7 +503,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             for (int s = 0; ok && s < S::kStages && s < copied; ++s) {
                 if (stage == 0) stage = S::kStages, phase ^= 1;
                 --stage;
-                ok = wait_cluster(empty + 8 * stage, phase, abort_flag);
+                ok = wait_cluster(empty + 8 * stage, phase, abort_flag, args.limit_ns);
             }
         }
         __syncwarp();
@@ -514,12 +517,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             uint32_t phase = 0, buffer_phase = 0;
             bool ok = true;
             while (ok && todo.next(t, u)) {
-                ok = wait_cluster(tmem_empty + 8 * buffer, buffer_phase ^ 1, abort_flag);
+                ok = wait_cluster(tmem_empty + 8 * buffer, buffer_phase ^ 1, abort_flag, args.limit_ns);
                 if (!ok) break;
                 fence_after();
                 const uint32_t d = tmem + buffer * kTileN;
                 for (int kb = u.k0; kb < u.k1; ++kb) {
-                    ok = wait_cluster(full + 8 * stage, phase, abort_flag);
+                    ok = wait_cluster(full + 8 * stage, phase, abort_flag, args.limit_ns);
                     if (!ok) break;
                     fence_after();
                     const uint32_t a = base + stage * S::kStageBytes, b = a + S::kBytesA;
@@ -582,7 +585,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     args.partial[((long long)last_g * args.rows + row) * args.slots + kParts * slot + quarter] = make_float2(run_m[i], run_s[i]);
             }
         };
-        const float undo = KIND == GRAD_REQUESTS || KIND == GRAD_HOSTS ? 1.0f / args.range.factor() : 1.0f;
+        // A gradient that a wait ran out on the way to is NaN: all of it after a launch before this one, the block's tiles after one of its own.
+        float undo = KIND == GRAD_REQUESTS || KIND == GRAD_HOSTS ? (tower_status ? __int_as_float(0x7FC00000) : 1.0f / args.range.factor()) : 1.0f;
         while (todo.next(t, u)) {
             const int local = u.m * kTileM + (int)rank * 128 + row_in;   // row of the launch
             if (KIND == STATS || KIND == GRAD) {
@@ -630,7 +634,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     columns += quarter * (BN / kParts) + 2 * (lane % 4);
                     parity ^= 1;
                 }
-                wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
+                wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag, args.limit_ns);
                 __syncwarp();   // (the loads are the whole warp's)
                 fence_after();
                 const uint32_t at = lane_at + buffer * kTileN;
@@ -752,7 +756,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                 }
             } else {
-                wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag);
+                if (!wait_cluster(tmem_full + 8 * buffer, buffer_phase, abort_flag, args.limit_ns)) undo = __int_as_float(0x7FC00000);
                 __syncwarp();
                 fence_after();
                 const int n_first = u.n * BN + quarter * (BN / kParts);
@@ -1082,7 +1086,7 @@ __global__ void sums_kernel(const float *sums, int splits, int groups, int rows,
     previous_done();
     const unsigned int quads = (width + 3) / 4;
     const long long n = (long long)groups * rows * quads;
-    const float undo = 1.0f / range.factor();
+    const float undo = tower_status ? __int_as_float(0x7FC00000) : 1.0f / range.factor();
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
         const float4 *const from = reinterpret_cast<const float4 *>(sums) + i;
         float4 s = from[0];
@@ -1190,6 +1194,13 @@ private:
     cudaStream_t stream_ = nullptr;
 };
 
+// Self-test: the thread's next launch of that kind copies nothing (nbos_probe_towers_stall).
+struct Stall {
+    int kind;
+    unsigned long long limit_ns;
+};
+thread_local Stall stall_next = {-1, 0};
+
 template <Kind KIND, int BN, bool MASK, int PLANES, typename T>
 cudaError_t launch_tower(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &g, const TowerArgs &args, int pairs, cudaStream_t stream)
 {
@@ -1205,7 +1216,13 @@ cudaError_t launch_tower(const CUtensorMap &a, const CUtensorMap &b, const CUten
         if (e != cudaSuccess) return e;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    return launch_next(kernel, dim3(2 * pairs), kThreads, Shape<KIND, BN>::kBytes, stream, a, b, g, args);
+    TowerArgs p = args;
+    p.limit_ns = kWaitLimitNs;
+    if (stall_next.kind == KIND) {
+        p.limit_ns = stall_next.limit_ns, p.stall = true;
+        stall_next.kind = -1;
+    }
+    return launch_next(kernel, dim3(2 * pairs), kThreads, Shape<KIND, BN>::kBytes, stream, a, b, g, p);
 }
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
@@ -1601,4 +1618,12 @@ extern "C" int nbos_policy_towers_status(void *cuda_stream)
     NBOS_CUDA_TRY(cudaMemcpyToSymbolAsync(tower_status, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, stream));
     NBOS_CUDA_TRY(cudaStreamSynchronize(stream));
     return fail(NBOS_ERR_DEVICE_TIMEOUT, "a two-tower kernel gave up on a bounded wait; its outputs are undefined");
+}
+
+extern "C" int nbos_probe_towers_stall(int kernel, uint64_t limit_ns)
+{
+    if (kernel < -1 || kernel > GRAD_HOSTS) return fail(NBOS_ERR_INVALID_ARG, "kernel must be in -1..%d (got %d)", (int)GRAD_HOSTS, kernel);
+    const uint64_t least = 1000000ull, most = 5000000000ull;
+    stall_next = {kernel, limit_ns < least ? least : limit_ns > most ? most : limit_ns};
+    return NBOS_OK;
 }

@@ -50,23 +50,23 @@ __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 // Bounded, as mbar_wait: false when the wait ran out or another thread of the block gave up.
-static __device__ __noinline__ bool wait_cluster_slow(uint32_t bar, uint32_t parity, volatile unsigned int *abort_flag)
+static __device__ __noinline__ bool wait_cluster_slow(uint32_t bar, uint32_t parity, volatile unsigned int *abort_flag, unsigned long long limit_ns)
 {
     const unsigned long long t0 = global_timer_ns();
     for (;;) {
         for (int i = 0; i < 32; ++i)
             if (try_wait_cluster(bar, parity)) return true;
         if (*abort_flag) return false;
-        if (global_timer_ns() - t0 > kWaitLimitNs) {
+        if (global_timer_ns() - t0 > limit_ns) {
             *abort_flag = 1u;
             return false;
         }
     }
 }
-__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile unsigned int *abort_flag)
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile unsigned int *abort_flag, unsigned long long limit_ns)
 {
     if (try_wait_cluster(bar, parity)) return true;
-    return wait_cluster_slow(bar, parity, abort_flag);
+    return wait_cluster_slow(bar, parity, abort_flag, limit_ns);
 }
 
 // ---- tensor copies ------------------------------------------------------------------------------------------

@@ -152,6 +152,8 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
                 policy.clip_gradients(net.parameters(), max_norm)
             optimizer.step()
             if reported:
+                if not table and binding.nbos_policy_towers_status() != binding.NBOS_OK:
+                    raise RuntimeError("a two-tower kernel gave up on a wait: the last steps' gradients are undefined")
                 history.append((distill.mean().item(), even.mean().item(), agreement(logits.detach(), wanted)))
                 report(f"step {step}: distillation {history[-1][0]:.4f}, balance {history[-1][1]:.2f}, "
                        f"best host among the rule's three {history[-1][2]:.3f}")
