@@ -616,15 +616,15 @@ int nbos_policy_block_norm_backward(const nbos_block *block, const float *stats,
  * The global norm over many tensors (the gradients of a policy), and clipping by it:
  *     norm = (sum over all values of x^2)^(1/2) [NBOS_NORM_2] or max |x| [NBOS_NORM_INF]
  *     out  = x * min(1, max_norm / (norm + 1e-6)), rounded once to the tensor's type
- * Squares are summed in 32 bits within 64 values of a thread, where that neither overflows nor loses small values, and in 64 bits
+ * Squares are summed in 32 bits within 64 bytes of values of a thread (16 or 32), where that neither overflows nor loses small values, and in 64 bits
  * beyond and otherwise; the sums do not change from run to run. (A norm beyond 32 bits is written as infinity, and
- * clips by its true value.) A NaN makes the norm and every output NaN; an infinity makes
- * the norm infinite, finite values 0 and itself NaN (as the formula says). No tensors, or none with values: norm 0.
+ * clips by its true value.) A NaN makes the norm and every output NaN; an infinity makes the norm infinite and, at a finite max_norm,
+ * finite values 0 and itself NaN (as the formula says). No tensors, or none with values: norm 0.
  *   data, numel, dtype  HOST arrays [n_tensors]: DEVICE address (aligned to its type), number of values (0 .. 2^40, contiguous) and
  *                       NBOS_* type of each tensor; types may be mixed
  *   out                 HOST array [n_tensors] of DEVICE addresses, or NULL: the norm alone. An output may be its own input (nothing is
  *                       written then when there is nothing to clip); it must not overlap any tensor otherwise.
- *   max_norm            >= 0; infinity clips nothing
+ *   max_norm            >= 0; infinity clips nothing (a NaN among the values still makes all of them NaN)
  *   out_norm            DEVICE float or NULL
  * The host arrays have been read when the call returns. Asynchronous on `cuda_stream`.
  */

@@ -140,6 +140,7 @@ struct Factor {
 };
 __device__ __forceinline__ Factor clip_factor(double norm, float max_norm)
 {
+    if (isinf(max_norm) && norm == norm) return {1.0f, 1.0f};   // inf / inf otherwise where a value is infinite
     const double f = (double)max_norm / (norm + 1e-6);
     if (f < 0x1p-100) return {(float)(f * 0x1p64), 0x1p-64f};
     return {f < 1.0 ? (float)f : (f != f ? __int_as_float(0x7FC00000) : 1.0f), 1.0f};
