@@ -57,6 +57,13 @@ int nbos_probe_wait_timeout_on_snapshot(struct nbos_snapshot *snap, uint64_t lim
  */
 int nbos_probe_towers_stall(int kernel, uint64_t limit_ns);
 
+/*
+ * The pieces in which nbos_policy_towers_backward holds the gradient of the scores (no device needed): how many there are, the entries
+ * that all of them have together (n_groups * rows * n_hosts, as it must be), and the bytes of the largest.
+ */
+int nbos_probe_towers_pieces(int32_t n_groups, int64_t rows, int32_t n_hosts, int32_t gradient_values, int64_t *out_pieces,
+                             int64_t *out_entries, int64_t *out_largest_bytes);
+
 #ifdef __cplusplus
 }
 #endif

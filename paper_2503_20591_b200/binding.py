@@ -66,7 +66,7 @@ EXPORTED_SYMBOLS = (
     "nbos_policy_block_norm", "nbos_policy_block_norm_backward", "nbos_policy_clip",
     "nbos_snapshot_status", "nbos_strerror", "nbos_last_error_detail",
     "nbos_probe_int32_issue", "nbos_probe_wait_timeout", "nbos_probe_wait_timeout_on_snapshot",
-    "nbos_probe_towers_stall",
+    "nbos_probe_towers_stall", "nbos_probe_towers_pieces",
 )
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
@@ -205,6 +205,7 @@ def load_library() -> ctypes.CDLL:
                                             P(ctypes.c_float)]
     lib.nbos_probe_wait_timeout_on_snapshot.argtypes = [vp, ctypes.c_uint64, vp, P(ctypes.c_float)]
     lib.nbos_probe_towers_stall.argtypes = [ctypes.c_int, ctypes.c_uint64]
+    lib.nbos_probe_towers_pieces.argtypes = [i32, i64, i32, i32, P(i64), P(i64), P(i64)]
     for name in EXPORTED_SYMBOLS:
         fn = getattr(lib, name)
         if name not in ("nbos_strerror", "nbos_last_error_detail"):
@@ -965,6 +966,13 @@ def nbos_probe_towers_stall(kernel: int, limit_ns: int) -> None:
     """Self-test: this thread's next launch of a two-tower kernel (0 forward scores, 1 backward scores, 2 requests' gradient, 3 hosts'
     gradient; -1 takes it back) copies nothing, so that its waits run out after limit_ns."""
     _check(load_library().nbos_probe_towers_stall(kernel, limit_ns))
+
+
+def nbos_probe_towers_pieces(n_groups: int, rows: int, n_hosts: int, gradient_values: int = 2):
+    """(pieces, entries in all of them, bytes of the largest) of the scores' gradient in nbos_policy_towers_backward."""
+    out = [ctypes.c_int64(0) for _ in range(3)]
+    _check(load_library().nbos_probe_towers_pieces(n_groups, rows, n_hosts, gradient_values, *map(ctypes.byref, out)))
+    return tuple(v.value for v in out)
 
 
 def launch_config(lanes_per_request=0, requests_per_lane=0, host_split=0, tile_hosts=0,

@@ -379,7 +379,7 @@ struct SortedEntries {
     {
         at = end = 0;
         if (row < a.rows) {
-            const int *const starts = a.key_starts + 5 * ((long long)group * ((a.rows + 31) / 32) + row / 32);
+            const int *const starts = a.key_starts + 5 * ((long long)group * (((unsigned int)a.rows + 31) / 32) + row / 32);
             list = a.keys + ((long long)group * a.rows + row) * a.k;
             x = a.entries + ((long long)group * a.rows + row) * a.entry_stride;
             stride = a.entry_stride;
@@ -883,7 +883,8 @@ __global__ void __launch_bounds__(256) sort_entries_kernel(const int32_t *ids, i
     __shared__ unsigned int warps[8];
     next_may_start();
     previous_done();
-    const int lists = (rows + 31) / 32, g = (int)(blockIdx.x / lists), row0 = (int)(blockIdx.x % lists) * 32, n = 4 * tiles;
+    const unsigned int lists = ((unsigned int)rows + 31) / 32;
+    const int g = (int)(blockIdx.x / lists), row0 = (int)(blockIdx.x % lists) * 32, n = 4 * tiles;
     const int count = min(32, rows - row0) * k;
     ids += ((long long)g * rows + row0) * k, keys += ((long long)g * rows + row0) * k, starts += 5ll * blockIdx.x;
     auto counter = [&](int id) { return counters + id / 64 % 4 * tiles + id / 256; };
@@ -1394,34 +1395,57 @@ cudaError_t launch_gradient(const CUtensorMap &a, const CUtensorMap &b, const To
     return narrow ? launch_tower<KIND, 128, false, 1, T>(a, b, a, args, p, stream) : launch_tower<KIND, 256, false, 1, T>(a, b, a, args, p, stream);
 }
 
+// Pieces of G: whole groups while they fit; of a group that does not, runs along its longer side, so that the gradient that has to be
+// added up over the pieces is the smaller one.
+struct Pieces {
+    int groups, rows, hosts;          // of a piece
+};
+Pieces plan_pieces(int groups, int rows, int hosts, int planes)
+{
+    const size_t group_bytes = (size_t)rows * ((hosts + 63) & ~63) * 2 * planes;
+    Pieces p = {1, rows, hosts};
+    auto even = [&](int n, int tile) {   // whole tiles, pieces of much the same size
+        const int pieces = (int)((group_bytes + kPieceBytes - 1) / kPieceBytes), size = ceil_div(ceil_div(n, pieces), tile) * tile;
+        return size < n ? size : n;
+    };
+    if (group_bytes <= kPieceBytes) {
+        p.groups = (int)(kPieceBytes / group_bytes);
+        if (p.groups > groups) p.groups = groups;
+    } else if (rows <= hosts) {
+        p.hosts = even(hosts, kTileN);
+    } else {
+        p.rows = even(rows, kTileM);
+    }
+    return p;
+}
+// do_one(first group, first row, first host) for one piece after the other, until it returns an error. (Counted in 64 bits: a piece
+// may end at 2^31.)
+template <typename F>
+int for_pieces(const Pieces &p, int groups, int rows, int hosts, F do_one)
+{
+    for (long long g0 = 0; g0 < groups; g0 += p.groups)
+        for (long long r0 = 0; r0 < rows; r0 += p.rows)
+            for (long long h0 = 0; h0 < hosts; h0 += p.hosts) {
+                const int rc = do_one((int)g0, (int)r0, (int)h0);
+                if (rc) return rc;
+            }
+    return NBOS_OK;
+}
+
 template <typename T>
 int backward(const Call &c, const float *stats, const float *grad_loss, float grad_scale, T *grad_a, long long a_stride, long long a_group_stride,
              T *grad_b, long long b_stride, long long b_group_stride)
 {
     const nbos_towers *in = c.in;
     const int groups = in->n_groups, rows = (int)in->rows, hosts = in->n_hosts, width = in->width, pairs = c.sms / 2;
-    // Pieces of G: whole groups while they fit; of a group that does not, runs along its longer side, so that the gradient
-    // that has to be added up over the pieces is the smaller one.
     // An entry of G is held as two 16-bit values, the second what rounding took off the first, and the contractions go over both. With one,
     // gradients are a sum of rounded terms: their errors against 64 bits are 1.4 times the plain form's, 2.5 where a group has one row, and far
     // more where the terms cancel. A row's p - q add up to 0, so what all hosts' vectors have in common does: where that is as large as what
     // tells them apart the error is 1.7 times the plain form's, at ten times as large 9.4 (2,048 x 4,096 of width 128; two values: 1.0 in
     // all of these). The second value doubles two of four products: 65,536 x 4,096 of width 256, both calls 528 us with one, 881 with two.
     const int planes = in->gradient_values == 1 ? 1 : 2;
-    const size_t group_bytes = (size_t)rows * ((hosts + 63) & ~63) * 2 * planes;
-    int piece_groups = 1, piece_rows = rows, piece_hosts = hosts;
-    auto even = [&](int n, int tile) {   // whole tiles, pieces of much the same size
-        const int pieces = (int)((group_bytes + kPieceBytes - 1) / kPieceBytes), size = ceil_div(ceil_div(n, pieces), tile) * tile;
-        return size < n ? size : n;
-    };
-    if (group_bytes <= kPieceBytes) {
-        piece_groups = (int)(kPieceBytes / group_bytes);
-        if (piece_groups > groups) piece_groups = groups;
-    } else if (rows <= hosts) {
-        piece_hosts = even(hosts, kTileN);
-    } else {
-        piece_rows = even(rows, kTileM);
-    }
+    const Pieces piece_of = plan_pieces(groups, rows, hosts, planes);
+    const int piece_groups = piece_of.groups, piece_rows = piece_of.rows, piece_hosts = piece_of.hosts;
     const bool cut_rows = piece_rows < rows, cut_hosts = piece_hosts < hosts;
     const int g_stride = (piece_hosts + 63) & ~63;
     const bool narrow = width <= 128;
@@ -1468,79 +1492,77 @@ int backward(const Call &c, const float *stats, const float *grad_loss, float gr
     const int az = a.table.group_stride != 0, bz = b.table.group_stride != 0;
     T *g = ws.at<T>(o_g);
 
-    for (int g0 = 0; g0 < groups; g0 += piece_groups)
-        for (int r0 = 0; r0 < rows; r0 += piece_rows)
-            for (int h0 = 0; h0 < hosts; h0 += piece_hosts) {
-                const int gn = groups - g0 < piece_groups ? groups - g0 : piece_groups;
-                const int rn = rows - r0 < piece_rows ? rows - r0 : piece_rows, hn = hosts - h0 < piece_hosts ? hosts - h0 : piece_hosts;
-                const Table piece{g, g_stride, (long long)piece_rows * g_stride, planes * gn, rn, hn};
-                CUtensorMap g_out, g_rows, g_cols;   // written, and read along rows and across them
-                if ((rc = make_map(&g_out, piece, 32, in->dtype, planes == 2 ? 32 : 64)) || (rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype)))
-                    return rc;
+    return for_pieces(piece_of, groups, rows, hosts, [&](int g0, int r0, int h0) -> int {
+        const int gn = groups - g0 < piece_groups ? groups - g0 : piece_groups;
+        const int rn = rows - r0 < piece_rows ? rows - r0 : piece_rows, hn = hosts - h0 < piece_hosts ? hosts - h0 : piece_hosts;
+        const Table piece{g, g_stride, (long long)piece_rows * g_stride, planes * gn, rn, hn};
+        CUtensorMap g_out, g_rows, g_cols;   // written, and read along rows and across them
+        if ((rc = make_map(&g_out, piece, 32, in->dtype, planes == 2 ? 32 : 64)) || (rc = make_map(&g_rows, piece, 128, in->dtype)) || (rc = make_map(&g_cols, piece, kBlockK, in->dtype)))
+            return rc;
 
-                TowerArgs p = {};
-                p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK));
-                p.a_z = az, p.a_z0 = g0 * az, p.b_z = bz, p.b_z0 = g0 * bz, p.a_m0 = r0, p.b_n0 = h0;
-                p.group0 = g0, p.row0 = r0, p.rows = rows, p.hosts = hosts, p.width = width, p.col0 = h0, p.col_end = hn, p.m_rows = rn;
-                p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
-                p.c = kLog2e / c.T, p.stats = stats, p.stats_stride = 2 + c.k, p.grad_loss = grad_loss, p.range = range;
-                const bool few = c.k <= kFewEntries;
-                if (few) p.ids = c.ids, p.teacher = c.teacher, p.teacher_stride = c.teacher_stride, p.k = c.k;
-                const int used = p.t.units < pairs ? (int)p.t.units : pairs;
-                if (planes == 2)
-                    e = in->asks ? launch_tower<GRAD, kTileN, true, 2, T>(a_rows, b_rows, g_out, p, used, c.stream)
-                                 : launch_tower<GRAD, kTileN, false, 2, T>(a_rows, b_rows, g_out, p, used, c.stream);
-                else
-                    e = in->asks ? launch_tower<GRAD, kTileN, true, 1, T>(a_rows, b_rows, g_out, p, used, c.stream)
-                                 : launch_tower<GRAD, kTileN, false, 1, T>(a_rows, b_rows, g_out, p, used, c.stream);
-                if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
+        TowerArgs p = {};
+        p.t = tiles(gn, rn, ceil_div(hn, kTileN), ceil_div(width, kBlockK));
+        p.a_z = az, p.a_z0 = g0 * az, p.b_z = bz, p.b_z0 = g0 * bz, p.a_m0 = r0, p.b_n0 = h0;
+        p.group0 = g0, p.row0 = r0, p.rows = rows, p.hosts = hosts, p.width = width, p.col0 = h0, p.col_end = hn, p.m_rows = rn;
+        p.asks = reinterpret_cast<const int4 *>(in->asks), p.room = reinterpret_cast<const int4 *>(in->room);
+        p.c = kLog2e / c.T, p.stats = stats, p.stats_stride = 2 + c.k, p.grad_loss = grad_loss, p.range = range;
+        const bool few = c.k <= kFewEntries;
+        if (few) p.ids = c.ids, p.teacher = c.teacher, p.teacher_stride = c.teacher_stride, p.k = c.k;
+        const int used = p.t.units < pairs ? (int)p.t.units : pairs;
+        if (planes == 2)
+            e = in->asks ? launch_tower<GRAD, kTileN, true, 2, T>(a_rows, b_rows, g_out, p, used, c.stream)
+                         : launch_tower<GRAD, kTileN, false, 2, T>(a_rows, b_rows, g_out, p, used, c.stream);
+        else
+            e = in->asks ? launch_tower<GRAD, kTileN, true, 1, T>(a_rows, b_rows, g_out, p, used, c.stream)
+                         : launch_tower<GRAD, kTileN, false, 1, T>(a_rows, b_rows, g_out, p, used, c.stream);
+        if (e != cudaSuccess) return cuda_fail(e, "towers: scores launch");
 
-                if (!few) {
-                    PatchArgs q = {};
-                    q.groups = gn, q.group0 = g0, q.row0 = r0, q.rows_here = rn, q.rows = rows, q.host0 = h0, q.hosts_here = hn, q.hosts = hosts, q.k = c.k;
-                    q.ids = c.ids, q.teacher = c.teacher, q.teacher_stride = c.teacher_stride, q.stats = stats, q.grad_loss = grad_loss, q.range = range;
-                    q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
-                    q.plane_stride = planes == 2 ? gn * piece.group_stride : 0;
-                    int lanes = 1;
-                    while (lanes < 32 && lanes < c.k) lanes *= 2;
-                    e = launch_next(patch_kernel<T>, dim3((unsigned int)(((long long)gn * rn * lanes + 255) / 256)), 256, 0, c.stream, q, lanes);
-                    if (e != cudaSuccess) return cuda_fail(e, "towers: teacher launch");
-                }
+        if (!few) {
+            PatchArgs q = {};
+            q.groups = gn, q.group0 = g0, q.row0 = r0, q.rows_here = rn, q.rows = rows, q.host0 = h0, q.hosts_here = hn, q.hosts = hosts, q.k = c.k;
+            q.ids = c.ids, q.teacher = c.teacher, q.teacher_stride = c.teacher_stride, q.stats = stats, q.grad_loss = grad_loss, q.range = range;
+            q.c = p.c, q.grad = g, q.grad_stride = g_stride, q.grad_group_stride = piece.group_stride;
+            q.plane_stride = planes == 2 ? gn * piece.group_stride : 0;
+            int lanes = 1;
+            while (lanes < 32 && lanes < c.k) lanes *= 2;
+            e = launch_next(patch_kernel<T>, dim3((unsigned int)(((long long)gn * rn * lanes + 255) / 256)), 256, 0, c.stream, q, lanes);
+            if (e != cudaSuccess) return cuda_fail(e, "towers: teacher launch");
+        }
 
-                if (grad_a) {
-                    TowerArgs d = {};
-                    d.t = ta, d.t.groups = gn, d.t.m_tiles = ceil_div(rn, kTileM), d.k_shift = planes - 1, d.plane_z = gn, d.t.k_blocks = planes * ceil_div(hn, kBlockK);
-                    d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
-                    d.a_z = 1, d.b_z = bz, d.b_z0 = g0 * bz, d.b_k0 = h0;
-                    d.group0 = g0, d.width = width, d.range = range, d.m_rows = rn, d.out_row0 = r0;
-                    d.out = grad_a, d.out_stride = a_stride, d.out_group_stride = a_group_stride, d.out_wide = readable(grad_a, rows, a_stride, groups, a_group_stride);
-                    d.sums = sums_a ? ws.at<float>(o_a) : nullptr, d.add = h0 > 0;
-                    e = launch_gradient<GRAD_REQUESTS, T>(g_rows, b_cols, d, narrow, pairs, c.stream);
-                    if (e == cudaSuccess && sums_a && h0 + hn == hosts) {
-                        const long long n = (long long)gn * rn * width, blocks = (n + 1023) / 1024;
-                        e = launch_next(sums_kernel<T>, dim3((unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms)), 256, 0, c.stream,
-                                        d.sums, ta.splits, gn, rn, width, range, grad_a + g0 * a_group_stride + r0 * a_stride, a_stride, a_group_stride);
-                    }
-                    if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
-                }
-                if (grad_b) {
-                    TowerArgs d = {};
-                    d.t = tb, d.t.groups = gn, d.t.m_tiles = ceil_div(hn, kTileM), d.k_shift = planes - 1, d.plane_z = gn, d.t.k_blocks = planes * ceil_div(rn, kBlockK);
-                    d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
-                    d.a_z = 1, d.b_z = az, d.b_z0 = g0 * az, d.b_k0 = r0;
-                    d.group0 = g0, d.width = width, d.range = range, d.m_rows = hn, d.out_row0 = h0;
-                    d.out = grad_b, d.out_stride = b_stride, d.out_group_stride = b_group_stride, d.out_wide = readable(grad_b, hosts, b_stride, groups, b_group_stride);
-                    d.sums = sums_b ? ws.at<float>(o_b) : nullptr, d.add = r0 > 0;
-                    e = launch_gradient<GRAD_HOSTS, T>(g_cols, a_cols, d, narrow, pairs, c.stream);
-                    if (e == cudaSuccess && sums_b && r0 + rn == rows) {
-                        const long long n = (long long)gn * hn * width, blocks = (n + 1023) / 1024;
-                        e = launch_next(sums_kernel<T>, dim3((unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms)), 256, 0, c.stream,
-                                        d.sums, tb.splits, gn, hn, width, range, grad_b + g0 * b_group_stride + h0 * b_stride, b_stride, b_group_stride);
-                    }
-                    if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
-                }
+        if (grad_a) {
+            TowerArgs d = {};
+            d.t = ta, d.t.groups = gn, d.t.m_tiles = ceil_div(rn, kTileM), d.k_shift = planes - 1, d.plane_z = gn, d.t.k_blocks = planes * ceil_div(hn, kBlockK);
+            d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
+            d.a_z = 1, d.b_z = bz, d.b_z0 = g0 * bz, d.b_k0 = h0;
+            d.group0 = g0, d.width = width, d.range = range, d.m_rows = rn, d.out_row0 = r0;
+            d.out = grad_a, d.out_stride = a_stride, d.out_group_stride = a_group_stride, d.out_wide = readable(grad_a, rows, a_stride, groups, a_group_stride);
+            d.sums = sums_a ? ws.at<float>(o_a) : nullptr, d.add = h0 > 0;
+            e = launch_gradient<GRAD_REQUESTS, T>(g_rows, b_cols, d, narrow, pairs, c.stream);
+            if (e == cudaSuccess && sums_a && h0 + hn == hosts) {
+                const long long n = (long long)gn * rn * width, blocks = (n + 1023) / 1024;
+                e = launch_next(sums_kernel<T>, dim3((unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms)), 256, 0, c.stream,
+                                d.sums, ta.splits, gn, rn, width, range, grad_a + g0 * a_group_stride + r0 * a_stride, a_stride, a_group_stride);
             }
-    return NBOS_OK;
+            if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
+        }
+        if (grad_b) {
+            TowerArgs d = {};
+            d.t = tb, d.t.groups = gn, d.t.m_tiles = ceil_div(hn, kTileM), d.k_shift = planes - 1, d.plane_z = gn, d.t.k_blocks = planes * ceil_div(rn, kBlockK);
+            d.t.units = (long long)gn * d.t.m_tiles * d.t.n_tiles * d.t.splits;
+            d.a_z = 1, d.b_z = az, d.b_z0 = g0 * az, d.b_k0 = r0;
+            d.group0 = g0, d.width = width, d.range = range, d.m_rows = hn, d.out_row0 = h0;
+            d.out = grad_b, d.out_stride = b_stride, d.out_group_stride = b_group_stride, d.out_wide = readable(grad_b, hosts, b_stride, groups, b_group_stride);
+            d.sums = sums_b ? ws.at<float>(o_b) : nullptr, d.add = r0 > 0;
+            e = launch_gradient<GRAD_HOSTS, T>(g_cols, a_cols, d, narrow, pairs, c.stream);
+            if (e == cudaSuccess && sums_b && r0 + rn == rows) {
+                const long long n = (long long)gn * hn * width, blocks = (n + 1023) / 1024;
+                e = launch_next(sums_kernel<T>, dim3((unsigned int)(blocks < 8 * c.sms ? blocks : 8 * c.sms)), 256, 0, c.stream,
+                                d.sums, tb.splits, gn, hn, width, range, grad_b + g0 * b_group_stride + h0 * b_stride, b_stride, b_group_stride);
+            }
+            if (e != cudaSuccess) return cuda_fail(e, "towers: gradient launch");
+        }
+        return NBOS_OK;
+    });
 }
 
 int check_gradient(const char *what, const void *data, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride, int width)
@@ -1626,4 +1648,25 @@ extern "C" int nbos_probe_towers_stall(int kernel, uint64_t limit_ns)
     const uint64_t least = 1000000ull, most = 5000000000ull;
     stall_next = {kernel, limit_ns < least ? least : limit_ns > most ? most : limit_ns};
     return NBOS_OK;
+}
+
+extern "C" int nbos_probe_towers_pieces(int32_t n_groups, int64_t rows, int32_t n_hosts, int32_t gradient_values, int64_t *out_pieces,
+                                        int64_t *out_entries, int64_t *out_largest_bytes)
+{
+    if (!out_pieces || !out_entries || !out_largest_bytes) return fail(NBOS_ERR_INVALID_ARG, "NULL output");
+    if (n_groups < 1 || n_groups > 65535 || rows < 1 || rows > NBOS_POLICY_MAX_ROWS / n_groups || n_hosts < 1 || n_hosts > NBOS_MAX_HOSTS ||
+        gradient_values < 1 || gradient_values > 2)
+        return fail(NBOS_ERR_INVALID_ARG, "probe arguments out of range");
+    const int n = (int)rows;
+    const Pieces p = plan_pieces(n_groups, n, n_hosts, gradient_values);
+    int64_t pieces = 0, entries = 0;
+    const int rc = for_pieces(p, n_groups, n, n_hosts, [&](int g0, int r0, int h0) -> int {
+        if (g0 < 0 || r0 < 0 || h0 < 0) return fail(NBOS_ERR_RANGE, "a piece starts at group %d, row %d, host %d", g0, r0, h0);
+        auto here = [](int all, int from, int size) { return (int64_t)(all - from < size ? all - from : size); };
+        ++pieces, entries += here(n_groups, g0, p.groups) * here(n, r0, p.rows) * here(n_hosts, h0, p.hosts);
+        return NBOS_OK;
+    });
+    *out_pieces = pieces, *out_entries = entries;
+    *out_largest_bytes = (int64_t)p.groups * p.rows * ((p.hosts + 63) & ~63) * 2 * gradient_values;
+    return rc;
 }
