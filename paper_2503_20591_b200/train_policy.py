@@ -10,7 +10,7 @@ both ways of placing are compared.
 
 --blocks gives either tower residual blocks, --max-norm clips the gradients by their global norm, --no-table trains on the
 two towers' vectors (in bfloat16) without the table of scores: for clusters whose table does not fit. There is no balance loss
-then, which needs the table.
+then, which needs the table; what is reported is measured on pieces of it.
 """
 from __future__ import annotations
 
@@ -22,6 +22,7 @@ from . import binding, policy, workloads
 
 BALANCE_WEIGHT = 0.01
 TEACHER_LOGITS = (2.0, 1.0, 0.0)   # best, second, third host
+PIECE = 1 << 22                    # scores that are looked at together when the policy is measured
 ANSWER = dict(temperature=0.7, top_k=16, top_p=0.95, min_p=0.01)   # how the policy is asked
 
 
@@ -87,12 +88,13 @@ class Cluster:
         binding.nbos_place_batch(self.snapshot, requests, out)
         return out
 
-    def fits(self, requests):
+    def fits(self, requests, snapshots=slice(None)):
         """[N, B, H]: which hosts can take which request (capacities and subscription limit)."""
-        s = {k: v[:, None, :] for k, v in self.state.items()}
+        s = {k: v[snapshots, None, :] for k, v in self.state.items()}
+        limit = [v[snapshots] for v in self.limit]
         g, v, c, m = (requests[..., i, None] for i in range(4))
         return ((s["gpus_total"] >= 1) & (g <= s["gpus_total"]) & (v <= s["vram_gb"]) & (c <= s["millicpus"])
-                & (m <= s["mem_mb"]) & ((s["gpus_subscribed"] + g) * self.limit[1] <= s["gpus_total"] * self.limit[0]))
+                & (m <= s["mem_mb"]) & ((s["gpus_subscribed"] + g) * limit[1] <= s["gpus_total"] * limit[0]))
 
     def close(self):
         binding.nbos_snapshot_destroy(self.snapshot)
@@ -118,15 +120,58 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
             m = torch.randint(1024, 65537, (snapshots, batch), generator=gen, device="cuda")
             return torch.stack([g, 16 * g, c, m], dim=-1).int()
 
-        def agreement(logits, wanted):
-            """Share of placeable requests whose best host by the policy is one of the rule's three."""
+        def agrees(logits, wanted):
+            """(requests whose best host by the policy is one of the rule's three, requests that can be placed)"""
             best = logits.argmax(-1, keepdim=True).int()
             there = wanted[..., :1] >= 0
-            return float(((best == wanted).any(-1, keepdim=True) & there).sum() / there.sum())
+            return ((best == wanted).any(-1, keepdim=True) & there).sum(), there.sum()
 
-        def answer(logits):
+        def draw_answers():
+            return torch.rand((snapshots, batch, 3), generator=gen, device="cuda")
+
+        def answer(logits, uniforms):
             """Three distinct hosts a request, drawn from the policy, and how many were there."""
-            return policy.sample_hosts(logits.detach(), torch.rand((snapshots, batch, 3), generator=gen, device="cuda"), **ANSWER)
+            return policy.sample_hosts(logits.detach(), uniforms, **ANSWER)
+
+        def measure(requests, wanted):
+            """The policy's answers to all requests and what they are like, in pieces of snapshots and requests: the table of all
+            scores is never there."""
+            uniforms = draw_answers()
+            n_step = max(1, min(snapshots, PIECE // hosts))
+            b_step = max(1, min(batch, PIECE // (hosts * n_step)))
+            total = dict(hits=0, there=0, found=0, infeasible=0, repeated=0)
+            even, used, used_by_rule = [], 0, 0
+            with torch.no_grad():
+                request, host = net.vectors(request_features(requests), cluster.features)
+                for n in range(0, snapshots, n_step):
+                    ns = slice(n, n + n_step)
+                    live = counts = rule_counts = shares = 0
+                    for b in range(0, batch, b_step):
+                        bs = slice(b, b + b_step)
+                        fits = cluster.fits(requests[ns, bs], ns)
+                        logits = (request[ns, bs] @ host[ns].transpose(1, 2)).masked_fill(~fits, float("-inf"))
+                        rule = wanted[ns, bs].contiguous()
+                        placed, found = answer(logits, uniforms[ns, bs].contiguous())
+                        chosen = placed >= 0
+                        hits, there = agrees(logits, rule)
+                        total["hits"] += hits
+                        total["there"] += there
+                        total["found"] += found.sum()
+                        total["infeasible"] += (~fits.gather(2, placed.clamp(min=0).long()) & chosen).sum()
+                        total["repeated"] += sum(((placed[..., i] == placed[..., j]) & chosen[..., i] & chosen[..., j]).sum()
+                                                 for i, j in ((0, 1), (0, 2), (1, 2)))
+                        _, own, share = policy.balance_loss(logits, placed)
+                        rows = chosen.any(-1).sum(1, keepdim=True)
+                        live, counts, shares = live + rows, counts + own, shares + share.double() * rows
+                        rule_counts = rule_counts + policy.balance_loss(logits, rule)[1]
+                    load = counts.double() / counts.sum(1, keepdim=True).clamp(min=1)
+                    even.append(hosts * (load * shares / live.clamp(min=1)).sum(1))
+                    used += (counts > 0).sum()
+                    used_by_rule += (rule_counts > 0).sum()
+            total = {k: int(v) for k, v in total.items()}
+            return dict(agreement=total["hits"] / max(1, total["there"]), feasible=total["infeasible"] == 0, distinct=total["repeated"] == 0,
+                        found=total["found"] / (snapshots * batch), even=float(torch.cat(even).mean()), hosts_used=int(used) / snapshots,
+                        hosts_used_by_rule=int(used_by_rule) / snapshots)
 
         history = []
         for step in range(steps):
@@ -136,16 +181,15 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
             if table:
                 logits = net(request_features(requests), cluster.features, cluster.fits(requests))
                 distill = policy.distill_loss(logits, wanted, teacher_logits)
-                even, _, _ = policy.balance_loss(logits, answer(logits)[0])   # the load is the policy's own, not the rule's
+                even, _, _ = policy.balance_loss(logits, answer(logits, draw_answers())[0])   # the load is the policy's own, not the rule's
                 loss = distill.mean() + BALANCE_WEIGHT * even.mean()
             else:
                 request, host = (v.bfloat16() for v in net.vectors(request_features(requests), cluster.features))
                 distill = policy.tower_distill_loss(request, host, wanted, teacher_logits, asks=requests, room=cluster.room)
                 loss = distill.mean()
                 if reported:
-                    with torch.no_grad():
-                        logits = net(request_features(requests), cluster.features, cluster.fits(requests))
-                        even, _, _ = policy.balance_loss(logits, answer(logits)[0])
+                    seen = measure(requests, wanted)
+                    shown = seen["even"], seen["agreement"]
             optimizer.zero_grad(set_to_none=True)
             loss.backward()
             if max_norm is not None:
@@ -154,26 +198,18 @@ def train(hosts: int = 256, snapshots: int = 16, batch: int = 512, steps: int = 
             if reported:
                 if not table and binding.nbos_policy_towers_status() != binding.NBOS_OK:
                     raise RuntimeError("a two-tower kernel gave up on a wait: the last steps' gradients are undefined")
-                history.append((distill.mean().item(), even.mean().item(), agreement(logits.detach(), wanted)))
+                if table:
+                    hits, there = agrees(logits.detach(), wanted)
+                    shown = even.mean().item(), float(hits / there)
+                history.append((distill.mean().item(), *shown))
                 report(f"step {step}: distillation {history[-1][0]:.4f}, balance {history[-1][1]:.2f}, "
                        f"best host among the rule's three {history[-1][2]:.3f}")
 
         requests = draw()
-        fits = cluster.fits(requests)
-        with torch.no_grad():
-            logits = net(request_features(requests), cluster.features, fits)
-        placed, found = answer(logits)
-        chosen = placed >= 0
-        feasible = fits.gather(2, placed.clamp(min=0).long()) | ~chosen
-        distinct = all(((placed[..., i] != placed[..., j]) | ~chosen[..., i] | ~chosen[..., j]).all().item()
-                       for i, j in ((0, 1), (0, 2), (1, 2)))
-        rule = cluster.teacher(requests)
-        _, rule_counts, _ = policy.balance_loss(logits, rule)
-        _, own_counts, _ = policy.balance_loss(logits, placed)
-        result = dict(history=history, agreement=agreement(logits, rule), feasible=bool(feasible.all()), distinct=distinct,
-                      found=float(found.float().mean()), hosts_used=float((own_counts > 0).float().sum(1).mean()),
-                      hosts_used_by_rule=float((rule_counts > 0).float().sum(1).mean()))
-        report(f"sampled: {result['found']:.2f} hosts a request, all feasible: {result['feasible']}, distinct: {distinct}; "
+        result = measure(requests, cluster.teacher(requests))
+        del result["even"]
+        result = dict(history=history, **result)
+        report(f"sampled: {result['found']:.2f} hosts a request, all feasible: {result['feasible']}, distinct: {result['distinct']}; "
                f"{result['hosts_used']:.0f} hosts of a snapshot used ({result['hosts_used_by_rule']:.0f} by the rule)")
         return result
     finally:
