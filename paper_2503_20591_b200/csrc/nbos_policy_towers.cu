@@ -326,7 +326,7 @@ __device__ __forceinline__ void row_entries(const TowerArgs &a, long long at, bo
 // their own, summed in another order, are off by some 1e-5: below T of that size p was 0 or infinite at a row's best host.) A warp sees
 // 32 rows, and one of a tile's four quarters, in ascending tiles.
 constexpr unsigned int kNoEntry = 0xFFFFFFFFu;
-// Up to kFewEntries a row: a lane has its row's own, in order, as host << 8 | place in the row's list; at[0] is the next one.
+// Up to kFewEntries a row (65,536 x 4,096, one entry: 94 us, sorted 99; four 102 / 107): a lane has its row's own, in order, as host << 8 | place in the row's list; at[0] is the next one.
 struct RowEntries {
     unsigned int at[kFewEntries];
     float *x;
@@ -876,18 +876,19 @@ __global__ void lay_out_kernel(const T *src, long long stride, long long group_s
 }
 
 // The entries of 32 rows (of one group) in the order of their quarters and tiles: counted, placed. What comes first within a tile differs from
-// run to run; what is done with it does not. Dynamic shared memory: a counter a quarter of a tile.
-__global__ void __launch_bounds__(256) sort_entries_kernel(const int32_t *ids, int rows, int k, int hosts, int tiles, unsigned int *keys, int *starts)
+// run to run; what is done with it does not. Dynamic shared memory: a counter for each quarter of a tile, or (`fine`) for each of its 64 columns:
+// where a quarter has more entries than columns, those that are read together are then on few columns.
+__global__ void __launch_bounds__(256) sort_entries_kernel(const int32_t *ids, int rows, int k, int hosts, int tiles, bool fine, unsigned int *keys, int *starts)
 {
-    extern __shared__ unsigned int counters[];   // [4][tiles]
+    extern __shared__ unsigned int counters[];   // [4][tiles][1 or 64]
     __shared__ unsigned int warps[8];
     next_may_start();
     previous_done();
     const unsigned int lists = ((unsigned int)rows + 31) / 32;
-    const int g = (int)(blockIdx.x / lists), row0 = (int)(blockIdx.x % lists) * 32, n = 4 * tiles;
+    const int g = (int)(blockIdx.x / lists), row0 = (int)(blockIdx.x % lists) * 32, quarter = tiles * (fine ? 64 : 1), n = 4 * quarter;
     const int count = min(32, rows - row0) * k;
     ids += ((long long)g * rows + row0) * k, keys += ((long long)g * rows + row0) * k, starts += 5ll * blockIdx.x;
-    auto counter = [&](int id) { return counters + id / 64 % 4 * tiles + id / 256; };
+    auto counter = [&](int id) { return counters + id / 64 % 4 * quarter + (fine ? id / 256 * 64 + id % 64 : id / 256); };
     for (int i = threadIdx.x; i < n; i += 256) counters[i] = 0u;
     __syncthreads();
     for (int e = threadIdx.x; e < count; e += 256) {
@@ -916,7 +917,7 @@ __global__ void __launch_bounds__(256) sort_entries_kernel(const int32_t *ids, i
         before += here;
     }
     __syncthreads();
-    if (threadIdx.x < 4) starts[threadIdx.x] = (int)counters[threadIdx.x * tiles];
+    if (threadIdx.x < 4) starts[threadIdx.x] = (int)counters[threadIdx.x * quarter];
     __syncthreads();
     for (int e = threadIdx.x; e < count; e += 256) {
         const int id = ids[e], row = e / k;
@@ -1366,11 +1367,12 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     args.entries = out_stats ? out_stats + 2 : ws.at<float>(o_entries), args.entry_stride = out_stats ? 2 + c.k : c.k;
     if (!few) {
         args.keys = ws.at<unsigned int>(o_keys), args.key_starts = ws.at<int>(o_starts);
-        const int shared = 4 * args.t.n_tiles * (int)sizeof(unsigned int);
+        const bool fine = in->n_hosts <= 32 * c.k;   // (64 rows x 256 hosts with 256 entries each: 139 -> 58 us)
+        const int shared = 4 * args.t.n_tiles * (fine ? 64 : 1) * (int)sizeof(unsigned int);
         e = allow_shared(sort_entries_kernel, shared);
         if (e == cudaSuccess)
             e = launch_next(sort_entries_kernel, dim3((unsigned int)lists), 256, shared, c.stream, c.ids, (int)in->rows, (int)c.k, (int)in->n_hosts,
-                            args.t.n_tiles, ws.at<unsigned int>(o_keys), ws.at<int>(o_starts));
+                            args.t.n_tiles, fine, ws.at<unsigned int>(o_keys), ws.at<int>(o_starts));
         if (e != cudaSuccess) return cuda_fail(e, "towers: entries launch");
     }
     e = in->asks ? launch_tower<STATS, kTileN, true, 1, T>(map_a, map_b, map_a, args, pairs, c.stream)
@@ -1382,8 +1384,9 @@ int forward(const Call &c, float *out_loss, float *out_stats)
     f.ids = c.ids, f.teacher = c.teacher, f.teacher_stride = c.teacher_stride, f.asks = args.asks, f.room = args.room;
     f.T = c.T, f.c = args.c, f.partial = args.partial, f.loss = out_loss, f.stats = out_stats;
     f.entries = args.entries, f.entry_stride = args.entry_stride;
-    // eight lanes a row where there is little to do for each; else a warp
-    e = c.k > 8 || args.slots > 32 ? launch_next(finish_kernel<32>, dim3((unsigned int)((rows + 7) / 8)), 256, 0, c.stream, f)
+    // A warp a row where a row has many parts, or few rows have many entries each; else eight lanes. (65,536 x 256, eight lanes / a warp: one
+    // entry 27 / 53 us, 32 entries 87 / 109; 4,099 x 10,007 with capacities, 32 entries 76 / 57; 48 x 65,536, 3 entries 18 / 15.)
+    e = args.slots > 32 || (c.k > 8 && rows <= 8192) ? launch_next(finish_kernel<32>, dim3((unsigned int)((rows + 7) / 8)), 256, 0, c.stream, f)
                                    : launch_next(finish_kernel<8>, dim3((unsigned int)((rows + 31) / 32)), 256, 0, c.stream, f);
     return e == cudaSuccess ? NBOS_OK : cuda_fail(e, "towers: loss launch");
 }
