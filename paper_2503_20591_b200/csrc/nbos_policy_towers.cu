@@ -452,6 +452,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         *abort_flag = 0u;
         barriers_visible();
     }
+    __syncthreads();
+    cluster_barrier();   // tensor memory is allocated by the pair as one: its other block has to be there (without this a pair waited for good, once in thousands of launches)
     if (warp == kEpilogue / 32) {
         if (lane == 0) prefetch_map(&map_a), prefetch_map(&map_b);
         __syncwarp();
@@ -840,6 +842,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     cluster_barrier();
     fence_after();
     if (warp == kEpilogue / 32) tmem_free(tmem, kTmemColumns);
+    cluster_barrier();   // and given back as one: neither leaves before
 }
 
 // ---- small kernels around the products ----------------------------------------------------------------------
@@ -854,8 +857,9 @@ __global__ void lay_out_kernel(const T *src, long long stride, long long group_s
     const long long n = (long long)rows * chunks, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     src += blockIdx.y * group_stride;
     dst += (long long)blockIdx.y * rows * wide;
-    // Eight values from the 16-byte pieces that hold them (of which each holds one at least): 6 x 31,616 rows of 475, value by value 214 us,
-    // this 66.
+    // Eight values from the 16-byte pieces that hold them (6 x 31,616 rows of 475, value by value 214 us, this 66). The pieces at a table's ends
+    // may reach up to 14 bytes beyond it, which nothing uses: a piece that holds one of its values lies on an aligned 16 bytes with it, and
+    // memory is mapped, and protected, in far larger units.
 #pragma unroll 4
     for (long long i = first; i < n; i += (long long)gridDim.x * blockDim.x) {
         const long long row = n <= 0xFFFFFFFFll ? (unsigned int)i / chunks : i / chunks;

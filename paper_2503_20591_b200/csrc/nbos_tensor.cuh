@@ -97,7 +97,8 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
 }
 
 // ---- tensor memory ------------------------------------------------------------------------------------------
-// Both warps of the pair call these; `at` is a word of shared memory that gets the address.
+// A warp of each block of the pair calls these, after a barrier of the pair and before one: both blocks have to be there. `at` is a word of
+// shared memory that gets the address.
 __device__ __forceinline__ void tmem_alloc(uint32_t at, int columns)
 {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(at), "r"(columns) : "memory");
