@@ -521,7 +521,8 @@ int nbos_policy_sample(const nbos_logits *logits, const float *uniforms, const f
 /*
  * Distillation of a two-tower policy without its table of logits. Such a policy scores a host for a request as the
  * product of two vectors; with many requests and hosts the table [rows, n_hosts] is far larger than the vectors, and is
- * never stored here: the forward call keeps a row's maximum and sum, the backward call computes the scores once more and holds
+ * never stored here: the forward call keeps a row's maximum and sum (and the scores at its hosts; more than four a row are sorted first, 4
+ * bytes each), the backward call computes the scores once more and holds
  * pieces of about 512 MB (or 256 rows / hosts, where that is more) of their gradient.
  *   x[g, r, h] = sum_i requests[g, r, i] * hosts[g, h, i], -inf unless the request fits the host: asks[g, r, i] <= room[g, h, i] and
  *   asks[g, r, i] >= 0 for all four i. (With asks = the requests of nbos_place_batch and room[0] = the GPUs that the host's size and

@@ -285,7 +285,9 @@ __device__ __forceinline__ void add_scaled(float (&s)[VEC], const float (&a)[VEC
 
 enum Gate { NO_GATE, SHARED_GATE, ROW_GATE };
 
-// Registers: what leaves room for enough threads to keep the memory busy (backward with 96: 280 -> 320 us for 32,768 x 2,048 f16). Weights are not among them: they lie in shared memory as
+// Registers: what leaves room for enough threads to keep the memory busy (backward with 96: 280 -> 320 us for 32,768 x 2,048 f16, a gate for each of
+// eight groups). Some backward forms do not fit: rows of 257 to 512 values spill 100 to 820 bytes a thread at 112 (4 groups, 512 bf16, 134 million values: 346 us, 71 % of the
+// tables' bytes; a gate a row 538, 61 %), rows beyond 8,192 values 250 to 890 at 64 (12,288 bf16: 732 us, 34 %). Weights are not among them: they lie in shared memory as
 // 32-bit floats, those of the branch's norm multiplied by the gate that the block's rows share. (Taken from the L1 cache row by row:
 // 8 x 8,192 x 2,048 bf16 forward 191 us, backward 414; this 188 and 312.)
 template <bool WIDE> constexpr int kForwardRegs = 64;

@@ -100,3 +100,28 @@ def test_a_listed_host_that_is_the_best(nb, rows, hosts, width, k, mask, twins, 
     sums = grads[0][..., 0].double().abs()   # all p of a row add up to 1, as its q do, whichever of its hosts are close
     assert (sums <= half * 4 * (1 + k)).all(), float(sums.max())
     assert torch.isfinite(grads[1]).all()
+
+
+@pytest.mark.parametrize("hosts,k,mask", [(700_001, 7, False), (1 << 20, 40, True), (1 << 20, 3, False), (8192, 256, False), (8193, 256, True), (130, 256, True)])
+def test_scores_at_the_entries_are_the_tables(nb, hosts, k, mask):
+    """What is saved of a row's entries, up to the largest number of hosts and with lists denser than the table: whole-numbered vectors,
+    so scores are exact; -inf where there is no host or no room."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    ints = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=gen, device="cuda")
+    rows = 37
+    a, b = ints(-3, 4, 1, rows, 24).bfloat16(), ints(-3, 4, 1, hosts, 24).bfloat16()
+    ids = ints(-2, hosts + 2, 1, rows, k).int()
+    ids[0, :, 0] = hosts - 1
+    ids[0, 5] = ids[0, 5, 0]              # one host over and over
+    asks, room = (ints(0, 9, 1, rows, 4).int(), ints(3, 20, 1, hosts, 4).int()) if mask else (None, None)
+    if mask:
+        asks[0, 7, 2] = -1
+    stats = torch.full((1, rows, 2 + k), -7.0, device="cuda")
+    nb.nbos_policy_towers(a, b, ids, None, None, stats, asks=asks, room=room)
+    there = (ids >= 0) & (ids < hosts)
+    at = (ids * there).long()
+    if mask:
+        there &= (asks[0, :, None] <= room[0, at[0]]).all(-1) & (asks[0] >= 0).all(-1)[:, None]
+    want = torch.einsum("rd,rkd->rk", a[0].double(), b[0, at[0]].double())
+    assert torch.equal(stats[0, :, 2:].double(), torch.where(there[0], want, -INF))
