@@ -182,11 +182,9 @@ BlockArgs arguments(const nbos_block *b)
     a.alpha = b->residual_scale, a.eps = b->eps, a.per_width = 1.0f / (float)b->width;
     return a;
 }
-int smaller(int a, int b) { return a < b ? a : b; }
-int gate_align(const nbos_block *b, const void *gate, int64_t stride)
+bool gate_anywhere(const nbos_block *b, const void *gate, int64_t stride)
 {
-    const int g = table_align(gate, gate && b->rows > b->rows_per_gate ? 2 : 1, stride, (int)dtype_bytes(b->gate_dtype));
-    return g;
+    return rows_anywhere(gate, gate && b->rows > b->rows_per_gate ? 2 : 1, stride, (int)dtype_bytes(b->gate_dtype));
 }
 
 int launched(cudaError_t e)
@@ -229,11 +227,10 @@ extern "C" int nbos_policy_block_norm(const nbos_block *block, void *out_residua
     if ((rc = check_sm100(&sms, &device))) return rc;
     BlockArgs a = arguments(block);
     a.out = out_residual, a.normed = out_normed, a.out_stride = out_residual_stride, a.normed_stride = out_normed_stride, a.stats = out_stats;
-    int align = gate_align(block, block->gate, block->gate_stride);
-    align = smaller(align, smaller(table_align(a.x, a.rows, a.x_stride, (int)elem), table_align(a.y, a.rows, a.y_stride, (int)elem)));
-    align = smaller(align, smaller(table_align(a.out, a.rows, a.out_stride, (int)elem), table_align(a.normed, a.rows, a.normed_stride, (int)elem)));
-    align = smaller(align, smaller(table_align(a.post, 1, 0, 4), table_align(a.pre, 1, 0, 4)));
-    const Shape s = plan(a.width, (int)elem, align);
+    bool any = gate_anywhere(block, block->gate, block->gate_stride) || rows_anywhere(a.post, 1, 0, 4) || rows_anywhere(a.pre, 1, 0, 4);
+    const struct { const void *p; int64_t stride; } tables[] = {{a.x, a.x_stride}, {a.y, a.y_stride}, {a.out, a.out_stride}, {a.normed, a.normed_stride}};
+    for (const auto &t : tables) any |= rows_anywhere(t.p, a.rows, t.stride, (int)elem);
+    const Shape s = plan(a.width, (int)elem, any);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     return launched(block->dtype == NBOS_F32    ? launch_forward<float>(a, s, sms, stream)
                     : block->dtype == NBOS_BF16 ? launch_forward<__nv_bfloat16>(a, s, sms, stream)
@@ -280,12 +277,12 @@ extern "C" int nbos_policy_block_norm_backward(const nbos_block *block, const fl
     a.saved = stats, a.dr = grad_residual, a.dh = grad_normed, a.dr_stride = grad_residual_stride, a.dh_stride = grad_normed_stride;
     a.dx = out_grad_residual, a.dy = out_grad_branch, a.dx_stride = out_grad_residual_stride, a.dy_stride = out_grad_branch_stride;
     a.dgate = out_grad_gate, a.dgate_stride = gates > 1 ? out_grad_gate_stride : 0;
-    int align = smaller(gate_align(block, block->gate, block->gate_stride), gate_align(block, out_grad_gate, out_grad_gate_stride));
+    bool any = gate_anywhere(block, block->gate, block->gate_stride) || gate_anywhere(block, out_grad_gate, out_grad_gate_stride) ||
+               rows_anywhere(a.post, 1, 0, 4) || rows_anywhere(a.pre, 1, 0, 4);
     const struct { const void *p; int64_t stride; } tables[] = {{a.x, a.x_stride}, {a.y, a.y_stride}, {a.dr, a.dr_stride}, {a.dh, a.dh_stride},
                                                                {a.dx, a.dx_stride}, {a.dy, a.dy_stride}};
-    for (const auto &t : tables) align = smaller(align, table_align(t.p, a.rows, t.stride, (int)elem));
-    align = smaller(align, smaller(table_align(a.post, 1, 0, 4), table_align(a.pre, 1, 0, 4)));
-    const Shape s = plan(a.width, (int)elem, align);
+    for (const auto &t : tables) any |= rows_anywhere(t.p, a.rows, t.stride, (int)elem);
+    const Shape s = plan(a.width, (int)elem, any);
     ColumnArgs c = {};
     c.width = a.width, c.gate = a.gate, c.post = a.post, c.gate_stride = a.gate_stride, c.gate_f32 = a.gate_f32, c.weight_f32 = a.weight_f32;
     c.dpost = out_grad_post, c.dpre = out_grad_pre, c.dgate = a.dgate, c.dgate_stride = a.dgate_stride;

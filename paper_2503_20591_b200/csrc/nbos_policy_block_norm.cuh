@@ -369,10 +369,10 @@ struct Shape {
     bool block, wide, any;   // any: some table's rows do not start on 16-byte boundaries
     int threads;
 };
-inline Shape plan(int width, int elem, int align)
+inline Shape plan(int width, int elem, bool any)
 {
     Shape s;
-    s.any = align < 16;
+    s.any = any;
     const int values = width > 256 ? 16 : 8;
     s.chunks = values * elem / 16;
     const int need = (width + values - 1) / values;
@@ -385,11 +385,10 @@ inline Shape plan(int width, int elem, int align)
     s.threads = s.block ? s.team : kTeams;
     return s;
 }
-inline int table_align(const void *p, int64_t rows, int64_t stride, int elem)
+// whether some row of a table starts off 16-byte boundaries
+inline bool rows_anywhere(const void *p, int64_t rows, int64_t stride, int elem)
 {
-    if (!p) return 16;
-    const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (rows > 1 ? (uintptr_t)(stride * elem) : 0);
-    return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+    return p && ((reinterpret_cast<uintptr_t>(p) | (rows > 1 ? (uintptr_t)(stride * elem) : 0)) & 15) != 0;
 }
 
 template <typename T, typename F>
