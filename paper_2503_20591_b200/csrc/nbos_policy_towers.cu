@@ -664,10 +664,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                     for (int sub = 0; sub < 2; ++sub) {
                         const bool first = PLANES == 2 || sub == 0, last = PLANES == 2 || sub == 1;   // of a box
-                        if (KIND == GRAD && first) {
-                            if (lane == 0) stores_read_wait<0>();         // what was in it before has left
-                            __syncwarp();
-                        }
+                        auto box_is_free = [&] {   // what was in it before has left (looked at as late as can be: the copy takes as long as the loads and compares)
+                            if (KIND == GRAD && first) {
+                                if (lane == 0) stores_read_wait<0>();
+                                __syncwarp();
+                            }
+                        };
                         // p f of two columns in one word, and (PLANES == 2) what was rounded off in another
                         auto words = [&](uint32_t (&w)[PLANES], uint32_t x0, uint32_t x1, float from, float less, float by, bool none) {
                             float e0, e1;
@@ -691,6 +693,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             tmem_wait(v[1]);
                             if (sub == 1) release();
                             mask_rows(v, columns + 32 * sub, ask);
+                            box_is_free();
                             if constexpr (KIND == STATS) {
 #pragma unroll
                                 for (int i = 0; i < ROWS; ++i) add8(run_m[i], run_s[i], v, i, args.c);
@@ -717,6 +720,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) v[i] = i < left ? v[i] : 0xFF800000u;
                             }
+                            box_is_free();
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 uint32_t w[4][PLANES];
