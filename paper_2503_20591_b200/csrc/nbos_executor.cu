@@ -40,6 +40,7 @@ struct ExecArgs {
     int32_t *out_executor, *out_can_run;
     long long n_kernels;
     int H;
+    unsigned int zero;      // 0, which the compiler does not know
 };
 
 // Gathering six separate arrays per replica costs 18 scattered loads per kernel; packed records
@@ -291,8 +292,12 @@ __global__ void __launch_bounds__(kRingThreads + 32, 2) select_executors_ring_ke
                 h[0] = ids[0];
                 h[1] = ids[1];
                 h[2] = ids[2];
-                __syncwarp();
-                if ((tid & 31) == 0) mbar_arrive(empty_bar + 8u * s);
+                // The stage is given back when every lane has its values: the barrier's address depends on them. (Nothing else keeps
+                // the loads before the arrival, which is one lane's and goes another way. On first calls with new memory, one process in
+                // six, a block's first tile was overwritten by its fifth before some warp had read its host ids.)
+                const unsigned int loaded = (unsigned int)(r.x ^ r.y ^ r.z ^ r.w ^ h[0] ^ h[1] ^ h[2]) & a.zero;
+                const uint32_t bar = empty_bar + 8u * s + __reduce_or_sync(0xFFFFFFFFu, loaded);
+                if ((tid & 31) == 0) mbar_arrive(bar);
             } else {
                 r = __ldg(a.requests + k);
 #pragma unroll
@@ -383,7 +388,7 @@ extern "C" int nbos_select_executors(const nbos_cluster_state *state, const int3
     e = cudaGetLastError();
     if (e == cudaSuccess) {
         ExecArgs a{fit, rank, rec, ratio, wide, reinterpret_cast<const int4 *>(requests), replica_hosts,
-                   out_executor, out_can_run, n_kernels, H};
+                   out_executor, out_can_run, n_kernels, H, 0u};
         // the ring form pays from about half a million kernels on (measured: never slower than
         // the plain form from 2^20 kernels, 15 - 25 % faster at 2^22 and above)
         const size_t table_bytes = ((size_t)(H + 1) * (sizeof(uint2) + sizeof(unsigned int)) + 127) & ~(size_t)127;
