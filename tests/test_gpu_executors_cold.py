@@ -1,5 +1,5 @@
 """Executor selection's first call in a process, on memory that is new to it: stages of the ring are not given back before they have
-been read. Each process compares its first call with its third on the same inputs, and the first results with the checker's."""
+been read. Each process compares its first call with its third on the same inputs, and the first results with the oracle's."""
 from __future__ import annotations
 
 import os
